@@ -507,6 +507,146 @@ so_status so_debug_set_step_variant(so_ctx *ctx, int32_t variant);
  * to launches made after the call. */
 so_status so_debug_set_spin_limit(so_ctx *ctx, int64_t polls);
 
+/*
+ * Operators at the two ends of a training step.
+ *
+ * What feeds the optimizer: token embedding, layer norm, and the loss on the
+ * logits, each with its gradient.  They need no context; like every other call
+ * they take caller-owned device memory, enqueue on `stream` and return, and
+ * check their arguments before anything is launched.  Common rules:
+ *   - matrices are rows of contiguous elements with a row stride in elements,
+ *     at least the row length (an input may also have stride 0: one row read for
+ *     all).  Base pointers need the element's alignment only; rows that all
+ *     start at the same offset from a 16-byte boundary are the fast case;
+ *   - dtypes are SO_DTYPE_*, equal to SO_GRAD_*, so that a gradient may be
+ *     written straight into a gradient arena; ids are 32- or 64-bit integers;
+ *   - sums, statistics and softmax are held in fp32 (totals over rows in fp64)
+ *     and every output is rounded once;
+ *   - results repeat bit for bit: no floating-point atomics anywhere;
+ *   - zero rows (tokens) are a valid input: forward outputs are empty, a loss
+ *     is 0, a reduced gradient is zero (or unchanged with `accumulate`);
+ *   - inputs and outputs do not overlap, except where stated.
+ */
+enum { SO_DTYPE_BF16 = 0, SO_DTYPE_FP32 = 1, SO_DTYPE_FP16 = 2 };
+enum { SO_IDS_INT32 = 0, SO_IDS_INT64 = 1 };
+
+/*
+ * so_layer_norm_forward -- y = (x - mean) * rstd * weight + bias over each row,
+ * mean and rstd = 1 / sqrt(var + eps) of that row (biased variance).
+ *   x, y         [rows, cols] of `dtype`; y may be x (same stride)
+ *   weight, bias [cols] of `param_dtype` (= dtype or fp32), each may be NULL
+ *   mean, rstd   fp32 [rows], both or neither (NULL when no backward follows)
+ * cols >= 1, eps >= 0.  Errors: SO_ERR_INVALID_ARG, SO_ERR_CUDA.
+ */
+so_status so_layer_norm_forward(const void *x, int64_t x_stride, const void *weight,
+                                const void *bias, void *y, int64_t y_stride, float *mean,
+                                float *rstd, int64_t rows, int64_t cols, int32_t dtype,
+                                int32_t param_dtype, double eps, void *stream);
+
+/*
+ * so_layer_norm_backward -- with xhat = (x - mean) * rstd and g = dy * weight:
+ *   dx      = rstd * (g - mean_row(g) - xhat * mean_row(g * xhat))
+ *   dweight = sum_rows(dy * xhat),  dbias = sum_rows(dy)
+ *   dx       [rows, cols] of `dtype`, may be dy (same stride)
+ *   dweight, dbias  [cols] of `grad_dtype`, each may be NULL; with `accumulate`
+ *            the sums are added to what is there (one rounding)
+ *   scratch  so_layer_norm_backward_scratch bytes of device memory, 16-byte
+ *            aligned, contents irrelevant; only needed if dweight or dbias is
+ *            wanted.  Free for other use once the call has run on its stream.
+ */
+so_status so_layer_norm_backward_scratch(int64_t rows, int64_t cols, uint64_t *bytes);
+so_status so_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x,
+                                 int64_t x_stride, const void *weight, const float *mean,
+                                 const float *rstd, void *dx, int64_t dx_stride, void *dweight,
+                                 void *dbias, int64_t rows, int64_t cols, int32_t dtype,
+                                 int32_t param_dtype, int32_t grad_dtype, int32_t accumulate,
+                                 void *scratch, uint64_t scratch_bytes, void *stream);
+
+/*
+ * so_embedding_forward -- out[t, :] = scale * table[ids[t], :].
+ *   table [vocab, cols], out [n, cols], both of `dtype`
+ * An id outside [0, vocab) reads nothing: its row is zero, and *bad_id (device
+ * int32, may be NULL, otherwise left alone) is set to 1.
+ */
+so_status so_embedding_forward(const void *ids, int32_t ids_dtype, int64_t n, const void *table,
+                               int64_t table_stride, int64_t vocab, int64_t cols, int32_t dtype,
+                               double scale, void *out, int64_t out_stride, int32_t *bad_id,
+                               void *stream);
+
+/*
+ * so_embedding_backward -- dtable[v, :] = scale * sum over t with ids[t] = v of
+ * dout[t, :], summed in ascending order of t in fixed groups.  The tokens are
+ * sorted by id (stably); no value is added atomically.
+ *   dout   [n, cols] of `dtype`; dtable [vocab, cols] of `grad_dtype`
+ *   accumulate 0: every row of dtable is written (rows of ids that do not occur
+ *          become zero); 1: the sums are added to what is there and other rows
+ *          are not touched (a head that shares the table has already written)
+ *   padding_id  takes no gradient (-1: none); neither do ids outside [0, vocab)
+ *   scratch  so_embedding_backward_scratch bytes, 16-byte aligned
+ * n and vocab are at most 2^30, here and in the lookup.
+ */
+so_status so_embedding_backward_scratch(int64_t n, int64_t vocab, int64_t cols, uint64_t *bytes);
+so_status so_embedding_backward(const void *ids, int32_t ids_dtype, int64_t n, const void *dout,
+                                int64_t dout_stride, int64_t vocab, int64_t cols, int32_t dtype,
+                                double scale, int64_t padding_id, void *dtable,
+                                int64_t dtable_stride, int32_t grad_dtype, int32_t accumulate,
+                                void *scratch, uint64_t scratch_bytes, void *stream);
+
+/*
+ * so_distill_loss -- distillation from a teacher's top logits, loss and
+ * gradient in one pass over the student's logits z.  Per row, with
+ * p = softmax(a / tau) over the row's top_k teacher logits a (renormalised over
+ * them) and q = softmax(z / tau) over the vocabulary:
+ *   row_loss = tau^2 * sum_k p_k (log p_k - log q[id_k])
+ *   loss     = sum_rows weight * row_loss
+ *   grad_j   = grad_scale * weight * tau * (q_j - sum of p_k with id_k = j)
+ * (top_k = 1 and tau = 1 is the cross entropy of a label.)
+ *   logits  [rows, vocab] of `dtype`;  grad the same, NULL for the loss alone,
+ *           may be `logits` (same stride): the gradient then replaces them
+ *   teacher_ids [rows, top_k], teacher_logits [rows, top_k] of `teacher_dtype`,
+ *           top_k <= 1024.  An entry with logit -inf or an id outside
+ *           [0, vocab) is empty (lists shorter than top_k are padded that way)
+ *   weight  fp32 [rows], NULL = 1 for every row.  A row of weight 0 is not
+ *           read: its loss and gradient are 0 whatever it holds; so are those of
+ *           a row whose teacher entries are all empty
+ *   row_loss fp32 [rows], loss fp32 [1]
+ * grad_scale carries 1 / (rows averaged over) and, for fp16 gradients, the loss
+ * scale.  A logit of -inf has probability 0; a row of nothing else, and one
+ * with NaN or +inf in it, has a NaN loss and gradient, which the optimizer's
+ * gradient check turns into a skipped iteration.
+ */
+#define SO_DISTILL_MAX_TOP_K 1024
+so_status so_distill_loss(const void *logits, int64_t logits_stride, const void *teacher_ids,
+                          int32_t ids_dtype, int64_t ids_stride, const void *teacher_logits,
+                          int64_t teacher_stride, int32_t teacher_dtype, int32_t top_k,
+                          const float *weight, int64_t rows, int64_t vocab, int32_t dtype,
+                          double temperature, double grad_scale, void *grad, int64_t grad_stride,
+                          float *row_loss, float *loss, void *stream);
+
+/*
+ * so_policy_loss -- clipped policy loss with a KL term, from the logits, loss
+ * and gradient in one pass.  Per row (one sampled token), with
+ * logp = log softmax(z / T)[token], r = exp(logp - old_logp), A = advantage and
+ * d = ref_logp - logp:
+ *   row_loss = -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A)
+ *              + kl_coef * (exp(d) - d - 1)
+ *   loss     = sum_rows weight * row_loss
+ *   slope    = -(r A where r A <= the clamped product, else 0) + kl_coef * (1 - exp(d))
+ *   grad_j   = grad_scale * weight / T * slope * ([j = token] - softmax(z / T)_j)
+ *   tokens  [rows]; a row whose token is outside [0, vocab) counts as masked
+ *   advantage, old_logp, ref_logp  fp32 [rows]; old_logp NULL: the tokens were
+ *           sampled from these logits (r = 1); ref_logp NULL: needs kl_coef = 0
+ *   weight, logits, grad, row_loss, loss as in so_distill_loss (masked rows
+ *           are not read); logp fp32 [rows], may be NULL, 0 for masked rows
+ *   0 <= clip_low <= 1, 0 <= clip_high (infinity: no upper bound), kl_coef >= 0
+ */
+so_status so_policy_loss(const void *logits, int64_t logits_stride, const void *tokens,
+                         int32_t ids_dtype, const float *advantage, const float *old_logp,
+                         const float *ref_logp, const float *weight, int64_t rows, int64_t vocab,
+                         int32_t dtype, double temperature, double clip_low, double clip_high,
+                         double kl_coef, double grad_scale, void *grad, int64_t grad_stride,
+                         float *logp, float *row_loss, float *loss, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,6 +22,9 @@ SO_GRAD_BF16, SO_GRAD_FP32, SO_GRAD_FP16 = 0, 1, 2
 SO_PARAM_BF16, SO_PARAM_FP16 = 0, 1
 SO_DECISION_COMMIT, SO_DECISION_SKIP, SO_DECISION_CLIP_RESTEP = 0, 1, 2
 SO_ALL = -1
+SO_DTYPE_BF16, SO_DTYPE_FP32, SO_DTYPE_FP16 = 0, 1, 2
+SO_IDS_INT32, SO_IDS_INT64 = 0, 1
+SO_DISTILL_MAX_TOP_K = 1024
 DECISION_NAMES = {0: "COMMIT", 1: "SKIP", 2: "CLIP_RESTEP"}
 
 
@@ -83,7 +86,10 @@ EXPORTS = ["so_layout_init", "so_layout_get_info", "so_layout_tensor", "so_layou
            "so_loss_scale_config", "so_get_loss_scale", "so_state_export", "so_state_import",
            "so_bucket_slot", "so_get_step", "so_set_step", "so_pending_buckets",
            "so_get_counters", "so_last_cuda_error", "so_strerror", "so_destroy",
-           "so_debug_set_dry_run", "so_debug_set_bucket_stats", "so_debug_set_step_variant"]
+           "so_debug_set_dry_run", "so_debug_set_bucket_stats", "so_debug_set_step_variant",
+           "so_layer_norm_forward", "so_layer_norm_backward_scratch", "so_layer_norm_backward",
+           "so_embedding_forward", "so_embedding_backward_scratch", "so_embedding_backward",
+           "so_distill_loss", "so_policy_loss"]
 
 
 def lib() -> C.CDLL:
@@ -131,6 +137,18 @@ def lib() -> C.CDLL:
         "so_debug_set_dry_run": [vp, i32],
         "so_debug_set_bucket_stats": [vp, i32, dbl, i32],
         "so_debug_set_step_variant": [vp, i32],
+        "so_layer_norm_forward": [vp, i64, vp, vp, vp, i64, vp, vp, i64, i64, i32, i32, dbl, vp],
+        "so_layer_norm_backward_scratch": [i64, i64, P(C.c_uint64)],
+        "so_layer_norm_backward": [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, i64, i64, i32, i32,
+                                   i32, i32, vp, C.c_uint64, vp],
+        "so_embedding_forward": [vp, i32, i64, vp, i64, i64, i64, i32, dbl, vp, i64, vp, vp],
+        "so_embedding_backward_scratch": [i64, i64, i64, P(C.c_uint64)],
+        "so_embedding_backward": [vp, i32, i64, vp, i64, i64, i64, i32, dbl, i64, vp, i64, i32, i32,
+                                  vp, C.c_uint64, vp],
+        "so_distill_loss": [vp, i64, vp, i32, i64, vp, i64, i32, i32, vp, i64, i64, i32, dbl, dbl, vp,
+                            i64, vp, vp, vp],
+        "so_policy_loss": [vp, i64, vp, i32, vp, vp, vp, vp, i64, i64, i32, dbl, dbl, dbl, dbl, dbl,
+                           vp, i64, vp, vp, vp, vp],
     }
     for name, argtypes in sig.items():
         fn = getattr(L, name)
@@ -380,3 +398,45 @@ def so_debug_set_spin_limit(ctx, polls: int) -> None:
 
 def so_debug_set_step_variant(ctx, variant: int) -> None:
     _ok(ctx, lib().so_debug_set_step_variant(ctx, variant), "so_debug_set_step_variant")
+
+
+# ---- operators of a training step (no context) ------------------------------
+# Raw device addresses (0 or None where the header allows NULL) and sizes, in the
+# header's order; paper_2509_21271_b200.operators takes tensors.
+
+def so_layer_norm_forward(*args) -> None:
+    _ok(None, lib().so_layer_norm_forward(*args), "so_layer_norm_forward")
+
+
+def so_layer_norm_backward_scratch(rows: int, cols: int) -> int:
+    n = C.c_uint64()
+    _ok(None, lib().so_layer_norm_backward_scratch(rows, cols, C.byref(n)),
+        "so_layer_norm_backward_scratch")
+    return n.value
+
+
+def so_layer_norm_backward(*args) -> None:
+    _ok(None, lib().so_layer_norm_backward(*args), "so_layer_norm_backward")
+
+
+def so_embedding_forward(*args) -> None:
+    _ok(None, lib().so_embedding_forward(*args), "so_embedding_forward")
+
+
+def so_embedding_backward_scratch(n: int, vocab: int, cols: int) -> int:
+    size = C.c_uint64()
+    _ok(None, lib().so_embedding_backward_scratch(n, vocab, cols, C.byref(size)),
+        "so_embedding_backward_scratch")
+    return size.value
+
+
+def so_embedding_backward(*args) -> None:
+    _ok(None, lib().so_embedding_backward(*args), "so_embedding_backward")
+
+
+def so_distill_loss(*args) -> None:
+    _ok(None, lib().so_distill_loss(*args), "so_distill_loss")
+
+
+def so_policy_loss(*args) -> None:
+    _ok(None, lib().so_policy_loss(*args), "so_policy_loss")

@@ -1,0 +1,207 @@
+// Shared by the operators of a training step (layer norm, embedding, losses on
+// logits): element types, 16-byte vectors, launch helpers, argument checks.
+//
+// The library is compiled without automatic multiply-add contraction; these
+// kernels ask for it where they want it (fmaf).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math_constants.h>
+#include <stdint.h>
+
+#include <atomic>
+#include <cmath>
+
+#include "superoffload.h"
+
+namespace so_ops {
+
+constexpr int kMaxDevices = 64;
+
+struct bf16_t { uint16_t bits; };
+struct f16_t { uint16_t bits; };
+
+// ---- one element -------------------------------------------------------------
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(bf16_t x) { return __uint_as_float((uint32_t)x.bits << 16); }
+__device__ __forceinline__ float to_f32(f16_t x) { return __half2float(__ushort_as_half(x.bits)); }
+
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ bf16_t from_f32<bf16_t>(float x)
+{
+    return bf16_t{__bfloat16_as_ushort(__float2bfloat16_rn(x))};
+}
+template <> __device__ __forceinline__ f16_t from_f32<f16_t>(float x)
+{
+    return f16_t{__half_as_ushort(__float2half_rn(x))};
+}
+
+// An element of an array whose type is known at run time (the small arrays:
+// weights, teacher logits, reduced gradients).
+__device__ __forceinline__ float load_any(const void *p, int64_t i, int32_t dtype)
+{
+    if (dtype == SO_DTYPE_FP32) return static_cast<const float *>(p)[i];
+    if (dtype == SO_DTYPE_BF16) return to_f32(static_cast<const bf16_t *>(p)[i]);
+    return to_f32(static_cast<const f16_t *>(p)[i]);
+}
+
+__device__ __forceinline__ void store_any(void *p, int64_t i, int32_t dtype, float x)
+{
+    if (dtype == SO_DTYPE_FP32) static_cast<float *>(p)[i] = x;
+    else if (dtype == SO_DTYPE_BF16) static_cast<bf16_t *>(p)[i] = from_f32<bf16_t>(x);
+    else static_cast<f16_t *>(p)[i] = from_f32<f16_t>(x);
+}
+
+__device__ __forceinline__ int64_t load_id(const void *p, int64_t i, int32_t ids_dtype)
+{
+    return ids_dtype == SO_IDS_INT64 ? static_cast<const int64_t *>(p)[i]
+                                     : (int64_t)static_cast<const int32_t *>(p)[i];
+}
+
+// ---- 16 bytes ----------------------------------------------------------------
+
+template <typename T> struct Vec { static constexpr int kElems = 16 / (int)sizeof(T); };
+
+template <typename T> __device__ __forceinline__ void unpack(const uint4 &v, float (&f)[Vec<T>::kElems]);
+
+template <> __device__ __forceinline__ void unpack<float>(const uint4 &v, float (&f)[4])
+{
+    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+}
+
+template <> __device__ __forceinline__ void unpack<bf16_t>(const uint4 &v, float (&f)[8])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+
+template <> __device__ __forceinline__ void unpack<f16_t>(const uint4 &v, float (&f)[8])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __half2float(__ushort_as_half((unsigned short)(w[i] & 0xFFFFu)));
+        f[2 * i + 1] = __half2float(__ushort_as_half((unsigned short)(w[i] >> 16)));
+    }
+}
+
+__device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t pack2_f16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <typename T> __device__ __forceinline__ uint4 pack(const float (&f)[Vec<T>::kElems]);
+
+template <> __device__ __forceinline__ uint4 pack<float>(const float (&f)[4])
+{
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                      __float_as_uint(f[3]));
+}
+template <> __device__ __forceinline__ uint4 pack<bf16_t>(const float (&f)[8])
+{
+    return make_uint4(pack2_bf16(f[0], f[1]), pack2_bf16(f[2], f[3]), pack2_bf16(f[4], f[5]),
+                      pack2_bf16(f[6], f[7]));
+}
+template <> __device__ __forceinline__ uint4 pack<f16_t>(const float (&f)[8])
+{
+    return make_uint4(pack2_f16(f[0], f[1]), pack2_f16(f[2], f[3]), pack2_f16(f[4], f[5]),
+                      pack2_f16(f[6], f[7]));
+}
+
+// ---- reductions ----------------------------------------------------------------
+
+__device__ __forceinline__ float warp_sum(float x)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x = __fadd_rn(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+    return x;
+}
+
+// ---- host helpers --------------------------------------------------------------
+
+inline bool valid_dtype(int32_t d) { return d == SO_DTYPE_BF16 || d == SO_DTYPE_FP32 || d == SO_DTYPE_FP16; }
+inline int elem_size(int32_t d) { return d == SO_DTYPE_FP32 ? 4 : 2; }
+inline bool valid_ids(int32_t d) { return d == SO_IDS_INT32 || d == SO_IDS_INT64; }
+inline bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// rows * stride elements must be addressable: rows, stride >= 0 and the last
+// element's byte offset below 2^62.
+inline bool valid_extent(int64_t rows, int64_t stride)
+{
+    return rows >= 0 && stride >= 0 && (rows == 0 || stride <= (int64_t(1) << 59) / rows);
+}
+
+// Row strides: an output's rows may not overlap, an input may repeat one row.
+inline bool valid_out_stride(int64_t rows, int64_t stride, int64_t cols) { return rows <= 1 || stride >= cols; }
+inline bool valid_in_stride(int64_t rows, int64_t stride, int64_t cols)
+{
+    return rows <= 1 || stride == 0 || stride >= cols;
+}
+
+// Number of SMs of the current device, asked for once per device.
+inline so_status device_sms(int *sms)
+{
+    static std::atomic<int> cache[kMaxDevices];
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SO_ERR_CUDA;
+    if (dev < 0 || dev >= kMaxDevices) return SO_ERR_UNSUPPORTED;
+    int n = cache[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0)
+            return SO_ERR_CUDA;
+        cache[dev].store(n, std::memory_order_relaxed);
+    }
+    *sms = n;
+    return SO_OK;
+}
+
+// Launch; `dependent` lets the kernel start while the previous kernel of the
+// stream drains (it then waits with grid_dependency_wait before it reads what
+// that kernel wrote).
+template <typename... KArgs, typename... Args>
+inline so_status launch(void (*kernel)(KArgs...), unsigned grid, unsigned block, size_t smem,
+                        cudaStream_t stream, bool dependent, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    if (dependent) {
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...) == cudaSuccess ? SO_OK : SO_ERR_CUDA;
+}
+
+__device__ __forceinline__ void grid_dependency_wait()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+__device__ __forceinline__ void grid_dependency_release()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+}  // namespace so_ops
