@@ -57,22 +57,35 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_forward_kernel(Looku
 // ---- tokens in the order of their ids ------------------------------------------
 //
 // A stable counting sort in one launch with no exchange between blocks.  Block b
-// owns the ids [b kRange, (b + 1) kRange) and reads every token: it counts the
+// owns the ids [b range, (b + 1) range) and reads every token: it counts the
 // tokens of its ids, and those of smaller ids, which gives the place where its
 // part of the sorted order begins.  Each warp takes a contiguous run of
 // tokens and keeps counters of its own, so that ranks follow from prefix sums
 // and do not depend on the order of the (integer, shared-memory) additions.
+//
+// The block knows then which of its ids have no token, and writes their zero
+// rows: that is most of the pass's traffic when the table is larger than
+// the batch, and it needs nothing from the sort of the others.
 
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kRange = 1024;              // ids a block owns, at most one per thread
+constexpr int kUnroll = 4;                // token loads in flight per lane
+
+// Runs of equal ids are summed by whoever owns the stretch of kChunk sorted
+// positions in which they begin; a run longer than kLong is cut at the
+// boundaries of the stretches instead, and the pieces are joined.
+constexpr int kChunk = 32, kLong = 64;
 
 struct SortArgs {
     const void *ids;
     int32_t *order;                       // [n] token positions by (id, position)
+    int32_t *key;                         // [n] their ids
     int32_t *start;                       // [vocab + 1] where each id's tokens begin
-    int32_t n, vocab, range;
-    int64_t padding_id;
-    int32_t ids_dtype;
+    uint32_t *arrived;                    // [n / kLong + 1][tiles] pieces of a long run summed so far
+    void *dtable;                         // rows without tokens become zero; nullptr: not wanted
+    int64_t padding_id, dtable_stride, row_bytes;
+    int32_t n, vocab, range, tiles, ids_dtype, grad_size;
+    bool wide;                            // 16-byte stores fit the rows
 };
 
 __device__ __forceinline__ int32_t usable_id(const SortArgs &a, int32_t t)
@@ -81,14 +94,28 @@ __device__ __forceinline__ int32_t usable_id(const SortArgs &a, int32_t t)
     return (id >= 0 && id < a.vocab && id != a.padding_id) ? (int32_t)id : -1;
 }
 
+__device__ __forceinline__ void zero_row(const SortArgs &a, int64_t v, int lane)
+{
+    char *row = static_cast<char *>(a.dtable) + v * a.dtable_stride * a.grad_size;
+    if (a.wide) {
+        for (int64_t i = lane; i < a.row_bytes / 16; i += 32)
+            __stcs(reinterpret_cast<uint4 *>(row) + i, make_uint4(0, 0, 0, 0));
+    } else if (a.grad_size == 4) {
+        for (int64_t i = lane; i < a.row_bytes / 4; i += 32) reinterpret_cast<uint32_t *>(row)[i] = 0;
+    } else {
+        for (int64_t i = lane; i < a.row_bytes / 2; i += 32) reinterpret_cast<uint16_t *>(row)[i] = 0;
+    }
+}
+
 __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a)
 {
     extern __shared__ int32_t s_hist[];   // [kSortWarps][range]
-    __shared__ int32_t s_below[kSortWarps], s_scan[kSortWarps];
+    __shared__ int32_t s_below[kSortWarps], s_scan[kSortWarps], s_zero[kRange], s_zeros;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int32_t lo = (int32_t)blockIdx.x * a.range;
     const int32_t hi = a.vocab - lo < a.range ? a.vocab : lo + a.range;
     for (int i = threadIdx.x; i < kSortWarps * a.range; i += kSortThreads) s_hist[i] = 0;
+    if (threadIdx.x == 0) s_zeros = 0;
     __syncthreads();
 
     const int32_t per_warp = (int32_t)(((int64_t)a.n + kSortThreads - 1) / kSortThreads) * 32;
@@ -97,10 +124,15 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
     const int32_t t1 = a.n - t0 < per_warp ? a.n : t0 + per_warp;
     int32_t *hist = s_hist + warp * a.range;
     int32_t below = 0;
-    for (int32_t t = t0 + lane; t < t1; t += 32) {
-        const int32_t id = usable_id(a, t);
-        if (id >= 0 && id < lo) ++below;
-        else if (id >= lo && id < hi) atomicAdd(&hist[id - lo], 1);
+    for (int32_t t = t0 + lane; t < t1; t += 32 * kUnroll) {
+        int32_t id[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) id[u] = t + 32 * u < t1 ? usable_id(a, t + 32 * u) : -1;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            if (id[u] >= 0 && id[u] < lo) ++below;
+            else if (id[u] >= lo && id[u] < hi) atomicAdd(&hist[id[u] - lo], 1);
+        }
     }
     for (int o = 16; o > 0; o >>= 1) below += __shfl_xor_sync(0xFFFFFFFFu, below, o);
     if (lane == 0) s_below[warp] = below;
@@ -117,6 +149,7 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
         if (lane >= o) incl += up;
     }
     if (lane == 31) s_scan[warp] = incl;
+    if (mine && count == 0 && a.dtable) s_zero[atomicAdd(&s_zeros, 1)] = lo + (int32_t)threadIdx.x;
     __syncthreads();
     int32_t base = 0;
     for (int w = 0; w < kSortWarps; ++w) base += s_below[w] + (w < warp ? s_scan[w] : 0);
@@ -124,6 +157,8 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
     if (mine) {
         a.start[lo + threadIdx.x] = at;
         if (lo + (int32_t)threadIdx.x == a.vocab - 1) a.start[a.vocab] = at + count;
+        if (count > kLong)                // two long runs never begin in the same kLong positions
+            for (int i = 0; i < a.tiles; ++i) a.arrived[(int64_t)(at / kLong) * a.tiles + i] = 0;
         for (int w = 0; w < kSortWarps; ++w) {
             const int32_t c = s_hist[w * a.range + threadIdx.x];
             s_hist[w * a.range + threadIdx.x] = at;
@@ -132,55 +167,217 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
     }
     __syncthreads();
 
-    for (int32_t t = t0; t < t1; t += 32) {
-        const int32_t id = t + lane < t1 ? usable_id(a, t + lane) : -1;
-        const bool in = id >= lo && id < hi;
-        const unsigned active = __ballot_sync(0xFFFFFFFFu, in);
-        if (in) {
-            const unsigned same = __match_any_sync(active, id);
-            const int rank = __popc(same & ((1u << lane) - 1u));
-            const int32_t pos = hist[id - lo];
-            __syncwarp(active);
-            if (rank == 0) hist[id - lo] = pos + __popc(same);
-            a.order[pos + rank] = t + lane;
+    for (int32_t t = t0; t < t1; t += 32 * kUnroll) {
+        int32_t id[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int32_t i = t + 32 * u + lane;
+            id[u] = i < t1 ? usable_id(a, i) : -1;
         }
-        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const bool in = id[u] >= lo && id[u] < hi;
+            const unsigned active = __ballot_sync(0xFFFFFFFFu, in);
+            if (in) {
+                const unsigned same = __match_any_sync(active, id[u]);
+                const int rank = __popc(same & ((1u << lane) - 1u));
+                const int32_t pos = hist[id[u] - lo];
+                __syncwarp(active);
+                if (rank == 0) hist[id[u] - lo] = pos + __popc(same);
+                a.order[pos + rank] = t + 32 * u + lane;
+                a.key[pos + rank] = id[u];
+            }
+            __syncwarp();
+        }
     }
+    const int32_t zeros = s_zeros;
+    for (int32_t i = warp; i < zeros; i += kSortWarps) zero_row(a, s_zero[i], lane);
 }
+
+// ---- sums over runs of equal ids ------------------------------------------------
+//
+// A block takes one stretch of kChunk sorted positions and one tile of columns
+// (one vector per thread).  It sums the runs that begin in the stretch, in order,
+// kBatch rows in flight; of a long run it sums the piece inside the stretch into
+// fp32 scratch, and the last block to finish a piece of that run adds the
+// pieces in their order (which block that is does not show in the result).
+
+constexpr int kSumThreads = 256, kBatch = 8;
 
 struct SumArgs {
     const void *dout;
-    const int32_t *order, *start;
+    const int32_t *order, *key, *start;
+    uint32_t *arrived;
+    float *pieces;                        // [chunks][2][cols]: of a run that began before, of one that begins here
     void *dtable;
     int64_t vocab, cols, dout_stride, dtable_stride;
-    int32_t grad_dtype, accumulate;
+    int32_t tiles, grad_dtype, accumulate;
     float scale;
 };
 
-// One warp per table row.
-template <typename T>
-__global__ void __launch_bounds__(kLookupThreads) embedding_sum_kernel(SumArgs a)
+template <int E>
+__device__ __forceinline__ void write_row(const SumArgs &a, int64_t id, int64_t col, const float (&sum)[E])
 {
-    grid_dependency_wait();
-    const int lane = threadIdx.x & 31;
-    const int64_t warps = (int64_t)gridDim.x * (kLookupThreads / 32);
-    for (int64_t v = (int64_t)blockIdx.x * (kLookupThreads / 32) + (threadIdx.x >> 5); v < a.vocab; v += warps) {
-        const int32_t s0 = a.start[v], s1 = a.start[v + 1];
-        if (s0 == s1 && a.accumulate) continue;
-        for (int64_t c = lane; c < a.cols; c += 32) {
-            float sum = 0.0f;
-            for (int32_t i = s0; i < s1; ++i)
-                sum += to_f32(static_cast<const T *>(a.dout)[(int64_t)a.order[i] * a.dout_stride + c]);
-            sum *= a.scale;
-            const int64_t at = v * a.dtable_stride + c;
-            if (a.accumulate) sum += load_any(a.dtable, at, a.grad_dtype);
-            store_any(a.dtable, at, a.grad_dtype, sum);
-        }
+    const int64_t at = id * a.dtable_stride + col;
+    float f[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        f[i] = sum[i] * a.scale;
+        if (a.accumulate) f[i] += load_any(a.dtable, at + i, a.grad_dtype);
+    }
+    if constexpr (E == 1) {
+        store_any(a.dtable, at, a.grad_dtype, f[0]);
+    } else if (a.grad_dtype == SO_DTYPE_FP32) {
+        float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(a.dtable) + at);
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i) p[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+    } else {
+        uint2 *p = reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.dtable) + at);
+        const bool bf = a.grad_dtype == SO_DTYPE_BF16;
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i)
+            p[i] = bf ? make_uint2(pack2_bf16(f[4 * i], f[4 * i + 1]), pack2_bf16(f[4 * i + 2], f[4 * i + 3]))
+                      : make_uint2(pack2_f16(f[4 * i], f[4 * i + 1]), pack2_f16(f[4 * i + 2], f[4 * i + 3]));
     }
 }
 
-// scratch: order [n], then start [vocab + 1], each rounded up to 16 bytes
+template <typename T, int E>               // E columns a thread: 16 bytes of T, or 1
+__global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(SumArgs a)
+{
+    __shared__ int32_t s_order[kChunk + kLong], s_key[kChunk + kLong + 1];
+    __shared__ uint32_t s_last;
+    grid_dependency_wait();
+    const int32_t chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
+    const int32_t total = a.start[a.vocab], p0 = chunk * kChunk;
+    if (p0 >= total) return;
+    const int32_t p1 = total - p0 < kChunk ? total : p0 + kChunk;
+    const int32_t first_id = a.key[p0], last_id = a.key[p1 - 1];
+    const int32_t first_start = a.start[first_id], first_end = a.start[first_id + 1];
+    const int32_t last_start = a.start[last_id], last_end = a.start[last_id + 1];
+    const bool first_long = first_end - first_start > kLong, last_long = last_end - last_start > kLong;
+    // a short run that began before belongs to another block; one that begins here is finished here
+    const int32_t begin = first_start < p0 && !first_long ? first_end : p0;
+    const int32_t end = last_long ? p1 : last_end;
+    if (begin >= p1) return;
+    for (int32_t i = threadIdx.x; i < end - begin; i += blockDim.x) {
+        s_order[i] = a.order[begin + i];
+        s_key[i] = a.key[begin + i];
+    }
+    if (threadIdx.x == 0) s_key[end - begin] = -1;
+    __syncthreads();
+
+    const int64_t col = ((int64_t)tile * blockDim.x + threadIdx.x) * E;
+    const bool on = col < a.cols;
+    const T *dout = static_cast<const T *>(a.dout) + (on ? col : 0);
+    float *head = a.pieces + (int64_t)chunk * 2 * a.cols + col, *tail = head + a.cols;
+    const int32_t count = end - begin;
+    float sum[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+    if (on) {
+        for (int32_t i = 0; i < count; i += kBatch) {
+            uint4 raw[E > 1 ? kBatch : 1];
+            T one[E > 1 ? 1 : kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+                if (i + u < count) {
+                    const T *src = dout + (int64_t)s_order[i + u] * a.dout_stride;
+                    if constexpr (E > 1) raw[u] = __ldcs(reinterpret_cast<const uint4 *>(src));
+                    else one[u] = *src;
+                }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                if (i + u >= count) break;
+                float f[E];
+                if constexpr (E > 1) unpack<T>(raw[u], f);
+                else f[0] = to_f32(one[u]);
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] += f[e];
+                const int32_t id = s_key[i + u];
+                if (s_key[i + u + 1] == id) continue;
+                const bool from_before = first_long && id == first_id && first_start < p0;
+                if (from_before || (last_long && id == last_id)) {
+                    float *piece = from_before ? head : tail;
+                    if constexpr (E > 1) {
+#pragma unroll
+                        for (int e = 0; e < E; e += 4)
+                            *reinterpret_cast<float4 *>(piece + e) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
+                    } else {
+                        *piece = sum[0];
+                    }
+                } else {
+                    write_row<E>(a, id, col, sum);
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+            }
+        }
+    }
+
+    // at most two long runs have a piece here: one from before, one that goes on
+    for (int which = 0; which < 2; ++which) {
+        if (which == 0 ? !(first_long && first_start < p0) : !(last_long && last_start >= p0)) continue;
+        const int32_t id = which == 0 ? first_id : last_id;
+        const int32_t s0 = which == 0 ? first_start : last_start, s1 = which == 0 ? first_end : last_end;
+        const int32_t c0 = s0 / kChunk, c1 = (s1 - 1) / kChunk;
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) s_last = atomicAdd(&a.arrived[(int64_t)(s0 / kLong) * a.tiles + tile], 1u);
+        __syncthreads();
+        if (s_last != (uint32_t)(c1 - c0)) continue;
+        __threadfence();
+        if (!on) continue;
+        // the tail of the first stretch, then the heads of the others
+        const float *piece = a.pieces + ((int64_t)c0 * 2 + 1) * a.cols + col;
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] = __ldcg(piece + e);
+        piece += a.cols;
+        for (int32_t c = c0 + 1; c <= c1; c += kBatch) {
+            float f[kBatch][E];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+                if (c + u <= c1) {
+                    const float *src = piece + (int64_t)(c + u - c0 - 1) * 2 * a.cols;
+                    if constexpr (E > 1) {
+#pragma unroll
+                        for (int e = 0; e < E; e += 4) {
+                            const float4 q = __ldcg(reinterpret_cast<const float4 *>(src + e));
+                            f[u][e] = q.x; f[u][e + 1] = q.y; f[u][e + 2] = q.z; f[u][e + 3] = q.w;
+                        }
+                    } else {
+                        f[u][0] = __ldcg(src);
+                    }
+                }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+                if (c + u <= c1)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) sum[e] += f[u][e];
+        }
+        write_row<E>(a, id, col, sum);
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+    }
+}
+
+// Scratch: order, key [n], start [vocab + 1], arrived [n / kLong + 1][tiles],
+// pieces [ceil(n / kChunk)][2][cols], each rounded up to 16 bytes.  A tile is at
+// least 32 columns.
 uint64_t round16(uint64_t b) { return (b + 15) & ~uint64_t(15); }
+
+struct Scratch {
+    uint64_t order, key, start, arrived, pieces, bytes;
+    Scratch(int64_t n, int64_t vocab, int64_t cols)
+    {
+        const uint64_t tiles = ((uint64_t)cols + 31) / 32;
+        order = 0;
+        key = order + round16((uint64_t)n * 4);
+        start = key + round16((uint64_t)n * 4);
+        arrived = start + round16(((uint64_t)vocab + 1) * 4);
+        pieces = arrived + round16(((uint64_t)n / kLong + 1) * tiles * 4);
+        bytes = pieces + round16(((uint64_t)n + kChunk - 1) / kChunk * 2 * (uint64_t)cols * 4);
+    }
+};
 
 so_status sort_tokens(const SortArgs &a, cudaStream_t st)
 {
@@ -196,6 +393,13 @@ so_status sort_tokens(const SortArgs &a, cudaStream_t st)
     }
     const unsigned grid = (unsigned)((a.vocab + a.range - 1) / a.range);
     return launch(embedding_sort_kernel, grid, kSortThreads, (size_t)kSortWarps * a.range * sizeof(int32_t), st, false, a);
+}
+
+template <typename T>
+so_status sum_runs(const SumArgs &a, bool vec, unsigned grid, unsigned threads, cudaStream_t st)
+{
+    return vec ? launch(embedding_sum_kernel<T, Vec<T>::kElems>, grid, threads, 0, st, true, a)
+               : launch(embedding_sum_kernel<T, 1>, grid, threads, 0, st, true, a);
 }
 
 }  // namespace
@@ -244,7 +448,7 @@ so_status so_embedding_backward_scratch(int64_t n, int64_t vocab, int64_t cols, 
 {
     if (!bytes || n < 0 || n > kMaxTokens || vocab < 1 || vocab > kMaxTokens || cols < 1 || cols > INT32_MAX)
         return SO_ERR_INVALID_ARG;
-    *bytes = round16((uint64_t)n * 4) + round16(((uint64_t)vocab + 1) * 4);
+    *bytes = Scratch(n, vocab, cols).bytes;
     return SO_OK;
 }
 
@@ -274,24 +478,37 @@ so_status so_embedding_backward(const void *ids, int32_t ids_dtype, int64_t n, c
     so_status s = device_sms(&sms);
     if (s != SO_OK) return s;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // a vector of dout per thread, if whole rows of both sides allow it
+    const bool vec = aligned(dout, 16) && (dout_stride * es) % 16 == 0 && (cols * es) % 16 == 0 && aligned(dtable, 16) &&
+                     (dtable_stride * gs) % 16 == 0 && (cols * gs) % 16 == 0;
+    const int64_t lanes = vec ? cols * es / 16 : cols;
+    const unsigned threads = lanes < kSumThreads ? (unsigned)((lanes + 31) / 32 * 32) : kSumThreads;
+    const int64_t tiles = (lanes + threads - 1) / threads, chunks = (n + kChunk - 1) / kChunk;
+    if (chunks * tiles > INT32_MAX) return SO_ERR_TOO_LARGE;
+    char *ws = static_cast<char *>(scratch);
+    const Scratch at(n, vocab, cols);
+
     SortArgs k = {};
-    k.ids = ids; k.order = static_cast<int32_t *>(scratch);
-    k.start = reinterpret_cast<int32_t *>(static_cast<char *>(scratch) + round16((uint64_t)n * 4));
-    k.n = (int32_t)n; k.vocab = (int32_t)vocab; k.padding_id = padding_id; k.ids_dtype = ids_dtype;
+    k.ids = ids; k.order = reinterpret_cast<int32_t *>(ws + at.order); k.key = reinterpret_cast<int32_t *>(ws + at.key);
+    k.start = reinterpret_cast<int32_t *>(ws + at.start); k.arrived = reinterpret_cast<uint32_t *>(ws + at.arrived);
+    k.dtable = accumulate ? nullptr : dtable; k.padding_id = padding_id; k.dtable_stride = dtable_stride;
+    k.row_bytes = cols * gs; k.n = (int32_t)n; k.vocab = (int32_t)vocab; k.tiles = (int32_t)tiles;
+    k.ids_dtype = ids_dtype; k.grad_size = gs;
+    k.wide = aligned(dtable, 16) && (dtable_stride * gs) % 16 == 0 && (cols * gs) % 16 == 0;
     k.range = (int32_t)((vocab + sms - 1) / sms);
     if (k.range > kRange) k.range = kRange;
     s = sort_tokens(k, st);
-    if (s != SO_OK) return s;
+    if (s != SO_OK || n == 0) return s;
 
     SumArgs a = {};
-    a.dout = dout; a.order = k.order; a.start = k.start; a.dtable = dtable; a.vocab = vocab; a.cols = cols;
-    a.dout_stride = dout_stride; a.dtable_stride = dtable_stride; a.grad_dtype = grad_dtype;
-    a.accumulate = accumulate; a.scale = (float)scale;
-    const int64_t want = (vocab + kLookupThreads / 32 - 1) / (kLookupThreads / 32);
-    const unsigned grid = (unsigned)(want < 8 * sms ? want : 8 * sms);
-    if (dtype == SO_DTYPE_BF16) return launch(embedding_sum_kernel<bf16_t>, grid, kLookupThreads, 0, st, true, a);
-    if (dtype == SO_DTYPE_FP16) return launch(embedding_sum_kernel<f16_t>, grid, kLookupThreads, 0, st, true, a);
-    return launch(embedding_sum_kernel<float>, grid, kLookupThreads, 0, st, true, a);
+    a.dout = dout; a.order = k.order; a.key = k.key; a.start = k.start; a.arrived = k.arrived;
+    a.pieces = reinterpret_cast<float *>(ws + at.pieces); a.dtable = dtable; a.vocab = vocab; a.cols = cols;
+    a.dout_stride = dout_stride; a.dtable_stride = dtable_stride; a.tiles = (int32_t)tiles;
+    a.grad_dtype = grad_dtype; a.accumulate = accumulate; a.scale = (float)scale;
+    const unsigned grid = (unsigned)(chunks * tiles);
+    if (dtype == SO_DTYPE_BF16) return sum_runs<bf16_t>(a, vec, grid, threads, st);
+    if (dtype == SO_DTYPE_FP16) return sum_runs<f16_t>(a, vec, grid, threads, st);
+    return sum_runs<float>(a, vec, grid, threads, st);
 }
 
 }  // extern "C"
