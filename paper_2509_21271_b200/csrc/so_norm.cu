@@ -49,39 +49,40 @@ __device__ __forceinline__ void load_raw(Raw<T, E> &r, const T *p)
 }
 
 template <typename T, int E>
-__device__ __forceinline__ void widen(const Raw<T, E> &r, float (&f)[E])
+__device__ __forceinline__ Vals<E> widen(const Raw<T, E> &r)
 {
-    if constexpr (E == 1) f[0] = to_f32(r.v);
-    else unpack<T>(r.v, f);
+    if constexpr (E == 1) return Vals<1>{to_f32(r.v)};
+    else return widen16<T>(r.v);
 }
 
 template <typename T, int E>
-__device__ __forceinline__ void store_vec(T *p, const float (&f)[E])
+__device__ __forceinline__ void store_vec(T *p, const Vals<E> &f)
 {
-    if constexpr (E == 1) *p = from_f32<T>(f[0]);
-    else *reinterpret_cast<uint4 *>(p) = pack<T>(f);
+    if constexpr (E == 1) *p = from_f32<T>(f.v);
+    else *reinterpret_cast<uint4 *>(p) = narrow16<T>(f);
 }
 
 // E parameters from element c, as fp32 (`fill` where the array is absent)
 template <int E>
-__device__ __forceinline__ void load_params(const void *p, int64_t c, int32_t dtype, float fill, float (&f)[E])
+__device__ __forceinline__ Vals<E> load_params(const void *p, int c, int32_t dtype, float fill)
 {
+    Vals<E> f;
     if (!p) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = fill;
+        f.set(fill);
     } else if constexpr (E == 1) {
-        f[0] = load_any(p, c, dtype);
+        f.v = load_any(p, c, dtype);
     } else if (dtype == SO_DTYPE_FP32) {
 #pragma unroll
         for (int e = 0; e < E; e += 4) {
             const float4 q = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + c + e);
-            f[e] = q.x; f[e + 1] = q.y; f[e + 2] = q.z; f[e + 3] = q.w;
+            f.p[e / 2] = pair(q.x, q.y);
+            f.p[e / 2 + 1] = pair(q.z, q.w);
         }
     } else if constexpr (E == 8) {
         const uint4 q = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + c);
-        if (dtype == SO_DTYPE_BF16) unpack<bf16_t>(q, f);
-        else unpack<f16_t>(q, f);
+        f = dtype == SO_DTYPE_BF16 ? widen16<bf16_t>(q) : widen16<f16_t>(q);
     }
+    return f;
 }
 
 // How the threads of a block are dealt to rows.
@@ -102,101 +103,83 @@ struct Group {
     }
 };
 
-constexpr int kRowThreads = 256;          // a block: one long row's threads, or several short rows'
-constexpr int kMaxRowThreads = 1024;
+constexpr int kRingBars = 64;             // groups x stages of a block, at most
+constexpr size_t kRingBytes = 50 * 1024;  // shared memory a ring aims for
+constexpr int kLongThreads = 512;         // threads of a long row, at most
+constexpr int kRowThreads = 256;
+constexpr int kGroupThreads = 128;        // a block has several groups up to this many threads
 
-template <typename T, int E, int kNV, int kMaxThreads>
+template <typename T, int kNV, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(NormArgs a, int per_row)
 {
-    // weight and bias stay in registers, unless 1024 threads leave 64 registers each
-    constexpr bool kHold = kNV * E <= 32 && kMaxThreads <= kRowThreads;
-    __shared__ float2 s_part[2][32];      // (mean, M2) of each warp, two rows in turn
+    constexpr int E = 1;
+    constexpr bool kHold = kNV <= 8;      // weight and bias stay in registers
+    __shared__ float4 s_part[2][32];      // (sum, mean, M2, count) of each warp, two rows in turn
     const Group g(per_row);
     const int cols = (int)a.cols;         // rows held in registers are short
     const int64_t step = (int64_t)gridDim.x * g.per_block;
     int64_t row = (int64_t)blockIdx.x * g.per_block + g.index;
     if (g.index >= g.per_block || row >= a.rows) return;
+    const auto has = [&](int i) { return g.thread + i * g.threads < cols; };
 
-    float w[kHold ? kNV : 1][E], b[kHold ? kNV : 1][E];
-    Raw<T, E> cur[kNV], next[kNV];
+    Vals<E> w[kHold ? kNV : 1], b[kHold ? kNV : 1];
+    Raw<T, E> even[kNV], odd[kNV];
     int mine = 0;                         // elements of this thread
+    const T *x = static_cast<const T *>(a.x) + row * a.x_stride + g.thread * E;
+    T *y = static_cast<T *>(a.y) + row * a.y_stride + g.thread * E;
+    const int64_t x_step = step * a.x_stride, y_step = step * a.y_stride;
+    const auto load_row = [&](Raw<T, E> (&r)[kNV]) {
 #pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-        const int c = (g.thread + i * g.threads) * E;
-        if (c < cols) {
-            load_raw<T, E>(cur[i], static_cast<const T *>(a.x) + row * a.x_stride + c);
-            mine += E;
-        }
-    }
+        for (int i = 0; i < kNV; ++i)
+            if (has(i)) load_raw<T, E>(r[i], x + i * g.threads * E);
+    };
+    load_row(even);
+#pragma unroll
+    for (int i = 0; i < kNV; ++i)
+        if (has(i)) mine += E;
     if constexpr (kHold) {
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (g.thread + i * g.threads) * E;
-            if (c < cols) {
-                load_params<E>(a.weight, c, a.param_dtype, 1.0f, w[i]);
-                load_params<E>(a.bias, c, a.param_dtype, 0.0f, b[i]);
+        for (int i = 0; i < kNV; ++i)
+            if (has(i)) {
+                w[i] = load_params<E>(a.weight, (g.thread + i * g.threads) * E, a.param_dtype, 1.0f);
+                b[i] = load_params<E>(a.bias, (g.thread + i * g.threads) * E, a.param_dtype, 0.0f);
             }
-        }
     }
-    const float warp_count = warp_sum((float)mine);
-    const float warp_inv = warp_count > 0.0f ? 1.0f / warp_count : 0.0f;
+    const float count = warp_sum((float)mine), inv_count = count > 0.0f ? 1.0f / count : 0.0f;
 
-    for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
-        const bool more = row + step < a.rows;
+    const auto one_row = [&](Raw<T, E> (&cur)[kNV], Raw<T, E> (&next)[kNV], float4 (&shared)[32]) {
+        x += x_step;
+        if (row + step < a.rows) load_row(next);
+        Vals<E> f[kNV], acc;
+        acc.set(0.0f);
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (g.thread + i * g.threads) * E;
-            if (more && c < cols) load_raw<T, E>(next[i], static_cast<const T *>(a.x) + (row + step) * a.x_stride + c);
-        }
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            if ((g.thread + i * g.threads) * E >= cols) break;
-            float f[E];
-            widen<T, E>(cur[i], f);
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum += f[e];
-        }
-        float mean = warp_sum(sum) * warp_inv, m2 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            if ((g.thread + i * g.threads) * E >= cols) break;
-            float f[E];
-            widen<T, E>(cur[i], f);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float d = f[e] - mean;
-                m2 = fmaf(d, d, m2);
+        for (int i = 0; i < kNV; ++i)
+            if (has(i)) {
+                f[i] = widen<T, E>(cur[i]);
+                acc = acc + f[i];
             }
-        }
-        m2 = warp_sum(m2);
+        const float sum = warp_sum(total(acc));
+        float mean = sum * inv_count;
+        acc.set(0.0f);
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (has(i)) {
+                const Vals<E> d = f[i] + -mean;
+                acc = fma(d, d, acc);
+            }
+        float m2 = warp_sum(total(acc));
         if (g.warps > 1) {
-            float2 *part = s_part[turn] + g.index * g.warps;
-            if ((threadIdx.x & 31) == 0) part[g.warp] = make_float2(mean, m2);
+            float4 *part = shared + g.index * g.warps;
+            if ((threadIdx.x & 31) == 0) part[g.warp] = make_float4(sum, mean, m2, count);
             g.sync();
-            // every warp but the last has 32 kNV E elements, or as the columns end
-            float total = 0.0f;
-            const float first = part[0].x;
-            for (int i = 0; i < g.warps; ++i) {
-                int n = 0;
-#pragma unroll
-                for (int j = 0; j < kNV; ++j) {
-                    const int left = cols - (i * 32 + j * g.threads) * E;
-                    n += left <= 0 ? 0 : left < 32 * E ? left : 32 * E;
-                }
-                total = fmaf((float)n, part[i].x - first, total);
-            }
-            mean = fmaf(total, a.inv_cols, first);
+            float all = 0.0f;
+            for (int i = 0; i < g.warps; ++i) all += part[i].x;
+            mean = all * a.inv_cols;
             m2 = 0.0f;
             for (int i = 0; i < g.warps; ++i) {
-                int n = 0;
-#pragma unroll
-                for (int j = 0; j < kNV; ++j) {
-                    const int left = cols - (i * 32 + j * g.threads) * E;
-                    n += left <= 0 ? 0 : left < 32 * E ? left : 32 * E;
-                }
-                const float d = part[i].x - mean;
-                m2 += n > 0 ? fmaf((float)n * d, d, part[i].y) : 0.0f;
+                const float4 q = part[i];
+                const float d = q.y - mean;
+                m2 += fmaf(q.w * d, d, q.z);
             }
         }
         const float rstd = 1.0f / sqrtf(fmaf(m2, a.inv_cols, a.eps));
@@ -204,126 +187,526 @@ __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(NormArgs a, i
             a.mean[row] = mean;
             a.rstd[row] = rstd;
         }
-        T *y = static_cast<T *>(a.y) + row * a.y_stride;
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (has(i)) {
+                const int c = (g.thread + i * g.threads) * E;
+                const Vals<E> xh = (f[i] + -mean) * rstd;
+                if constexpr (kHold) store_vec<T, E>(y + i * g.threads * E, fma(xh, w[i], b[i]));
+                else store_vec<T, E>(y + i * g.threads * E, fma(xh, load_params<E>(a.weight, c, a.param_dtype, 1.0f),
+                                                                load_params<E>(a.bias, c, a.param_dtype, 0.0f)));
+            }
+        y += y_step;
+        row += step;
+    };
+    while (true) {
+        one_row(even, odd, s_part[0]);
+        if (row >= a.rows) break;
+        one_row(odd, even, s_part[1]);
+        if (row >= a.rows) break;
+    }
+}
+
+// Sum over the warp of each of the N values (a power of two), all of them at
+// once: every exchange halves the values a lane still carries, so it takes N - 1 +
+// 5 - log2 N exchanges instead of 5 N.  Lane l ends with the sum of value
+// l >> (5 - log2 N).
+template <int N>
+__device__ __forceinline__ float warp_sum_many(float (&v)[N])
+{
+    const int lane = threadIdx.x & 31;
+    int mask = 16;
+#pragma unroll
+    for (int n = N / 2; n > 0; n >>= 1, mask >>= 1) {
+        const bool high = (lane & mask) != 0;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float give = high ? v[i] : v[i + n], keep = high ? v[i + n] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, mask);
+        }
+    }
+    float r = v[0];
+    for (; mask > 0; mask >>= 1) r += __shfl_xor_sync(0xFFFFFFFFu, r, mask);
+    return r;
+}
+
+// Forward, rows whose vectors are aligned: rows come through a ring of bulk copies
+// in shared memory, so that no register waits for memory and the loads of several
+// groups of rows are always on their way.  A group takes R rows at a time, whose
+// sums share one exchange and one barrier; that barrier also tells the group's
+// first thread that everyone is done with the rows before, whose place in the ring
+// it refills.
+//
+// Statistics in one exchange: a thread has the mean m_t of its n_t elements and
+// their squares around it, Q_t.  With c the first lane's mean, a warp sums
+//   D = sum n_t (m_t - c),  Q = sum (Q_t + n_t (m_t - c)^2)
+// so its mean is c + D / n and its squares around that Q - D^2 / n; c is within
+// sqrt(32) standard deviations of the mean, so the difference loses 5 bits at most,
+// however large the mean.  Warps are joined by M2 = sum M2_w + sum n_w (mean_w - mean)^2.
+//
+// A copy that does not arrive within kPolls polls turns what the group writes into
+// NaN (the optimizer's gradient check then skips the iteration).
+template <typename T, int E, int kNV, int R, bool kFull, int kMaxThreads>
+__global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 1) norm_forward_ring_kernel(NormArgs a, int per_row, int stages)
+{
+    extern __shared__ __align__(128) uint8_t s_ring[];   // [groups][stages][R][cols]
+    constexpr int kSums = 2 * R;
+    __shared__ __align__(16) float s_part[2][32][kSums], s_centre[2][32][R];
+    __shared__ float s_count[32];
+    __shared__ __align__(8) uint64_t s_full[kRingBars];
+    const Group g(per_row);
+    const int cols = (int)a.cols, lane = threadIdx.x & 31;
+    const uint32_t row_bytes = (uint32_t)cols * sizeof(T), stage_bytes = row_bytes * R;
+    const uint32_t ring = smem_addr(s_ring) + (uint32_t)(g.index * stages) * stage_bytes;
+    const uint32_t bars = smem_addr(s_full) + (uint32_t)(g.index * stages) * 8;
+    const int64_t step = (int64_t)gridDim.x * g.per_block * R;
+    const int64_t row = ((int64_t)blockIdx.x * g.per_block + g.index) * R;
+    const auto has = [&](int i) { return kFull || (g.thread + i * g.threads) * E < cols; };
+    float mine_n = 0.0f;                  // elements of this thread
+#pragma unroll
+    for (int i = 0; i < kNV; ++i)
+        if (has(i)) mine_n += E;
+    const float inv_n = mine_n > 0.0f ? 1.0f / mine_n : 0.0f, warp_n = warp_sum(mine_n);
+    if (lane == 0) s_count[threadIdx.x >> 5] = warp_n;
+    if (threadIdx.x < (unsigned)(g.per_block * stages)) mbar_init(smem_addr(s_full + threadIdx.x), 1);
+    __syncthreads();
+    mbar_init_fence();
+    const float first_inv = 1.0f / s_count[g.index * g.warps];
+
+    const auto load_rows = [&](int64_t from, int s) {
+        const int n = a.rows - from < R ? (int)(a.rows - from) : R;
+        const uint32_t bar = bars + s * 8, dst = ring + s * stage_bytes;
+        mbar_expect(bar, row_bytes * n);
+        for (int r = 0; r < n; ++r)
+            bulk_load(dst + r * row_bytes, static_cast<const T *>(a.x) + (from + r) * a.x_stride, row_bytes, bar);
+    };
+    if (g.thread == 0)
+        for (int s = 0; s < stages; ++s)
+            if (row + s * step < a.rows) load_rows(row + s * step, s);
+
+    Vals<E> w[kNV], b[kNV];
+#pragma unroll
+    for (int i = 0; i < kNV; ++i)
+        if (has(i)) {
+            w[i] = load_params<E>(a.weight, (g.thread + i * g.threads) * E, a.param_dtype, 1.0f);
+            b[i] = load_params<E>(a.bias, (g.thread + i * g.threads) * E, a.param_dtype, 0.0f);
+        }
+    T *y = static_cast<T *>(a.y) + row * a.y_stride + g.thread * E;
+    const int64_t y_step = (step - R) * a.y_stride;
+    float *mean_to = a.mean ? a.mean + row + g.thread : nullptr, *rstd_to = a.rstd + row + g.thread;
+    const uint32_t mine = ring + (uint32_t)g.thread * 16;
+    uint32_t limit = kPolls, phase = 0;
+    int stage = 0, turn = 0;
+    bool first = true;
+
+    for (int64_t left = a.rows - row; left > 0; left -= step) {
+        if (limit != 0 && !mbar_wait(bars + stage * 8, phase, limit)) limit = 0;
+        const uint32_t at = mine + stage * stage_bytes;
+        const int n = left < R ? (int)left : R;
+        float sums[kSums], centre[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float m = 0.0f, q = 0.0f;
+            if (r < n) {
+                Vals<E> f[kNV], acc;
+                acc.set(0.0f);
+#pragma unroll
+                for (int i = 0; i < kNV; ++i)
+                    if (has(i)) {
+                        f[i] = widen16<T>(lds16(at + r * row_bytes + i * g.threads * 16));
+                        acc = acc + f[i];
+                    }
+                m = total(acc) * inv_n;
+                acc.set(0.0f);
+#pragma unroll
+                for (int i = 0; i < kNV; ++i)
+                    if (has(i)) {
+                        const Vals<E> d = f[i] + -m;
+                        acc = fma(d, d, acc);
+                    }
+                q = total(acc);
+            }
+            centre[r] = __shfl_sync(0xFFFFFFFFu, m, 0);
+            const float d = mine_n > 0.0f ? m - centre[r] : 0.0f;
+            sums[2 * r] = d * mine_n;
+            sums[2 * r + 1] = fmaf(d * mine_n, d, q);
+        }
+        const float one = warp_sum_many<kSums>(sums);
+        float (*part)[kSums] = s_part[turn] + g.index * g.warps;
+        float (*cent)[R] = s_centre[turn] + g.index * g.warps;
+        const float *count = s_count + g.index * g.warps;
+        turn ^= 1;
+        if (lane % (32 / kSums) == 0) part[g.warp][lane / (32 / kSums)] = one;
+        if (lane == 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) cent[g.warp][r] = centre[r];
+        }
+        if (g.warps > 1) g.sync();
+        else __syncwarp();
+        if (g.thread == 0 && !first && limit != 0) {      // the stage before this one is free
+            const int before = stage == 0 ? stages - 1 : stage - 1;
+            const int64_t ahead = (int64_t)(stages - 1) * step;
+            if (left > ahead) load_rows(a.rows - left + ahead, before);
+        }
+        first = false;
+        // the warps' sums, moved to a common centre (the first warp's mean), one warp a lane
+        float mean[R], m2[R], rstd[R];
+        if (g.warps > 1) {
+            float base[R], both[kSums];
+#pragma unroll
+            for (int r = 0; r < R; ++r) base[r] = fmaf(part[0][2 * r], first_inv, cent[0][r]);
+            const bool in = lane < g.warps;
+            const float n_w = in ? count[lane] : 0.0f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float k = in ? cent[lane][r] - base[r] : 0.0f, d = in ? part[lane][2 * r] : 0.0f;
+                both[2 * r] = fmaf(n_w, k, d);
+                both[2 * r + 1] = in ? fmaf(k, fmaf(n_w, k, 2.0f * d), part[lane][2 * r + 1]) : 0.0f;
+            }
+            const float joined = warp_sum_many<kSums>(both);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float d = __shfl_sync(0xFFFFFFFFu, joined, 2 * r * (32 / kSums));
+                const float q = __shfl_sync(0xFFFFFFFFu, joined, (2 * r + 1) * (32 / kSums));
+                const float shift = d * a.inv_cols;
+                mean[r] = base[r] + shift;
+                m2[r] = fmaf(-d, shift, q);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float d = part[0][2 * r], shift = d * a.inv_cols;
+                mean[r] = cent[0][r] + shift;
+                m2[r] = fmaf(-d, shift, part[0][2 * r + 1]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            rstd[r] = 1.0f / sqrtf(fmaf(fmaxf(m2[r], 0.0f), a.inv_cols, a.eps));
+            if (limit == 0 || m2[r] != m2[r]) rstd[r] = CUDART_NAN_F;
+            if (mean_to && g.thread == r && r < n) {
+                *mean_to = mean[r];
+                *rstd_to = rstd[r];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < n) {
+#pragma unroll
+                for (int i = 0; i < kNV; ++i)
+                    if (has(i)) {
+                        const Vals<E> x = widen16<T>(lds16(at + r * row_bytes + i * g.threads * 16));
+                        store_vec<T, E>(y + i * g.threads * E, fma((x + -mean[r]) * rstd[r], w[i], b[i]));
+                    }
+                y += a.y_stride;
+            }
+        y += y_step;
+        if (mean_to) {
+            mean_to += step;
+            rstd_to += step;
+        }
+        if (++stage == stages) {
+            stage = 0;
+            phase ^= 1;
+        }
+    }
+    // let the copies that were issued land before the block goes
+    if (limit == 0)
+        for (int s = 0; s < stages; ++s) mbar_wait(bars + s * 8, phase ^ (s < stage ? 0u : 1u), kPolls);
+    __syncthreads();
+}
+
+// Backward, rows whose vectors are aligned: the rows of x and dy come through a ring
+// of bulk copies in shared memory, kStages deep per group, so that no register
+// waits for memory and the loads of several groups of rows are always on their
+// way.  A group takes R rows at a time: their two sums each share one exchange
+// and one barrier.  That barrier also tells the group's first thread that
+// everyone is done with the rows before, whose place in the ring it refills.
+// A thread keeps its columns' part of dweight and dbias for all its rows.
+//
+// A copy that does not arrive within kPolls polls turns what the group writes into
+// NaN (the optimizer's gradient check then skips the iteration).
+template <typename T, int E, int kNV, int R, bool kFull, int kMaxThreads>
+__global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 1) norm_backward_ring_kernel(NormArgs a, int per_row, int stages)
+{
+    extern __shared__ __align__(128) uint8_t s_ring[];   // [groups][stages][R][x, dy][cols]
+    constexpr int kSums = 2 * R;          // of each row: sum(g), sum(g xhat)
+    __shared__ __align__(16) float s_part[2][32][kSums];
+    __shared__ __align__(8) uint64_t s_full[kRingBars];
+    const Group g(per_row);
+    const int cols = (int)a.cols;
+    const uint32_t row_bytes = (uint32_t)cols * sizeof(T), stage_bytes = row_bytes * 2 * R;
+    const uint32_t ring = smem_addr(s_ring) + (uint32_t)(g.index * stages) * stage_bytes;
+    const uint32_t bars = smem_addr(s_full) + (uint32_t)(g.index * stages) * 8;
+    const int64_t step = (int64_t)gridDim.x * g.per_block * R;
+    const int64_t row = ((int64_t)blockIdx.x * g.per_block + g.index) * R;
+    const auto has = [&](int i) { return kFull || (g.thread + i * g.threads) * E < cols; };
+    if (threadIdx.x < (unsigned)(g.per_block * stages)) mbar_init(smem_addr(s_full + threadIdx.x), 1);
+    __syncthreads();
+    mbar_init_fence();
+    grid_dependency_release();            // the sum over blocks may be set up meanwhile
+
+    // the group's first thread: the copies of the R rows from `from`, into stage s
+    const auto load_rows = [&](int64_t from, int s) {
+        const int n = a.rows - from < R ? (int)(a.rows - from) : R;
+        const uint32_t bar = bars + s * 8, dst = ring + s * stage_bytes;
+        mbar_expect(bar, row_bytes * 2 * n);
+        for (int r = 0; r < n; ++r) {
+            bulk_load(dst + r * 2 * row_bytes, static_cast<const T *>(a.x) + (from + r) * a.x_stride, row_bytes, bar);
+            bulk_load(dst + (r * 2 + 1) * row_bytes, static_cast<const T *>(a.dy) + (from + r) * a.dy_stride, row_bytes, bar);
+        }
+    };
+    if (g.thread == 0)
+        for (int s = 0; s < stages; ++s)
+            if (row + s * step < a.rows) load_rows(row + s * step, s);
+
+    Vals<E> w[kNV], dw[kNV], db[kNV];
+    float mean[R], rstd[R];
+    const float *mean_at = a.mean + row, *rstd_at = a.rstd + row;
+    const auto load_stats = [&](int n) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < n) {
+                mean[r] = mean_at[r];
+                rstd[r] = rstd_at[r];
+            }
+    };
+    int64_t left = a.rows - row;          // rows from here on
+    if (left > 0) load_stats(left < R ? (int)left : R);
+#pragma unroll
+    for (int i = 0; i < kNV; ++i) {
+        if (has(i)) w[i] = load_params<E>(a.weight, (g.thread + i * g.threads) * E, a.param_dtype, 1.0f);
+        dw[i].set(0.0f);
+        db[i].set(0.0f);
+    }
+    T *dx = static_cast<T *>(a.y) + row * a.y_stride + g.thread * E;
+    const int64_t dx_step = (step - R) * a.y_stride;
+    const uint32_t mine = ring + (uint32_t)g.thread * 16;
+    uint32_t limit = kPolls, phase = 0;
+    int stage = 0, turn = 0;
+    bool first = true;
+
+    for (; left > 0; left -= step) {
+        if (limit != 0 && !mbar_wait(bars + stage * 8, phase, limit)) limit = 0;
+        const uint32_t at = mine + stage * stage_bytes;
+        const int n = left < R ? (int)left : R;
+        float sums[kSums];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            Vals<E> ag, agx;
+            ag.set(0.0f);
+            agx.set(0.0f);
+            if (r < n) {
+                const float off = -mean[r] * rstd[r];
+#pragma unroll
+                for (int i = 0; i < kNV; ++i) {
+                    if (!has(i)) break;
+                    const Vals<E> x = widen16<T>(lds16(at + r * 2 * row_bytes + i * g.threads * 16));
+                    const Vals<E> d = widen16<T>(lds16(at + (r * 2 + 1) * row_bytes + i * g.threads * 16));
+                    const Vals<E> t = d * fma(x, rstd[r], off);
+                    ag = fma(d, w[i], ag);
+                    agx = fma(t, w[i], agx);
+                    dw[i] = dw[i] + t;
+                    db[i] = db[i] + d;
+                }
+            }
+            sums[2 * r] = total(ag);
+            sums[2 * r + 1] = total(agx);
+        }
+        const int lane = threadIdx.x & 31;
+        const float one = warp_sum_many<kSums>(sums);
+        float (*part)[kSums] = s_part[turn] + g.index * g.warps;
+        turn ^= 1;
+        if (lane % (32 / kSums) == 0) part[g.warp][lane / (32 / kSums)] = one;
+        if (g.warps > 1) g.sync();
+        else __syncwarp();
+        if (g.thread == 0 && !first && limit != 0) {      // the stage before this one is free
+            const int before = stage == 0 ? stages - 1 : stage - 1;
+            const int64_t ahead = (int64_t)(stages - 1) * step;
+            if (left > ahead) load_rows(a.rows - left + ahead, before);
+        }
+        first = false;
+        Vals<kSums> all;
+        all.set(0.0f);
+        for (int j = 0; j < g.warps; ++j) {
+            Vals<kSums> p;
+#pragma unroll
+            for (int i = 0; i < R; ++i) p.p[i] = *reinterpret_cast<const f32x2 *>(&part[j][2 * i]);
+            all = all + p;
+        }
+        float row_sum[kSums];
+        all.get(row_sum);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (r < n) {
+                // dx = rstd (dy w - m_g - xhat m_gx), gathered by factors of dy w and of x
+                const float rs = limit != 0 ? rstd[r] : CUDART_NAN_F;
+                const float by_x = -rs * rs * (row_sum[2 * r + 1] * a.inv_cols);
+                const float rest = fmaf(-mean[r], by_x, -rs * (row_sum[2 * r] * a.inv_cols));
+#pragma unroll
+                for (int i = 0; i < kNV; ++i) {
+                    if (!has(i)) break;
+                    const Vals<E> x = widen16<T>(lds16(at + r * 2 * row_bytes + i * g.threads * 16));
+                    const Vals<E> d = widen16<T>(lds16(at + (r * 2 + 1) * row_bytes + i * g.threads * 16));
+                    store_vec<T, E>(dx + i * g.threads * E, fma(d * w[i], rs, fma(x, by_x, rest)));
+                }
+                dx += a.y_stride;
+            }
+        }
+        dx += dx_step;
+        mean_at += step;
+        rstd_at += step;
+        if (left > step) load_stats(left - step < R ? (int)(left - step) : R);
+        if (++stage == stages) {
+            stage = 0;
+            phase ^= 1;
+        }
+    }
+    if (limit == 0) {
+        // let the copies that were issued land before the block goes
+        for (int s = 0; s < stages; ++s) mbar_wait(bars + s * 8, phase ^ (s < stage ? 0u : 1u), kPolls);
+#pragma unroll
+        for (int i = 0; i < kNV; ++i) dw[i].set(CUDART_NAN_F);
+    }
+    __syncthreads();
+
+    if (!a.partials) return;
+    float *out = a.partials + (int64_t)blockIdx.x * 2 * a.cols;
+    float *sums = g.per_block > 1 ? reinterpret_cast<float *>(s_ring) : out;   // the ring is done with
+    for (int turn = 0; turn < g.per_block; ++turn) {
+        if (turn > 0) __syncthreads();
+        if (g.index != turn) continue;
 #pragma unroll
         for (int i = 0; i < kNV; ++i) {
             const int c = (g.thread + i * g.threads) * E;
             if (c >= cols) break;
-            float f[E], wi[E], bi[E];
-            widen<T, E>(cur[i], f);
-            if constexpr (!kHold) {
-                load_params<E>(a.weight, c, a.param_dtype, 1.0f, wi);
-                load_params<E>(a.bias, c, a.param_dtype, 0.0f, bi);
-            }
+            float fw[E], fb[E];
+            dw[i].get(fw);
+            db[i].get(fb);
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                f[e] = fmaf((f[e] - mean) * rstd, kHold ? w[i][e] : wi[e], kHold ? b[i][e] : bi[e]);
-            store_vec<T, E>(y + c, f);
-            cur[i] = next[i];
+            for (int e = 0; e < E; ++e) {
+                const float pw = turn > 0 ? sums[c + e] + fw[e] : fw[e];
+                const float pb = turn > 0 ? sums[a.cols + c + e] + fb[e] : fb[e];
+                float *to = turn == g.per_block - 1 ? out : sums;
+                to[c + e] = pw;
+                to[a.cols + c + e] = pb;
+            }
         }
     }
 }
 
-// Backward: as above with both x and dy in registers, and each thread's part of
-// dweight and dbias, which it keeps for all its rows.  Groups of a block are
-// joined in shared memory in their order, blocks by norm_reduce_kernel.
-template <typename T, int E, int kNV, int kMaxThreads>
+// Backward, other rows: the same from registers, element by element.  A thread keeps its part of dweight and dbias for
+// all its rows.  Groups of a block are joined in shared memory in their order,
+// blocks by norm_reduce_kernel.
+template <typename T, int kNV, int R, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(NormArgs a, int per_row)
 {
     extern __shared__ float s_sums[];     // [2][cols], if a block has several groups
-    __shared__ float2 s_part[2][32];
+    constexpr int E = 1;
+    constexpr int kSums = 2 * R;          // of each row: sum(g), sum(g xhat)
+    __shared__ __align__(16) float s_part[2][32][kSums];
     const Group g(per_row);
     const int cols = (int)a.cols;         // rows held in registers are short
-    const int64_t step = (int64_t)gridDim.x * g.per_block;
-    int64_t row = (int64_t)blockIdx.x * g.per_block + g.index;
+    const int64_t step = (int64_t)gridDim.x * g.per_block * R;
+    int64_t row = ((int64_t)blockIdx.x * g.per_block + g.index) * R;
     const bool working = g.index < g.per_block && row < a.rows;
 
-    float w[kNV][E], dw[kNV][E], db[kNV][E];
-    Raw<T, E> xc[kNV], yc[kNV], xn[kNV], yn[kNV];
-    float mean = 0.0f, rstd = 0.0f;
+    const auto has = [&](int i) { return g.thread + i * g.threads < cols; };
+
+    Vals<E> w[kNV], dw[kNV], db[kNV];
+    struct Rows { Raw<T, E> x[R][kNV], dy[R][kNV]; float mean[R], rstd[R]; } even, odd;
+    const T *x = static_cast<const T *>(a.x) + row * a.x_stride + g.thread * E;
+    const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride + g.thread * E;
+    T *dx = static_cast<T *>(a.y) + row * a.y_stride + g.thread * E;
+    const float *mean = a.mean + row, *rstd = a.rstd + row;
+    const int64_t x_step = step * a.x_stride, dy_step = step * a.dy_stride, dx_step = step * a.y_stride;
+    const auto load_rows = [&](Rows &to, int64_t from) {
 #pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-        const int c = (g.thread + i * g.threads) * E;
-        if (working && c < cols) {
-            load_raw<T, E>(xc[i], static_cast<const T *>(a.x) + row * a.x_stride + c);
-            load_raw<T, E>(yc[i], static_cast<const T *>(a.dy) + row * a.dy_stride + c);
+        for (int r = 0; r < R; ++r) {
+            if (from + r >= a.rows) break;
+            to.mean[r] = mean[r];
+            to.rstd[r] = rstd[r];
+#pragma unroll
+            for (int i = 0; i < kNV; ++i)
+                if (has(i)) {
+                    load_raw<T, E>(to.x[r][i], x + r * a.x_stride + i * g.threads * E);
+                    load_raw<T, E>(to.dy[r][i], dy + r * a.dy_stride + i * g.threads * E);
+                }
         }
-#pragma unroll
-        for (int e = 0; e < E; ++e) dw[i][e] = db[i][e] = 0.0f;
-    }
-    if (working) {
-        mean = a.mean[row];
-        rstd = a.rstd[row];
-    }
+    };
+    if (working) load_rows(even, row);
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
-        const int c = (g.thread + i * g.threads) * E;
-        if (working && c < cols) load_params<E>(a.weight, c, a.param_dtype, 1.0f, w[i]);
+        if (working && has(i)) w[i] = load_params<E>(a.weight, (g.thread + i * g.threads) * E, a.param_dtype, 1.0f);
+        dw[i].set(0.0f);
+        db[i].set(0.0f);
     }
 
-    for (int turn = 0; working && row < a.rows; row += step, turn ^= 1) {
-        const bool more = row + step < a.rows;
-        float mean_n = 0.0f, rstd_n = 0.0f;
-        if (more) {
-            mean_n = a.mean[row + step];
-            rstd_n = a.rstd[row + step];
-        }
+    const auto some_rows = [&](Rows &cur, Rows &next, float (&shared)[32][kSums]) {
+        x += x_step;
+        dy += dy_step;
+        mean += step;
+        rstd += step;
+        load_rows(next, row + step);
+        float sums[kSums];
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (g.thread + i * g.threads) * E;
-            if (more && c < cols) {
-                load_raw<T, E>(xn[i], static_cast<const T *>(a.x) + (row + step) * a.x_stride + c);
-                load_raw<T, E>(yn[i], static_cast<const T *>(a.dy) + (row + step) * a.dy_stride + c);
+        for (int r = 0; r < R; ++r) {
+            Vals<E> ag, agx;
+            ag.set(0.0f);
+            agx.set(0.0f);
+            if (row + r < a.rows) {
+                const float off = -cur.mean[r] * cur.rstd[r];
+#pragma unroll
+                for (int i = 0; i < kNV; ++i) {
+                    if (!has(i)) break;
+                    const Vals<E> d = widen<T, E>(cur.dy[r][i]), t = d * fma(widen<T, E>(cur.x[r][i]), cur.rstd[r], off);
+                    ag = fma(d, w[i], ag);
+                    agx = fma(t, w[i], agx);
+                    dw[i] = dw[i] + t;
+                    db[i] = db[i] + d;
+                }
+            }
+            sums[2 * r] = total(ag);
+            sums[2 * r + 1] = total(agx);
+        }
+        const int lane = threadIdx.x & 31;
+        const float mine = warp_sum_many<kSums>(sums);
+        float (*part)[kSums] = shared + g.index * g.warps;
+        if (lane % (32 / kSums) == 0) part[g.warp][lane / (32 / kSums)] = mine;
+        if (g.warps > 1) g.sync();
+        else __syncwarp();
+        Vals<kSums> all;
+        all.set(0.0f);
+        for (int j = 0; j < g.warps; ++j) {
+            Vals<kSums> p;
+#pragma unroll
+            for (int i = 0; i < R; ++i) p.p[i] = *reinterpret_cast<const f32x2 *>(&part[j][2 * i]);
+            all = all + p;
+        }
+        float row_sum[kSums];
+        all.get(row_sum);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (row + r >= a.rows) break;
+            // dx = rstd (dy w - m_g - xhat m_gx), gathered by factors of dy w and of x
+            const float rs = cur.rstd[r], by_x = -rs * rs * (row_sum[2 * r + 1] * a.inv_cols);
+            const float rest = fmaf(-cur.mean[r], by_x, -rs * (row_sum[2 * r] * a.inv_cols));
+#pragma unroll
+            for (int i = 0; i < kNV; ++i) {
+                if (!has(i)) break;
+                const Vals<E> gw = widen<T, E>(cur.dy[r][i]) * w[i];
+                store_vec<T, E>(dx + r * a.y_stride + i * g.threads * E,
+                                fma(gw, rs, fma(widen<T, E>(cur.x[r][i]), by_x, rest)));
             }
         }
-        float sg = 0.0f, sgx = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            if ((g.thread + i * g.threads) * E >= cols) break;
-            float x[E], d[E];
-            widen<T, E>(xc[i], x);
-            widen<T, E>(yc[i], d);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float xh = (x[e] - mean) * rstd, gw = d[e] * w[i][e];
-                sg += gw;
-                sgx = fmaf(gw, xh, sgx);
-                dw[i][e] = fmaf(d[e], xh, dw[i][e]);
-                db[i][e] += d[e];
-            }
-        }
-        sg = warp_sum(sg);
-        sgx = warp_sum(sgx);
-        if (g.warps > 1) {
-            float2 *part = s_part[turn] + g.index * g.warps;
-            if ((threadIdx.x & 31) == 0) part[g.warp] = make_float2(sg, sgx);
-            g.sync();
-            sg = sgx = 0.0f;
-            for (int i = 0; i < g.warps; ++i) {
-                sg += part[i].x;
-                sgx += part[i].y;
-            }
-        }
-        const float mg = sg * a.inv_cols, mgx = sgx * a.inv_cols;
-        T *dx = static_cast<T *>(a.y) + row * a.y_stride;
-#pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (g.thread + i * g.threads) * E;
-            if (c >= cols) break;
-            float x[E], d[E];
-            widen<T, E>(xc[i], x);
-            widen<T, E>(yc[i], d);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float xh = (x[e] - mean) * rstd;
-                d[e] = rstd * fmaf(-xh, mgx, fmaf(d[e], w[i][e], -mg));
-            }
-            store_vec<T, E>(dx + c, d);
-            xc[i] = xn[i];
-            yc[i] = yn[i];
-        }
-        mean = mean_n;
-        rstd = rstd_n;
+        dx += dx_step;
+        row += step;
+    };
+    while (working) {
+        some_rows(even, odd, s_part[0]);
+        if (row >= a.rows) break;
+        some_rows(odd, even, s_part[1]);
+        if (row >= a.rows) break;
     }
 
     if (!a.partials) return;
@@ -336,10 +719,13 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(NormArgs a, 
         for (int i = 0; i < kNV; ++i) {
             const int c = (g.thread + i * g.threads) * E;
             if (c >= cols) break;
+            float fw[E], fb[E];
+            dw[i].get(fw);
+            db[i].get(fb);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float pw = turn > 0 ? sums[c + e] + dw[i][e] : dw[i][e];
-                const float pb = turn > 0 ? sums[a.cols + c + e] + db[i][e] : db[i][e];
+                const float pw = turn > 0 ? sums[c + e] + fw[e] : fw[e];
+                const float pb = turn > 0 ? sums[a.cols + c + e] + fb[e] : fb[e];
                 float *to = turn == g.per_block - 1 ? out : sums;
                 to[c + e] = pw;
                 to[a.cols + c + e] = pb;
@@ -459,7 +845,7 @@ norm_reduce_kernel(const float *partials, int n_blocks, int64_t cols, void *dwei
     store_any(out, c, grad_dtype, sum);
 }
 
-constexpr int kMaxPartials = 512;         // blocks that may leave a partial row
+constexpr int kMaxPartials = 1024;        // blocks that may leave a partial row
 
 // ---- which kernel ----------------------------------------------------------------
 
@@ -467,23 +853,42 @@ constexpr int kMaxPartials = 512;         // blocks that may leave a partial row
 // blocks of `block` threads; per_row = 0: the row does not fit, use the loop.
 struct Plan { int per_row, nv, block; };
 
-// A warp takes a row of up to `warp_nv` vectors a lane, then a block of at most
-// `max_threads`, with the fewest vectors a thread that are compiled.
-inline Plan plan_row(int64_t vectors, int warp_nv, const int *nvs, int n_nvs, int max_threads)
+inline Plan make_plan(int64_t vectors, int nv)
 {
-    Plan p = {0, 0, 0};
-    for (int i = 0; i < n_nvs && p.per_row == 0; ++i) {
-        const int64_t threads = (vectors + nvs[i] - 1) / nvs[i];
-        if (nvs[i] <= warp_nv && threads <= 32) p.per_row = 32, p.nv = nvs[i];
-    }
-    for (int i = 0; i < n_nvs && p.per_row == 0; ++i) {
-        const int64_t threads = (vectors + nvs[i] - 1) / nvs[i];
-        const int64_t most = i + 1 < n_nvs ? kRowThreads : max_threads;
-        if (threads <= most) p.per_row = (int)((threads + 31) / 32 * 32), p.nv = nvs[i];
-    }
-    p.block = p.per_row >= kRowThreads || p.per_row == 0 ? p.per_row : kRowThreads / p.per_row * p.per_row;
+    Plan p;
+    p.per_row = (int)(((vectors + nv - 1) / nv + 31) / 32 * 32);
+    p.nv = nv;
+    p.block = p.per_row >= kGroupThreads ? p.per_row : kGroupThreads / p.per_row * p.per_row;
     return p;
 }
+
+// Forward, element by element: as few warps a row as its elements fit into, but
+// enough rows in flight; with few rows, more and more warps share one.
+inline Plan plan_forward(int64_t cols, const int *nvs, int n, int64_t rows, int sms)
+{
+    Plan p = {0, 0, 0};
+    for (int i = n - 1; i >= 0; --i) {
+        const Plan q = make_plan(cols, nvs[i]);
+        if (q.per_row > kLongThreads) break;
+        if (p.per_row != 0 && rows * (p.per_row / 32) >= (int64_t)8 * sms) break;
+        if (i > 0 && (cols + nvs[i - 1] - 1) / nvs[i - 1] <= 32) continue;   // a warp does with fewer
+        p = q;
+    }
+    return p;
+}
+
+// Backward, element by element: columns stay with a thread for all rows, which costs
+// three registers an element besides the rows, so as few elements a thread as possible.
+inline Plan plan_backward(int64_t cols, const int *nvs, int n)
+{
+    for (int i = 0; i < n; ++i) {
+        const Plan q = make_plan(cols, nvs[i]);
+        if (q.per_row <= (i + 1 < n ? kRowThreads : kLongThreads)) return q;
+    }
+    return {0, 0, 0};
+}
+
+constexpr int kMaxShared = 220 * 1024;    // dynamic shared memory of a block, at most
 
 // Resident blocks per SM of a kernel, asked for once per device.
 template <typename K>
@@ -493,12 +898,12 @@ so_status resident(K kernel, int block, size_t smem, std::atomic<int> (&cache)[k
     if (cudaGetDevice(&dev) != cudaSuccess) return SO_ERR_CUDA;
     if (dev < 0 || dev >= kMaxDevices) return SO_ERR_UNSUPPORTED;
     // one word: the block size and shared memory it was asked for, and the answer
-    const int tag = (int)((block / 32) * 4096 + (int)(smem >> 10) * 32);
+    const int tag = (block / 32) << 13 | (int)(smem >> 10) << 5;
     int v = cache[dev].load(std::memory_order_relaxed);
     if (v == 0 || (v & ~31) != tag) {
         int n = 0;
-        if (smem > 48 * 1024 &&
-            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        if (smem > 40 * 1024 &&
+            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxShared) != cudaSuccess)
             return SO_ERR_CUDA;
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, block, smem) != cudaSuccess || n < 1)
             return SO_ERR_CUDA;
@@ -509,81 +914,167 @@ so_status resident(K kernel, int block, size_t smem, std::atomic<int> (&cache)[k
     return SO_OK;
 }
 
-template <typename T, int E, int kNV, int kMaxThreads>
+template <typename T, int kNV, int kMaxThreads>
 so_status launch_forward(const NormArgs &a, const Plan &p, int sms, cudaStream_t st)
 {
     static std::atomic<int> cache[kMaxDevices];
     int per_sm = 0;
-    const so_status s = resident(norm_forward_kernel<T, E, kNV, kMaxThreads>, p.block, 0, cache, &per_sm);
+    const so_status s = resident(norm_forward_kernel<T, kNV, kMaxThreads>, p.block, 0, cache, &per_sm);
     if (s != SO_OK) return s;
     const int groups = p.block / p.per_row;
     const int64_t want = (a.rows + groups - 1) / groups, most = (int64_t)per_sm * sms;
-    return launch(norm_forward_kernel<T, E, kNV, kMaxThreads>, (unsigned)(want < most ? want : most), p.block, 0, st,
+    return launch(norm_forward_kernel<T, kNV, kMaxThreads>, (unsigned)(want < most ? want : most), p.block, 0, st,
                   false, a, p.per_row);
 }
 
-template <typename T, int E, int kNV, int kMaxThreads>
+template <typename T, int kNV, int R, int kMaxThreads>
 so_status launch_backward(const NormArgs &a, const Plan &p, int sms, cudaStream_t st, int *blocks)
 {
     static std::atomic<int> cache[kMaxDevices];
     const int groups = p.block / p.per_row;
     const size_t smem = groups > 1 ? (size_t)a.cols * 2 * sizeof(float) : 0;
     int per_sm = 0;
-    const so_status s = resident(norm_backward_kernel<T, E, kNV, kMaxThreads>, p.block, smem, cache, &per_sm);
+    const so_status s = resident(norm_backward_kernel<T, kNV, R, kMaxThreads>, p.block, smem, cache, &per_sm);
     if (s != SO_OK) return s;
-    const int64_t want = (a.rows + groups - 1) / groups;
+    const int64_t want = (a.rows + groups * R - 1) / (groups * R);
     int64_t most = (int64_t)per_sm * sms;
     if (most > kMaxPartials) most = kMaxPartials;
     *blocks = (int)(want < most ? want : most);
-    return launch(norm_backward_kernel<T, E, kNV, kMaxThreads>, (unsigned)*blocks, p.block, smem, st, false, a, p.per_row);
+    return launch(norm_backward_kernel<T, kNV, R, kMaxThreads>, (unsigned)*blocks, p.block, smem, st, false, a, p.per_row);
+}
+
+// Stages of a ring: up to four, in the shared memory that four blocks share an SM with
+// (two blocks' if only two stages of long rows fit there).
+inline int ring_stages(size_t stage_bytes, int groups)
+{
+    int stages = (int)(kRingBytes / stage_bytes);
+    if (stages > 4) stages = 4;
+    if (stages < 2) stages = 2;
+    return stages < kRingBars / groups ? stages : kRingBars / groups;
+}
+
+template <typename T, int E, int kNV, int R, bool kFull, int kMaxThreads>
+so_status launch_forward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t st)
+{
+    const int groups = p.block / p.per_row;
+    const size_t stage = (size_t)a.cols * sizeof(T) * R * groups;
+    const int stages = ring_stages(stage, groups);
+    static std::atomic<int> cache[kMaxDevices];
+    int per_sm = 0;
+    const auto kernel = norm_forward_ring_kernel<T, E, kNV, R, kFull, kMaxThreads>;
+    const so_status s = resident(kernel, p.block, stage * stages, cache, &per_sm);
+    if (s != SO_OK) return s;
+    const int64_t want = (a.rows + groups * R - 1) / (groups * R), most = (int64_t)per_sm * sms;
+    return launch(kernel, (unsigned)(want < most ? want : most), p.block, stage * stages, st, false, a, p.per_row, stages);
+}
+
+template <typename T, int E, int kNV, int R, bool kFull, int kMaxThreads>
+so_status launch_backward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t st, int *blocks)
+{
+    const int groups = p.block / p.per_row;
+    const size_t stage = (size_t)a.cols * sizeof(T) * 2 * R * groups;
+    const int stages = ring_stages(stage, groups);
+    static std::atomic<int> cache[kMaxDevices];
+    int per_sm = 0;
+    const auto kernel = norm_backward_ring_kernel<T, E, kNV, R, kFull, kMaxThreads>;
+    const so_status s = resident(kernel, p.block, stage * stages, cache, &per_sm);
+    if (s != SO_OK) return s;
+    const int64_t want = (a.rows + groups * R - 1) / (groups * R);
+    int64_t most = (int64_t)per_sm * sms;
+    if (most > kMaxPartials) most = kMaxPartials;
+    *blocks = (int)(want < most ? want : most);
+    return launch(kernel, (unsigned)*blocks, p.block, stage * stages, st, false, a, p.per_row, stages);
+}
+
+// Vectors per thread for the ring kernels: the choice that leaves the fewest lanes
+// idle, and the largest of equals (fewer warps share a row, less goes into the
+// exchange).
+inline Plan plan_ring(int64_t vectors, int most_nv)
+{
+    Plan best = {0, 0, 0};
+    int64_t waste = INT64_MAX;
+    for (int nv = most_nv; nv > 0; --nv) {
+        const Plan p = make_plan(vectors, nv);
+        const int64_t idle = (int64_t)p.per_row * nv - vectors;
+        if (p.per_row <= kLongThreads && idle < waste) best = p, waste = idle;
+    }
+    return best;
+}
+
+template <typename T, int kNV, int R>
+so_status forward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t st)
+{
+    constexpr int E = Vec<T>::kElems;
+    const bool full = (int64_t)p.per_row * kNV * E == a.cols;
+    if (p.block <= kRowThreads)
+        return full ? launch_forward_ring<T, E, kNV, R, true, kRowThreads>(a, p, sms, st)
+                    : launch_forward_ring<T, E, kNV, R, false, kRowThreads>(a, p, sms, st);
+    return launch_forward_ring<T, E, kNV, R, false, kLongThreads>(a, p, sms, st);
 }
 
 template <typename T>
 so_status forward(const NormArgs &a, bool vec, int sms, cudaStream_t st)
 {
-    constexpr int E = Vec<T>::kElems;
-    static const int vec_nv[] = {1, 2, 3, 4}, one_nv[] = {4, 8, 16};
-    const Plan p = vec ? plan_row(a.cols / E, 4, vec_nv, 4, kMaxRowThreads) : plan_row(a.cols, 16, one_nv, 3, kMaxRowThreads);
-    if (p.per_row == 0) {
-        const unsigned grid = (unsigned)(a.rows < 4 * sms ? a.rows : 4 * sms);
-        return launch(norm_forward_loop_kernel<T>, grid, kLoopThreads, 0, st, false, a);
-    }
-    const bool wide = p.block > kRowThreads;
     if (vec) {
-        if (p.nv == 1) return launch_forward<T, E, 1, kRowThreads>(a, p, sms, st);
-        if (p.nv == 2) return launch_forward<T, E, 2, kRowThreads>(a, p, sms, st);
-        if (p.nv == 3) return launch_forward<T, E, 3, kRowThreads>(a, p, sms, st);
-        if (!wide) return launch_forward<T, E, 4, kRowThreads>(a, p, sms, st);
-        return launch_forward<T, E, 4, kMaxRowThreads>(a, p, sms, st);
+        const Plan p = plan_ring(a.cols / Vec<T>::kElems, 4);
+        if (p.per_row != 0 && a.cols * (int64_t)sizeof(T) * 2 <= kMaxShared) {
+            if (p.nv == 4) return forward_ring<T, 4, 1>(a, p, sms, st);
+            if (p.nv == 3) return forward_ring<T, 3, 1>(a, p, sms, st);
+            if (p.nv == 2) return forward_ring<T, 2, 2>(a, p, sms, st);
+            return forward_ring<T, 1, 4>(a, p, sms, st);
+        }
+    } else {
+        static const int nvs[] = {4, 8, 16};
+        const Plan p = plan_forward(a.cols, nvs, 3, a.rows, sms);
+        if (p.per_row != 0) {
+            if (p.nv == 4) return launch_forward<T, 4, kLongThreads>(a, p, sms, st);
+            if (p.nv == 8) return launch_forward<T, 8, kLongThreads>(a, p, sms, st);
+            return launch_forward<T, 16, kLongThreads>(a, p, sms, st);
+        }
     }
-    if (p.nv == 4) return launch_forward<T, 1, 4, kRowThreads>(a, p, sms, st);
-    if (p.nv == 8) return launch_forward<T, 1, 8, kRowThreads>(a, p, sms, st);
-    return launch_forward<T, 1, 16, kMaxRowThreads>(a, p, sms, st);
+    const unsigned grid = (unsigned)(a.rows < 4 * sms ? a.rows : 4 * sms);
+    return launch(norm_forward_loop_kernel<T>, grid, kLoopThreads, 0, st, false, a);
 }
 
-// The backward pass keeps three values per element besides the rows, so it
-// takes fewer elements a thread.
+template <typename T, int kNV, int R>
+so_status backward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t st, int *blocks)
+{
+    constexpr int E = Vec<T>::kElems;
+    const bool full = (int64_t)p.per_row * kNV * E == a.cols;
+    if (p.block <= kRowThreads)
+        return full ? launch_backward_ring<T, E, kNV, R, true, kRowThreads>(a, p, sms, st, blocks)
+                    : launch_backward_ring<T, E, kNV, R, false, kRowThreads>(a, p, sms, st, blocks);
+    return launch_backward_ring<T, E, kNV, R, false, kLongThreads>(a, p, sms, st, blocks);
+}
+
 template <typename T>
 so_status backward(const NormArgs &a, bool vec, int sms, cudaStream_t st, int *blocks)
 {
-    constexpr int E = Vec<T>::kElems;
-    static const int vec_nv[] = {1, 2}, one_nv[] = {4, 8};
-    constexpr int kMost = 512;
-    const Plan p = vec ? plan_row(a.cols / E, 1, vec_nv, 2, kMost) : plan_row(a.cols, 8, one_nv, 2, kMost);
-    if (p.per_row == 0) {
-        int64_t most = 2 * sms < kMaxPartials ? 2 * sms : kMaxPartials;
-        *blocks = (int)(a.rows < most ? a.rows : most);
-        return launch(norm_backward_loop_kernel<T>, (unsigned)*blocks, kLoopThreads, 0, st, false, a);
-    }
-    const bool wide = p.block > kRowThreads;
     if (vec) {
-        if (p.nv == 1) return launch_backward<T, E, 1, kRowThreads>(a, p, sms, st, blocks);
-        if (!wide) return launch_backward<T, E, 2, kRowThreads>(a, p, sms, st, blocks);
-        return launch_backward<T, E, 2, kMost>(a, p, sms, st, blocks);
+        const Plan p = plan_ring(a.cols / Vec<T>::kElems, 2);
+        const int64_t row = a.cols * (int64_t)sizeof(T);
+        if (p.per_row != 0 && row * 4 <= kMaxShared) {
+            // rows at a time: four, or as many as leave three stages in shared memory
+            const int r = row * 24 <= kMaxShared ? 4 : row * 12 <= kMaxShared ? 2 : 1;
+            if (p.nv == 2) {
+                if (r == 4) return backward_ring<T, 2, 4>(a, p, sms, st, blocks);
+                if (r == 2) return backward_ring<T, 2, 2>(a, p, sms, st, blocks);
+                return backward_ring<T, 2, 1>(a, p, sms, st, blocks);
+            }
+            if (r == 4) return backward_ring<T, 1, 4>(a, p, sms, st, blocks);
+            return backward_ring<T, 1, 1>(a, p, sms, st, blocks);
+        }
+    } else {
+        static const int nvs[] = {4, 8};
+        const Plan p = plan_backward(a.cols, nvs, 2);
+        if (p.per_row != 0) {
+            if (p.nv == 4) return launch_backward<T, 4, 2, kLongThreads>(a, p, sms, st, blocks);
+            return launch_backward<T, 8, 1, kLongThreads>(a, p, sms, st, blocks);
+        }
     }
-    if (p.nv == 4) return launch_backward<T, 1, 4, kRowThreads>(a, p, sms, st, blocks);
-    if (!wide) return launch_backward<T, 1, 8, kRowThreads>(a, p, sms, st, blocks);
-    return launch_backward<T, 1, 8, kMost>(a, p, sms, st, blocks);
+    const int64_t most = 2 * sms < kMaxPartials ? 2 * sms : kMaxPartials;
+    *blocks = (int)(a.rows < most ? a.rows : most);
+    return launch(norm_backward_loop_kernel<T>, (unsigned)*blocks, kLoopThreads, 0, st, false, a);
 }
 
 }  // namespace
