@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             rstd[r] = 1.0f / sqrtf(fmaf(fmaxf(m2[r], 0.0f), a.inv_cols, a.eps));
-            if (limit == 0 || m2[r] != m2[r]) rstd[r] = CUDART_NAN_F;
+            if (limit == 0 || m2[r] != m2[r]) rstd[r] = kNan;
             if (mean_to && g.thread == r && r < n) {
                 *mean_to = mean[r];
                 *rstd_to = rstd[r];
@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         for (int r = 0; r < R; ++r) {
             if (r < n) {
                 // dx = rstd (dy w - m_g - xhat m_gx), gathered by factors of dy w and of x
-                const float rs = limit != 0 ? rstd[r] : CUDART_NAN_F;
+                const float rs = limit != 0 ? rstd[r] : kNan;
                 const float by_x = -rs * rs * (row_sum[2 * r + 1] * a.inv_cols);
                 const float rest = fmaf(-mean[r], by_x, -rs * (row_sum[2 * r] * a.inv_cols));
 #pragma unroll
@@ -566,7 +566,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         // let the copies that were issued land before the block goes
         for (int s = 0; s < stages; ++s) mbar_wait(bars + s * 8, phase ^ (s < stage ? 0u : 1u), kPolls);
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) dw[i].set(CUDART_NAN_F);
+        for (int i = 0; i < kNV; ++i) dw[i].set(kNan);
     }
     __syncthreads();
 

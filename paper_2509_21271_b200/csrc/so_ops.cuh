@@ -8,7 +8,6 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
-#include <math_constants.h>
 #include <stdint.h>
 
 #include <atomic>
@@ -20,6 +19,8 @@
 namespace so_ops {
 
 constexpr int kMaxDevices = 64;
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kNan = __builtin_nanf("");
 
 struct bf16_t { uint16_t bits; };
 struct f16_t { uint16_t bits; };
