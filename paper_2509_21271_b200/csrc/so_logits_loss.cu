@@ -85,48 +85,64 @@ __device__ __forceinline__ MaxSum warp_merge(MaxSum a, float c)
     return a;
 }
 
-// One warp fills the targets of a distillation row: the teacher's softmax over
-// the entries that are there.
+// One warp fills the targets of a distillation row: ids, the student's logits there, the
+// teacher's softmax over the entries that are there and its logarithm.  False if none is.
 template <typename T>
 __device__ bool load_teacher(const LossArgs &a, int64_t row, int32_t *t_id, float *t_p, float *t_logp, float *t_z)
 {
+    constexpr int kAtOnce = 4;            // loads in flight per lane; the logits wait for the ids
     const int lane = threadIdx.x & 31;
     const T *z = static_cast<const T *>(a.logits) + row * a.stride;
-    MaxSum ms{-kInf, 0.0f};
+    float top = -kInf;
     bool any = false;
-    for (int k = lane; k < a.top_k; k += 32) {
-        const int64_t id = load_id(a.ids, row * a.ids_stride + k, a.ids_dtype);
-        const float x = load_any(a.teacher, row * a.teacher_stride + k, a.teacher_dtype);
-        const bool ok = id >= 0 && id < a.vocab && x != -kInf;
-        t_id[k] = ok ? (int32_t)id : -1;
-        t_logp[k] = x;
-        t_z[k] = ok ? to_f32(z[id]) : 0.0f;
-        if (ok) {
-            any = true;
-            if (x > ms.m) {
-                ms.s = ms.m == -kInf ? ms.s : ms.s * expf((ms.m - x) * a.inv_temperature);
-                ms.m = x;
+    for (int k0 = lane; k0 < a.top_k; k0 += 32 * kAtOnce) {
+        int32_t id[kAtOnce];
+        float x[kAtOnce], zk[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int k = k0 + 32 * u;
+            id[u] = -1;
+            x[u] = -kInf;
+            if (k < a.top_k) {
+                const int64_t wide = load_id(a.ids, row * a.ids_stride + k, a.ids_dtype);
+                x[u] = load_any(a.teacher, row * a.teacher_stride + k, a.teacher_dtype);
+                id[u] = wide >= 0 && wide < a.vocab ? (int32_t)wide : -1;
             }
-            ms.s += expf((x - (ms.m == -kInf ? 0.0f : ms.m)) * a.inv_temperature);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            if (x[u] == -kInf) id[u] = -1;
+            zk[u] = id[u] >= 0 ? to_f32(z[id[u]]) : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int k = k0 + 32 * u;
+            if (k >= a.top_k) break;
+            t_id[k] = id[u];
+            t_logp[k] = x[u];
+            t_z[k] = zk[u];
+            if (id[u] >= 0) {
+                any = true;
+                top = fmaxf(top, x[u]);
+            }
         }
     }
-    for (int o = 16; o > 0; o >>= 1) {
-        MaxSum b;
-        b.m = __shfl_xor_sync(0xFFFFFFFFu, ms.m, o);
-        b.s = __shfl_xor_sync(0xFFFFFFFFu, ms.s, o);
-        const float m = fmaxf(ms.m, b.m);
-        const float sa = ms.m == m || ms.m == -kInf ? ms.s : ms.s * expf((ms.m - m) * a.inv_temperature);
-        const float sb = b.m == m || b.m == -kInf ? b.s : b.s * expf((b.m - m) * a.inv_temperature);
-        ms.m = m;
-        ms.s = sa + sb;
-    }
-    const float inv = 1.0f / ms.s, log_s = logf(ms.s);
-    for (int k = lane; k < a.top_k; k += 32) {
-        const float d = (t_logp[k] - ms.m) * a.inv_temperature;
-        t_p[k] = t_id[k] >= 0 ? expf(d) * inv : 0.0f;
-        t_logp[k] = d - log_s;
-    }
     any = __any_sync(0xFFFFFFFFu, any);
+    asm("redux.sync.max.f32 %0, %0, 0xFFFFFFFF;" : "+f"(top));
+    float sum = 0.0f;
+    for (int k = lane; k < a.top_k; k += 32) {
+        const float d = (t_logp[k] - top) * a.inv_temperature;
+        const float e = t_id[k] >= 0 ? expf(d) : 0.0f;
+        t_logp[k] = d;
+        t_p[k] = e;
+        sum += e;
+    }
+    sum = warp_sum(sum);
+    const float inv = 1.0f / sum, log_s = logf(sum);
+    for (int k = lane; k < a.top_k; k += 32) {
+        t_p[k] *= inv;
+        t_logp[k] -= log_s;
+    }
     __syncwarp();
     return any;
 }
@@ -253,36 +269,74 @@ __global__ void __launch_bounds__(kRowThreads) loss_two_pass_kernel(LossArgs a)
 // ring of bulk copies.  The chunks of a row stay until their gradient is written;
 // the ring is larger than a share, so the next row is on its way meanwhile.
 //
+//   row warp        deals out the cluster's rows
 //   producer warp   keeps the ring full, row after row
-//   target warp     loads the teacher's list (or the token) of the next row, the
-//                   student's logits there and the teacher's softmax
+//   target warps    take the rows in turn, `depth` of them: load the teacher's list (or
+//                   the token) of a row to come, the student's logits there and the
+//                   teacher's softmax; when the row is done, its loss, and its
+//                   gradient at the targets
 //   the others      phase 1: maximum and sum over the chunks as they arrive; the
-//                   blocks of the cluster exchange theirs through each other's
-//                   shared memory; phase 2: gradient, chunk by chunk, each freed after;
-//                   then the row's few targets are written over
+//                   warps of the cluster exchange theirs through each other's
+//                   shared memory; phase 2: gradient, chunk by chunk, each freed after
 //
 // The elements before a row's first 16-byte boundary and after its last are loaded by
 // single threads.  Rows may start anywhere; a gradient whose rows start at another
 // offset from a 16-byte boundary than the logits' is stored element by element.
 //
-// A wait that runs out of polls makes the loss and the gradient of its row, and of
-// those after it, NaN (the optimizer's gradient check then skips the iteration).
+// A wait that runs out of polls ends its block's work: the loss comes out as NaN and the
+// gradient is not complete.
 
-constexpr int kPerThread = 2;             // 16-byte vectors of a chunk per thread
+#ifndef BIGT
+#define BIGT 512
+#endif
+#ifndef KPT
+#define KPT 2
+#endif
+#ifndef KTOG
+#define KTOG 2
+#endif
+constexpr int kTogether = KTOG;           // of which so many at once
+constexpr int kPerThread = KPT;           // 16-byte vectors of a chunk per thread
 constexpr int kMaxSlots = 32;
 constexpr int kMaxCluster = 8;
+constexpr int kMaxDepth = 4;
+constexpr int kQueue = 8;                 // rows dealt out ahead
+constexpr float kLn2 = 0.693147180559945f;
 
 struct RingShape {
-    int threads;                          // that compute; the block has two warps more
-    int cluster, slots;
+    int threads;                          // that compute; the block has 2 + depth warps more
+    int cluster, slots, depth;            // blocks a row, chunks of the ring, rows whose targets are at hand
     int chunk_bytes;
+    int balance;                          // deal out masked rows separately
     size_t smem;
 };
 
 struct RowInfo {
+    int64_t row;                          // -1: no more
     float weight;
     int32_t load, live;                   // read the row at all; its loss and gradient are not zero
+    int32_t repeats;                      // some id is in its list more than once
 };
+
+// Places of the table that finds repeated ids: a power of two, at least twice the list; none
+// for a list short enough to be compared with itself.
+__host__ __device__ inline int table_places(int top_k)
+{
+    if (top_k <= 128) return 0;
+    int n = 256;
+    while (n < 2 * top_k) n *= 2;
+    return n;
+}
+
+// Whether the condition holds for any of the computing threads; a barrier for them.
+__device__ __forceinline__ bool any_of(bool condition, int threads)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\t"
+                 "selp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)condition), "r"(threads) : "memory");
+    return r != 0;
+}
 
 __device__ __forceinline__ uint32_t cluster_rank()
 {
@@ -328,16 +382,13 @@ __device__ __forceinline__ MaxSum join(const MaxSum &a, const MaxSum &b, float c
     return r;
 }
 
-template <int kLanes>
+// The same over the lanes of a warp.
 __device__ __forceinline__ MaxSum join_lanes(MaxSum a, float c)
 {
-#pragma unroll
-    for (int o = kLanes / 2; o > 0; o >>= 1) {
-        MaxSum b;
-        b.m = __shfl_xor_sync(0xFFFFFFFFu, a.m, o);
-        b.s = __shfl_xor_sync(0xFFFFFFFFu, a.s, o);
-        a = join(a, b, c);
-    }
+    float top;
+    asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(top) : "f"(a.m));
+    a.s = warp_sum(a.m == top || a.m == -kInf ? a.s : a.s * rescale(a.m, top, c));
+    a.m = top;
     return a;
 }
 
@@ -366,73 +417,140 @@ template <> __device__ __forceinline__ float largest<f16_t>(const uint4 &v)
 }
 
 // exp((z - m) / T) of a vector
-template <int E>
-__device__ __forceinline__ Vals<E> exponentials(const Vals<E> &z, float m, float ref, bool is_plain, float c)
+template <bool kPlainRow, int E>
+__device__ __forceinline__ Vals<E> exponentials(const Vals<E> &z, float m, float ref, float c)
 {
-    const Vals<E> x = is_plain ? fma(z, c, -ref) : (z + -m) * c;
-    float f[E];
-    x.get(f);
+    Vals<E> x = kPlainRow ? fma(z, c, -ref) : (z + -m) * c;
 #pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = exp2_fast(f[e]);
-    Vals<E> r;
-    r.put(f);
-    return r;
+    for (int i = 0; i < E / 2; ++i) {
+        float lo, hi;
+        split(x.p[i], lo, hi);
+        x.p[i] = pair(exp2_fast(lo), exp2_fast(hi));
+    }
+    return x;
 }
 
-// Running maximum and sum of a thread.
+// Running sum of a thread, against a reference that need not be the maximum: it is
+// taken from the first vectors and moved only when something exceeds it by a factor of
+// 2^kSlack, which fp32 holds with ease.  (Were it the maximum, some lane of a warp
+// would move it with almost every vector.)
+constexpr float kSlack = 16.0f;
+
 template <typename T>
 struct Running {
     static constexpr int E = Vec<T>::kElems;
-    float m, ref;
+    float m, ref, bound;                  // reference, the same in units of log2, and where it moves
     bool is_plain;
     Vals<E> s;
 
-    __device__ __forceinline__ Running() : m(-kInf), ref(0.0f), is_plain(false) { s.set(0.0f); }
-    __device__ __forceinline__ void raise(float to, float c)
+    __device__ __forceinline__ Running() : m(-kInf), ref(0.0f), bound(-kInf), is_plain(false) { s.set(0.0f); }
+
+    template <int N>
+    __device__ __forceinline__ void add(const uint4 (&v)[N], float c, float slack)   // slack = kSlack / c
     {
-        const float k = m == -kInf ? 1.0f : rescale(m, to, c);   // a sum of nothing (or NaN) stays
-        s = s * k;
-        m = to;
-        is_plain = plain(m);
-        ref = m * c;
-    }
-    __device__ __forceinline__ void add(const uint4 &v, float c)
-    {
-        // while everything was -inf: (-inf) - 0 = -inf, nothing to add
-        s = s + exponentials<E>(widen16<T>(v), m == -kInf ? 0.0f : m, ref, is_plain, c);
+        float top = largest<T>(v[0]);
+#pragma unroll
+        for (int i = 1; i < N; ++i) top = fmaxf(top, largest<T>(v[i]));
+        if (top > bound) {
+            if (m != -kInf) s = s * rescale(m, top, c);   // a sum of nothing (or NaN) stays
+            m = top;
+            ref = m * c;
+            bound = m + slack;
+            is_plain = plain(m);
+        }
+        if (is_plain) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) s = s + exponentials<true>(widen16<T>(v[i]), m, ref, c);
+        } else {
+            // while everything was -inf: (-inf) - 0 = -inf, nothing to add
+            const float base = m == -kInf ? 0.0f : m;
+#pragma unroll
+            for (int i = 0; i < N; ++i) s = s + exponentials<false>(widen16<T>(v[i]), base, ref, c);
+        }
     }
 };
 
-template <typename T, int kMode, bool kGrad>
-__global__ void __launch_bounds__(576, 1) loss_ring_kernel(LossArgs a, RingShape shape)
+// The rows of a cluster, in ascending order, by one warp.  Where a cluster has many long
+// rows (`balance`), masked rows, which cost less than the others, are dealt out
+// separately, both kinds in turn by their own count: the warp looks at 32 rows at a
+// time, and all clusters come to the same counts.  Otherwise every n-th row.
+template <typename Wanted, typename Give>
+__device__ void walk_rows(const Wanted &wanted, int64_t rows, int n, int mine, bool balance, Give give)
+{
+    const int lane = threadIdx.x & 31;
+    if (!balance) {
+        // a lane looks at the row that is its turn, 32 turns at a time
+        for (int64_t base = mine; base < rows; base += (int64_t)32 * n) {
+            const int64_t row = base + (int64_t)lane * n;
+            const uint32_t reads = __ballot_sync(0xFFFFFFFFu, row < rows && wanted(row));
+            for (int i = 0; i < 32 && base + (int64_t)i * n < rows; ++i)
+                if (!give(base + (int64_t)i * n, (reads >> i) & 1u)) return;
+        }
+        return;
+    }
+    constexpr int kAhead = 4;             // windows whose loads are in flight
+    bool next[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) next[i] = 32 * i + lane < rows && wanted(32 * i + lane);
+    int live_turn = 0, dead_turn = 0;     // whose turn it is
+    for (int64_t base = 0; base < rows; base += 32) {
+        const bool here = base + lane < rows, live = next[0];
+#pragma unroll
+        for (int i = 0; i + 1 < kAhead; ++i) next[i] = next[i + 1];
+        const int64_t ahead = base + 32 * kAhead + lane;
+        next[kAhead - 1] = ahead < rows && wanted(ahead);
+        const uint32_t lives = __ballot_sync(0xFFFFFFFFu, here && live), deads = __ballot_sync(0xFFFFFFFFu, here && !live);
+        const uint32_t before = (1u << lane) - 1u;
+        const int turn = live ? live_turn + __popc(lives & before) : dead_turn + __popc(deads & before);
+        uint32_t todo = __ballot_sync(0xFFFFFFFFu, here && turn % n == mine);
+        live_turn = (live_turn + __popc(lives)) % n;
+        dead_turn = (dead_turn + __popc(deads)) % n;
+        for (; todo; todo &= todo - 1) {
+            const int at = __ffs(todo) - 1;
+            if (!give(base + at, (lives >> at) & 1u)) return;
+        }
+    }
+}
+
+// kBig: one block an SM of up to 512 computing threads, else two or more of up to 256
+template <typename T, int kMode, bool kGrad, bool kBig>
+__global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ring_kernel(LossArgs a, RingShape shape)
 {
     constexpr int E = Vec<T>::kElems;
-    extern __shared__ __align__(128) uint8_t s_ring[];   // [slots][chunk], then the targets of two rows
-    __shared__ __align__(8) uint64_t s_full[kMaxSlots], s_empty[kMaxSlots], s_target_full[2], s_target_empty[2], s_exchange[2];
-    __shared__ __align__(8) MaxSum s_warp[2][16], s_block[2][kMaxCluster];
-    __shared__ RowInfo s_info[2];
+    extern __shared__ __align__(128) uint8_t s_ring[];   // [slots][chunk], then the targets of `depth` rows and a table
+    __shared__ __align__(8) uint64_t s_full[kMaxSlots], s_empty[kMaxSlots], s_exchange[2];
+    __shared__ __align__(8) uint64_t s_target_full[kMaxDepth], s_target_empty[kMaxDepth];
+    __shared__ __align__(8) uint64_t s_queue_full[kQueue], s_queue_empty[kQueue];
+    __shared__ int64_t s_queue[kQueue];                  // 2 row + (is it read), -1: no more
+    __shared__ __align__(8) MaxSum s_block[2][kMaxCluster * 24];
+    __shared__ RowInfo s_info[kMaxDepth];
+    __shared__ float4 s_result[kMaxDepth];               // reference, sum: its logarithm and inverse; the gradient's factor
     const int warps = shape.threads >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cluster = shape.cluster, slots = shape.slots;
+    const int cluster = shape.cluster, slots = shape.slots, depth = shape.depth;
     const uint32_t rank = cluster > 1 ? cluster_rank() : 0u;
-    const int64_t first_row = blockIdx.x / cluster, row_step = gridDim.x / cluster;
-    const int top_k = kMode == kDistill ? a.top_k : 1;
-    // targets of row buffer b: id, probability, its logarithm, logit
+    const int my_cluster = (int)(blockIdx.x / cluster), clusters = (int)(gridDim.x / cluster);
+    // targets of a row buffer: id, probability, its logarithm, logit, each padded to whole vectors
+    const int top_k = kMode == kDistill ? a.top_k : 1, pad_k = (top_k + 3) & ~3;   // lists start at 16 bytes
     float *s_targets = reinterpret_cast<float *>(s_ring + (size_t)slots * shape.chunk_bytes);
-    const auto target_id = [&](int b) { return reinterpret_cast<int32_t *>(s_targets + (size_t)b * 4 * top_k); };
-    const auto target_p = [&](int b) { return s_targets + (size_t)b * 4 * top_k + top_k; };
-    const auto target_logp = [&](int b) { return s_targets + (size_t)b * 4 * top_k + 2 * top_k; };
-    const auto target_z = [&](int b) { return s_targets + (size_t)b * 4 * top_k + 3 * top_k; };
+    const auto target_id = [&](int b) { return reinterpret_cast<int32_t *>(s_targets + (size_t)b * 4 * pad_k); };
+    const auto target_p = [&](int b) { return s_targets + (size_t)b * 4 * pad_k + pad_k; };
+    const auto target_logp = [&](int b) { return s_targets + (size_t)b * 4 * pad_k + 2 * pad_k; };
+    const auto target_z = [&](int b) { return s_targets + (size_t)b * 4 * pad_k + 3 * pad_k; };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < slots; ++i) {
             mbar_init(smem_addr(&s_full[i]), 1);
             mbar_init(smem_addr(&s_empty[i]), warps);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < depth; ++i) {
             mbar_init(smem_addr(&s_target_full[i]), 1);
             mbar_init(smem_addr(&s_target_empty[i]), warps);
-            mbar_init(smem_addr(&s_exchange[i]), 1);
         }
+        for (int i = 0; i < kQueue; ++i) {
+            mbar_init(smem_addr(&s_queue_full[i]), 1);
+            mbar_init(smem_addr(&s_queue_empty[i]), 2);
+        }
+        for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&s_exchange[i]), 1);
         mbar_init_fence();
     }
     __syncwarp();
@@ -454,77 +572,192 @@ __global__ void __launch_bounds__(576, 1) loss_ring_kernel(LossArgs a, RingShape
         p.mine = p.count - p.from < per ? p.count - p.from : per;
         return p;
     };
-    const auto wanted = [&](int64_t row, float &w) {      // is the row read at all
-        w = a.weight ? a.weight[row] : 1.0f;
-        if (kMode == kDistill) return w != 0.0f;
+    const auto wanted = [&](int64_t row) {                // is the row read at all
+        if (a.weight && a.weight[row] == 0.0f) return false;
+        if (kMode == kDistill) return true;
         const int64_t token = load_id(a.ids, row, a.ids_dtype);
-        return w != 0.0f && token >= 0 && token < a.vocab;
+        return token >= 0 && token < a.vocab;
     };
     const int per_chunk = shape.chunk_bytes / 16;
     uint32_t limit = kPolls;
+    // the next row of the queue (by the producer and the target warp), -1 at the end
+    const auto next_row = [&](uint32_t taken, bool &load) {
+        const uint32_t at = taken % kQueue;
+        if (limit != 0 && !mbar_wait(smem_addr(&s_queue_full[at]), (taken / kQueue) & 1, limit)) limit = 0;
+        limit = __shfl_sync(0xFFFFFFFFu, limit, 0);
+        const int64_t v = limit == 0 ? -1 : s_queue[at];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&s_queue_empty[at]));
+        load = v >= 0 && (v & 1) != 0;
+        return v >= 0 ? v >> 1 : -1;
+    };
 
-    if (warp == warps) {
+    if (warp == warps + 1) {
+        // ---- rows ----
+        uint32_t given = 0;
+        const auto give = [&](int64_t row, uint32_t load) {
+            const uint32_t at = given % kQueue;
+            if (limit != 0 && !mbar_wait(smem_addr(&s_queue_empty[at]), ((given / kQueue) & 1) ^ 1, limit)) limit = 0;
+            limit = __shfl_sync(0xFFFFFFFFu, limit, 0);
+            if (limit == 0) return false;
+            if (lane == 0) {
+                s_queue[at] = row < 0 ? -1 : 2 * row + load;
+                mbar_arrive(smem_addr(&s_queue_full[at]));
+            }
+            ++given;
+            return true;
+        };
+        walk_rows(wanted, a.rows, clusters, my_cluster, shape.balance != 0 && a.rows > clusters, give);
+        for (int i = 0; i < depth; ++i)       // an end mark for every target warp
+            if (!give(-1, 0)) break;
+    } else if (warp == warps) {
         // ---- producer ----
         uint32_t slot = 0, phase = 0, issued = 0;
-        float w;
-        bool load = first_row < a.rows && wanted(first_row, w);
-        for (int64_t row = first_row; row < a.rows; row += row_step) {
-            const bool load_next = row + row_step < a.rows && wanted(row + row_step, w);
-            if (load) {
-                const Part p = part_of(row);
-                const T *src = static_cast<const T *>(a.logits) + row * a.stride + p.head + (int64_t)p.from * E;
-                for (int v = 0; v < p.mine && limit != 0; v += per_chunk) {
-                    if (!mbar_wait(smem_addr(&s_empty[slot]), phase ^ 1, limit)) limit = 0;
-                    if (lane == 0 && limit != 0) {
-                        const uint32_t bytes = (uint32_t)(p.mine - v < per_chunk ? p.mine - v : per_chunk) * 16;
-                        const uint32_t bar = smem_addr(&s_full[slot]);
-                        mbar_expect(bar, bytes);
-                        bulk_load(smem_addr(s_ring) + slot * shape.chunk_bytes, src + (int64_t)v * E, bytes, bar);
-                    }
-                    if (limit == 0) break;
-                    ++issued;
-                    if (++slot == (uint32_t)slots) slot = 0, phase ^= 1;
+        bool load;
+        uint32_t taken = 0;
+        for (int64_t row = next_row(taken++, load); row >= 0; row = next_row(taken++, load)) {
+            if (!load) continue;
+            const Part p = part_of(row);
+            const T *src = static_cast<const T *>(a.logits) + row * a.stride + p.head + (int64_t)p.from * E;
+            for (int v = 0; v < p.mine && limit != 0; v += per_chunk) {
+                if (!mbar_wait(smem_addr(&s_empty[slot]), phase ^ 1, limit)) limit = 0;
+                limit = __shfl_sync(0xFFFFFFFFu, limit, 0);
+                if (limit == 0) break;
+                if (lane == 0) {
+                    const uint32_t bytes = (uint32_t)(p.mine - v < per_chunk ? p.mine - v : per_chunk) * 16;
+                    const uint32_t bar = smem_addr(&s_full[slot]);
+                    mbar_expect(bar, bytes);
+                    bulk_load(smem_addr(s_ring) + slot * shape.chunk_bytes, src + (int64_t)v * E, bytes, bar);
                 }
+                ++issued;
+                if (++slot == (uint32_t)slots) slot = 0, phase ^= 1;
             }
-            load = load_next;
         }
         // whatever was issued lands before the block goes (consumed already, unless a wait ran out)
         for (uint32_t i = issued > (uint32_t)slots ? issued - slots : 0; i < issued; ++i)
             mbar_wait(smem_addr(&s_full[i % slots]), (i / slots) & 1, kPolls);
-    } else if (warp == warps + 1) {
-        // ---- targets ----
-        int buf = 0;
-        uint32_t phase = 0;
-        float w = 0.0f;
-        bool load = first_row < a.rows && wanted(first_row, w);
-        for (int64_t row = first_row; row < a.rows; row += row_step) {
-            float w_next = 0.0f;
-            const bool load_next = row + row_step < a.rows && wanted(row + row_step, w_next);
-            if (limit != 0 && !mbar_wait(smem_addr(&s_target_empty[buf]), phase ^ 1, limit)) limit = 0;
-            bool live = load;
-            if (load && kMode == kDistill) {
+    } else if (warp >= warps + 2) {
+        // ---- targets: the lists of rows to come; of the rows that are done, the
+        // loss and the gradient at the targets, over what phase 2 wrote there ----
+        const auto finish = [&](int buf, uint32_t parity) {
+            if (limit != 0 && !mbar_wait(smem_addr(&s_target_empty[buf]), parity, limit)) limit = 0;
+            const RowInfo info = s_info[buf];
+            const float4 done = s_result[buf];
+            const float c = a.log2e_over_t, ref = done.x * c;
+            const bool is_plain = plain(done.x);
+            const auto exponent = [&](float z) { return is_plain ? fmaf(z, c, -ref) : (z - done.x) * c; };
+            if (limit == 0) {
+                if (rank == 0 && lane == 0) a.row_loss[info.row] = kNan;
+                return;
+            }
+            if (!info.live) {
+                if (rank == 0 && lane == 0) {
+                    a.row_loss[info.row] = 0.0f;
+                    if (kMode == kPolicy && a.logp) a.logp[info.row] = 0.0f;
+                }
+                return;
+            }
+            const int32_t *ids = target_id(buf);
+            const float *probs = target_p(buf);
+            if (kMode == kDistill && rank == 0) {
+                const float loss = distill_row_loss(a, ids, probs, target_logp(buf), target_z(buf),
+                                                    [&](float z) { return fmaf(exponent(z), kLn2, -done.y); });
+                if (lane == 0) a.row_loss[info.row] = loss;
+            }
+            if (kGrad) {
+                const Part p = part_of(info.row);
+                T *g = static_cast<T *>(a.grad) + info.row * a.grad_stride;
+                for (int k = lane; k < top_k; k += 32) {
+                    const int32_t id = ids[k];
+                    if (id < 0) continue;
+                    // the block that has the element
+                    const int v = (id - p.head) / E;
+                    const bool my_part = id < p.head ? rank == 0
+                                         : v >= p.count ? rank == (uint32_t)cluster - 1
+                                                        : v >= p.from && v < p.from + p.mine;
+                    if (!my_part) continue;
+                    float prob = probs[k];
+                    if (info.repeats) {
+                        prob = 0.0f;
+                        for (int i = 0; i < top_k; ++i)
+                            if (ids[i] == id) prob += probs[i];
+                    }
+                    g[id] = from_f32<T>(done.w * fmaf(exp2_fast(exponent(target_z(buf)[k])), done.z, -prob));
+                }
+            }
+            __syncwarp();
+        };
+        // Does an id occur twice in a list?  A short list is compared with itself.  The ids of
+        // a long one are put into a table of at least twice as many places, each at the
+        // first free one from where its hash points.
+        const int buf = warp - (warps + 2), places = table_places(top_k);
+        int32_t *table = reinterpret_cast<int32_t *>(s_targets + (size_t)depth * 4 * pad_k) + buf * places;
+        const auto repeats = [&](const int32_t *ids) {
+            bool twice = false;
+            if (places == 0) {
+                for (int k = lane; k < top_k; k += 32) {
+                    int same = 0;
+#pragma unroll 4
+                    for (int i = 0; i < pad_k; i += 4) {
+                        const int4 q = *reinterpret_cast<const int4 *>(ids + i);
+                        same += (q.x == ids[k]) + (q.y == ids[k]) + (q.z == ids[k]) + (q.w == ids[k]);
+                    }
+                    twice |= ids[k] >= 0 && same > 1;
+                }
+                return __any_sync(0xFFFFFFFFu, twice) != 0;
+            }
+            for (int i = lane; i < places; i += 32) table[i] = -1;
+            __syncwarp();
+            for (int k = lane; k < top_k; k += 32) {
+                const int32_t id = ids[k];
+                uint32_t at = ((uint32_t)id * 2654435761u) >> 16;
+                for (int tries = 0; id >= 0 && tries < places; ++tries, ++at) {
+                    const int32_t was = atomicCAS(&table[at & (places - 1)], -1, id);
+                    twice |= was == id;
+                    if (was == -1 || was == id) break;
+                }
+            }
+            return __any_sync(0xFFFFFFFFu, twice) != 0;
+        };
+        bool load = false;
+        for (uint32_t it = buf;; it += depth) {
+            const int64_t row = next_row(it, load);
+            if (limit == 0 && lane == 0) a.row_loss[my_cluster] = kNan;
+            if (it >= (uint32_t)depth) finish(buf, ((it / depth) & 1) ^ 1);
+            bool live = row >= 0 && load, twice = false;
+            if (live && kMode == kDistill) {
                 live = load_teacher<T>(a, row, target_id(buf), target_p(buf), target_logp(buf), target_z(buf));
-            } else if (load && lane == 0) {
+                if (lane < pad_k - top_k) target_id(buf)[top_k + lane] = -1;
+                __syncwarp();
+                twice = kGrad && live && repeats(target_id(buf));
+            } else if (live && lane == 0) {
                 const int64_t token = load_id(a.ids, row, a.ids_dtype);
                 target_id(buf)[0] = (int32_t)token;
                 target_p(buf)[0] = 1.0f;
                 target_z(buf)[0] = to_f32(static_cast<const T *>(a.logits)[row * a.stride + token]);
             }
-            if (lane == 0) s_info[buf] = RowInfo{w, load, live};
+            if (lane == 0) s_info[buf] = RowInfo{row, row >= 0 && a.weight ? a.weight[row] : 1.0f, row >= 0 && load, live, twice};
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&s_target_full[buf]));
-            load = load_next;
-            w = w_next;
-            if (++buf == 2) buf = 0, phase ^= 1;
+            if (row < 0) break;
         }
     } else {
         // ---- the rest ----
-        const float c = a.log2e_over_t;
+        const float c = a.log2e_over_t, slack = kSlack / c;
+        const uint32_t ring = smem_addr(s_ring) + threadIdx.x * 16, vector_step = (uint32_t)shape.threads * 16;
         uint32_t slot = 0, phase = 0, row_phase = 0, computed = 0;   // rows computed so far: even and odd ones take turns
         int buf = 0;
-        for (int64_t row = first_row; row < a.rows; row += row_step) {
-            if (limit != 0 && !mbar_wait(smem_addr(&s_target_full[buf]), row_phase, limit)) limit = 0;
+        while (true) {
+            // one warp waits for the row's targets, the others for that warp; all agree
+            // on whether some wait ran out, which ends the block's work
+            if (warp == 0 && limit != 0 && !mbar_wait(smem_addr(&s_target_full[buf]), row_phase, limit)) limit = 0;
+            if (any_of(limit == 0, shape.threads)) {
+                if (threadIdx.x == 0) a.row_loss[my_cluster] = kNan;
+                break;
+            }
             const RowInfo info = s_info[buf];
+            const int64_t row = info.row;
+            if (row < 0) break;
             const Part p = part_of(row);
             const T *z = static_cast<const T *>(a.logits) + row * a.stride;
             T *g = kGrad ? static_cast<T *>(a.grad) + row * a.grad_stride : nullptr;
@@ -554,10 +787,6 @@ __global__ void __launch_bounds__(576, 1) loss_ring_kernel(LossArgs a, RingShape
                     }
                     if (edge >= 0) g[edge] = from_f32<T>(0.0f);
                 }
-                if (rank == 0 && threadIdx.x == 0) {
-                    a.row_loss[row] = 0.0f;
-                    if (kMode == kPolicy && a.logp) a.logp[row] = 0.0f;
-                }
             } else {
                 float edge_z = 0.0f;
                 if (edge >= 0) edge_z = to_f32(z[edge]);
@@ -572,19 +801,20 @@ __global__ void __launch_bounds__(576, 1) loss_ring_kernel(LossArgs a, RingShape
                 Running<T> run;
                 for (int v = 0; v < p.mine; v += per_chunk) {
                     if (limit != 0 && !mbar_wait(smem_addr(&s_full[slot]), phase, limit)) limit = 0;
-                    const uint32_t at = smem_addr(s_ring) + slot * shape.chunk_bytes + threadIdx.x * 16;
-                    const int i0 = v + (int)threadIdx.x, i1 = i0 + shape.threads;
-                    if (i1 < p.mine) {
-                        const uint4 q0 = lds16(at), q1 = lds16(at + shape.threads * 16);
-                        const float top = fmaxf(largest<T>(q0), largest<T>(q1));
-                        if (top > run.m) run.raise(top, c);
-                        run.add(q0, c);
-                        run.add(q1, c);
-                    } else if (i0 < p.mine) {
-                        const uint4 q0 = lds16(at);
-                        const float top = largest<T>(q0);
-                        if (top > run.m) run.raise(top, c);
-                        run.add(q0, c);
+                    const uint32_t at = ring + slot * shape.chunk_bytes;
+                    if (v + per_chunk <= p.mine) {
+#pragma unroll
+                        for (int u = 0; u < kPerThread; u += kTogether) {
+                            uint4 q[kTogether];
+#pragma unroll
+                            for (int i = 0; i < kTogether; ++i) q[i] = lds16(at + (u + i) * vector_step);
+                            run.add(q, c, slack);
+                        }
+                    } else {
+                        for (int u = 0; v + u * shape.threads + (int)threadIdx.x < p.mine; ++u) {
+                            const uint4 q[1] = {lds16(at + u * vector_step)};
+                            run.add(q, c, slack);
+                        }
                     }
                     if (!kGrad) {
                         __syncwarp();
@@ -598,45 +828,36 @@ __global__ void __launch_bounds__(576, 1) loss_ring_kernel(LossArgs a, RingShape
                     const float own = plain(edge_z) ? exp2_fast(fmaf(edge_z, c, -(edge_z * c))) : exp2_fast(edge_z - edge_z);
                     ms = join(ms, MaxSum{edge_z, edge_z == -kInf ? 0.0f : own}, c);
                 }
+                ms = join_lanes(ms, c);
                 if (limit == 0) ms.s = kNan;
-                ms = join_lanes<32>(ms, c);
+                // every warp's part to every block of the cluster
                 const int turn = computed & 1;
-                if (lane == 0) s_warp[turn][warp] = ms;
-                asm volatile("bar.sync 1, %0;" ::"r"(shape.threads) : "memory");
-                if (cluster == 1 || warp == 0) {
-                    // at most 16 warps, the same in both halves of this one
-                    ms = (lane & 15) < warps ? s_warp[turn][lane & 15] : MaxSum{-kInf, 0.0f};
-                    ms = join_lanes<16>(ms, c);
-                }
                 if (cluster > 1) {
                     const uint32_t bar = smem_addr(&s_exchange[turn]);
-                    if (warp == 0) {
-                        if (lane == 0) mbar_expect(bar, (uint32_t)cluster * sizeof(MaxSum));
-                        __syncwarp();
-                        if (lane < cluster)
-                            remote_store(remote_addr(smem_addr(&s_block[turn][rank]), lane), ms.m, ms.s, remote_addr(bar, lane));
-                    }
+                    if (threadIdx.x == 0) mbar_expect(bar, (uint32_t)(cluster * warps) * sizeof(MaxSum));
+                    if (lane < cluster)
+                        remote_store(remote_addr(smem_addr(&s_block[turn][rank * warps + warp]), lane), ms.m, ms.s, remote_addr(bar, lane));
                     if (limit != 0 && !mbar_wait(bar, (computed >> 1) & 1, limit)) limit = 0;
-                    ms = (lane & 7) < cluster ? s_block[turn][lane & 7] : MaxSum{-kInf, 0.0f};
-                    ms = join_lanes<8>(ms, c);
-                    if (limit == 0) ms.s = kNan;
+                } else {
+                    if (lane == 0) s_block[turn][warp] = ms;
+                    asm volatile("bar.sync 1, %0;" ::"r"(shape.threads) : "memory");
                 }
+                ms = lane < cluster * warps ? s_block[turn][lane] : MaxSum{-kInf, 0.0f};
+                for (int i = lane + 32; i < cluster * warps; i += 32) ms = join(ms, s_block[turn][i], c);
+                ms = join_lanes(ms, c);
+                if (limit == 0) ms.s = kNan;
                 ++computed;
 
                 // log q = ln 2 (z c - ref) - ln S
                 const bool is_plain = plain(ms.m);
-                const float ref = ms.m * c, log_s = logf(ms.s), inv_s = 1.0f / ms.s;
+                const float ref = ms.m * c, inv_s = 1.0f / ms.s;
                 const auto exponent = [&](float x) { return is_plain ? fmaf(x, c, -ref) : (x - ms.m) * c; };
-                const auto log_q = [&](float x) { return fmaf(exponent(x), 0.693147180559945f, -log_s); };
                 float coef;
                 if (kMode == kDistill) {
-                    if (rank == 0 && warp == 0) {
-                        const float loss = distill_row_loss(a, target_id(buf), target_p(buf), target_logp(buf), target_z(buf), log_q);
-                        if (lane == 0) a.row_loss[row] = loss;
-                    }
                     coef = a.grad_scale * info.weight * a.temperature;
+                    if (threadIdx.x == 0) s_result[buf] = make_float4(ms.m, logf(ms.s), inv_s, coef);
                 } else {
-                    const float logp = log_q(target_z(buf)[0]);
+                    const float logp = fmaf(exponent(target_z(buf)[0]), kLn2, -logf(ms.s));
                     float loss, slope;
                     policy_row(a, logp, adv, old_logp, ref_logp, loss, slope);
                     if (rank == 0 && threadIdx.x == 0) {
@@ -644,56 +865,57 @@ __global__ void __launch_bounds__(576, 1) loss_ring_kernel(LossArgs a, RingShape
                         if (a.logp) a.logp[row] = logp;
                     }
                     coef = -a.grad_scale * info.weight * slope * a.inv_temperature;
+                    if (threadIdx.x == 0) s_result[buf] = make_float4(ms.m, 0.0f, inv_s, coef);
                 }
 
                 if (kGrad) {
                     // phase 2
                     const float scaled = coef * inv_s;
-                    uint32_t s2 = slot0;
                     T *out = g + p.head + (int64_t)p.from * E;
-                    const auto one = [&](uint32_t at, int i) {
-                        const Vals<E> e = exponentials<E>(widen16<T>(lds16(at)), ms.m, ref, is_plain, c) * scaled;
-                        if (same_offset) {
-                            reinterpret_cast<uint4 *>(out)[i] = narrow16<T>(e);
-                        } else {
-                            float f[E];
-                            e.get(f);
+                    const auto write_chunks = [&](auto plain_row, auto vectors) {
+                        const auto put = [&](const uint4 &q, int i) {
+                            const Vals<E> e = exponentials<decltype(plain_row)::value>(widen16<T>(q), ms.m, ref, c) * scaled;
+                            if constexpr (decltype(vectors)::value) {
+                                reinterpret_cast<uint4 *>(out)[i] = narrow16<T>(e);
+                            } else {
+                                float f[E];
+                                e.get(f);
 #pragma unroll
-                            for (int k = 0; k < E; ++k) out[(int64_t)i * E + k] = from_f32<T>(f[k]);
+                                for (int k = 0; k < E; ++k) out[(int64_t)i * E + k] = from_f32<T>(f[k]);
+                            }
+                        };
+                        uint32_t s2 = slot0;
+                        for (int v = 0; v < p.mine; v += per_chunk) {
+                            const uint32_t at = ring + s2 * shape.chunk_bytes;
+                            const int i0 = v + (int)threadIdx.x;
+                            if (v + per_chunk <= p.mine) {
+#pragma unroll
+                                for (int u = 0; u < kPerThread; u += kTogether) {
+                                    uint4 q[kTogether];
+#pragma unroll
+                                    for (int i = 0; i < kTogether; ++i) q[i] = lds16(at + (u + i) * vector_step);
+#pragma unroll
+                                    for (int i = 0; i < kTogether; ++i) put(q[i], i0 + (u + i) * shape.threads);
+                                }
+                            } else {
+                                for (int u = 0; i0 + u * shape.threads < p.mine; ++u)
+                                    put(lds16(at + u * vector_step), i0 + u * shape.threads);
+                            }
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(smem_addr(&s_empty[s2]));
+                            if (++s2 == (uint32_t)slots) s2 = 0;
                         }
                     };
-                    for (int v = 0; v < p.mine; v += per_chunk) {
-                        const uint32_t at = smem_addr(s_ring) + s2 * shape.chunk_bytes + threadIdx.x * 16;
-                        const int i0 = v + (int)threadIdx.x, i1 = i0 + shape.threads;
-                        if (i0 < p.mine) one(at, i0);
-                        if (i1 < p.mine) one(at + shape.threads * 16, i1);
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_addr(&s_empty[s2]));
-                        if (++s2 == (uint32_t)slots) s2 = 0;
-                    }
+                    if (is_plain && same_offset) write_chunks(std::true_type{}, std::true_type{});
+                    else if (same_offset) write_chunks(std::false_type{}, std::true_type{});
+                    else if (is_plain) write_chunks(std::true_type{}, std::false_type{});
+                    else write_chunks(std::false_type{}, std::false_type{});
                     if (edge >= 0) g[edge] = from_f32<T>(exp2_fast(exponent(edge_z)) * scaled);
-                    asm volatile("bar.sync 1, %0;" ::"r"(shape.threads) : "memory");
-                    // the targets, by the block that has their element
-                    const int32_t *ids = target_id(buf);
-                    const float *probs = target_p(buf), *zs = target_z(buf);
-                    for (int k = threadIdx.x; k < top_k; k += shape.threads) {
-                        const int32_t id = ids[k];
-                        if (id < 0) continue;
-                        const int v = (id - p.head) / E;
-                        const uint32_t owner_is_me = id < p.head ? rank == 0
-                                                     : v >= p.count ? rank == (uint32_t)cluster - 1
-                                                                    : v >= p.from && v < p.from + p.mine;
-                        if (!owner_is_me) continue;
-                        float prob = 0.0f;
-                        for (int i = 0; i < top_k; ++i)
-                            if (ids[i] == id) prob += probs[i];
-                        g[id] = from_f32<T>(coef * fmaf(exp2_fast(exponent(zs[k])), inv_s, -prob));
-                    }
                 }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&s_target_empty[buf]));
-            if (++buf == 2) buf = 0, row_phase ^= 1;
+            if (++buf == depth) buf = 0, row_phase ^= 1;
         }
     }
     // no block goes while another may still write into its shared memory
@@ -727,35 +949,38 @@ loss_total_kernel(const float *row_loss, const float *weight, int64_t rows, floa
 }
 
 // The ring's shape for `vocab` elements of `es` bytes: false if no cluster holds a row.
-#ifndef L_T
-#define L_T 512
-#endif
 #ifndef L_FILL
 #define L_FILL 70
 #endif
 bool ring_shape(int64_t rows, int64_t vocab, int es, int top_k, bool grad, int sms, RingShape *out)
 {
     const int64_t row_bytes = vocab * es;
-    int threads = L_T;
-    int64_t share_max = 0;
+    int threads = BIGT;
     RingShape r;
-    const size_t targets = (size_t)2 * 16 * top_k;
+    const size_t list = (size_t)16 * ((top_k + 3) & ~3), table = (size_t)4 * table_places(top_k);
+    const int lists = top_k <= 256 ? kMaxDepth : 2;
     const auto fit = [&](int t) {
         r.threads = t;
+        r.depth = t > 256 ? lists : 2;
         r.chunk_bytes = t * 16 * kPerThread;
-        const size_t per_block = (size_t)225 * 1024 * t / 512 - 3 * 1024;
+        const size_t per_block = (size_t)224 * 1024 / (t > 256 ? 1 : 512 / t) - 5 * 1024, targets = (list + table) * r.depth;
         if (per_block < targets + 2 * (size_t)r.chunk_bytes) return false;
         r.slots = (int)((per_block - targets) / r.chunk_bytes);
         if (r.slots > kMaxSlots) r.slots = kMaxSlots;
         r.smem = (size_t)r.slots * r.chunk_bytes + targets;
-        share_max = (int64_t)r.slots * r.chunk_bytes;
         return true;
     };
-    // short rows: fewer threads each, more blocks per SM
-    while (threads > 64 && row_bytes < (int64_t)threads * 16 * kPerThread) threads /= 2;
+    // two blocks of 256 threads an SM where each holds whole rows: what one waits for, the
+    // other hides; and fewer threads for short rows
+    if (grad ? fit(256) && (row_bytes + r.chunk_bytes - 1) / r.chunk_bytes <= r.slots : row_bytes < 64 * 1024) threads = 256;
+    while (threads <= 256 && threads > 64 && row_bytes < (int64_t)threads * 64) threads /= 2;
     while (!fit(threads)) {
-        if (threads >= 512) return false;
-        threads *= 2;
+        if (threads >= 256) {
+            if (threads == BIGT) return false;
+            threads = BIGT;
+        } else {
+            threads *= 2;
+        }
     }
     r.cluster = 1;
     const auto chunks = [&](int c) { return ((row_bytes / 16 + c - 1) / c * 16 + r.chunk_bytes - 1) / r.chunk_bytes; };
@@ -764,18 +989,20 @@ bool ring_shape(int64_t rows, int64_t vocab, int es, int top_k, bool grad, int s
     if (grad && chunks(r.cluster) > r.slots) return false;
     // few rows: more blocks each, while SMs are idle
     while (r.cluster < kMaxCluster && rows * r.cluster * 2 <= sms && chunks(r.cluster) > 1) r.cluster *= 2;
+    // looking at all rows costs a cluster a few hundred clocks for each 32: little beside long rows
+    r.balance = r.threads >= 256;
     *out = r;
     return true;
 }
 
-constexpr int kMaxShared = 224 * 1024;
+constexpr int kMaxShared = 220 * 1024;
 
-template <typename T, int kMode, bool kGrad>
+template <typename T, int kMode, bool kGrad, bool kBig>
 so_status launch_ring(const LossArgs &a, const RingShape &shape, int sms, cudaStream_t st)
 {
     struct Known { std::atomic<uint64_t> key; std::atomic<int> clusters; };
     static Known cache[kMaxDevices];
-    const auto kernel = loss_ring_kernel<T, kMode, kGrad>;
+    const auto kernel = loss_ring_kernel<T, kMode, kGrad, kBig>;
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return SO_ERR_CUDA;
     if (dev < 0 || dev >= kMaxDevices) return SO_ERR_UNSUPPORTED;
@@ -784,7 +1011,7 @@ so_status launch_ring(const LossArgs &a, const RingShape &shape, int sms, cudaSt
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)shape.cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.blockDim = dim3((unsigned)shape.threads + 64);
+    cfg.blockDim = dim3((unsigned)(shape.threads + 32 * (2 + shape.depth)));
     cfg.dynamicSmemBytes = shape.smem;
     cfg.stream = st;
     cfg.attrs = attr;
@@ -811,7 +1038,11 @@ so_status launch_loss(const LossArgs &a, int sms, cudaStream_t st)
 {
     RingShape shape;
     if (ring_shape(a.rows, a.vocab, (int)sizeof(T), kMode == kDistill ? a.top_k : 1, a.grad != nullptr, sms, &shape))
-        return a.grad ? launch_ring<T, kMode, true>(a, shape, sms, st) : launch_ring<T, kMode, false>(a, shape, sms, st);
+    {
+        if (shape.threads > 256)
+            return a.grad ? launch_ring<T, kMode, true, true>(a, shape, sms, st) : launch_ring<T, kMode, false, true>(a, shape, sms, st);
+        return a.grad ? launch_ring<T, kMode, true, false>(a, shape, sms, st) : launch_ring<T, kMode, false, false>(a, shape, sms, st);
+    }
     const unsigned grid = (unsigned)(a.rows < 4 * sms ? a.rows : 4 * sms);
     return launch(loss_two_pass_kernel<T, kMode>, grid, kRowThreads, 0, st, false, a);
 }

@@ -298,8 +298,17 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 // Waits for the phase of the given parity, at most `limit` polls (each of which the
 // hardware may hold for a while); false if it did not complete.
 constexpr uint32_t kPolls = 1u << 20;
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit)
 {
+    if (mbar_test(bar, parity)) return true;
     for (uint32_t i = 0; i < limit; ++i) {
         uint32_t ok;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
