@@ -316,6 +316,10 @@ struct RowInfo {
     float weight;
     int32_t load, live;                   // read the row at all; its loss and gradient are not zero
     int32_t repeats;                      // some id is in its list more than once
+    // its 16-byte part: `head` elements before it, then `count` vectors, of which this
+    // block has [from, from + mine)
+    int32_t head, count, from, mine;
+    float advantage, old_logp, ref_logp;
 };
 
 // Places of the table that finds repeated ids: a power of two, at least twice the list; none
@@ -430,10 +434,13 @@ __device__ __forceinline__ Vals<E> exponentials(const Vals<E> &z, float m, float
     return x;
 }
 
-// Running sum of a thread, against a reference that need not be the maximum: it is
-// taken from the first vectors and moved only when something exceeds it by a factor of
-// 2^kSlack, which fp32 holds with ease.  (Were it the maximum, some lane of a warp
-// would move it with almost every vector.)
+// Running sum of a thread, against a reference that need not be the maximum: it is the
+// largest of the first vectors that have a finite element.  What fp32 holds leaves room
+// for elements a factor of 2^127 above it.  Where the row stays at hand, the elements after
+// that are added without a look at their size, and a sum that came out infinite is done
+// again with one; otherwise the reference moves when something exceeds it by a factor of
+// 2^kSlack.  (Were it the maximum, some lane of a warp would move it with almost every
+// vector.)
 constexpr float kSlack = 16.0f;
 
 template <typename T>
@@ -444,6 +451,19 @@ struct Running {
     Vals<E> s;
 
     __device__ __forceinline__ Running() : m(-kInf), ref(0.0f), bound(-kInf), is_plain(false) { s.set(0.0f); }
+
+    // Against the reference as it is, if there is one.  An element that exceeds it by 2^128
+    // or more makes the sum infinite, for the caller to find.
+    template <int N>
+    __device__ __forceinline__ void add_unchecked(const uint4 (&v)[N], float c, float slack)
+    {
+        if (is_plain) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) s = s + exponentials<true>(widen16<T>(v[i]), m, ref, c);
+        } else {
+            add(v, c, slack);
+        }
+    }
 
     template <int N>
     __device__ __forceinline__ void add(const uint4 (&v)[N], float c, float slack)   // slack = kSlack / c
@@ -513,6 +533,9 @@ __device__ void walk_rows(const Wanted &wanted, int64_t rows, int n, int mine, b
 }
 
 // kBig: one block an SM of up to 512 computing threads, else two or more of up to 256
+#ifndef MORE
+#define MORE 1
+#endif
 template <typename T, int kMode, bool kGrad, bool kBig>
 __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ring_kernel(LossArgs a, RingShape shape)
 {
@@ -558,11 +581,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
     else __syncthreads();
     grid_dependency_release();            // the sum over rows may be set up meanwhile
 
-    // a row's 16-byte part: `head` elements before it, then `count` vectors, of which
-    // this block has [from, from + mine)
-    struct Part { int head, count, from, mine; };
-    const auto part_of = [&](int64_t row) {
-        Part p;
+    const auto set_part = [&](RowInfo &p, int64_t row) {
         const uintptr_t at = reinterpret_cast<uintptr_t>(static_cast<const T *>(a.logits) + row * a.stride);
         const int64_t head = (int64_t)(((16u - (unsigned)(at & 15u)) & 15u) / sizeof(T));
         p.head = (int)(head < a.vocab ? head : a.vocab);
@@ -570,7 +589,6 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
         const int per = (p.count + cluster - 1) / cluster;
         p.from = per * (int)rank < p.count ? per * (int)rank : p.count;
         p.mine = p.count - p.from < per ? p.count - p.from : per;
-        return p;
     };
     const auto wanted = [&](int64_t row) {                // is the row read at all
         if (a.weight && a.weight[row] == 0.0f) return false;
@@ -583,7 +601,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
     // the next row of the queue (by the producer and the target warp), -1 at the end
     const auto next_row = [&](uint32_t taken, bool &load) {
         const uint32_t at = taken % kQueue;
-        if (limit != 0 && !mbar_wait(smem_addr(&s_queue_full[at]), (taken / kQueue) & 1, limit)) limit = 0;
+        if (limit != 0 && !mbar_wait_idle(smem_addr(&s_queue_full[at]), (taken / kQueue) & 1, limit)) limit = 0;
         limit = __shfl_sync(0xFFFFFFFFu, limit, 0);
         const int64_t v = limit == 0 ? -1 : s_queue[at];
         __syncwarp();
@@ -597,7 +615,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
         uint32_t given = 0;
         const auto give = [&](int64_t row, uint32_t load) {
             const uint32_t at = given % kQueue;
-            if (limit != 0 && !mbar_wait(smem_addr(&s_queue_empty[at]), ((given / kQueue) & 1) ^ 1, limit)) limit = 0;
+            if (limit != 0 && !mbar_wait_idle(smem_addr(&s_queue_empty[at]), ((given / kQueue) & 1) ^ 1, limit)) limit = 0;
             limit = __shfl_sync(0xFFFFFFFFu, limit, 0);
             if (limit == 0) return false;
             if (lane == 0) {
@@ -617,10 +635,11 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
         uint32_t taken = 0;
         for (int64_t row = next_row(taken++, load); row >= 0; row = next_row(taken++, load)) {
             if (!load) continue;
-            const Part p = part_of(row);
+            RowInfo p;
+            set_part(p, row);
             const T *src = static_cast<const T *>(a.logits) + row * a.stride + p.head + (int64_t)p.from * E;
             for (int v = 0; v < p.mine && limit != 0; v += per_chunk) {
-                if (!mbar_wait(smem_addr(&s_empty[slot]), phase ^ 1, limit)) limit = 0;
+                if (!mbar_wait_idle(smem_addr(&s_empty[slot]), phase ^ 1, limit)) limit = 0;
                 limit = __shfl_sync(0xFFFFFFFFu, limit, 0);
                 if (limit == 0) break;
                 if (lane == 0) {
@@ -640,7 +659,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
         // ---- targets: the lists of rows to come; of the rows that are done, the
         // loss and the gradient at the targets, over what phase 2 wrote there ----
         const auto finish = [&](int buf, uint32_t parity) {
-            if (limit != 0 && !mbar_wait(smem_addr(&s_target_empty[buf]), parity, limit)) limit = 0;
+            if (limit != 0 && !mbar_wait_idle(smem_addr(&s_target_empty[buf]), parity, limit)) limit = 0;
             const RowInfo info = s_info[buf];
             const float4 done = s_result[buf];
             const float c = a.log2e_over_t, ref = done.x * c;
@@ -665,7 +684,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
                 if (lane == 0) a.row_loss[info.row] = loss;
             }
             if (kGrad) {
-                const Part p = part_of(info.row);
+                const RowInfo &p = info;
                 T *g = static_cast<T *>(a.grad) + info.row * a.grad_stride;
                 for (int k = lane; k < top_k; k += 32) {
                     const int32_t id = ids[k];
@@ -736,7 +755,23 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
                 target_p(buf)[0] = 1.0f;
                 target_z(buf)[0] = to_f32(static_cast<const T *>(a.logits)[row * a.stride + token]);
             }
-            if (lane == 0) s_info[buf] = RowInfo{row, row >= 0 && a.weight ? a.weight[row] : 1.0f, row >= 0 && load, live, twice};
+            if (lane == 0) {
+                RowInfo info = {};
+                info.row = row;
+                if (row >= 0) {
+                    info.weight = a.weight ? a.weight[row] : 1.0f;
+                    info.load = load;
+                    info.live = live;
+                    info.repeats = twice;
+                    set_part(info, row);
+                    if (kMode == kPolicy && live) {
+                        info.advantage = a.advantage[row];
+                        info.old_logp = a.old_logp ? a.old_logp[row] : 0.0f;
+                        info.ref_logp = a.ref_logp ? a.ref_logp[row] : 0.0f;
+                    }
+                }
+                s_info[buf] = info;
+            }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&s_target_full[buf]));
             if (row < 0) break;
@@ -745,7 +780,16 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
         // ---- the rest ----
         const float c = a.log2e_over_t, slack = kSlack / c;
         const uint32_t ring = smem_addr(s_ring) + threadIdx.x * 16, vector_step = (uint32_t)shape.threads * 16;
-        uint32_t slot = 0, phase = 0, row_phase = 0, computed = 0;   // rows computed so far: even and odd ones take turns
+        const uint32_t full_bar = smem_addr(s_full), empty_bar = smem_addr(s_empty), ring_bytes = (uint32_t)slots * shape.chunk_bytes;
+        // a chunk of the ring: its bytes, its barriers' offset, and their phase
+        struct Place { uint32_t at, bar, phase; };
+        const auto advance = [&](Place &p) {
+            p.at += shape.chunk_bytes;
+            p.bar += 8;
+            if (p.at == ring_bytes) p = Place{0, 0, p.phase ^ 1};
+        };
+        Place place = {0, 0, 0};
+        uint32_t row_phase = 0, computed = 0;   // rows computed so far: even and odd ones take turns
         int buf = 0;
         while (true) {
             // one warp waits for the row's targets, the others for that warp; all agree
@@ -758,7 +802,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
             const RowInfo info = s_info[buf];
             const int64_t row = info.row;
             if (row < 0) break;
-            const Part p = part_of(row);
+            const RowInfo &p = info;
             const T *z = static_cast<const T *>(a.logits) + row * a.stride;
             T *g = kGrad ? static_cast<T *>(a.grad) + row * a.grad_stride : nullptr;
             const bool same_offset = kGrad && ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
@@ -771,11 +815,11 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
             if (!info.live) {
                 // nothing to compute: a chunk that is on its way is let go, the gradient is zero
                 if (info.load)
-                    for (int v = 0; v < p.mine; v += per_chunk) {
-                        if (limit != 0 && !mbar_wait(smem_addr(&s_full[slot]), phase, limit)) limit = 0;
+                    for (int left = p.mine; left > 0; left -= per_chunk) {
+                        if (limit != 0 && !mbar_wait(full_bar + place.bar, place.phase, limit)) limit = 0;
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_addr(&s_empty[slot]));
-                        if (++slot == (uint32_t)slots) slot = 0, phase ^= 1;
+                        if (lane == 0) mbar_arrive(empty_bar + place.bar);
+                        advance(place);
                     }
                 if (kGrad) {
                     T *out = g + p.head + (int64_t)p.from * E;
@@ -790,39 +834,49 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
             } else {
                 float edge_z = 0.0f;
                 if (edge >= 0) edge_z = to_f32(z[edge]);
-                float adv = 0.0f, old_logp = 0.0f, ref_logp = 0.0f;
-                if (kMode == kPolicy) {
-                    adv = a.advantage[row];
-                    if (a.old_logp) old_logp = a.old_logp[row];
-                    if (a.ref_logp) ref_logp = a.ref_logp[row];
-                }
                 // phase 1
-                const uint32_t slot0 = slot;
+                const Place place0 = place;
                 Running<T> run;
-                for (int v = 0; v < p.mine; v += per_chunk) {
-                    if (limit != 0 && !mbar_wait(smem_addr(&s_full[slot]), phase, limit)) limit = 0;
-                    const uint32_t at = ring + slot * shape.chunk_bytes;
-                    if (v + per_chunk <= p.mine) {
+                for (int left = p.mine; left > 0; left -= per_chunk) {
+                    if (!mbar_test(full_bar + place.bar, place.phase) && limit != 0 &&
+                        !mbar_wait(full_bar + place.bar, place.phase, limit))
+                        limit = 0;
+                    const uint32_t at = ring + place.at;
+                    if (left >= per_chunk) {
 #pragma unroll
                         for (int u = 0; u < kPerThread; u += kTogether) {
                             uint4 q[kTogether];
 #pragma unroll
                             for (int i = 0; i < kTogether; ++i) q[i] = lds16(at + (u + i) * vector_step);
-                            run.add(q, c, slack);
+                            if constexpr (kGrad) run.add_unchecked(q, c, slack);
+                            else run.add(q, c, slack);
                         }
                     } else {
-                        for (int u = 0; v + u * shape.threads + (int)threadIdx.x < p.mine; ++u) {
+                        for (int i = threadIdx.x, u = 0; i < left; i += shape.threads, ++u) {
                             const uint4 q[1] = {lds16(at + u * vector_step)};
                             run.add(q, c, slack);
                         }
                     }
                     if (!kGrad) {
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_addr(&s_empty[slot]));
+                        if (lane == 0) mbar_arrive(empty_bar + place.bar);
                     }
-                    if (++slot == (uint32_t)slots) slot = 0, phase ^= 1;
+                    advance(place);
                 }
                 MaxSum ms{run.m, total(run.s)};
+                if (kGrad && !(ms.s < kInf)) {
+                    // once more, with a look at every vector's largest element
+                    run = Running<T>();
+                    Place there = place0;
+                    for (int left = p.mine; left > 0; left -= per_chunk) {
+                        for (int i = threadIdx.x, u = 0; i < left && u < kPerThread; i += shape.threads, ++u) {
+                            const uint4 q[1] = {lds16(ring + there.at + u * vector_step)};
+                            run.add(q, c, slack);
+                        }
+                        advance(there);
+                    }
+                    ms = MaxSum{run.m, total(run.s)};
+                }
                 if (edge >= 0) {
                     // exp2 of its exponent against its own reference: 1 but for the rounding of that
                     const float own = plain(edge_z) ? exp2_fast(fmaf(edge_z, c, -(edge_z * c))) : exp2_fast(edge_z - edge_z);
@@ -859,7 +913,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
                 } else {
                     const float logp = fmaf(exponent(target_z(buf)[0]), kLn2, -logf(ms.s));
                     float loss, slope;
-                    policy_row(a, logp, adv, old_logp, ref_logp, loss, slope);
+                    policy_row(a, logp, info.advantage, info.old_logp, info.ref_logp, loss, slope);
                     if (rank == 0 && threadIdx.x == 0) {
                         a.row_loss[row] = loss;
                         if (a.logp) a.logp[row] = logp;
@@ -873,37 +927,37 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
                     const float scaled = coef * inv_s;
                     T *out = g + p.head + (int64_t)p.from * E;
                     const auto write_chunks = [&](auto plain_row, auto vectors) {
-                        const auto put = [&](const uint4 &q, int i) {
+                        const auto put = [&](const uint4 &q, T *at) {
                             const Vals<E> e = exponentials<decltype(plain_row)::value>(widen16<T>(q), ms.m, ref, c) * scaled;
                             if constexpr (decltype(vectors)::value) {
-                                reinterpret_cast<uint4 *>(out)[i] = narrow16<T>(e);
+                                *reinterpret_cast<uint4 *>(at) = narrow16<T>(e);
                             } else {
                                 float f[E];
                                 e.get(f);
 #pragma unroll
-                                for (int k = 0; k < E; ++k) out[(int64_t)i * E + k] = from_f32<T>(f[k]);
+                                for (int k = 0; k < E; ++k) at[k] = from_f32<T>(f[k]);
                             }
                         };
-                        uint32_t s2 = slot0;
-                        for (int v = 0; v < p.mine; v += per_chunk) {
-                            const uint32_t at = ring + s2 * shape.chunk_bytes;
-                            const int i0 = v + (int)threadIdx.x;
-                            if (v + per_chunk <= p.mine) {
+                        Place there = place0;
+                        T *to = out + (int64_t)threadIdx.x * E;
+                        for (int left = p.mine; left > 0; left -= per_chunk, to += (int64_t)per_chunk * E) {
+                            const uint32_t at = ring + there.at;
+                            if (left >= per_chunk) {
 #pragma unroll
                                 for (int u = 0; u < kPerThread; u += kTogether) {
                                     uint4 q[kTogether];
 #pragma unroll
                                     for (int i = 0; i < kTogether; ++i) q[i] = lds16(at + (u + i) * vector_step);
 #pragma unroll
-                                    for (int i = 0; i < kTogether; ++i) put(q[i], i0 + (u + i) * shape.threads);
+                                    for (int i = 0; i < kTogether; ++i) put(q[i], to + (u + i) * shape.threads * E);
                                 }
                             } else {
-                                for (int u = 0; i0 + u * shape.threads < p.mine; ++u)
-                                    put(lds16(at + u * vector_step), i0 + u * shape.threads);
+                                for (int i = threadIdx.x, u = 0; i < left; i += shape.threads, ++u)
+                                    put(lds16(at + u * vector_step), to + u * shape.threads * E);
                             }
                             __syncwarp();
-                            if (lane == 0) mbar_arrive(smem_addr(&s_empty[s2]));
-                            if (++s2 == (uint32_t)slots) s2 = 0;
+                            if (lane == 0) mbar_arrive(empty_bar + there.bar);
+                            advance(there);
                         }
                     };
                     if (is_plain && same_offset) write_chunks(std::true_type{}, std::true_type{});
@@ -950,7 +1004,7 @@ loss_total_kernel(const float *row_loss, const float *weight, int64_t rows, floa
 
 // The ring's shape for `vocab` elements of `es` bytes: false if no cluster holds a row.
 #ifndef L_FILL
-#define L_FILL 70
+#define L_FILL 100
 #endif
 bool ring_shape(int64_t rows, int64_t vocab, int es, int top_k, bool grad, int sms, RingShape *out)
 {

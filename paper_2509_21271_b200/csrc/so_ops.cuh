@@ -298,6 +298,9 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 // Waits for the phase of the given parity, at most `limit` polls (each of which the
 // hardware may hold for a while); false if it did not complete.
 constexpr uint32_t kPolls = 1u << 20;
+#ifndef IDLE_NS
+#define IDLE_NS 300
+#endif
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
@@ -315,6 +318,17 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
                      "selp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
         if (ok) return true;
+    }
+    return false;
+}
+
+// The same for a warp with nothing else to do while others compute: it sleeps between
+// polls, which otherwise come every 70 clocks or so and take issue slots from them.
+__device__ __forceinline__ bool mbar_wait_idle(uint32_t bar, uint32_t parity, uint32_t limit)
+{
+    for (uint32_t i = 0; i < limit; ++i) {
+        if (mbar_test(bar, parity)) return true;
+        __nanosleep(IDLE_NS);
     }
     return false;
 }
