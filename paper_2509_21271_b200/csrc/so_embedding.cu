@@ -23,7 +23,7 @@ struct LookupArgs {
     float scale;
 };
 
-constexpr int kLookupThreads = 256;
+constexpr int kLookupThreads = 256, kLookupBatch = 8;
 
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(kLookupThreads) embedding_forward_kernel(LookupArgs a)
@@ -36,20 +36,36 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_forward_kernel(Looku
         const bool ok = id >= 0 && id < a.vocab;
         if (!ok && a.bad_id && lane == 0) *a.bad_id = 1;
         const T *row = static_cast<const T *>(a.table) + (ok ? id : 0) * a.table_stride;
+        // loads of a batch before its stores: several are in flight
         if constexpr (kVec) {
             constexpr int E = Vec<T>::kElems;
-            for (int64_t v = lane; v < a.cols / E; v += 32) {
-                float f[E];
-                uint4 raw = make_uint4(0, 0, 0, 0);
-                if (ok) raw = reinterpret_cast<const uint4 *>(row)[v];
-                unpack<T>(raw, f);
+            const int vectors = (int)(a.cols / E);
+            for (int v0 = lane; v0 < vectors; v0 += 32 * kLookupBatch) {
+                uint4 raw[kLookupBatch];
 #pragma unroll
-                for (int i = 0; i < E; ++i) f[i] *= a.scale;
-                reinterpret_cast<uint4 *>(out)[v] = ok ? pack<T>(f) : raw;
+                for (int u = 0; u < kLookupBatch; ++u) {
+                    raw[u] = make_uint4(0, 0, 0, 0);
+                    if (ok && v0 + 32 * u < vectors) raw[u] = __ldg(reinterpret_cast<const uint4 *>(row) + v0 + 32 * u);
+                }
+#pragma unroll
+                for (int u = 0; u < kLookupBatch; ++u)
+                    if (v0 + 32 * u < vectors) {
+                        // streamed out: the table's rows keep their place in L2
+                        __stcs(reinterpret_cast<uint4 *>(out) + v0 + 32 * u,
+                               ok && a.scale != 1.0f ? narrow16<T>(widen16<T>(raw[u]) * a.scale) : raw[u]);
+                    }
             }
         } else {
-            for (int64_t c = lane; c < a.cols; c += 32)
-                out[c] = ok ? from_f32<T>(to_f32(row[c]) * a.scale) : from_f32<T>(0.0f);
+            const int cols = (int)a.cols;
+            for (int c0 = lane; c0 < cols; c0 += 32 * kLookupBatch) {
+                T raw[kLookupBatch];
+#pragma unroll
+                for (int u = 0; u < kLookupBatch; ++u)
+                    raw[u] = ok && c0 + 32 * u < cols ? row[c0 + 32 * u] : from_f32<T>(0.0f);
+#pragma unroll
+                for (int u = 0; u < kLookupBatch; ++u)
+                    if (c0 + 32 * u < cols) out[c0 + 32 * u] = from_f32<T>(to_f32(raw[u]) * (ok ? a.scale : 1.0f));
+            }
         }
     }
 }
