@@ -79,29 +79,31 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_forward_kernel(Looku
 // tokens and keeps counters of its own, so that ranks follow from prefix sums
 // and do not depend on the order of the (integer, shared-memory) additions.
 //
-// The block knows then which of its ids have no token, and writes their zero
-// rows: that is most of the pass's traffic when the table is larger than
-// the batch, and it needs nothing from the sort of the others.
+// A token goes out with all that the sum needs to know of its run, so that a block of
+// the sum has one load to wait for before it reads rows.  Which ids occur at all goes
+// out as bits: the rows of the others are zeroed by further blocks of the sum's launch.
 
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kRange = 1024;              // ids a block owns, at most one per thread
 constexpr int kUnroll = 4;                // token loads in flight per lane
+constexpr int kKeep = 256;                // tokens of its ids that a warp keeps from the count for the placing
 
-// Runs of equal ids are summed by whoever owns the stretch of kChunk sorted
-// positions in which they begin; a run longer than kLong is cut at the
+// Runs of equal ids are summed by whoever owns the stretch of `chunk` sorted positions
+// (16, 32 or 64) in which they begin; a run longer than two stretches is cut at the
 // boundaries of the stretches instead, and the pieces are joined.
-constexpr int kChunk = 32, kLong = 64;
+constexpr int kMinChunk = 16, kMaxChunk = 64;
+
+// A token in sorted order: its position, its id, and where the tokens of that id are.
+struct __align__(16) Sorted { int32_t token, id, start, count; };
 
 struct SortArgs {
     const void *ids;
-    int32_t *order;                       // [n] token positions by (id, position)
-    int32_t *key;                         // [n] their ids
-    int32_t *start;                       // [vocab + 1] where each id's tokens begin
-    uint32_t *arrived;                    // [n / kLong + 1][tiles] pieces of a long run summed so far
-    void *dtable;                         // rows without tokens become zero; nullptr: not wanted
-    int64_t padding_id, dtable_stride, row_bytes;
-    int32_t n, vocab, range, tiles, ids_dtype, grad_size;
-    bool wide;                            // 16-byte stores fit the rows
+    Sorted *sorted;                       // [n] by (id, position)
+    int32_t *total;                       // tokens that take part
+    uint32_t *present;                    // bit per id: it has tokens
+    uint32_t *arrived;                    // [n / (2 chunk) + 1][tiles] pieces of a long run summed so far
+    int64_t padding_id;
+    int32_t n, vocab, range, tiles, chunk, ids_dtype;
 };
 
 __device__ __forceinline__ int32_t usable_id(const SortArgs &a, int32_t t)
@@ -110,28 +112,14 @@ __device__ __forceinline__ int32_t usable_id(const SortArgs &a, int32_t t)
     return (id >= 0 && id < a.vocab && id != a.padding_id) ? (int32_t)id : -1;
 }
 
-__device__ __forceinline__ void zero_row(const SortArgs &a, int64_t v, int lane)
-{
-    char *row = static_cast<char *>(a.dtable) + v * a.dtable_stride * a.grad_size;
-    if (a.wide) {
-        for (int64_t i = lane; i < a.row_bytes / 16; i += 32)
-            __stcs(reinterpret_cast<uint4 *>(row) + i, make_uint4(0, 0, 0, 0));
-    } else if (a.grad_size == 4) {
-        for (int64_t i = lane; i < a.row_bytes / 4; i += 32) reinterpret_cast<uint32_t *>(row)[i] = 0;
-    } else {
-        for (int64_t i = lane; i < a.row_bytes / 2; i += 32) reinterpret_cast<uint16_t *>(row)[i] = 0;
-    }
-}
-
 __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a)
 {
-    extern __shared__ int32_t s_hist[];   // [kSortWarps][range]
-    __shared__ int32_t s_below[kSortWarps], s_scan[kSortWarps], s_zero[kRange], s_zeros;
+    extern __shared__ int32_t s_hist[];   // [kSortWarps][range], then [kSortWarps][kKeep] kept tokens, and ids
+    __shared__ int32_t s_below[kSortWarps], s_scan[kSortWarps], s_first[kRange], s_count[kRange];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int32_t lo = (int32_t)blockIdx.x * a.range;
     const int32_t hi = a.vocab - lo < a.range ? a.vocab : lo + a.range;
     for (int i = threadIdx.x; i < kSortWarps * a.range; i += kSortThreads) s_hist[i] = 0;
-    if (threadIdx.x == 0) s_zeros = 0;
     __syncthreads();
 
     const int32_t per_warp = (int32_t)(((int64_t)a.n + kSortThreads - 1) / kSortThreads) * 32;
@@ -139,15 +127,28 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
     const int32_t t0 = first < a.n ? (int32_t)first : a.n;
     const int32_t t1 = a.n - t0 < per_warp ? a.n : t0 + per_warp;
     int32_t *hist = s_hist + warp * a.range;
-    int32_t below = 0;
-    for (int32_t t = t0 + lane; t < t1; t += 32 * kUnroll) {
+    int32_t *kept_token = s_hist + kSortWarps * a.range + warp * kKeep, *kept_id = kept_token + kSortWarps * kKeep;
+    const uint32_t lower_lanes = (1u << lane) - 1u, width = (uint32_t)(hi - lo);
+    int32_t below = 0, kept = 0;
+    for (int32_t t = t0; t < t1; t += 32 * kUnroll) {
         int32_t id[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) id[u] = t + 32 * u < t1 ? usable_id(a, t + 32 * u) : -1;
+        for (int u = 0; u < kUnroll; ++u) id[u] = t + 32 * u + lane < t1 ? usable_id(a, t + 32 * u + lane) : -1;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            if (id[u] >= 0 && id[u] < lo) ++below;
-            else if (id[u] >= lo && id[u] < hi) atomicAdd(&hist[id[u] - lo], 1);
+            below += (uint32_t)id[u] < (uint32_t)lo;
+            const bool in = (uint32_t)(id[u] - lo) < width && id[u] >= 0;
+            const uint32_t found = __ballot_sync(0xFFFFFFFFu, in);
+            if (found == 0) continue;
+            const int at = kept + __popc(found & lower_lanes);
+            if (in) {
+                atomicAdd(&hist[id[u] - lo], 1);
+                if (at < kKeep) {
+                    kept_token[at] = t + 32 * u + lane;
+                    kept_id[at] = id[u];
+                }
+            }
+            kept += __popc(found);
         }
     }
     for (int o = 16; o > 0; o >>= 1) below += __shfl_xor_sync(0xFFFFFFFFu, below, o);
@@ -165,16 +166,19 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
         if (lane >= o) incl += up;
     }
     if (lane == 31) s_scan[warp] = incl;
-    if (mine && count == 0 && a.dtable) s_zero[atomicAdd(&s_zeros, 1)] = lo + (int32_t)threadIdx.x;
+    // ranges are multiples of 32: a warp's ids are one word of the bits
+    const uint32_t bits = __ballot_sync(0xFFFFFFFFu, mine && count > 0);
+    if (lane == 0 && lo + warp * 32 < hi) a.present[(lo >> 5) + warp] = bits;
     __syncthreads();
     int32_t base = 0;
     for (int w = 0; w < kSortWarps; ++w) base += s_below[w] + (w < warp ? s_scan[w] : 0);
     int32_t at = base + incl - count;
     if (mine) {
-        a.start[lo + threadIdx.x] = at;
-        if (lo + (int32_t)threadIdx.x == a.vocab - 1) a.start[a.vocab] = at + count;
-        if (count > kLong)                // two long runs never begin in the same kLong positions
-            for (int i = 0; i < a.tiles; ++i) a.arrived[(int64_t)(at / kLong) * a.tiles + i] = 0;
+        s_first[threadIdx.x] = at;
+        s_count[threadIdx.x] = count;
+        if (lo + (int32_t)threadIdx.x == a.vocab - 1) *a.total = at + count;
+        if (count > 2 * a.chunk)          // two long runs never begin in the same 2 chunk positions
+            for (int i = 0; i < a.tiles; ++i) a.arrived[(int64_t)(at / (2 * a.chunk)) * a.tiles + i] = 0;
         for (int w = 0; w < kSortWarps; ++w) {
             const int32_t c = s_hist[w * a.range + threadIdx.x];
             s_hist[w * a.range + threadIdx.x] = at;
@@ -183,66 +187,110 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
     }
     __syncthreads();
 
+    // 32 tokens in order: those of one id follow each other
+    const auto place = [&](int32_t token, int32_t id, bool in) {
+        const unsigned active = __ballot_sync(0xFFFFFFFFu, in);
+        if (in) {
+            const unsigned same = __match_any_sync(active, id);
+            const int rank = __popc(same & lower_lanes);
+            const int32_t pos = hist[id - lo];
+            __syncwarp(active);
+            if (rank == 0) hist[id - lo] = pos + __popc(same);
+            a.sorted[pos + rank] = Sorted{token, id, s_first[id - lo], s_count[id - lo]};
+        }
+        __syncwarp();
+    };
+    if (kept <= kKeep) {
+        for (int32_t i = 0; i < kept; i += 32) {
+            const bool in = i + lane < kept;
+            place(in ? kept_token[i + lane] : 0, in ? kept_id[i + lane] : lo, in);
+        }
+        return;
+    }
     for (int32_t t = t0; t < t1; t += 32 * kUnroll) {
         int32_t id[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int32_t i = t + 32 * u + lane;
-            id[u] = i < t1 ? usable_id(a, i) : -1;
-        }
+        for (int u = 0; u < kUnroll; ++u) id[u] = t + 32 * u + lane < t1 ? usable_id(a, t + 32 * u + lane) : -1;
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const bool in = id[u] >= lo && id[u] < hi;
-            const unsigned active = __ballot_sync(0xFFFFFFFFu, in);
-            if (in) {
-                const unsigned same = __match_any_sync(active, id[u]);
-                const int rank = __popc(same & ((1u << lane) - 1u));
-                const int32_t pos = hist[id[u] - lo];
-                __syncwarp(active);
-                if (rank == 0) hist[id[u] - lo] = pos + __popc(same);
-                a.order[pos + rank] = t + 32 * u + lane;
-                a.key[pos + rank] = id[u];
-            }
-            __syncwarp();
-        }
+        for (int u = 0; u < kUnroll; ++u) place(t + 32 * u + lane, id[u], id[u] >= lo && id[u] < hi);
     }
-    const int32_t zeros = s_zeros;
-    for (int32_t i = warp; i < zeros; i += kSortWarps) zero_row(a, s_zero[i], lane);
 }
 
 // ---- sums over runs of equal ids ------------------------------------------------
 //
-// A block takes one stretch of kChunk sorted positions and one tile of columns
+// A block takes one stretch of sorted positions and one tile of columns
 // (one vector per thread).  It sums the runs that begin in the stretch, in order,
 // kBatch rows in flight; of a long run it sums the piece inside the stretch into
 // fp32 scratch, and the last block to finish a piece of that run adds the
 // pieces in their order (which block that is does not show in the result).
 
 constexpr int kSumThreads = 256, kBatch = 8;
+constexpr int kStrided = 4;               // columns of a thread where rows are not aligned
+constexpr int kZeroRows = 64;             // ids that a block of the zeroing looks at
 
 struct SumArgs {
     const void *dout;
-    const int32_t *order, *key, *start;
+    const Sorted *sorted;
+    const int32_t *total;
+    const uint32_t *present;
     uint32_t *arrived;
     float *pieces;                        // [chunks][2][cols]: of a run that began before, of one that begins here
     void *dtable;
     int64_t vocab, cols, dout_stride, dtable_stride;
-    int32_t tiles, grad_dtype, accumulate;
+    int32_t tiles, sum_blocks, chunk, grad_dtype, accumulate;
+    bool wide;                            // 16-byte stores fit the rows
     float scale;
 };
 
-template <int E>
-__device__ __forceinline__ void write_row(const SumArgs &a, int64_t id, int64_t col, const float (&sum)[E])
+// The rows of ids [64 block, ...) that have no token become zero, a warp at a time.
+__device__ __forceinline__ void zero_rows(const SumArgs &a, int64_t block)
 {
-    const int64_t at = id * a.dtable_stride + col;
+    const int lane = threadIdx.x & 31, size = a.grad_dtype == SO_DTYPE_FP32 ? 4 : 2;
+    const int64_t row_bytes = a.cols * size;
+    for (int i = threadIdx.x >> 5; i < kZeroRows; i += blockDim.x >> 5) {
+        const int64_t v = block * kZeroRows + i;
+        if (v >= a.vocab) return;
+        if ((a.present[v >> 5] >> (v & 31)) & 1u) continue;
+        char *row = static_cast<char *>(a.dtable) + v * a.dtable_stride * size;
+        if (a.wide) {
+            for (int64_t j = lane; j < row_bytes / 16; j += 32) __stcs(reinterpret_cast<uint4 *>(row) + j, make_uint4(0, 0, 0, 0));
+        } else if (size == 4) {
+            for (int64_t j = lane; j < a.cols; j += 32) reinterpret_cast<uint32_t *>(row)[j] = 0;
+        } else {
+            for (int64_t j = lane; j < a.cols; j += 32) reinterpret_cast<uint16_t *>(row)[j] = 0;
+        }
+    }
+}
+
+// A thread's E columns: a vector of them, or (kVec false) one in every blockDim.x, for rows
+// that are not aligned.
+template <int E, bool kVec>
+struct Columns {
+    int64_t first;
+    int32_t step, count;                  // between them, and how many there are
+    __device__ Columns(int tile, int64_t cols)
+    {
+        first = (int64_t)tile * blockDim.x * E + (int64_t)threadIdx.x * (kVec ? E : 1);
+        step = kVec ? 1 : (int)blockDim.x;
+        const int64_t left = cols - first;
+        count = left <= 0 ? 0 : kVec ? E : (int)((left + step - 1) / step < E ? (left + step - 1) / step : E);
+    }
+};
+
+template <int E, bool kVec>
+__device__ __forceinline__ void write_row(const SumArgs &a, int64_t id, const Columns<E, kVec> &c, const float (&sum)[E])
+{
+    const int64_t at = id * a.dtable_stride + c.first;
     float f[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
         f[i] = sum[i] * a.scale;
-        if (a.accumulate) f[i] += load_any(a.dtable, at + i, a.grad_dtype);
+        if (a.accumulate && i < c.count) f[i] += load_any(a.dtable, at + i * c.step, a.grad_dtype);
     }
-    if constexpr (E == 1) {
-        store_any(a.dtable, at, a.grad_dtype, f[0]);
+    if constexpr (!kVec) {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (i < c.count) store_any(a.dtable, at + i * c.step, a.grad_dtype, f[i]);
     } else if (a.grad_dtype == SO_DTYPE_FP32) {
         float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(a.dtable) + at);
 #pragma unroll
@@ -257,73 +305,107 @@ __device__ __forceinline__ void write_row(const SumArgs &a, int64_t id, int64_t 
     }
 }
 
-template <typename T, int E>               // E columns a thread: 16 bytes of T, or 1
+template <int E, bool kVec>
+__device__ __forceinline__ void store_piece(float *piece, const Columns<E, kVec> &c, const float (&sum)[E])
+{
+    if constexpr (kVec) {
+#pragma unroll
+        for (int e = 0; e < E; e += 4)
+            *reinterpret_cast<float4 *>(piece + c.first + e) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < c.count) piece[c.first + e * c.step] = sum[e];
+    }
+}
+
+template <int E, bool kVec>
+__device__ __forceinline__ void load_piece(const float *piece, const Columns<E, kVec> &c, float (&f)[E])
+{
+    if constexpr (kVec) {
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+            const float4 q = __ldcg(reinterpret_cast<const float4 *>(piece + c.first + e));
+            f[e] = q.x; f[e + 1] = q.y; f[e + 2] = q.z; f[e + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[e] = e < c.count ? __ldcg(piece + c.first + e * c.step) : 0.0f;
+    }
+}
+
+template <typename T, int E, bool kVec>
 __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(SumArgs a)
 {
-    __shared__ int32_t s_order[kChunk + kLong], s_key[kChunk + kLong + 1];
+    __shared__ int32_t s_order[3 * kMaxChunk], s_key[3 * kMaxChunk + 1];
     __shared__ uint32_t s_last;
     grid_dependency_wait();
+    if ((int32_t)blockIdx.x >= a.sum_blocks) {
+        zero_rows(a, (int64_t)blockIdx.x - a.sum_blocks);
+        return;
+    }
     const int32_t chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
-    const int32_t total = a.start[a.vocab], p0 = chunk * kChunk;
+    const int32_t total = *a.total, p0 = chunk * a.chunk;
+    const int32_t p1 = total - p0 < a.chunk ? total : p0 + a.chunk;
+    // looked at before they are known to be there: the array has room for whole chunks
+    const Sorted first = a.sorted[p0], last = a.sorted[p1 > p0 ? p1 - 1 : p0];
     if (p0 >= total) return;
-    const int32_t p1 = total - p0 < kChunk ? total : p0 + kChunk;
-    const int32_t first_id = a.key[p0], last_id = a.key[p1 - 1];
-    const int32_t first_start = a.start[first_id], first_end = a.start[first_id + 1];
-    const int32_t last_start = a.start[last_id], last_end = a.start[last_id + 1];
-    const bool first_long = first_end - first_start > kLong, last_long = last_end - last_start > kLong;
+    const int32_t first_id = first.id, last_id = last.id;
+    const int32_t first_start = first.start, first_end = first.start + first.count;
+    const int32_t last_start = last.start, last_end = last.start + last.count;
+    const bool first_long = first.count > 2 * a.chunk, last_long = last.count > 2 * a.chunk;
     // a short run that began before belongs to another block; one that begins here is finished here
     const int32_t begin = first_start < p0 && !first_long ? first_end : p0;
     const int32_t end = last_long ? p1 : last_end;
     if (begin >= p1) return;
     for (int32_t i = threadIdx.x; i < end - begin; i += blockDim.x) {
-        s_order[i] = a.order[begin + i];
-        s_key[i] = a.key[begin + i];
+        const Sorted q = a.sorted[begin + i];
+        s_order[i] = q.token;
+        s_key[i] = q.id;
     }
     if (threadIdx.x == 0) s_key[end - begin] = -1;
     __syncthreads();
 
-    const int64_t col = ((int64_t)tile * blockDim.x + threadIdx.x) * E;
-    const bool on = col < a.cols;
-    const T *dout = static_cast<const T *>(a.dout) + (on ? col : 0);
-    float *head = a.pieces + (int64_t)chunk * 2 * a.cols + col, *tail = head + a.cols;
+    const Columns<E, kVec> c(tile, a.cols);
+    const T *dout = static_cast<const T *>(a.dout) + (c.count ? c.first : 0);
+    float *head = a.pieces + (int64_t)chunk * 2 * a.cols, *tail = head + a.cols;
     const int32_t count = end - begin;
     float sum[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-    if (on) {
+    if (c.count) {
         for (int32_t i = 0; i < count; i += kBatch) {
-            uint4 raw[E > 1 ? kBatch : 1];
-            T one[E > 1 ? 1 : kBatch];
+            uint4 raw[kVec ? kBatch : 1];
+            T one[kVec ? 1 : kBatch][kVec ? 1 : E];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u)
                 if (i + u < count) {
                     const T *src = dout + (int64_t)s_order[i + u] * a.dout_stride;
-                    if constexpr (E > 1) raw[u] = __ldcs(reinterpret_cast<const uint4 *>(src));
-                    else one[u] = *src;
+                    if constexpr (kVec) {
+                        raw[u] = __ldcs(reinterpret_cast<const uint4 *>(src));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (e < c.count) one[u][e] = src[e * c.step];
+                    }
                 }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 if (i + u >= count) break;
                 float f[E];
-                if constexpr (E > 1) unpack<T>(raw[u], f);
-                else f[0] = to_f32(one[u]);
+                if constexpr (kVec) {
+                    unpack<T>(raw[u], f);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) f[e] = e < c.count ? to_f32(one[u][e]) : 0.0f;
+                }
 #pragma unroll
                 for (int e = 0; e < E; ++e) sum[e] += f[e];
                 const int32_t id = s_key[i + u];
                 if (s_key[i + u + 1] == id) continue;
                 const bool from_before = first_long && id == first_id && first_start < p0;
-                if (from_before || (last_long && id == last_id)) {
-                    float *piece = from_before ? head : tail;
-                    if constexpr (E > 1) {
-#pragma unroll
-                        for (int e = 0; e < E; e += 4)
-                            *reinterpret_cast<float4 *>(piece + e) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
-                    } else {
-                        *piece = sum[0];
-                    }
-                } else {
-                    write_row<E>(a, id, col, sum);
-                }
+                if (from_before || (last_long && id == last_id)) store_piece(from_before ? head : tail, c, sum);
+                else write_row(a, id, c, sum);
 #pragma unroll
                 for (int e = 0; e < E; ++e) sum[e] = 0.0f;
             }
@@ -335,63 +417,50 @@ __global__ void __launch_bounds__(kSumThreads) embedding_sum_kernel(SumArgs a)
         if (which == 0 ? !(first_long && first_start < p0) : !(last_long && last_start >= p0)) continue;
         const int32_t id = which == 0 ? first_id : last_id;
         const int32_t s0 = which == 0 ? first_start : last_start, s1 = which == 0 ? first_end : last_end;
-        const int32_t c0 = s0 / kChunk, c1 = (s1 - 1) / kChunk;
+        const int32_t c0 = s0 / a.chunk, c1 = (s1 - 1) / a.chunk;
         __threadfence();
         __syncthreads();
-        if (threadIdx.x == 0) s_last = atomicAdd(&a.arrived[(int64_t)(s0 / kLong) * a.tiles + tile], 1u);
+        if (threadIdx.x == 0) s_last = atomicAdd(&a.arrived[(int64_t)(s0 / (2 * a.chunk)) * a.tiles + tile], 1u);
         __syncthreads();
         if (s_last != (uint32_t)(c1 - c0)) continue;
         __threadfence();
-        if (!on) continue;
+        if (!c.count) continue;
         // the tail of the first stretch, then the heads of the others
-        const float *piece = a.pieces + ((int64_t)c0 * 2 + 1) * a.cols + col;
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] = __ldcg(piece + e);
+        const float *piece = a.pieces + ((int64_t)c0 * 2 + 1) * a.cols;
+        load_piece(piece, c, sum);
         piece += a.cols;
-        for (int32_t c = c0 + 1; c <= c1; c += kBatch) {
+        for (int32_t k = c0 + 1; k <= c1; k += kBatch) {
             float f[kBatch][E];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u)
-                if (c + u <= c1) {
-                    const float *src = piece + (int64_t)(c + u - c0 - 1) * 2 * a.cols;
-                    if constexpr (E > 1) {
-#pragma unroll
-                        for (int e = 0; e < E; e += 4) {
-                            const float4 q = __ldcg(reinterpret_cast<const float4 *>(src + e));
-                            f[u][e] = q.x; f[u][e + 1] = q.y; f[u][e + 2] = q.z; f[u][e + 3] = q.w;
-                        }
-                    } else {
-                        f[u][0] = __ldcg(src);
-                    }
-                }
+                if (k + u <= c1) load_piece(piece + (int64_t)(k + u - c0 - 1) * 2 * a.cols, c, f[u]);
 #pragma unroll
             for (int u = 0; u < kBatch; ++u)
-                if (c + u <= c1)
+                if (k + u <= c1)
 #pragma unroll
                     for (int e = 0; e < E; ++e) sum[e] += f[u][e];
         }
-        write_row<E>(a, id, col, sum);
+        write_row(a, id, c, sum);
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = 0.0f;
     }
 }
 
-// Scratch: order, key [n], start [vocab + 1], arrived [n / kLong + 1][tiles],
-// pieces [ceil(n / kChunk)][2][cols], each rounded up to 16 bytes.  A tile is at
-// least 32 columns.
+// Scratch: sorted [n], total, present [vocab / 32], arrived, pieces, at their sizes for the
+// shortest stretches, each rounded up to 16 bytes.  A tile is at least 32 columns.
 uint64_t round16(uint64_t b) { return (b + 15) & ~uint64_t(15); }
 
 struct Scratch {
-    uint64_t order, key, start, arrived, pieces, bytes;
+    uint64_t sorted, total, present, arrived, pieces, bytes;
     Scratch(int64_t n, int64_t vocab, int64_t cols)
     {
-        const uint64_t tiles = ((uint64_t)cols + 31) / 32;
-        order = 0;
-        key = order + round16((uint64_t)n * 4);
-        start = key + round16((uint64_t)n * 4);
-        arrived = start + round16(((uint64_t)vocab + 1) * 4);
-        pieces = arrived + round16(((uint64_t)n / kLong + 1) * tiles * 4);
-        bytes = pieces + round16(((uint64_t)n + kChunk - 1) / kChunk * 2 * (uint64_t)cols * 4);
+        const uint64_t tiles = ((uint64_t)cols + 31) / 32, chunks = ((uint64_t)n + kMinChunk - 1) / kMinChunk;
+        sorted = 0;
+        total = sorted + ((uint64_t)n + kMaxChunk) * sizeof(Sorted);
+        present = total + 16;
+        arrived = present + round16(((uint64_t)vocab + 31) / 32 * 4);
+        pieces = arrived + round16(((uint64_t)n / (2 * kMinChunk) + 1) * tiles * 4);
+        bytes = pieces + round16(chunks * 2 * (uint64_t)cols * 4);
     }
 };
 
@@ -403,19 +472,19 @@ so_status sort_tokens(const SortArgs &a, cudaStream_t st)
     if (dev < 0 || dev >= kMaxDevices) return SO_ERR_UNSUPPORTED;
     if (!ready[dev].load(std::memory_order_acquire)) {
         if (cudaFuncSetAttribute(embedding_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kSortWarps * kRange * (int)sizeof(int32_t)) != cudaSuccess)
+                                 kSortWarps * (kRange + 2 * kKeep) * (int)sizeof(int32_t)) != cudaSuccess)
             return SO_ERR_CUDA;
         ready[dev].store(true, std::memory_order_release);
     }
     const unsigned grid = (unsigned)((a.vocab + a.range - 1) / a.range);
-    return launch(embedding_sort_kernel, grid, kSortThreads, (size_t)kSortWarps * a.range * sizeof(int32_t), st, false, a);
+    return launch(embedding_sort_kernel, grid, kSortThreads, (size_t)kSortWarps * (a.range + 2 * kKeep) * sizeof(int32_t), st, false, a);
 }
 
 template <typename T>
 so_status sum_runs(const SumArgs &a, bool vec, unsigned grid, unsigned threads, cudaStream_t st)
 {
-    return vec ? launch(embedding_sum_kernel<T, Vec<T>::kElems>, grid, threads, 0, st, true, a)
-               : launch(embedding_sum_kernel<T, 1>, grid, threads, 0, st, true, a);
+    return vec ? launch(embedding_sum_kernel<T, Vec<T>::kElems, true>, grid, threads, 0, st, true, a)
+               : launch(embedding_sum_kernel<T, kStrided, false>, grid, threads, 0, st, true, a);
 }
 
 }  // namespace
@@ -497,31 +566,36 @@ so_status so_embedding_backward(const void *ids, int32_t ids_dtype, int64_t n, c
     // a vector of dout per thread, if whole rows of both sides allow it
     const bool vec = aligned(dout, 16) && (dout_stride * es) % 16 == 0 && (cols * es) % 16 == 0 && aligned(dtable, 16) &&
                      (dtable_stride * gs) % 16 == 0 && (cols * gs) % 16 == 0;
-    const int64_t lanes = vec ? cols * es / 16 : cols;
+    const int64_t lanes = vec ? cols * es / 16 : (cols + kStrided - 1) / kStrided;
     const unsigned threads = lanes < kSumThreads ? (unsigned)((lanes + 31) / 32 * 32) : kSumThreads;
-    const int64_t tiles = (lanes + threads - 1) / threads, chunks = (n + kChunk - 1) / kChunk;
-    if (chunks * tiles > INT32_MAX) return SO_ERR_TOO_LARGE;
+    const int64_t tiles = (lanes + threads - 1) / threads;
+    // short stretches spread few tokens over the SMs, long ones spend less on finding out
+    // what to do: the longest with eight blocks an SM
+    int chunk = kMinChunk;
+    while (chunk < kMaxChunk && n / (2 * chunk) * tiles >= (int64_t)8 * sms) chunk *= 2;
+    const int64_t chunks = (n + chunk - 1) / chunk;
+    const int64_t zero_blocks = accumulate ? 0 : (vocab + kZeroRows - 1) / kZeroRows;
+    if (chunks * tiles + zero_blocks > INT32_MAX) return SO_ERR_TOO_LARGE;
     char *ws = static_cast<char *>(scratch);
     const Scratch at(n, vocab, cols);
 
     SortArgs k = {};
-    k.ids = ids; k.order = reinterpret_cast<int32_t *>(ws + at.order); k.key = reinterpret_cast<int32_t *>(ws + at.key);
-    k.start = reinterpret_cast<int32_t *>(ws + at.start); k.arrived = reinterpret_cast<uint32_t *>(ws + at.arrived);
-    k.dtable = accumulate ? nullptr : dtable; k.padding_id = padding_id; k.dtable_stride = dtable_stride;
-    k.row_bytes = cols * gs; k.n = (int32_t)n; k.vocab = (int32_t)vocab; k.tiles = (int32_t)tiles;
-    k.ids_dtype = ids_dtype; k.grad_size = gs;
-    k.wide = aligned(dtable, 16) && (dtable_stride * gs) % 16 == 0 && (cols * gs) % 16 == 0;
-    k.range = (int32_t)((vocab + sms - 1) / sms);
+    k.ids = ids; k.sorted = reinterpret_cast<Sorted *>(ws + at.sorted); k.total = reinterpret_cast<int32_t *>(ws + at.total);
+    k.present = reinterpret_cast<uint32_t *>(ws + at.present); k.arrived = reinterpret_cast<uint32_t *>(ws + at.arrived);
+    k.padding_id = padding_id; k.n = (int32_t)n; k.vocab = (int32_t)vocab; k.tiles = (int32_t)tiles; k.chunk = chunk;
+    k.ids_dtype = ids_dtype;
+    k.range = (int32_t)((vocab + sms - 1) / sms + 31) / 32 * 32;
     if (k.range > kRange) k.range = kRange;
     s = sort_tokens(k, st);
-    if (s != SO_OK || n == 0) return s;
+    if (s != SO_OK) return s;
 
     SumArgs a = {};
-    a.dout = dout; a.order = k.order; a.key = k.key; a.start = k.start; a.arrived = k.arrived;
+    a.dout = dout; a.sorted = k.sorted; a.total = k.total; a.present = k.present; a.arrived = k.arrived;
     a.pieces = reinterpret_cast<float *>(ws + at.pieces); a.dtable = dtable; a.vocab = vocab; a.cols = cols;
-    a.dout_stride = dout_stride; a.dtable_stride = dtable_stride; a.tiles = (int32_t)tiles;
-    a.grad_dtype = grad_dtype; a.accumulate = accumulate; a.scale = (float)scale;
-    const unsigned grid = (unsigned)(chunks * tiles);
+    a.dout_stride = dout_stride; a.dtable_stride = dtable_stride; a.tiles = (int32_t)tiles; a.chunk = chunk;
+    a.sum_blocks = (int32_t)(chunks * tiles); a.grad_dtype = grad_dtype; a.accumulate = accumulate; a.scale = (float)scale;
+    a.wide = aligned(dtable, 16) && (dtable_stride * gs) % 16 == 0 && (cols * gs) % 16 == 0;
+    const unsigned grid = (unsigned)(chunks * tiles + zero_blocks);
     if (dtype == SO_DTYPE_BF16) return sum_runs<bf16_t>(a, vec, grid, threads, st);
     if (dtype == SO_DTYPE_FP16) return sum_runs<f16_t>(a, vec, grid, threads, st);
     return sum_runs<float>(a, vec, grid, threads, st);
