@@ -611,7 +611,8 @@ so_status so_embedding_backward(const void *ids, int32_t ids_dtype, int64_t n, c
  *           a row whose teacher entries are all empty
  *   row_loss fp32 [rows], loss fp32 [1]
  * grad_scale carries 1 / (rows averaged over) and, for fp16 gradients, the loss
- * scale.  A logit of -inf has probability 0; a row of nothing else, and one
+ * scale.  Probabilities below 2^-126 come out as 0.  A logit of -inf has
+ * probability 0; a row of nothing else, and one
  * with NaN or +inf in it, has a NaN loss and gradient, which the optimizer's
  * gradient check turns into a skipped iteration.
  */

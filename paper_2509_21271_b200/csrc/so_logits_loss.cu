@@ -286,17 +286,8 @@ __global__ void __launch_bounds__(kRowThreads) loss_two_pass_kernel(LossArgs a)
 // A wait that runs out of polls ends its block's work: the loss comes out as NaN and the
 // gradient is not complete.
 
-#ifndef BIGT
-#define BIGT 512
-#endif
-#ifndef KPT
-#define KPT 2
-#endif
-#ifndef KTOG
-#define KTOG 2
-#endif
-constexpr int kTogether = KTOG;           // of which so many at once
-constexpr int kPerThread = KPT;           // 16-byte vectors of a chunk per thread
+constexpr int kBigThreads = 512;          // that compute, in a block that has an SM to itself
+constexpr int kPerThread = 2;             // 16-byte vectors of a chunk per thread
 constexpr int kMaxSlots = 32;
 constexpr int kMaxCluster = 8;
 constexpr int kMaxDepth = 4;
@@ -365,16 +356,22 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Reference of the exponents in units of log2: z c - ref(m) is the exponent of z.  The
-// same rounded number is used everywhere, so its rounding cancels.  Beyond kPlain
-// the product may overflow and (z - m) c is used instead.
-constexpr float kPlain = 1e38f;
-__device__ __forceinline__ bool plain(float m) { return fabsf(m) <= kPlain; }
+// Reference of the exponents in units of log2: the exponent of z is z c - ref with
+// ref = m c rounded.  The same rounded number is used everywhere, so its rounding
+// cancels.  Beyond kPlain that rounding is not small any more (and the product may
+// overflow), and (z - m) c is used instead.
+constexpr float kPlain = 1048576.0f;
+__device__ __forceinline__ bool plain(float ref) { return fabsf(ref) <= kPlain; }
 
-__device__ __forceinline__ float rescale(float from, float to, float c)   // exp2(ref(from) - ref(to))
+// Factor that takes a sum from one reference to another.
+__device__ __forceinline__ float rescale(float from, float to, float c)
 {
-    if (plain(from) && plain(to)) return exp2_fast(__fsub_rn(from * c, to * c));
-    return exp2_fast((from - to) * c);
+    const float rf = from * c, rt = to * c;
+    if (plain(rf) && plain(rt)) return exp2_fast(rf - rt);
+    float d = (from - to) * c;
+    if (plain(rf)) d -= fmaf(from, c, -rf);
+    if (plain(rt)) d += fmaf(to, c, -rt);
+    return exp2_fast(d);
 }
 
 __device__ __forceinline__ MaxSum join(const MaxSum &a, const MaxSum &b, float c)
@@ -476,7 +473,7 @@ struct Running {
             m = top;
             ref = m * c;
             bound = m + slack;
-            is_plain = plain(m);
+            is_plain = plain(ref);
         }
         if (is_plain) {
 #pragma unroll
@@ -533,11 +530,8 @@ __device__ void walk_rows(const Wanted &wanted, int64_t rows, int n, int mine, b
 }
 
 // kBig: one block an SM of up to 512 computing threads, else two or more of up to 256
-#ifndef MORE
-#define MORE 1
-#endif
 template <typename T, int kMode, bool kGrad, bool kBig>
-__global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ring_kernel(LossArgs a, RingShape shape)
+__global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 384, kBig ? 1 : 2) loss_ring_kernel(LossArgs a, RingShape shape)
 {
     constexpr int E = Vec<T>::kElems;
     extern __shared__ __align__(128) uint8_t s_ring[];   // [slots][chunk], then the targets of `depth` rows and a table
@@ -545,7 +539,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
     __shared__ __align__(8) uint64_t s_target_full[kMaxDepth], s_target_empty[kMaxDepth];
     __shared__ __align__(8) uint64_t s_queue_full[kQueue], s_queue_empty[kQueue];
     __shared__ int64_t s_queue[kQueue];                  // 2 row + (is it read), -1: no more
-    __shared__ __align__(8) MaxSum s_block[2][kMaxCluster * 24];
+    __shared__ __align__(8) MaxSum s_block[2][kMaxCluster * kBigThreads / 32];
     __shared__ RowInfo s_info[kMaxDepth];
     __shared__ float4 s_result[kMaxDepth];               // reference, sum: its logarithm and inverse; the gradient's factor
     const int warps = shape.threads >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -663,7 +657,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
             const RowInfo info = s_info[buf];
             const float4 done = s_result[buf];
             const float c = a.log2e_over_t, ref = done.x * c;
-            const bool is_plain = plain(done.x);
+            const bool is_plain = plain(ref);
             const auto exponent = [&](float z) { return is_plain ? fmaf(z, c, -ref) : (z - done.x) * c; };
             if (limit == 0) {
                 if (rank == 0 && lane == 0) a.row_loss[info.row] = kNan;
@@ -843,14 +837,11 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
                         limit = 0;
                     const uint32_t at = ring + place.at;
                     if (left >= per_chunk) {
+                        uint4 q[kPerThread];
 #pragma unroll
-                        for (int u = 0; u < kPerThread; u += kTogether) {
-                            uint4 q[kTogether];
-#pragma unroll
-                            for (int i = 0; i < kTogether; ++i) q[i] = lds16(at + (u + i) * vector_step);
-                            if constexpr (kGrad) run.add_unchecked(q, c, slack);
-                            else run.add(q, c, slack);
-                        }
+                        for (int i = 0; i < kPerThread; ++i) q[i] = lds16(at + i * vector_step);
+                        if constexpr (kGrad) run.add_unchecked(q, c, slack);
+                        else run.add(q, c, slack);
                     } else {
                         for (int i = threadIdx.x, u = 0; i < left; i += shape.threads, ++u) {
                             const uint4 q[1] = {lds16(at + u * vector_step)};
@@ -879,7 +870,7 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
                 }
                 if (edge >= 0) {
                     // exp2 of its exponent against its own reference: 1 but for the rounding of that
-                    const float own = plain(edge_z) ? exp2_fast(fmaf(edge_z, c, -(edge_z * c))) : exp2_fast(edge_z - edge_z);
+                    const float own = plain(edge_z * c) ? exp2_fast(fmaf(edge_z, c, -(edge_z * c))) : exp2_fast(edge_z - edge_z);
                     ms = join(ms, MaxSum{edge_z, edge_z == -kInf ? 0.0f : own}, c);
                 }
                 ms = join_lanes(ms, c);
@@ -903,8 +894,8 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
                 ++computed;
 
                 // log q = ln 2 (z c - ref) - ln S
-                const bool is_plain = plain(ms.m);
                 const float ref = ms.m * c, inv_s = 1.0f / ms.s;
+                const bool is_plain = plain(ref);
                 const auto exponent = [&](float x) { return is_plain ? fmaf(x, c, -ref) : (x - ms.m) * c; };
                 float coef;
                 if (kMode == kDistill) {
@@ -943,14 +934,11 @@ __global__ void __launch_bounds__(kBig ? BIGT + 192 : 384, kBig ? 1 : 2) loss_ri
                         for (int left = p.mine; left > 0; left -= per_chunk, to += (int64_t)per_chunk * E) {
                             const uint32_t at = ring + there.at;
                             if (left >= per_chunk) {
+                                uint4 q[kPerThread];
 #pragma unroll
-                                for (int u = 0; u < kPerThread; u += kTogether) {
-                                    uint4 q[kTogether];
+                                for (int i = 0; i < kPerThread; ++i) q[i] = lds16(at + i * vector_step);
 #pragma unroll
-                                    for (int i = 0; i < kTogether; ++i) q[i] = lds16(at + (u + i) * vector_step);
-#pragma unroll
-                                    for (int i = 0; i < kTogether; ++i) put(q[i], to + (u + i) * shape.threads * E);
-                                }
+                                for (int i = 0; i < kPerThread; ++i) put(q[i], to + i * shape.threads * E);
                             } else {
                                 for (int i = threadIdx.x, u = 0; i < left; i += shape.threads, ++u)
                                     put(lds16(at + u * vector_step), to + u * shape.threads * E);
@@ -1003,13 +991,10 @@ loss_total_kernel(const float *row_loss, const float *weight, int64_t rows, floa
 }
 
 // The ring's shape for `vocab` elements of `es` bytes: false if no cluster holds a row.
-#ifndef L_FILL
-#define L_FILL 100
-#endif
 bool ring_shape(int64_t rows, int64_t vocab, int es, int top_k, bool grad, int sms, RingShape *out)
 {
     const int64_t row_bytes = vocab * es;
-    int threads = BIGT;
+    int threads = kBigThreads;
     RingShape r;
     const size_t list = (size_t)16 * ((top_k + 3) & ~3), table = (size_t)4 * table_places(top_k);
     const int lists = top_k <= 256 ? kMaxDepth : 2;
@@ -1030,8 +1015,8 @@ bool ring_shape(int64_t rows, int64_t vocab, int es, int top_k, bool grad, int s
     while (threads <= 256 && threads > 64 && row_bytes < (int64_t)threads * 64) threads /= 2;
     while (!fit(threads)) {
         if (threads >= 256) {
-            if (threads == BIGT) return false;
-            threads = BIGT;
+            if (threads == kBigThreads) return false;
+            threads = kBigThreads;
         } else {
             threads *= 2;
         }
@@ -1039,7 +1024,7 @@ bool ring_shape(int64_t rows, int64_t vocab, int es, int top_k, bool grad, int s
     r.cluster = 1;
     const auto chunks = [&](int c) { return ((row_bytes / 16 + c - 1) / c * 16 + r.chunk_bytes - 1) / r.chunk_bytes; };
     if (grad)
-        while (r.cluster < kMaxCluster && chunks(r.cluster) * 100 > (int64_t)r.slots * L_FILL) r.cluster *= 2;
+        while (r.cluster < kMaxCluster && chunks(r.cluster) > r.slots) r.cluster *= 2;
     if (grad && chunks(r.cluster) > r.slots) return false;
     // few rows: more blocks each, while SMs are idle
     while (r.cluster < kMaxCluster && rows * r.cluster * 2 <= sms && chunks(r.cluster) > 1) r.cluster *= 2;

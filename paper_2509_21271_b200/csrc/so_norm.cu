@@ -22,38 +22,12 @@ struct NormArgs {
     float eps, inv_cols;
 };
 
-// ---- rows held in registers ------------------------------------------------------
+// ---- rows through shared memory ----------------------------------------------------
 //
-// A group of threads takes a row: a warp, or a whole block if the row is
-// longer.  A thread holds kNV vectors of E elements (16 bytes, or one element
-// where rows are not aligned) of the row it works on, and the next row's are on
-// their way meanwhile; groups walk the rows with a stride of the grid, so weight
-// and bias are read once per thread and stay in registers.
-//
-// Statistics: each warp has the mean of its elements and the sum of squares
-// around it (two passes over registers); warps are joined by
-//   M2 = sum M2_w + sum n_w (mean_w - mean)^2
-// which needs one barrier a row and loses nothing when the mean is large.
-
-template <typename T, int E> struct Raw;
-template <typename T> struct Raw<T, 1> { T v; };
-template <> struct Raw<float, 4> { uint4 v; };
-template <> struct Raw<bf16_t, 8> { uint4 v; };
-template <> struct Raw<f16_t, 8> { uint4 v; };
-
-template <typename T, int E>
-__device__ __forceinline__ void load_raw(Raw<T, E> &r, const T *p)
-{
-    if constexpr (E == 1) r.v = *p;
-    else r.v = __ldcs(reinterpret_cast<const uint4 *>(p));
-}
-
-template <typename T, int E>
-__device__ __forceinline__ Vals<E> widen(const Raw<T, E> &r)
-{
-    if constexpr (E == 1) return Vals<1>{to_f32(r.v)};
-    else return widen16<T>(r.v);
-}
+// A group of threads takes a row: a warp, or as many as its elements ask for, several
+// groups to a block if they are small.  A thread holds its columns' weight and bias in
+// registers for all its rows: kNV vectors of 16 bytes, or, where the rows do not all
+// start at a 16-byte boundary (E = 1), kNV single elements.
 
 template <typename T, int E>
 __device__ __forceinline__ void store_vec(T *p, const Vals<E> &f)
@@ -109,101 +83,74 @@ constexpr int kLongThreads = 512;         // threads of a long row, at most
 constexpr int kRowThreads = 256;
 constexpr int kGroupThreads = 128;        // a block has several groups up to this many threads
 
-template <typename T, int kNV, int kMaxThreads>
-__global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(NormArgs a, int per_row)
-{
-    constexpr int E = 1;
-    constexpr bool kHold = kNV <= 8;      // weight and bias stay in registers
-    __shared__ float4 s_part[2][32];      // (sum, mean, M2, count) of each warp, two rows in turn
-    const Group g(per_row);
-    const int cols = (int)a.cols;         // rows held in registers are short
-    const int64_t step = (int64_t)gridDim.x * g.per_block;
-    int64_t row = (int64_t)blockIdx.x * g.per_block + g.index;
-    if (g.index >= g.per_block || row >= a.rows) return;
-    const auto has = [&](int i) { return g.thread + i * g.threads < cols; };
+// Where R rows of a matrix lie in a stage of the ring, and their copies.  Rows of
+// vectors are copied as they are.  Otherwise the 16-byte granules that a row touches
+// are copied whole, so that it starts as far from a boundary as in memory; the granule
+// in front of the first row and that behind the last one may reach out of the matrix,
+// and their elements are loaded one by one.
+template <typename T, int E>
+struct RowCopies {
+    const char *base;
+    int64_t step;                         // bytes between rows
+    uintptr_t end;                        // of the matrix
+    uint32_t bytes, pitch;                // of a row, in memory and in the ring
 
-    Vals<E> w[kHold ? kNV : 1], b[kHold ? kNV : 1];
-    Raw<T, E> even[kNV], odd[kNV];
-    int mine = 0;                         // elements of this thread
-    const T *x = static_cast<const T *>(a.x) + row * a.x_stride + g.thread * E;
-    T *y = static_cast<T *>(a.y) + row * a.y_stride + g.thread * E;
-    const int64_t x_step = step * a.x_stride, y_step = step * a.y_stride;
-    const auto load_row = [&](Raw<T, E> (&r)[kNV]) {
-#pragma unroll
-        for (int i = 0; i < kNV; ++i)
-            if (has(i)) load_raw<T, E>(r[i], x + i * g.threads * E);
-    };
-    load_row(even);
-#pragma unroll
-    for (int i = 0; i < kNV; ++i)
-        if (has(i)) mine += E;
-    if constexpr (kHold) {
-#pragma unroll
-        for (int i = 0; i < kNV; ++i)
-            if (has(i)) {
-                w[i] = load_params<E>(a.weight, (g.thread + i * g.threads) * E, a.param_dtype, 1.0f);
-                b[i] = load_params<E>(a.bias, (g.thread + i * g.threads) * E, a.param_dtype, 0.0f);
-            }
+    __device__ RowCopies(const void *p, int64_t stride, int64_t rows, int64_t cols)
+        : base(static_cast<const char *>(p)), step(stride * (int64_t)sizeof(T)),
+          end(reinterpret_cast<uintptr_t>(p) + (uintptr_t)((rows - 1) * stride * (int64_t)sizeof(T)) + (uintptr_t)cols * sizeof(T)),
+          bytes((uint32_t)cols * sizeof(T)), pitch(E == 1 ? (bytes + 30 + 15) / 16 * 16 : bytes)
+    {
     }
-    const float count = warp_sum((float)mine), inv_count = count > 0.0f ? 1.0f / count : 0.0f;
+    // bytes from the row's place in the ring to its first element
+    __device__ __forceinline__ uint32_t shift(int64_t row) const
+    {
+        return E == 1 ? ((uint32_t)reinterpret_cast<uintptr_t>(base) + (uint32_t)row * (uint32_t)step) & 15u : 0u;
+    }
+    __device__ __forceinline__ void load(int64_t row, uint32_t dst, uint32_t bar) const
+    {
+        const char *src = base + row * step;
+        if constexpr (E > 1) {
+            bulk_load(dst, src, bytes, bar);
+        } else {
+            const uint32_t before = shift(row), whole = (before + bytes + 15) / 16 * 16;
+            uint32_t from = 0, to = whole;
+            if (src - before < base) {
+                from = 16;
+                for (uint32_t i = before; i < 16 && i < before + bytes; i += sizeof(T)) put(dst + i, src + (i - before));
+            }
+            if (reinterpret_cast<uintptr_t>(src) - before + whole > end && whole > from) {
+                to = whole - 16;
+                for (uint32_t i = to < before ? before : to; i < before + bytes; i += sizeof(T)) put(dst + i, src + (i - before));
+            }
+            if (to > from) {
+                asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(to - from) : "memory");
+                bulk_load(dst + from, src - before + from, to - from, bar);
+            }
+        }
+    }
+    static __device__ __forceinline__ void put(uint32_t dst, const char *src)
+    {
+        if constexpr (sizeof(T) == 4)
+            asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst), "r"(*reinterpret_cast<const uint32_t *>(src)) : "memory");
+        else
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst), "h"(*reinterpret_cast<const uint16_t *>(src)) : "memory");
+    }
+};
 
-    const auto one_row = [&](Raw<T, E> (&cur)[kNV], Raw<T, E> (&next)[kNV], float4 (&shared)[32]) {
-        x += x_step;
-        if (row + step < a.rows) load_row(next);
-        Vals<E> f[kNV], acc;
-        acc.set(0.0f);
-#pragma unroll
-        for (int i = 0; i < kNV; ++i)
-            if (has(i)) {
-                f[i] = widen<T, E>(cur[i]);
-                acc = acc + f[i];
-            }
-        const float sum = warp_sum(total(acc));
-        float mean = sum * inv_count;
-        acc.set(0.0f);
-#pragma unroll
-        for (int i = 0; i < kNV; ++i)
-            if (has(i)) {
-                const Vals<E> d = f[i] + -mean;
-                acc = fma(d, d, acc);
-            }
-        float m2 = warp_sum(total(acc));
-        if (g.warps > 1) {
-            float4 *part = shared + g.index * g.warps;
-            if ((threadIdx.x & 31) == 0) part[g.warp] = make_float4(sum, mean, m2, count);
-            g.sync();
-            float all = 0.0f;
-            for (int i = 0; i < g.warps; ++i) all += part[i].x;
-            mean = all * a.inv_cols;
-            m2 = 0.0f;
-            for (int i = 0; i < g.warps; ++i) {
-                const float4 q = part[i];
-                const float d = q.y - mean;
-                m2 += fmaf(q.w * d, d, q.z);
-            }
-        }
-        const float rstd = 1.0f / sqrtf(fmaf(m2, a.inv_cols, a.eps));
-        if (a.mean && g.thread == 0) {
-            a.mean[row] = mean;
-            a.rstd[row] = rstd;
-        }
-#pragma unroll
-        for (int i = 0; i < kNV; ++i)
-            if (has(i)) {
-                const int c = (g.thread + i * g.threads) * E;
-                const Vals<E> xh = (f[i] + -mean) * rstd;
-                if constexpr (kHold) store_vec<T, E>(y + i * g.threads * E, fma(xh, w[i], b[i]));
-                else store_vec<T, E>(y + i * g.threads * E, fma(xh, load_params<E>(a.weight, c, a.param_dtype, 1.0f),
-                                                                load_params<E>(a.bias, c, a.param_dtype, 0.0f)));
-            }
-        y += y_step;
-        row += step;
-    };
-    while (true) {
-        one_row(even, odd, s_part[0]);
-        if (row >= a.rows) break;
-        one_row(odd, even, s_part[1]);
-        if (row >= a.rows) break;
+// E elements from shared memory
+template <typename T, int E>
+__device__ __forceinline__ Vals<E> from_shared(uint32_t at)
+{
+    if constexpr (E > 1) {
+        return widen16<T>(lds16(at));
+    } else if constexpr (sizeof(T) == 4) {
+        float f;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(at));
+        return Vals<1>{f};
+    } else {
+        uint16_t h;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
+        return Vals<1>{to_f32(T{h})};
     }
 }
 
@@ -230,8 +177,7 @@ __device__ __forceinline__ float warp_sum_many(float (&v)[N])
     return r;
 }
 
-// Forward, rows whose vectors are aligned: rows come through a ring of bulk copies
-// in shared memory, so that no register waits for memory and the loads of several
+// Forward: rows come through a ring of bulk copies in shared memory, so that no register waits for memory and the loads of several
 // groups of rows are always on their way.  A group takes R rows at a time, whose
 // sums share one exchange and one barrier; that barrier also tells the group's
 // first thread that everyone is done with the rows before, whose place in the ring
@@ -256,7 +202,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     __shared__ __align__(8) uint64_t s_full[kRingBars];
     const Group g(per_row);
     const int cols = (int)a.cols, lane = threadIdx.x & 31;
-    const uint32_t row_bytes = (uint32_t)cols * sizeof(T), stage_bytes = row_bytes * R;
+    const RowCopies<T, E> xs(a.x, a.x_stride, a.rows, a.cols);
+    const uint32_t stage_bytes = xs.pitch * R;
     const uint32_t ring = smem_addr(s_ring) + (uint32_t)(g.index * stages) * stage_bytes;
     const uint32_t bars = smem_addr(s_full) + (uint32_t)(g.index * stages) * 8;
     const int64_t step = (int64_t)gridDim.x * g.per_block * R;
@@ -276,9 +223,9 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     const auto load_rows = [&](int64_t from, int s) {
         const int n = a.rows - from < R ? (int)(a.rows - from) : R;
         const uint32_t bar = bars + s * 8, dst = ring + s * stage_bytes;
-        mbar_expect(bar, row_bytes * n);
-        for (int r = 0; r < n; ++r)
-            bulk_load(dst + r * row_bytes, static_cast<const T *>(a.x) + (from + r) * a.x_stride, row_bytes, bar);
+        if (E > 1) mbar_expect(bar, xs.bytes * n);
+        for (int r = 0; r < n; ++r) xs.load(from + r, dst + r * xs.pitch, bar);
+        if (E == 1) mbar_arrive(bar);
     };
     if (g.thread == 0)
         for (int s = 0; s < stages; ++s)
@@ -294,7 +241,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     T *y = static_cast<T *>(a.y) + row * a.y_stride + g.thread * E;
     const int64_t y_step = (step - R) * a.y_stride;
     float *mean_to = a.mean ? a.mean + row + g.thread : nullptr, *rstd_to = a.rstd + row + g.thread;
-    const uint32_t mine = ring + (uint32_t)g.thread * 16;
+    constexpr uint32_t kBytes = E * sizeof(T);
+    const uint32_t mine = ring + (uint32_t)g.thread * kBytes, vector_step = (uint32_t)g.threads * kBytes;
     uint32_t limit = kPolls, phase = 0;
     int stage = 0, turn = 0;
     bool first = true;
@@ -303,6 +251,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         if (limit != 0 && !mbar_wait(bars + stage * 8, phase, limit)) limit = 0;
         const uint32_t at = mine + stage * stage_bytes;
         const int n = left < R ? (int)left : R;
+        const auto row_at = [&](int r) { return at + r * xs.pitch + xs.shift(a.rows - left + r); };
         float sums[kSums], centre[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -313,7 +262,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 #pragma unroll
                 for (int i = 0; i < kNV; ++i)
                     if (has(i)) {
-                        f[i] = widen16<T>(lds16(at + r * row_bytes + i * g.threads * 16));
+                        f[i] = from_shared<T, E>(row_at(r) + i * vector_step);
                         acc = acc + f[i];
                     }
                 m = total(acc) * inv_n;
@@ -395,7 +344,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 #pragma unroll
                 for (int i = 0; i < kNV; ++i)
                     if (has(i)) {
-                        const Vals<E> x = widen16<T>(lds16(at + r * row_bytes + i * g.threads * 16));
+                        const Vals<E> x = from_shared<T, E>(row_at(r) + i * vector_step);
                         store_vec<T, E>(y + i * g.threads * E, fma((x + -mean[r]) * rstd[r], w[i], b[i]));
                     }
                 y += a.y_stride;
@@ -416,10 +365,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     __syncthreads();
 }
 
-// Backward, rows whose vectors are aligned: the rows of x and dy come through a ring
-// of bulk copies in shared memory, kStages deep per group, so that no register
-// waits for memory and the loads of several groups of rows are always on their
-// way.  A group takes R rows at a time: their two sums each share one exchange
+// Backward: the rows of x and dy come through a ring of bulk copies.  A group takes R rows at a time: their two sums each share one exchange
 // and one barrier.  That barrier also tells the group's first thread that
 // everyone is done with the rows before, whose place in the ring it refills.
 // A thread keeps its columns' part of dweight and dbias for all its rows.
@@ -435,7 +381,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     __shared__ __align__(8) uint64_t s_full[kRingBars];
     const Group g(per_row);
     const int cols = (int)a.cols;
-    const uint32_t row_bytes = (uint32_t)cols * sizeof(T), stage_bytes = row_bytes * 2 * R;
+    const RowCopies<T, E> xs(a.x, a.x_stride, a.rows, a.cols), ys(a.dy, a.dy_stride, a.rows, a.cols);
+    const uint32_t stage_bytes = xs.pitch * 2 * R;
     const uint32_t ring = smem_addr(s_ring) + (uint32_t)(g.index * stages) * stage_bytes;
     const uint32_t bars = smem_addr(s_full) + (uint32_t)(g.index * stages) * 8;
     const int64_t step = (int64_t)gridDim.x * g.per_block * R;
@@ -450,11 +397,12 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     const auto load_rows = [&](int64_t from, int s) {
         const int n = a.rows - from < R ? (int)(a.rows - from) : R;
         const uint32_t bar = bars + s * 8, dst = ring + s * stage_bytes;
-        mbar_expect(bar, row_bytes * 2 * n);
+        if (E > 1) mbar_expect(bar, xs.bytes * 2 * n);
         for (int r = 0; r < n; ++r) {
-            bulk_load(dst + r * 2 * row_bytes, static_cast<const T *>(a.x) + (from + r) * a.x_stride, row_bytes, bar);
-            bulk_load(dst + (r * 2 + 1) * row_bytes, static_cast<const T *>(a.dy) + (from + r) * a.dy_stride, row_bytes, bar);
+            xs.load(from + r, dst + r * 2 * xs.pitch, bar);
+            ys.load(from + r, dst + (r * 2 + 1) * xs.pitch, bar);
         }
+        if (E == 1) mbar_arrive(bar);
     };
     if (g.thread == 0)
         for (int s = 0; s < stages; ++s)
@@ -481,7 +429,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     }
     T *dx = static_cast<T *>(a.y) + row * a.y_stride + g.thread * E;
     const int64_t dx_step = (step - R) * a.y_stride;
-    const uint32_t mine = ring + (uint32_t)g.thread * 16;
+    constexpr uint32_t kBytes = E * sizeof(T);
+    const uint32_t mine = ring + (uint32_t)g.thread * kBytes, vector_step = (uint32_t)g.threads * kBytes;
     uint32_t limit = kPolls, phase = 0;
     int stage = 0, turn = 0;
     bool first = true;
@@ -490,6 +439,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         if (limit != 0 && !mbar_wait(bars + stage * 8, phase, limit)) limit = 0;
         const uint32_t at = mine + stage * stage_bytes;
         const int n = left < R ? (int)left : R;
+        const auto x_at = [&](int r) { return at + r * 2 * xs.pitch + xs.shift(a.rows - left + r); };
+        const auto dy_at = [&](int r) { return at + (r * 2 + 1) * xs.pitch + ys.shift(a.rows - left + r); };
         float sums[kSums];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -501,8 +452,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 #pragma unroll
                 for (int i = 0; i < kNV; ++i) {
                     if (!has(i)) break;
-                    const Vals<E> x = widen16<T>(lds16(at + r * 2 * row_bytes + i * g.threads * 16));
-                    const Vals<E> d = widen16<T>(lds16(at + (r * 2 + 1) * row_bytes + i * g.threads * 16));
+                    const Vals<E> x = from_shared<T, E>(x_at(r) + i * vector_step);
+                    const Vals<E> d = from_shared<T, E>(dy_at(r) + i * vector_step);
                     const Vals<E> t = d * fma(x, rstd[r], off);
                     ag = fma(d, w[i], ag);
                     agx = fma(t, w[i], agx);
@@ -546,8 +497,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 #pragma unroll
                 for (int i = 0; i < kNV; ++i) {
                     if (!has(i)) break;
-                    const Vals<E> x = widen16<T>(lds16(at + r * 2 * row_bytes + i * g.threads * 16));
-                    const Vals<E> d = widen16<T>(lds16(at + (r * 2 + 1) * row_bytes + i * g.threads * 16));
+                    const Vals<E> x = from_shared<T, E>(x_at(r) + i * vector_step);
+                    const Vals<E> d = from_shared<T, E>(dy_at(r) + i * vector_step);
                     store_vec<T, E>(dx + i * g.threads * E, fma(d * w[i], rs, fma(x, by_x, rest)));
                 }
                 dx += a.y_stride;
@@ -573,145 +524,6 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     if (!a.partials) return;
     float *out = a.partials + (int64_t)blockIdx.x * 2 * a.cols;
     float *sums = g.per_block > 1 ? reinterpret_cast<float *>(s_ring) : out;   // the ring is done with
-    for (int turn = 0; turn < g.per_block; ++turn) {
-        if (turn > 0) __syncthreads();
-        if (g.index != turn) continue;
-#pragma unroll
-        for (int i = 0; i < kNV; ++i) {
-            const int c = (g.thread + i * g.threads) * E;
-            if (c >= cols) break;
-            float fw[E], fb[E];
-            dw[i].get(fw);
-            db[i].get(fb);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float pw = turn > 0 ? sums[c + e] + fw[e] : fw[e];
-                const float pb = turn > 0 ? sums[a.cols + c + e] + fb[e] : fb[e];
-                float *to = turn == g.per_block - 1 ? out : sums;
-                to[c + e] = pw;
-                to[a.cols + c + e] = pb;
-            }
-        }
-    }
-}
-
-// Backward, other rows: the same from registers, element by element.  A thread keeps its part of dweight and dbias for
-// all its rows.  Groups of a block are joined in shared memory in their order,
-// blocks by norm_reduce_kernel.
-template <typename T, int kNV, int R, int kMaxThreads>
-__global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(NormArgs a, int per_row)
-{
-    extern __shared__ float s_sums[];     // [2][cols], if a block has several groups
-    constexpr int E = 1;
-    constexpr int kSums = 2 * R;          // of each row: sum(g), sum(g xhat)
-    __shared__ __align__(16) float s_part[2][32][kSums];
-    const Group g(per_row);
-    const int cols = (int)a.cols;         // rows held in registers are short
-    const int64_t step = (int64_t)gridDim.x * g.per_block * R;
-    int64_t row = ((int64_t)blockIdx.x * g.per_block + g.index) * R;
-    const bool working = g.index < g.per_block && row < a.rows;
-
-    const auto has = [&](int i) { return g.thread + i * g.threads < cols; };
-
-    Vals<E> w[kNV], dw[kNV], db[kNV];
-    struct Rows { Raw<T, E> x[R][kNV], dy[R][kNV]; float mean[R], rstd[R]; } even, odd;
-    const T *x = static_cast<const T *>(a.x) + row * a.x_stride + g.thread * E;
-    const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride + g.thread * E;
-    T *dx = static_cast<T *>(a.y) + row * a.y_stride + g.thread * E;
-    const float *mean = a.mean + row, *rstd = a.rstd + row;
-    const int64_t x_step = step * a.x_stride, dy_step = step * a.dy_stride, dx_step = step * a.y_stride;
-    const auto load_rows = [&](Rows &to, int64_t from) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (from + r >= a.rows) break;
-            to.mean[r] = mean[r];
-            to.rstd[r] = rstd[r];
-#pragma unroll
-            for (int i = 0; i < kNV; ++i)
-                if (has(i)) {
-                    load_raw<T, E>(to.x[r][i], x + r * a.x_stride + i * g.threads * E);
-                    load_raw<T, E>(to.dy[r][i], dy + r * a.dy_stride + i * g.threads * E);
-                }
-        }
-    };
-    if (working) load_rows(even, row);
-#pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-        if (working && has(i)) w[i] = load_params<E>(a.weight, (g.thread + i * g.threads) * E, a.param_dtype, 1.0f);
-        dw[i].set(0.0f);
-        db[i].set(0.0f);
-    }
-
-    const auto some_rows = [&](Rows &cur, Rows &next, float (&shared)[32][kSums]) {
-        x += x_step;
-        dy += dy_step;
-        mean += step;
-        rstd += step;
-        load_rows(next, row + step);
-        float sums[kSums];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            Vals<E> ag, agx;
-            ag.set(0.0f);
-            agx.set(0.0f);
-            if (row + r < a.rows) {
-                const float off = -cur.mean[r] * cur.rstd[r];
-#pragma unroll
-                for (int i = 0; i < kNV; ++i) {
-                    if (!has(i)) break;
-                    const Vals<E> d = widen<T, E>(cur.dy[r][i]), t = d * fma(widen<T, E>(cur.x[r][i]), cur.rstd[r], off);
-                    ag = fma(d, w[i], ag);
-                    agx = fma(t, w[i], agx);
-                    dw[i] = dw[i] + t;
-                    db[i] = db[i] + d;
-                }
-            }
-            sums[2 * r] = total(ag);
-            sums[2 * r + 1] = total(agx);
-        }
-        const int lane = threadIdx.x & 31;
-        const float mine = warp_sum_many<kSums>(sums);
-        float (*part)[kSums] = shared + g.index * g.warps;
-        if (lane % (32 / kSums) == 0) part[g.warp][lane / (32 / kSums)] = mine;
-        if (g.warps > 1) g.sync();
-        else __syncwarp();
-        Vals<kSums> all;
-        all.set(0.0f);
-        for (int j = 0; j < g.warps; ++j) {
-            Vals<kSums> p;
-#pragma unroll
-            for (int i = 0; i < R; ++i) p.p[i] = *reinterpret_cast<const f32x2 *>(&part[j][2 * i]);
-            all = all + p;
-        }
-        float row_sum[kSums];
-        all.get(row_sum);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (row + r >= a.rows) break;
-            // dx = rstd (dy w - m_g - xhat m_gx), gathered by factors of dy w and of x
-            const float rs = cur.rstd[r], by_x = -rs * rs * (row_sum[2 * r + 1] * a.inv_cols);
-            const float rest = fmaf(-cur.mean[r], by_x, -rs * (row_sum[2 * r] * a.inv_cols));
-#pragma unroll
-            for (int i = 0; i < kNV; ++i) {
-                if (!has(i)) break;
-                const Vals<E> gw = widen<T, E>(cur.dy[r][i]) * w[i];
-                store_vec<T, E>(dx + r * a.y_stride + i * g.threads * E,
-                                fma(gw, rs, fma(widen<T, E>(cur.x[r][i]), by_x, rest)));
-            }
-        }
-        dx += dx_step;
-        row += step;
-    };
-    while (working) {
-        some_rows(even, odd, s_part[0]);
-        if (row >= a.rows) break;
-        some_rows(odd, even, s_part[1]);
-        if (row >= a.rows) break;
-    }
-
-    if (!a.partials) return;
-    float *out = a.partials + (int64_t)blockIdx.x * 2 * a.cols;
-    float *sums = g.per_block > 1 ? s_sums : out;
     for (int turn = 0; turn < g.per_block; ++turn) {
         if (turn > 0) __syncthreads();
         if (g.index != turn) continue;
@@ -862,32 +674,6 @@ inline Plan make_plan(int64_t vectors, int nv)
     return p;
 }
 
-// Forward, element by element: as few warps a row as its elements fit into, but
-// enough rows in flight; with few rows, more and more warps share one.
-inline Plan plan_forward(int64_t cols, const int *nvs, int n, int64_t rows, int sms)
-{
-    Plan p = {0, 0, 0};
-    for (int i = n - 1; i >= 0; --i) {
-        const Plan q = make_plan(cols, nvs[i]);
-        if (q.per_row > kLongThreads) break;
-        if (p.per_row != 0 && rows * (p.per_row / 32) >= (int64_t)8 * sms) break;
-        if (i > 0 && (cols + nvs[i - 1] - 1) / nvs[i - 1] <= 32) continue;   // a warp does with fewer
-        p = q;
-    }
-    return p;
-}
-
-// Backward, element by element: columns stay with a thread for all rows, which costs
-// three registers an element besides the rows, so as few elements a thread as possible.
-inline Plan plan_backward(int64_t cols, const int *nvs, int n)
-{
-    for (int i = 0; i < n; ++i) {
-        const Plan q = make_plan(cols, nvs[i]);
-        if (q.per_row <= (i + 1 < n ? kRowThreads : kLongThreads)) return q;
-    }
-    return {0, 0, 0};
-}
-
 constexpr int kMaxShared = 220 * 1024;    // dynamic shared memory of a block, at most
 
 // Resident blocks per SM of a kernel, asked for once per device.
@@ -914,35 +700,6 @@ so_status resident(K kernel, int block, size_t smem, std::atomic<int> (&cache)[k
     return SO_OK;
 }
 
-template <typename T, int kNV, int kMaxThreads>
-so_status launch_forward(const NormArgs &a, const Plan &p, int sms, cudaStream_t st)
-{
-    static std::atomic<int> cache[kMaxDevices];
-    int per_sm = 0;
-    const so_status s = resident(norm_forward_kernel<T, kNV, kMaxThreads>, p.block, 0, cache, &per_sm);
-    if (s != SO_OK) return s;
-    const int groups = p.block / p.per_row;
-    const int64_t want = (a.rows + groups - 1) / groups, most = (int64_t)per_sm * sms;
-    return launch(norm_forward_kernel<T, kNV, kMaxThreads>, (unsigned)(want < most ? want : most), p.block, 0, st,
-                  false, a, p.per_row);
-}
-
-template <typename T, int kNV, int R, int kMaxThreads>
-so_status launch_backward(const NormArgs &a, const Plan &p, int sms, cudaStream_t st, int *blocks)
-{
-    static std::atomic<int> cache[kMaxDevices];
-    const int groups = p.block / p.per_row;
-    const size_t smem = groups > 1 ? (size_t)a.cols * 2 * sizeof(float) : 0;
-    int per_sm = 0;
-    const so_status s = resident(norm_backward_kernel<T, kNV, R, kMaxThreads>, p.block, smem, cache, &per_sm);
-    if (s != SO_OK) return s;
-    const int64_t want = (a.rows + groups * R - 1) / (groups * R);
-    int64_t most = (int64_t)per_sm * sms;
-    if (most > kMaxPartials) most = kMaxPartials;
-    *blocks = (int)(want < most ? want : most);
-    return launch(norm_backward_kernel<T, kNV, R, kMaxThreads>, (unsigned)*blocks, p.block, smem, st, false, a, p.per_row);
-}
-
 // Stages of a ring: up to four, in the shared memory that four blocks share an SM with
 // (two blocks' if only two stages of long rows fit there).
 inline int ring_stages(size_t stage_bytes, int groups)
@@ -953,11 +710,19 @@ inline int ring_stages(size_t stage_bytes, int groups)
     return stages < kRingBars / groups ? stages : kRingBars / groups;
 }
 
+// Bytes of a row in the ring.
+template <typename T, int E>
+size_t ring_pitch(int64_t cols)
+{
+    const size_t bytes = (size_t)cols * sizeof(T);
+    return E == 1 ? (bytes + 30 + 15) / 16 * 16 : bytes;
+}
+
 template <typename T, int E, int kNV, int R, bool kFull, int kMaxThreads>
 so_status launch_forward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t st)
 {
     const int groups = p.block / p.per_row;
-    const size_t stage = (size_t)a.cols * sizeof(T) * R * groups;
+    const size_t stage = ring_pitch<T, E>(a.cols) * R * groups;
     const int stages = ring_stages(stage, groups);
     static std::atomic<int> cache[kMaxDevices];
     int per_sm = 0;
@@ -972,7 +737,7 @@ template <typename T, int E, int kNV, int R, bool kFull, int kMaxThreads>
 so_status launch_backward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t st, int *blocks)
 {
     const int groups = p.block / p.per_row;
-    const size_t stage = (size_t)a.cols * sizeof(T) * 2 * R * groups;
+    const size_t stage = ring_pitch<T, E>(a.cols) * 2 * R * groups;
     const int stages = ring_stages(stage, groups);
     static std::atomic<int> cache[kMaxDevices];
     int per_sm = 0;
@@ -1001,13 +766,12 @@ inline Plan plan_ring(int64_t vectors, int most_nv)
     return best;
 }
 
-template <typename T, int kNV, int R>
+template <typename T, int E, int kNV, int R>
 so_status forward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t st)
 {
-    constexpr int E = Vec<T>::kElems;
-    const bool full = (int64_t)p.per_row * kNV * E == a.cols;
+    const bool full = E > 1 && (int64_t)p.per_row * kNV * E == a.cols;
     if (p.block <= kRowThreads)
-        return full ? launch_forward_ring<T, E, kNV, R, true, kRowThreads>(a, p, sms, st)
+        return full ? launch_forward_ring<T, E, kNV, R, E != 1, kRowThreads>(a, p, sms, st)
                     : launch_forward_ring<T, E, kNV, R, false, kRowThreads>(a, p, sms, st);
     return launch_forward_ring<T, E, kNV, R, false, kLongThreads>(a, p, sms, st);
 }
@@ -1015,34 +779,29 @@ so_status forward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t s
 template <typename T>
 so_status forward(const NormArgs &a, bool vec, int sms, cudaStream_t st)
 {
-    if (vec) {
-        const Plan p = plan_ring(a.cols / Vec<T>::kElems, 4);
-        if (p.per_row != 0 && a.cols * (int64_t)sizeof(T) * 2 <= kMaxShared) {
-            if (p.nv == 4) return forward_ring<T, 4, 1>(a, p, sms, st);
-            if (p.nv == 3) return forward_ring<T, 3, 1>(a, p, sms, st);
-            if (p.nv == 2) return forward_ring<T, 2, 2>(a, p, sms, st);
-            return forward_ring<T, 1, 4>(a, p, sms, st);
-        }
-    } else {
-        static const int nvs[] = {4, 8, 16};
-        const Plan p = plan_forward(a.cols, nvs, 3, a.rows, sms);
-        if (p.per_row != 0) {
-            if (p.nv == 4) return launch_forward<T, 4, kLongThreads>(a, p, sms, st);
-            if (p.nv == 8) return launch_forward<T, 8, kLongThreads>(a, p, sms, st);
-            return launch_forward<T, 16, kLongThreads>(a, p, sms, st);
-        }
+    constexpr int E = Vec<T>::kElems;
+    const bool fits = a.cols * (int64_t)sizeof(T) * 2 + 128 <= kMaxShared;   // two stages of one row
+    if (vec && fits) {
+        const Plan p = plan_ring(a.cols / E, 4);
+        if (p.nv == 4) return forward_ring<T, E, 4, 1>(a, p, sms, st);
+        if (p.nv == 3) return forward_ring<T, E, 3, 1>(a, p, sms, st);
+        if (p.nv == 2) return forward_ring<T, E, 2, 2>(a, p, sms, st);
+        if (p.nv == 1) return forward_ring<T, E, 1, 4>(a, p, sms, st);
+    } else if (fits) {
+        const Plan p = make_plan(a.cols, a.cols <= 8 * kLongThreads ? 8 : 16);
+        if (p.nv == 8) return forward_ring<T, 1, 8, 2>(a, p, sms, st);
+        if (p.per_row <= kLongThreads) return forward_ring<T, 1, 16, 1>(a, p, sms, st);
     }
     const unsigned grid = (unsigned)(a.rows < 4 * sms ? a.rows : 4 * sms);
     return launch(norm_forward_loop_kernel<T>, grid, kLoopThreads, 0, st, false, a);
 }
 
-template <typename T, int kNV, int R>
+template <typename T, int E, int kNV, int R>
 so_status backward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t st, int *blocks)
 {
-    constexpr int E = Vec<T>::kElems;
-    const bool full = (int64_t)p.per_row * kNV * E == a.cols;
+    const bool full = E > 1 && (int64_t)p.per_row * kNV * E == a.cols;
     if (p.block <= kRowThreads)
-        return full ? launch_backward_ring<T, E, kNV, R, true, kRowThreads>(a, p, sms, st, blocks)
+        return full ? launch_backward_ring<T, E, kNV, R, E != 1, kRowThreads>(a, p, sms, st, blocks)
                     : launch_backward_ring<T, E, kNV, R, false, kRowThreads>(a, p, sms, st, blocks);
     return launch_backward_ring<T, E, kNV, R, false, kLongThreads>(a, p, sms, st, blocks);
 }
@@ -1050,27 +809,28 @@ so_status backward_ring(const NormArgs &a, const Plan &p, int sms, cudaStream_t 
 template <typename T>
 so_status backward(const NormArgs &a, bool vec, int sms, cudaStream_t st, int *blocks)
 {
-    if (vec) {
-        const Plan p = plan_ring(a.cols / Vec<T>::kElems, 2);
-        const int64_t row = a.cols * (int64_t)sizeof(T);
-        if (p.per_row != 0 && row * 4 <= kMaxShared) {
-            // rows at a time: four, or as many as leave three stages in shared memory
-            const int r = row * 24 <= kMaxShared ? 4 : row * 12 <= kMaxShared ? 2 : 1;
-            if (p.nv == 2) {
-                if (r == 4) return backward_ring<T, 2, 4>(a, p, sms, st, blocks);
-                if (r == 2) return backward_ring<T, 2, 2>(a, p, sms, st, blocks);
-                return backward_ring<T, 2, 1>(a, p, sms, st, blocks);
-            }
-            if (r == 4) return backward_ring<T, 1, 4>(a, p, sms, st, blocks);
-            return backward_ring<T, 1, 1>(a, p, sms, st, blocks);
+    constexpr int E = Vec<T>::kElems;
+    const int64_t row = a.cols * (int64_t)sizeof(T) + (vec ? 0 : 48);
+    // rows at a time: four, or as many as leave three stages in shared memory
+    const int r = row * 24 <= kMaxShared ? 4 : row * 12 <= kMaxShared ? 2 : 1;
+    if (vec && row * 4 <= kMaxShared) {
+        const Plan p = plan_ring(a.cols / E, 2);
+        if (p.nv == 2) {
+            if (r == 4) return backward_ring<T, E, 2, 4>(a, p, sms, st, blocks);
+            if (r == 2) return backward_ring<T, E, 2, 2>(a, p, sms, st, blocks);
+            return backward_ring<T, E, 2, 1>(a, p, sms, st, blocks);
         }
-    } else {
-        static const int nvs[] = {4, 8};
-        const Plan p = plan_backward(a.cols, nvs, 2);
-        if (p.per_row != 0) {
-            if (p.nv == 4) return launch_backward<T, 4, 2, kLongThreads>(a, p, sms, st, blocks);
-            return launch_backward<T, 8, 1, kLongThreads>(a, p, sms, st, blocks);
+        if (p.nv == 1) {
+            if (r == 4) return backward_ring<T, E, 1, 4>(a, p, sms, st, blocks);
+            return backward_ring<T, E, 1, 1>(a, p, sms, st, blocks);
         }
+    } else if (row * 4 <= kMaxShared) {
+        const Plan p = make_plan(a.cols, a.cols <= 8 * kLongThreads ? 8 : 16);
+        if (p.nv == 8) {
+            if (r == 4) return backward_ring<T, 1, 8, 4>(a, p, sms, st, blocks);
+            return backward_ring<T, 1, 8, 2>(a, p, sms, st, blocks);
+        }
+        if (p.per_row <= kLongThreads) return backward_ring<T, 1, 16, 1>(a, p, sms, st, blocks);
     }
     const int64_t most = 2 * sms < kMaxPartials ? 2 * sms : kMaxPartials;
     *blocks = (int)(a.rows < most ? a.rows : most);

@@ -298,9 +298,6 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 // Waits for the phase of the given parity, at most `limit` polls (each of which the
 // hardware may hold for a while); false if it did not complete.
 constexpr uint32_t kPolls = 1u << 20;
-#ifndef IDLE_NS
-#define IDLE_NS 300
-#endif
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
@@ -328,7 +325,7 @@ __device__ __forceinline__ bool mbar_wait_idle(uint32_t bar, uint32_t parity, ui
 {
     for (uint32_t i = 0; i < limit; ++i) {
         if (mbar_test(bar, parity)) return true;
-        __nanosleep(IDLE_NS);
+        __nanosleep(300);
     }
     return false;
 }

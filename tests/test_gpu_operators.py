@@ -8,7 +8,8 @@ of the absolute values of the terms (so cancellation is covered, not hidden).
 Paths: a sum of n terms is split over at least 256 accumulators where n is large,
 so n / 256 additions in a row, and at most 64 more for the trees, the partial sums
 of blocks and the arithmetic of a term.  The hardware exponential is good to 2^-22
-relative.  fp16 results below its normal range are rounded to multiples of 2^-24."""
+relative and gives 0 below 2^-126 (fp32 and bf16 results).  fp16 results below its
+normal range are rounded to multiples of 2^-24."""
 from __future__ import annotations
 
 import math
@@ -24,7 +25,7 @@ pytestmark = pytest.mark.gpu
 
 BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
 U = {BF16: 2.0 ** -8, FP16: 2.0 ** -11, FP32: 2.0 ** -24}
-FLOOR = {BF16: 2.0 ** -133, FP16: 2.0 ** -25, FP32: 2.0 ** -126}
+FLOOR = {BF16: 2.0 ** -126, FP16: 2.0 ** -25, FP32: 2.0 ** -126}
 E = 2.0 ** -24
 EXP = 2.0 ** -22
 INF = float("inf")
@@ -624,6 +625,41 @@ def test_losses_in_place_and_alone(dtype, rows, vocab, offset):
     tok, adv = ids[:, 0].contiguous(), randn(gen(4), rows)
     first = ops.policy_loss(z, tok, adv)
     assert same_bits(ops.policy_loss(z, tok, adv, grad=z)[3], first[3])
+
+
+@pytest.mark.parametrize("dtype,vocab", [(FP32, 480_001), (BF16, 950_003), (FP16, 440_011)])
+def test_losses_of_vocabularies_beyond_the_shared_memory_of_a_cluster(dtype, vocab):
+    z, ids, teacher = distill_inputs(94, 3, vocab, 20, dtype)
+    ids[1, 5] = ids[1, 4]
+    weight = torch.tensor([0.5, 1.0, 0.0], device="cuda")
+    check_distill(z, ids, teacher, weight, 1.5, 256.0 if dtype == FP16 else 1.0)
+    zp, tokens, adv, old, ref = policy_inputs(95, 3, vocab, dtype)
+    check_policy(zp, tokens, adv, weight, old, ref, kl=0.1, grad_scale=256.0 if dtype == FP16 else 1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("at", [3, 700, 49_999])
+def test_losses_of_rows_that_rise_far_above_their_first_elements(dtype, at):
+    """One logit exceeds the others by far more than fp32's exponent holds (2^127 is 88 nats)."""
+    z, ids, teacher = distill_inputs(96, 6, 50_257, 4, dtype)
+    z[:, at] = torch.tensor([60.0, 88.0, 100.0, 300.0, 3e4, 1e30], device="cuda").to(dtype)
+    ids[:, 0] = at
+    check_distill(z, ids, teacher)
+    check_policy(z, ids[:, 0].contiguous(), torch.ones(6, device="cuda"))
+    z = -z.abs() * 40.0
+    z[:, at] = 0.0
+    check_distill(z, ids, teacher)
+
+
+@pytest.mark.parametrize("rows,vocab,masked", [(1500, 20_011, 0.5), (3000, 300, 0.9), (700, 50_257, 0.0), (2000, 7, 0.3)])
+def test_many_rows_with_masked_ones_among_them(rows, vocab, masked):
+    z, ids, teacher = distill_inputs(97, rows, vocab, 3, BF16)
+    weight = (torch.rand(rows, generator=gen(6), device="cuda") >= masked).float()
+    check_distill(z, ids, teacher, weight)
+    z[weight == 0] = float("nan")
+    adv = randn(gen(7), rows)
+    loss, row, logp, grad = check_policy(z, ids[:, 0].contiguous(), adv, weight)
+    assert torch.isfinite(loss).all()
 
 
 def test_distill_of_one_entry_is_cross_entropy():
