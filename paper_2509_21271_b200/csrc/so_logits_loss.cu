@@ -363,6 +363,13 @@ __device__ __forceinline__ void cluster_sync()
 constexpr float kPlain = 1048576.0f;
 __device__ __forceinline__ bool plain(float ref) { return fabsf(ref) <= kPlain; }
 
+// Exponent of z against the reference of m.
+__device__ __forceinline__ float exponent_of(float z, float m, float c)
+{
+    const float ref = m * c;
+    return plain(ref) ? fmaf(z, c, -ref) : (z - m) * c;
+}
+
 // Factor that takes a sum from one reference to another.
 __device__ __forceinline__ float rescale(float from, float to, float c)
 {
@@ -656,9 +663,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
             if (limit != 0 && !mbar_wait_idle(smem_addr(&s_target_empty[buf]), parity, limit)) limit = 0;
             const RowInfo info = s_info[buf];
             const float4 done = s_result[buf];
-            const float c = a.log2e_over_t, ref = done.x * c;
-            const bool is_plain = plain(ref);
-            const auto exponent = [&](float z) { return is_plain ? fmaf(z, c, -ref) : (z - done.x) * c; };
+            const auto exponent = [&](float z) { return exponent_of(z, done.x, a.log2e_over_t); };
             if (limit == 0) {
                 if (rank == 0 && lane == 0) a.row_loss[info.row] = kNan;
                 return;
@@ -803,8 +808,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
             // the single element of a few threads: the first block's head, the last block's tail
             int64_t edge = -1;
             if (rank == 0 && (int)threadIdx.x < p.head) edge = threadIdx.x;
-            const int64_t tail = p.head + (int64_t)p.count * E + ((int)threadIdx.x - 32);
-            if (rank == (uint32_t)cluster - 1 && threadIdx.x >= 32 && tail < a.vocab) edge = tail;
+            if (rank == (uint32_t)cluster - 1 && warp == 1 && p.head + p.count * E + lane < a.vocab) edge = p.head + p.count * E + lane;
 
             if (!info.live) {
                 // nothing to compute: a chunk that is on its way is let go, the gradient is zero
@@ -875,51 +879,53 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
                 }
                 ms = join_lanes(ms, c);
                 if (limit == 0) ms.s = kNan;
-                // every warp's part to every block of the cluster
+                // every warp's part to every block of the cluster, where one warp joins them and
+                // works out what the row comes to
                 const int turn = computed & 1;
+                const uint32_t bar = smem_addr(&s_exchange[turn]);
                 if (cluster > 1) {
-                    const uint32_t bar = smem_addr(&s_exchange[turn]);
                     if (threadIdx.x == 0) mbar_expect(bar, (uint32_t)(cluster * warps) * sizeof(MaxSum));
                     if (lane < cluster)
                         remote_store(remote_addr(smem_addr(&s_block[turn][rank * warps + warp]), lane), ms.m, ms.s, remote_addr(bar, lane));
-                    if (limit != 0 && !mbar_wait(bar, (computed >> 1) & 1, limit)) limit = 0;
                 } else {
                     if (lane == 0) s_block[turn][warp] = ms;
                     asm volatile("bar.sync 1, %0;" ::"r"(shape.threads) : "memory");
                 }
-                ms = lane < cluster * warps ? s_block[turn][lane] : MaxSum{-kInf, 0.0f};
-                for (int i = lane + 32; i < cluster * warps; i += 32) ms = join(ms, s_block[turn][i], c);
-                ms = join_lanes(ms, c);
-                if (limit == 0) ms.s = kNan;
-                ++computed;
-
-                // log q = ln 2 (z c - ref) - ln S
-                const float ref = ms.m * c, inv_s = 1.0f / ms.s;
-                const bool is_plain = plain(ref);
-                const auto exponent = [&](float x) { return is_plain ? fmaf(x, c, -ref) : (x - ms.m) * c; };
-                float coef;
-                if (kMode == kDistill) {
-                    coef = a.grad_scale * info.weight * a.temperature;
-                    if (threadIdx.x == 0) s_result[buf] = make_float4(ms.m, logf(ms.s), inv_s, coef);
-                } else {
-                    const float logp = fmaf(exponent(target_z(buf)[0]), kLn2, -logf(ms.s));
-                    float loss, slope;
-                    policy_row(a, logp, info.advantage, info.old_logp, info.ref_logp, loss, slope);
-                    if (rank == 0 && threadIdx.x == 0) {
-                        a.row_loss[row] = loss;
-                        if (a.logp) a.logp[row] = logp;
+                if (warp == 0) {
+                    if (cluster > 1 && limit != 0 && !mbar_wait(bar, (computed >> 1) & 1, limit)) limit = 0;
+                    ms = lane < cluster * warps ? s_block[turn][lane] : MaxSum{-kInf, 0.0f};
+                    for (int i = lane + 32; i < cluster * warps; i += 32) ms = join(ms, s_block[turn][i], c);
+                    ms = join_lanes(ms, c);
+                    if (limit == 0) ms.s = kNan;
+                    const float log_s = logf(ms.s);
+                    float coef;
+                    if (kMode == kDistill) {
+                        coef = a.grad_scale * info.weight * a.temperature;
+                    } else {
+                        // log q = ln 2 (z c - ref) - ln S
+                        const float logp = fmaf(exponent_of(target_z(buf)[0], ms.m, c), kLn2, -log_s);
+                        float loss, slope;
+                        policy_row(a, logp, info.advantage, info.old_logp, info.ref_logp, loss, slope);
+                        if (rank == 0 && lane == 0) {
+                            a.row_loss[row] = loss;
+                            if (a.logp) a.logp[row] = logp;
+                        }
+                        coef = -a.grad_scale * info.weight * slope * a.inv_temperature;
                     }
-                    coef = -a.grad_scale * info.weight * slope * a.inv_temperature;
-                    if (threadIdx.x == 0) s_result[buf] = make_float4(ms.m, 0.0f, inv_s, coef);
+                    if (lane == 0) s_result[buf] = make_float4(ms.m, log_s, 1.0f / ms.s, coef);
                 }
+                ++computed;
+                asm volatile("bar.sync 1, %0;" ::"r"(shape.threads) : "memory");
 
                 if (kGrad) {
                     // phase 2
-                    const float scaled = coef * inv_s;
+                    const float4 done = s_result[buf];
+                    const float m = done.x, ref = m * c, scaled = done.w * done.z;
+                    const bool is_plain = plain(ref);
                     T *out = g + p.head + (int64_t)p.from * E;
                     const auto write_chunks = [&](auto plain_row, auto vectors) {
                         const auto put = [&](const uint4 &q, T *at) {
-                            const Vals<E> e = exponentials<decltype(plain_row)::value>(widen16<T>(q), ms.m, ref, c) * scaled;
+                            const Vals<E> e = exponentials<decltype(plain_row)::value>(widen16<T>(q), m, ref, c) * scaled;
                             if constexpr (decltype(vectors)::value) {
                                 *reinterpret_cast<uint4 *>(at) = narrow16<T>(e);
                             } else {
@@ -952,7 +958,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
                     else if (same_offset) write_chunks(std::false_type{}, std::true_type{});
                     else if (is_plain) write_chunks(std::true_type{}, std::false_type{});
                     else write_chunks(std::false_type{}, std::false_type{});
-                    if (edge >= 0) g[edge] = from_f32<T>(exp2_fast(exponent(edge_z)) * scaled);
+                    if (edge >= 0) g[edge] = from_f32<T>(exp2_fast(exponent_of(edge_z, m, c)) * scaled);
                 }
             }
             __syncwarp();
