@@ -424,6 +424,13 @@ template <> __device__ __forceinline__ float largest<f16_t>(const uint4 &v)
                  __half2float(__ushort_as_half((unsigned short)(a >> 16))));
 }
 
+// A vector of -inf.
+template <typename T> __device__ __forceinline__ uint4 nothing()
+{
+    const uint32_t w = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, bf16_t>::value ? 0xFF80FF80u : 0xFC00FC00u;
+    return make_uint4(w, w, w, w);
+}
+
 // exp((z - m) / T) of a vector
 template <bool kPlainRow, int E>
 __device__ __forceinline__ Vals<E> exponentials(const Vals<E> &z, float m, float ref, float c)
@@ -847,10 +854,13 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
                         if constexpr (kGrad) run.add_unchecked(q, c, slack);
                         else run.add(q, c, slack);
                     } else {
-                        for (int i = threadIdx.x, u = 0; i < left; i += shape.threads, ++u) {
-                            const uint4 q[1] = {lds16(at + u * vector_step)};
-                            run.add(q, c, slack);
-                        }
+                        // the last chunk: -inf where there is nothing
+                        uint4 q[kPerThread];
+#pragma unroll
+                        for (int i = 0; i < kPerThread; ++i)
+                            q[i] = (int)threadIdx.x + i * shape.threads < left ? lds16(at + i * vector_step) : nothing<T>();
+                        if constexpr (kGrad) run.add_unchecked(q, c, slack);
+                        else run.add(q, c, slack);
                     }
                     if (!kGrad) {
                         __syncwarp();
@@ -946,8 +956,13 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
 #pragma unroll
                                 for (int i = 0; i < kPerThread; ++i) put(q[i], to + i * shape.threads * E);
                             } else {
-                                for (int i = threadIdx.x, u = 0; i < left; i += shape.threads, ++u)
-                                    put(lds16(at + u * vector_step), to + u * shape.threads * E);
+                                uint4 q[kPerThread];
+#pragma unroll
+                                for (int i = 0; i < kPerThread; ++i)
+                                    q[i] = (int)threadIdx.x + i * shape.threads < left ? lds16(at + i * vector_step) : nothing<T>();
+#pragma unroll
+                                for (int i = 0; i < kPerThread; ++i)
+                                    if ((int)threadIdx.x + i * shape.threads < left) put(q[i], to + i * shape.threads * E);
                             }
                             __syncwarp();
                             if (lane == 0) mbar_arrive(empty_bar + there.bar);
