@@ -501,6 +501,149 @@ struct Running {
     }
 };
 
+// ---- a block per row, the row held in registers ----------------------------------------
+//
+// For short rows, where a cluster's set-up would cost more than the row: as many threads
+// as hold its vectors, four each, and as many rows at a time as the SMs have room for.
+// A thread keeps the exponentials against its own maximum, so each is taken once; the
+// gradient is that times one factor per thread.
+
+constexpr int kShortVectors = 4, kShortThreads = 512;
+
+template <typename T, int kMode, bool kGrad>
+__global__ void __launch_bounds__(kShortThreads) loss_short_kernel(LossArgs a)
+{
+    constexpr int E = Vec<T>::kElems;
+    __shared__ MaxSum s_warp[kShortThreads / 32];
+    __shared__ float4 s_result;           // reference, logarithm of the sum, its inverse, the gradient's factor
+    __shared__ int s_any;
+    extern __shared__ __align__(16) float s_lists[];      // ids, probabilities, their logarithms, logits
+    const int top_k = kMode == kDistill ? a.top_k : 1, threads = blockDim.x, tid = threadIdx.x;
+    const int warp = tid >> 5, lane = tid & 31;
+    int32_t *ids = reinterpret_cast<int32_t *>(s_lists);
+    float *probs = s_lists + top_k, *logs = probs + top_k, *zs = logs + top_k;
+    const float c = a.log2e_over_t;
+    grid_dependency_release();            // the sum over rows may be set up meanwhile
+    const int64_t row = blockIdx.x;
+    const T *z = static_cast<const T *>(a.logits) + row * a.stride;
+    T *g = kGrad ? static_cast<T *>(a.grad) + row * a.grad_stride : nullptr;
+    const int vocab = (int)a.vocab;
+    const int to_boundary = (int)((16u - (unsigned)(reinterpret_cast<uintptr_t>(z) & 15u)) & 15u) / (int)sizeof(T);
+    const int head = to_boundary < vocab ? to_boundary : vocab, count = (vocab - head) / E;
+    const bool same_offset = kGrad && ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(g)) & 15u) == 0;
+    // single elements: the head by the first threads, the tail by others
+    int edge = -1;
+    if (tid < head) edge = tid;
+    else if (tid >= 8 && tid < 16 && head + count * E + (tid - 8) < vocab) edge = head + count * E + (tid - 8);
+
+    const float w = a.weight ? a.weight[row] : 1.0f;
+    int64_t token = -1;
+    if (kMode == kPolicy) token = load_id(a.ids, row, a.ids_dtype);
+    bool live = w != 0.0f && (kMode == kDistill || (token >= 0 && token < a.vocab));
+    uint4 q[kShortVectors];
+    float edge_z = -kInf;
+    if (live) {
+#pragma unroll
+        for (int i = 0; i < kShortVectors; ++i)
+            q[i] = tid + i * threads < count ? __ldcs(reinterpret_cast<const uint4 *>(z + head) + tid + i * threads) : nothing<T>();
+        if (edge >= 0) edge_z = to_f32(z[edge]);
+        if (warp == 0) {
+            bool any = true;
+            if (kMode == kDistill) {
+                any = load_teacher<T>(a, row, ids, probs, logs, zs);
+            } else if (lane == 0) {
+                ids[0] = (int32_t)token;
+                probs[0] = 1.0f;
+                zs[0] = to_f32(z[token]);
+            }
+            if (lane == 0) s_any = any;
+        }
+    }
+    const auto put = [&](const Vals<E> &v, int i) {
+        T *at = g + head + (int64_t)i * E;
+        if (same_offset) {
+            *reinterpret_cast<uint4 *>(at) = narrow16<T>(v);
+        } else {
+            float f[E];
+            v.get(f);
+#pragma unroll
+            for (int k = 0; k < E; ++k) at[k] = from_f32<T>(f[k]);
+        }
+    };
+
+    Vals<E> e[kShortVectors];
+    MaxSum ms{-kInf, 0.0f};
+    if (live) {
+        float top = edge_z == edge_z ? edge_z : -kInf;
+#pragma unroll
+        for (int i = 0; i < kShortVectors; ++i) top = fmaxf(top, largest<T>(q[i]));
+        const float base = top == -kInf ? 0.0f : top, ref = base * c;
+        Vals<E> sum;
+        sum.set(0.0f);
+#pragma unroll
+        for (int i = 0; i < kShortVectors; ++i) {
+            e[i] = plain(ref) ? exponentials<true>(widen16<T>(q[i]), base, ref, c) : exponentials<false>(widen16<T>(q[i]), base, ref, c);
+            sum = sum + e[i];
+        }
+        if (edge >= 0) edge_z = exp2_fast(exponent_of(edge_z, base, c));
+        ms = MaxSum{top, total(sum) + (edge >= 0 ? edge_z : 0.0f)};
+        const MaxSum joined = join_lanes(ms, c);
+        if (lane == 0) s_warp[warp] = joined;
+    }
+    __syncthreads();
+    live = live && s_any;
+    if (!live) {
+        if (kGrad) {
+            Vals<E> none;
+            none.set(0.0f);
+            for (int i = tid; i < count; i += threads) put(none, i);
+            if (edge >= 0) g[edge] = from_f32<T>(0.0f);
+        }
+        if (tid == 0) {
+            a.row_loss[row] = 0.0f;
+            if (kMode == kPolicy && a.logp) a.logp[row] = 0.0f;
+        }
+        return;
+    }
+    if (warp == 0) {
+        const MaxSum all = join_lanes(lane < threads / 32 ? s_warp[lane] : MaxSum{-kInf, 0.0f}, c);
+        const float log_s = logf(all.s);
+        const auto log_q = [&](float x) { return fmaf(exponent_of(x, all.m, c), kLn2, -log_s); };
+        float coef, loss, slope;
+        if (kMode == kDistill) {
+            loss = distill_row_loss(a, ids, probs, logs, zs, log_q);
+            coef = a.grad_scale * w * a.temperature;
+        } else {
+            const float logp = log_q(zs[0]);
+            policy_row(a, logp, a.advantage[row], a.old_logp ? a.old_logp[row] : 0.0f, a.ref_logp ? a.ref_logp[row] : 0.0f, loss, slope);
+            if (lane == 0 && a.logp) a.logp[row] = logp;
+            coef = -a.grad_scale * w * slope * a.inv_temperature;
+        }
+        if (lane == 0) {
+            a.row_loss[row] = loss;
+            s_result = make_float4(all.m, log_s, 1.0f / all.s, coef);
+        }
+    }
+    if (!kGrad) return;
+    __syncthreads();
+    const float4 done = s_result;
+    // a thread without a finite element has exponentials of 0, or NaN that stay so
+    const float scaled = done.w * done.z * (ms.m == -kInf ? (done.x == -kInf ? kNan : 1.0f) : rescale(ms.m, done.x, c));
+#pragma unroll
+    for (int i = 0; i < kShortVectors; ++i)
+        if (tid + i * threads < count) put(e[i] * scaled, tid + i * threads);
+    if (edge >= 0) g[edge] = from_f32<T>(edge_z * scaled);
+    __syncthreads();
+    for (int k = tid; k < top_k; k += threads) {
+        const int32_t id = ids[k];
+        if (id < 0) continue;
+        float p = 0.0f;
+        for (int i = 0; i < top_k; ++i)
+            if (ids[i] == id) p += probs[i];
+        g[id] = from_f32<T>(done.w * fmaf(exp2_fast(exponent_of(zs[k], done.x, c)), done.z, -p));
+    }
+}
+
 // The rows of a cluster, in ascending order, by one warp.  Where a cluster has many long
 // rows (`balance`), masked rows, which cost less than the others, are dealt out
 // separately, both kinds in turn by their own count: the warp looks at 32 rows at a
@@ -1096,6 +1239,13 @@ so_status launch_ring(const LossArgs &a, const RingShape &shape, int sms, cudaSt
 template <typename T, int kMode>
 so_status launch_loss(const LossArgs &a, int sms, cudaStream_t st)
 {
+    const int64_t vectors = a.vocab / Vec<T>::kElems;
+    if (vectors <= kShortVectors * kShortThreads && a.rows <= INT32_MAX) {
+        const int per_thread = (int)((vectors + kShortVectors - 1) / kShortVectors);
+        const unsigned threads = per_thread <= 32 ? 32u : (unsigned)((per_thread + 31) / 32 * 32);
+        const size_t lists = (size_t)16 * (kMode == kDistill ? a.top_k : 1);
+        return launch(a.grad ? loss_short_kernel<T, kMode, true> : loss_short_kernel<T, kMode, false>, (unsigned)a.rows, threads, lists, st, false, a);
+    }
     RingShape shape;
     if (ring_shape(a.rows, a.vocab, (int)sizeof(T), kMode == kDistill ? a.top_k : 1, a.grad != nullptr, sms, &shape))
     {
