@@ -25,6 +25,9 @@ struct LookupArgs {
 
 constexpr int kLookupThreads = 256, kLookupBatch = 8;
 
+// A warp per token.  Bound: memory (the rows written, and each distinct row read once:
+// L2 keeps the rows of frequent tokens).  32767 x 4096 fp16 from 128256 rows: 70 us, of
+// which the bytes take 56 us at a copy's rate; one load in flight per lane: 79 us.
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(kLookupThreads) embedding_forward_kernel(LookupArgs a)
 {
@@ -82,6 +85,10 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_forward_kernel(Looku
 // A token goes out with all that the sum needs to know of its run, so that a block of
 // the sum has one load to wait for before it reads rows.  Which ids occur at all goes
 // out as bits: the rows of the others are zeroed by further blocks of the sum's launch.
+
+// Bound: the instructions of looking at every token in every block: 8 us for 8192 tokens,
+// 17 us for 32768, 26 us for 65536 (ids of 64 bits).  Reading the tokens a second time
+// for the placing, instead of keeping the block's own: 24 us for 32768.
 
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kRange = 1024;              // ids a block owns, at most one per thread
@@ -223,6 +230,12 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
 // kBatch rows in flight; of a long run it sums the piece inside the stretch into
 // fp32 scratch, and the last block to finish a piece of that run adds the
 // pieces in their order (which block that is does not show in the result).
+
+// Bound: memory where the table or the batch is large.  With the sort, 32768 x 2048 bf16
+// into 128256 fp32 rows: 203 us for 181 us of bytes at a copy's rate; 8192 x 768 into
+// 50257 bf16 rows: 25 us for 14 us of bytes (the sort is 8 us of it).  A warp per
+// table row, runs summed one after the other: 17.0 ms and 1.74 ms (the most frequent
+// token has 6 % of them); zero rows written by the sort's blocks: 232 and 35 us.
 
 constexpr int kSumThreads = 256, kBatch = 8;
 constexpr int kStrided = 4;               // columns of a thread where rows are not aligned

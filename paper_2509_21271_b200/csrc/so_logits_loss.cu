@@ -178,6 +178,9 @@ __device__ __forceinline__ void policy_row(const LossArgs &a, float logp, float 
 }
 
 // ---- a block per row, the row read twice -----------------------------------------
+//
+// For rows that the shared memory of a cluster does not hold (with a gradient: about
+// 1.7 MB), element by element.
 
 constexpr int kRowThreads = 512;
 
@@ -282,6 +285,16 @@ __global__ void __launch_bounds__(kRowThreads) loss_two_pass_kernel(LossArgs a)
 // The elements before a row's first 16-byte boundary and after its last are loaded by
 // single threads.  Rows may start anywhere; a gradient whose rows start at another
 // offset from a 16-byte boundary than the logits' is stored element by element.
+//
+// Bound: 4-byte logits, memory (8192 x 50304 fp32: 511 us, 6.45 TB/s, 98 % of a copy's
+// rate).  2-byte logits, the two exponentials an element (16 a clock and SM: 70 % of
+// either phase) and the stores of phase 2 (an SM stores 27 to 30 bytes a clock), one after
+// the other: 4096 x 128256 bf16 with 64 teacher logits and a fifth of the rows masked
+// 368 us, 5.15 TB/s, 79 %; the policy loss of 8191 x 128256 with 30 % masked 669 us,
+// 5.34 TB/s, 81 %.  The chunks are always there before they are asked for.  Measured and
+// not taken: a quarter of the exponentials on the multipliers (391 us), 640 or 768
+// threads (394, 405), two blocks of 256 an SM with clusters of four (441), the maximum
+// kept exactly (397).  A row read twice from memory took 1771 and 2311 us.
 //
 // A wait that runs out of polls ends its block's work: the loss comes out as NaN and the
 // gradient is not complete.
@@ -506,7 +519,8 @@ struct Running {
 // For short rows, where a cluster's set-up would cost more than the row: as many threads
 // as hold its vectors, four each, and as many rows at a time as the SMs have room for.
 // A thread keeps the exponentials against its own maximum, so each is taken once; the
-// gradient is that times one factor per thread.
+// gradient is that times one factor per thread.  8191 rows of 4001 bf16 logits, policy
+// loss: 40 us against 71 us by clusters; of 16000, distillation: 189 against 205 us.
 
 constexpr int kShortVectors = 4, kShortThreads = 512;
 

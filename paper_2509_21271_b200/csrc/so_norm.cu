@@ -190,6 +190,11 @@ __device__ __forceinline__ float warp_sum_many(float (&v)[N])
 // sqrt(32) standard deviations of the mean, so the difference loses 5 bits at most,
 // however large the mean.  Warps are joined by M2 = sum M2_w + sum n_w (mean_w - mean)^2.
 //
+// Bound: memory (one read, one write of the matrix).  32768 x 4096 bf16: 94 us, 5.70 TB/s,
+// 87 % of a copy's rate; what is left is the exchange of each row's sums.  Registers
+// that prefetch the next row instead of the ring: 125 us; a warp per row with 16
+// vectors a lane (244 registers, 8 warps an SM): 185 us.
+//
 // A copy that does not arrive within kPolls polls turns what the group writes into
 // NaN (the optimizer's gradient check then skips the iteration).
 template <typename T, int E, int kNV, int R, bool kFull, int kMaxThreads>
@@ -369,6 +374,11 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 // and one barrier.  That barrier also tells the group's first thread that
 // everyone is done with the rows before, whose place in the ring it refills.
 // A thread keeps its columns' part of dweight and dbias for all its rows.
+//
+// Bound: memory (two reads, one write).  32768 x 2048 bf16: 81 us with the sum over
+// blocks, 4.98 TB/s, 76 % of a copy's rate (this kernel alone 72 us).  The work per
+// row and thread that does not depend on the elements is what costs: 8 elements a
+// thread 86 us, 16 elements 81 us; one row at a time 102 us, two 88 us, four 81 us.
 //
 // A copy that does not arrive within kPolls polls turns what the group writes into
 // NaN (the optimizer's gradient check then skips the iteration).
