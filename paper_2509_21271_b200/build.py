@@ -37,7 +37,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         return LIB_PATH
     tmp = LIB_PATH + f".tmp{os.getpid()}"
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3",
-           "-std=c++17", "--fmad=false", "-Xcompiler", "-fPIC,-O2,-Wall", "-shared",
+           "-std=c++17", "--fmad=false", "--threads=0", "-Xcompiler", "-fPIC,-O2,-Wall", "-shared",
            "-I", INCLUDE, "-I", CSRC, "-o", tmp] + SOURCES
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
