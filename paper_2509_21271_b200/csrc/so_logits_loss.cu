@@ -459,13 +459,18 @@ __device__ __forceinline__ Vals<E> exponentials(const Vals<E> &z, float m, float
 }
 
 // Running sum of a thread, against a reference that need not be the maximum: it is the
-// largest of the first vectors that have a finite element.  What fp32 holds leaves room
-// for elements a factor of 2^127 above it.  Where the row stays at hand, the elements after
-// that are added without a look at their size, and a sum that came out infinite is done
-// again with one; otherwise the reference moves when something exceeds it by a factor of
-// 2^kSlack.  (Were it the maximum, some lane of a warp would move it with almost every
-// vector.)
-constexpr float kSlack = 16.0f;
+// largest of the first vectors that have a finite element.  Where the row stays at hand, the
+// elements after that are added without a look at their size, and a sum that came out above
+// kMost is done again with one; otherwise the reference moves when something exceeds it by
+// a factor of 2^kSlack.  (Were it the maximum, some lane of a warp would move it with almost
+// every vector.)
+//
+// kMost is far below what fp32 holds, for three reasons.  The sums of a cluster's 4096
+// threads are added: 2^72 at most.  A sum is taken to a reference above its own by a factor
+// that the exponential unit flushes to 0 below 2^-126: what is lost of a sum of 2^60 is
+// below 2^-66 of the total.  And the gradient's factor coef / S has to be a normal number:
+// it is, down to |coef| = 2^-54.  Exponents up to 60 round to 2^-19, 1.3e-6 of an exponential.
+constexpr float kSlack = 16.0f, kMost = 0x1p60f;
 
 template <typename T>
 struct Running {
@@ -476,8 +481,8 @@ struct Running {
 
     __device__ __forceinline__ Running() : m(-kInf), ref(0.0f), bound(-kInf), is_plain(false) { s.set(0.0f); }
 
-    // Against the reference as it is, if there is one.  An element that exceeds it by 2^128
-    // or more makes the sum infinite, for the caller to find.
+    // Against the reference as it is, if there is one.  The sum may exceed kMost, up to
+    // infinity, for the caller to find.
     template <int N>
     __device__ __forceinline__ void add_unchecked(const uint4 (&v)[N], float c, float slack)
     {
@@ -1026,7 +1031,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
                     advance(place);
                 }
                 MaxSum ms{run.m, total(run.s)};
-                if (kGrad && !(ms.s < kInf)) {
+                if (kGrad && !(ms.s < kMost)) {
                     // once more, with a look at every vector's largest element
                     run = Running<T>();
                     Place there = place0;

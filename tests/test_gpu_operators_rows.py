@@ -1,0 +1,71 @@
+"""Losses on logits whose rows are far from even: elements that lie up to 88 nats
+above what the kernels see of the row first, with weights as small as those of a
+large batch.  References, tolerances and their derivation: ``test_gpu_operators``."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2509_21271_b200 import build as so_build
+from test_gpu_operators import BF16, FP16, FP32, check_distill, check_policy, gen, randn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    so_build.build_library()
+    torch.cuda.set_device(0)
+
+
+# 2^60 is 41.6 nats, 2^100 69.3, 2^128 88.7
+HEIGHTS = (20.0, 30.0, 41.5, 43.0, 60.0, 70.0, 77.0, 80.0, 82.0, 85.0, 86.0, 88.5)
+
+
+def uneven_rows(rows, vocab, dtype, temperature, kind, first):
+    """Logits whose first `first` elements (or, at "shares", the first of every eighth) lie
+    a height below the others; at "spikes" all are level but for a few."""
+    h = torch.tensor(HEIGHTS, device="cuda")[torch.arange(rows, device="cuda") % len(HEIGHTS)] * temperature
+    at = torch.arange(vocab, device="cuda")
+    noise = 0.05 * temperature * randn(gen(rows + vocab), rows, vocab)
+    if kind == "spikes":
+        up = torch.zeros(vocab, dtype=torch.bool, device="cuda")
+        up[torch.tensor([10_000, 20_000, 20_001, vocab - 9_000], device="cuda")] = True
+        z = torch.where(up, h[:, None].expand(rows, vocab), noise)
+    elif kind == "prefix":
+        z = torch.where(at < first, -h[:, None], 0.0) + noise
+    else:
+        z = torch.where(at % (vocab // 8 + 1) < first, -h[:, None], 0.0) + noise
+    return z.to(dtype)
+
+
+# (rows, vocabulary): one block a row, two, eight
+@pytest.mark.parametrize("rows,vocab", [(180, 50_257), (160, 128_256), (13, 128_256)])
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("temperature", [1.0, 0.1])
+@pytest.mark.parametrize("kind,first", [("spikes", 0), ("prefix", 2048), ("prefix", 4096), ("prefix", 8192), ("shares", 8192)])
+def test_losses_of_rows_that_rise_above_what_is_seen_first(rows, vocab, dtype, temperature, kind, first):
+    z = uneven_rows(rows, vocab, dtype, temperature, kind, first)
+    ids = torch.tensor([3, 9_999, 10_000, 20_001, vocab - 1], device="cuda").expand(rows, 5).contiguous()
+    teacher = randn(gen(8), rows, 5) * temperature
+    # a mean over 8192 rows, as a loss scale carries it to fp16
+    weight = torch.full((rows,), 1 / 8192, device="cuda")
+    scale = 2.0 ** 20 if dtype == FP16 else 1.0
+    check_distill(z, ids, teacher, weight, temperature, scale)
+    check_distill(z, ids, teacher, weight, temperature, grad=False)
+    tokens = ids[:, 2].clone()
+    tokens[::2] = 3
+    adv = randn(gen(9), rows)
+    check_policy(z, tokens, adv, weight, temperature=temperature, grad_scale=scale)
+
+
+@pytest.mark.parametrize("height", [40.0, 69.0, 77.0, 88.0])
+@pytest.mark.parametrize("weight", [1e-6, 1e-12])
+def test_small_weights_keep_the_gradients_digits(height, weight):
+    """coef / S stays a normal number: fp32 gradients of rows whose sum is large against
+    the first elements, with small coefficients."""
+    z = torch.zeros(90, 50_257, device="cuda")
+    z[:, :8192] = -height
+    ids = torch.full((90, 1), 30_000, device="cuda")
+    check_distill(z, ids, torch.zeros(90, 1, device="cuda"), torch.full((90,), weight, device="cuda"))
+    check_policy(z, ids[:, 0].contiguous(), torch.ones(90, device="cuda"), torch.full((90,), weight, device="cuda"))
