@@ -686,27 +686,30 @@ inline Plan make_plan(int64_t vectors, int nv)
 
 constexpr int kMaxShared = 220 * 1024;    // dynamic shared memory of a block, at most
 
-// Resident blocks per SM of a kernel, asked for once per device.
+// Resident blocks per SM of a kernel, asked for again only when its block or its shared
+// memory changes.  The grid follows from the answer, and with it the order in which the
+// backward pass sums dweight and dbias: the key is exact, so that a width's sums do not
+// depend on the widths called before it.
 template <typename K>
-so_status resident(K kernel, int block, size_t smem, std::atomic<int> (&cache)[kMaxDevices], int *out)
+so_status resident(K kernel, int block, size_t smem, std::atomic<uint64_t> (&cache)[kMaxDevices], int *out)
 {
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return SO_ERR_CUDA;
     if (dev < 0 || dev >= kMaxDevices) return SO_ERR_UNSUPPORTED;
     // one word: the block size and shared memory it was asked for, and the answer
-    const int tag = (block / 32) << 13 | (int)(smem >> 10) << 5;
-    int v = cache[dev].load(std::memory_order_relaxed);
-    if (v == 0 || (v & ~31) != tag) {
+    const uint64_t tag = (uint64_t)smem << 24 | (uint64_t)block << 8;
+    uint64_t v = cache[dev].load(std::memory_order_relaxed);
+    if ((v & ~uint64_t(255)) != tag) {
         int n = 0;
         if (smem > 40 * 1024 &&
             cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxShared) != cudaSuccess)
             return SO_ERR_CUDA;
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, block, smem) != cudaSuccess || n < 1)
             return SO_ERR_CUDA;
-        v = tag | (n < 31 ? n : 31);
+        v = tag | (uint64_t)(n < 255 ? n : 255);
         cache[dev].store(v, std::memory_order_relaxed);
     }
-    *out = v & 31;
+    *out = (int)(v & 255);
     return SO_OK;
 }
 
@@ -734,7 +737,7 @@ so_status launch_forward_ring(const NormArgs &a, const Plan &p, int sms, cudaStr
     const int groups = p.block / p.per_row;
     const size_t stage = ring_pitch<T, E>(a.cols) * R * groups;
     const int stages = ring_stages(stage, groups);
-    static std::atomic<int> cache[kMaxDevices];
+    static std::atomic<uint64_t> cache[kMaxDevices];
     int per_sm = 0;
     const auto kernel = norm_forward_ring_kernel<T, E, kNV, R, kFull, kMaxThreads>;
     const so_status s = resident(kernel, p.block, stage * stages, cache, &per_sm);
@@ -749,7 +752,7 @@ so_status launch_backward_ring(const NormArgs &a, const Plan &p, int sms, cudaSt
     const int groups = p.block / p.per_row;
     const size_t stage = ring_pitch<T, E>(a.cols) * 2 * R * groups;
     const int stages = ring_stages(stage, groups);
-    static std::atomic<int> cache[kMaxDevices];
+    static std::atomic<uint64_t> cache[kMaxDevices];
     int per_sm = 0;
     const auto kernel = norm_backward_ring_kernel<T, E, kNV, R, kFull, kMaxThreads>;
     const so_status s = resident(kernel, p.block, stage * stages, cache, &per_sm);
