@@ -220,9 +220,11 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         if (has(i)) mine_n += E;
     const float inv_n = mine_n > 0.0f ? 1.0f / mine_n : 0.0f, warp_n = warp_sum(mine_n);
     if (lane == 0) s_count[threadIdx.x >> 5] = warp_n;
-    if (threadIdx.x < (unsigned)(g.per_block * stages)) mbar_init(smem_addr(s_full + threadIdx.x), 1);
+    if (threadIdx.x < (unsigned)(g.per_block * stages)) {
+        mbar_init(smem_addr(s_full + threadIdx.x), 1);
+        mbar_init_fence();                // before any group's first thread issues a copy
+    }
     __syncthreads();
-    mbar_init_fence();
     const float first_inv = 1.0f / s_count[g.index * g.warps];
 
     const auto load_rows = [&](int64_t from, int s) {
@@ -398,9 +400,11 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     const int64_t step = (int64_t)gridDim.x * g.per_block * R;
     const int64_t row = ((int64_t)blockIdx.x * g.per_block + g.index) * R;
     const auto has = [&](int i) { return kFull || (g.thread + i * g.threads) * E < cols; };
-    if (threadIdx.x < (unsigned)(g.per_block * stages)) mbar_init(smem_addr(s_full + threadIdx.x), 1);
+    if (threadIdx.x < (unsigned)(g.per_block * stages)) {
+        mbar_init(smem_addr(s_full + threadIdx.x), 1);
+        mbar_init_fence();                // before any group's first thread issues a copy
+    }
     __syncthreads();
-    mbar_init_fence();
     grid_dependency_release();            // the sum over blocks may be set up meanwhile
 
     // the group's first thread: the copies of the R rows from `from`, into stage s
