@@ -122,6 +122,9 @@ struct RowCopies {
                 to = whole - 16;
                 for (uint32_t i = to < before ? before : to; i < before + bytes; i += sizeof(T)) put(dst + i, src + (i - before));
             }
+            // ordinary stores into a place that a later bulk copy will overwrite: ordered between
+            // the two kinds of access here, by the thread that issues that copy (two rows have any)
+            if (from != 0 || to != whole) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             if (to > from) {
                 asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(to - from) : "memory");
                 bulk_load(dst + from, src - before + from, to - from, bar);
