@@ -648,6 +648,14 @@ so_status so_policy_loss(const void *logits, int64_t logits_stride, const void *
                          double kl_coef, double grad_scale, void *grad, int64_t grad_stride,
                          float *logp, float *row_loss, float *loss, void *stream);
 
+/* How many times the operators' kernels poll for a copy or an exchange between
+ * blocks before they give up (0 .. 2^20, the default): in the block or cluster
+ * `unit` of each launch, or with -1 in all of them.  What gives up comes out as
+ * NaN and nowhere as a plausible number.  As in so_debug_set_spin_limit the waits
+ * that drain copies in flight always use the full limit, so 0 is how that path is
+ * tested.  For the whole process; applies to launches made after the call. */
+so_status so_debug_set_operator_polls(int64_t polls, int32_t unit);
+
 #ifdef __cplusplus
 }
 #endif

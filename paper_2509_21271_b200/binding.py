@@ -89,7 +89,7 @@ EXPORTS = ["so_layout_init", "so_layout_get_info", "so_layout_tensor", "so_layou
            "so_debug_set_dry_run", "so_debug_set_bucket_stats", "so_debug_set_step_variant",
            "so_layer_norm_forward", "so_layer_norm_backward_scratch", "so_layer_norm_backward",
            "so_embedding_forward", "so_embedding_backward_scratch", "so_embedding_backward",
-           "so_distill_loss", "so_policy_loss"]
+           "so_distill_loss", "so_policy_loss", "so_debug_set_operator_polls"]
 
 
 def lib() -> C.CDLL:
@@ -137,6 +137,7 @@ def lib() -> C.CDLL:
         "so_debug_set_dry_run": [vp, i32],
         "so_debug_set_bucket_stats": [vp, i32, dbl, i32],
         "so_debug_set_step_variant": [vp, i32],
+        "so_debug_set_operator_polls": [i64, i32],
         "so_layer_norm_forward": [vp, i64, vp, vp, vp, i64, vp, vp, i64, i64, i32, i32, dbl, vp],
         "so_layer_norm_backward_scratch": [i64, i64, P(C.c_uint64)],
         "so_layer_norm_backward": [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, i64, i64, i32, i32,
@@ -440,3 +441,7 @@ def so_distill_loss(*args) -> None:
 
 def so_policy_loss(*args) -> None:
     _ok(None, lib().so_policy_loss(*args), "so_policy_loss")
+
+
+def so_debug_set_operator_polls(polls: int, unit: int = -1) -> None:
+    _ok(None, lib().so_debug_set_operator_polls(polls, unit), "so_debug_set_operator_polls")

@@ -20,6 +20,7 @@ struct NormArgs {
     int64_t x_stride, dy_stride, y_stride, rows, cols;
     int32_t param_dtype;
     float eps, inv_cols;
+    Patience patience;
 };
 
 // ---- rows through shared memory ----------------------------------------------------
@@ -180,6 +181,28 @@ __device__ __forceinline__ float warp_sum_many(float (&v)[N])
     return r;
 }
 
+// The wait for a stage, once a look has not found it there.  What a group's threads know
+// of a wait that ran out is in shared memory: a register for it would be one too many.
+__device__ __forceinline__ bool has_given_up(uint32_t flag)
+{
+    uint32_t v;
+    asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(v) : "r"(flag));
+    return v != 0;
+}
+__device__ __forceinline__ void wait_or_give_up(uint32_t bar, uint32_t parity, uint32_t polls, uint32_t flag)
+{
+    if (!has_given_up(flag) && !mbar_wait(bar, parity, polls))
+        asm volatile("st.volatile.shared.u32 [%0], 1;" ::"r"(flag) : "memory");
+}
+
+// Waits, with the full limit, for the last fills of a ring: fill k went into stage
+// k % stages, and one is issued only when the one before it in its stage has been seen.
+__device__ __forceinline__ void land(uint32_t bars, int issued, int stages)
+{
+    for (int k = issued > stages ? issued - stages : 0; k < issued; ++k)
+        mbar_wait(bars + (k % stages) * 8, (uint32_t)(k / stages) & 1u, kPolls);
+}
+
 // Forward: rows come through a ring of bulk copies in shared memory, so that no register waits for memory and the loads of several
 // groups of rows are always on their way.  A group takes R rows at a time, whose
 // sums share one exchange and one barrier; that barrier also tells the group's
@@ -198,8 +221,9 @@ __device__ __forceinline__ float warp_sum_many(float (&v)[N])
 // that prefetch the next row instead of the ring: 125 us; a warp per row with 16
 // vectors a lane (244 registers, 8 warps an SM): 185 us.
 //
-// A copy that does not arrive within kPolls polls turns what the group writes into
-// NaN (the optimizer's gradient check then skips the iteration).
+// A copy that does not arrive in time turns the rows that the group has not written into
+// NaN, statistics and gradients of the weights included (the optimizer's gradient check
+// then skips the iteration).
 template <typename T, int E, int kNV, int R, bool kFull, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 1) norm_forward_ring_kernel(NormArgs a, int per_row, int stages)
 {
@@ -208,6 +232,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     __shared__ __align__(16) float s_part[2][32][kSums], s_centre[2][32][R];
     __shared__ float s_count[32];
     __shared__ __align__(8) uint64_t s_full[kRingBars];
+    __shared__ int s_issued[kGroupThreads / 32];         // fills of a group's stages so far
+    __shared__ int s_gave_up[kGroupThreads / 32];        // a wait of the group ran out
     const Group g(per_row);
     const int cols = (int)a.cols, lane = threadIdx.x & 31;
     const RowCopies<T, E> xs(a.x, a.x_stride, a.rows, a.cols);
@@ -227,6 +253,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         mbar_init(smem_addr(s_full + threadIdx.x), 1);
         mbar_init_fence();                // before any group's first thread issues a copy
     }
+    if (g.thread == 0) s_gave_up[g.index] = a.patience.of((int)blockIdx.x) == 0;
     __syncthreads();
     const float first_inv = 1.0f / s_count[g.index * g.warps];
 
@@ -237,9 +264,11 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         for (int r = 0; r < n; ++r) xs.load(from + r, dst + r * xs.pitch, bar);
         if (E == 1) mbar_arrive(bar);
     };
-    if (g.thread == 0)
-        for (int s = 0; s < stages; ++s)
-            if (row + s * step < a.rows) load_rows(row + s * step, s);
+    if (g.thread == 0) {
+        int n = 0;
+        for (; n < stages && row + n * step < a.rows; ++n) load_rows(row + n * step, n);
+        s_issued[g.index] = n;
+    }
 
     Vals<E> w[kNV], b[kNV];
 #pragma unroll
@@ -250,15 +279,14 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         }
     T *y = static_cast<T *>(a.y) + row * a.y_stride + g.thread * E;
     const int64_t y_step = (step - R) * a.y_stride;
-    float *mean_to = a.mean ? a.mean + row + g.thread : nullptr, *rstd_to = a.rstd + row + g.thread;
     constexpr uint32_t kBytes = E * sizeof(T);
     const uint32_t mine = ring + (uint32_t)g.thread * kBytes, vector_step = (uint32_t)g.threads * kBytes;
-    uint32_t limit = kPolls, phase = 0;
+    uint32_t phase = 0;
     int stage = 0, turn = 0;
     bool first = true;
 
     for (int64_t left = a.rows - row; left > 0; left -= step) {
-        if (limit != 0 && !mbar_wait(bars + stage * 8, phase, limit)) limit = 0;
+        if (!mbar_test(bars + stage * 8, phase)) wait_or_give_up(bars + stage * 8, phase, a.patience.of((int)blockIdx.x), smem_addr(s_gave_up + g.index));
         const uint32_t at = mine + stage * stage_bytes;
         const int n = left < R ? (int)left : R;
         const auto row_at = [&](int r) { return at + r * xs.pitch + xs.shift(a.rows - left + r); };
@@ -302,10 +330,14 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         }
         if (g.warps > 1) g.sync();
         else __syncwarp();
-        if (g.thread == 0 && !first && limit != 0) {      // the stage before this one is free
+        const bool gave_up = has_given_up(smem_addr(s_gave_up + g.index));
+        if (g.thread == 0 && !first && !gave_up) {      // the stage before this one is free
             const int before = stage == 0 ? stages - 1 : stage - 1;
             const int64_t ahead = (int64_t)(stages - 1) * step;
-            if (left > ahead) load_rows(a.rows - left + ahead, before);
+            if (left > ahead) {
+                load_rows(a.rows - left + ahead, before);
+                ++s_issued[g.index];
+            }
         }
         first = false;
         // the warps' sums, moved to a common centre (the first warp's mean), one warp a lane
@@ -342,10 +374,11 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             rstd[r] = 1.0f / sqrtf(fmaf(fmaxf(m2[r], 0.0f), a.inv_cols, a.eps));
-            if (limit == 0 || m2[r] != m2[r]) rstd[r] = kNan;
-            if (mean_to && g.thread == r && r < n) {
-                *mean_to = mean[r];
-                *rstd_to = rstd[r];
+            if (m2[r] != m2[r]) rstd[r] = kNan;
+            if (gave_up) mean[r] = rstd[r] = kNan;
+            if (a.mean && g.thread == r && r < n) {
+                a.mean[a.rows - left + r] = mean[r];
+                a.rstd[a.rows - left + r] = rstd[r];
             }
         }
 #pragma unroll
@@ -360,18 +393,13 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
                 y += a.y_stride;
             }
         y += y_step;
-        if (mean_to) {
-            mean_to += step;
-            rstd_to += step;
-        }
         if (++stage == stages) {
             stage = 0;
             phase ^= 1;
         }
     }
-    // let the copies that were issued land before the block goes
-    if (limit == 0)
-        for (int s = 0; s < stages; ++s) mbar_wait(bars + s * 8, phase ^ (s < stage ? 0u : 1u), kPolls);
+    // the copies that were issued land before the block goes (all have, unless the wait ran out)
+    if (s_gave_up[g.index] && g.thread == 0) land(bars, s_issued[g.index], stages);
     __syncthreads();
 }
 
@@ -385,8 +413,9 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 // row and thread that does not depend on the elements is what costs: 8 elements a
 // thread 86 us, 16 elements 81 us; one row at a time 102 us, two 88 us, four 81 us.
 //
-// A copy that does not arrive within kPolls polls turns what the group writes into
-// NaN (the optimizer's gradient check then skips the iteration).
+// A copy that does not arrive in time turns the rows that the group has not written into
+// NaN, statistics and gradients of the weights included (the optimizer's gradient check
+// then skips the iteration).
 template <typename T, int E, int kNV, int R, bool kFull, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 1) norm_backward_ring_kernel(NormArgs a, int per_row, int stages)
 {
@@ -394,6 +423,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     constexpr int kSums = 2 * R;          // of each row: sum(g), sum(g xhat)
     __shared__ __align__(16) float s_part[2][32][kSums];
     __shared__ __align__(8) uint64_t s_full[kRingBars];
+    __shared__ int s_issued[kGroupThreads / 32];         // fills of a group's stages so far
+    __shared__ int s_gave_up[kGroupThreads / 32];        // a wait of the group ran out
     const Group g(per_row);
     const int cols = (int)a.cols;
     const RowCopies<T, E> xs(a.x, a.x_stride, a.rows, a.cols), ys(a.dy, a.dy_stride, a.rows, a.cols);
@@ -407,6 +438,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         mbar_init(smem_addr(s_full + threadIdx.x), 1);
         mbar_init_fence();                // before any group's first thread issues a copy
     }
+    if (g.thread == 0) s_gave_up[g.index] = a.patience.of((int)blockIdx.x) == 0;
     __syncthreads();
     grid_dependency_release();            // the sum over blocks may be set up meanwhile
 
@@ -421,9 +453,11 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         }
         if (E == 1) mbar_arrive(bar);
     };
-    if (g.thread == 0)
-        for (int s = 0; s < stages; ++s)
-            if (row + s * step < a.rows) load_rows(row + s * step, s);
+    if (g.thread == 0) {
+        int n = 0;
+        for (; n < stages && row + n * step < a.rows; ++n) load_rows(row + n * step, n);
+        s_issued[g.index] = n;
+    }
 
     Vals<E> w[kNV], dw[kNV], db[kNV];
     float mean[R], rstd[R];
@@ -448,12 +482,12 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
     const int64_t dx_step = (step - R) * a.y_stride;
     constexpr uint32_t kBytes = E * sizeof(T);
     const uint32_t mine = ring + (uint32_t)g.thread * kBytes, vector_step = (uint32_t)g.threads * kBytes;
-    uint32_t limit = kPolls, phase = 0;
+    uint32_t phase = 0;
     int stage = 0, turn = 0;
     bool first = true;
 
     for (; left > 0; left -= step) {
-        if (limit != 0 && !mbar_wait(bars + stage * 8, phase, limit)) limit = 0;
+        if (!mbar_test(bars + stage * 8, phase)) wait_or_give_up(bars + stage * 8, phase, a.patience.of((int)blockIdx.x), smem_addr(s_gave_up + g.index));
         const uint32_t at = mine + stage * stage_bytes;
         const int n = left < R ? (int)left : R;
         const auto x_at = [&](int r) { return at + r * 2 * xs.pitch + xs.shift(a.rows - left + r); };
@@ -488,10 +522,14 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         if (lane % (32 / kSums) == 0) part[g.warp][lane / (32 / kSums)] = one;
         if (g.warps > 1) g.sync();
         else __syncwarp();
-        if (g.thread == 0 && !first && limit != 0) {      // the stage before this one is free
+        const bool gave_up = has_given_up(smem_addr(s_gave_up + g.index));
+        if (g.thread == 0 && !first && !gave_up) {      // the stage before this one is free
             const int before = stage == 0 ? stages - 1 : stage - 1;
             const int64_t ahead = (int64_t)(stages - 1) * step;
-            if (left > ahead) load_rows(a.rows - left + ahead, before);
+            if (left > ahead) {
+                load_rows(a.rows - left + ahead, before);
+                ++s_issued[g.index];
+            }
         }
         first = false;
         Vals<kSums> all;
@@ -508,7 +546,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
         for (int r = 0; r < R; ++r) {
             if (r < n) {
                 // dx = rstd (dy w - m_g - xhat m_gx), gathered by factors of dy w and of x
-                const float rs = limit != 0 ? rstd[r] : kNan;
+                const float rs = gave_up ? kNan : rstd[r];
                 const float by_x = -rs * rs * (row_sum[2 * r + 1] * a.inv_cols);
                 const float rest = fmaf(-mean[r], by_x, -rs * (row_sum[2 * r] * a.inv_cols));
 #pragma unroll
@@ -530,11 +568,14 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
             phase ^= 1;
         }
     }
-    if (limit == 0) {
-        // let the copies that were issued land before the block goes
-        for (int s = 0; s < stages; ++s) mbar_wait(bars + s * 8, phase ^ (s < stage ? 0u : 1u), kPolls);
+    if (s_gave_up[g.index]) {
+        // the copies that were issued land before the block goes and the ring is used again
+        if (g.thread == 0) land(bars, s_issued[g.index], stages);
 #pragma unroll
-        for (int i = 0; i < kNV; ++i) dw[i].set(kNan);
+        for (int i = 0; i < kNV; ++i) {
+            dw[i].set(kNan);
+            db[i].set(kNan);
+        }
     }
     __syncthreads();
 
@@ -861,6 +902,13 @@ so_status backward(const NormArgs &a, bool vec, int sms, cudaStream_t st, int *b
 
 extern "C" {
 
+so_status so_debug_set_operator_polls(int64_t polls, int32_t unit)
+{
+    if (polls < 0 || polls > (int64_t)kPolls || unit < -1) return SO_ERR_INVALID_ARG;
+    g_patience.store((uint64_t)polls << 32 | (uint32_t)unit, std::memory_order_relaxed);
+    return SO_OK;
+}
+
 so_status so_layer_norm_forward(const void *x, int64_t x_stride, const void *weight,
                                 const void *bias, void *y, int64_t y_stride, float *mean,
                                 float *rstd, int64_t rows, int64_t cols, int32_t dtype,
@@ -882,6 +930,7 @@ so_status so_layer_norm_forward(const void *x, int64_t x_stride, const void *wei
     a.x = x; a.weight = weight; a.bias = bias; a.y = y; a.mean = mean; a.rstd = rstd;
     a.x_stride = x_stride; a.y_stride = y_stride; a.rows = rows; a.cols = cols;
     a.param_dtype = param_dtype; a.eps = (float)eps; a.inv_cols = (float)(1.0 / (double)cols);
+    a.patience = patience();
     int sms = 0;
     const so_status s = device_sms(&sms);
     if (s != SO_OK) return s;
@@ -940,6 +989,7 @@ so_status so_layer_norm_backward(const void *dy, int64_t dy_stride, const void *
     a.partials = reduce ? static_cast<float *>(scratch) : nullptr;
     a.x_stride = x_stride; a.dy_stride = dy_stride; a.y_stride = dx_stride; a.rows = rows; a.cols = cols;
     a.param_dtype = param_dtype; a.inv_cols = (float)(1.0 / (double)cols);
+    a.patience = patience();
     int sms = 0;
     so_status s = device_sms(&sms);
     if (s != SO_OK) return s;

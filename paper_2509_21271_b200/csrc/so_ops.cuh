@@ -298,6 +298,15 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 // Waits for the phase of the given parity, at most `limit` polls (each of which the
 // hardware may hold for a while); false if it did not complete.
 constexpr uint32_t kPolls = 1u << 20;
+
+// How patient a launch is: `unit` (a block, or a cluster of them; -1: all) polls `polls`
+// times, the others kPolls.  0 gives up without a look.
+struct Patience {
+    uint32_t polls;
+    int32_t unit;
+    __device__ __forceinline__ uint32_t of(int mine) const { return unit < 0 || unit == mine ? polls : kPolls; }
+};
+
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
@@ -354,6 +363,14 @@ __device__ __forceinline__ float warp_sum(float x)
 }
 
 // ---- host helpers --------------------------------------------------------------
+
+// What so_debug_set_operator_polls says: polls in the upper word, unit in the lower.
+inline std::atomic<uint64_t> g_patience{(uint64_t)kPolls << 32 | 0xFFFFFFFFu};
+inline Patience patience()
+{
+    const uint64_t v = g_patience.load(std::memory_order_relaxed);
+    return Patience{(uint32_t)(v >> 32), (int32_t)(uint32_t)v};
+}
 
 inline bool valid_dtype(int32_t d) { return d == SO_DTYPE_BF16 || d == SO_DTYPE_FP32 || d == SO_DTYPE_FP16; }
 inline int elem_size(int32_t d) { return d == SO_DTYPE_FP32 ? 4 : 2; }

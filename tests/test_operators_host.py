@@ -149,3 +149,8 @@ def test_tensors_that_are_not_on_a_gpu_are_refused():
                  lambda: ops.distill_loss(x, ids[:, None], x[:, :1]), lambda: ops.policy_loss(x, ids, x[:, 0])):
         with pytest.raises(B.SuperOffloadError, match="CUDA device"):
             call()
+
+
+@pytest.mark.parametrize("polls,unit", [(-1, -1), (2 ** 20 + 1, -1), (2 ** 40, 0), (5, -2)])
+def test_operator_polls_refuse(polls, unit):
+    assert refused(B.so_debug_set_operator_polls, polls, unit)
