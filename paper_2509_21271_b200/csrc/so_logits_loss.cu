@@ -32,6 +32,7 @@ struct LossArgs {
     // policy (ids: the tokens)
     const float *advantage, *old_logp, *ref_logp;
     float clip_lo, clip_hi, kl_coef;      // clip_lo = 1 - clip_low, clip_hi = 1 + clip_high
+    Patience patience;
 };
 
 // The targets of a row, in shared memory.  id < 0 marks an empty entry.
@@ -296,8 +297,9 @@ __global__ void __launch_bounds__(kRowThreads) loss_two_pass_kernel(LossArgs a)
 // threads (394, 405), two blocks of 256 an SM with clusters of four (441), the maximum
 // kept exactly (397).  A row read twice from memory took 1771 and 2311 us.
 //
-// A wait that runs out of polls ends its block's work: the loss comes out as NaN and the
-// gradient is not complete.
+// A wait that runs out of polls ends its block's work.  When all blocks of the cluster have
+// come to their end they hear of it, and write NaN over all rows of the cluster: their
+// losses, log probabilities and whole gradients, those of masked rows too.
 
 constexpr int kBigThreads = 512;          // that compute, in a block that has an SM to itself
 constexpr int kPerThread = 2;             // 16-byte vectors of a chunk per thread
@@ -357,6 +359,10 @@ __device__ __forceinline__ uint32_t remote_addr(uint32_t addr, uint32_t rank)
     uint32_t r;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
+}
+__device__ __forceinline__ void remote_set(uint32_t addr, uint32_t rank)
+{
+    asm volatile("st.shared::cluster.u32 [%0], 1;" ::"r"(remote_addr(addr, rank)) : "memory");
 }
 // Two floats into the shared memory of a block of the cluster, counted by its mbarrier.
 __device__ __forceinline__ void remote_store(uint32_t addr, float x, float y, uint32_t bar)
@@ -715,6 +721,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
     __shared__ __align__(8) uint64_t s_target_full[kMaxDepth], s_target_empty[kMaxDepth];
     __shared__ __align__(8) uint64_t s_queue_full[kQueue], s_queue_empty[kQueue];
     __shared__ int64_t s_queue[kQueue];                  // 2 row + (is it read), -1: no more
+    __shared__ uint32_t s_gave_up;                       // some wait of the cluster ran out
     __shared__ __align__(8) MaxSum s_block[2][kMaxCluster * kBigThreads / 32];
     __shared__ RowInfo s_info[kMaxDepth];
     __shared__ float4 s_result[kMaxDepth];               // reference, sum: its logarithm and inverse; the gradient's factor
@@ -745,6 +752,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
         }
         for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&s_exchange[i]), 1);
         mbar_init_fence();
+        s_gave_up = 0;
     }
     __syncwarp();
     if (cluster > 1) cluster_sync();
@@ -767,7 +775,8 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
         return token >= 0 && token < a.vocab;
     };
     const int per_chunk = shape.chunk_bytes / 16;
-    uint32_t limit = kPolls;
+    uint32_t limit = a.patience.of(my_cluster);
+    const bool balance = shape.balance != 0 && a.rows > clusters;
     // the next row of the queue (by the producer and the target warp), -1 at the end
     const auto next_row = [&](uint32_t taken, bool &load) {
         const uint32_t at = taken % kQueue;
@@ -795,7 +804,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
             ++given;
             return true;
         };
-        walk_rows(wanted, a.rows, clusters, my_cluster, shape.balance != 0 && a.rows > clusters, give);
+        walk_rows(wanted, a.rows, clusters, my_cluster, balance, give);
         for (int i = 0; i < depth; ++i)       // an end mark for every target warp
             if (!give(-1, 0)) break;
     } else if (warp == warps) {
@@ -830,13 +839,11 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
         // loss and the gradient at the targets, over what phase 2 wrote there ----
         const auto finish = [&](int buf, uint32_t parity) {
             if (limit != 0 && !mbar_wait_idle(smem_addr(&s_target_empty[buf]), parity, limit)) limit = 0;
+            limit = __shfl_sync(0xFFFFFFFFu, limit, 0);
+            if (limit == 0) return;
             const RowInfo info = s_info[buf];
             const float4 done = s_result[buf];
             const auto exponent = [&](float z) { return exponent_of(z, done.x, a.log2e_over_t); };
-            if (limit == 0) {
-                if (rank == 0 && lane == 0) a.row_loss[info.row] = kNan;
-                return;
-            }
             if (!info.live) {
                 if (rank == 0 && lane == 0) {
                     a.row_loss[info.row] = 0.0f;
@@ -909,8 +916,8 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
         bool load = false;
         for (uint32_t it = buf;; it += depth) {
             const int64_t row = next_row(it, load);
-            if (limit == 0 && lane == 0) a.row_loss[my_cluster] = kNan;
             if (it >= (uint32_t)depth) finish(buf, ((it / depth) & 1) ^ 1);
+            if (limit == 0) break;            // the buffer may still be in use: it stays as it is
             bool live = row >= 0 && load, twice = false;
             if (live && kMode == kDistill) {
                 live = load_teacher<T>(a, row, target_id(buf), target_p(buf), target_logp(buf), target_z(buf));
@@ -963,10 +970,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
             // one warp waits for the row's targets, the others for that warp; all agree
             // on whether some wait ran out, which ends the block's work
             if (warp == 0 && limit != 0 && !mbar_wait(smem_addr(&s_target_full[buf]), row_phase, limit)) limit = 0;
-            if (any_of(limit == 0, shape.threads)) {
-                if (threadIdx.x == 0) a.row_loss[my_cluster] = kNan;
-                break;
-            }
+            if (any_of(limit == 0, shape.threads)) break;
             const RowInfo info = s_info[buf];
             const int64_t row = info.row;
             if (row < 0) break;
@@ -1143,11 +1147,31 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
             if (++buf == depth) buf = 0, row_phase ^= 1;
         }
     }
-    // no block goes while another may still write into its shared memory
-    if (cluster > 1) {
-        __syncwarp();
-        cluster_sync();
+    // No block goes while another may still write into its shared memory, and all hear of a
+    // wait that ran out.
+    if (__any_sync(0xFFFFFFFFu, limit == 0) && lane < cluster) {
+        if (cluster > 1) remote_set(smem_addr(&s_gave_up), lane);
+        else s_gave_up = 1;
     }
+    __syncwarp();
+    if (cluster > 1) cluster_sync();
+    else __syncthreads();
+    if (s_gave_up == 0) return;
+    walk_rows(wanted, a.rows, clusters, my_cluster, balance, [&](int64_t row, uint32_t) {
+        if (rank == 0 && threadIdx.x == 0) {
+            a.row_loss[row] = kNan;
+            if (kMode == kPolicy && a.logp) a.logp[row] = kNan;
+        }
+        if (kGrad) {
+            T *g = static_cast<T *>(a.grad) + row * a.grad_stride;
+            for (int64_t j = (int64_t)rank * blockDim.x + threadIdx.x; j < a.vocab; j += (int64_t)cluster * blockDim.x) g[j] = from_f32<T>(kNan);
+        }
+        return true;
+    });
+    // An exchange that was not waited for may still be under way to this block (a store takes
+    // about a microsecond, and nothing tells of the last one): it stays for a millisecond.
+    if (cluster > 1)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
 }
 
 // loss = sum of weight * row_loss, in fp64 and in a fixed order
@@ -1318,6 +1342,7 @@ so_status common_args(LossArgs &a, const void *logits, int64_t stride, const flo
     a.grad_stride = grad_stride; a.rows = rows; a.vocab = vocab; a.temperature = t; a.inv_temperature = inv;
     a.log2e_over_t = (float)(1.4426950408889634 / temperature); a.grad_scale = (float)grad_scale;
     a.ids = ids; a.ids_dtype = ids_dtype;
+    a.patience = patience();
     return SO_OK;
 }
 

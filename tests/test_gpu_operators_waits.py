@@ -70,3 +70,49 @@ def test_layer_norm_rows_whose_copies_do_not_arrive(rows, cols, dtype):
     assert torch.isnan(z).all() and torch.isnan(d).all()
     again = ops.layer_norm_forward(x, w, b) + ops.layer_norm_backward(dy, x, want[1], want[2], w)
     assert all(same_bits(p, q) for p, q in zip(again, want + back))
+
+
+# one block a row, two, eight; balanced and not; the loss alone
+LOSS_SHAPES = [(700, 50_257, BF16), (400, 128_256, BF16), (20, 128_256, FP16), (300, 20_011, FP32), (9, 50_257, FP32)]
+
+
+def loss_calls(rows, vocab, dtype):
+    g = gen(rows + vocab)
+    z = (randn(g, rows, vocab) * 2).to(dtype)
+    ids = torch.randint(vocab, (rows, 6), generator=g, device="cuda")
+    teacher, adv = randn(g, rows, 6), randn(g, rows)
+    weight = (torch.rand(rows, generator=g, device="cuda") < 0.6).float()
+    weight[0] = 0.0
+    return z, weight, {
+        "distill": lambda zz, w, grad: ops.distill_loss(zz, ids, teacher, w, grad=grad),
+        "policy": lambda zz, w, grad: ops.policy_loss(zz, ids[:, 0].contiguous(), adv, w, grad=grad)}
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", LOSS_SHAPES)
+@pytest.mark.parametrize("which", ["distill", "policy"])
+def test_losses_whose_waits_run_out(rows, vocab, dtype, which):
+    z, weight, calls = loss_calls(rows, vocab, dtype)
+    fn = calls[which]
+    want = fn(z, weight, None)
+    alone = fn(z, weight, False)
+    for unit in (-1, 0, 5):
+        with no_patience(unit):
+            got = fn(z, weight, None)
+            only = fn(z, weight, False)
+        gone = rows_gone(got[-1], want[-1])              # whole rows of the gradient, masked ones too
+        assert gone.all() if unit < 0 else 0 < gone.sum() < rows
+        per_row = torch.stack(got[1:-1], 1)
+        assert torch.equal(rows_gone(per_row, torch.stack(want[1:-1], 1)), gone)
+        gone_alone = rows_gone(torch.stack(only[1:-1], 1), torch.stack(alone[1:-1], 1))
+        assert gone_alone.all() if unit < 0 else 0 < gone_alone.sum() < rows
+        for g, w, lost in ((got, want, gone), (only, alone, gone_alone)):
+            if (lost & (weight != 0)).any():
+                assert torch.isnan(g[0]).all()
+            else:
+                assert same_bits(g[0], w[0])
+    # over the logits: none of them is left in the place of a gradient
+    zz = z.clone()
+    with no_patience():
+        fn(zz, weight, zz)
+    assert torch.isnan(zz).all()
+    assert all(same_bits(p, q) for p, q in zip(fn(z, weight, None), want))
