@@ -13,6 +13,13 @@ Every function runs on the current stream, or on ``stream`` (a
 ``torch.cuda.Stream``; the tensors it is given are then recorded on it, ordering
 it behind their producers is the caller's).  Tensors live on the current device.
 Nothing here waits for the device.
+
+Autograd does not record these calls: the backward passes are calls of their own.
+With gradients enabled a tensor that requires grad is refused rather than cut off
+from its graph; call them under ``torch.no_grad()`` or from a
+``torch.autograd.Function``.  Tensors that are written over (``out=x``,
+``grad=logits``, gradients added to) count as modified in place, so that a graph
+which saved one of them notices.
 """
 from __future__ import annotations
 
@@ -26,13 +33,22 @@ _DTYPES = {torch.bfloat16: B.SO_DTYPE_BF16, torch.float32: B.SO_DTYPE_FP32, torc
 _IDS = {torch.int32: B.SO_IDS_INT32, torch.int64: B.SO_IDS_INT64}
 
 
-# The plain forms of these two go through Python layers that cost as much as a launch.
+# The plain forms of these go through Python layers that cost as much as a launch.
 _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+_increment_version = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version
 
 
 def _refuse(where: str, what: str):
     raise B.SuperOffloadError(B.SO_ERR_INVALID_ARG, f"{where}: {what}")
+
+
+def _unrecorded(where, *tensors):
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                _refuse(where, "autograd does not record this call, and a tensor given to it requires grad: "
+                               "use torch.no_grad() or a torch.autograd.Function")
 
 
 def _device(where, name, t) -> int:
@@ -108,9 +124,11 @@ _norm_scratch = lru_cache(maxsize=512)(B.so_layer_norm_backward_scratch)      # 
 _embedding_scratch = lru_cache(maxsize=512)(B.so_embedding_backward_scratch)
 
 
-def _done(status: int, where: str) -> None:
+def _done(status: int, where: str, written) -> None:
+    """Raises, or notes that the tensors in `written` were."""
     if status != B.SO_OK:
         raise B.SuperOffloadError(status, "so_" + where)
+    _increment_version(written)
 
 
 def _on_stream(stream, fn, *args, **kw):
@@ -134,6 +152,7 @@ def layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, *, out=None
         return _on_stream(stream, layer_norm_forward, x, weight, bias, eps, out=out, mean=mean, rstd=rstd,
                           save_stats=save_stats)
     where = "layer_norm_forward"
+    _unrecorded(where, x, weight, bias)
     dev = _device(where, "x", x)
     dt = _dtype(where, "x", x)
     rows, cols, stride = _rows(where, "x", x, dev)
@@ -158,7 +177,7 @@ def layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, *, out=None
     _done(B.lib().so_layer_norm_forward(x.data_ptr(), stride, wp, bp, out.data_ptr(), out_stride,
                             _vector(where, "mean", mean, rows, dev, torch.float32),
                             _vector(where, "rstd", rstd, rows, dev, torch.float32),
-                            rows, cols, dt, pt, eps, _raw_stream(dev)), where)
+                            rows, cols, dt, pt, eps, _raw_stream(dev)), where, (out, mean, rstd) if save_stats else (out,))
     return out, mean, rstd
 
 
@@ -172,6 +191,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, *, dx=None, dweight=None
         return _on_stream(stream, layer_norm_backward, dy, x, mean, rstd, weight, dx=dx, dweight=dweight,
                           dbias=dbias, accumulate=accumulate, scratch=scratch)
     where = "layer_norm_backward"
+    _unrecorded(where, dy, x, mean, rstd, weight)
     dev = _device(where, "x", x)
     dt = _dtype(where, "x", x)
     _same(where, "dy", dy, "x", x)
@@ -207,7 +227,8 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, *, dx=None, dweight=None
                              _vector(where, "rstd", rstd, rows, dev, torch.float32),
                              dx.data_ptr(), dx_stride, _vector(where, "dweight", dweight, cols, dev),
                              _vector(where, "dbias", dbias, cols, dev), rows, cols, dt, pt, gt, int(accumulate),
-                             ws, need, _raw_stream(dev)), where)
+                             ws, need, _raw_stream(dev)), where,
+          [t for t in (dx, dweight, dbias) if t is not None])
     return dx, dweight, dbias
 
 
@@ -219,6 +240,7 @@ def embedding_forward(ids, table, scale: float = 1.0, *, out=None, bad_id=None, 
     if stream is not None:
         return _on_stream(stream, embedding_forward, ids, table, scale, out=out, bad_id=bad_id)
     where = "embedding_forward"
+    _unrecorded(where, table)
     dev = _device(where, "table", table)
     it = _ids_dtype(where, "ids", ids)
     dt = _dtype(where, "table", table)
@@ -234,7 +256,7 @@ def embedding_forward(ids, table, scale: float = 1.0, *, out=None, bad_id=None, 
     _, _, out_stride = _rows(where, "out", out, dev)
     _done(B.lib().so_embedding_forward(ip, it, n, table.data_ptr(), stride, vocab, cols, dt, scale, out.data_ptr(),
                            out_stride, _vector(where, "bad_id", bad_id, 1, dev, torch.int32),
-                           _raw_stream(dev)), where)
+                           _raw_stream(dev)), where, (out,) if bad_id is None else (out, bad_id))
     return out
 
 
@@ -249,6 +271,7 @@ def embedding_backward(ids, dout, dtable, scale: float = 1.0, *, padding_id: int
         return _on_stream(stream, embedding_backward, ids, dout, dtable, scale, padding_id=padding_id,
                           accumulate=accumulate, scratch=scratch)
     where = "embedding_backward"
+    _unrecorded(where, dout, dtable)
     dev = _device(where, "dtable", dtable)
     it = _ids_dtype(where, "ids", ids)
     dt = _dtype(where, "dout", dout)
@@ -265,7 +288,7 @@ def embedding_backward(ids, dout, dtable, scale: float = 1.0, *, padding_id: int
         scratch = torch.empty(_embedding_scratch(n, vocab, cols), dtype=torch.uint8, device=dtable.device)
     _done(B.lib().so_embedding_backward(ip, it, n, dout.data_ptr(), dout_stride, vocab, cols, dt, scale, padding_id,
                             dtable.data_ptr(), stride, gt, int(accumulate), scratch.data_ptr(),
-                            _scratch(where, scratch, dev), _raw_stream(dev)), where)
+                            _scratch(where, scratch, dev), _raw_stream(dev)), where, (dtable,))
     return dtable
 
 
@@ -302,6 +325,7 @@ def distill_loss(logits, teacher_ids, teacher_logits, weight=None, *, temperatur
         return _on_stream(stream, distill_loss, logits, teacher_ids, teacher_logits, weight,
                           temperature=temperature, grad_scale=grad_scale, grad=grad, loss=loss, row_loss=row_loss)
     where = "distill_loss"
+    _unrecorded(where, logits, teacher_logits, weight)
     dev = _device(where, "logits", logits)
     dt = _dtype(where, "logits", logits)
     rows, vocab, stride = _rows(where, "logits", logits, dev)
@@ -317,7 +341,8 @@ def distill_loss(logits, teacher_ids, teacher_logits, weight=None, *, temperatur
                       _vector(where, "weight", weight, rows, dev, torch.float32), rows, vocab, dt, temperature,
                       grad_scale, None if grad is None else grad.data_ptr(), grad_stride,
                       _vector(where, "row_loss", row_loss, rows, dev, torch.float32),
-                      _vector(where, "loss", loss, 1, dev, torch.float32), _raw_stream(dev)), where)
+                      _vector(where, "loss", loss, 1, dev, torch.float32), _raw_stream(dev)), where,
+          (loss, row_loss) if grad is None else (loss, row_loss, grad))
     return loss, row_loss, grad
 
 
@@ -337,6 +362,7 @@ def policy_loss(logits, tokens, advantage, weight=None, *, old_logp=None, ref_lo
                           ref_logp=ref_logp, temperature=temperature, clip_low=clip_low, clip_high=clip_high,
                           kl_coef=kl_coef, grad_scale=grad_scale, grad=grad, loss=loss, row_loss=row_loss, logp=logp)
     where = "policy_loss"
+    _unrecorded(where, logits, advantage, weight, old_logp, ref_logp)
     dev = _device(where, "logits", logits)
     dt = _dtype(where, "logits", logits)
     rows, vocab, stride = _rows(where, "logits", logits, dev)
@@ -352,5 +378,6 @@ def policy_loss(logits, tokens, advantage, weight=None, *, old_logp=None, ref_lo
                      _vector(where, "weight", weight, rows, dev, f32), rows, vocab, dt, temperature, clip_low,
                      clip_high, kl_coef, grad_scale, None if grad is None else grad.data_ptr(), grad_stride,
                      _vector(where, "logp", logp, rows, dev, f32), _vector(where, "row_loss", row_loss, rows, dev, f32),
-                     _vector(where, "loss", loss, 1, dev, f32), _raw_stream(dev)), where)
+                     _vector(where, "loss", loss, 1, dev, f32), _raw_stream(dev)), where,
+          (loss, row_loss, logp) if grad is None else (loss, row_loss, logp, grad))
     return loss, row_loss, logp, grad

@@ -154,3 +154,21 @@ def test_tensors_that_are_not_on_a_gpu_are_refused():
 @pytest.mark.parametrize("polls,unit", [(-1, -1), (2 ** 20 + 1, -1), (2 ** 40, 0), (5, -2)])
 def test_operator_polls_refuse(polls, unit):
     assert refused(B.so_debug_set_operator_polls, polls, unit)
+
+
+def test_tensors_that_require_grad_are_refused():
+    """Their result would be cut off from the graph without a word."""
+    x, ids = torch.zeros(2, 8), torch.zeros(2, dtype=torch.int64)
+    r = torch.zeros(2, 8, requires_grad=True)
+    calls = [lambda: ops.layer_norm_forward(r), lambda: ops.layer_norm_forward(x, r[0]),
+             lambda: ops.layer_norm_forward(x, x[0], r[0]), lambda: ops.layer_norm_backward(r, x, x[:, 0], x[:, 0]),
+             lambda: ops.layer_norm_backward(x, x, x[:, 0], x[:, 0], r[0]), lambda: ops.embedding_forward(ids, r),
+             lambda: ops.embedding_backward(ids, r, x), lambda: ops.distill_loss(r, ids[:, None], x[:, :1]),
+             lambda: ops.distill_loss(x, ids[:, None], r[:, :1]), lambda: ops.policy_loss(r, ids, x[:, 0]),
+             lambda: ops.policy_loss(x, ids, r[:, 0]), lambda: ops.policy_loss(x, ids, x[:, 0], r[:, 0])]
+    for call in calls:
+        with pytest.raises(B.SuperOffloadError, match="requires grad") as err:
+            call()
+        assert err.value.status == B.SO_ERR_INVALID_ARG
+        with torch.no_grad(), pytest.raises(B.SuperOffloadError, match="CUDA device"):
+            call()                                # the next check: these are not on a GPU
