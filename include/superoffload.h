@@ -615,6 +615,7 @@ so_status so_embedding_backward(const void *ids, int32_t ids_dtype, int64_t n, c
  * probability 0; a row of nothing else, and one
  * with NaN or +inf in it, has a NaN loss and gradient, which the optimizer's
  * gradient check turns into a skipped iteration.
+ * rows is at most 2^31 - 1 and vocab at most 2^30, here and in so_policy_loss.
  */
 #define SO_DISTILL_MAX_TOP_K 1024
 so_status so_distill_loss(const void *logits, int64_t logits_stride, const void *teacher_ids,

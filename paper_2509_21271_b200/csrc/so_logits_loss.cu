@@ -19,7 +19,7 @@ enum Mode { kDistill = 0, kPolicy = 1 };
 
 struct LossArgs {
     const void *logits;
-    void *grad;                           // nullptr: the loss alone
+    void *grad;                           // nullptr: the loss alone (not in loss_two_pass_kernel)
     const float *weight;                  // nullptr: 1
     float *row_loss, *logp;
     int64_t stride, grad_stride, rows, vocab;
@@ -180,8 +180,8 @@ __device__ __forceinline__ void policy_row(const LossArgs &a, float logp, float 
 
 // ---- a block per row, the row read twice -----------------------------------------
 //
-// For rows that the shared memory of a cluster does not hold (with a gradient: about
-// 1.7 MB), element by element.
+// For rows with a gradient that the shared memory of a cluster does not hold (1.7 MB, 1.3
+// with the longest lists), element by element.
 
 constexpr int kRowThreads = 512;
 
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kRowThreads) loss_two_pass_kernel(LossArgs a)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *z = static_cast<const T *>(a.logits) + row * a.stride;
-        T *g = a.grad ? static_cast<T *>(a.grad) + row * a.grad_stride : nullptr;
+        T *g = static_cast<T *>(a.grad) + row * a.grad_stride;
         const float w = a.weight ? a.weight[row] : 1.0f;
         int64_t token = -1;
         if (kMode == kPolicy) token = load_id(a.ids, row, a.ids_dtype);
@@ -212,8 +212,7 @@ __global__ void __launch_bounds__(kRowThreads) loss_two_pass_kernel(LossArgs a)
         __syncthreads();
         live = live && t.live;
         if (!live) {
-            if (g)
-                for (int64_t j = threadIdx.x; j < a.vocab; j += kRowThreads) g[j] = from_f32<T>(0.0f);
+            for (int64_t j = threadIdx.x; j < a.vocab; j += kRowThreads) g[j] = from_f32<T>(0.0f);
             if (threadIdx.x == 0) {
                 a.row_loss[row] = 0.0f;
                 if (kMode == kPolicy && a.logp) a.logp[row] = 0.0f;
@@ -246,20 +245,18 @@ __global__ void __launch_bounds__(kRowThreads) loss_two_pass_kernel(LossArgs a)
             }
             coef = -a.grad_scale * w * slope * a.inv_temperature;
         }
-        if (g) {
-            const float inv_s = 1.0f / ms.s, scaled = coef * inv_s;
-            for (int64_t j = threadIdx.x; j < a.vocab; j += kRowThreads)
-                g[j] = from_f32<T>(exp2_fast((to_f32(z[j]) - ms.m) * a.log2e_over_t) * scaled);
-            __syncthreads();
-            const int n = kMode == kDistill ? a.top_k : 1;
-            for (int k = threadIdx.x; k < n; k += kRowThreads) {
-                const int32_t id = t.id[k];
-                if (id < 0) continue;
-                float p = 0.0f;
-                for (int i = 0; i < n; ++i)
-                    if (t.id[i] == id) p += t.p[i];
-                g[id] = from_f32<T>(coef * (exp2_fast((t.z[k] - ms.m) * a.log2e_over_t) * inv_s - p));
-            }
+        const float inv_s = 1.0f / ms.s, scaled = coef * inv_s;
+        for (int64_t j = threadIdx.x; j < a.vocab; j += kRowThreads)
+            g[j] = from_f32<T>(exp2_fast((to_f32(z[j]) - ms.m) * a.log2e_over_t) * scaled);
+        __syncthreads();
+        const int n = kMode == kDistill ? a.top_k : 1;
+        for (int k = threadIdx.x; k < n; k += kRowThreads) {
+            const int32_t id = t.id[k];
+            if (id < 0) continue;
+            float p = 0.0f;
+            for (int i = 0; i < n; ++i)
+                if (t.id[i] == id) p += t.p[i];
+            g[id] = from_f32<T>(coef * (exp2_fast((t.z[k] - ms.m) * a.log2e_over_t) * inv_s - p));
         }
         __syncthreads();
     }
@@ -313,7 +310,6 @@ struct RingShape {
     int threads;                          // that compute; the block has 2 + depth warps more
     int cluster, slots, depth;            // blocks a row, chunks of the ring, rows whose targets are at hand
     int chunk_bytes;
-    int balance;                          // deal out masked rows separately
     size_t smem;
 };
 
@@ -669,22 +665,16 @@ __global__ void __launch_bounds__(kShortThreads) loss_short_kernel(LossArgs a)
     }
 }
 
-// The rows of a cluster, in ascending order, by one warp.  Where a cluster has many long
-// rows (`balance`), masked rows, which cost less than the others, are dealt out
-// separately, both kinds in turn by their own count: the warp looks at 32 rows at a
-// time, and all clusters come to the same counts.  Otherwise every n-th row.
+// The rows of a cluster, in ascending order, by one warp.  Masked rows, which cost less
+// than the others, are dealt out separately, both kinds in turn by their own count: the
+// warp looks at 32 rows at a time, a few hundred clocks beside rows of 32 KB and more, and
+// all clusters come to the same counts.
 template <typename Wanted, typename Give>
-__device__ void walk_rows(const Wanted &wanted, int64_t rows, int n, int mine, bool balance, Give give)
+__device__ void walk_rows(const Wanted &wanted, int64_t rows, int n, int mine, Give give)
 {
     const int lane = threadIdx.x & 31;
-    if (!balance) {
-        // a lane looks at the row that is its turn, 32 turns at a time
-        for (int64_t base = mine; base < rows; base += (int64_t)32 * n) {
-            const int64_t row = base + (int64_t)lane * n;
-            const uint32_t reads = __ballot_sync(0xFFFFFFFFu, row < rows && wanted(row));
-            for (int i = 0; i < 32 && base + (int64_t)i * n < rows; ++i)
-                if (!give(base + (int64_t)i * n, (reads >> i) & 1u)) return;
-        }
+    if (rows == n) {                      // one row each
+        give(mine, wanted(mine));
         return;
     }
     constexpr int kAhead = 4;             // windows whose loads are in flight
@@ -711,7 +701,7 @@ __device__ void walk_rows(const Wanted &wanted, int64_t rows, int n, int mine, b
     }
 }
 
-// kBig: one block an SM of up to 512 computing threads, else two or more of up to 256
+// kBig: one block an SM of 512 computing threads, else two of 256
 template <typename T, int kMode, bool kGrad, bool kBig>
 __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 384, kBig ? 1 : 2) loss_ring_kernel(LossArgs a, RingShape shape)
 {
@@ -776,7 +766,6 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
     };
     const int per_chunk = shape.chunk_bytes / 16;
     uint32_t limit = a.patience.of(my_cluster);
-    const bool balance = shape.balance != 0 && a.rows > clusters;
     // the next row of the queue (by the producer and the target warp), -1 at the end
     const auto next_row = [&](uint32_t taken, bool &load) {
         const uint32_t at = taken % kQueue;
@@ -804,7 +793,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
             ++given;
             return true;
         };
-        walk_rows(wanted, a.rows, clusters, my_cluster, balance, give);
+        walk_rows(wanted, a.rows, clusters, my_cluster, give);
         for (int i = 0; i < depth; ++i)       // an end mark for every target warp
             if (!give(-1, 0)) break;
     } else if (warp == warps) {
@@ -1157,7 +1146,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
     if (cluster > 1) cluster_sync();
     else __syncthreads();
     if (s_gave_up == 0) return;
-    walk_rows(wanted, a.rows, clusters, my_cluster, balance, [&](int64_t row, uint32_t) {
+    walk_rows(wanted, a.rows, clusters, my_cluster, [&](int64_t row, uint32_t) {
         if (rank == 0 && threadIdx.x == 0) {
             a.row_loss[row] = kNan;
             if (kMode == kPolicy && a.logp) a.logp[row] = kNan;
@@ -1197,37 +1186,28 @@ loss_total_kernel(const float *row_loss, const float *weight, int64_t rows, floa
     if (threadIdx.x == 0) *loss = (float)sum;
 }
 
-// The ring's shape for `vocab` elements of `es` bytes: false if no cluster holds a row.
+// The ring's shape for rows of more than kShortVectors * kShortThreads vectors: false if no
+// cluster holds one for its gradient.
 bool ring_shape(int64_t rows, int64_t vocab, int es, int top_k, bool grad, int sms, RingShape *out)
 {
     const int64_t row_bytes = vocab * es;
-    int threads = kBigThreads;
     RingShape r;
     const size_t list = (size_t)16 * ((top_k + 3) & ~3), table = (size_t)4 * table_places(top_k);
     const int lists = top_k <= 256 ? kMaxDepth : 2;
+    // the ring takes what the lists leave: 7 chunks at least (1024 entries, 256 threads)
     const auto fit = [&](int t) {
         r.threads = t;
         r.depth = t > 256 ? lists : 2;
         r.chunk_bytes = t * 16 * kPerThread;
-        const size_t per_block = (size_t)224 * 1024 / (t > 256 ? 1 : 512 / t) - 5 * 1024, targets = (list + table) * r.depth;
-        if (per_block < targets + 2 * (size_t)r.chunk_bytes) return false;
+        const size_t per_block = (size_t)224 * 1024 / (kBigThreads / t) - 5 * 1024, targets = (list + table) * r.depth;
         r.slots = (int)((per_block - targets) / r.chunk_bytes);
         if (r.slots > kMaxSlots) r.slots = kMaxSlots;
         r.smem = (size_t)r.slots * r.chunk_bytes + targets;
-        return true;
     };
     // two blocks of 256 threads an SM where each holds whole rows: what one waits for, the
-    // other hides; and fewer threads for short rows
-    if (grad ? fit(256) && (row_bytes + r.chunk_bytes - 1) / r.chunk_bytes <= r.slots : row_bytes < 64 * 1024) threads = 256;
-    while (threads <= 256 && threads > 64 && row_bytes < (int64_t)threads * 64) threads /= 2;
-    while (!fit(threads)) {
-        if (threads >= 256) {
-            if (threads == kBigThreads) return false;
-            threads = kBigThreads;
-        } else {
-            threads *= 2;
-        }
-    }
+    // other hides
+    fit(256);
+    if (grad ? (row_bytes + r.chunk_bytes - 1) / r.chunk_bytes > r.slots : row_bytes >= 64 * 1024) fit(kBigThreads);
     r.cluster = 1;
     const auto chunks = [&](int c) { return ((row_bytes / 16 + c - 1) / c * 16 + r.chunk_bytes - 1) / r.chunk_bytes; };
     if (grad)
@@ -1235,8 +1215,6 @@ bool ring_shape(int64_t rows, int64_t vocab, int es, int top_k, bool grad, int s
     if (grad && chunks(r.cluster) > r.slots) return false;
     // few rows: more blocks each, while SMs are idle
     while (r.cluster < kMaxCluster && rows * r.cluster * 2 <= sms && chunks(r.cluster) > 1) r.cluster *= 2;
-    // looking at all rows costs a cluster a few hundred clocks for each 32: little beside long rows
-    r.balance = r.threads >= 256;
     *out = r;
     return true;
 }
@@ -1283,7 +1261,7 @@ template <typename T, int kMode>
 so_status launch_loss(const LossArgs &a, int sms, cudaStream_t st)
 {
     const int64_t vectors = a.vocab / Vec<T>::kElems;
-    if (vectors <= kShortVectors * kShortThreads && a.rows <= INT32_MAX) {
+    if (vectors <= kShortVectors * kShortThreads) {
         const int per_thread = (int)((vectors + kShortVectors - 1) / kShortVectors);
         const unsigned threads = per_thread <= 32 ? 32u : (unsigned)((per_thread + 31) / 32 * 32);
         const size_t lists = (size_t)16 * (kMode == kDistill ? a.top_k : 1);
@@ -1321,7 +1299,7 @@ so_status common_args(LossArgs &a, const void *logits, int64_t stride, const flo
                       int64_t grad_stride, float *row_loss, float *loss, const void *ids, int32_t ids_dtype)
 {
     if (!valid_dtype(dtype) || !valid_ids(ids_dtype)) return SO_ERR_INVALID_ARG;
-    if (rows < 0 || vocab < 1 || vocab > (int64_t(1) << 30)) return SO_ERR_INVALID_ARG;
+    if (rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > (int64_t(1) << 30)) return SO_ERR_INVALID_ARG;
     if (!(temperature > 0.0) || !std::isfinite(temperature) || !std::isfinite(grad_scale)) return SO_ERR_INVALID_ARG;
     const float t = (float)temperature, inv = (float)(1.0 / temperature);
     if (!(t > 0.0f) || !std::isfinite(t) || !(inv > 0.0f) || !std::isfinite(inv) || !std::isfinite((float)grad_scale))

@@ -172,3 +172,10 @@ def test_tensors_that_require_grad_are_refused():
         assert err.value.status == B.SO_ERR_INVALID_ARG
         with torch.no_grad(), pytest.raises(B.SuperOffloadError, match="CUDA device"):
             call()                                # the next check: these are not on a GPU
+
+
+@pytest.mark.parametrize("which", [DISTILL, POLICY])
+@pytest.mark.parametrize("vocab", [1, 1000, 200_000])
+def test_losses_refuse_more_rows_than_a_grid_has_blocks(which, vocab):
+    fn = B.so_distill_loss if which is DISTILL else B.so_policy_loss
+    assert refused(fn, *dict(which, rows=2 ** 31, vocab=vocab, logits_stride=vocab, grad_stride=vocab).values())
