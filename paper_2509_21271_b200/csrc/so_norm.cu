@@ -872,19 +872,16 @@ so_status backward(const NormArgs &a, bool vec, int sms, cudaStream_t st, int *b
 {
     constexpr int E = Vec<T>::kElems;
     const int64_t row = a.cols * (int64_t)sizeof(T) + (vec ? 0 : 48);
-    // rows at a time: four, or as many as leave three stages in shared memory
-    const int r = row * 24 <= kMaxShared ? 4 : row * 12 <= kMaxShared ? 2 : 1;
+    // rows at a time: four, or two where that leaves less than three stages in shared memory
+    // (more than 9 KB a row; the plans below hold at most 16 KB, or take one row themselves)
+    const int r = row * 24 <= kMaxShared ? 4 : 2;
     if (vec && row * 4 <= kMaxShared) {
         const Plan p = plan_ring(a.cols / E, 2);
         if (p.nv == 2) {
             if (r == 4) return backward_ring<T, E, 2, 4>(a, p, sms, st, blocks);
-            if (r == 2) return backward_ring<T, E, 2, 2>(a, p, sms, st, blocks);
-            return backward_ring<T, E, 2, 1>(a, p, sms, st, blocks);
+            return backward_ring<T, E, 2, 2>(a, p, sms, st, blocks);
         }
-        if (p.nv == 1) {
-            if (r == 4) return backward_ring<T, E, 1, 4>(a, p, sms, st, blocks);
-            return backward_ring<T, E, 1, 1>(a, p, sms, st, blocks);
-        }
+        if (p.nv == 1) return backward_ring<T, E, 1, 4>(a, p, sms, st, blocks);   // 8 KB a row at most
     } else if (row * 4 <= kMaxShared) {
         const Plan p = make_plan(a.cols, a.cols <= 8 * kLongThreads ? 8 : 16);
         if (p.nv == 8) {
