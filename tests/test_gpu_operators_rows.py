@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2509_21271_b200 import build as so_build
-from test_gpu_operators import BF16, FP16, FP32, check_distill, check_policy, gen, randn
+from test_gpu_operators import BF16, FP16, FP32, check_distill, check_policy, gen, randn, same_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +69,29 @@ def test_small_weights_keep_the_gradients_digits(height, weight):
     ids = torch.full((90, 1), 30_000, device="cuda")
     check_distill(z, ids, torch.zeros(90, 1, device="cuda"), torch.full((90,), weight, device="cuda"))
     check_policy(z, ids[:, 0].contiguous(), torch.ones(90, device="cuda"), torch.full((90,), weight, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype,vocab", [(FP16, 950_003), (BF16, 950_008), (FP32, 480_001)])
+def test_vocabularies_that_no_cluster_holds(dtype, vocab):
+    """More than 1.7 MB a row: the loop that reads a row twice, each type, in place and beside
+    lists that are empty, repeat an id or are as long as they get."""
+    g = gen(vocab)
+    z = (randn(g, 5, vocab) * 2).to(dtype)
+    ids = torch.randint(vocab, (5, 30), generator=g, device="cuda")
+    ids[1, :] = -1                                # nothing there: counts as masked
+    ids[2, 5:9] = ids[2, 4]
+    teacher = randn(g, 5, 30)
+    teacher[3, 7:] = -float("inf")
+    weight = torch.tensor([1.0, 0.5, 0.25, 2.0, 0.0], device="cuda")
+    scale = 512.0 if dtype == FP16 else 1.0
+    _, row, grad = check_distill(z, ids, teacher, weight, 1.3, scale)
+    assert row[1] == 0 and (grad[1] == 0).all()
+    check_distill(z, ids[:, :1].repeat(1, 1024), randn(g, 5, 1024), weight, 1.0, scale)
+    over = z.clone()
+    check_distill(over, ids, teacher, weight, 1.3, scale, grad=over)
+    assert same_bits(over, grad)
+    tokens, adv = ids[:, 0].contiguous(), randn(g, 5)
+    _, _, _, grad = check_policy(z, tokens, adv, weight, temperature=0.8, grad_scale=scale)
+    over = z.clone()
+    check_policy(over, tokens, adv, weight, temperature=0.8, grad_scale=scale, grad=over)
+    assert same_bits(over, grad)
