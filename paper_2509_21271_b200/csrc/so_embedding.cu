@@ -59,8 +59,8 @@ __global__ void __launch_bounds__(kLookupThreads) embedding_forward_kernel(Looku
                     }
             }
         } else {
-            const int cols = (int)a.cols;
-            for (int c0 = lane; c0 < cols; c0 += 32 * kLookupBatch) {
+            const uint32_t cols = (uint32_t)a.cols;   // up to 2^31 - 1: the last step passes 2^31
+            for (uint32_t c0 = lane; c0 < cols; c0 += 32 * kLookupBatch) {
                 T raw[kLookupBatch];
 #pragma unroll
                 for (int u = 0; u < kLookupBatch; ++u)

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2509_21271_b200 import build as so_build
+from paper_2509_21271_b200 import operators as ops
 from test_gpu_operators import BF16, FP16, FP32, check_distill, check_policy, gen, randn, same_bits
 
 pytestmark = pytest.mark.gpu
@@ -95,3 +96,12 @@ def test_vocabularies_that_no_cluster_holds(dtype, vocab):
     over = z.clone()
     check_policy(over, tokens, adv, weight, temperature=0.8, grad_scale=scale, grad=over)
     assert same_bits(over, grad)
+
+
+def test_lookup_of_the_widest_rows():
+    """Rows of 2^31 - 1 elements: the last step of the loop over columns ends beyond 2^31."""
+    cols = 2 ** 31 - 1
+    table = torch.empty(1, cols, dtype=FP16, device="cuda")
+    table.view(torch.int16).random_(0, 0x7C00)       # finite, every magnitude
+    out = ops.embedding_forward(torch.zeros(1, dtype=torch.int64, device="cuda"), table)
+    assert torch.equal(out.view(torch.int16), table.view(torch.int16))
