@@ -523,6 +523,7 @@ so_status so_debug_set_spin_limit(so_ctx *ctx, int64_t polls);
  *   - sums, statistics and softmax are held in fp32 (totals over rows in fp64)
  *     and every output is rounded once;
  *   - results repeat bit for bit: no floating-point atomics anywhere;
+ *   - scales, eps, temperature and coefficients have to be finite in fp32, where they are held;
  *   - zero rows (tokens) are a valid input: forward outputs are empty, a loss
  *     is 0, a reduced gradient is zero (or unchanged with `accumulate`);
  *   - inputs and outputs do not overlap, except where stated.

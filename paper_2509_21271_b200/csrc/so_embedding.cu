@@ -509,7 +509,7 @@ so_status so_embedding_forward(const void *ids, int32_t ids_dtype, int64_t n, co
                                double scale, void *out, int64_t out_stride, int32_t *bad_id,
                                void *stream)
 {
-    if (!valid_ids(ids_dtype) || !valid_dtype(dtype) || !std::isfinite(scale)) return SO_ERR_INVALID_ARG;
+    if (!valid_ids(ids_dtype) || !valid_dtype(dtype) || !std::isfinite((float)scale)) return SO_ERR_INVALID_ARG;
     if (n < 0 || n > kMaxTokens || vocab < 1 || vocab > kMaxTokens || cols < 1 || cols > INT32_MAX)
         return SO_ERR_INVALID_ARG;
     const int es = elem_size(dtype);
@@ -557,7 +557,7 @@ so_status so_embedding_backward(const void *ids, int32_t ids_dtype, int64_t n, c
                                 void *scratch, uint64_t scratch_bytes, void *stream)
 {
     uint64_t need = 0;
-    if (!valid_ids(ids_dtype) || !valid_dtype(dtype) || !valid_dtype(grad_dtype) || !std::isfinite(scale) ||
+    if (!valid_ids(ids_dtype) || !valid_dtype(dtype) || !valid_dtype(grad_dtype) || !std::isfinite((float)scale) ||
         (accumulate != 0 && accumulate != 1))
         return SO_ERR_INVALID_ARG;
     if (so_embedding_backward_scratch(n, vocab, cols, &need) != SO_OK) return SO_ERR_INVALID_ARG;

@@ -1301,8 +1301,9 @@ so_status common_args(LossArgs &a, const void *logits, int64_t stride, const flo
     if (!valid_dtype(dtype) || !valid_ids(ids_dtype)) return SO_ERR_INVALID_ARG;
     if (rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > (int64_t(1) << 30)) return SO_ERR_INVALID_ARG;
     if (!(temperature > 0.0) || !std::isfinite(temperature) || !std::isfinite(grad_scale)) return SO_ERR_INVALID_ARG;
-    const float t = (float)temperature, inv = (float)(1.0 / temperature);
-    if (!(t > 0.0f) || !std::isfinite(t) || !(inv > 0.0f) || !std::isfinite(inv) || !std::isfinite((float)grad_scale))
+    // what the kernels hold of them in fp32: T, 1 / T, and log2(e) / T, the largest of the three
+    const float t = (float)temperature, inv = (float)(1.0 / temperature), log2e_over_t = (float)(1.4426950408889634 / temperature);
+    if (!(t > 0.0f) || !std::isfinite(t) || !(inv > 0.0f) || !std::isfinite(log2e_over_t) || !std::isfinite((float)grad_scale))
         return SO_ERR_INVALID_ARG;
     if (!loss || !aligned(loss, 4) || !aligned(weight, 4)) return SO_ERR_INVALID_ARG;
     const int es = elem_size(dtype);
@@ -1318,7 +1319,7 @@ so_status common_args(LossArgs &a, const void *logits, int64_t stride, const flo
     }
     a.logits = logits; a.grad = grad; a.weight = weight; a.row_loss = row_loss; a.stride = stride;
     a.grad_stride = grad_stride; a.rows = rows; a.vocab = vocab; a.temperature = t; a.inv_temperature = inv;
-    a.log2e_over_t = (float)(1.4426950408889634 / temperature); a.grad_scale = (float)grad_scale;
+    a.log2e_over_t = log2e_over_t; a.grad_scale = (float)grad_scale;
     a.ids = ids; a.ids_dtype = ids_dtype;
     a.patience = patience();
     return SO_OK;
@@ -1362,7 +1363,7 @@ so_status so_policy_loss(const void *logits, int64_t logits_stride, const void *
                                     grad, grad_stride, row_loss, loss, tokens, ids_dtype);
     if (s != SO_OK) return s;
     if (!(clip_low >= 0.0 && clip_low <= 1.0) || !(clip_high >= 0.0)) return SO_ERR_INVALID_ARG;
-    if (!(kl_coef >= 0.0) || !std::isfinite(kl_coef) || (kl_coef != 0.0 && !ref_logp)) return SO_ERR_INVALID_ARG;
+    if (!(kl_coef >= 0.0) || !std::isfinite((float)kl_coef) || (kl_coef != 0.0 && !ref_logp)) return SO_ERR_INVALID_ARG;
     if (!aligned(advantage, 4) || !aligned(old_logp, 4) || !aligned(ref_logp, 4) || !aligned(logp, 4))
         return SO_ERR_INVALID_ARG;
     if (rows > 0 && !advantage) return SO_ERR_INVALID_ARG;

@@ -912,7 +912,7 @@ so_status so_layer_norm_forward(const void *x, int64_t x_stride, const void *wei
                                 int32_t param_dtype, double eps, void *stream)
 {
     if (!valid_dtype(dtype) || (param_dtype != dtype && param_dtype != SO_DTYPE_FP32)) return SO_ERR_INVALID_ARG;
-    if (rows < 0 || cols < 1 || cols > INT32_MAX || !(eps >= 0.0) || !std::isfinite(eps)) return SO_ERR_INVALID_ARG;
+    if (rows < 0 || cols < 1 || cols > INT32_MAX || !(eps >= 0.0) || !std::isfinite((float)eps)) return SO_ERR_INVALID_ARG;
     const int es = elem_size(dtype), ps = elem_size(param_dtype);
     if ((weight && !aligned(weight, ps)) || (bias && !aligned(bias, ps))) return SO_ERR_INVALID_ARG;
     if ((mean == nullptr) != (rstd == nullptr)) return SO_ERR_INVALID_ARG;

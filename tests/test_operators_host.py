@@ -179,3 +179,13 @@ def test_tensors_that_require_grad_are_refused():
 def test_losses_refuse_more_rows_than_a_grid_has_blocks(which, vocab):
     fn = B.so_distill_loss if which is DISTILL else B.so_policy_loss
     assert refused(fn, *dict(which, rows=2 ** 31, vocab=vocab, logits_stride=vocab, grad_stride=vocab).values())
+
+
+@pytest.mark.parametrize("fn,good,name,value", [
+    (B.so_layer_norm_forward, NORM_FORWARD, "eps", 1e39), (B.so_embedding_forward, EMBEDDING_FORWARD, "scale", 1e39),
+    (B.so_embedding_forward, EMBEDDING_FORWARD, "scale", -1e300), (B.so_embedding_backward, EMBEDDING_BACKWARD, "scale", 4e38),
+    (B.so_policy_loss, POLICY, "kl_coef", 1e60), (B.so_distill_loss, DISTILL, "temperature", 4e-39),
+    (B.so_policy_loss, POLICY, "temperature", 3e-39)])
+def test_scalars_that_fp32_does_not_hold_are_refused(fn, good, name, value):
+    """They are finite as given; in fp32 they, or log2(e) / T, are not."""
+    assert refused(fn, *dict(good, **{name: value}).values())
