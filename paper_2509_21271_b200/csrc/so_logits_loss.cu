@@ -304,8 +304,6 @@ constexpr int kMaxSlots = 32;
 constexpr int kMaxCluster = 8;
 constexpr int kMaxDepth = 4;
 constexpr int kQueue = 8;                 // rows dealt out ahead
-constexpr float kLn2 = 0.693147180559945f;
-
 struct RingShape {
     int threads;                          // that compute; the block has 2 + depth warps more
     int cluster, slots, depth;            // blocks a row, chunks of the ring, rows whose targets are at hand
@@ -383,6 +381,16 @@ __device__ __forceinline__ float exponent_of(float z, float m, float c)
 {
     const float ref = m * c;
     return plain(ref) ? fmaf(z, c, -ref) : (z - m) * c;
+}
+
+constexpr float kLn2 = 0.693147180559945f;
+
+// log q of a logit: ln 2 (z c - ref) - ln S, or (z - m) / T - ln S where the exponent in units
+// of log2 exceeds what fp32 holds (a logit of the type's lowest value).
+__device__ __forceinline__ float log_prob(const LossArgs &a, float z, float m, float log_s)
+{
+    const float x = exponent_of(z, m, a.log2e_over_t);
+    return x == -kInf && z != -kInf ? (z - m) * a.inv_temperature - log_s : fmaf(x, kLn2, -log_s);
 }
 
 // Factor that takes a sum from one reference to another.
@@ -629,7 +637,7 @@ __global__ void __launch_bounds__(kShortThreads) loss_short_kernel(LossArgs a)
     if (warp == 0) {
         const MaxSum all = join_lanes(lane < threads / 32 ? s_warp[lane] : MaxSum{-kInf, 0.0f}, c);
         const float log_s = logf(all.s);
-        const auto log_q = [&](float x) { return fmaf(exponent_of(x, all.m, c), kLn2, -log_s); };
+        const auto log_q = [&](float x) { return log_prob(a, x, all.m, log_s); };
         float coef, loss, slope;
         if (kMode == kDistill) {
             loss = distill_row_loss(a, ids, probs, logs, zs, log_q);
@@ -844,7 +852,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
             const float *probs = target_p(buf);
             if (kMode == kDistill && rank == 0) {
                 const float loss = distill_row_loss(a, ids, probs, target_logp(buf), target_z(buf),
-                                                    [&](float z) { return fmaf(exponent(z), kLn2, -done.y); });
+                                                    [&](float z) { return log_prob(a, z, done.x, done.y); });
                 if (lane == 0) a.row_loss[info.row] = loss;
             }
             if (kGrad) {
@@ -1067,8 +1075,7 @@ __global__ void __launch_bounds__(kBig ? kBigThreads + 32 * (2 + kMaxDepth) : 38
                     if (kMode == kDistill) {
                         coef = a.grad_scale * info.weight * a.temperature;
                     } else {
-                        // log q = ln 2 (z c - ref) - ln S
-                        const float logp = fmaf(exponent_of(target_z(buf)[0], ms.m, c), kLn2, -log_s);
+                        const float logp = log_prob(a, target_z(buf)[0], ms.m, log_s);
                         float loss, slope;
                         policy_row(a, logp, info.advantage, info.old_logp, info.ref_logp, loss, slope);
                         if (rank == 0 && lane == 0) {

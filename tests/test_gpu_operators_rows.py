@@ -105,3 +105,28 @@ def test_lookup_of_the_widest_rows():
     table.view(torch.int16).random_(0, 0x7C00)       # finite, every magnitude
     out = ops.embedding_forward(torch.zeros(1, dtype=torch.int64, device="cuda"), table)
     assert torch.equal(out.view(torch.int16), table.view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("vocab", [517, 50_257])
+@pytest.mark.parametrize("rows", [3, 300])
+@pytest.mark.parametrize("temperature", [1.0, 2.0])
+def test_targets_masked_with_the_types_lowest_value(dtype, vocab, rows, temperature):
+    """log q is then the lowest value over T: a number in nats, none in units of log2."""
+    g = gen(vocab + rows)
+    z = (randn(g, rows, vocab) * 2).to(dtype)
+    ids = (5 + 7 * torch.arange(6, device="cuda")).expand(rows, 6).contiguous()
+    z[:, 5] = torch.finfo(dtype).min
+    z[1] = torch.finfo(dtype).min                 # a row of nothing else: uniform
+    teacher = randn(g, rows, 6)
+    weight = torch.full((rows,), 1 / rows, device="cuda")
+    _, row, grad = check_distill(z, ids, teacher, weight, temperature)
+    assert torch.isfinite(row).all() and torch.isfinite(grad).all() and (row[0] > 1e36).all()
+    check_distill(z, ids, teacher, weight, temperature, grad=False)
+    tokens, adv = ids[:, 0].contiguous(), torch.ones(rows, device="cuda")
+    _, _, logp, _ = check_policy(z, tokens, adv, weight, temperature=temperature)
+    assert torch.isfinite(logp).all()
+    # sampled under the same logits: the ratio is 1 and nothing is infinite
+    loss, row, again, grad = ops.policy_loss(z, tokens, adv, weight, old_logp=logp, ref_logp=logp, kl_coef=0.1,
+                                             temperature=temperature)
+    assert same_bits(again, logp) and (row == -1).all() and torch.isfinite(grad).all()
