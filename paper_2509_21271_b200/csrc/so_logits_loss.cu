@@ -163,7 +163,8 @@ __device__ float distill_row_loss(const LossArgs &a, const int32_t *t_id, const 
 __device__ __forceinline__ void policy_row(const LossArgs &a, float logp, float adv, float old_logp, float ref_logp,
                                            float &loss, float &slope)
 {
-    const float ratio = a.old_logp ? expf(logp - old_logp) : 1.0f;
+    float ratio = a.old_logp ? expf(logp - old_logp) : 1.0f;
+    if (ratio == kInf && adv == 0.0f) ratio = 1.0f;      // beyond fp32, but times 0
     const float free_gain = ratio * adv;
     const float held_gain = fminf(fmaxf(ratio, a.clip_lo), a.clip_hi) * adv;
     // written so that a NaN ratio or advantage stays NaN in both

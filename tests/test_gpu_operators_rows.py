@@ -130,3 +130,21 @@ def test_targets_masked_with_the_types_lowest_value(dtype, vocab, rows, temperat
     loss, row, again, grad = ops.policy_loss(z, tokens, adv, weight, old_logp=logp, ref_logp=logp, kl_coef=0.1,
                                              temperature=temperature)
     assert same_bits(again, logp) and (row == -1).all() and torch.isfinite(grad).all()
+
+
+@pytest.mark.parametrize("vocab", [517, 50_257, 480_001])
+@pytest.mark.parametrize("high", [0.2, float("inf")])
+def test_no_advantage_is_no_loss_however_large_the_ratio(vocab, high):
+    """exp(logp - old_logp) is infinite in fp32 beyond 88.7; times 0 it is still 0."""
+    z = randn(gen(vocab), 4, vocab)
+    tokens = torch.tensor([0, 5, 300, vocab - 1], device="cuda")
+    old = torch.tensor([-200.0, -99.0, -1e4, -1e30], device="cuda")
+    adv = torch.tensor([0.0, -0.0, 0.0, 0.0], device="cuda")
+    loss, row, logp, grad = ops.policy_loss(z, tokens, adv, old_logp=old, clip_high=high)
+    assert (row == 0).all() and (loss == 0).all() and (grad == 0).all()
+    adv[1], z[2, 7] = -1.0, float("nan")          # a loss with a ratio like that, and NaN, stay what they are
+    loss, row, logp, grad = ops.policy_loss(z, tokens, adv, old_logp=old, clip_high=high)
+    assert row[0] == 0 and torch.isnan(row[2]) and torch.isnan(grad[2]).all()
+    # the difference rounds to 2^-24 of some 90, the exponential to 2^-22
+    ratio = (logp[1].double() - old[1].double()).exp()
+    assert row[1] == float("inf") if ratio > torch.finfo(FP32).max else abs(row[1].double() - ratio) <= 1e-5 * ratio
