@@ -8,7 +8,7 @@ import torch
 
 from paper_2509_21271_b200 import build as so_build
 from paper_2509_21271_b200 import operators as ops
-from test_gpu_operators import BF16, FP16, FP32, check_distill, check_policy, gen, randn, same_bits
+from test_gpu_operators import BF16, FP16, FP32, check_distill, check_policy, close, gen, path, randn, same_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -148,3 +148,21 @@ def test_no_advantage_is_no_loss_however_large_the_ratio(vocab, high):
     # the difference rounds to 2^-24 of some 90, the exponential to 2^-22
     ratio = (logp[1].double() - old[1].double()).exp()
     assert row[1] == float("inf") if ratio > torch.finfo(FP32).max else abs(row[1].double() - ratio) <= 1e-5 * ratio
+
+
+@pytest.mark.parametrize("offset", [-7.5, 9.0, 300.0, 1e4, 1e6])
+@pytest.mark.parametrize("rows,cols", [(70, 768), (33, 4096), (40, 515), (9, 5000), (5, 9000)])
+def test_layer_norm_backward_of_rows_far_from_zero(rows, cols, offset):
+    """x - mean first, as the formula has it: its rounding is relative to the difference, not
+    to x.  fp32, whose outputs would show it; the mean and rstd are inputs, taken as given."""
+    g = gen(rows + cols)
+    x, dy, w = randn(g, rows, cols) + offset, randn(g, rows, cols) * 0.1, 1 + 0.2 * randn(g, cols)
+    _, mean, rstd = ops.layer_norm_forward(x)
+    dx, dw, db = ops.layer_norm_backward(dy, x, mean, rstd, w)
+    xh = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    gw, r = dy.double() * w.double(), rstd.double()[:, None]
+    want = r * (gw - gw.mean(1, keepdim=True) - xh * (gw * xh).mean(1, keepdim=True))
+    size = r * (gw.abs() + gw.abs().mean(1, keepdim=True) + xh.abs() * (gw * xh).abs().mean(1, keepdim=True))
+    close(dx, want, path(cols) * size, "dx")
+    close(dw, (dy.double() * xh).sum(0), path(rows) * (dy.double() * xh).abs().sum(0), "dweight")
+    close(db, dy.double().sum(0), path(rows) * dy.double().abs().sum(0), "dbias")
