@@ -535,7 +535,8 @@ enum { SO_IDS_INT32 = 0, SO_IDS_INT64 = 1 };
  * so_layer_norm_forward -- y = (x - mean) * rstd * weight + bias over each row,
  * mean and rstd = 1 / sqrt(var + eps) of that row (biased variance).
  *   x, y         [rows, cols] of `dtype`; y may be x (same stride)
- *   weight, bias [cols] of `param_dtype` (= dtype or fp32), each may be NULL
+ *   weight, bias [cols] of `param_dtype` (= dtype or fp32), each may be NULL; off a
+ *                16-byte boundary they send the whole call down the path for odd rows
  *   mean, rstd   fp32 [rows], both or neither (NULL when no backward follows)
  * cols >= 1, eps >= 0.  Errors: SO_ERR_INVALID_ARG, SO_ERR_CUDA.
  */

@@ -26,8 +26,10 @@ struct LookupArgs {
 constexpr int kLookupThreads = 256, kLookupBatch = 8;
 
 // A warp per token.  Bound: memory (the rows written, and each distinct row read once:
-// L2 keeps the rows of frequent tokens).  32767 x 4096 fp16 from 128256 rows: 70 us, of
-// which the bytes take 56 us at a copy's rate; one load in flight per lane: 79 us.
+// L2 keeps the rows of frequent tokens, but for an eighth that is read again).  32767 x 4096
+// fp16 from 128256 rows: 68 us, of which the bytes take 56 us at a copy's rate; one load in
+// flight per lane: 79 us.  Rows that are not aligned, element by element: 32768 x 1001 bf16
+// 39 us for 17 of bytes.
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(kLookupThreads) embedding_forward_kernel(LookupArgs a)
 {
@@ -233,7 +235,8 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
 
 // Bound: memory where the table or the batch is large.  With the sort, 32768 x 2048 bf16
 // into 128256 fp32 rows: 203 us for 181 us of bytes at a copy's rate; 8192 x 768 into
-// 50257 bf16 rows: 25 us for 14 us of bytes (the sort is 8 us of it).  A warp per
+// 50257 bf16 rows: 25 us for 14 us of bytes (the sort is 8 us of it); unaligned rows, four
+// columns a thread: 32768 x 1001 into 50257 bf16 rows 106 us for 25 of bytes.  A warp per
 // table row, runs summed one after the other: 17.0 ms and 1.74 ms (the most frequent
 // token has 6 % of them); zero rows written by the sort's blocks: 232 and 35 us.
 

@@ -289,11 +289,14 @@ __global__ void __launch_bounds__(kRowThreads) loss_two_pass_kernel(LossArgs a)
 // rate).  2-byte logits, the two exponentials an element (16 a clock and SM: 70 % of
 // either phase) and the stores of phase 2 (an SM stores 27 to 30 bytes a clock), one after
 // the other: 4096 x 128256 bf16 with 64 teacher logits and a fifth of the rows masked
-// 368 us, 5.15 TB/s, 79 %; the policy loss of 8191 x 128256 with 30 % masked 669 us,
-// 5.34 TB/s, 81 %.  The chunks are always there before they are asked for.  Measured and
-// not taken: a quarter of the exponentials on the multipliers (391 us), 640 or 768
-// threads (394, 405), two blocks of 256 an SM with clusters of four (441), the maximum
-// kept exactly (397).  A row read twice from memory took 1771 and 2311 us.
+// 364 to 373 us, 5.1 TB/s, 79 %; the policy loss of 8191 x 128256 with 30 % masked 657 to
+// 676 us, 5.4 TB/s, 82 %; the loss alone of 8192 x 128256 464 us (policy) for 321 of bytes.
+// The chunks are always there before they are asked for.  Few rows: a chain of waits, each
+// polled with sleeps, from the row's number to its targets' softmax: 63 x 50257 fp16 16 us,
+// the sum over rows included, for 1.9 of bytes.  Measured and not taken: a quarter of the
+// exponentials on the multipliers (391 us), 640 or 768 threads (394, 405), two blocks of 256
+// an SM with clusters of four (441), the maximum kept exactly (397).  A row read twice from
+// memory took 1771 and 2311 us.
 //
 // A wait that runs out of polls ends its block's work.  When all blocks of the cluster have
 // come to their end they hear of it, and write NaN over all rows of the cluster: their
@@ -305,6 +308,7 @@ constexpr int kMaxSlots = 32;
 constexpr int kMaxCluster = 8;
 constexpr int kMaxDepth = 4;
 constexpr int kQueue = 8;                 // rows dealt out ahead
+
 struct RingShape {
     int threads;                          // that compute; the block has 2 + depth warps more
     int cluster, slots, depth;            // blocks a row, chunks of the ring, rows whose targets are at hand
@@ -481,6 +485,8 @@ __device__ __forceinline__ Vals<E> exponentials(const Vals<E> &z, float m, float
 // that the exponential unit flushes to 0 below 2^-126: what is lost of a sum of 2^60 is
 // below 2^-66 of the total.  And the gradient's factor coef / S has to be a normal number:
 // it is, down to |coef| = 2^-54.  Exponents up to 60 round to 2^-19, 1.3e-6 of an exponential.
+// Rows that need the second sum take longer: 8192 x 50257 bf16 with an element 50 (72 in
+// units of log2) above the others 435 us, without one 331 us.
 constexpr float kSlack = 16.0f, kMost = 0x1p60f;
 
 template <typename T>
@@ -536,7 +542,10 @@ struct Running {
 // as hold its vectors, four each, and as many rows at a time as the SMs have room for.
 // A thread keeps the exponentials against its own maximum, so each is taken once; the
 // gradient is that times one factor per thread.  8191 rows of 4001 bf16 logits, policy
-// loss: 40 us against 71 us by clusters; of 16000, distillation: 189 against 205 us.
+// loss: 38 us against 71 us by clusters, for 20 us of bytes; of 16000, distillation: 189
+// against 205 us, for 80 (with 64 teacher logits 202 us, the policy loss 128).  Loads, the
+// list by one warp, barriers and stores of a row follow each other, and two blocks an SM
+// (60 registers) hide little of that.
 
 constexpr int kShortVectors = 4, kShortThreads = 512;
 

@@ -216,10 +216,12 @@ __device__ __forceinline__ void land(uint32_t bars, int issued, int stages)
 // sqrt(32) standard deviations of the mean, so the difference loses 5 bits at most,
 // however large the mean.  Warps are joined by M2 = sum M2_w + sum n_w (mean_w - mean)^2.
 //
-// Bound: memory (one read, one write of the matrix).  32768 x 4096 bf16: 94 us, 5.70 TB/s,
-// 87 % of a copy's rate; what is left is the exchange of each row's sums.  Registers
-// that prefetch the next row instead of the ring: 125 us; a warp per row with 16
-// vectors a lane (244 registers, 8 warps an SM): 185 us.
+// Bound: memory (one read, one write of the matrix).  32768 x 4096 bf16: 95 to 99 us, 5.4 to
+// 5.7 TB/s, 83 to 86 % of a copy's rate; what is left is the exchange of each row's sums.
+// Registers that prefetch the next row instead of the ring: 125 us; a warp per row with 16
+// vectors a lane (244 registers, 8 warps an SM): 185 us.  Widths that leave lanes idle with
+// four vectors a thread spill: 16384 x 8184 bf16 166 us for 82 of bytes.  Elements one by one
+// (E = 1), each a shared-memory access and a store: 65536 x 1001 bf16 140 us for 40 of bytes.
 //
 // A copy that does not arrive in time turns the rows that the group has not written into
 // NaN, statistics and gradients of the weights included (the optimizer's gradient check
@@ -408,8 +410,10 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 // everyone is done with the rows before, whose place in the ring it refills.
 // A thread keeps its columns' part of dweight and dbias for all its rows.
 //
-// Bound: memory (two reads, one write).  32768 x 2048 bf16: 81 us with the sum over
-// blocks, 4.98 TB/s, 76 % of a copy's rate (this kernel alone 72 us).  The work per
+// Bound: memory (two reads, one write).  32768 x 2048 bf16: 78 to 80 us with the sum over
+// blocks, 5.1 TB/s, 78 % of a copy's rate (this kernel alone 73 us); 32768 x 4096 bf16 190 us
+// for 123 of bytes, 65536 x 1001 bf16 element by element 153 us for 60; 2047 x 768 fp16 14 us
+// on the device, for the 512 partial rows of blocks with one turn each.  The work per
 // row and thread that does not depend on the elements is what costs: 8 elements a
 // thread 86 us, 16 elements 81 us; one row at a time 102 us, two 88 us, four 81 us.
 //
@@ -611,6 +615,11 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= kRowThreads ? 2 : 
 }
 
 // ---- rows too long for that ------------------------------------------------------
+//
+// Forward beyond 32 KB a row of vectors, backward beyond 16 KB (512 threads of four and two
+// vectors), and rows of more than 8192 elements that are not aligned.  The rows come from L2
+// again, and the backward pass updates its partial row in memory: 8192 x 5120 fp32 backward
+// 273 us for 77 of bytes, 16384 x 16384 bf16 1957 us for 246.
 
 // Sum over the block, returned to every thread.  `s` holds one float per warp;
 // the caller alternates between two of them so that one barrier is enough.
