@@ -15,7 +15,7 @@ it behind their producers is the caller's).  Tensors live on the current device.
 Nothing here waits for the device.
 
 Autograd does not record these calls: the backward passes are calls of their own.
-With gradients enabled a tensor that requires grad is refused rather than cut off
+With gradients enabled an input that requires grad is refused rather than cut off
 from its graph; call them under ``torch.no_grad()`` or from a
 ``torch.autograd.Function``.  Tensors that are written over (``out=x``,
 ``grad=logits``, gradients added to) count as modified in place, so that a graph
