@@ -43,12 +43,11 @@ def _refuse(where: str, what: str):
     raise B.SuperOffloadError(B.SO_ERR_INVALID_ARG, f"{where}: {what}")
 
 
-def _unrecorded(where, *tensors):
+def _recorded(where):
+    """Some input requires grad: refused where autograd would be expected to record the call."""
     if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                _refuse(where, "autograd does not record this call, and a tensor given to it requires grad: "
-                               "use torch.no_grad() or a torch.autograd.Function")
+        _refuse(where, "autograd does not record this call, and a tensor given to it requires grad: "
+                       "use torch.no_grad() or a torch.autograd.Function")
 
 
 def _device(where, name, t) -> int:
@@ -152,7 +151,8 @@ def layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, *, out=None
         return _on_stream(stream, layer_norm_forward, x, weight, bias, eps, out=out, mean=mean, rstd=rstd,
                           save_stats=save_stats)
     where = "layer_norm_forward"
-    _unrecorded(where, x, weight, bias)
+    if x.requires_grad or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad:
+        _recorded(where)
     dev = _device(where, "x", x)
     dt = _dtype(where, "x", x)
     rows, cols, stride = _rows(where, "x", x, dev)
@@ -191,7 +191,8 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, *, dx=None, dweight=None
         return _on_stream(stream, layer_norm_backward, dy, x, mean, rstd, weight, dx=dx, dweight=dweight,
                           dbias=dbias, accumulate=accumulate, scratch=scratch)
     where = "layer_norm_backward"
-    _unrecorded(where, dy, x, mean, rstd, weight)
+    if dy.requires_grad or x.requires_grad or weight is not None and weight.requires_grad:
+        _recorded(where)
     dev = _device(where, "x", x)
     dt = _dtype(where, "x", x)
     _same(where, "dy", dy, "x", x)
@@ -240,7 +241,8 @@ def embedding_forward(ids, table, scale: float = 1.0, *, out=None, bad_id=None, 
     if stream is not None:
         return _on_stream(stream, embedding_forward, ids, table, scale, out=out, bad_id=bad_id)
     where = "embedding_forward"
-    _unrecorded(where, table)
+    if table.requires_grad:
+        _recorded(where)
     dev = _device(where, "table", table)
     it = _ids_dtype(where, "ids", ids)
     dt = _dtype(where, "table", table)
@@ -271,7 +273,8 @@ def embedding_backward(ids, dout, dtable, scale: float = 1.0, *, padding_id: int
         return _on_stream(stream, embedding_backward, ids, dout, dtable, scale, padding_id=padding_id,
                           accumulate=accumulate, scratch=scratch)
     where = "embedding_backward"
-    _unrecorded(where, dout, dtable)
+    if dout.requires_grad or dtable.requires_grad:
+        _recorded(where)
     dev = _device(where, "dtable", dtable)
     it = _ids_dtype(where, "ids", ids)
     dt = _dtype(where, "dout", dout)
@@ -325,7 +328,8 @@ def distill_loss(logits, teacher_ids, teacher_logits, weight=None, *, temperatur
         return _on_stream(stream, distill_loss, logits, teacher_ids, teacher_logits, weight,
                           temperature=temperature, grad_scale=grad_scale, grad=grad, loss=loss, row_loss=row_loss)
     where = "distill_loss"
-    _unrecorded(where, logits, teacher_logits, weight)
+    if logits.requires_grad or teacher_logits.requires_grad or weight is not None and weight.requires_grad:
+        _recorded(where)
     dev = _device(where, "logits", logits)
     dt = _dtype(where, "logits", logits)
     rows, vocab, stride = _rows(where, "logits", logits, dev)
@@ -362,7 +366,8 @@ def policy_loss(logits, tokens, advantage, weight=None, *, old_logp=None, ref_lo
                           ref_logp=ref_logp, temperature=temperature, clip_low=clip_low, clip_high=clip_high,
                           kl_coef=kl_coef, grad_scale=grad_scale, grad=grad, loss=loss, row_loss=row_loss, logp=logp)
     where = "policy_loss"
-    _unrecorded(where, logits, advantage, weight, old_logp, ref_logp)
+    if logits.requires_grad or any(t is not None and t.requires_grad for t in (advantage, weight, old_logp, ref_logp)):
+        _recorded(where)
     dev = _device(where, "logits", logits)
     dt = _dtype(where, "logits", logits)
     rows, vocab, stride = _rows(where, "logits", logits, dev)
