@@ -651,6 +651,119 @@ so_status so_policy_loss(const void *logits, int64_t logits_stride, const void *
                          double kl_coef, double grad_scale, void *grad, int64_t grad_stride,
                          float *logp, float *row_loss, float *loss, void *stream);
 
+/*
+ * so_residual_norm_forward -- what lies between two blocks of a residual network,
+ * in one pass: with N the layer norm (kind SO_NORM_LAYER) or the RMS norm
+ * (SO_NORM_RMS: mean 0) of a row,
+ *   u = N(block) * post_weight + post_bias   (post = 1; otherwise u = block)
+ *   h = scale * x + gate * u                 rounded to `dtype`
+ *   y = N(h) * weight + bias                 of h as rounded
+ *   x, block, h, y  [rows, cols] of `dtype`; h may be x or block (same stride)
+ *   gate    [groups, cols] or NULL (1): group i gates the i-th of `groups` equal runs
+ *           of rows (a sequence each; 1 for a gate per channel).  groups <= 65535
+ *   post_weight, post_bias, weight, bias  [cols], each may be NULL; these and gate are of
+ *           `param_dtype` (= dtype or fp32)
+ *   stats   fp32 [4, rows]: mean and rstd of block (0 and 1 without post), of h (mean 0
+ *           with RMS); NULL when no backward follows
+ */
+enum { SO_NORM_LAYER = 0, SO_NORM_RMS = 1 };
+so_status so_residual_norm_forward(const void *x, int64_t x_stride, const void *block, int64_t block_stride,
+                                   const void *gate, int64_t groups, const void *post_weight, const void *post_bias,
+                                   const void *weight, const void *bias, void *h, int64_t h_stride, void *y,
+                                   int64_t y_stride, float *stats, int64_t rows, int64_t cols, int32_t dtype,
+                                   int32_t param_dtype, int32_t kind, int32_t post, double scale, double eps,
+                                   void *stream);
+
+/*
+ * so_residual_norm_backward -- the gradients of that, from dy and dh (what the residual
+ * stream itself passes back; NULL: nothing).  With hat = (h - mean) rstd, e = dy weight,
+ * bhat = (block - post mean) post rstd, the means over a row, and the terms in brackets
+ * for the layer norm alone:
+ *   t      = dh + rstd (e - [mean(e)] - hat mean(e hat)),  dx = scale t
+ *   q      = t gate post_weight,  dblock = post rstd (q - [mean(q)] - bhat mean(q bhat)),
+ *            or t gate without post
+ *   dgate  = sum over its rows of t u,  dpost_weight = sum t gate bhat,
+ *   dpost_bias = sum t gate,  dweight = sum dy hat,  dbias = sum dy
+ *   dgate [groups, cols] and the others [cols] of `grad_dtype`, each may be NULL; with
+ *            `accumulate` the sums are added to what is there (one rounding)
+ *   scratch  so_residual_norm_backward_scratch bytes, 16-byte aligned, only needed if one
+ *            of those is wanted; free for other use once the call has run on its stream
+ * dx and dblock are apart from each other and from the inputs.
+ */
+so_status so_residual_norm_backward_scratch(int64_t rows, int64_t cols, int64_t groups, uint64_t *bytes);
+so_status so_residual_norm_backward(const void *dy, int64_t dy_stride, const void *dh, int64_t dh_stride,
+                                    const void *h, int64_t h_stride, const void *block, int64_t block_stride,
+                                    const float *stats, const void *gate, int64_t groups, const void *post_weight,
+                                    const void *post_bias, const void *weight, void *dx, int64_t dx_stride,
+                                    void *dblock, int64_t dblock_stride, void *dgate, void *dpost_weight,
+                                    void *dpost_bias, void *dweight, void *dbias, int64_t rows, int64_t cols,
+                                    int32_t dtype, int32_t param_dtype, int32_t grad_dtype, int32_t kind, int32_t post,
+                                    int32_t accumulate, double scale, void *scratch, uint64_t scratch_bytes, void *stream);
+
+/*
+ * so_tensor_adamw_* -- AdamW over a list of tensors where they lie: one optimizer
+ * step without arenas for parameters and gradients, its moments in 32 or in 8 bits.
+ *
+ *   g  = grad * grad_scale * c,  c = min(1, max_grad_norm / (norm + 1e-6))
+ *   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g^2
+ *   p' = p - (lr wd p + lr / (1 - beta1^t) m' / (sqrt(v') / sqrt(1 - beta2^t) + eps))
+ *
+ * in fp32, operation by operation; parameters are fp32 and may have a copy in bf16 or
+ * fp16, written in the same pass.  With `clip` the gradients are read once more, before:
+ * norm is that of all gradients times grad_scale, in fp64; where it is not finite (a
+ * square beyond fp32 counts) nothing is written and t stays.  max_grad_norm <= 0 then
+ * looks without clipping.  Without `clip` c = 1 and every gradient is taken as it is.
+ *
+ * The moments belong to the caller: arenas of `blocks` blocks of 256 elements, in which
+ * every tensor begins with a new block; zeros are a fresh start.  8-bit moments have a
+ * byte of scale per block and moment; a block holds magnitudes of m down to 1/1984 of its
+ * largest and of v down to 1/507904, smaller ones as 0 (m) or as that (v, where it is not
+ * 0).  `stochastic` rounds them up or down with the probability that keeps their mean (to
+ * 2^-17 of a code), by a hash of seed, t and the element's place; otherwise to the nearest
+ * code, where an average that moves by less than half a code a step (beta2 = 0.999: always)
+ * stays where it is.  A value that is not finite makes its block NaN.
+ *
+ * t, the last norm and the seeds' state live in `record` (SO_TENSOR_RECORD_BYTES of device
+ * memory, 16-byte aligned, zeros for t = 0), so that a captured step may be replayed:
+ *   int64 t; float norm, c, skipped (0 or 1)
+ * `scratch` (so_tensor_adamw_layout's bytes, 16-byte aligned) is needed with `clip` and free
+ * for other use once the call has run on its stream.  Calls on one record are made one after
+ * the other.  Tensors of no elements are passed over; the sums' order depends on the sizes
+ * alone, and results repeat bit for bit.
+ * Errors: SO_ERR_INVALID_ARG, SO_ERR_CUDA.
+ */
+#define SO_TENSOR_BLOCK 256
+#define SO_TENSOR_RECORD_BYTES 64
+#define SO_TENSOR_MAX_BLOCKS (INT64_C(1) << 33)
+#define SO_TENSOR_NO_COPY (-1)
+
+typedef struct so_tensor {
+    void *param;                  /* fp32 [numel], 4-byte aligned (32: the fast case) */
+    const void *grad;             /* [numel] of grad_dtype */
+    void *copy;                   /* [numel] of copy_dtype, or unused */
+    int64_t numel;
+} so_tensor;
+
+typedef struct so_tensor_adamw_info {
+    int64_t blocks;
+    uint64_t bytes_moment;        /* each of m and v, 32-byte aligned */
+    uint64_t bytes_scale;         /* each of their scales, 0 with 32 bits */
+    uint64_t bytes_record, bytes_scratch;
+} so_tensor_adamw_info;
+
+so_status so_tensor_adamw_layout(const so_tensor *tensors, int32_t n_tensors, int32_t state_bits,
+                                 so_tensor_adamw_info *info);
+so_status so_tensor_adamw_step(const so_tensor *tensors, int32_t n_tensors, int32_t grad_dtype,
+                               int32_t copy_dtype, int32_t state_bits, void *m, void *v,
+                               uint8_t *m_scale, uint8_t *v_scale, const so_hparams *hp,
+                               double grad_scale, int32_t clip, int32_t stochastic, uint64_t seed,
+                               void *record, void *scratch, uint64_t scratch_bytes, void *stream);
+
+/* 8-bit moments as bf16 [blocks * 256], which holds every value they stand for. */
+so_status so_tensor_adamw_moments(const void *m, const void *v, const uint8_t *m_scale,
+                                  const uint8_t *v_scale, int64_t blocks, void *m_out, void *v_out,
+                                  void *stream);
+
 /* How many times the operators' kernels poll for a copy or an exchange between
  * blocks before they give up (0 .. 2^20, the default): in the block or cluster
  * `unit` of each launch, or with -1 in all of them.  What gives up comes out as

@@ -25,6 +25,8 @@ SO_ALL = -1
 SO_DTYPE_BF16, SO_DTYPE_FP32, SO_DTYPE_FP16 = 0, 1, 2
 SO_IDS_INT32, SO_IDS_INT64 = 0, 1
 SO_DISTILL_MAX_TOP_K = 1024
+SO_NORM_LAYER, SO_NORM_RMS = 0, 1
+SO_TENSOR_BLOCK, SO_TENSOR_NO_COPY = 256, -1
 DECISION_NAMES = {0: "COMMIT", 1: "SKIP", 2: "CLIP_RESTEP"}
 
 
@@ -64,6 +66,15 @@ class so_counters(C.Structure):
                 ("timeouts", C.c_int64)]
 
 
+class so_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("numel", C.c_int64)]
+
+
+class so_tensor_adamw_info(C.Structure):
+    _fields_ = [("blocks", C.c_int64), ("bytes_moment", C.c_uint64), ("bytes_scale", C.c_uint64),
+                ("bytes_record", C.c_uint64), ("bytes_scratch", C.c_uint64)]
+
+
 class SuperOffloadError(RuntimeError):
     def __init__(self, status: int, where: str, cuda_error: int = 0):
         self.status = status
@@ -89,7 +100,9 @@ EXPORTS = ["so_layout_init", "so_layout_get_info", "so_layout_tensor", "so_layou
            "so_debug_set_dry_run", "so_debug_set_bucket_stats", "so_debug_set_step_variant",
            "so_layer_norm_forward", "so_layer_norm_backward_scratch", "so_layer_norm_backward",
            "so_embedding_forward", "so_embedding_backward_scratch", "so_embedding_backward",
-           "so_distill_loss", "so_policy_loss", "so_debug_set_operator_polls"]
+           "so_distill_loss", "so_policy_loss", "so_debug_set_operator_polls",
+           "so_residual_norm_forward", "so_residual_norm_backward_scratch", "so_residual_norm_backward",
+           "so_tensor_adamw_layout", "so_tensor_adamw_step", "so_tensor_adamw_moments"]
 
 
 def lib() -> C.CDLL:
@@ -150,6 +163,15 @@ def lib() -> C.CDLL:
                             i64, vp, vp, vp],
         "so_policy_loss": [vp, i64, vp, i32, vp, vp, vp, vp, i64, i64, i32, dbl, dbl, dbl, dbl, dbl,
                            vp, i64, vp, vp, vp, vp],
+        "so_residual_norm_forward": [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32,
+                                     i32, dbl, dbl, vp],
+        "so_residual_norm_backward_scratch": [i64, i64, i64, P(C.c_uint64)],
+        "so_residual_norm_backward": [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp,
+                                      vp, vp, vp, i64, i64, i32, i32, i32, i32, i32, i32, dbl, vp, C.c_uint64, vp],
+        "so_tensor_adamw_layout": [P(so_tensor), i32, i32, P(so_tensor_adamw_info)],
+        "so_tensor_adamw_step": [P(so_tensor), i32, i32, i32, i32, vp, vp, vp, vp, P(so_hparams), dbl, i32, i32,
+                                 C.c_uint64, vp, vp, C.c_uint64, vp],
+        "so_tensor_adamw_moments": [vp, vp, vp, vp, i64, vp, vp, vp],
     }
     for name, argtypes in sig.items():
         fn = getattr(L, name)
@@ -441,6 +463,35 @@ def so_distill_loss(*args) -> None:
 
 def so_policy_loss(*args) -> None:
     _ok(None, lib().so_policy_loss(*args), "so_policy_loss")
+
+
+def so_residual_norm_forward(*args) -> None:
+    _ok(None, lib().so_residual_norm_forward(*args), "so_residual_norm_forward")
+
+
+def so_residual_norm_backward_scratch(rows: int, cols: int, groups: int) -> int:
+    n = C.c_uint64()
+    _ok(None, lib().so_residual_norm_backward_scratch(rows, cols, groups, C.byref(n)), "so_residual_norm_backward_scratch")
+    return n.value
+
+
+def so_residual_norm_backward(*args) -> None:
+    _ok(None, lib().so_residual_norm_backward(*args), "so_residual_norm_backward")
+
+
+def so_tensor_adamw_layout(tensors, n: int, state_bits: int) -> so_tensor_adamw_info:
+    """`tensors`: an array of so_tensor (only the sizes are looked at)."""
+    info = so_tensor_adamw_info()
+    _ok(None, lib().so_tensor_adamw_layout(tensors, n, state_bits, C.byref(info)), "so_tensor_adamw_layout")
+    return info
+
+
+def so_tensor_adamw_step(*args) -> None:
+    _ok(None, lib().so_tensor_adamw_step(*args), "so_tensor_adamw_step")
+
+
+def so_tensor_adamw_moments(*args) -> None:
+    _ok(None, lib().so_tensor_adamw_moments(*args), "so_tensor_adamw_moments")
 
 
 def so_debug_set_operator_polls(polls: int, unit: int = -1) -> None:

@@ -1,0 +1,546 @@
+// AdamW over a list of tensors where they lie, with its moments in 32 or in 8 bits.
+//
+//   g  = grad * (grad_scale * clip),  clip = min(1, max_norm / (norm + 1e-6))
+//   m' = beta1 m + (1 - beta1) g,     v' = beta2 v + (1 - beta2) g g
+//   p' = p - (lr wd p + lr / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps))
+//
+// in fp32, every operation rounded by itself (no contraction).  The moments lie in arenas
+// of the optimizer, each tensor's from a block of 256 elements on.
+//
+// An 8-bit moment has 4 bits of fraction and, for m, 3 bits of exponent and a sign, for v,
+// 4 bits of exponent.  With f and e those bits it stands for f units where e = 0, for
+// (16 + f) 2^(e - 1) otherwise; a unit is 2^(s - 127) with s a byte of the block, chosen so
+// that the block's largest value fits.  The largest m is 1984 units, the largest v 507904,
+// so that a block spans 2^11 in m and, as v is a square, 2^9.5 in the size of gradients.
+// s = 0 marks a block of zeros, s = 255 one that holds a value which is not finite (all of
+// it is NaN then).  A v that is not zero is never rounded to zero: a moment without a
+// second moment would be divided by eps alone.
+//
+// That code is the bit pattern of an fp32 number of as many units of 2^-130, cut off above
+// its last 19 bits: fp32 has the same step from its subnormal to its normal numbers.  So a
+// value is encoded by two multiplications (the second rounds to 2^-19 of a unit), the
+// addition of 2^18 (to nearest) or of 16 random bits (stochastically) to the bits below,
+// and a shift.
+#include "so_ops.cuh"
+
+using namespace so_ops;
+
+namespace {
+
+constexpr int kBlock = SO_TENSOR_BLOCK;   // elements that share a scale, and what a warp takes at a time
+constexpr int kLane = kBlock / 32;        // consecutive elements of a lane
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxTensors = 640;          // of a launch: the table is a kernel parameter of 25 KB
+constexpr int kMaxRun = 8;                // blocks a warp takes in a row
+constexpr int kNormBlocks = 1184;         // thread blocks of a norm launch, at most; the same on every device
+
+struct Entry {
+    float *param;
+    const void *grad;
+    void *copy;
+    int64_t numel, first;                 // its first block, counted over the list
+};
+
+// What the device knows of an optimizer's progress: SO_TENSOR_RECORD_BYTES of the caller's.
+struct Record {
+    int64_t t;                            // steps taken
+    float norm, coef, skipped;            // of the last step: norm of the gradients, clip factor, 1 if it was skipped
+    float factor;                         // grad_scale * clip
+    float rsqrt_bc2, step_size;           // 1 / sqrt(1 - beta2^t), lr / (1 - beta1^t)
+    uint32_t key;                         // of the step's random numbers
+    uint32_t done;                        // thread blocks whose sums are in place
+};
+static_assert(sizeof(Record) <= SO_TENSOR_RECORD_BYTES, "the record fits");
+
+struct Hyper {
+    double lr, beta1, beta2, max_norm, grad_scale;
+    uint64_t seed;
+    int32_t clip;
+};
+
+// MurmurHash3's 32-bit finalizer (Appleby; public domain).
+__host__ __device__ __forceinline__ uint32_t mix(uint32_t x)
+{
+    x ^= x >> 16;
+    x *= 0x85EBCA6Bu;
+    x ^= x >> 13;
+    x *= 0xC2B2AE35u;
+    return x ^ (x >> 16);
+}
+
+// Closes the gradients' look and opens the step: one thread.
+__device__ void begin_step(Record *r, double sumsq, const Hyper &h)
+{
+    float norm = 0.0f, coef = 1.0f;
+    bool skip = false;
+    if (h.clip) {
+        const double wide = sqrt(sumsq) * fabs(h.grad_scale);
+        skip = !(wide <= 1.7976931348623157e308);        // infinite, or NaN
+        norm = (float)wide;
+        if (h.max_norm > 0.0) coef = (float)fmin(1.0, h.max_norm / (wide + 1e-6));
+        if (skip) coef = 0.0f;
+    }
+    r->norm = norm;
+    r->coef = coef;
+    r->skipped = skip ? 1.0f : 0.0f;
+    r->factor = __fmul_rn((float)h.grad_scale, coef);
+    if (skip) return;
+    const int64_t t = r->t + 1;
+    r->t = t;
+    r->rsqrt_bc2 = (float)(1.0 / sqrt(1.0 - pow(h.beta2, (double)t)));
+    r->step_size = (float)(h.lr / (1.0 - pow(h.beta1, (double)t)));
+    r->key = mix(mix((uint32_t)h.seed) ^ mix((uint32_t)(h.seed >> 32) ^ 0x9E3779B9u) ^ (uint32_t)t);
+}
+
+__global__ void begin_kernel(Record *r, const __grid_constant__ Hyper h) { begin_step(r, 0.0, h); }
+
+struct Table {
+    int32_t n;
+    int64_t blocks;                       // of all its tensors
+    int64_t first;                        // of its first tensor
+    Entry e[kMaxTensors];
+};
+
+// Index of the tensor that holds block b (tensors without elements have none).
+__device__ __forceinline__ int tensor_of(const Table &t, int64_t b)
+{
+    int lo = 0, hi = t.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (t.e[mid].first <= b) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// kLane elements of a matrix of any alignment, those from `n` on as zeros.
+template <typename T>
+__device__ __forceinline__ void load_lane(const T *p, int n, bool vectors, float (&f)[kLane])
+{
+    if (vectors && n >= kLane) {
+        if constexpr (sizeof(T) == 4) {
+            uint32_t w[8];
+            asm("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
+        } else {
+            unpack<T>(__ldcs(reinterpret_cast<const uint4 *>(p)), f);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) f[i] = i < n ? to_f32(p[i]) : 0.0f;
+    }
+}
+
+// The same of an array that this kernel writes.
+__device__ __forceinline__ void load_own(const float *p, int n, bool vectors, float (&f)[kLane])
+{
+    if (vectors && n >= kLane) {
+        asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]) : "l"(p));
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) f[i] = i < n ? p[i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void store_own(float *p, int n, bool vectors, const float (&f)[kLane])
+{
+    if (vectors && n >= kLane) {
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]),
+                     "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]) : "memory");
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLane; ++i)
+            if (i < n) p[i] = f[i];
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_copy(T *p, int n, bool vectors, const float (&f)[kLane])
+{
+    if (vectors && n >= kLane) {
+        __stcs(reinterpret_cast<uint4 *>(p), pack<T>(f));
+    } else {
+#pragma unroll
+        for (int i = 0; i < kLane; ++i)
+            if (i < n) p[i] = from_f32<T>(f[i]);
+    }
+}
+
+// Sum of the squares of all gradients: fp32 over a lane's eight, fp64 from there on, in a fixed
+// order.  The thread block that comes last adds the blocks' sums and opens the step.
+template <typename G>
+__global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ Table t, const __grid_constant__ Hyper h, Record *record,
+                                                        double *sums, uint32_t first_sum, uint32_t all_sums)
+{
+    __shared__ double s_sum[kWarps];
+    __shared__ bool s_last;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    double sum = 0.0;
+    const int64_t warps = (int64_t)gridDim.x * kWarps, me = (int64_t)blockIdx.x * kWarps + warp;
+    const int64_t each = (t.blocks + warps - 1) / warps;
+    int64_t b = t.first + me * each, end = b + each;
+    if (end > t.first + t.blocks) end = t.first + t.blocks;
+    int k = b < end ? tensor_of(t, b) : 0;
+    while (b < end) {
+        const Entry &e = t.e[k];
+        const G *grad = static_cast<const G *>(e.grad);
+        const bool vectors = (reinterpret_cast<uintptr_t>(grad) & (sizeof(G) * kLane - 1)) == 0;
+        const int64_t have = (e.numel + kBlock - 1) / kBlock + e.first;
+        const int64_t stop = end < have ? end : have;
+        for (; b < stop; b += 4) {
+            float f[4][kLane];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t at = (b + u - e.first) * kBlock + lane * kLane;
+                const int64_t left = b + u < stop ? e.numel - at : 0;
+                load_lane(grad + at, left > kLane ? kLane : (int)left, vectors, f[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                float q = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kLane; ++i) q = fmaf(f[u][i], f[u][i], q);
+                sum += (double)q;
+            }
+        }
+        b = stop;
+        if (b < end) do ++k; while (k + 1 < t.n && t.e[k + 1].first <= b);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double s = 0.0;
+        for (int i = 0; i < kWarps; ++i) s += s_sum[i];
+        sums[first_sum + blockIdx.x] = s;
+        __threadfence();
+        s_last = atomicAdd(&record->done, 1u) == all_sums - 1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    sum = 0.0;
+    for (uint32_t i = threadIdx.x; i < all_sums; i += kThreads) sum += __ldcg(sums + i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double s = 0.0;
+        for (int i = 0; i < kWarps; ++i) s += s_sum[i];
+        record->done = 0;
+        begin_step(record, s, h);
+    }
+}
+
+struct Step {
+    float beta1, omb1, beta2, omb2, eps, decay;
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;
+    const Record *record;
+    int32_t run, stochastic;
+};
+
+// Values of 8 codes in units of 2^-4 of the block's scale, times `factor`.
+template <bool kSigned>
+__device__ __forceinline__ void decode(uint2 codes, uint32_t scale, float (&f)[kLane])
+{
+    const float factor = scale == 255 ? kNan : __uint_as_float((scale + 4) << 23);
+    const uint32_t w[2] = {codes.x, codes.y};
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) {
+        const uint32_t c = (w[i >> 2] >> (8 * (i & 3))) & 255u;
+        const uint32_t bits = kSigned ? ((c & 127u) << 19) | ((c & 128u) << 24) : c << 19;
+        f[i] = __fmul_rn(__fmul_rn(__uint_as_float(bits), 0x1p126f), factor);
+    }
+}
+
+// The scale of a block from the bit pattern of its largest magnitude: the largest code
+// stands for 31/16 2^kTop units.
+template <int kTop>
+__device__ __forceinline__ uint32_t scale_of(uint32_t most)
+{
+    const int exponent = (int)(most >> 23);
+    if (exponent == 255) return 255;
+    if (most == 0) return 0;
+    const int s = exponent + ((most & 0x7FFFFFu) > 0x780000u) - kTop;
+    return s < 1 ? 1u : (uint32_t)s;
+}
+
+template <bool kSigned>
+__device__ __forceinline__ uint2 encode(const float (&f)[kLane], uint32_t scale, const uint32_t (&noise)[kLane])
+{
+    if (scale == 255) return make_uint2(0, 0);
+    const float up = __uint_as_float((254u - (scale < 1 ? 1u : scale)) << 23);
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) {
+        const uint32_t y = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(f[i]), up), 0x1p-130f));
+        uint32_t c = (y + noise[i]) >> 19;
+        if (kSigned) c |= (__float_as_uint(f[i]) >> 24) & 128u;
+        else if (c == 0 && f[i] > 0.0f) c = 1;
+        w[i >> 2] |= c << (8 * (i & 3));
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+__device__ __forceinline__ uint32_t most_of(const float (&f)[kLane])
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) most = max(most, __float_as_uint(f[i]) & 0x7FFFFFFFu);
+    return __reduce_max_sync(0xFFFFFFFFu, most);
+}
+
+// A warp takes `run` blocks in a row, a lane eight consecutive elements of each.
+template <int kBits, typename G, typename C>
+__global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ Table t, const __grid_constant__ Step s)
+{
+    const int lane = threadIdx.x & 31;
+    int64_t b = t.first + ((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * s.run, end = b + s.run;
+    if (end > t.first + t.blocks) end = t.first + t.blocks;
+    if (b >= end) return;
+    int k = tensor_of(t, b);
+    grid_dependency_wait();
+    if (s.record->skipped != 0.0f) return;
+    const float factor = s.record->factor, rsqrt_bc2 = s.record->rsqrt_bc2, step_size = s.record->step_size;
+    const uint32_t key = s.record->key;
+    for (; b < end; ++b) {
+        while (k + 1 < t.n && t.e[k + 1].first <= b) ++k;
+        const Entry &e = t.e[k];
+        const int64_t at = (b - e.first) * kBlock + lane * kLane, left = e.numel - at;
+        const int n = left >= kLane ? kLane : left > 0 ? (int)left : 0;
+        const int64_t slot = b * kBlock + lane * kLane;
+        float *param = e.param + at;
+        const G *grad = static_cast<const G *>(e.grad) + at;
+        const bool own = (reinterpret_cast<uintptr_t>(param) & 31) == 0;
+        float p[kLane], g[kLane], m[kLane], v[kLane];
+        load_own(param, n, own, p);
+        load_lane(grad, n, (reinterpret_cast<uintptr_t>(grad) & (sizeof(G) * kLane - 1)) == 0, g);
+        if constexpr (kBits == 8) {
+            const uint2 mc = *reinterpret_cast<const uint2 *>(static_cast<uint8_t *>(s.m) + slot);
+            const uint2 vc = *reinterpret_cast<const uint2 *>(static_cast<uint8_t *>(s.v) + slot);
+            decode<true>(mc, s.m_scale[b], m);
+            decode<false>(vc, s.v_scale[b], v);
+        } else {
+            load_own(static_cast<float *>(s.m) + slot, kLane, true, m);
+            load_own(static_cast<float *>(s.v) + slot, kLane, true, v);
+        }
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) {
+            const float x = __fmul_rn(g[i], factor);
+            m[i] = __fadd_rn(__fmul_rn(m[i], s.beta1), __fmul_rn(x, s.omb1));
+            v[i] = __fadd_rn(__fmul_rn(v[i], s.beta2), __fmul_rn(__fmul_rn(x, s.omb2), x));
+            const float u = __fdiv_rn(m[i], __fadd_rn(__fmul_rn(__fsqrt_rn(v[i]), rsqrt_bc2), s.eps));
+            p[i] = __fsub_rn(p[i], __fadd_rn(__fmul_rn(p[i], s.decay), __fmul_rn(u, step_size)));
+            if (i >= n) m[i] = v[i] = 0.0f;   // behind a tensor's end the arenas hold zeros
+        }
+        store_own(param, n, own, p);
+        if constexpr (!std::is_same<C, void>::value) {
+            C *copy = static_cast<C *>(e.copy) + at;
+            store_copy<C>(copy, n, (reinterpret_cast<uintptr_t>(copy) & 15) == 0, p);
+        }
+        if constexpr (kBits == 8) {
+            const uint32_t ms = scale_of<10>(most_of(m)), vs = scale_of<18>(most_of(v));
+            uint32_t nm[kLane], nv[kLane];
+            if (s.stochastic) {
+                const uint32_t high = mix(key + (uint32_t)(slot >> 32)), low = (uint32_t)slot;
+#pragma unroll
+                for (int i = 0; i < kLane; ++i) {
+                    const uint32_t x = mix((low + i) ^ high);
+                    nm[i] = ((x & 0xFFFFu) << 3) + 4;
+                    nv[i] = ((x >> 16) << 3) + 4;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kLane; ++i) nm[i] = nv[i] = 1u << 18;
+            }
+            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(s.m) + slot) = encode<true>(m, ms, nm);
+            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(s.v) + slot) = encode<false>(v, vs, nv);
+            if (lane == 0) {
+                s.m_scale[b] = (uint8_t)ms;
+                s.v_scale[b] = (uint8_t)vs;
+            }
+        } else {
+            store_own(static_cast<float *>(s.m) + slot, kLane, true, m);
+            store_own(static_cast<float *>(s.v) + slot, kLane, true, v);
+        }
+    }
+}
+
+// 8-bit moments as the values they stand for; bf16 holds each of them.
+__global__ void __launch_bounds__(kThreads) moments_kernel(const uint8_t *m, const uint8_t *v, const uint8_t *m_scale,
+                                                           const uint8_t *v_scale, bf16_t *m_out, bf16_t *v_out, int64_t blocks)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t b = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    if (b >= blocks) return;
+    const int64_t slot = b * kBlock + lane * kLane;
+    float f[kLane];
+    decode<true>(__ldcs(reinterpret_cast<const uint2 *>(m + slot)), m_scale[b], f);
+    __stcs(reinterpret_cast<uint4 *>(m_out + slot), pack<bf16_t>(f));
+    decode<false>(__ldcs(reinterpret_cast<const uint2 *>(v + slot)), v_scale[b], f);
+    __stcs(reinterpret_cast<uint4 *>(v_out + slot), pack<bf16_t>(f));
+}
+
+// ---- host ------------------------------------------------------------------------
+
+int64_t blocks_of(int64_t numel) { return numel / kBlock + (numel % kBlock != 0); }
+
+bool finite32(double x) { return std::isfinite(x) && std::isfinite((float)x); }
+
+// Blocks of the whole list, -1 if a size or their sum is not one of a list.
+int64_t list_blocks(const so_tensor *t, int32_t n)
+{
+    int64_t sum = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (t[i].numel < 0 || t[i].numel > int64_t(1) << 40) return -1;
+        sum += blocks_of(t[i].numel);
+        if (sum > SO_TENSOR_MAX_BLOCKS) return -1;
+    }
+    return sum;
+}
+
+unsigned norm_grid(int64_t blocks)
+{
+    // a warp takes four blocks at a time
+    const int64_t want = (blocks + 4 * kWarps - 1) / (4 * kWarps);
+    return want < 1 ? 1u : want > kNormBlocks ? (unsigned)kNormBlocks : (unsigned)want;
+}
+
+// Calls `fn(table)` for every kMaxTensors of the list.
+template <typename F>
+so_status for_tables(const so_tensor *t, int32_t n, F fn)
+{
+    Table table;
+    int64_t block = 0;
+    int32_t i = 0;
+    while (i < n) {
+        table.n = 0;
+        table.first = block;
+        for (; i < n && table.n < kMaxTensors; ++i) {
+            if (t[i].numel == 0) continue;
+            Entry &e = table.e[table.n++];
+            e.param = static_cast<float *>(t[i].param);
+            e.grad = t[i].grad;
+            e.copy = t[i].copy;
+            e.numel = t[i].numel;
+            e.first = block;
+            block += blocks_of(t[i].numel);
+        }
+        table.blocks = block - table.first;
+        if (table.n == 0) continue;
+        const so_status st = fn(table);
+        if (st != SO_OK) return st;
+    }
+    return SO_OK;
+}
+
+template <int kBits, typename G, typename C>
+so_status launch_step(const Table &t, const Step &s, cudaStream_t stream)
+{
+    const int64_t runs = (t.blocks + s.run - 1) / s.run;
+    return launch(step_kernel<kBits, G, C>, (unsigned)((runs + kWarps - 1) / kWarps), kThreads, 0, stream, true, t, s);
+}
+template <int kBits, typename G>
+so_status launch_step(int32_t copy_dtype, const Table &t, const Step &s, cudaStream_t stream)
+{
+    if (copy_dtype == SO_DTYPE_BF16) return launch_step<kBits, G, bf16_t>(t, s, stream);
+    if (copy_dtype == SO_DTYPE_FP16) return launch_step<kBits, G, f16_t>(t, s, stream);
+    return launch_step<kBits, G, void>(t, s, stream);
+}
+template <int kBits>
+so_status launch_step(int32_t grad_dtype, int32_t copy_dtype, const Table &t, const Step &s, cudaStream_t stream)
+{
+    if (grad_dtype == SO_DTYPE_BF16) return launch_step<kBits, bf16_t>(copy_dtype, t, s, stream);
+    if (grad_dtype == SO_DTYPE_FP16) return launch_step<kBits, f16_t>(copy_dtype, t, s, stream);
+    return launch_step<kBits, float>(copy_dtype, t, s, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+so_status so_tensor_adamw_layout(const so_tensor *tensors, int32_t n_tensors, int32_t state_bits, so_tensor_adamw_info *info)
+{
+    if (!info || n_tensors < 0 || (n_tensors > 0 && !tensors) || (state_bits != 8 && state_bits != 32)) return SO_ERR_INVALID_ARG;
+    const int64_t blocks = list_blocks(tensors, n_tensors);
+    if (blocks < 0) return SO_ERR_INVALID_ARG;
+    info->blocks = blocks;
+    info->bytes_moment = (uint64_t)blocks * kBlock * (state_bits / 8);
+    info->bytes_scale = state_bits == 8 ? (uint64_t)blocks : 0;
+    info->bytes_record = SO_TENSOR_RECORD_BYTES;
+    // one sum per thread block of the norm's launches
+    info->bytes_scratch = ((uint64_t)n_tensors / kMaxTensors + 1) * kNormBlocks * sizeof(double);
+    return SO_OK;
+}
+
+so_status so_tensor_adamw_step(const so_tensor *tensors, int32_t n_tensors, int32_t grad_dtype, int32_t copy_dtype,
+                               int32_t state_bits, void *m, void *v, uint8_t *m_scale, uint8_t *v_scale,
+                               const so_hparams *hp, double grad_scale, int32_t clip, int32_t stochastic,
+                               uint64_t seed, void *record, void *scratch, uint64_t scratch_bytes, void *stream)
+{
+    so_tensor_adamw_info info;
+    const so_status st = so_tensor_adamw_layout(tensors, n_tensors, state_bits, &info);
+    if (st != SO_OK) return st;
+    if (!valid_dtype(grad_dtype) || (copy_dtype != SO_TENSOR_NO_COPY && copy_dtype != SO_DTYPE_BF16 && copy_dtype != SO_DTYPE_FP16))
+        return SO_ERR_INVALID_ARG;
+    if ((clip != 0 && clip != 1) || (stochastic != 0 && stochastic != 1) || (stochastic && state_bits != 8)) return SO_ERR_INVALID_ARG;
+    if (!hp || !record || !aligned(record, 16) || !finite32(grad_scale)) return SO_ERR_INVALID_ARG;
+    if (!(hp->lr >= 0.0) || !finite32(hp->lr) || !(hp->beta1 >= 0.0 && hp->beta1 < 1.0) || !(hp->beta2 >= 0.0 && hp->beta2 < 1.0) ||
+        !(hp->eps > 0.0) || (float)hp->eps == 0.0f || !finite32(hp->eps) || !(hp->weight_decay >= 0.0) || !finite32(hp->lr * hp->weight_decay) ||
+        !finite32(hp->lr / (1.0 - hp->beta1)) || std::isnan(hp->max_grad_norm))
+        return SO_ERR_INVALID_ARG;
+    if (clip && (!scratch || !aligned(scratch, 16) || scratch_bytes < info.bytes_scratch)) return SO_ERR_INVALID_ARG;
+    if (info.blocks > 0) {
+        if (!m || !v || !aligned(m, 32) || !aligned(v, 32)) return SO_ERR_INVALID_ARG;
+        if (state_bits == 8 && (!m_scale || !v_scale)) return SO_ERR_INVALID_ARG;
+    }
+    for (int32_t i = 0; i < n_tensors; ++i) {
+        const so_tensor &t = tensors[i];
+        if (t.numel == 0) continue;
+        if (!t.param || !aligned(t.param, 4) || !t.grad || !aligned(t.grad, elem_size(grad_dtype))) return SO_ERR_INVALID_ARG;
+        if (copy_dtype != SO_TENSOR_NO_COPY && (!t.copy || !aligned(t.copy, 2))) return SO_ERR_INVALID_ARG;
+    }
+    const cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    Record *r = static_cast<Record *>(record);
+    const Hyper h = {hp->lr, hp->beta1, hp->beta2, hp->max_grad_norm, grad_scale, seed, clip};
+    so_status done;
+    if (clip && info.blocks > 0) {
+        uint32_t sums = 0, at = 0;
+        for_tables(tensors, n_tensors, [&](const Table &t) { sums += norm_grid(t.blocks); return SO_OK; });
+        done = for_tables(tensors, n_tensors, [&](const Table &t) {
+            const unsigned grid = norm_grid(t.blocks);
+            const auto kernel = grad_dtype == SO_DTYPE_BF16 ? norm_kernel<bf16_t> : grad_dtype == SO_DTYPE_FP16 ? norm_kernel<f16_t> : norm_kernel<float>;
+            const so_status one = launch(kernel, grid, kThreads, 0, cs, false, t, h, r, static_cast<double *>(scratch), at, sums);
+            at += grid;
+            return one;
+        });
+    } else {
+        done = launch(begin_kernel, 1, 1, 0, cs, false, r, h);
+    }
+    if (done != SO_OK) return done;
+    Step s = {(float)hp->beta1, (float)(1.0 - hp->beta1), (float)hp->beta2, (float)(1.0 - hp->beta2), (float)hp->eps,
+              (float)(hp->lr * hp->weight_decay), m, v, m_scale, v_scale, r, 1, stochastic};
+    return for_tables(tensors, n_tensors, [&](const Table &t) {
+        // runs as long as leave every SM of a B200 a few dozen warps
+        const int64_t run = t.blocks / (148 * 64);
+        s.run = (int32_t)(run < 1 ? 1 : run > kMaxRun ? kMaxRun : run);
+        return state_bits == 8 ? launch_step<8>(grad_dtype, copy_dtype, t, s, cs) : launch_step<32>(grad_dtype, copy_dtype, t, s, cs);
+    });
+}
+
+so_status so_tensor_adamw_moments(const void *m, const void *v, const uint8_t *m_scale, const uint8_t *v_scale, int64_t blocks,
+                                  void *m_out, void *v_out, void *stream)
+{
+    if (blocks < 0 || blocks > SO_TENSOR_MAX_BLOCKS) return SO_ERR_INVALID_ARG;
+    if (blocks == 0) return SO_OK;
+    if (!m || !v || !m_scale || !v_scale || !m_out || !v_out || !aligned(m, 8) || !aligned(v, 8) || !aligned(m_out, 16) || !aligned(v_out, 16))
+        return SO_ERR_INVALID_ARG;
+    return launch(moments_kernel, (unsigned)((blocks + kWarps - 1) / kWarps), kThreads, 0, static_cast<cudaStream_t>(stream), false,
+                  static_cast<const uint8_t *>(m), static_cast<const uint8_t *>(v), m_scale, v_scale, static_cast<bf16_t *>(m_out),
+                  static_cast<bf16_t *>(v_out), blocks);
+}
+
+}  // extern "C"

@@ -1,7 +1,7 @@
-"""Operators at the two ends of a training step, on torch tensors.
+"""Operators of a training step around its matrix products, on torch tensors.
 
-Token embedding, layer norm, and the losses on the logits, each with its
-gradient; every one is a call of the C ABI (``include/superoffload.h`` has the
+Token embedding, layer norm, the norms on both sides of a residual, and the losses
+on the logits, each with its gradient; every one is a call of the C ABI (``include/superoffload.h`` has the
 formulas and the rules on strides, types and masked rows).  Torch allocates the
 results that the caller does not bring and names the stream, nothing else.
 
@@ -121,6 +121,8 @@ def _scratch(where, scratch, dev):
 
 _norm_scratch = lru_cache(maxsize=512)(B.so_layer_norm_backward_scratch)      # sizes alone decide
 _embedding_scratch = lru_cache(maxsize=512)(B.so_embedding_backward_scratch)
+_residual_scratch = lru_cache(maxsize=512)(B.so_residual_norm_backward_scratch)
+_KINDS = {"layer": B.SO_NORM_LAYER, "rms": B.SO_NORM_RMS}
 
 
 def _done(status: int, where: str, written) -> None:
@@ -231,6 +233,151 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, *, dx=None, dweight=None
                              ws, need, _raw_stream(dev)), where,
           [t for t in (dx, dweight, dbias) if t is not None])
     return dx, dweight, dbias
+
+
+# ---- the norms on both sides of a residual ------------------------------------------
+
+def _params(where, dt, dev, cols, gate, named):
+    """(dtype, gate's address, number of gates, the others' addresses) of parameters of one dtype."""
+    first = gate
+    for _, t in named:
+        first = t if first is None else first
+    if first is None:
+        return dt, None, 1, [None] * len(named)
+    pt = _dtype(where, "weight", first)
+    groups = 1 if gate is None or gate.dim() == 1 else gate.shape[0]
+    if gate is not None and (gate.dim() > 2 or gate.shape[-1] != cols):
+        _refuse(where, "gate must be a row, or a matrix of one row per group of rows")
+    return pt, _vector(where, "gate", gate, groups * cols, dev, first.dtype), groups, \
+        [_vector(where, name, t, cols, dev, first.dtype) for name, t in named]
+
+
+def residual_norm_forward(x, block, gate=None, post_weight=None, post_bias=None, weight=None, bias=None, *,
+                          kind: str = "layer", post: bool = True, scale: float = 1.0, eps: float = 1e-5, h=None,
+                          y=None, stats=None, save_stats: bool = True, stream=None):
+    """What lies between two blocks: with u the norm of `block` (times `post_weight`,
+    plus `post_bias`), or `block` itself where `post` is False,
+    h = scale * x + gate * u and y = norm(h) * weight + bias; returns (h, y, stats).
+
+    `kind` is "layer" or "rms".  `gate` is a row, or [groups, cols] with a row for each
+    of `groups` equal runs of rows; the parameters have one dtype, x's or fp32.  `h` may
+    be `x` or `block`.  `stats` (fp32 [4, rows]) is for the backward pass; None with
+    ``save_stats=False``."""
+    if stream is not None:
+        return _on_stream(stream, residual_norm_forward, x, block, gate, post_weight, post_bias, weight, bias,
+                          kind=kind, post=post, scale=scale, eps=eps, h=h, y=y, stats=stats, save_stats=save_stats)
+    where = "residual_norm_forward"
+    if x.requires_grad or block.requires_grad or any(
+            t is not None and t.requires_grad for t in (gate, post_weight, post_bias, weight, bias)):
+        _recorded(where)
+    dev = _device(where, "x", x)
+    dt = _dtype(where, "x", x)
+    _same(where, "block", block, "x", x)
+    rows, cols, stride = _rows(where, "x", x, dev)
+    _, _, block_stride = _rows(where, "block", block, dev)
+    if kind not in _KINDS:
+        _refuse(where, "kind is 'layer' or 'rms'")
+    if h is None:
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _same(where, "h", h, "x", x)
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _same(where, "y", y, "x", x)
+    _, _, h_stride = _rows(where, "h", h, dev)
+    _, _, y_stride = _rows(where, "y", y, dev)
+    pt, gp, groups, (pw, pb, w, b) = _params(where, dt, dev, cols, gate, (
+        ("post_weight", post_weight), ("post_bias", post_bias), ("weight", weight), ("bias", bias)))
+    if not save_stats:
+        if stats is not None:
+            _refuse(where, "stats are not written with save_stats=False")
+    elif stats is None:
+        stats = torch.empty(4, rows, dtype=torch.float32, device=x.device)
+    _done(B.lib().so_residual_norm_forward(
+        x.data_ptr(), stride, block.data_ptr(), block_stride, gp, groups, pw, pb, w, b, h.data_ptr(), h_stride,
+        y.data_ptr(), y_stride, _vector(where, "stats", stats, 4 * rows, dev, torch.float32), rows, cols, dt, pt,
+        _KINDS[kind], int(post), scale, eps, _raw_stream(dev)), where, (h, y) if stats is None else (h, y, stats))
+    return h, y, stats
+
+
+def residual_norm_backward(dy, dh, h, block, stats, gate=None, post_weight=None, post_bias=None, weight=None, *,
+                           kind: str = "layer", post: bool = True, scale: float = 1.0, dx=None, dblock=None,
+                           dgate=None, dpost_weight=None, dpost_bias=None, dweight=None, dbias=None,
+                           accumulate: bool = False, scratch=None, stream=None):
+    """Gradients of the forward pass from `dy` and `dh` (the residual stream's own; None:
+    nothing); returns (dx, dblock, dgate, dpost_weight, dpost_bias, dweight, dbias).
+
+    The parameters' gradients are written (with `accumulate`: added to) where given, of
+    one dtype, and not computed where False.  Where None they are allocated in the
+    parameters' dtype: dgate, dpost_weight and dpost_bias if that parameter is given,
+    dweight always, dbias with the layer norm.  `scratch`:
+    so_residual_norm_backward_scratch bytes."""
+    if stream is not None:
+        return _on_stream(stream, residual_norm_backward, dy, dh, h, block, stats, gate, post_weight, post_bias, weight,
+                          kind=kind, post=post, scale=scale, dx=dx, dblock=dblock, dgate=dgate,
+                          dpost_weight=dpost_weight, dpost_bias=dpost_bias, dweight=dweight, dbias=dbias,
+                          accumulate=accumulate, scratch=scratch)
+    where = "residual_norm_backward"
+    if dy.requires_grad or h.requires_grad or block.requires_grad or any(
+            t is not None and t.requires_grad for t in (dh, gate, post_weight, post_bias, weight)):
+        _recorded(where)
+    dev = _device(where, "h", h)
+    dt = _dtype(where, "h", h)
+    rows, cols, h_stride = _rows(where, "h", h, dev)
+    _same(where, "dy", dy, "h", h)
+    _same(where, "block", block, "h", h)
+    _, _, dy_stride = _rows(where, "dy", dy, dev)
+    _, _, block_stride = _rows(where, "block", block, dev)
+    dh_stride = 0
+    if dh is not None:
+        _same(where, "dh", dh, "h", h)
+        _, _, dh_stride = _rows(where, "dh", dh, dev)
+    if kind not in _KINDS:
+        _refuse(where, "kind is 'layer' or 'rms'")
+    if dx is None:
+        dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    else:
+        _same(where, "dx", dx, "h", h)
+    if dblock is None:
+        dblock = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    else:
+        _same(where, "dblock", dblock, "h", h)
+    _, _, dx_stride = _rows(where, "dx", dx, dev)
+    _, _, dblock_stride = _rows(where, "dblock", dblock, dev)
+    pt, gp, groups, (pw, pb, w) = _params(where, dt, dev, cols, gate, (
+        ("post_weight", post_weight), ("post_bias", post_bias), ("weight", weight)))
+    kind_of = next((t.dtype for t in (gate, post_weight, post_bias, weight) if t is not None), h.dtype)
+    grads = []
+    for name, g, n, wanted in (("dgate", dgate, groups * cols, gate is not None),
+                               ("dpost_weight", dpost_weight, cols, post_weight is not None),
+                               ("dpost_bias", dpost_bias, cols, post_bias is not None),
+                               ("dweight", dweight, cols, True), ("dbias", dbias, cols, kind == "layer")):
+        if g is None and wanted:
+            if accumulate:
+                _refuse(where, f"accumulate needs {name} (or False)")
+            g = torch.empty(gate.shape if name == "dgate" else (cols,), dtype=kind_of, device=h.device)
+        elif g is False:
+            g = None
+        elif g is not None and not wanted and name == "dgate":
+            _refuse(where, "there is no gate to have a gradient")
+        grads.append((name, g, n))
+    some = next((g for _, g, _ in grads if g is not None), None)
+    gt, need, ws = dt, 0, None
+    if some is not None:
+        gt = _dtype(where, "a parameter's gradient", some)
+        if scratch is None:
+            scratch = torch.empty(_residual_scratch(rows, cols, groups), dtype=torch.uint8, device=h.device)
+        need, ws = _scratch(where, scratch, dev), scratch.data_ptr()
+    out = tuple(g for _, g, _ in grads)
+    _done(B.lib().so_residual_norm_backward(
+        dy.data_ptr(), dy_stride, None if dh is None else dh.data_ptr(), dh_stride, h.data_ptr(), h_stride,
+        block.data_ptr(), block_stride, _vector(where, "stats", stats, 4 * rows, dev, torch.float32), gp, groups, pw, pb,
+        w, dx.data_ptr(), dx_stride, dblock.data_ptr(), dblock_stride,
+        *[_vector(where, name, g, n, dev, some.dtype if g is not None else None) for name, g, n in grads], rows, cols, dt,
+        pt, gt, _KINDS[kind], int(post), int(accumulate), scale, ws, need, _raw_stream(dev)), where,
+        [t for t in (dx, dblock, *out) if t is not None])
+    return (dx, dblock, *out)
 
 
 # ---- embedding -------------------------------------------------------------------
