@@ -652,6 +652,44 @@ so_status so_policy_loss(const void *logits, int64_t logits_stride, const void *
                          float *logp, float *row_loss, float *loss, void *stream);
 
 /*
+ * so_linear_cross_entropy -- cross entropy of labels, from the hidden states and the
+ * table of the head, with both gradients, in pieces of the vocabulary: the logits
+ * z = hidden table^T are never kept.
+ *   row_loss = log sum_j exp z_j - z_label,  loss = sum_rows weight * row_loss
+ *   P        = weight (softmax(z) - [label])
+ *   dhidden  = grad_scale P table,  dtable = grad_scale P^T hidden
+ *   hidden  [rows, cols], table [vocab, cols], of `dtype` (bf16 or fp16)
+ *   labels  [rows]; a row whose label is outside [0, vocab), and a row of weight 0, is not
+ *           read: its loss and gradient are 0 whatever it holds
+ *   weight  fp32 [rows], NULL = 1 for every row
+ *   dhidden [rows, cols] of `dtype`, NULL: not wanted; may be hidden (same stride)
+ *   dtable  [vocab, cols] of `grad_dtype`, NULL: not wanted; with `accumulate` added to
+ *           what is there (one rounding)
+ *   row_loss fp32 [rows], loss fp32 [1]
+ *   scratch  so_linear_cross_entropy_scratch bytes, 256-byte aligned, contents irrelevant;
+ *           free for other use once the call has run on its stream.  `packed`: 1 unless
+ *           table is 16-byte aligned and its stride a multiple of 8; such a table is copied,
+ *           piece by piece.  `gradients`: 1 if either is wanted
+ * Products are summed in fp32.  P is rounded to `dtype`, relative to a power of two near the
+ * largest |weight| (fp16 holds what is above 2^-39 of that); where dtable is fp32 it is summed
+ * from parts that hold P to 24 bits.  A row with a logit of NaN or +inf, or of -inf throughout,
+ * has a NaN loss, and NaN in its row of dhidden and in all of dtable.
+ */
+#define SO_LINEAR_MAX_ROWS (INT64_C(1) << 22)
+#define SO_LINEAR_MAX_VOCAB (INT64_C(1) << 26)
+#define SO_LINEAR_MAX_COLS (INT64_C(1) << 16)
+so_status so_linear_cross_entropy_scratch(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype,
+                                          int32_t grad_dtype, int32_t gradients, int32_t packed,
+                                          uint64_t *bytes);
+so_status so_linear_cross_entropy(const void *hidden, int64_t hidden_stride, const void *table,
+                                  int64_t table_stride, const void *labels, int32_t ids_dtype,
+                                  const float *weight, int64_t rows, int64_t vocab, int64_t cols,
+                                  int32_t dtype, double grad_scale, void *dhidden,
+                                  int64_t dhidden_stride, void *dtable, int64_t dtable_stride,
+                                  int32_t grad_dtype, int32_t accumulate, float *row_loss,
+                                  float *loss, void *scratch, uint64_t scratch_bytes, void *stream);
+
+/*
  * so_residual_norm_forward -- what lies between two blocks of a residual network,
  * in one pass: with N the layer norm (kind SO_NORM_LAYER) or the RMS norm
  * (SO_NORM_RMS: mean 0) of a row,

@@ -101,6 +101,7 @@ EXPORTS = ["so_layout_init", "so_layout_get_info", "so_layout_tensor", "so_layou
            "so_layer_norm_forward", "so_layer_norm_backward_scratch", "so_layer_norm_backward",
            "so_embedding_forward", "so_embedding_backward_scratch", "so_embedding_backward",
            "so_distill_loss", "so_policy_loss", "so_debug_set_operator_polls",
+           "so_linear_cross_entropy_scratch", "so_linear_cross_entropy",
            "so_residual_norm_forward", "so_residual_norm_backward_scratch", "so_residual_norm_backward",
            "so_tensor_adamw_layout", "so_tensor_adamw_step", "so_tensor_adamw_moments"]
 
@@ -163,6 +164,9 @@ def lib() -> C.CDLL:
                             i64, vp, vp, vp],
         "so_policy_loss": [vp, i64, vp, i32, vp, vp, vp, vp, i64, i64, i32, dbl, dbl, dbl, dbl, dbl,
                            vp, i64, vp, vp, vp, vp],
+        "so_linear_cross_entropy_scratch": [i64, i64, i64, i32, i32, i32, i32, P(C.c_uint64)],
+        "so_linear_cross_entropy": [vp, i64, vp, i64, vp, i32, vp, i64, i64, i64, i32, dbl, vp, i64, vp, i64, i32, i32, vp, vp,
+                                    vp, C.c_uint64, vp],
         "so_residual_norm_forward": [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, i64, i32, i32, i32,
                                      i32, dbl, dbl, vp],
         "so_residual_norm_backward_scratch": [i64, i64, i64, P(C.c_uint64)],
@@ -463,6 +467,18 @@ def so_distill_loss(*args) -> None:
 
 def so_policy_loss(*args) -> None:
     _ok(None, lib().so_policy_loss(*args), "so_policy_loss")
+
+
+def so_linear_cross_entropy_scratch(rows: int, vocab: int, cols: int, dtype: int, grad_dtype: int, gradients: int,
+                                    packed: int) -> int:
+    n = C.c_uint64()
+    _ok(None, lib().so_linear_cross_entropy_scratch(rows, vocab, cols, dtype, grad_dtype, gradients, packed, C.byref(n)),
+        "so_linear_cross_entropy_scratch")
+    return n.value
+
+
+def so_linear_cross_entropy(*args) -> None:
+    _ok(None, lib().so_linear_cross_entropy(*args), "so_linear_cross_entropy")
 
 
 def so_residual_norm_forward(*args) -> None:

@@ -1,0 +1,1148 @@
+// Cross entropy of labels from the hidden states and the table of the head, with both
+// gradients, in pieces of the vocabulary: the logits are never kept.
+//
+//   z = H W^T,  row_loss = log sum_j exp z_j - z_label,  loss = sum w row_loss
+//   P = w (softmax(z) - [label]),  dH = s P W,  dW = s P^T H
+//
+// Rows of weight 0 or without a label in the vocabulary are left out from the start: the
+// others are gathered into a matrix of their own, which also gives every row an aligned
+// start and whole tiles.  Then
+//   statistics     a pass over all logits, tile by tile: each row's maximum and sum
+//   for each piece the piece's logits once more, as P in 16 bits; dH += P W; dW = P^T H
+// are all one kernel, a persistent matrix product on the tensor cores (tcgen05: operands
+// through TMA into swizzled shared memory, two accumulators of 256 columns in tensor
+// memory, so that one is read while the next is computed) with four ways to end a tile.
+//
+// P is w (q - [label]) as a multiple of a power of two near the largest |w| (for fp16 of
+// 2^-15 of it: its normal numbers then reach down to 2^-29 of a row's largest).  Its
+// rounding to 16 bits is one rounding of every term of sums that are themselves
+// rounded to 16 bits; where dW is fp32, it sums P in several parts of 16 bits that
+// together hold all 24.
+#include <cuda.h>
+
+#include "so_ops.cuh"
+
+using namespace so_ops;
+
+namespace {
+
+constexpr int kTileN = 256;               // columns of a tile
+constexpr int kTileK = 64;                // of a step: 128 bytes, the width of the swizzle
+constexpr int kRowsOfCta = 128;           // rows of a tile that a block holds
+constexpr int kThreads = 192;             // a warp that copies, one that multiplies, four that end tiles
+constexpr int kRowPad = 256;              // rows are padded to whole tiles of a pair of blocks
+constexpr float kLog2e = 1.44269504088896340736f;
+
+enum Mode { kStats, kProb, kHidden, kTable };
+
+// What the device finds out about a call, in scratch.
+struct Control {
+    int32_t live;                         // rows that take part
+    float unit;                           // P is a multiple of this: a power of two
+    uint32_t ticket;                      // blocks of the statistics' join that are done
+    int32_t gave_up;                      // a wait ran out: every result becomes NaN
+};
+
+// ---- tensor memory, matrix instructions, tensor copies -----------------------------
+
+__device__ __forceinline__ uint32_t cta_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address of this block's `addr` in the block of rank `rank`
+__device__ __forceinline__ uint32_t of_rank(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+template <int kCtas>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    if constexpr (kCtas == 2)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+template <int kCtas>
+__device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t cols)
+{
+    if constexpr (kCtas == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <int kCtas>
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t cols)
+{
+    if constexpr (kCtas == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(cols) : "memory");
+}
+template <int kCtas>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    if constexpr (kCtas == 2)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// The barrier (of both blocks of a pair) is arrived at once the instructions so far are done.
+template <int kCtas>
+__device__ __forceinline__ void commit(uint32_t bar)
+{
+    if constexpr (kCtas == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 32 columns of the warp's 32 lanes of tensor memory
+__device__ __forceinline__ void tmem_load(uint32_t at, float (&f)[32])
+{
+    uint32_t r[32];
+    __syncwarp();                         // all lanes, whatever they did with the columns before
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+                   "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+                   "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(at));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
+}
+
+// Descriptors.  An operand whose K elements are contiguous lies in rows of 128 bytes (64 of
+// them), groups of eight rows 1024 bytes apart.  One whose M (or N) elements are contiguous
+// lies in rows of 128 bytes for each k: groups of eight k 1024 bytes apart, groups of 64 of its
+// M (or N) elements kMajorStep bytes apart.  Either is swizzled over 128 bytes.
+constexpr uint32_t kMajorStep = kTileK * 128;
+constexpr uint64_t kDescBase = (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+__device__ __forceinline__ uint64_t descriptor(uint32_t addr, bool k_contiguous)
+{
+    return kDescBase | (uint64_t)((k_contiguous ? 16 : kMajorStep) >> 4) << 16 | (uint64_t)((addr & 0x3FFFF) >> 4);
+}
+// bytes from one instruction's operand (16 elements of K) to the next one's
+template <bool kContiguous> constexpr uint32_t kStepBytes = kContiguous ? 32 : 16 * 128;
+
+// fp32 accumulators; A and B bf16 or fp16; contiguous in K (0) or in M, N (1)
+template <typename T>
+__host__ __device__ constexpr uint32_t instruction(int m, int n, bool a_k, bool b_k)
+{
+    const uint32_t type = std::is_same<T, bf16_t>::value ? 1 : 0;
+    return 1u << 4 | type << 7 | type << 10 | (a_k ? 0u : 1u) << 15 | (b_k ? 0u : 1u) << 16 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
+}
+
+// ---- the product ----------------------------------------------------------------------
+
+struct Product {
+    Control *control;
+    int64_t width;                        // vocabulary of this launch
+    int64_t first;                        // its first entry
+    int64_t table_row;                    // row of the (perhaps packed) table where that is
+    int64_t vocab, cols;
+    int32_t rows_pad;
+    int32_t splits;                       // kHidden: parts that the vocabulary is summed in
+    int32_t planes;                       // kProb, kTable: parts of P
+    int32_t begin;                        // kHidden: the sums begin here rather than going on
+    const int32_t *label;                 // [rows_pad], of the gathered rows
+    float *label_logit;                   // [rows_pad]
+    const float *lse2;                    // [rows_pad], in units of log 2
+    const float *coef;                    // [rows_pad], w over the unit
+    float2 *stats;                        // [tiles of the vocabulary][rows_pad]: maximum, sum
+    void *prob;                           // [planes][rows_pad][prob_stride]
+    int64_t prob_stride;
+    float *part;                          // [splits][rows_pad][part_stride]
+    int64_t part_stride;
+    void *table_grad;
+    int64_t grad_stride;
+    int32_t grad_dtype, accumulate, grad_vectors;
+    float grad_scale;
+    Patience patience;
+};
+
+// Which tile, and which steps of K.
+struct Item {
+    int m, n, split, steps, k0;           // k0: first step
+};
+
+template <int kMode, int kCtas>
+struct Work {
+    int m_tiles, n_tiles, k_steps;
+    int64_t items;
+    __device__ Work(const Product &p, int live)
+    {
+        constexpr int kTileM = kRowsOfCta * kCtas;
+        const int row_tiles = (live + kTileM - 1) / kTileM, col_tiles = (int)((p.cols + kTileN - 1) / kTileN);
+        if (kMode == kStats || kMode == kProb) {
+            m_tiles = row_tiles;
+            n_tiles = (int)((p.width + kTileN - 1) / kTileN);
+            k_steps = (int)((p.cols + kTileK - 1) / kTileK);
+        } else if (kMode == kHidden) {
+            m_tiles = row_tiles;
+            n_tiles = col_tiles;
+            k_steps = (int)((p.width + kTileK - 1) / kTileK);
+        } else {
+            m_tiles = live ? (int)((p.width + kTileM - 1) / kTileM) : 0;
+            n_tiles = col_tiles;
+            k_steps = (live + kTileK - 1) / kTileK;
+        }
+        items = (int64_t)m_tiles * n_tiles * (kMode == kHidden ? p.splits : 1);
+    }
+    __device__ __forceinline__ Item item(const Product &p, int64_t i) const
+    {
+        Item r;
+        r.split = 0;
+        r.k0 = 0;
+        r.steps = k_steps;
+        if (kMode == kStats || kMode == kProb) {
+            // the rows' tiles one after the other: a tile of the table is read once, the hidden states stay in L2
+            r.n = (int)(i / m_tiles);
+            r.m = (int)(i - (int64_t)r.n * m_tiles);
+        } else {
+            const int64_t q = i / n_tiles;
+            r.n = (int)(i - q * n_tiles);
+            r.m = (int)(q % m_tiles);
+            r.split = (int)(q / m_tiles);
+        }
+        if (kMode == kHidden) {
+            r.k0 = (int)((int64_t)k_steps * r.split / p.splits);
+            r.steps = (int)((int64_t)k_steps * (r.split + 1) / p.splits) - r.k0;
+        } else if (kMode == kTable) {
+            r.steps = k_steps * p.planes;
+        }
+        return r;
+    }
+};
+
+template <int kCtas>
+struct Shape {
+    static constexpr uint32_t kA = kRowsOfCta * 128, kB = kTileN / kCtas * 128, kStage = kA + kB;
+    static constexpr int kStages = kCtas == 2 ? 6 : 4;
+    static constexpr size_t kBytes = (size_t)kStage * kStages + 1024;
+};
+
+struct Shared {
+    uint64_t full[8], empty[8], done[2], free[2], last;
+    uint32_t tmem;
+    volatile uint32_t gave_up;
+};
+
+// A wait that ends when the barrier's phase does, when it runs out, or when another of the block
+// has run out; false unless the first.
+__device__ __forceinline__ bool await(uint32_t bar, uint32_t parity, uint32_t polls, Shared &s, Control *c)
+{
+    if (s.gave_up) return false;
+    for (uint32_t left = polls; left > 0;) {
+        const uint32_t now = left < 1024 ? left : 1024;
+        if (mbar_wait(bar, parity, now)) return true;
+        if (s.gave_up) return false;
+        left -= now;
+    }
+    s.gave_up = 1;
+    atomicExch(&c->gave_up, 1);
+    return false;
+}
+
+// 16 elements of a row as T (or 8 as fp32) in one store
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                 "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+__device__ __forceinline__ void load32(const void *p, uint32_t (&w)[8])
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    if constexpr (std::is_same<T, bf16_t>::value) return pack2_bf16(lo, hi);
+    else return pack2_f16(lo, hi);
+}
+template <typename T> __device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi)
+{
+    lo = to_f32(T{(uint16_t)(w & 0xFFFFu)});
+    hi = to_f32(T{(uint16_t)(w >> 16)});
+}
+
+// A row's maximum and sum over the tile's columns, and its label's logit if that is here.
+__device__ __forceinline__ void end_stats(const Product &p, uint32_t tmem, int64_t row, int live, int n)
+{
+    const int64_t n0 = p.first + (int64_t)n * kTileN;
+    const int cols = p.vocab - n0 < kTileN ? (int)(p.vocab - n0) : kTileN;
+    const bool in = row < live;
+    const int64_t label = in ? (int64_t)p.label[row] - n0 : -1;
+    float top = -kInf;
+    for (int c = 0; c < cols; c += 32) {
+        float f[32];
+        tmem_load(tmem + c, f);
+        if (c + 32 <= cols) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = fmaxf(top, f[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (c + i < cols) top = fmaxf(top, f[i]);
+        }
+        if (__any_sync(0xFFFFFFFFu, label >= c && label < c + 32)) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (label == c + i) p.label_logit[row] = f[i];
+        }
+    }
+    const float ref = top == -kInf ? 0.0f : top * kLog2e;   // a tile of nothing else adds nothing
+    float sum0 = 0.0f, sum1 = 0.0f;
+    for (int c = 0; c < cols; c += 32) {
+        float f[32];
+        tmem_load(tmem + c, f);
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            sum0 += c + i < cols ? exp2_fast(fmaf(f[i], kLog2e, -ref)) : 0.0f;
+            sum1 += c + i + 1 < cols ? exp2_fast(fmaf(f[i + 1], kLog2e, -ref)) : 0.0f;
+        }
+    }
+    if (in) p.stats[(n0 / kTileN) * p.rows_pad + row] = make_float2(top, sum0 + sum1);
+}
+
+// P of the tile, in `planes` parts of 16 bits; zero in rows and columns that are not there.
+template <typename T>
+__device__ __forceinline__ void end_prob(const Product &p, uint32_t tmem, int64_t row, int live, int n)
+{
+    const int64_t n0 = p.first + (int64_t)n * kTileN;
+    const int cols = p.vocab - n0 < kTileN ? (int)(p.vocab - n0) : kTileN;
+    const bool in = row < live;
+    const int64_t label = in ? (int64_t)p.label[row] - n0 : -1;
+    const float lse2 = in ? p.lse2[row] : 0.0f, coef = in ? p.coef[row] : 0.0f;
+    T *out = static_cast<T *>(p.prob) + row * p.prob_stride + (int64_t)n * kTileN;
+    for (int c = 0; c < kTileN; c += 32) {
+        float f[32];
+        tmem_load(tmem + c, f);
+        const bool here = __any_sync(0xFFFFFFFFu, label >= c && label < c + 32);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            float q = exp2_fast(fmaf(f[i], kLog2e, -lse2));
+            if (here && label == c + i) q -= 1.0f;
+            f[i] = in && c + i < cols ? q * coef : 0.0f;
+        }
+        for (int plane = 0;; ++plane) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = pack2<T>(f[2 * i], f[2 * i + 1]);
+            T *to = out + (int64_t)plane * p.rows_pad * p.prob_stride + c;
+            const uint32_t a[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]}, b[8] = {w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]};
+            store32(to, a);
+            store32(to + 16, b);
+            if (plane + 1 == p.planes) break;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float lo, hi;
+                unpack2<T>(w[i], lo, hi);
+                f[2 * i] -= lo;
+                f[2 * i + 1] -= hi;
+            }
+        }
+    }
+}
+
+// The tile added to (or begun as) a part of dH, fp32; `nothing`: a short piece had no columns for it.
+__device__ __forceinline__ void end_hidden(const Product &p, uint32_t tmem, int64_t row, int live, int n, int split, bool nothing)
+{
+    float *out = p.part + ((int64_t)split * p.rows_pad + row) * p.part_stride + (int64_t)n * kTileN;
+    for (int c = 0; c < kTileN; c += 32) {
+        float f[32];
+        tmem_load(tmem + c, f);
+        if (row >= live) continue;
+        if (nothing) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f[i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+            uint32_t w[8];
+            if (!p.begin) {
+                load32(out + c + i, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[i + j] += __uint_as_float(w[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(f[i + j]);
+            store32(out + c + i, w);
+        }
+    }
+}
+
+// The tile as rows of dW, in the gradient's type.
+__device__ __forceinline__ void end_table(const Product &p, uint32_t tmem, int64_t row, int n, float scale)
+{
+    const int64_t v = p.first + row;
+    const bool in = row < p.width && v < p.vocab;
+    const int64_t c0 = (int64_t)n * kTileN;
+    for (int c = 0; c < kTileN && c0 + c < p.cols; c += 32) {
+        float f[32];
+        tmem_load(tmem + c, f);
+        if (!in) continue;
+        const int64_t at = v * p.grad_stride + c0 + c;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) f[i] *= scale;
+        if (p.grad_vectors && c0 + c + 32 <= p.cols) {
+            if (p.grad_dtype == SO_DTYPE_FP32) {
+                float *out = static_cast<float *>(p.table_grad) + at;
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    uint32_t w[8];
+                    if (p.accumulate) {
+                        load32(out + i, w);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) f[i + j] += __uint_as_float(w[j]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(f[i + j]);
+                    store32(out + i, w);
+                }
+            } else {
+                uint16_t *out = static_cast<uint16_t *>(p.table_grad) + at;
+                const bool bf = p.grad_dtype == SO_DTYPE_BF16;
+#pragma unroll
+                for (int i = 0; i < 32; i += 16) {
+                    uint32_t w[8];
+                    if (p.accumulate) {
+                        load32(out + i, w);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            float lo, hi;
+                            if (bf) unpack2<bf16_t>(w[j], lo, hi);
+                            else unpack2<f16_t>(w[j], lo, hi);
+                            f[i + 2 * j] += lo;
+                            f[i + 2 * j + 1] += hi;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = bf ? pack2_bf16(f[i + 2 * j], f[i + 2 * j + 1]) : pack2_f16(f[i + 2 * j], f[i + 2 * j + 1]);
+                    store32(out + i, w);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (c0 + c + i < p.cols)
+                    store_any(p.table_grad, at + i, p.grad_dtype, p.accumulate ? f[i] + load_any(p.table_grad, at + i, p.grad_dtype) : f[i]);
+        }
+    }
+}
+
+template <typename T, int kMode, int kCtas>
+__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                               const __grid_constant__ Product p)
+{
+    using S = Shape<kCtas>;
+    constexpr bool kAK = kMode != kTable;                    // A contiguous in K: H, H, P; P transposed is not
+    constexpr bool kBK = kMode == kStats || kMode == kProb;  // B: W by its columns, else W and H by their rows
+    extern __shared__ uint8_t s_raw[];
+    __shared__ __align__(8) Shared s;
+    const uint32_t tiles = (smem_addr(s_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = kCtas == 2 ? cta_rank() : 0;
+    const int unit = (int)(blockIdx.x / kCtas), units = (int)(gridDim.x / kCtas);
+    const uint32_t polls = p.patience.of(unit);
+    const uint32_t full = smem_addr(s.full), empty = smem_addr(s.empty), done = smem_addr(s.done), free = smem_addr(s.free);
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(done + 8 * i, 1);
+            mbar_init(free + 8 * i, 4 * kCtas);
+        }
+        mbar_init(smem_addr(&s.last), 1);
+        mbar_init_fence();
+        s.gave_up = polls == 0;
+        if (polls == 0) atomicExch(&p.control->gave_up, 1);
+    }
+    if (warp == 1) tmem_alloc<kCtas>(smem_addr(&s.tmem), 512);
+    fence_before();
+    __syncthreads();
+    if (kCtas == 2) cluster_sync();
+    fence_after();
+    const uint32_t tmem = s.tmem;
+    grid_dependency_wait();
+    const int live = p.control->live;
+    const Work<kMode, kCtas> work(p, live);
+
+    if (warp == 0 && lane == 0) {
+        // copies: this block's rows of A and its share of B
+        int stage = 0, issued = 0;
+        uint32_t phase = 1;
+        bool ok = true;
+        for (int64_t i = unit; ok && i < work.items; i += units) {
+            const Item it = work.item(p, i);
+            const int m0 = (it.m * kCtas + (int)rank) * kRowsOfCta, n0 = it.n * kTileN + (int)rank * (kTileN / kCtas);
+            for (int k = 0; k < it.steps; ++k) {
+                if (!(ok = await(empty + 8 * stage, phase, polls, s, p.control))) break;
+                const uint32_t bar = kCtas == 2 ? of_rank(full + 8 * stage, 0) : full + 8 * stage;
+                const uint32_t a = tiles + stage * S::kStage, b = a + S::kA;
+                if (rank == 0) mbar_expect(full + 8 * stage, S::kStage * kCtas);
+                int step = it.k0 + k, plane = 0;
+                if (kMode == kTable) plane = step / work.k_steps, step -= plane * work.k_steps;
+                const int k0 = step * kTileK;
+                if (kAK) {
+                    tma_load<kCtas>(a, &map_a, k0, m0, bar);
+                } else {
+#pragma unroll
+                    for (int g = 0; g < kRowsOfCta / 64; ++g) tma_load<kCtas>(a + g * kMajorStep, &map_a, m0 + 64 * g, plane * p.rows_pad + k0, bar);
+                }
+                if (kBK) {
+#pragma unroll
+                    for (int g = 0; g < 2 / kCtas; ++g) tma_load<kCtas>(b + g * 128 * 128, &map_b, k0, (int)p.table_row + n0 + 128 * g, bar);
+                } else {
+#pragma unroll
+                    for (int g = 0; g < kTileN / kCtas / 64; ++g)
+                        tma_load<kCtas>(b + g * kMajorStep, &map_b, n0 + 64 * g, (kMode == kHidden ? (int)p.table_row : 0) + k0, bar);
+                }
+                ++issued;
+                if (++stage == S::kStages) stage = 0, phase ^= 1;
+            }
+        }
+        // a block that gives up waits for what is still on its way
+        if (!ok && rank == 0)
+            for (int k = issued > S::kStages ? issued - S::kStages : 0; k < issued; ++k)
+                mbar_wait(full + 8 * (k % S::kStages), (uint32_t)(k / S::kStages) & 1u, kPolls);
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        constexpr uint32_t kInstruction = instruction<T>(kRowsOfCta * kCtas, kTileN, kAK, kBK);
+        int stage = 0, buffer = 0;
+        uint32_t phase = 0, free_phase = 1;
+        bool ok = true;
+        for (int64_t i = unit; ok && i < work.items; i += units) {
+            const Item it = work.item(p, i);
+            if (!(ok = await(free + 8 * buffer, free_phase, polls, s, p.control))) break;
+            fence_after();
+            const uint32_t d = tmem + buffer * kTileN;
+            for (int k = 0; k < it.steps; ++k) {
+                if (!(ok = await(full + 8 * stage, phase, polls, s, p.control))) break;
+                fence_after();
+                const uint32_t a = tiles + stage * S::kStage, b = a + S::kA;
+                const uint64_t da = descriptor(a, kAK), db = descriptor(b, kBK);
+#pragma unroll
+                for (int j = 0; j < kTileK / 16; ++j)
+                    mma<kCtas>(d, da + (j * kStepBytes<kAK> >> 4), db + (j * kStepBytes<kBK> >> 4), kInstruction, (k | j) != 0);
+                commit<kCtas>(empty + 8 * stage);
+                if (++stage == S::kStages) stage = 0, phase ^= 1;
+            }
+            if (!ok) break;
+            commit<kCtas>(done + 8 * buffer);
+            buffer ^= 1;
+            if (buffer == 0) free_phase ^= 1;
+        }
+        if (!ok) {
+            commit<kCtas>(smem_addr(&s.last));
+            mbar_wait(smem_addr(&s.last), 0, kPolls);
+        }
+    } else if (warp >= 2) {
+        const uint32_t lanes = (uint32_t)(warp & 3) * 32;    // of tensor memory that this warp reaches
+        const float scale = p.grad_scale * p.control->unit;
+        int buffer = 0;
+        uint32_t phase = 0;
+        for (int64_t i = unit; i < work.items; i += units) {
+            const Item it = work.item(p, i);
+            const bool ok = await(done + 8 * buffer, phase, polls, s, p.control);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            fence_after();
+            const uint32_t at = tmem + buffer * kTileN + (lanes << 16);
+            const int64_t row = ((int64_t)it.m * kCtas + rank) * kRowsOfCta + lanes + lane;
+            if (kMode == kStats) end_stats(p, at, row, live, it.n);
+            else if (kMode == kProb) end_prob<T>(p, at, row, live, it.n);
+            else if (kMode == kHidden) end_hidden(p, at, row, live, it.n, it.split, it.steps == 0);
+            else end_table(p, at, row, it.n, scale);
+            fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (kCtas == 2) arrive_at(of_rank(free + 8 * buffer, 0));
+                else mbar_arrive(free + 8 * buffer);
+            }
+            buffer ^= 1;
+            if (buffer == 0) phase ^= 1;
+        }
+    }
+    __syncthreads();
+    if (kCtas == 2) cluster_sync();
+    __syncwarp();
+    if (warp == 1) tmem_free<kCtas>(tmem, 512);
+}
+
+// ---- around the products ----------------------------------------------------------------
+
+struct Rows {
+    Control *control;
+    const void *hidden;
+    int64_t hidden_stride;
+    const void *labels;
+    int32_t ids_dtype;
+    const float *weight;
+    int64_t rows, vocab, cols;
+    int32_t rows_pad;
+    void *gathered;                       // [rows_pad][gathered_stride]
+    int64_t gathered_stride;
+    int32_t *index, *label;               // [rows_pad]: where a gathered row is from
+    float *w;                             // [rows_pad]
+    float *row_loss;
+    void *dhidden;
+    int64_t dhidden_stride;
+    int32_t fp16, gradient, vectors, dhidden_vectors;
+};
+
+__device__ __forceinline__ bool is_live(const Rows &r, int64_t i)
+{
+    if (r.weight && r.weight[i] == 0.0f) return false;
+    const int64_t label = load_id(r.labels, i, r.ids_dtype);
+    return label >= 0 && label < r.vocab;
+}
+
+constexpr int kGatherThreads = 256, kGatherRows = 32;
+
+// 16-bit elements [0, n) of a row of `n_pad` (a multiple of 8), zeros behind; `src` NULL: zeros.
+__device__ __forceinline__ void copy_row(uint16_t *dst, const uint16_t *src, int64_t n, int64_t n_pad, bool vectors, int lane)
+{
+    for (int64_t c = lane * 8; c < n_pad; c += 256) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (src && vectors && c + 8 <= n) {
+            v = *reinterpret_cast<const uint4 *>(src + c);
+        } else if (src) {
+            uint16_t e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = c + i < n ? src[c + i] : (uint16_t)0;
+            v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+        }
+        *reinterpret_cast<uint4 *>(dst + c) = v;
+    }
+}
+
+// Gathers the rows that take part, 32 of the caller's rows a block; a block counts those before
+// its own for itself.  The last block knows them all.
+__global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_constant__ Rows r)
+{
+    __shared__ int s_count[kGatherThreads / 32];
+    __shared__ float s_top[kGatherThreads / 32];
+    __shared__ int s_base, s_mask;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t row0 = (int64_t)blockIdx.x * kGatherRows;
+    const bool last = blockIdx.x == gridDim.x - 1;
+    int count = 0;
+    float top = 0.0f;
+    for (int64_t i = threadIdx.x; i < row0; i += kGatherThreads) {
+        const bool in = is_live(r, i);
+        count += in;
+        if (last && in) top = fmaxf(top, r.weight ? fabsf(r.weight[i]) : 1.0f);
+    }
+    count = __reduce_add_sync(0xFFFFFFFFu, count);
+    if (lane == 0) s_count[warp] = count;
+    if (warp == 0) {
+        const int64_t i = row0 + lane;
+        const bool in = i < r.rows && is_live(r, i);
+        if (in) top = fmaxf(top, r.weight ? fabsf(r.weight[i]) : 1.0f);
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, in);
+        if (lane == 0) s_mask = (int)mask;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if (lane == 0) s_top[warp] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int base = 0;
+        for (int i = 0; i < kGatherThreads / 32; ++i) base += s_count[i];
+        s_base = base;
+    }
+    __syncthreads();
+    const uint32_t mask = (uint32_t)s_mask;
+    const int base = s_base;
+    for (int k = warp; k < kGatherRows; k += kGatherThreads / 32) {
+        const int64_t i = row0 + k;
+        if (i >= r.rows) break;
+        if (mask >> k & 1u) {
+            const int at = base + __popc(mask & ((1u << k) - 1u));
+            copy_row(static_cast<uint16_t *>(r.gathered) + at * r.gathered_stride, static_cast<const uint16_t *>(r.hidden) + i * r.hidden_stride,
+                     r.cols, r.gathered_stride, r.vectors, lane);
+            if (lane == 0) {
+                r.index[at] = (int32_t)i;
+                r.label[at] = (int32_t)load_id(r.labels, i, r.ids_dtype);
+                r.w[at] = r.weight ? r.weight[i] : 1.0f;
+            }
+        } else {
+            if (lane == 0) r.row_loss[i] = 0.0f;
+            if (r.gradient && r.dhidden) {
+                uint16_t *out = static_cast<uint16_t *>(r.dhidden) + i * r.dhidden_stride;
+                if (r.dhidden_vectors) copy_row(out, nullptr, r.cols, r.cols, true, lane);
+                else
+                    for (int64_t c = lane; c < r.cols; c += 32) out[c] = 0;
+            }
+        }
+    }
+    if (!last) return;
+    const int live = base + __popc(mask);
+    // rows up to the end of a tile count in sums over rows, with factors of zero
+    for (int at = live + warp; at < (live + kRowPad - 1) / kRowPad * kRowPad; at += kGatherThreads / 32)
+        copy_row(static_cast<uint16_t *>(r.gathered) + at * r.gathered_stride, nullptr, r.cols, r.gathered_stride, true, lane);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kGatherThreads / 32; ++i) top = fmaxf(top, s_top[i]);
+        int e = 0;
+        if (top > 0.0f && top < kInf) frexpf(top, &e);       // top < 2^e
+        if (r.fp16) e -= 15;
+        e = e < -126 ? -126 : e > 126 ? 126 : e;
+        r.control->live = live;
+        r.control->unit = ldexpf(1.0f, e);
+        r.control->ticket = 0;
+        r.control->gave_up = 0;
+    }
+}
+
+struct Join {
+    Control *control;
+    const float2 *stats;
+    const float *label_logit, *w;
+    const int32_t *index;
+    float *lse2, *coef, *row_loss, *loss;
+    double *sums;                         // [blocks]
+    int32_t rows_pad, tiles;
+};
+
+constexpr int kJoinWarps = 8;
+
+// Joins the tiles' statistics, 32 rows a block (a lane each, the tiles dealt out to warps); the
+// block that comes last adds up the loss.
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_constant__ Join j)
+{
+    __shared__ float2 s_part[kJoinWarps][32];
+    __shared__ double s_sum[kJoinWarps];
+    __shared__ bool s_last;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    grid_dependency_wait();
+    const int live = j.control->live;
+    const int row = blockIdx.x * 32 + lane;
+    float top = -kInf, sum = 0.0f;
+    if (blockIdx.x * 32 < live) {
+        // rows behind the last one are read as they lie in scratch, and dropped
+        const float2 *at = j.stats + row;
+        for (int t0 = warp; t0 < j.tiles; t0 += 8 * kJoinWarps) {
+            float2 v[8];
+            float most = top;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int t = t0 + u * kJoinWarps;
+                v[u] = t < j.tiles && row < live ? at[(int64_t)t * j.rows_pad] : make_float2(-kInf, 0.0f);
+                most = fmaxf(most, v[u].x);
+            }
+            const float ref = most == -kInf ? 0.0f : most;
+            sum *= exp2_fast((top - ref) * kLog2e);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) sum += v[u].y == 0.0f ? 0.0f : v[u].y * exp2_fast((v[u].x - ref) * kLog2e);
+            top = most;
+        }
+    }
+    s_part[warp][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (warp == 0) {
+        double mine = 0.0;
+        if (row < live) {
+            float most = -kInf;
+            for (int i = 0; i < kJoinWarps; ++i) most = fmaxf(most, s_part[i][lane].x);
+            float total = 0.0f;
+            for (int i = 0; i < kJoinWarps; ++i)
+                total += s_part[i][lane].y == 0.0f ? 0.0f : s_part[i][lane].y * exp2_fast((s_part[i][lane].x - most) * kLog2e);
+            const float w = j.w[row], loss = (most - j.label_logit[row]) + logf(total);
+            j.row_loss[j.index[row]] = loss;
+            j.lse2[row] = fmaf(most, kLog2e, log2f(total));
+            j.coef[row] = w / j.control->unit;
+            mine = (double)w * (double)loss;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+        if (lane == 0) {
+            j.sums[blockIdx.x] = mine;
+            __threadfence();
+            s_last = atomicAdd(&j.control->ticket, 1u) == gridDim.x - 1;
+        }
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    double all = 0.0;
+    for (unsigned i = threadIdx.x; i < gridDim.x; i += 32 * kJoinWarps) all += __ldcg(j.sums + i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
+    if (lane == 0) s_sum[warp] = all;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        all = 0.0;
+        for (int i = 0; i < kJoinWarps; ++i) all += s_sum[i];
+        *j.loss = (float)all;
+    }
+}
+
+struct Finish {
+    Control *control;
+    const float *part;
+    const int32_t *index;
+    void *dhidden, *table_grad;
+    float *row_loss, *loss;
+    int64_t rows, vocab, cols, dhidden_stride, grad_stride, part_stride;
+    int32_t rows_pad, splits, grad_dtype, vectors;
+    float grad_scale;
+};
+
+constexpr int kFinishThreads = 256;
+
+// dH from its parts, a row a turn; NaN everywhere after a wait that ran out.
+template <typename T>
+__global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ Finish f)
+{
+    grid_dependency_wait();
+    const int live = f.control->live;
+    if (f.control->gave_up) {
+        const int64_t me = (int64_t)blockIdx.x * kFinishThreads + threadIdx.x, all = (int64_t)gridDim.x * kFinishThreads;
+        for (int64_t i = me; i < f.rows; i += all) f.row_loss[i] = kNan;
+        if (me == 0) *f.loss = kNan;
+        if (f.dhidden)
+            for (int64_t i = me; i < f.rows * f.cols; i += all) static_cast<T *>(f.dhidden)[i / f.cols * f.dhidden_stride + i % f.cols] = from_f32<T>(kNan);
+        if (f.table_grad)
+            for (int64_t i = me; i < f.vocab * f.cols; i += all) store_any(f.table_grad, i / f.cols * f.grad_stride + i % f.cols, f.grad_dtype, kNan);
+        return;
+    }
+    if (!f.dhidden) return;
+    const float scale = f.grad_scale * f.control->unit;
+    for (int row = blockIdx.x; row < live; row += gridDim.x) {
+        const float *in = f.part + (int64_t)row * f.part_stride;
+        T *out = static_cast<T *>(f.dhidden) + (int64_t)f.index[row] * f.dhidden_stride;
+        for (int64_t c = threadIdx.x * 8; c < f.cols; c += kFinishThreads * 8) {
+            float sum[8] = {};
+            for (int k = 0; k < f.splits; ++k) {
+                uint32_t w[8];
+                load32(in + (int64_t)k * f.rows_pad * f.part_stride + c, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += __uint_as_float(w[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] *= scale;
+            if (f.vectors && c + 8 <= f.cols) {
+                *reinterpret_cast<uint4 *>(out + c) = pack<T>(sum);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c + i < f.cols) out[c + i] = from_f32<T>(sum[i]);
+            }
+        }
+    }
+}
+
+// dW without any row that takes part: zeros, unless it is added to.
+__global__ void __launch_bounds__(256) no_rows_kernel(const Control *control, void *grad, int64_t stride, int64_t vocab, int64_t cols, int32_t dtype)
+{
+    grid_dependency_wait();
+    if (control->live != 0) return;
+    for (int64_t v = blockIdx.x; v < vocab; v += gridDim.x)
+        for (int64_t c = threadIdx.x; c < cols; c += 256) store_any(grad, v * stride + c, dtype, 0.0f);
+}
+
+// A piece of a table whose rows cannot be copied as they are, rows padded to whole steps.
+__global__ void __launch_bounds__(256) pack_kernel(const uint16_t *table, int64_t stride, int64_t rows, int64_t cols, uint16_t *out, int64_t out_stride)
+{
+    grid_dependency_wait();
+    for (int64_t v = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); v < rows; v += (int64_t)gridDim.x * 8)
+        copy_row(out + v * out_stride, table + v * stride, cols, out_stride, false, threadIdx.x & 31);
+}
+
+// ---- host ---------------------------------------------------------------------------------
+
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Where everything lies in scratch.
+struct Layout {
+    int64_t rows_pad, ld, pieces, piece, splits, planes, part_stride, tiles;
+    bool packed;
+    uint64_t control, index, label, w, label_logit, lse2, coef, sums, stats, gathered, prob, part, table, bytes;
+};
+
+constexpr int64_t kPieceBytes = int64_t(128) << 20;   // of P, unless rows are so many that pieces would get short
+constexpr int64_t kShortPiece = 4096;
+
+constexpr int kSms = 148;                 // of a B200: sums are split alike on every device
+
+Layout layout(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t grad_dtype, bool gradients, bool packed)
+{
+    const int units = rows > kRowsOfCta ? kSms / 2 : kSms;   // blocks, or pairs of them, that work at a time
+    Layout l = {};
+    l.packed = packed;
+    l.rows_pad = up(rows > 0 ? rows : 1, kRowPad);
+    l.ld = up(cols, kTileK);
+    l.tiles = (vocab + kTileN - 1) / kTileN;
+    l.planes = grad_dtype != SO_DTYPE_FP32 ? 1 : dtype == SO_DTYPE_BF16 ? 3 : 2;
+    l.piece = up(vocab, kTileN);
+    if (gradients || packed) {
+        int64_t c = kPieceBytes / (2 * l.planes * l.rows_pad) / kTileN * kTileN;
+        if (c < kShortPiece) c = kShortPiece;
+        if (c < l.piece) l.piece = c;
+    }
+    l.pieces = (vocab + l.piece - 1) / l.piece;
+    l.part_stride = up(cols, kTileN);
+    // parts of the sums over the vocabulary: as many as fill the units best, each split costing
+    // its write and reading
+    const int64_t tile_m = rows > kRowsOfCta ? 2 * kRowsOfCta : kRowsOfCta;
+    const int64_t tiles = (l.rows_pad < tile_m ? 1 : up(rows > 0 ? rows : 1, tile_m) / tile_m) * (l.part_stride / kTileN);
+    l.splits = 1;
+    double best = 1e30;
+    for (int64_t s = 1; s <= 64 && s * 4 <= l.piece / kTileK; ++s) {
+        const double cost = (double)((tiles * s + units - 1) / units) / (double)s * (1.0 + 0.01 * (double)(s - 1));
+        if (cost < best * 0.999) best = cost, l.splits = s;
+    }
+    uint64_t at = 0;
+    const auto take = [&](uint64_t bytes) {
+        const uint64_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    const uint64_t rp = (uint64_t)l.rows_pad;
+    l.control = take(sizeof(Control));
+    l.index = take(rp * 4);
+    l.label = take(rp * 4);
+    l.w = take(rp * 4);
+    l.label_logit = take(rp * 4);
+    l.lse2 = take(rp * 4);
+    l.coef = take(rp * 4);
+    l.sums = take(rp / 32 * 8);
+    l.stats = take(rp * (uint64_t)l.tiles * 8);
+    l.gathered = take(rp * (uint64_t)l.ld * 2);
+    if (gradients) {
+        l.prob = take(rp * (uint64_t)(l.planes * l.piece) * 2);
+        l.part = take(rp * (uint64_t)(l.splits * l.part_stride) * 4);
+    }
+    if (packed) l.table = take((uint64_t)(l.piece * l.ld) * 2);
+    l.bytes = at;
+    return l;
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                              const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encoder()
+{
+    static std::atomic<void *> found{nullptr};
+    void *fn = found.load(std::memory_order_acquire);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult how;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &how) != cudaSuccess || how != cudaDriverEntryPointSuccess) return nullptr;
+        found.store(fn, std::memory_order_release);
+    }
+    return reinterpret_cast<EncodeFn>(fn);
+}
+
+// A matrix of 16-bit elements, copied 64 columns and `box_rows` rows at a time.
+bool make_map(CUtensorMap *m, const void *base, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, int box_rows)
+{
+    const EncodeFn fn = encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    return fn(m, dtype == SO_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(base), dims, strides,
+              box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int kMode, int kCtas>
+so_status launch_product(const CUtensorMap &a, const CUtensorMap &b, const Product &p, int units, cudaStream_t st)
+{
+    static std::atomic<bool> ready[kMaxDevices];
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return SO_ERR_CUDA;
+    const auto kernel = product_kernel<T, kMode, kCtas>;
+    if (!ready[dev].load(std::memory_order_relaxed)) {
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<kCtas>::kBytes) != cudaSuccess) return SO_ERR_CUDA;
+        ready[dev].store(true, std::memory_order_relaxed);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(units * kCtas));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Shape<kCtas>::kBytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kCtas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a, b, p) == cudaSuccess ? SO_OK : SO_ERR_CUDA;
+}
+
+struct Call {
+    const void *hidden, *table, *labels;
+    const float *weight;
+    int64_t hidden_stride, table_stride, rows, vocab, cols, dhidden_stride, dtable_stride;
+    int32_t ids_dtype, dtype, grad_dtype, accumulate;
+    float grad_scale;
+    void *dhidden, *dtable;
+    float *row_loss, *loss;
+};
+
+#define SO_TRY(x) do { const so_status so_try_ = (x); if (so_try_ != SO_OK) return so_try_; } while (0)
+
+template <typename T, int kCtas>
+so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream_t st)
+{
+    const bool gradients = c.dhidden || c.dtable;
+    const int units = sms / kCtas;
+    Control *control = reinterpret_cast<Control *>(scratch + l.control);
+    int32_t *index = reinterpret_cast<int32_t *>(scratch + l.index), *label = reinterpret_cast<int32_t *>(scratch + l.label);
+    float *w = reinterpret_cast<float *>(scratch + l.w);
+    Rows r = {};
+    r.control = control, r.hidden = c.hidden, r.hidden_stride = c.hidden_stride, r.labels = c.labels, r.ids_dtype = c.ids_dtype, r.weight = c.weight;
+    r.rows = c.rows, r.vocab = c.vocab, r.cols = c.cols, r.rows_pad = (int32_t)l.rows_pad;
+    r.gathered = scratch + l.gathered, r.gathered_stride = l.ld, r.index = index, r.label = label, r.w = w, r.row_loss = c.row_loss;
+    r.dhidden = c.dhidden, r.dhidden_stride = c.dhidden_stride, r.fp16 = c.dtype == SO_DTYPE_FP16, r.gradient = gradients;
+    r.vectors = aligned(c.hidden, 16) && (c.rows <= 1 || c.hidden_stride % 8 == 0);
+    r.dhidden_vectors = aligned(c.dhidden, 16) && c.cols % 8 == 0 && (c.rows <= 1 || c.dhidden_stride % 8 == 0);
+    SO_TRY(launch(gather_kernel, (unsigned)(c.rows > 0 ? (c.rows + kGatherRows - 1) / kGatherRows : 1), kGatherThreads, 0, st, false, r));
+
+    Product p = {};
+    p.control = control, p.vocab = c.vocab, p.cols = c.cols, p.rows_pad = (int32_t)l.rows_pad, p.splits = (int32_t)l.splits, p.planes = (int32_t)l.planes;
+    p.label = label;
+    p.label_logit = reinterpret_cast<float *>(scratch + l.label_logit);
+    float *lse2 = reinterpret_cast<float *>(scratch + l.lse2), *coef = reinterpret_cast<float *>(scratch + l.coef);
+    p.lse2 = lse2, p.coef = coef;
+    p.stats = reinterpret_cast<float2 *>(scratch + l.stats);
+    p.prob = scratch + l.prob, p.prob_stride = l.piece;
+    p.part = reinterpret_cast<float *>(scratch + l.part), p.part_stride = l.part_stride;
+    p.table_grad = c.dtable, p.grad_stride = c.dtable_stride, p.grad_dtype = c.grad_dtype, p.accumulate = c.accumulate, p.grad_scale = c.grad_scale;
+    p.grad_vectors = aligned(c.dtable, 32) && (c.dtable_stride * elem_size(c.grad_dtype)) % 32 == 0;
+    p.patience = patience();
+
+    // the table as it is, or a packed piece of it
+    const uint16_t *table = static_cast<const uint16_t *>(c.table);
+    uint16_t *packed = reinterpret_cast<uint16_t *>(scratch + l.table);
+    CUtensorMap hidden_k, hidden_m, table_k, table_m, prob_k, prob_m;
+    if (!make_map(&hidden_k, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld, kRowsOfCta) || !make_map(&hidden_m, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld, kTileK))
+        return SO_ERR_CUDA;
+    const auto table_maps = [&](int64_t rows) {
+        const void *at = l.packed ? static_cast<const void *>(packed) : c.table;
+        const int64_t stride = l.packed ? l.ld : c.vocab == 1 ? l.ld : c.table_stride;
+        return make_map(&table_k, at, c.dtype, rows, c.cols, stride, 128) && make_map(&table_m, at, c.dtype, rows, c.cols, stride, kTileK);
+    };
+    const auto pack_piece = [&](int64_t first, int64_t width) {
+        return launch(pack_kernel, (unsigned)(4 * sms), 256, 0, st, false, table + first * c.table_stride, c.table_stride, width, c.cols, packed, l.ld);
+    };
+
+    if (l.packed) {
+        for (int64_t first = 0; first < c.vocab; first += l.piece) {
+            const int64_t width = c.vocab - first < l.piece ? c.vocab - first : l.piece;
+            SO_TRY(pack_piece(first, width));
+            if (!table_maps(width)) return SO_ERR_CUDA;
+            Product q = p;
+            q.first = first, q.width = width, q.table_row = 0;
+            SO_TRY((launch_product<T, kStats, kCtas>(hidden_k, table_k, q, units, st)));
+        }
+    } else {
+        if (!table_maps(c.vocab)) return SO_ERR_CUDA;
+        p.width = c.vocab;
+        SO_TRY((launch_product<T, kStats, kCtas>(hidden_k, table_k, p, units, st)));
+    }
+    Join j = {control, p.stats, p.label_logit, w, index, lse2, coef, c.row_loss, c.loss, reinterpret_cast<double *>(scratch + l.sums), (int32_t)l.rows_pad, (int32_t)l.tiles};
+    SO_TRY(launch(join_kernel, (unsigned)(l.rows_pad / 32), 32 * kJoinWarps, 0, st, true, j));
+    if (gradients) {
+        if (!make_map(&prob_k, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, kRowsOfCta) ||
+            !make_map(&prob_m, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, kTileK))
+            return SO_ERR_CUDA;
+        for (int64_t first = 0; first < c.vocab; first += l.piece) {
+            Product q = p;
+            q.first = q.table_row = first;
+            q.width = c.vocab - first < l.piece ? c.vocab - first : l.piece;
+            q.begin = first == 0;
+            if (l.packed) {
+                SO_TRY(pack_piece(first, q.width));
+                if (!table_maps(q.width)) return SO_ERR_CUDA;
+                q.table_row = 0;
+            }
+            SO_TRY((launch_product<T, kProb, kCtas>(hidden_k, table_k, q, units, st)));
+            if (c.dhidden) SO_TRY((launch_product<T, kHidden, kCtas>(prob_k, table_m, q, units, st)));
+            if (c.dtable) SO_TRY((launch_product<T, kTable, kCtas>(prob_m, hidden_m, q, units, st)));
+        }
+        if (c.dtable && !c.accumulate)
+            SO_TRY(launch(no_rows_kernel, (unsigned)(4 * sms), 256, 0, st, true, control, c.dtable, c.dtable_stride, c.vocab, c.cols, c.grad_dtype));
+    }
+    Finish f = {control, p.part, index, c.dhidden, c.dtable, c.row_loss, c.loss, c.rows, c.vocab, c.cols, c.dhidden_stride, c.dtable_stride, l.part_stride,
+                (int32_t)l.rows_pad, (int32_t)l.splits, c.grad_dtype, r.dhidden_vectors, c.grad_scale};
+    return launch(finish_kernel<T>, (unsigned)(4 * sms), kFinishThreads, 0, st, true, f);
+}
+
+so_status check_sizes(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t grad_dtype)
+{
+    if ((dtype != SO_DTYPE_BF16 && dtype != SO_DTYPE_FP16) || !valid_dtype(grad_dtype)) return SO_ERR_INVALID_ARG;
+    if (rows < 0 || rows > SO_LINEAR_MAX_ROWS || vocab < 1 || vocab > SO_LINEAR_MAX_VOCAB || cols < 1 || cols > SO_LINEAR_MAX_COLS) return SO_ERR_INVALID_ARG;
+    return SO_OK;
+}
+
+bool needs_packing(const void *table, int64_t stride, int64_t vocab) { return !aligned(table, 16) || (vocab > 1 && stride % 8 != 0); }
+
+}  // namespace
+
+extern "C" {
+
+so_status so_linear_cross_entropy_scratch(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t grad_dtype, int32_t gradients,
+                                          int32_t packed, uint64_t *bytes)
+{
+    if (!bytes || (gradients != 0 && gradients != 1) || (packed != 0 && packed != 1)) return SO_ERR_INVALID_ARG;
+    SO_TRY(check_sizes(rows, vocab, cols, dtype, grad_dtype));
+    *bytes = layout(rows, vocab, cols, dtype, grad_dtype, gradients != 0, packed != 0).bytes;
+    return SO_OK;
+}
+
+so_status so_linear_cross_entropy(const void *hidden, int64_t hidden_stride, const void *table, int64_t table_stride, const void *labels,
+                                  int32_t ids_dtype, const float *weight, int64_t rows, int64_t vocab, int64_t cols, int32_t dtype,
+                                  double grad_scale, void *dhidden, int64_t dhidden_stride, void *dtable, int64_t dtable_stride,
+                                  int32_t grad_dtype, int32_t accumulate, float *row_loss, float *loss, void *scratch,
+                                  uint64_t scratch_bytes, void *stream)
+{
+    SO_TRY(check_sizes(rows, vocab, cols, dtype, grad_dtype));
+    if (!valid_ids(ids_dtype) || (accumulate != 0 && accumulate != 1) || !std::isfinite(grad_scale) || !std::isfinite((float)grad_scale)) return SO_ERR_INVALID_ARG;
+    if (!loss || !aligned(loss, 4) || (rows > 0 && !row_loss) || !aligned(row_loss, 4) || !aligned(weight, 4)) return SO_ERR_INVALID_ARG;
+    if (!table || !aligned(table, 2) || !valid_extent(vocab, table_stride) || !valid_out_stride(vocab, table_stride, cols)) return SO_ERR_INVALID_ARG;
+    if (dtable && (!aligned(dtable, elem_size(grad_dtype)) || !valid_extent(vocab, dtable_stride) || !valid_out_stride(vocab, dtable_stride, cols))) return SO_ERR_INVALID_ARG;
+    if (rows > 0) {
+        if (!hidden || !aligned(hidden, 2) || !valid_extent(rows, hidden_stride) || !valid_in_stride(rows, hidden_stride, cols)) return SO_ERR_INVALID_ARG;
+        if (!labels || !aligned(labels, ids_dtype == SO_IDS_INT64 ? 8 : 4)) return SO_ERR_INVALID_ARG;
+        if (dhidden && (!aligned(dhidden, 2) || !valid_extent(rows, dhidden_stride) || !valid_out_stride(rows, dhidden_stride, cols))) return SO_ERR_INVALID_ARG;
+        if (dhidden && dhidden == hidden && dhidden_stride != hidden_stride) return SO_ERR_INVALID_ARG;
+    }
+    if (dtable && (dtable == table || dtable == hidden || dtable == dhidden)) return SO_ERR_INVALID_ARG;
+    if (dhidden && dhidden == table) return SO_ERR_INVALID_ARG;
+    if (!scratch || !aligned(scratch, 256)) return SO_ERR_INVALID_ARG;
+    const Layout l = layout(rows, vocab, cols, dtype, grad_dtype, dhidden || dtable, needs_packing(table, table_stride, vocab));
+    if (scratch_bytes < l.bytes) return SO_ERR_INVALID_ARG;
+    int sms;
+    SO_TRY(device_sms(&sms));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const Call c = {hidden, table, labels, weight, hidden_stride, table_stride, rows, vocab, cols, dhidden_stride, dtable_stride, ids_dtype, dtype, grad_dtype,
+                    accumulate, (float)grad_scale, rows > 0 ? dhidden : nullptr, dtable, row_loss, loss};
+    if (dtype == SO_DTYPE_BF16) return rows > kRowsOfCta ? run<bf16_t, 2>(c, l, static_cast<char *>(scratch), sms, st) : run<bf16_t, 1>(c, l, static_cast<char *>(scratch), sms, st);
+    return rows > kRowsOfCta ? run<f16_t, 2>(c, l, static_cast<char *>(scratch), sms, st) : run<f16_t, 1>(c, l, static_cast<char *>(scratch), sms, st);
+}
+
+}  // extern "C"

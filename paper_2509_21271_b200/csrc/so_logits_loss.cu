@@ -44,13 +44,6 @@ struct Targets {
     int32_t live;                         // 0: no entry, the row counts as masked
 };
 
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // Running maximum m and sum s of exp((z - m) / T) over the elements seen.  A sum
 // stays 0 while everything was -inf; NaN reaches the sum, not the maximum.
 struct MaxSum { float m, s; };

@@ -128,6 +128,13 @@ template <> __device__ __forceinline__ uint4 pack<f16_t>(const float (&f)[8])
                       pack2_f16(f[6], f[7]));
 }
 
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // ---- two fp32 operations in one instruction --------------------------------------
 
 using f32x2 = unsigned long long;         // two floats in a register pair, the first in the low half

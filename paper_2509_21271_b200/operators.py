@@ -122,6 +122,7 @@ def _scratch(where, scratch, dev):
 _norm_scratch = lru_cache(maxsize=512)(B.so_layer_norm_backward_scratch)      # sizes alone decide
 _embedding_scratch = lru_cache(maxsize=512)(B.so_embedding_backward_scratch)
 _residual_scratch = lru_cache(maxsize=512)(B.so_residual_norm_backward_scratch)
+_linear_scratch = lru_cache(maxsize=512)(B.so_linear_cross_entropy_scratch)
 _KINDS = {"layer": B.SO_NORM_LAYER, "rms": B.SO_NORM_RMS}
 
 
@@ -533,3 +534,78 @@ def policy_loss(logits, tokens, advantage, weight=None, *, old_logp=None, ref_lo
                      _vector(where, "loss", loss, 1, dev, f32), _raw_stream(dev)), where,
           (loss, row_loss, logp) if grad is None else (loss, row_loss, logp, grad))
     return loss, row_loss, logp, grad
+
+
+# ---- the loss from the hidden states -------------------------------------------------
+
+def linear_cross_entropy(hidden, table, labels, weight=None, *, grad_scale: float = 1.0, dhidden=None, dtable=None,
+                         accumulate: bool = False, loss=None, row_loss=None, scratch=None, stream=None):
+    """Cross entropy of `labels` under the logits hidden @ table.T, which are never kept;
+    returns (loss, row_loss, dhidden, dtable).
+
+    `hidden` [rows, cols] and `table` [vocab, cols] are bfloat16 or float16, `labels`
+    [rows], `weight` fp32 [rows] (None: 1 each; 0 masks a row, as does a label outside
+    the vocabulary).  The gradients, multiplied by `grad_scale`, are allocated where
+    None, left out where False, and written where a tensor is given: `dhidden` may be
+    `hidden` itself, `dtable` has a dtype of its own and with `accumulate` is added to.
+    `scratch`: so_linear_cross_entropy_scratch bytes on a 256-byte boundary."""
+    if stream is not None:
+        return _on_stream(stream, linear_cross_entropy, hidden, table, labels, weight, grad_scale=grad_scale,
+                          dhidden=dhidden, dtable=dtable, accumulate=accumulate, loss=loss, row_loss=row_loss,
+                          scratch=scratch)
+    where = "linear_cross_entropy"
+    if hidden.requires_grad or table.requires_grad or weight is not None and weight.requires_grad:
+        _recorded(where)
+    dev = _device(where, "hidden", hidden)
+    dt = _dtype(where, "hidden", hidden)
+    if dt == B.SO_DTYPE_FP32:
+        _refuse(where, "hidden has dtype torch.float32: bfloat16 and float16 are supported")
+    if table.dtype != hidden.dtype:
+        _refuse(where, "table must have the dtype of hidden")
+    if table.dim() != 2:
+        _refuse(where, "table must be a matrix")
+    rows, cols, stride = _rows(where, "hidden", hidden, dev)
+    vocab, table_cols, table_stride = _rows(where, "table", table, dev)
+    if table_cols != cols:
+        _refuse(where, "table must have rows as long as hidden's")
+    it = _ids_dtype(where, "labels", labels)
+    lp = _vector(where, "labels", labels, rows, dev)
+    if dhidden is None:
+        dhidden = torch.empty(hidden.shape, dtype=hidden.dtype, device=hidden.device)
+    elif dhidden is False:
+        dhidden = None
+    else:
+        _same(where, "dhidden", dhidden, "hidden", hidden)
+    if dtable is None:
+        if accumulate:
+            _refuse(where, "accumulate needs dtable (or False)")
+        dtable = torch.empty(table.shape, dtype=table.dtype, device=table.device)
+    elif dtable is False:
+        dtable = None
+    elif dtable.shape != table.shape:
+        _refuse(where, "dtable must have the shape of table")
+    dhidden_stride = dtable_stride = 0
+    gt = dt
+    if dhidden is not None:
+        _, _, dhidden_stride = _rows(where, "dhidden", dhidden, dev)
+    if dtable is not None:
+        _, _, dtable_stride = _rows(where, "dtable", dtable, dev)
+        gt = _dtype(where, "dtable", dtable)
+    if loss is None:
+        loss = torch.empty(1, dtype=torch.float32, device=hidden.device)
+    if row_loss is None:
+        row_loss = torch.empty(rows, dtype=torch.float32, device=hidden.device)
+    tp = table.data_ptr()
+    if scratch is None:
+        packed = tp % 16 != 0 or vocab > 1 and table_stride % 8 != 0
+        scratch = torch.empty(_linear_scratch(rows, vocab, cols, dt, gt, int(dhidden is not None or dtable is not None),
+                                              int(packed)), dtype=torch.uint8, device=hidden.device)
+    f32 = torch.float32
+    _done(B.lib().so_linear_cross_entropy(
+        hidden.data_ptr(), stride, tp, table_stride, lp, it, _vector(where, "weight", weight, rows, dev, f32), rows, vocab,
+        cols, dt, grad_scale, None if dhidden is None else dhidden.data_ptr(), dhidden_stride,
+        None if dtable is None else dtable.data_ptr(), dtable_stride, gt, int(accumulate),
+        _vector(where, "row_loss", row_loss, rows, dev, f32), _vector(where, "loss", loss, 1, dev, f32), scratch.data_ptr(),
+        _scratch(where, scratch, dev), _raw_stream(dev)), where,
+        [t for t in (loss, row_loss, dhidden, dtable) if t is not None])
+    return loss, row_loss, dhidden, dtable
