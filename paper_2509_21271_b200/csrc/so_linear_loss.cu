@@ -76,6 +76,17 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, i
         asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+// The same from a matrix seen as groups of 64 columns: 64 rows of two groups.
+template <int kCtas>
+__device__ __forceinline__ void tma_load_groups(uint32_t dst, const CUtensorMap *map, int y, int group, uint32_t bar)
+{
+    if constexpr (kCtas == 2)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(group), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(group), "r"(bar) : "memory");
+}
 template <int kCtas>
 __device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t cols)
 {
@@ -165,6 +176,7 @@ struct Product {
     int32_t rows_pad;
     int32_t splits;                       // kHidden: parts that the vocabulary is summed in
     int32_t planes;                       // kProb, kTable: parts of P
+    int32_t table_groups;                 // kHidden: the table's map is of groups of 64 columns
     int32_t begin;                        // kHidden: the sums begin here rather than going on
     const int32_t *label;                 // [rows_pad], of the gathered rows
     float *label_logit;                   // [rows_pad]
@@ -239,7 +251,7 @@ struct Work {
 template <int kCtas>
 struct Shape {
     static constexpr uint32_t kA = kRowsOfCta * 128, kB = kTileN / kCtas * 128, kStage = kA + kB;
-    static constexpr int kStages = kCtas == 2 ? 6 : 4;
+    static constexpr int kStages = kCtas == 2 ? 7 : 4;       // 224 and 192 KB
     static constexpr size_t kBytes = (size_t)kStage * kStages + 1024;
 };
 
@@ -251,7 +263,7 @@ struct Shared {
 
 // A wait that ends when the barrier's phase does, when it runs out, or when another of the block
 // has run out; false unless the first.
-__device__ __forceinline__ bool await(uint32_t bar, uint32_t parity, uint32_t polls, Shared &s, Control *c)
+__device__ __noinline__ bool await_long(uint32_t bar, uint32_t parity, uint32_t polls, Shared &s, Control *c)
 {
     if (s.gave_up) return false;
     for (uint32_t left = polls; left > 0;) {
@@ -263,6 +275,21 @@ __device__ __forceinline__ bool await(uint32_t bar, uint32_t parity, uint32_t po
     s.gave_up = 1;
     atomicExch(&c->gave_up, 1);
     return false;
+}
+// All lanes of a warp, which go on together.
+__device__ __forceinline__ bool await(uint32_t bar, uint32_t parity, uint32_t polls, Shared &s, Control *c)
+{
+    bool ok = mbar_test(bar, parity);
+    if (!__all_sync(0xFFFFFFFFu, ok)) ok = await_long(bar, parity, polls, s, c);
+    return __all_sync(0xFFFFFFFFu, ok);
+}
+
+// One lane of a converged warp, the same one each time.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
 }
 
 // 16 elements of a row as T (or 8 as fp32) in one store
@@ -492,7 +519,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const int live = p.control->live;
     const Work<kMode, kCtas> work(p, live);
 
-    if (warp == 0 && lane == 0) {
+    // The warps that copy and multiply go through their loops with all lanes, so that addresses and
+    // descriptors stay in uniform registers, and one lane issues: with one lane alone in the loop a
+    // step took 800 clocks, of which the tensor cores need 512.
+    if (warp == 0) {
         // copies: this block's rows of A and its share of B
         int stage = 0, issued = 0;
         uint32_t phase = 1;
@@ -500,64 +530,72 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         for (int64_t i = unit; ok && i < work.items; i += units) {
             const Item it = work.item(p, i);
             const int m0 = (it.m * kCtas + (int)rank) * kRowsOfCta, n0 = it.n * kTileN + (int)rank * (kTileN / kCtas);
+            int step = it.k0, row0 = 0;                      // row0: of the part of P
             for (int k = 0; k < it.steps; ++k) {
                 if (!(ok = await(empty + 8 * stage, phase, polls, s, p.control))) break;
                 const uint32_t bar = kCtas == 2 ? of_rank(full + 8 * stage, 0) : full + 8 * stage;
                 const uint32_t a = tiles + stage * S::kStage, b = a + S::kA;
-                if (rank == 0) mbar_expect(full + 8 * stage, S::kStage * kCtas);
-                int step = it.k0 + k, plane = 0;
-                if (kMode == kTable) plane = step / work.k_steps, step -= plane * work.k_steps;
                 const int k0 = step * kTileK;
-                if (kAK) {
-                    tma_load<kCtas>(a, &map_a, k0, m0, bar);
-                } else {
+                if (elected()) {
+                    if (rank == 0) mbar_expect(full + 8 * stage, S::kStage * kCtas);
+                    if (kAK) tma_load<kCtas>(a, &map_a, k0, m0, bar);
+                    else tma_load_groups<kCtas>(a, &map_a, row0 + k0, m0 / 64, bar);
+                    if (kBK) {
 #pragma unroll
-                    for (int g = 0; g < kRowsOfCta / 64; ++g) tma_load<kCtas>(a + g * kMajorStep, &map_a, m0 + 64 * g, plane * p.rows_pad + k0, bar);
+                        for (int g = 0; g < 2 / kCtas; ++g) tma_load<kCtas>(b + g * 128 * 128, &map_b, k0, (int)p.table_row + n0 + 128 * g, bar);
+                    } else if (kMode == kTable || p.table_groups) {
+#pragma unroll
+                        for (int g = 0; g < 2 / kCtas; ++g)
+                            tma_load_groups<kCtas>(b + 2 * g * kMajorStep, &map_b, (kMode == kHidden ? (int)p.table_row : 0) + k0, n0 / 64 + 2 * g, bar);
+                    } else {
+#pragma unroll
+                        for (int g = 0; g < kTileN / kCtas / 64; ++g) tma_load<kCtas>(b + g * kMajorStep, &map_b, n0 + 64 * g, (int)p.table_row + k0, bar);
+                    }
                 }
-                if (kBK) {
-#pragma unroll
-                    for (int g = 0; g < 2 / kCtas; ++g) tma_load<kCtas>(b + g * 128 * 128, &map_b, k0, (int)p.table_row + n0 + 128 * g, bar);
-                } else {
-#pragma unroll
-                    for (int g = 0; g < kTileN / kCtas / 64; ++g)
-                        tma_load<kCtas>(b + g * kMajorStep, &map_b, n0 + 64 * g, (kMode == kHidden ? (int)p.table_row : 0) + k0, bar);
-                }
+                __syncwarp();
                 ++issued;
                 if (++stage == S::kStages) stage = 0, phase ^= 1;
+                if (++step == work.k_steps && kMode == kTable) step = 0, row0 += p.rows_pad;
             }
         }
         // a block that gives up waits for what is still on its way
         if (!ok && rank == 0)
             for (int k = issued > S::kStages ? issued - S::kStages : 0; k < issued; ++k)
                 mbar_wait(full + 8 * (k % S::kStages), (uint32_t)(k / S::kStages) & 1u, kPolls);
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
         constexpr uint32_t kInstruction = instruction<T>(kRowsOfCta * kCtas, kTileN, kAK, kBK);
         int stage = 0, buffer = 0;
         uint32_t phase = 0, free_phase = 1;
-        bool ok = true;
+        bool ok = true, ready = false;                       // ready: the stage is known to be filled
         for (int64_t i = unit; ok && i < work.items; i += units) {
             const Item it = work.item(p, i);
             if (!(ok = await(free + 8 * buffer, free_phase, polls, s, p.control))) break;
-            fence_after();
             const uint32_t d = tmem + buffer * kTileN;
             for (int k = 0; k < it.steps; ++k) {
-                if (!(ok = await(full + 8 * stage, phase, polls, s, p.control))) break;
+                if (!ready && !(ok = await(full + 8 * stage, phase, polls, s, p.control))) break;
                 fence_after();
-                const uint32_t a = tiles + stage * S::kStage, b = a + S::kA;
-                const uint64_t da = descriptor(a, kAK), db = descriptor(b, kBK);
-#pragma unroll
-                for (int j = 0; j < kTileK / 16; ++j)
-                    mma<kCtas>(d, da + (j * kStepBytes<kAK> >> 4), db + (j * kStepBytes<kBK> >> 4), kInstruction, (k | j) != 0);
-                commit<kCtas>(empty + 8 * stage);
+                const uint32_t a = tiles + stage * S::kStage, b = a + S::kA, used = empty + 8 * stage;
                 if (++stage == S::kStages) stage = 0, phase ^= 1;
+                // a look at the next stage while this one's instructions are still to come
+                ready = k + 1 < it.steps && __all_sync(0xFFFFFFFFu, mbar_test(full + 8 * stage, phase));
+                const uint64_t da = descriptor(a, kAK), db = descriptor(b, kBK);
+                if (elected()) {
+#pragma unroll
+                    for (int j = 0; j < kTileK / 16; ++j)
+                        mma<kCtas>(d, da + (j * kStepBytes<kAK> >> 4), db + (j * kStepBytes<kBK> >> 4), kInstruction, (k | j) != 0);
+                    commit<kCtas>(used);
+                }
+                __syncwarp();
             }
             if (!ok) break;
-            commit<kCtas>(done + 8 * buffer);
+            if (elected()) commit<kCtas>(done + 8 * buffer);
+            __syncwarp();
             buffer ^= 1;
             if (buffer == 0) free_phase ^= 1;
         }
         if (!ok) {
-            commit<kCtas>(smem_addr(&s.last));
+            if (elected()) commit<kCtas>(smem_addr(&s.last));
+            __syncwarp();
             mbar_wait(smem_addr(&s.last), 0, kPolls);
         }
     } else if (warp >= 2) {
@@ -567,8 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         uint32_t phase = 0;
         for (int64_t i = unit; i < work.items; i += units) {
             const Item it = work.item(p, i);
-            const bool ok = await(done + 8 * buffer, phase, polls, s, p.control);
-            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            if (!await(done + 8 * buffer, phase, polls, s, p.control)) break;
             fence_after();
             const uint32_t at = tmem + buffer * kTileN + (lanes << 16);
             const int64_t row = ((int64_t)it.m * kCtas + rank) * kRowsOfCta + lanes + lane;
@@ -883,7 +920,7 @@ struct Layout {
     uint64_t control, index, label, w, label_logit, lse2, coef, sums, stats, gathered, prob, part, table, bytes;
 };
 
-constexpr int64_t kPieceBytes = int64_t(128) << 20;   // of P, unless rows are so many that pieces would get short
+constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of P, unless rows are so many that pieces would get short
 constexpr int64_t kShortPiece = 4096;
 
 constexpr int kSms = 148;                 // of a B200: sums are split alike on every device
@@ -968,6 +1005,18 @@ bool make_map(CUtensorMap *m, const void *base, int32_t dtype, int64_t rows, int
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same as groups of 64 columns (the stride is a multiple of 64), 64 rows of two groups at a time.
+bool make_group_map(CUtensorMap *m, const void *base, int32_t dtype, int64_t rows, int64_t cols, int64_t stride)
+{
+    const EncodeFn fn = encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(cols + 63) / 64}, strides[2] = {(cuuint64_t)stride * 2, 128};
+    const cuuint32_t box[3] = {64, kTileK, 2}, step[3] = {1, 1, 1};
+    return fn(m, dtype == SO_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides,
+              box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int kMode, int kCtas>
 so_status launch_product(const CUtensorMap &a, const CUtensorMap &b, const Product &p, int units, cudaStream_t st)
 {
@@ -1033,18 +1082,20 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     p.part = reinterpret_cast<float *>(scratch + l.part), p.part_stride = l.part_stride;
     p.table_grad = c.dtable, p.grad_stride = c.dtable_stride, p.grad_dtype = c.grad_dtype, p.accumulate = c.accumulate, p.grad_scale = c.grad_scale;
     p.grad_vectors = aligned(c.dtable, 32) && (c.dtable_stride * elem_size(c.grad_dtype)) % 32 == 0;
+    p.table_groups = l.packed || c.cols % 64 == 0;           // a row's last group ends with it
     p.patience = patience();
 
     // the table as it is, or a packed piece of it
     const uint16_t *table = static_cast<const uint16_t *>(c.table);
     uint16_t *packed = reinterpret_cast<uint16_t *>(scratch + l.table);
     CUtensorMap hidden_k, hidden_m, table_k, table_m, prob_k, prob_m;
-    if (!make_map(&hidden_k, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld, kRowsOfCta) || !make_map(&hidden_m, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld, kTileK))
+    if (!make_map(&hidden_k, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld, kRowsOfCta) || !make_group_map(&hidden_m, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld))
         return SO_ERR_CUDA;
     const auto table_maps = [&](int64_t rows) {
         const void *at = l.packed ? static_cast<const void *>(packed) : c.table;
         const int64_t stride = l.packed ? l.ld : c.vocab == 1 ? l.ld : c.table_stride;
-        return make_map(&table_k, at, c.dtype, rows, c.cols, stride, 128) && make_map(&table_m, at, c.dtype, rows, c.cols, stride, kTileK);
+        return make_map(&table_k, at, c.dtype, rows, c.cols, stride, 128) &&
+               (p.table_groups ? make_group_map(&table_m, at, c.dtype, rows, c.cols, stride) : make_map(&table_m, at, c.dtype, rows, c.cols, stride, kTileK));
     };
     const auto pack_piece = [&](int64_t first, int64_t width) {
         return launch(pack_kernel, (unsigned)(4 * sms), 256, 0, st, false, table + first * c.table_stride, c.table_stride, width, c.cols, packed, l.ld);
@@ -1068,7 +1119,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     SO_TRY(launch(join_kernel, (unsigned)(l.rows_pad / 32), 32 * kJoinWarps, 0, st, true, j));
     if (gradients) {
         if (!make_map(&prob_k, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, kRowsOfCta) ||
-            !make_map(&prob_m, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, kTileK))
+            !make_group_map(&prob_m, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece))
             return SO_ERR_CUDA;
         for (int64_t first = 0; first < c.vocab; first += l.piece) {
             Product q = p;
