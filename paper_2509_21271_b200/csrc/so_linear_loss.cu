@@ -29,7 +29,9 @@ namespace {
 constexpr int kTileN = 256;               // columns of a tile
 constexpr int kTileK = 64;                // of a step: 128 bytes, the width of the swizzle
 constexpr int kRowsOfCta = 128;           // rows of a tile that a block holds
-constexpr int kThreads = 192;             // a warp that copies, one that multiplies, four that end tiles
+constexpr int kEnders = 8;                // warps that end tiles: two for each 32 rows, with half of the columns each
+constexpr int kThreads = 64 + 32 * kEnders;   // and a warp that copies, one that multiplies
+constexpr int kEndCols = kTileN / 2;
 constexpr int kRowPad = 256;              // rows are padded to whole tiles of a pair of blocks
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -182,7 +184,8 @@ struct Product {
     float *label_logit;                   // [rows_pad]
     const float *lse2;                    // [rows_pad], in units of log 2
     const float *coef;                    // [rows_pad], w over the unit
-    float2 *stats;                        // [tiles of the vocabulary][rows_pad]: maximum, sum
+    float2 *stats;                        // [half tiles of the vocabulary][rows_pad]: maximum, sum
+    float *kept;                          // kStats: [rows_pad][prob_stride], where all logits are kept
     void *prob;                           // [planes][rows_pad][prob_stride]
     int64_t prob_stride;
     float *part;                          // [splits][rows_pad][part_stride]
@@ -314,11 +317,13 @@ template <typename T> __device__ __forceinline__ void unpack2(uint32_t w, float 
     hi = to_f32(T{(uint16_t)(w >> 16)});
 }
 
-// A row's maximum and sum over the tile's columns, and its label's logit if that is here.
+// Half a tile, n-th of the columns.  A row's maximum and sum over it, its label's logit if that is
+// here, and the logits themselves where they are kept.
 __device__ __forceinline__ void end_stats(const Product &p, uint32_t tmem, int64_t row, int live, int n)
 {
-    const int64_t n0 = p.first + (int64_t)n * kTileN;
-    const int cols = p.vocab - n0 < kTileN ? (int)(p.vocab - n0) : kTileN;
+    const int64_t n0 = p.first + (int64_t)n * kEndCols;
+    const int cols = p.vocab - n0 < kEndCols ? (int)(p.vocab - n0) : kEndCols;
+    if (cols <= 0) return;                // the second half of a last tile
     const bool in = row < live;
     const int64_t label = in ? (int64_t)p.label[row] - n0 : -1;
     float top = -kInf;
@@ -344,26 +349,59 @@ __device__ __forceinline__ void end_stats(const Product &p, uint32_t tmem, int64
     for (int c = 0; c < cols; c += 32) {
         float f[32];
         tmem_load(tmem + c, f);
+        if (p.kept && in) {
+            float *out = p.kept + row * p.prob_stride + n0 + c;
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+                uint32_t w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(f[i + j]);
+                store32(out + i, w);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
             sum0 += c + i < cols ? exp2_fast(fmaf(f[i], kLog2e, -ref)) : 0.0f;
             sum1 += c + i + 1 < cols ? exp2_fast(fmaf(f[i + 1], kLog2e, -ref)) : 0.0f;
         }
     }
-    if (in) p.stats[(n0 / kTileN) * p.rows_pad + row] = make_float2(top, sum0 + sum1);
+    if (in) p.stats[(n0 / kEndCols) * p.rows_pad + row] = make_float2(top, sum0 + sum1);
+}
+
+// 32 elements of P in `planes` parts of 16 bits; `f` is used up.
+template <typename T>
+__device__ __forceinline__ void store_prob(const Product &p, float (&f)[32], T *to)
+{
+    for (int plane = 0;; ++plane) {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = pack2<T>(f[2 * i], f[2 * i + 1]);
+        const uint32_t a[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]}, b[8] = {w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]};
+        store32(to, a);
+        store32(to + 16, b);
+        if (plane + 1 == p.planes) break;
+        to += (int64_t)p.rows_pad * p.prob_stride;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float lo, hi;
+            unpack2<T>(w[i], lo, hi);
+            f[2 * i] -= lo;
+            f[2 * i + 1] -= hi;
+        }
+    }
 }
 
 // P of the tile, in `planes` parts of 16 bits; zero in rows and columns that are not there.
 template <typename T>
 __device__ __forceinline__ void end_prob(const Product &p, uint32_t tmem, int64_t row, int live, int n)
 {
-    const int64_t n0 = p.first + (int64_t)n * kTileN;
-    const int cols = p.vocab - n0 < kTileN ? (int)(p.vocab - n0) : kTileN;
+    const int64_t n0 = p.first + (int64_t)n * kEndCols;
+    const int cols = p.vocab - n0 < kEndCols ? (int)(p.vocab - n0) : kEndCols;
     const bool in = row < live;
     const int64_t label = in ? (int64_t)p.label[row] - n0 : -1;
     const float lse2 = in ? p.lse2[row] : 0.0f, coef = in ? p.coef[row] : 0.0f;
-    T *out = static_cast<T *>(p.prob) + row * p.prob_stride + (int64_t)n * kTileN;
-    for (int c = 0; c < kTileN; c += 32) {
+    T *out = static_cast<T *>(p.prob) + row * p.prob_stride + (int64_t)n * kEndCols;
+    for (int c = 0; c < kEndCols; c += 32) {
         float f[32];
         tmem_load(tmem + c, f);
         const bool here = __any_sync(0xFFFFFFFFu, label >= c && label < c + 32);
@@ -373,31 +411,15 @@ __device__ __forceinline__ void end_prob(const Product &p, uint32_t tmem, int64_
             if (here && label == c + i) q -= 1.0f;
             f[i] = in && c + i < cols ? q * coef : 0.0f;
         }
-        for (int plane = 0;; ++plane) {
-            uint32_t w[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = pack2<T>(f[2 * i], f[2 * i + 1]);
-            T *to = out + (int64_t)plane * p.rows_pad * p.prob_stride + c;
-            const uint32_t a[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]}, b[8] = {w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]};
-            store32(to, a);
-            store32(to + 16, b);
-            if (plane + 1 == p.planes) break;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float lo, hi;
-                unpack2<T>(w[i], lo, hi);
-                f[2 * i] -= lo;
-                f[2 * i + 1] -= hi;
-            }
-        }
+        store_prob<T>(p, f, out + c);
     }
 }
 
 // The tile added to (or begun as) a part of dH, fp32; `nothing`: a short piece had no columns for it.
 __device__ __forceinline__ void end_hidden(const Product &p, uint32_t tmem, int64_t row, int live, int n, int split, bool nothing)
 {
-    float *out = p.part + ((int64_t)split * p.rows_pad + row) * p.part_stride + (int64_t)n * kTileN;
-    for (int c = 0; c < kTileN; c += 32) {
+    float *out = p.part + ((int64_t)split * p.rows_pad + row) * p.part_stride + (int64_t)n * kEndCols;
+    for (int c = 0; c < kEndCols; c += 32) {
         float f[32];
         tmem_load(tmem + c, f);
         if (row >= live) continue;
@@ -425,8 +447,8 @@ __device__ __forceinline__ void end_table(const Product &p, uint32_t tmem, int64
 {
     const int64_t v = p.first + row;
     const bool in = row < p.width && v < p.vocab;
-    const int64_t c0 = (int64_t)n * kTileN;
-    for (int c = 0; c < kTileN && c0 + c < p.cols; c += 32) {
+    const int64_t c0 = (int64_t)n * kEndCols;
+    for (int c = 0; c < kEndCols && c0 + c < p.cols; c += 32) {
         float f[32];
         tmem_load(tmem + c, f);
         if (!in) continue;
@@ -502,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(done + 8 * i, 1);
-            mbar_init(free + 8 * i, 4 * kCtas);
+            mbar_init(free + 8 * i, kEnders * kCtas);
         }
         mbar_init(smem_addr(&s.last), 1);
         mbar_init_fence();
@@ -516,6 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     fence_after();
     const uint32_t tmem = s.tmem;
     grid_dependency_wait();
+    grid_dependency_release();            // the next launch waits for this one's end before it reads anything
     const int live = p.control->live;
     const Work<kMode, kCtas> work(p, live);
 
@@ -600,6 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         }
     } else if (warp >= 2) {
         const uint32_t lanes = (uint32_t)(warp & 3) * 32;    // of tensor memory that this warp reaches
+        const int half = (warp - 2) / (kEnders / 2);
         const float scale = p.grad_scale * p.control->unit;
         int buffer = 0;
         uint32_t phase = 0;
@@ -607,12 +631,12 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             const Item it = work.item(p, i);
             if (!await(done + 8 * buffer, phase, polls, s, p.control)) break;
             fence_after();
-            const uint32_t at = tmem + buffer * kTileN + (lanes << 16);
+            const uint32_t at = tmem + buffer * kTileN + half * kEndCols + (lanes << 16);
             const int64_t row = ((int64_t)it.m * kCtas + rank) * kRowsOfCta + lanes + lane;
-            if (kMode == kStats) end_stats(p, at, row, live, it.n);
-            else if (kMode == kProb) end_prob<T>(p, at, row, live, it.n);
-            else if (kMode == kHidden) end_hidden(p, at, row, live, it.n, it.split, it.steps == 0);
-            else end_table(p, at, row, it.n, scale);
+            if (kMode == kStats) end_stats(p, at, row, live, 2 * it.n + half);
+            else if (kMode == kProb) end_prob<T>(p, at, row, live, 2 * it.n + half);
+            else if (kMode == kHidden) end_hidden(p, at, row, live, 2 * it.n + half, it.split, it.steps == 0);
+            else end_table(p, at, row, 2 * it.n + half, scale);
             fence_before();
             __syncwarp();
             if (lane == 0) {
@@ -647,7 +671,8 @@ struct Rows {
     float *row_loss;
     void *dhidden;
     int64_t dhidden_stride;
-    int32_t fp16, gradient, vectors, dhidden_vectors;
+    float2 *counts;                       // [chunks]: rows that take part (as bits), largest weight; NULL: one chunk
+    int32_t fp16, vectors, dhidden_vectors;
 };
 
 __device__ __forceinline__ bool is_live(const Rows &r, int64_t i)
@@ -657,11 +682,13 @@ __device__ __forceinline__ bool is_live(const Rows &r, int64_t i)
     return label >= 0 && label < r.vocab;
 }
 
-constexpr int kGatherThreads = 256, kGatherRows = 32;
+constexpr int kGatherThreads = 256, kGatherRows = kGatherThreads / 32;
+constexpr int kChunk = 4096;              // rows that one block counts; batches beyond it are counted by chunks first
 
 // 16-bit elements [0, n) of a row of `n_pad` (a multiple of 8), zeros behind; `src` NULL: zeros.
 __device__ __forceinline__ void copy_row(uint16_t *dst, const uint16_t *src, int64_t n, int64_t n_pad, bool vectors, int lane)
 {
+#pragma unroll 4
     for (int64_t c = lane * 8; c < n_pad; c += 256) {
         uint4 v = make_uint4(0, 0, 0, 0);
         if (src && vectors && c + 8 <= n) {
@@ -676,49 +703,67 @@ __device__ __forceinline__ void copy_row(uint16_t *dst, const uint16_t *src, int
     }
 }
 
-// Gathers the rows that take part, 32 of the caller's rows a block; a block counts those before
-// its own for itself.  The last block knows them all.
-__global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_constant__ Rows r)
+// Rows that take part among [from, to), and the largest weight there; known to every thread.
+__device__ __forceinline__ int count_rows(const Rows &r, int64_t from, int64_t to, float *top)
 {
     __shared__ int s_count[kGatherThreads / 32];
     __shared__ float s_top[kGatherThreads / 32];
-    __shared__ int s_base, s_mask;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t row0 = (int64_t)blockIdx.x * kGatherRows;
-    const bool last = blockIdx.x == gridDim.x - 1;
     int count = 0;
-    float top = 0.0f;
-    for (int64_t i = threadIdx.x; i < row0; i += kGatherThreads) {
-        const bool in = is_live(r, i);
-        count += in;
-        if (last && in) top = fmaxf(top, r.weight ? fabsf(r.weight[i]) : 1.0f);
+    float most = 0.0f;
+#pragma unroll 4
+    for (int64_t i = from + threadIdx.x; i < to; i += kGatherThreads) {
+        const float w = r.weight ? r.weight[i] : 1.0f;
+        const int64_t label = load_id(r.labels, i, r.ids_dtype);
+        if (w != 0.0f && label >= 0 && label < r.vocab) {
+            ++count;
+            most = fmaxf(most, fabsf(w));
+        }
     }
     count = __reduce_add_sync(0xFFFFFFFFu, count);
-    if (lane == 0) s_count[warp] = count;
-    if (warp == 0) {
-        const int64_t i = row0 + lane;
-        const bool in = i < r.rows && is_live(r, i);
-        if (in) top = fmaxf(top, r.weight ? fabsf(r.weight[i]) : 1.0f);
-        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, in);
-        if (lane == 0) s_mask = (int)mask;
-    }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    if (lane == 0) s_top[warp] = top;
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+    if (lane == 0) s_count[warp] = count, s_top[warp] = most;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        int base = 0;
-        for (int i = 0; i < kGatherThreads / 32; ++i) base += s_count[i];
-        s_base = base;
+    count = 0;
+#pragma unroll
+    for (int i = 0; i < kGatherThreads / 32; ++i) count += s_count[i], most = fmaxf(most, s_top[i]);
+    *top = most;
+    return count;
+}
+
+// Counts of chunks of rows, for batches of many.
+__global__ void __launch_bounds__(kGatherThreads) count_kernel(const __grid_constant__ Rows r)
+{
+    grid_dependency_wait();
+    const int64_t from = (int64_t)blockIdx.x * kChunk, to = from + kChunk;
+    float top;
+    const int count = count_rows(r, from, to < r.rows ? to : r.rows, &top);
+    if (threadIdx.x == 0) r.counts[blockIdx.x] = make_float2(__int_as_float(count), top);
+}
+
+// Gathers the rows that take part, a row a warp; a block counts the rows before its own for
+// itself (those of its chunk, behind what earlier chunks have).  The last block knows them all.
+__global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_constant__ Rows r)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t row0 = (int64_t)blockIdx.x * kGatherRows, chunk = r.counts ? row0 / kChunk : 0;
+    grid_dependency_wait();
+    grid_dependency_release();
+    float top;
+    int base = count_rows(r, chunk * kChunk, row0, &top);
+    for (int64_t i = 0; i < chunk; ++i) {
+        const float2 c = r.counts[i];
+        base += __float_as_int(c.x);
+        top = fmaxf(top, c.y);
     }
-    __syncthreads();
-    const uint32_t mask = (uint32_t)s_mask;
-    const int base = s_base;
-    for (int k = warp; k < kGatherRows; k += kGatherThreads / 32) {
-        const int64_t i = row0 + k;
-        if (i >= r.rows) break;
-        if (mask >> k & 1u) {
-            const int at = base + __popc(mask & ((1u << k) - 1u));
+    // lane k of every warp looks at the block's k-th row
+    const bool in = lane < kGatherRows && row0 + lane < r.rows && is_live(r, row0 + lane);
+    const uint32_t mask = __ballot_sync(0xFFFFFFFFu, in);
+    const int64_t i = row0 + warp;
+    if (i < r.rows) {
+        if (mask >> warp & 1u) {
+            const int at = base + __popc(mask & ((1u << warp) - 1u));
             copy_row(static_cast<uint16_t *>(r.gathered) + at * r.gathered_stride, static_cast<const uint16_t *>(r.hidden) + i * r.hidden_stride,
                      r.cols, r.gathered_stride, r.vectors, lane);
             if (lane == 0) {
@@ -728,7 +773,7 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
             }
         } else {
             if (lane == 0) r.row_loss[i] = 0.0f;
-            if (r.gradient && r.dhidden) {
+            if (r.dhidden) {
                 uint16_t *out = static_cast<uint16_t *>(r.dhidden) + i * r.dhidden_stride;
                 if (r.dhidden_vectors) copy_row(out, nullptr, r.cols, r.cols, true, lane);
                 else
@@ -736,13 +781,15 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
             }
         }
     }
-    if (!last) return;
+    if (blockIdx.x != gridDim.x - 1) return;
     const int live = base + __popc(mask);
     // rows up to the end of a tile count in sums over rows, with factors of zero
     for (int at = live + warp; at < (live + kRowPad - 1) / kRowPad * kRowPad; at += kGatherThreads / 32)
         copy_row(static_cast<uint16_t *>(r.gathered) + at * r.gathered_stride, nullptr, r.cols, r.gathered_stride, true, lane);
+    if (in) top = fmaxf(top, r.weight ? fabsf(r.weight[row0 + lane]) : 1.0f);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kGatherThreads / 32; ++i) top = fmaxf(top, s_top[i]);
         int e = 0;
         if (top > 0.0f && top < kInf) frexpf(top, &e);       // top < 2^e
         if (r.fp16) e -= 15;
@@ -754,6 +801,38 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
     }
 }
 
+// P from logits that were kept: 32 columns of a row a thread, rows up to whole steps of the sums over them.
+template <typename T>
+__global__ void __launch_bounds__(256) prob_kernel(const __grid_constant__ Product p)
+{
+    grid_dependency_wait();
+    grid_dependency_release();
+    const int live = p.control->live;
+    const int64_t groups = p.prob_stride / 32, all = (int64_t)((live + kTileK - 1) / kTileK * kTileK) * groups;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / groups, c = (i - row * groups) * 32;
+        const bool in = row < live;
+        float f[32] = {};
+        if (in) {
+            const int64_t label = p.label[row] - c;
+            const float lse2 = p.lse2[row], coef = p.coef[row];
+            const float *z = p.kept + row * p.prob_stride + c;
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {
+                uint32_t w[8];
+                load32(z + k, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float q = exp2_fast(fmaf(__uint_as_float(w[j]), kLog2e, -lse2));
+                    if (label == k + j) q -= 1.0f;
+                    f[k + j] = c + k + j < p.vocab ? q * coef : 0.0f;
+                }
+            }
+        }
+        store_prob<T>(p, f, static_cast<T *>(p.prob) + row * p.prob_stride + c);
+    }
+}
+
 struct Join {
     Control *control;
     const float2 *stats;
@@ -761,13 +840,14 @@ struct Join {
     const int32_t *index;
     float *lse2, *coef, *row_loss, *loss;
     double *sums;                         // [blocks]
-    int32_t rows_pad, tiles;
+    int32_t rows_pad, halves;
+    int64_t rows;
 };
 
 constexpr int kJoinWarps = 8;
 
 // Joins the tiles' statistics, 32 rows a block (a lane each, the tiles dealt out to warps); the
-// block that comes last adds up the loss.
+// block that comes last adds up the loss.  After a wait that ran out both are NaN, masked rows too.
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_constant__ Join j)
 {
     __shared__ float2 s_part[kJoinWarps][32];
@@ -775,19 +855,25 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_cons
     __shared__ bool s_last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     grid_dependency_wait();
+    grid_dependency_release();
     const int live = j.control->live;
     const int row = blockIdx.x * 32 + lane;
+    if (j.control->gave_up) {
+        if (warp == 0 && row < j.rows) j.row_loss[row] = kNan;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *j.loss = kNan;
+        return;
+    }
     float top = -kInf, sum = 0.0f;
     if (blockIdx.x * 32 < live) {
         // rows behind the last one are read as they lie in scratch, and dropped
         const float2 *at = j.stats + row;
-        for (int t0 = warp; t0 < j.tiles; t0 += 8 * kJoinWarps) {
+        for (int t0 = warp; t0 < j.halves; t0 += 8 * kJoinWarps) {
             float2 v[8];
             float most = top;
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const int t = t0 + u * kJoinWarps;
-                v[u] = t < j.tiles && row < live ? at[(int64_t)t * j.rows_pad] : make_float2(-kInf, 0.0f);
+                v[u] = t < j.halves && row < live ? at[(int64_t)t * j.rows_pad] : make_float2(-kInf, 0.0f);
                 most = fmaxf(most, v[u].x);
             }
             const float ref = most == -kInf ? 0.0f : most;
@@ -844,67 +930,64 @@ struct Finish {
     void *dhidden, *table_grad;
     float *row_loss, *loss;
     int64_t rows, vocab, cols, dhidden_stride, grad_stride, part_stride;
-    int32_t rows_pad, splits, grad_dtype, vectors;
+    int32_t rows_pad, splits, grad_dtype, vectors, accumulate;
     float grad_scale;
 };
 
-constexpr int kFinishThreads = 256;
+constexpr int kFinishThreads = 128;
 
-// dH from its parts, a row a turn; NaN everywhere after a wait that ran out.
+// dH from its parts, 128 x 8 columns of a row a turn.  dW where no row took part: zeros, unless it
+// is added to.  NaN everywhere after a wait that ran out.
 template <typename T>
 __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ Finish f)
 {
     grid_dependency_wait();
     const int live = f.control->live;
-    if (f.control->gave_up) {
-        const int64_t me = (int64_t)blockIdx.x * kFinishThreads + threadIdx.x, all = (int64_t)gridDim.x * kFinishThreads;
+    const bool gave_up = f.control->gave_up != 0;
+    const int64_t me = (int64_t)blockIdx.x * kFinishThreads + threadIdx.x, all = (int64_t)gridDim.x * kFinishThreads;
+    if (f.table_grad && (gave_up || (live == 0 && !f.accumulate)))
+        for (int64_t i = me; i < f.vocab * f.cols; i += all)
+            store_any(f.table_grad, i / f.cols * f.grad_stride + i % f.cols, f.grad_dtype, gave_up ? kNan : 0.0f);
+    if (gave_up) {
         for (int64_t i = me; i < f.rows; i += all) f.row_loss[i] = kNan;
         if (me == 0) *f.loss = kNan;
         if (f.dhidden)
             for (int64_t i = me; i < f.rows * f.cols; i += all) static_cast<T *>(f.dhidden)[i / f.cols * f.dhidden_stride + i % f.cols] = from_f32<T>(kNan);
-        if (f.table_grad)
-            for (int64_t i = me; i < f.vocab * f.cols; i += all) store_any(f.table_grad, i / f.cols * f.grad_stride + i % f.cols, f.grad_dtype, kNan);
         return;
     }
     if (!f.dhidden) return;
     const float scale = f.grad_scale * f.control->unit;
-    for (int row = blockIdx.x; row < live; row += gridDim.x) {
-        const float *in = f.part + (int64_t)row * f.part_stride;
-        T *out = static_cast<T *>(f.dhidden) + (int64_t)f.index[row] * f.dhidden_stride;
-        for (int64_t c = threadIdx.x * 8; c < f.cols; c += kFinishThreads * 8) {
-            float sum[8] = {};
-            for (int k = 0; k < f.splits; ++k) {
-                uint32_t w[8];
-                load32(in + (int64_t)k * f.rows_pad * f.part_stride + c, w);
+    const int64_t per_row = (f.cols + kFinishThreads * 8 - 1) / (kFinishThreads * 8), step = (int64_t)f.rows_pad * f.part_stride;
+    for (int64_t item = blockIdx.x; item < live * per_row; item += gridDim.x) {
+        const int64_t row = item / per_row, c = (item - row * per_row) * kFinishThreads * 8 + threadIdx.x * 8;
+        if (c >= f.cols) continue;
+        const float *in = f.part + row * f.part_stride + c;
+        T *out = static_cast<T *>(f.dhidden) + (int64_t)f.index[row] * f.dhidden_stride + c;
+        float sum[8] = {};
+#pragma unroll 8
+        for (int k = 0; k < f.splits; ++k) {
+            uint32_t w[8];
+            load32(in + k * step, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] += __uint_as_float(w[i]);
-            }
+            for (int i = 0; i < 8; ++i) sum[i] += __uint_as_float(w[i]);
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] *= scale;
-            if (f.vectors && c + 8 <= f.cols) {
-                *reinterpret_cast<uint4 *>(out + c) = pack<T>(sum);
-            } else {
+        for (int i = 0; i < 8; ++i) sum[i] *= scale;
+        if (f.vectors && c + 8 <= f.cols) {
+            *reinterpret_cast<uint4 *>(out) = pack<T>(sum);
+        } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c + i < f.cols) out[c + i] = from_f32<T>(sum[i]);
-            }
+            for (int i = 0; i < 8; ++i)
+                if (c + i < f.cols) out[i] = from_f32<T>(sum[i]);
         }
     }
-}
-
-// dW without any row that takes part: zeros, unless it is added to.
-__global__ void __launch_bounds__(256) no_rows_kernel(const Control *control, void *grad, int64_t stride, int64_t vocab, int64_t cols, int32_t dtype)
-{
-    grid_dependency_wait();
-    if (control->live != 0) return;
-    for (int64_t v = blockIdx.x; v < vocab; v += gridDim.x)
-        for (int64_t c = threadIdx.x; c < cols; c += 256) store_any(grad, v * stride + c, dtype, 0.0f);
 }
 
 // A piece of a table whose rows cannot be copied as they are, rows padded to whole steps.
 __global__ void __launch_bounds__(256) pack_kernel(const uint16_t *table, int64_t stride, int64_t rows, int64_t cols, uint16_t *out, int64_t out_stride)
 {
     grid_dependency_wait();
+    grid_dependency_release();
     for (int64_t v = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); v < rows; v += (int64_t)gridDim.x * 8)
         copy_row(out + v * out_stride, table + v * stride, cols, out_stride, false, threadIdx.x & 31);
 }
@@ -915,13 +998,16 @@ int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // Where everything lies in scratch.
 struct Layout {
-    int64_t rows_pad, ld, pieces, piece, splits, planes, part_stride, tiles;
-    bool packed;
-    uint64_t control, index, label, w, label_logit, lse2, coef, sums, stats, gathered, prob, part, table, bytes;
+    int64_t rows_pad, ld, pieces, piece, splits, planes, part_stride, halves;
+    bool packed, keep;
+    uint64_t control, counts, index, label, w, label_logit, lse2, coef, sums, stats, gathered, kept, prob, part, table, bytes;
 };
 
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of P, unless rows are so many that pieces would get short
 constexpr int64_t kShortPiece = 4096;
+// Up to so many bytes of fp32 logits are kept from the statistics to P: a batch that small would
+// read the table again and multiply again for less than that costs.
+constexpr int64_t kKeptBytes = int64_t(256) << 20;
 
 constexpr int kSms = 148;                 // of a B200: sums are split alike on every device
 
@@ -932,7 +1018,7 @@ Layout layout(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t 
     l.packed = packed;
     l.rows_pad = up(rows > 0 ? rows : 1, kRowPad);
     l.ld = up(cols, kTileK);
-    l.tiles = (vocab + kTileN - 1) / kTileN;
+    l.halves = (vocab + kEndCols - 1) / kEndCols;
     l.planes = grad_dtype != SO_DTYPE_FP32 ? 1 : dtype == SO_DTYPE_BF16 ? 3 : 2;
     l.piece = up(vocab, kTileN);
     if (gradients || packed) {
@@ -960,6 +1046,7 @@ Layout layout(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t 
     };
     const uint64_t rp = (uint64_t)l.rows_pad;
     l.control = take(sizeof(Control));
+    l.counts = take((rp / kChunk + 1) * sizeof(float2));
     l.index = take(rp * 4);
     l.label = take(rp * 4);
     l.w = take(rp * 4);
@@ -967,8 +1054,10 @@ Layout layout(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t 
     l.lse2 = take(rp * 4);
     l.coef = take(rp * 4);
     l.sums = take(rp / 32 * 8);
-    l.stats = take(rp * (uint64_t)l.tiles * 8);
+    l.stats = take(rp * (uint64_t)l.halves * 8);
     l.gathered = take(rp * (uint64_t)l.ld * 2);
+    l.keep = gradients && l.pieces == 1 && l.rows_pad * l.piece * 4 <= kKeptBytes;
+    if (l.keep) l.kept = take(rp * (uint64_t)l.piece * 4);
     if (gradients) {
         l.prob = take(rp * (uint64_t)(l.planes * l.piece) * 2);
         l.part = take(rp * (uint64_t)(l.splits * l.part_stride) * 4);
@@ -1033,12 +1122,14 @@ so_status launch_product(const CUtensorMap &a, const CUtensorMap &b, const Produ
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = Shape<kCtas>::kBytes;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kCtas;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCtas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a, b, p) == cudaSuccess ? SO_OK : SO_ERR_CUDA;
 }
 
@@ -1066,10 +1157,12 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     r.control = control, r.hidden = c.hidden, r.hidden_stride = c.hidden_stride, r.labels = c.labels, r.ids_dtype = c.ids_dtype, r.weight = c.weight;
     r.rows = c.rows, r.vocab = c.vocab, r.cols = c.cols, r.rows_pad = (int32_t)l.rows_pad;
     r.gathered = scratch + l.gathered, r.gathered_stride = l.ld, r.index = index, r.label = label, r.w = w, r.row_loss = c.row_loss;
-    r.dhidden = c.dhidden, r.dhidden_stride = c.dhidden_stride, r.fp16 = c.dtype == SO_DTYPE_FP16, r.gradient = gradients;
+    r.dhidden = c.dhidden, r.dhidden_stride = c.dhidden_stride, r.fp16 = c.dtype == SO_DTYPE_FP16;
     r.vectors = aligned(c.hidden, 16) && (c.rows <= 1 || c.hidden_stride % 8 == 0);
     r.dhidden_vectors = aligned(c.dhidden, 16) && c.cols % 8 == 0 && (c.rows <= 1 || c.dhidden_stride % 8 == 0);
-    SO_TRY(launch(gather_kernel, (unsigned)(c.rows > 0 ? (c.rows + kGatherRows - 1) / kGatherRows : 1), kGatherThreads, 0, st, false, r));
+    r.counts = c.rows > kChunk ? reinterpret_cast<float2 *>(scratch + l.counts) : nullptr;
+    if (r.counts) SO_TRY(launch(count_kernel, (unsigned)((c.rows + kChunk - 1) / kChunk), kGatherThreads, 0, st, false, r));
+    SO_TRY(launch(gather_kernel, (unsigned)(c.rows > 0 ? (c.rows + kGatherRows - 1) / kGatherRows : 1), kGatherThreads, 0, st, r.counts != nullptr, r));
 
     Product p = {};
     p.control = control, p.vocab = c.vocab, p.cols = c.cols, p.rows_pad = (int32_t)l.rows_pad, p.splits = (int32_t)l.splits, p.planes = (int32_t)l.planes;
@@ -1079,6 +1172,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     p.lse2 = lse2, p.coef = coef;
     p.stats = reinterpret_cast<float2 *>(scratch + l.stats);
     p.prob = scratch + l.prob, p.prob_stride = l.piece;
+    p.kept = l.keep ? reinterpret_cast<float *>(scratch + l.kept) : nullptr;
     p.part = reinterpret_cast<float *>(scratch + l.part), p.part_stride = l.part_stride;
     p.table_grad = c.dtable, p.grad_stride = c.dtable_stride, p.grad_dtype = c.grad_dtype, p.accumulate = c.accumulate, p.grad_scale = c.grad_scale;
     p.grad_vectors = aligned(c.dtable, 32) && (c.dtable_stride * elem_size(c.grad_dtype)) % 32 == 0;
@@ -1098,7 +1192,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
                (p.table_groups ? make_group_map(&table_m, at, c.dtype, rows, c.cols, stride) : make_map(&table_m, at, c.dtype, rows, c.cols, stride, kTileK));
     };
     const auto pack_piece = [&](int64_t first, int64_t width) {
-        return launch(pack_kernel, (unsigned)(4 * sms), 256, 0, st, false, table + first * c.table_stride, c.table_stride, width, c.cols, packed, l.ld);
+        return launch(pack_kernel, (unsigned)(4 * sms), 256, 0, st, true, table + first * c.table_stride, c.table_stride, width, c.cols, packed, l.ld);
     };
 
     if (l.packed) {
@@ -1115,7 +1209,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
         p.width = c.vocab;
         SO_TRY((launch_product<T, kStats, kCtas>(hidden_k, table_k, p, units, st)));
     }
-    Join j = {control, p.stats, p.label_logit, w, index, lse2, coef, c.row_loss, c.loss, reinterpret_cast<double *>(scratch + l.sums), (int32_t)l.rows_pad, (int32_t)l.tiles};
+    Join j = {control, p.stats, p.label_logit, w, index, lse2, coef, c.row_loss, c.loss, reinterpret_cast<double *>(scratch + l.sums), (int32_t)l.rows_pad, (int32_t)l.halves, c.rows};
     SO_TRY(launch(join_kernel, (unsigned)(l.rows_pad / 32), 32 * kJoinWarps, 0, st, true, j));
     if (gradients) {
         if (!make_map(&prob_k, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, kRowsOfCta) ||
@@ -1131,16 +1225,16 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
                 if (!table_maps(q.width)) return SO_ERR_CUDA;
                 q.table_row = 0;
             }
-            SO_TRY((launch_product<T, kProb, kCtas>(hidden_k, table_k, q, units, st)));
+            if (l.keep) SO_TRY(launch(prob_kernel<T>, (unsigned)(8 * sms), 256, 0, st, true, q));
+            else SO_TRY((launch_product<T, kProb, kCtas>(hidden_k, table_k, q, units, st)));
             if (c.dhidden) SO_TRY((launch_product<T, kHidden, kCtas>(prob_k, table_m, q, units, st)));
             if (c.dtable) SO_TRY((launch_product<T, kTable, kCtas>(prob_m, hidden_m, q, units, st)));
         }
-        if (c.dtable && !c.accumulate)
-            SO_TRY(launch(no_rows_kernel, (unsigned)(4 * sms), 256, 0, st, true, control, c.dtable, c.dtable_stride, c.vocab, c.cols, c.grad_dtype));
     }
+    if (!gradients) return SO_OK;
     Finish f = {control, p.part, index, c.dhidden, c.dtable, c.row_loss, c.loss, c.rows, c.vocab, c.cols, c.dhidden_stride, c.dtable_stride, l.part_stride,
-                (int32_t)l.rows_pad, (int32_t)l.splits, c.grad_dtype, r.dhidden_vectors, c.grad_scale};
-    return launch(finish_kernel<T>, (unsigned)(4 * sms), kFinishThreads, 0, st, true, f);
+                (int32_t)l.rows_pad, (int32_t)l.splits, c.grad_dtype, r.dhidden_vectors, c.accumulate, c.grad_scale};
+    return launch(finish_kernel<T>, (unsigned)(16 * sms), kFinishThreads, 0, st, true, f);
 }
 
 so_status check_sizes(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t grad_dtype)
