@@ -32,6 +32,7 @@ constexpr int kRowsOfCta = 128;           // rows of a tile that a block holds
 constexpr int kEnders = 8;                // warps that end tiles: two for each 32 rows, with half of the columns each
 constexpr int kThreads = 64 + 32 * kEnders;   // and a warp that copies, one that multiplies
 constexpr int kEndCols = kTileN / 2;
+constexpr uint32_t kBox = 32 * 128;       // what such a warp copies out at a time: 32 rows of 128 bytes
 constexpr int kRowPad = 256;              // rows are padded to whole tiles of a pair of blocks
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -89,6 +90,20 @@ __device__ __forceinline__ void tma_load_groups(uint32_t dst, const CUtensorMap 
         asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                      ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(group), "r"(bar) : "memory");
 }
+// A box in shared memory to its place in a matrix, or added to what is there (fp32); what lies
+// outside of the matrix is left out.  By the same thread of a warp each time.
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, uint32_t src, bool add)
+{
+    if (add)
+        asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];"
+                     ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 template <int kCtas>
 __device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t cols)
 {
@@ -192,7 +207,7 @@ struct Product {
     int64_t part_stride;
     void *table_grad;
     int64_t grad_stride;
-    int32_t grad_dtype, accumulate, grad_vectors;
+    int32_t grad_dtype, accumulate, grad_vectors, grad_boxes;
     float grad_scale;
     Patience patience;
 };
@@ -254,8 +269,8 @@ struct Work {
 template <int kCtas>
 struct Shape {
     static constexpr uint32_t kA = kRowsOfCta * 128, kB = kTileN / kCtas * 128, kStage = kA + kB;
-    static constexpr int kStages = kCtas == 2 ? 7 : 4;       // 224 and 192 KB
-    static constexpr size_t kBytes = (size_t)kStage * kStages + 1024;
+    static constexpr int kStages = kCtas == 2 ? 6 : 4;       // 192 KB
+    static constexpr size_t kBytes = (size_t)kStage * kStages + kEnders * kBox + 1024;
 };
 
 struct Shared {
@@ -315,6 +330,23 @@ template <typename T> __device__ __forceinline__ void unpack2(uint32_t w, float 
 {
     lo = to_f32(T{(uint16_t)(w & 0xFFFFu)});
     hi = to_f32(T{(uint16_t)(w >> 16)});
+}
+
+// 128 bytes of each lane's row, swizzled, through shared memory to rows y.. and columns x.. of a
+// matrix.  Stores of a lane's own 32 bytes into 32 rows take a cycle or two for every row: 255 us
+// where the table's gradient of one token (128256 x 4096 bf16) takes 1XX us this way.
+__device__ __forceinline__ void copy_out(const CUtensorMap *map, uint32_t box, int x, int y, const uint32_t (&w)[32], bool add)
+{
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) tma_stores_read();     // the box is free again
+    __syncwarp();
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128 + ((u ^ (lane & 7)) << 4)), "r"(w[4 * u]), "r"(w[4 * u + 1]),
+                     "r"(w[4 * u + 2]), "r"(w[4 * u + 3]) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) tma_store(map, x, y, box, add);
 }
 
 // Half a tile, n-th of the columns.  A row's maximum and sum over it, its label's logit if that is
@@ -393,57 +425,95 @@ __device__ __forceinline__ void store_prob(const Product &p, float (&f)[32], T *
 
 // P of the tile, in `planes` parts of 16 bits; zero in rows and columns that are not there.
 template <typename T>
-__device__ __forceinline__ void end_prob(const Product &p, uint32_t tmem, int64_t row, int live, int n)
+__device__ __forceinline__ void end_prob(const Product &p, const CUtensorMap *map, uint32_t box, uint32_t tmem, int64_t row, int live, int n)
 {
     const int64_t n0 = p.first + (int64_t)n * kEndCols;
     const int cols = p.vocab - n0 < kEndCols ? (int)(p.vocab - n0) : kEndCols;
     const bool in = row < live;
     const int64_t label = in ? (int64_t)p.label[row] - n0 : -1;
     const float lse2 = in ? p.lse2[row] : 0.0f, coef = in ? p.coef[row] : 0.0f;
-    T *out = static_cast<T *>(p.prob) + row * p.prob_stride + (int64_t)n * kEndCols;
-    for (int c = 0; c < kEndCols; c += 32) {
-        float f[32];
-        tmem_load(tmem + c, f);
-        const bool here = __any_sync(0xFFFFFFFFu, label >= c && label < c + 32);
+    const int y = (int)row - (int)(threadIdx.x & 31);
+    for (int c = 0; c < kEndCols; c += 64) {
+        float f[2][32];
+        uint32_t w[32];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            float q = exp2_fast(fmaf(f[i], kLog2e, -lse2));
-            if (here && label == c + i) q -= 1.0f;
-            f[i] = in && c + i < cols ? q * coef : 0.0f;
+        for (int h = 0; h < 2; ++h) {
+            tmem_load(tmem + c + 32 * h, f[h]);
+            const int c0 = c + 32 * h;
+            const bool here = __any_sync(0xFFFFFFFFu, label >= c0 && label < c0 + 32);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                float q = exp2_fast(fmaf(f[h][i], kLog2e, -lse2));
+                if (here && label == c0 + i) q -= 1.0f;
+                f[h][i] = in && c0 + i < cols ? q * coef : 0.0f;
+            }
         }
-        store_prob<T>(p, f, out + c);
+        for (int plane = 0;; ++plane) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = pack2<T>(f[i / 16][2 * (i % 16)], f[i / 16][2 * (i % 16) + 1]);
+            copy_out(map, box, n * kEndCols + c, plane * p.rows_pad + y, w, false);
+            if (plane + 1 == p.planes) break;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                float lo, hi;
+                unpack2<T>(w[i], lo, hi);
+                f[i / 16][2 * (i % 16)] -= lo;
+                f[i / 16][2 * (i % 16) + 1] -= hi;
+            }
+        }
     }
 }
 
 // The tile added to (or begun as) a part of dH, fp32; `nothing`: a short piece had no columns for it.
-__device__ __forceinline__ void end_hidden(const Product &p, uint32_t tmem, int64_t row, int live, int n, int split, bool nothing)
+// One tile of a launch adds to an element, so that the order of the sums is that of the launches.
+__device__ __forceinline__ void end_hidden(const Product &p, const CUtensorMap *map, uint32_t box, uint32_t tmem, int64_t row, int n, int split, bool nothing)
 {
-    float *out = p.part + ((int64_t)split * p.rows_pad + row) * p.part_stride + (int64_t)n * kEndCols;
+    if (nothing && !p.begin) return;
+    const int y = split * p.rows_pad + (int)row - (int)(threadIdx.x & 31);
     for (int c = 0; c < kEndCols; c += 32) {
         float f[32];
+        uint32_t w[32];
         tmem_load(tmem + c, f);
-        if (row >= live) continue;
-        if (nothing) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) f[i] = 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < 32; i += 8) {
-            uint32_t w[8];
-            if (!p.begin) {
-                load32(out + c + i, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[i + j] += __uint_as_float(w[j]);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(f[i + j]);
-            store32(out + c + i, w);
-        }
+        for (int i = 0; i < 32; ++i) w[i] = nothing ? 0u : __float_as_uint(f[i]);
+        copy_out(map, box, n * kEndCols + c, y, w, !p.begin);
     }
 }
 
 // The tile as rows of dW, in the gradient's type.
-__device__ __forceinline__ void end_table(const Product &p, uint32_t tmem, int64_t row, int n, float scale)
+__device__ __forceinline__ void end_table(const Product &p, const CUtensorMap *map, uint32_t box, uint32_t tmem, int64_t row, int n, float scale)
+{
+    const int c0 = n * kEndCols, y = (int)(p.first + row) - (int)(threadIdx.x & 31);
+    if (p.grad_dtype == SO_DTYPE_FP32) {
+        for (int c = 0; c < kEndCols && c0 + c < p.cols; c += 32) {
+            float f[32];
+            uint32_t w[32];
+            tmem_load(tmem + c, f);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(f[i] * scale);
+            copy_out(map, box, c0 + c, y, w, false);
+        }
+        return;
+    }
+    const bool bf = p.grad_dtype == SO_DTYPE_BF16;
+    for (int c = 0; c < kEndCols && c0 + c < p.cols; c += 64) {
+        uint32_t w[32];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float f[32];
+            tmem_load(tmem + c + 32 * h, f);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float lo = f[2 * i] * scale, hi = f[2 * i + 1] * scale;
+                w[16 * h + i] = bf ? pack2_bf16(lo, hi) : pack2_f16(lo, hi);
+            }
+        }
+        copy_out(map, box, c0 + c, y, w, false);
+    }
+}
+
+// The same where it is added to what is there, or where rows do not start at 16-byte boundaries.
+__device__ __forceinline__ void end_table_by_lanes(const Product &p, uint32_t tmem, int64_t row, int n, float scale)
 {
     const int64_t v = p.first + row;
     const bool in = row < p.width && v < p.vocab;
@@ -503,7 +573,7 @@ __device__ __forceinline__ void end_table(const Product &p, uint32_t tmem, int64
 
 template <typename T, int kMode, int kCtas>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                               const __grid_constant__ Product p)
+                                                               const __grid_constant__ CUtensorMap map_out, const __grid_constant__ Product p)
 {
     using S = Shape<kCtas>;
     constexpr bool kAK = kMode != kTable;                    // A contiguous in K: H, H, P; P transposed is not
@@ -624,6 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     } else if (warp >= 2) {
         const uint32_t lanes = (uint32_t)(warp & 3) * 32;    // of tensor memory that this warp reaches
         const int half = (warp - 2) / (kEnders / 2);
+        const uint32_t box = tiles + S::kStage * S::kStages + (warp - 2) * kBox;
         const float scale = p.grad_scale * p.control->unit;
         int buffer = 0;
         uint32_t phase = 0;
@@ -634,9 +705,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             const uint32_t at = tmem + buffer * kTileN + half * kEndCols + (lanes << 16);
             const int64_t row = ((int64_t)it.m * kCtas + rank) * kRowsOfCta + lanes + lane;
             if (kMode == kStats) end_stats(p, at, row, live, 2 * it.n + half);
-            else if (kMode == kProb) end_prob<T>(p, at, row, live, 2 * it.n + half);
-            else if (kMode == kHidden) end_hidden(p, at, row, live, 2 * it.n + half, it.split, it.steps == 0);
-            else end_table(p, at, row, 2 * it.n + half, scale);
+            else if (kMode == kProb) end_prob<T>(p, &map_out, box, at, row, live, 2 * it.n + half);
+            else if (kMode == kHidden) end_hidden(p, &map_out, box, at, row, 2 * it.n + half, it.split, it.steps == 0);
+            else if (p.grad_boxes) end_table(p, &map_out, box, at, row, 2 * it.n + half, scale);
+            else end_table_by_lanes(p, at, row, 2 * it.n + half, scale);
             fence_before();
             __syncwarp();
             if (lane == 0) {
@@ -646,6 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             buffer ^= 1;
             if (buffer == 0) phase ^= 1;
         }
+        if (kMode != kStats && lane == 0) tma_stores_done();
     }
     __syncthreads();
     if (kCtas == 2) cluster_sync();
@@ -743,11 +816,14 @@ __global__ void __launch_bounds__(kGatherThreads) count_kernel(const __grid_cons
 }
 
 // Gathers the rows that take part, a row a warp; a block counts the rows before its own for
-// itself (those of its chunk, behind what earlier chunks have).  The last block knows them all.
+// itself (those of its chunk, behind what earlier chunks have).  Eight more blocks know them all.
 __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_constant__ Rows r)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t row0 = (int64_t)blockIdx.x * kGatherRows, chunk = r.counts ? row0 / kChunk : 0;
+    int64_t row0 = (int64_t)blockIdx.x * kGatherRows;
+    const bool behind = row0 >= r.rows;   // one of the blocks behind the last row: they know all rows
+    if (behind) row0 = r.rows;
+    const int64_t chunk = r.counts ? row0 / kChunk : 0;
     grid_dependency_wait();
     grid_dependency_release();
     float top;
@@ -781,14 +857,13 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
             }
         }
     }
-    if (blockIdx.x != gridDim.x - 1) return;
-    const int live = base + __popc(mask);
-    // rows up to the end of a tile count in sums over rows, with factors of zero
-    for (int at = live + warp; at < (live + kRowPad - 1) / kRowPad * kRowPad; at += kGatherThreads / 32)
+    if (!behind) return;
+    // rows up to the end of a step of the sums over rows count there, with factors of zero
+    const int first = (int)(((r.rows + kGatherRows - 1) / kGatherRows)), at = base + ((int)blockIdx.x - first) * kGatherRows + warp;
+    if (at < (base + kTileK - 1) / kTileK * kTileK)
         copy_row(static_cast<uint16_t *>(r.gathered) + at * r.gathered_stride, nullptr, r.cols, r.gathered_stride, true, lane);
-    if (in) top = fmaxf(top, r.weight ? fabsf(r.weight[row0 + lane]) : 1.0f);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if (blockIdx.x != gridDim.x - 1) return;
+    const int live = base;
     if (threadIdx.x == 0) {
         int e = 0;
         if (top > 0.0f && top < kInf) frexpf(top, &e);       // top < 2^e
@@ -844,7 +919,7 @@ struct Join {
     int64_t rows;
 };
 
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 32;
 
 // Joins the tiles' statistics, 32 rows a block (a lane each, the tiles dealt out to warps); the
 // block that comes last adds up the loss.  After a wait that ran out both are NaN, masked rows too.
@@ -936,7 +1011,7 @@ struct Finish {
 
 constexpr int kFinishThreads = 128;
 
-// dH from its parts, 128 x 8 columns of a row a turn.  dW where no row took part: zeros, unless it
+// dH from its parts.  dW where no row took part: zeros, unless it
 // is added to.  NaN everywhere after a wait that ran out.
 template <typename T>
 __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ Finish f)
@@ -957,20 +1032,39 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_con
     }
     if (!f.dhidden) return;
     const float scale = f.grad_scale * f.control->unit;
-    const int64_t per_row = (f.cols + kFinishThreads * 8 - 1) / (kFinishThreads * 8), step = (int64_t)f.rows_pad * f.part_stride;
-    for (int64_t item = blockIdx.x; item < live * per_row; item += gridDim.x) {
-        const int64_t row = item / per_row, c = (item - row * per_row) * kFinishThreads * 8 + threadIdx.x * 8;
-        if (c >= f.cols) continue;
-        const float *in = f.part + row * f.part_stride + c;
-        T *out = static_cast<T *>(f.dhidden) + (int64_t)f.index[row] * f.dhidden_stride + c;
+    // a warp has 256 columns; where there are many parts, the block's four share them
+    __shared__ float s_sum[3][32][9];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool share = f.splits >= 8;
+    const int64_t per_row = (f.cols + 255) / 256, step = (int64_t)f.rows_pad * f.part_stride, items = live * per_row;
+    for (int64_t first = share ? blockIdx.x : (int64_t)blockIdx.x * 4; first < items; first += share ? gridDim.x : (int64_t)gridDim.x * 4) {
+        const int64_t item = share ? first : first + warp, row = item / per_row, c = (item - row * per_row) * 256 + lane * 8;
+        const bool in = item < items && c < f.cols;
         float sum[8] = {};
+        if (in) {
+            const float *at = f.part + row * f.part_stride + c;
 #pragma unroll 8
-        for (int k = 0; k < f.splits; ++k) {
-            uint32_t w[8];
-            load32(in + k * step, w);
+            for (int k = share ? warp : 0; k < f.splits; k += share ? 4 : 1) {
+                uint32_t w[8];
+                load32(at + k * step, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += __uint_as_float(w[i]);
+                for (int i = 0; i < 8; ++i) sum[i] += __uint_as_float(w[i]);
+            }
         }
+        if (share) {
+            if (warp > 0)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s_sum[warp - 1][lane][i] = sum[i];
+            __syncthreads();
+            if (warp == 0)
+#pragma unroll
+                for (int w = 0; w < 3; ++w)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[i] += s_sum[w][lane][i];
+            __syncthreads();
+        }
+        if (!in || (share && warp > 0)) continue;
+        T *out = static_cast<T *>(f.dhidden) + (int64_t)f.index[row] * f.dhidden_stride + c;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] *= scale;
         if (f.vectors && c + 8 <= f.cols) {
@@ -1070,6 +1164,11 @@ Layout layout(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t 
 using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                               const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
+CUtensorMapDataType type_of(int32_t dtype)
+{
+    return dtype == SO_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : dtype == SO_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+}
+
 EncodeFn encoder()
 {
     static std::atomic<void *> found{nullptr};
@@ -1082,32 +1181,31 @@ EncodeFn encoder()
     return reinterpret_cast<EncodeFn>(fn);
 }
 
-// A matrix of 16-bit elements, copied 64 columns and `box_rows` rows at a time.
+// A matrix, copied 128 bytes of `box_rows` rows at a time.
 bool make_map(CUtensorMap *m, const void *base, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, int box_rows)
 {
     const EncodeFn fn = encoder();
     if (!fn) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, step[2] = {1, 1};
-    return fn(m, dtype == SO_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(base), dims, strides,
-              box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const int size = elem_size(dtype);
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(stride * size)};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / size), (cuuint32_t)box_rows}, step[2] = {1, 1};
+    return fn(m, type_of(dtype), 2, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The same as groups of 64 columns (the stride is a multiple of 64), 64 rows of two groups at a time.
+// One of 16-bit elements as groups of 64 columns (the stride is a multiple of 64), 64 rows of two groups at a time.
 bool make_group_map(CUtensorMap *m, const void *base, int32_t dtype, int64_t rows, int64_t cols, int64_t stride)
 {
     const EncodeFn fn = encoder();
     if (!fn) return false;
     const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(cols + 63) / 64}, strides[2] = {(cuuint64_t)stride * 2, 128};
     const cuuint32_t box[3] = {64, kTileK, 2}, step[3] = {1, 1, 1};
-    return fn(m, dtype == SO_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides,
-              box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(m, type_of(dtype), 3, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename T, int kMode, int kCtas>
-so_status launch_product(const CUtensorMap &a, const CUtensorMap &b, const Product &p, int units, cudaStream_t st)
+so_status launch_product(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const Product &p, int units, cudaStream_t st)
 {
     static std::atomic<bool> ready[kMaxDevices];
     int dev = -1;
@@ -1130,7 +1228,7 @@ so_status launch_product(const CUtensorMap &a, const CUtensorMap &b, const Produ
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a, b, p) == cudaSuccess ? SO_OK : SO_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kernel, a, b, out, p) == cudaSuccess ? SO_OK : SO_ERR_CUDA;
 }
 
 struct Call {
@@ -1162,7 +1260,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     r.dhidden_vectors = aligned(c.dhidden, 16) && c.cols % 8 == 0 && (c.rows <= 1 || c.dhidden_stride % 8 == 0);
     r.counts = c.rows > kChunk ? reinterpret_cast<float2 *>(scratch + l.counts) : nullptr;
     if (r.counts) SO_TRY(launch(count_kernel, (unsigned)((c.rows + kChunk - 1) / kChunk), kGatherThreads, 0, st, false, r));
-    SO_TRY(launch(gather_kernel, (unsigned)(c.rows > 0 ? (c.rows + kGatherRows - 1) / kGatherRows : 1), kGatherThreads, 0, st, r.counts != nullptr, r));
+    SO_TRY(launch(gather_kernel, (unsigned)((c.rows + kGatherRows - 1) / kGatherRows + kTileK / kGatherRows), kGatherThreads, 0, st, r.counts != nullptr, r));
 
     Product p = {};
     p.control = control, p.vocab = c.vocab, p.cols = c.cols, p.rows_pad = (int32_t)l.rows_pad, p.splits = (int32_t)l.splits, p.planes = (int32_t)l.planes;
@@ -1202,12 +1300,12 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
             if (!table_maps(width)) return SO_ERR_CUDA;
             Product q = p;
             q.first = first, q.width = width, q.table_row = 0;
-            SO_TRY((launch_product<T, kStats, kCtas>(hidden_k, table_k, q, units, st)));
+            SO_TRY((launch_product<T, kStats, kCtas>(hidden_k, table_k, hidden_k, q, units, st)));
         }
     } else {
         if (!table_maps(c.vocab)) return SO_ERR_CUDA;
         p.width = c.vocab;
-        SO_TRY((launch_product<T, kStats, kCtas>(hidden_k, table_k, p, units, st)));
+        SO_TRY((launch_product<T, kStats, kCtas>(hidden_k, table_k, hidden_k, p, units, st)));
     }
     Join j = {control, p.stats, p.label_logit, w, index, lse2, coef, c.row_loss, c.loss, reinterpret_cast<double *>(scratch + l.sums), (int32_t)l.rows_pad, (int32_t)l.halves, c.rows};
     SO_TRY(launch(join_kernel, (unsigned)(l.rows_pad / 32), 32 * kJoinWarps, 0, st, true, j));
@@ -1215,6 +1313,14 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
         if (!make_map(&prob_k, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, kRowsOfCta) ||
             !make_group_map(&prob_m, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece))
             return SO_ERR_CUDA;
+        // what a warp copies out: 32 rows
+        CUtensorMap prob_out = prob_k, part_out = prob_k, grad_out = prob_k;
+        if (!make_map(&prob_out, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, 32) ||
+            !make_map(&part_out, p.part, SO_DTYPE_FP32, l.rows_pad * l.splits, l.part_stride, l.part_stride, 32))
+            return SO_ERR_CUDA;
+        const int grad_size = elem_size(c.grad_dtype);
+        p.grad_boxes = c.dtable && !c.accumulate && aligned(c.dtable, 16) && c.dtable_stride * grad_size % 16 == 0;
+        if (p.grad_boxes && !make_map(&grad_out, c.dtable, c.grad_dtype, c.vocab, c.cols, c.dtable_stride, 32)) return SO_ERR_CUDA;
         for (int64_t first = 0; first < c.vocab; first += l.piece) {
             Product q = p;
             q.first = q.table_row = first;
@@ -1226,9 +1332,9 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
                 q.table_row = 0;
             }
             if (l.keep) SO_TRY(launch(prob_kernel<T>, (unsigned)(8 * sms), 256, 0, st, true, q));
-            else SO_TRY((launch_product<T, kProb, kCtas>(hidden_k, table_k, q, units, st)));
-            if (c.dhidden) SO_TRY((launch_product<T, kHidden, kCtas>(prob_k, table_m, q, units, st)));
-            if (c.dtable) SO_TRY((launch_product<T, kTable, kCtas>(prob_m, hidden_m, q, units, st)));
+            else SO_TRY((launch_product<T, kProb, kCtas>(hidden_k, table_k, prob_out, q, units, st)));
+            if (c.dhidden) SO_TRY((launch_product<T, kHidden, kCtas>(prob_k, table_m, part_out, q, units, st)));
+            if (c.dtable) SO_TRY((launch_product<T, kTable, kCtas>(prob_m, hidden_m, grad_out, q, units, st)));
         }
     }
     if (!gradients) return SO_OK;
