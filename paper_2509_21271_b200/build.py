@@ -14,7 +14,7 @@ SOURCES = [os.path.join(CSRC, "superoffload.cu"), os.path.join(CSRC, "so_static_
            os.path.join(CSRC, "so_norm.cu"), os.path.join(CSRC, "so_embedding.cu"),
            os.path.join(CSRC, "so_logits_loss.cu"), os.path.join(CSRC, "so_tensor_adamw.cu"),
            os.path.join(CSRC, "so_residual_norm.cu"), os.path.join(CSRC, "so_linear_loss.cu")]
-_DEPS = SOURCES + [os.path.join(CSRC, "so_ops.cuh"), os.path.join(CSRC, "so_kernels.cuh"), os.path.join(CSRC, "so_step_tma.cuh"), os.path.join(CSRC, "so_types.h"), os.path.join(CSRC, "so_pack.cuh"),
+_DEPS = SOURCES + [os.path.join(CSRC, "so_ops.cuh"), os.path.join(CSRC, "so_rows.cuh"), os.path.join(CSRC, "so_kernels.cuh"), os.path.join(CSRC, "so_step_tma.cuh"), os.path.join(CSRC, "so_types.h"), os.path.join(CSRC, "so_pack.cuh"),
                    os.path.join(INCLUDE, "superoffload.h")]
 
 

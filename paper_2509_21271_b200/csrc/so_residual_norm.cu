@@ -12,7 +12,7 @@
 //             S1 = sum t bhat, S2 = sum t   over the rows of a gate's group
 //             dgate = pw S1 + pb S2,  dpw = sum over groups of gate S1,  dpb = .. gate S2
 //             dw = sum dy hat,  db = sum dy
-#include "so_ops.cuh"
+#include "so_rows.cuh"
 
 using namespace so_ops;
 
@@ -28,6 +28,9 @@ struct Args {
     int64_t rows, cols, group_rows;       // rows that share a gate
     int32_t param_dtype, post;
     float scale, eps, inv_cols;
+    int64_t each;                         // consecutive rows of a group of threads (or of a part of the column sums)
+    float *partials;                      // backward: [groups of threads + gates - 1][4][cols]
+    Patience patience;
 };
 
 // E elements of a row from element c
@@ -45,7 +48,7 @@ __device__ __forceinline__ void store_row(void *p, int64_t at, const float (&f)[
 }
 // E parameters (`fill` where there are none); aligned like the rows
 template <int E>
-__device__ __forceinline__ void load_params(const void *p, int64_t at, int32_t dtype, float fill, float (&f)[E])
+__device__ __forceinline__ void params_at(const void *p, int64_t at, int32_t dtype, float fill, float (&f)[E])
 {
     if (!p) {
 #pragma unroll
@@ -117,11 +120,11 @@ __global__ void __launch_bounds__(kLoopThreads) forward_loop_kernel(const __grid
             float u[E], r[E], g[E];
             load_row<T, E>(block, c, u);
             load_row<T, E>(x, c, r);
-            load_params<E>(a.gate, gate + c, a.param_dtype, 1.0f, g);
+            params_at<E>(a.gate, gate + c, a.param_dtype, 1.0f, g);
             if (a.post) {
                 float pw[E], pb[E];
-                load_params<E>(a.pw, c, a.param_dtype, 1.0f, pw);
-                load_params<E>(a.pb, c, a.param_dtype, 0.0f, pb);
+                params_at<E>(a.pw, c, a.param_dtype, 1.0f, pw);
+                params_at<E>(a.pb, c, a.param_dtype, 0.0f, pb);
 #pragma unroll
                 for (int i = 0; i < E; ++i) u[i] = fmaf((u[i] - pmean) * prstd, pw[i], pb[i]);
             }
@@ -147,8 +150,8 @@ __global__ void __launch_bounds__(kLoopThreads) forward_loop_kernel(const __grid
         for (int64_t c = threadIdx.x * E; c < a.cols; c += kLoopThreads * E) {
             float f[E], w[E], b[E];
             load_row<T, E>(h, c, f);
-            load_params<E>(a.w, c, a.param_dtype, 1.0f, w);
-            load_params<E>(a.b, c, a.param_dtype, 0.0f, b);
+            params_at<E>(a.w, c, a.param_dtype, 1.0f, w);
+            params_at<E>(a.b, c, a.param_dtype, 0.0f, b);
 #pragma unroll
             for (int i = 0; i < E; ++i) f[i] = fmaf((f[i] - mean) * rstd, w[i], b[i]);
             store_row<T, E>(y, c, f);
@@ -177,7 +180,7 @@ __device__ __forceinline__ void total_gradient(const Args &a, int64_t row, int64
     float dy[E], h[E], w[E];
     load_row<T, E>(a.dy, row * a.dy_stride + c, dy);
     load_row<T, E>(a.hin, row * a.h_stride + c, h);
-    load_params<E>(a.w, c, a.param_dtype, 1.0f, w);
+    params_at<E>(a.w, c, a.param_dtype, 1.0f, w);
     if (a.dh) load_row<T, E>(a.dh, row * a.dh_stride + c, t);
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -198,7 +201,7 @@ __global__ void __launch_bounds__(kLoopThreads) backward_loop_kernel(const __gri
             float dy[E], h[E], w[E];
             load_row<T, E>(a.dy, row * a.dy_stride + c, dy);
             load_row<T, E>(a.hin, row * a.h_stride + c, h);
-            load_params<E>(a.w, c, a.param_dtype, 1.0f, w);
+            params_at<E>(a.w, c, a.param_dtype, 1.0f, w);
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 const float e = dy[i] * w[i];
@@ -219,8 +222,8 @@ __global__ void __launch_bounds__(kLoopThreads) backward_loop_kernel(const __gri
                 float t[E], u[E], g[E], pw[E];
                 total_gradient<T, E>(a, row, c, s, me, meh, t);
                 load_row<T, E>(a.block, row * a.block_stride + c, u);
-                load_params<E>(a.gate, gate + c, a.param_dtype, 1.0f, g);
-                load_params<E>(a.pw, c, a.param_dtype, 1.0f, pw);
+                params_at<E>(a.gate, gate + c, a.param_dtype, 1.0f, g);
+                params_at<E>(a.pw, c, a.param_dtype, 1.0f, pw);
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
                     const float q = t[i] * g[i] * pw[i];
@@ -235,11 +238,11 @@ __global__ void __launch_bounds__(kLoopThreads) backward_loop_kernel(const __gri
         for (int64_t c = threadIdx.x * E; c < a.cols; c += kLoopThreads * E) {
             float t[E], d[E], g[E];
             total_gradient<T, E>(a, row, c, s, me, meh, t);
-            load_params<E>(a.gate, gate + c, a.param_dtype, 1.0f, g);
+            params_at<E>(a.gate, gate + c, a.param_dtype, 1.0f, g);
             if (a.post) {
                 float u[E], pw[E];
                 load_row<T, E>(a.block, row * a.block_stride + c, u);
-                load_params<E>(a.pw, c, a.param_dtype, 1.0f, pw);
+                params_at<E>(a.pw, c, a.param_dtype, 1.0f, pw);
 #pragma unroll
                 for (int i = 0; i < E; ++i)
                     d[i] = s.prstd * (fmaf(t[i] * g[i], pw[i], -mq) - (u[i] - s.pmean) * s.prstd * mqb);
@@ -256,56 +259,499 @@ __global__ void __launch_bounds__(kLoopThreads) backward_loop_kernel(const __gri
     }
 }
 
-// Column sums of the rows of a part: S1, S2, sum dy hat, sum dy, each thread E columns.
-// Parts never cross from one gate's rows to the next's.
-template <typename T, int E>
-__global__ void __launch_bounds__(kLoopThreads) columns_kernel(const __grid_constant__ Args a, float *partials, int parts_per_group, bool gates)
+
+// ---- aligned rows through a ring of bulk copies ----------------------------------------
+//
+// A group of threads, a warp or several, takes consecutive rows: a thread holds its columns'
+// parameters in registers for all of them (the gate's until the next one's rows begin), the
+// rows come through a ring of bulk copies in shared memory.  A row is read from there once for
+// each of its two norms, whose sums the group exchanges; the second exchange also tells the
+// group's first thread that everyone is done with the row's place, which it refills.
+//
+// A copy that does not arrive in time turns the rows that the group has not written into NaN,
+// statistics and gradients of parameters included.
+
+constexpr int kRingBars = 64;             // groups x stages of a block, at most
+constexpr int kMaxWarps = 16;             // of a group
+
+struct RingShared {
+    uint64_t full[kRingBars];
+    float2 part[2][kMaxWarps];            // of each exchange of a row
+    float count[kMaxWarps];               // elements of a warp
+    int gave_up[8], issued[8];
+};
+
+// One row in `kNV` vectors a thread
+template <typename T, int E, int kNV>
+struct Columns {
+    const Group &g;
+    int cols;
+    float mine, warp_n;                   // elements of this thread, of its warp
+    __device__ Columns(const Group &g_, int cols_) : g(g_), cols(cols_)
+    {
+        mine = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (has(i)) mine += E;
+        warp_n = warp_sum(mine);
+    }
+    __device__ __forceinline__ int at(int i) const { return (g.thread + i * g.threads) * E; }
+    __device__ __forceinline__ bool has(int i) const { return at(i) < cols; }
+};
+
+__device__ __forceinline__ float2 warp_sum2(float a, float b)
 {
-    const int64_t c = ((int64_t)blockIdx.x * kLoopThreads + threadIdx.x) * E;
-    const int64_t part = blockIdx.y, group = part / parts_per_group;
-    const int64_t each = (a.group_rows + parts_per_group - 1) / parts_per_group;
-    int64_t row = part % parts_per_group * each, end = row + each;
-    if (end > a.group_rows) end = a.group_rows;
-    row += group * a.group_rows;
-    end += group * a.group_rows;
-    if (end > a.rows) end = a.rows;
-    if (c >= a.cols) return;
-    float s1[E] = {}, s2[E] = {}, t1[E] = {}, t2[E] = {};
-    for (; row < end; ++row) {
-        const RowStats s = row_stats(a, row);
-        float dy[E], h[E];
-        load_row<T, E>(a.dy, row * a.dy_stride + c, dy);
-        load_row<T, E>(a.hin, row * a.h_stride + c, h);
+    float v[2] = {a, b};
+    const float one = warp_sum_many<2>(v);                   // lanes 0 to 15: the first, the others: the second
+    return make_float2(__shfl_sync(0xFFFFFFFFu, one, 0), __shfl_sync(0xFFFFFFFFu, one, 16));
+}
+
+// Sums of two values over the group, known to all of it.
+__device__ __forceinline__ float2 group_sum2(const Group &g, float2 (*part), float a, float b)
+{
+    float2 r = warp_sum2(a, b);
+    if (g.warps == 1) {
+        __syncwarp();
+        return r;
+    }
+    if ((threadIdx.x & 31) == 0) part[g.warp] = r;
+    g.sync();
+    r = make_float2(0.0f, 0.0f);
+    for (int i = 0; i < g.warps; ++i) {
+        const float2 o = part[i];
+        r.x += o.x;
+        r.y += o.y;
+    }
+    return r;
+}
+__device__ __forceinline__ float group_sum(const Group &g, float2 (*part), float a)
+{
+    a = warp_sum(a);
+    if (g.warps == 1) {
+        __syncwarp();
+        return a;
+    }
+    if ((threadIdx.x & 31) == 0) part[g.warp].x = a;
+    g.sync();
+    a = 0.0f;
+    for (int i = 0; i < g.warps; ++i) a += part[i].x;
+    return a;
+}
+
+// Mean (0 with the RMS norm) and 1 / sqrt(variance + eps) of a row.  Layer norm in one exchange:
+// a warp has the mean of its first lane's elements as its centre c, and with n_t, m_t, Q_t each
+// thread's number, mean and squares around that mean,
+//   D = sum n_t (m_t - c),  Q = sum (Q_t + n_t (m_t - c)^2),
+// so that its mean is c + D / n, and its squares around that Q - D^2 / n; warps are joined by
+// M2 = sum (M2_w + n_w (mean_w - mean)^2).
+template <bool kLayer, typename T, int E, int kNV>
+__device__ __forceinline__ float2 row_statistics(const Columns<T, E, kNV> &c, const Group &g, float2 (*part), const float *count, const Vals<E> (&f)[kNV],
+                                                 float inv_cols, float eps)
+{
+    Vals<E> acc;
+    acc.set(0.0f);
+    if constexpr (!kLayer) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            t1[i] = fmaf(dy[i], (h[i] - s.mean) * s.rstd, t1[i]);
-            t2[i] += dy[i];
-        }
-        if (gates) {
-            float t[E], u[E];
-            total_gradient<T, E>(a, row, c, s, a.moments[row], a.moments[a.rows + row], t);
-            load_row<T, E>(a.block, row * a.block_stride + c, u);
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) acc = fma(f[i], f[i], acc);
+        const float sq = group_sum(g, part, total(acc));
+        return make_float2(0.0f, 1.0f / sqrtf(sq * inv_cols + eps));
+    } else {
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                s1[i] = fmaf(t[i], (u[i] - s.pmean) * s.prstd, s1[i]);
-                s2[i] += t[i];
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) acc = acc + f[i];
+        const float m = c.mine > 0.0f ? total(acc) / c.mine : 0.0f;
+        acc.set(0.0f);
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                const Vals<E> d = f[i] + -m;
+                acc = fma(d, d, acc);
             }
+        const float centre = __shfl_sync(0xFFFFFFFFu, m, 0), d = c.mine > 0.0f ? m - centre : 0.0f;
+        const float2 s = warp_sum2(d * c.mine, fmaf(d * c.mine, d, total(acc)));
+        float2 r = make_float2(centre + s.x / c.warp_n, s.y - s.x * s.x / c.warp_n);
+        if (g.warps == 1) {
+            __syncwarp();
+        } else {
+            if ((threadIdx.x & 31) == 0) part[g.warp] = r;
+            g.sync();
+            float mean = 0.0f, m2 = 0.0f;
+            for (int i = 0; i < g.warps; ++i) mean = fmaf(part[i].x, count[i], mean);
+            mean *= inv_cols;
+            for (int i = 0; i < g.warps; ++i) m2 += fmaf((part[i].x - mean) * count[i], part[i].x - mean, part[i].y);
+            r = make_float2(mean, m2);
+        }
+        return make_float2(r.x, 1.0f / sqrtf(r.y * inv_cols + eps));
+    }
+}
+
+// What the two kernels share: the ring of `kMats` rows a stage, and who waits for what.
+template <int kMats>
+struct Ring {
+    const Group &g;
+    RingShared &s;
+    uint32_t base, bars, row_bytes, stage_bytes;
+    int stages, stage, turn;
+    uint32_t phase, polls;
+    __device__ Ring(const Group &g_, RingShared &s_, uint8_t *room, uint32_t row_bytes_, int stages_, uint32_t polls_)
+        : g(g_), s(s_), row_bytes(row_bytes_), stages(stages_), stage(0), turn(1), phase(0), polls(polls_)
+    {
+        stage_bytes = row_bytes * kMats;
+        base = smem_addr(room) + (uint32_t)(g.index * stages) * stage_bytes;
+        bars = smem_addr(s.full) + (uint32_t)(g.index * stages) * 8;
+        if (threadIdx.x < (unsigned)(g.per_block * stages)) {
+            mbar_init(smem_addr(s.full + threadIdx.x), 1);
+            mbar_init_fence();            // before any group's first thread issues a copy
+        }
+        if (g.thread == 0) {
+            s.gave_up[g.index] = polls == 0;
+            s.issued[g.index] = 0;
         }
     }
-    float *out = partials + part * 4 * a.cols + c;
+    // by the group's first thread: row copies into stage `at`
+    __device__ __forceinline__ void fill(int at, const char *const (&src)[kMats]) const
+    {
+        uint32_t n = 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        out[i] = s1[i];
-        out[a.cols + i] = s2[i];
-        out[2 * a.cols + i] = t1[i];
-        out[3 * a.cols + i] = t2[i];
+        for (int k = 0; k < kMats; ++k) n += src[k] ? row_bytes : 0;
+        mbar_expect(bars + at * 8, n);
+#pragma unroll
+        for (int k = 0; k < kMats; ++k)
+            if (src[k]) bulk_load(base + at * stage_bytes + k * row_bytes, src[k], row_bytes, bars + at * 8);
+        ++s.issued[g.index];
+    }
+    // The turn (from 1 on) whose wait ran out is in shared memory; a thread that is a turn behind the
+    // one that ran out goes by the number, so that all of the group stop at the same row.
+    __device__ __forceinline__ bool gave_up() const
+    {
+        const int at = *const_cast<const volatile int *>(&s.gave_up[g.index]);
+        return at != 0 && at <= turn;
+    }
+    __device__ __forceinline__ void wait() const
+    {
+        if (!mbar_test(bars + stage * 8, phase) && !gave_up() && !mbar_wait(bars + stage * 8, phase, polls))
+            *const_cast<volatile int *>(&s.gave_up[g.index]) = turn;
+    }
+    __device__ __forceinline__ uint32_t row(int k) const { return base + stage * stage_bytes + k * row_bytes; }
+    __device__ __forceinline__ void next()
+    {
+        ++turn;
+        if (++stage == stages) stage = 0, phase ^= 1;
+    }
+};
+
+// Bound: memory (two reads, two writes).
+template <typename T, bool kLayer, int kNV, int kMaxThreads>
+__global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forward_ring_kernel(const __grid_constant__ Args a, int per_row, int stages)
+{
+    constexpr int E = Vec<T>::kElems;
+    extern __shared__ __align__(128) uint8_t s_room[];
+    __shared__ __align__(8) RingShared s;
+    const Group g(per_row);
+    Ring<2> ring(g, s, s_room, (uint32_t)a.cols * sizeof(T), stages, a.patience.of((int)blockIdx.x));
+    const Columns<T, E, kNV> c(g, (int)a.cols);
+    if ((threadIdx.x & 31) == 0) s.count[threadIdx.x >> 5] = c.warp_n;
+    __syncthreads();
+    float2 (*part)[kMaxWarps] = s.part;
+    const int w0 = g.index * g.warps;     // the group's first warp
+    const float *count = s.count + w0;
+    int64_t row = ((int64_t)blockIdx.x * g.per_block + g.index) * a.each, end = row + a.each;
+    if (end > a.rows) end = a.rows;
+    const auto fill = [&](int at, int64_t r) {
+        const char *const src[2] = {reinterpret_cast<const char *>(static_cast<const T *>(a.x) + r * a.x_stride),
+                                    reinterpret_cast<const char *>(static_cast<const T *>(a.block) + r * a.block_stride)};
+        ring.fill(at, src);
+    };
+    if (g.thread == 0)
+        for (int n = 0; n < stages && row + n < end; ++n) fill(n, row + n);
+    Vals<E> w[kNV], b[kNV], gw[kNV], gb[kNV];                // gw, gb: gate times the first norm's
+#pragma unroll
+    for (int i = 0; i < kNV; ++i)
+        if (c.has(i)) {
+            w[i] = load_params<E>(a.w, c.at(i), a.param_dtype, 1.0f);
+            if (kLayer || a.b) b[i] = load_params<E>(a.b, c.at(i), a.param_dtype, 0.0f);
+        }
+    int64_t gate_end = 0;
+    for (; row < end; ++row) {
+        if (row >= gate_end) {
+            const int64_t gate = row / a.group_rows;
+            gate_end = (gate + 1) * a.group_rows;
+#pragma unroll
+            for (int i = 0; i < kNV; ++i)
+                if (c.has(i)) {
+                    gw[i] = a.gate ? load_params<E>(static_cast<const char *>(a.gate) + gate * a.cols * (a.param_dtype == SO_DTYPE_FP32 ? 4 : 2), c.at(i), a.param_dtype, 1.0f)
+                                   : spread<E>(1.0f);
+                    gb[i] = a.pb ? gw[i] * load_params<E>(a.pb, c.at(i), a.param_dtype, 0.0f) : spread<E>(0.0f);
+                    if (a.pw) gw[i] = gw[i] * load_params<E>(a.pw, c.at(i), a.param_dtype, 1.0f);
+                }
+        }
+        ring.wait();
+        float2 post = make_float2(0.0f, 1.0f);
+        Vals<E> f[kNV];
+        if (a.post) {
+#pragma unroll
+            for (int i = 0; i < kNV; ++i)
+                if (c.has(i)) f[i] = from_shared<T, E>(ring.row(1) + c.at(i) * sizeof(T));
+            post = row_statistics<kLayer>(c, g, part[0] + w0, count, f, a.inv_cols, a.eps);
+        }
+        T *h = static_cast<T *>(a.h) + row * a.h_stride, *y = static_cast<T *>(a.y) + row * a.y_stride;
+        const float shift = -post.x * post.y;
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                const Vals<E> u = from_shared<T, E>(ring.row(1) + c.at(i) * sizeof(T)), x = from_shared<T, E>(ring.row(0) + c.at(i) * sizeof(T));
+                // in fp32 the mean is taken off first: rows far from zero keep their digits
+                const Vals<E> hat = !kLayer ? u * post.y : sizeof(T) == 4 ? (u + -post.x) * post.y : fma(u, post.y, shift);
+                const uint4 bits = narrow16<T>(fma(gw[i], hat, fma(x, a.scale, gb[i])));
+                *reinterpret_cast<uint4 *>(h + c.at(i)) = bits;
+                f[i] = widen16<T>(bits);
+            }
+        const float2 st = row_statistics<kLayer>(c, g, part[1] + w0, count, f, a.inv_cols, a.eps);
+        if (ring.gave_up()) break;
+        if (g.thread == 0 && row + stages < end) fill(ring.stage, row + stages);
+        const float back = -st.x * st.y;
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                const Vals<E> hat = !kLayer ? f[i] * st.y : sizeof(T) == 4 ? (f[i] + -st.x) * st.y : fma(f[i], st.y, back);
+                *reinterpret_cast<uint4 *>(y + c.at(i)) = narrow16<T>(kLayer || a.b ? fma(hat, w[i], b[i]) : hat * w[i]);
+            }
+        if (a.stats && g.thread == 0) {
+            a.stats[row] = post.x;
+            a.stats[a.rows + row] = post.y;
+            a.stats[2 * a.rows + row] = st.x;
+            a.stats[3 * a.rows + row] = st.y;
+        }
+        ring.next();
+    }
+    if (row >= end) return;
+    if (g.thread == 0) land(ring.bars, s.issued[g.index], stages);
+    const uint4 nan = narrow16<T>(spread<E>(kNan));
+    for (; row < end; ++row) {
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                *reinterpret_cast<uint4 *>(static_cast<T *>(a.h) + row * a.h_stride + c.at(i)) = nan;
+                *reinterpret_cast<uint4 *>(static_cast<T *>(a.y) + row * a.y_stride + c.at(i)) = nan;
+            }
+        if (a.stats && g.thread == 0)
+            for (int k = 0; k < 4; ++k) a.stats[k * a.rows + row] = kNan;
+    }
+}
+
+// kSums: the thread keeps its columns' S1, S2, sum dy hat and sum dy, and leaves them as a part
+// of its own where a gate's rows or its own end: part t + i for the t-th group of threads in the
+// rows of gate i.  Without kSums the rows' means are left for the sums to be taken from.
+//
+// Bound: memory (four reads, two writes).
+template <typename T, bool kLayer, bool kSums, int kNV, int kMaxThreads>
+__global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backward_ring_kernel(const __grid_constant__ Args a, int per_row, int stages)
+{
+    constexpr int E = Vec<T>::kElems;
+    extern __shared__ __align__(128) uint8_t s_room[];
+    __shared__ __align__(8) RingShared s;
+    const Group g(per_row);
+    Ring<4> ring(g, s, s_room, (uint32_t)a.cols * sizeof(T), stages, a.patience.of((int)blockIdx.x));
+    const Columns<T, E, kNV> c(g, (int)a.cols);
+    __syncthreads();
+    float2 (*part)[kMaxWarps] = s.part;
+    const int w0 = g.index * g.warps;
+    const int64_t me = (int64_t)blockIdx.x * g.per_block + g.index;
+    int64_t row = me * a.each, end = row + a.each;
+    if (end > a.rows) end = a.rows;
+    const auto fill = [&](int at, int64_t r) {
+        const char *const src[4] = {reinterpret_cast<const char *>(static_cast<const T *>(a.dy) + r * a.dy_stride),
+                                    reinterpret_cast<const char *>(static_cast<const T *>(a.hin) + r * a.h_stride),
+                                    a.dh ? reinterpret_cast<const char *>(static_cast<const T *>(a.dh) + r * a.dh_stride) : nullptr,
+                                    a.block ? reinterpret_cast<const char *>(static_cast<const T *>(a.block) + r * a.block_stride) : nullptr};
+        ring.fill(at, src);
+    };
+    if (g.thread == 0)
+        for (int n = 0; n < stages && row + n < end; ++n) fill(n, row + n);
+    Vals<E> w[kNV], gw[kNV], s1[kNV], s2[kNV], t1[kNV], t2[kNV];   // gw: gate times the first norm's weight
+#pragma unroll
+    for (int i = 0; i < kNV; ++i) {
+        if (c.has(i)) w[i] = load_params<E>(a.w, c.at(i), a.param_dtype, 1.0f);
+        if (kSums) s1[i].set(0.0f), s2[i].set(0.0f), t1[i].set(0.0f), t2[i].set(0.0f);
+    }
+    const auto leave = [&](int64_t gate) {
+        float *out = a.partials + (me + gate) * 4 * a.cols;
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                Vals<E> *const v[4] = {&s1[i], &s2[i], &t1[i], &t2[i]};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float f[E];
+                    v[k]->get(f);
+#pragma unroll
+                    for (int j = 0; j < E; j += 4)
+                        *reinterpret_cast<float4 *>(out + k * a.cols + c.at(i) + j) = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+                    v[k]->set(0.0f);
+                }
+            }
+    };
+    int64_t gate_end = 0, gate = 0;
+    bool lost = false;
+    for (; row < end; ++row) {
+        if (row >= gate_end) {
+            if (kSums && gate_end > 0) leave(gate);
+            gate = row / a.group_rows;
+            gate_end = (gate + 1) * a.group_rows;
+#pragma unroll
+            for (int i = 0; i < kNV; ++i)
+                if (c.has(i)) {
+                    gw[i] = a.gate ? load_params<E>(static_cast<const char *>(a.gate) + gate * a.cols * (a.param_dtype == SO_DTYPE_FP32 ? 4 : 2), c.at(i), a.param_dtype, 1.0f)
+                                   : spread<E>(1.0f);
+                    if (a.pw) gw[i] = gw[i] * load_params<E>(a.pw, c.at(i), a.param_dtype, 1.0f);
+                }
+        }
+        const RowStats st = row_stats(a, row);
+        ring.wait();
+        const auto from = [&](int k, int i) { return from_shared<T, E>(ring.row(k) + c.at(i) * sizeof(T)); };
+        const auto norm = [&](const Vals<E> &v, float mean, float rstd) {
+            return !kLayer ? v * rstd : sizeof(T) == 4 ? (v + -mean) * rstd : fma(v, rstd, -mean * rstd);
+        };
+        Vals<E> sum, dot;
+        sum.set(0.0f), dot.set(0.0f);
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                const Vals<E> dy = from(0, i), hat = norm(from(1, i), st.mean, st.rstd), e = dy * w[i];
+                if (kLayer) sum = sum + e;
+                dot = fma(e, hat, dot);
+                if (kSums) t1[i] = fma(dy, hat, t1[i]), t2[i] = t2[i] + dy;
+            }
+        float me_ = 0.0f, meh;
+        if (kLayer) {
+            const float2 r = group_sum2(g, part[0] + w0, total(sum), total(dot));
+            me_ = r.x * a.inv_cols, meh = r.y * a.inv_cols;
+        } else {
+            meh = group_sum(g, part[0] + w0, total(dot)) * a.inv_cols;
+        }
+        if (!kSums && a.moments && g.thread == 0) {
+            a.moments[row] = me_;
+            a.moments[a.rows + row] = meh;
+        }
+        // t = dh + rstd (e - me) - rstd meh hat
+        const float c0 = -st.rstd * me_, c1 = -st.rstd * meh;
+        Vals<E> t[kNV];
+        sum.set(0.0f), dot.set(0.0f);
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                const Vals<E> hat = norm(from(1, i), st.mean, st.rstd);
+                t[i] = fma(hat, c1, fma(from(0, i) * w[i], st.rstd, c0));
+                if (a.dh) t[i] = t[i] + from(2, i);
+                if (a.post || kSums) {
+                    const Vals<E> bhat = norm(from(3, i), st.pmean, st.prstd), q = t[i] * gw[i];
+                    if (kLayer) sum = sum + q;
+                    dot = fma(q, bhat, dot);
+                    if (kSums) s1[i] = fma(t[i], bhat, s1[i]), s2[i] = s2[i] + t[i];
+                }
+            }
+        float mq = 0.0f, mqb = 0.0f;
+        // without a first norm the exchange has nothing to tell but that everyone is done with phase 1
+        if (kLayer) {
+            const float2 r = group_sum2(g, part[1] + w0, total(sum), total(dot));
+            mq = r.x * a.inv_cols, mqb = r.y * a.inv_cols;
+        } else {
+            mqb = group_sum(g, part[1] + w0, total(dot)) * a.inv_cols;
+        }
+        if (ring.gave_up()) {
+            lost = true;
+            break;
+        }
+        T *dx = static_cast<T *>(a.dx) + row * a.dx_stride, *dblock = static_cast<T *>(a.dblock) + row * a.dblock_stride;
+        const float c2 = -st.prstd * mq, c3 = -st.prstd * mqb;
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                *reinterpret_cast<uint4 *>(dx + c.at(i)) = narrow16<T>(t[i] * a.scale);
+                Vals<E> d = t[i] * gw[i];
+                if (a.post) d = fma(norm(from(3, i), st.pmean, st.prstd), c3, fma(d, st.prstd, c2));
+                *reinterpret_cast<uint4 *>(dblock + c.at(i)) = narrow16<T>(d);
+            }
+        if (g.warps > 1) g.sync();        // the block's row has been read a last time
+        else __syncwarp();
+        if (g.thread == 0 && row + stages < end) fill(ring.stage, row + stages);
+        ring.next();
+    }
+    if (!lost) {
+        if (kSums && gate_end > 0) leave(gate);
+        return;
+    }
+    if (g.thread == 0) land(ring.bars, s.issued[g.index], stages);
+    if (kSums)
+        for (const int64_t last = (end - 1) / a.group_rows; gate <= last; ++gate) {
+#pragma unroll
+            for (int i = 0; i < kNV; ++i) s1[i].set(kNan), s2[i].set(kNan), t1[i].set(kNan), t2[i].set(kNan);
+            leave(gate);
+        }
+    const uint4 nan = narrow16<T>(spread<E>(kNan));
+    for (; row < end; ++row) {
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                *reinterpret_cast<uint4 *>(static_cast<T *>(a.dx) + row * a.dx_stride + c.at(i)) = nan;
+                *reinterpret_cast<uint4 *>(static_cast<T *>(a.dblock) + row * a.dblock_stride + c.at(i)) = nan;
+            }
+        if (!kSums && a.moments && g.thread == 0) a.moments[row] = a.moments[a.rows + row] = kNan;
+    }
+}
+
+// ---- sums over rows ------------------------------------------------------------------
+
+// Column sums of the rows of a part: S1, S2, sum dy hat, sum dy, each thread E columns.  A part that
+// crosses from one gate's rows to the next's leaves two sums, as above.
+template <typename T, int E>
+__global__ void __launch_bounds__(kLoopThreads) columns_kernel(const __grid_constant__ Args a, bool gates)
+{
+    grid_dependency_wait();
+    const int64_t c = ((int64_t)blockIdx.x * kLoopThreads + threadIdx.x) * E;
+    int64_t row = (int64_t)blockIdx.y * a.each, end = row + a.each;
+    if (end > a.rows) end = a.rows;
+    if (c >= a.cols) return;
+    while (row < end) {
+        const int64_t gate = row / a.group_rows;
+        const int64_t stop = end < (gate + 1) * a.group_rows ? end : (gate + 1) * a.group_rows;
+        float s1[E] = {}, s2[E] = {}, t1[E] = {}, t2[E] = {};
+        for (; row < stop; ++row) {
+            const RowStats s = row_stats(a, row);
+            float dy[E], h[E];
+            load_row<T, E>(a.dy, row * a.dy_stride + c, dy);
+            load_row<T, E>(a.hin, row * a.h_stride + c, h);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                t1[i] = fmaf(dy[i], (h[i] - s.mean) * s.rstd, t1[i]);
+                t2[i] += dy[i];
+            }
+            if (gates) {
+                float t[E], u[E];
+                total_gradient<T, E>(a, row, c, s, a.moments[row], a.moments[a.rows + row], t);
+                load_row<T, E>(a.block, row * a.block_stride + c, u);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    s1[i] = fmaf(t[i], (u[i] - s.pmean) * s.prstd, s1[i]);
+                    s2[i] += t[i];
+                }
+            }
+        }
+        float *out = a.partials + ((int64_t)blockIdx.y + gate) * 4 * a.cols + c;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            out[i] = s1[i];
+            out[a.cols + i] = s2[i];
+            out[2 * a.cols + i] = t1[i];
+            out[3 * a.cols + i] = t2[i];
+        }
     }
 }
 
 struct Grads {
-    const float *partials;
     void *dgate, *dpw, *dpb, *dw, *db;
-    int32_t dtype, accumulate, groups, parts_per_group;
+    int32_t dtype, accumulate, groups;
 };
 
 __device__ __forceinline__ void put(const Grads &g, void *p, int64_t at, float x)
@@ -315,42 +761,59 @@ __device__ __forceinline__ void put(const Grads &g, void *p, int64_t at, float x
     store_any(p, at, g.dtype, x);
 }
 
-// Sums the parts, 32 columns a block and a warp to every eighth part, in a fixed order.
-constexpr int kSumWarps = 8;
+// Sums the parts, 32 columns a block, in a fixed order.  kByGate: a warp to every gate in turn,
+// else all warps to the parts of one gate after the other.
+constexpr int kSumWarps = 16;
+template <bool kByGate>
 __global__ void __launch_bounds__(32 * kSumWarps) sum_kernel(const __grid_constant__ Args a, const __grid_constant__ Grads g)
 {
     __shared__ float s[4][kSumWarps][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
-    const bool in = c < a.cols;
+    const bool in = c < a.cols, gates = g.dgate || g.dpw || g.dpb;
+    const float pw = in && a.pw ? load_any(a.pw, c, a.param_dtype) : 1.0f, pb = in && a.pb ? load_any(a.pb, c, a.param_dtype) : 0.0f;
     float dpw = 0.0f, dpb = 0.0f, dw = 0.0f, db = 0.0f;
     grid_dependency_wait();
-    for (int group = 0; group < g.groups; ++group) {
+    for (int gate = kByGate ? warp : 0; gate < g.groups; gate += kByGate ? kSumWarps : 1) {
         float sum[4] = {};
-        if (in)
-            for (int p = warp; p < g.parts_per_group; p += kSumWarps) {
-                const float *at = g.partials + ((int64_t)group * g.parts_per_group + p) * 4 * a.cols + c;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) sum[k] += at[k * a.cols];
+        if (in && a.rows > 0) {
+            // the parts whose rows reach into this gate's
+            const int64_t first = gate * a.group_rows / a.each, last = ((gate + 1) * a.group_rows - 1) / a.each;
+#pragma unroll 4
+            for (int64_t t = first + (kByGate ? 0 : warp); t <= last; t += kByGate ? 1 : kSumWarps) {
+                const float *at = a.partials + (t + gate) * 4 * a.cols + c;
+                if (gates) sum[0] += at[0], sum[1] += at[a.cols];
+                sum[2] += at[2 * a.cols], sum[3] += at[3 * a.cols];
             }
+        }
+        if (!kByGate) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[k][warp][lane] = sum[k];
-        __syncthreads();
-        if (warp == 0 && in) {
+            for (int k = 0; k < 4; ++k) s[k][warp][lane] = sum[k];
+            __syncthreads();
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 sum[k] = 0.0f;
-                for (int i = 0; i < kSumWarps; ++i) sum[k] += s[k][i][lane];
+                if (warp == 0)
+                    for (int i = 0; i < kSumWarps; ++i) sum[k] += s[k][i][lane];
             }
-            const float gate = a.gate ? load_any(a.gate, group * a.cols + c, a.param_dtype) : 1.0f;
-            const float pw = a.pw ? load_any(a.pw, c, a.param_dtype) : 1.0f, pb = a.pb ? load_any(a.pb, c, a.param_dtype) : 0.0f;
-            put(g, g.dgate, group * a.cols + c, fmaf(pw, sum[0], pb * sum[1]));
-            dpw = fmaf(gate, sum[0], dpw);
-            dpb = fmaf(gate, sum[1], dpb);
+            __syncthreads();
+        }
+        if (in && (kByGate || warp == 0)) {
+            const float weight = a.gate ? load_any(a.gate, gate * a.cols + c, a.param_dtype) : 1.0f;
+            put(g, g.dgate, gate * a.cols + c, fmaf(pw, sum[0], pb * sum[1]));
+            dpw = fmaf(weight, sum[0], dpw);
+            dpb = fmaf(weight, sum[1], dpb);
             dw += sum[2];
             db += sum[3];
         }
+    }
+    if (kByGate) {
+        s[0][warp][lane] = dpw, s[1][warp][lane] = dpb, s[2][warp][lane] = dw, s[3][warp][lane] = db;
         __syncthreads();
+        if (warp == 0) {
+            dpw = dpb = dw = db = 0.0f;
+            for (int i = 0; i < kSumWarps; ++i) dpw += s[0][i][lane], dpb += s[1][i][lane], dw += s[2][i][lane], db += s[3][i][lane];
+        }
     }
     if (warp != 0 || !in) return;
     put(g, g.dpw, c, dpw);
@@ -361,15 +824,13 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_kernel(const __grid_consta
 
 // ---- host ------------------------------------------------------------------------
 
-constexpr int kMaxParts = 1024;           // per gate's rows, at most
-
-// Parts a gate's rows are cut into, by the sizes alone: about 600 over all, of 16 rows at least.
-int parts_of(int64_t rows, int64_t groups)
+// Groups of threads (or parts of the column sums) whose sums there is room for: about 16 MB of them.
+int64_t most_parts(int64_t rows, int64_t cols)
 {
-    const int64_t group_rows = groups > 0 ? rows / groups : 0;
-    int64_t n = (600 + groups - 1) / (groups > 0 ? groups : 1);
-    if (n > (group_rows + 15) / 16) n = (group_rows + 15) / 16;
-    return n < 1 ? 1 : n > kMaxParts ? kMaxParts : (int)n;
+    int64_t n = (int64_t(1) << 24) / (16 * cols);
+    if (n > 1184) n = 1184;
+    if (n < 148) n = 148;
+    return n < rows ? n : rows > 0 ? rows : 1;
 }
 
 bool row_ok(const void *p, int64_t stride, int64_t rows, int64_t cols, int size, bool out)
@@ -398,38 +859,137 @@ so_status common(int64_t rows, int64_t cols, int64_t groups, int32_t dtype, int3
     return SO_OK;
 }
 
-template <typename T>
-so_status forward(const Args &a, bool vec, bool layer, int sms, cudaStream_t st)
+// How a row is dealt out: `per_row` threads with `nv` vectors each, blocks of `block`; 0: by the loop.
+struct Plan { int per_row, nv, block; };
+
+// The choice that leaves the fewest lanes idle, and the most vectors a thread of equals.
+Plan plan_rows(int64_t vectors, int most_nv)
 {
-    constexpr int E = Vec<T>::kElems;
-    const unsigned grid = (unsigned)(a.rows < 8 * sms ? a.rows : 8 * sms);
-    const auto kernel = vec ? (layer ? forward_loop_kernel<T, E, true> : forward_loop_kernel<T, E, false>)
-                            : (layer ? forward_loop_kernel<T, 1, true> : forward_loop_kernel<T, 1, false>);
-    return launch(kernel, grid, kLoopThreads, 0, st, false, a);
+    Plan best = {0, 0, 0};
+    int64_t waste = INT64_MAX;
+    for (int nv = most_nv; nv > 0; --nv) {
+        const int64_t threads = ((vectors + nv - 1) / nv + 31) / 32 * 32, idle = threads * nv - vectors;
+        if (threads > 32 * kMaxWarps || idle >= waste) continue;
+        waste = idle;
+        best = {(int)threads, nv, threads >= 256 ? (int)threads : (int)(256 / threads * threads)};
+    }
+    return best;
 }
 
-template <typename T>
-so_status backward(const Args &a, const Grads &g, bool sums, bool vec, bool layer, int sms, cudaStream_t st)
+constexpr int kRingBytes = 100 * 1024;    // of a block's ring, if two stages fit there
+constexpr int kMostShared = 220 * 1024;
+
+int ring_stages(size_t stage_bytes, int groups)
+{
+    int stages = (int)(kRingBytes / stage_bytes);
+    stages = stages > 4 ? 4 : stages < 2 ? 2 : stages;
+    return stages < kRingBars / groups ? stages : kRingBars / groups;
+}
+
+// Launches a ring kernel on as many groups of threads as the device has room for (at most `most`),
+// each with its share of consecutive rows; a.each is set to it.
+template <typename K>
+so_status launch_ring(K kernel, std::atomic<uint64_t> (&cache)[kMaxDevices], Args &a, const Plan &p, int mats, int size, int64_t most, int sms, cudaStream_t st)
+{
+    const int groups = p.block / p.per_row;
+    const size_t stage = (size_t)a.cols * size * mats * groups;
+    const int stages = ring_stages(stage, groups);
+    const size_t smem = stage * stages;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SO_ERR_CUDA;
+    if (dev < 0 || dev >= kMaxDevices) return SO_ERR_UNSUPPORTED;
+    // resident blocks per SM, asked for again only when block or shared memory change (the key is exact)
+    const uint64_t tag = (uint64_t)smem << 24 | (uint64_t)p.block << 8;
+    uint64_t v = cache[dev].load(std::memory_order_relaxed);
+    if ((v & ~uint64_t(255)) != tag) {
+        int n = 0;
+        if (smem > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) != cudaSuccess) return SO_ERR_CUDA;
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, p.block, smem) != cudaSuccess || n < 1) return SO_ERR_CUDA;
+        v = tag | (uint64_t)(n < 255 ? n : 255);
+        cache[dev].store(v, std::memory_order_relaxed);
+    }
+    int64_t units = (int64_t)(v & 255) * sms * groups;
+    if (units > most) units = most / groups * groups;
+    if (units < groups) units = groups;
+    a.each = (a.rows + units - 1) / units;
+    const int64_t used = (a.rows + a.each - 1) / a.each;
+    return launch(kernel, (unsigned)((used + groups - 1) / groups), p.block, smem, st, false, a, p.per_row, stages);
+}
+
+template <typename T, bool kLayer, int kNV>
+so_status forward_ring(Args &a, const Plan &p, int sms, cudaStream_t st)
+{
+    static std::atomic<uint64_t> cache[2][kMaxDevices];
+    if (p.block <= 256) return launch_ring(forward_ring_kernel<T, kLayer, kNV, 256>, cache[0], a, p, 2, sizeof(T), INT64_MAX, sms, st);
+    return launch_ring(forward_ring_kernel<T, kLayer, kNV, 512>, cache[1], a, p, 2, sizeof(T), INT64_MAX, sms, st);
+}
+
+template <typename T, bool kLayer>
+so_status forward(Args &a, bool vec, int sms, cudaStream_t st)
 {
     constexpr int E = Vec<T>::kElems;
-    so_status s = SO_OK;
+    if (vec && a.cols * (int64_t)sizeof(T) * 2 * 2 <= kMostShared) {
+        const Plan p = plan_rows(a.cols / E, sizeof(T) == 4 ? 4 : 2);
+        if (sizeof(T) == 4 && p.nv == 4) return forward_ring<T, kLayer, sizeof(T) == 4 ? 4 : 1>(a, p, sms, st);
+        if (sizeof(T) == 4 && p.nv == 3) return forward_ring<T, kLayer, sizeof(T) == 4 ? 3 : 1>(a, p, sms, st);
+        if (p.nv == 2) return forward_ring<T, kLayer, 2>(a, p, sms, st);
+        if (p.nv == 1) return forward_ring<T, kLayer, 1>(a, p, sms, st);
+    }
+    const unsigned grid = (unsigned)(a.rows < 8 * sms ? a.rows : 8 * sms);
+    return launch(vec ? forward_loop_kernel<T, E, kLayer> : forward_loop_kernel<T, 1, kLayer>, grid, kLoopThreads, 0, st, false, a);
+}
+
+template <typename T, bool kLayer, bool kSums, int kNV>
+so_status backward_ring(Args &a, const Plan &p, int64_t most, int sms, cudaStream_t st)
+{
+    static std::atomic<uint64_t> cache[2][kMaxDevices];
+    if (p.block <= 256) return launch_ring(backward_ring_kernel<T, kLayer, kSums, kNV, 256>, cache[0], a, p, 4, sizeof(T), most, sms, st);
+    return launch_ring(backward_ring_kernel<T, kLayer, kSums, kNV, 512>, cache[1], a, p, 4, sizeof(T), most, sms, st);
+}
+
+template <typename T, bool kLayer>
+so_status backward(Args &a, const Grads &g, bool sums, bool vec, int sms, cudaStream_t st)
+{
+    constexpr int E = Vec<T>::kElems;
+    const int64_t most = most_parts(a.rows, a.cols);
+    a.each = 1;
+    bool taken = false;                   // the rows' kernel has left the parts of the sums
     if (a.rows > 0) {
-        const unsigned grid = (unsigned)(a.rows < 8 * sms ? a.rows : 8 * sms);
-        const auto kernel = vec ? (layer ? backward_loop_kernel<T, E, true> : backward_loop_kernel<T, E, false>)
-                                : (layer ? backward_loop_kernel<T, 1, true> : backward_loop_kernel<T, 1, false>);
-        s = launch(kernel, grid, kLoopThreads, 0, st, false, a);
+        const bool ring = vec && a.cols * (int64_t)sizeof(T) * 4 * 2 <= kMostShared;
+        const Plan with = ring ? plan_rows(a.cols / E, sizeof(T) == 4 ? 2 : 1) : Plan{0, 0, 0}, without = ring ? plan_rows(a.cols / E, sizeof(T) == 4 ? 4 : 2) : Plan{0, 0, 0};
+        so_status s;
+        if (sums && with.nv) {
+            taken = true;
+            if (sizeof(T) == 4 && with.nv == 2) s = backward_ring<T, kLayer, true, sizeof(T) == 4 ? 2 : 1>(a, with, most, sms, st);
+            else s = backward_ring<T, kLayer, true, 1>(a, with, most, sms, st);
+        } else if (without.nv) {
+            if (sizeof(T) == 4 && without.nv == 4) s = backward_ring<T, kLayer, false, sizeof(T) == 4 ? 4 : 1>(a, without, INT64_MAX, sms, st);
+            else if (sizeof(T) == 4 && without.nv == 3) s = backward_ring<T, kLayer, false, sizeof(T) == 4 ? 3 : 1>(a, without, INT64_MAX, sms, st);
+            else if (without.nv == 2) s = backward_ring<T, kLayer, false, 2>(a, without, INT64_MAX, sms, st);
+            else s = backward_ring<T, kLayer, false, 1>(a, without, INT64_MAX, sms, st);
+        } else {
+            const unsigned grid = (unsigned)(a.rows < 8 * sms ? a.rows : 8 * sms);
+            s = launch(vec ? backward_loop_kernel<T, E, kLayer> : backward_loop_kernel<T, 1, kLayer>, grid, kLoopThreads, 0, st, false, a);
+        }
         if (s != SO_OK || !sums) return s;
     }
     if (!sums) return SO_OK;
-    const bool gates = g.dgate || g.dpw || g.dpb;
-    const int e = vec ? E : 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((a.cols + (int64_t)kLoopThreads * e - 1) / ((int64_t)kLoopThreads * e)), (unsigned)(g.groups * g.parts_per_group));
-    cfg.blockDim = dim3(kLoopThreads);
-    cfg.stream = st;
-    const auto columns = vec ? columns_kernel<T, E> : columns_kernel<T, 1>;
-    if (cudaLaunchKernelEx(&cfg, columns, a, const_cast<float *>(g.partials), g.parts_per_group, gates) != cudaSuccess) return SO_ERR_CUDA;
-    return launch(sum_kernel, (unsigned)((a.cols + 31) / 32), 32 * kSumWarps, 0, st, false, a, g);
+    if (!taken && a.rows > 0) {
+        const bool gates = g.dgate || g.dpw || g.dpb;
+        const int64_t across = (a.cols + (int64_t)kLoopThreads * (vec ? E : 1) - 1) / ((int64_t)kLoopThreads * (vec ? E : 1));
+        // some thousand blocks in all, of 16 rows at least
+        int64_t parts = (4096 + across - 1) / across;
+        if (parts > (a.rows + 15) / 16) parts = (a.rows + 15) / 16;
+        if (parts > most) parts = most;
+        a.each = (a.rows + parts - 1) / parts;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)across, (unsigned)((a.rows + a.each - 1) / a.each));
+        cfg.blockDim = dim3(kLoopThreads);
+        cfg.stream = st;
+        if (cudaLaunchKernelEx(&cfg, vec ? columns_kernel<T, E> : columns_kernel<T, 1>, a, gates) != cudaSuccess) return SO_ERR_CUDA;
+    }
+    const auto kernel = g.groups >= kSumWarps ? sum_kernel<true> : sum_kernel<false>;
+    return launch(kernel, (unsigned)((a.cols + 31) / 32), 32 * kSumWarps, 0, st, true, a, g);
 }
 
 }  // namespace
@@ -459,6 +1019,7 @@ so_status so_residual_norm_forward(const void *x, int64_t x_stride, const void *
     a.x_stride = x_stride, a.block_stride = block_stride, a.h_stride = h_stride, a.y_stride = y_stride;
     a.rows = rows, a.cols = cols, a.group_rows = rows / groups, a.param_dtype = param_dtype, a.post = post;
     a.scale = (float)scale, a.eps = (float)eps, a.inv_cols = 1.0f / (float)cols;
+    a.patience = patience();
     bool vec = cols * size % 16 == 0 && on16(x, x_stride, rows, size) && on16(block, block_stride, rows, size) &&
                on16(h, h_stride, rows, size) && on16(y, y_stride, rows, size);
     if (!params_ok(a, param_dtype, &vec)) return SO_ERR_INVALID_ARG;
@@ -467,16 +1028,16 @@ so_status so_residual_norm_forward(const void *x, int64_t x_stride, const void *
     if (d != SO_OK) return d;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool layer = kind == SO_NORM_LAYER;
-    if (dtype == SO_DTYPE_BF16) return forward<bf16_t>(a, vec, layer, sms, st);
-    if (dtype == SO_DTYPE_FP16) return forward<f16_t>(a, vec, layer, sms, st);
-    return forward<float>(a, vec, layer, sms, st);
+    if (dtype == SO_DTYPE_BF16) return layer ? forward<bf16_t, true>(a, vec, sms, st) : forward<bf16_t, false>(a, vec, sms, st);
+    if (dtype == SO_DTYPE_FP16) return layer ? forward<f16_t, true>(a, vec, sms, st) : forward<f16_t, false>(a, vec, sms, st);
+    return layer ? forward<float, true>(a, vec, sms, st) : forward<float, false>(a, vec, sms, st);
 }
 
 so_status so_residual_norm_backward_scratch(int64_t rows, int64_t cols, int64_t groups, uint64_t *bytes)
 {
     if (!bytes || common(rows, cols, groups, SO_DTYPE_FP32, SO_DTYPE_FP32, SO_NORM_RMS, 0, 1.0) != SO_OK) return SO_ERR_INVALID_ARG;
     // the sums of the parts, and two means per row
-    *bytes = ((uint64_t)parts_of(rows, groups) * groups * 4 * cols + 2 * (uint64_t)rows) * sizeof(float);
+    *bytes = ((uint64_t)(most_parts(rows, cols) + groups - 1) * 4 * cols + 2 * (uint64_t)rows) * sizeof(float);
     return SO_OK;
 }
 
@@ -525,15 +1086,15 @@ so_status so_residual_norm_backward(const void *dy, int64_t dy_stride, const voi
     int sms;
     const so_status d = device_sms(&sms);
     if (d != SO_OK) return d;
-    const int parts = parts_of(rows, groups);
-    float *partials = static_cast<float *>(scratch);
-    a.moments = sums ? partials + (int64_t)parts * groups * 4 * cols : nullptr;
-    const Grads g = {partials, dgate, dpost_weight, dpost_bias, dweight, dbias, grad_dtype, accumulate, (int32_t)groups, parts};
+    a.partials = static_cast<float *>(scratch);
+    a.moments = sums ? a.partials + (most_parts(rows, cols) + groups - 1) * 4 * cols : nullptr;
+    a.patience = patience();
+    const Grads g = {dgate, dpost_weight, dpost_bias, dweight, dbias, grad_dtype, accumulate, (int32_t)groups};
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool layer = kind == SO_NORM_LAYER;
-    if (dtype == SO_DTYPE_BF16) return backward<bf16_t>(a, g, sums, vec, layer, sms, st);
-    if (dtype == SO_DTYPE_FP16) return backward<f16_t>(a, g, sums, vec, layer, sms, st);
-    return backward<float>(a, g, sums, vec, layer, sms, st);
+    if (dtype == SO_DTYPE_BF16) return layer ? backward<bf16_t, true>(a, g, sums, vec, sms, st) : backward<bf16_t, false>(a, g, sums, vec, sms, st);
+    if (dtype == SO_DTYPE_FP16) return layer ? backward<f16_t, true>(a, g, sums, vec, sms, st) : backward<f16_t, false>(a, g, sums, vec, sms, st);
+    return layer ? backward<float, true>(a, g, sums, vec, sms, st) : backward<float, false>(a, g, sums, vec, sms, st);
 }
 
 }  // extern "C"

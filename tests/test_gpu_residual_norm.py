@@ -61,7 +61,9 @@ class Case:
         e = path(n)
         pm, pr = statistics(u, self.layer) if self.post else (torch.zeros_like(x[:, 0]), torch.ones_like(x[:, 0]))
         spread = lambda t, r: (1.0 + t.abs().amax(1) * r * e)[:, None] if self.layer else torch.ones_like(t[:, :1])  # noqa: E731
-        hat, size = (u - pm[:, None]) * pr[:, None], (u.abs() + pm.abs()[:, None]) * pr[:, None] * spread(u, pr)
+        # a mean is a sum of terms whose magnitudes, not whose sum, its roundings are relative to:
+        # |error| <= path(n) mean |x|, also where the mean itself is next to nothing
+        hat, size = (u - pm[:, None]) * pr[:, None], (u.abs() + u.abs().mean(1, keepdim=True)) * pr[:, None] * spread(u, pr)
         pw, pb = wide(self.pw, x, 1.0), wide(self.pb, x, 0.0)
         v, size = hat * pw + pb, size * pw.abs() + pb.abs()
         g = gates(self.gate, x)
@@ -70,7 +72,7 @@ class Case:
         seen = h.double()
         m, r = statistics(seen, self.layer)
         w, b = wide(self.w, x, 1.0), wide(self.b, x, 0.0)
-        size = (seen.abs() + m.abs()[:, None]) * r[:, None] * spread(seen, r)
+        size = (seen.abs() + seen.abs().mean(1, keepdim=True)) * r[:, None] * spread(seen, r)
         close(y, (seen - m[:, None]) * r[:, None] * w + b, e * (size * w.abs() + b.abs()), "y")
         for got, t, mean, rstd in ((stats[:2], u, pm, pr), (stats[2:], seen, m, r)):
             close(got[0], mean, e * t.abs().amax(1), "mean")
@@ -302,3 +304,44 @@ def test_captured_and_replayed():
         first = ops.residual_norm_forward(c.x, c.block, c.gate, c.pw, c.pb, c.w, c.b, **c.kw, eps=EPS)
         then = ops.residual_norm_backward(c.dy, c.dh, first[0], c.block, first[2], c.gate, c.pw, c.pb, c.w, **c.kw)
         assert all(same_bits(a, b) for a, b in zip(got, (*first, *then)))
+
+
+@pytest.mark.parametrize("rows,cols,dtype,groups", [(3000, 256, BF16, 1), (2001, 768, FP16, 3), (900, 4096, BF16, 5), (700, 1024, FP32, 700), (500, 8192, BF16, 1)])
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_rows_whose_copies_do_not_arrive(rows, cols, dtype, groups, kind):
+    """NaN in the rows of the groups that gave up and in the gradients of parameters, all else as ever."""
+    c = Case(31, rows, cols, dtype, FP32, kind, groups=groups)
+    args = (c.x, c.block, c.gate, c.pw, c.pb, c.w, c.b)
+    want = ops.residual_norm_forward(*args, **c.kw, eps=EPS)
+    back = (c.dy, c.dh, want[0], c.block, want[2], c.gate, c.pw, c.pb, c.w)
+    grads = ops.residual_norm_backward(*back, **c.kw)
+    for unit in (-1, 0, 2):
+        B.so_debug_set_operator_polls(0, unit)
+        try:
+            got = ops.residual_norm_forward(*args, **c.kw, eps=EPS)
+            lost = ops.residual_norm_backward(*back, **c.kw)
+        finally:
+            B.so_debug_set_operator_polls(1 << 20)
+        gone = torch.isnan(got[1]).all(1)
+        assert gone.all() if unit < 0 else 0 < gone.sum() < rows
+        for a, b in zip(got, want):
+            a, b = (a, b) if a.shape[0] == rows else (a.t(), b.t())
+            assert torch.isnan(a[gone]).all() and same_bits(a[~gone], b[~gone])
+        gone = torch.isnan(lost[0]).all(1)
+        assert gone.all() if unit < 0 else 0 < gone.sum() < rows
+        for a, b in zip(lost[:2], grads[:2]):
+            assert torch.isnan(a[gone]).all() and same_bits(a[~gone], b[~gone])
+        assert torch.isnan(lost[2]).any()
+        for name, a, b in zip(NAMES[3:], lost[3:], grads[3:]):
+            # wide rows have sums of their own, of which those of dy alone need nothing of what was lost
+            if a is not None and cols == 8192 and name in ("dweight", "dbias"):
+                assert same_bits(a, b)
+            elif a is not None:
+                assert torch.isnan(a).all()
+    z = c.x.clone()
+    B.so_debug_set_operator_polls(0, -1)
+    try:
+        ops.residual_norm_forward(z, *args[1:], **c.kw, eps=EPS, h=z)
+    finally:
+        B.so_debug_set_operator_polls(1 << 20)
+    assert torch.isnan(z).all()
