@@ -27,6 +27,7 @@ struct Args {
     int64_t x_stride, block_stride, dy_stride, dh_stride, h_stride, y_stride, dx_stride, dblock_stride;
     int64_t rows, cols, group_rows;       // rows that share a gate
     int32_t param_dtype, post;
+    int32_t needs_block;                  // backward: the first norm, or a sum, goes by the block
     float scale, eps, inv_cols;
     int64_t each;                         // consecutive rows of a group of threads (or of a part of the column sums)
     float *partials;                      // backward: [groups of threads + gates - 1][4][cols]
@@ -276,13 +277,16 @@ constexpr int kMaxWarps = 16;             // of a group
 
 struct RingShared {
     uint64_t full[kRingBars];
-    float2 part[2][kMaxWarps];            // of each exchange of a row
+    float part[2][2][kMaxWarps];          // of each exchange of a row: two values of every warp
     float count[kMaxWarps];               // elements of a warp
     int gave_up[8], issued[8];
 };
 
-// One row in `kNV` vectors a thread
-template <typename T, int E, int kNV>
+// What a kernel leaves out: biases and their gradients with the RMS norm; the mean with either.
+enum Form { kPlainRms, kBiasedRms, kLayerNorm };
+
+// One row in `kNV` vectors a thread; kFull: every thread has all of them.
+template <typename T, int E, int kNV, bool kFull>
 struct Columns {
     const Group &g;
     int cols;
@@ -296,47 +300,78 @@ struct Columns {
         warp_n = warp_sum(mine);
     }
     __device__ __forceinline__ int at(int i) const { return (g.thread + i * g.threads) * E; }
-    __device__ __forceinline__ bool has(int i) const { return at(i) < cols; }
+    __device__ __forceinline__ bool has(int i) const { return kFull || at(i) < cols; }
 };
 
-__device__ __forceinline__ float2 warp_sum2(float a, float b)
-{
-    float v[2] = {a, b};
-    const float one = warp_sum_many<2>(v);                   // lanes 0 to 15: the first, the others: the second
-    return make_float2(__shfl_sync(0xFFFFFFFFu, one, 0), __shfl_sync(0xFFFFFFFFu, one, 16));
-}
+// The exchanges of a row.  A warp sums two values at once (lanes 0 to 15 end with the first, the
+// others with the second) and leaves them in shared memory; behind the barrier lane l takes what
+// warp l & 15 left of the first or the second, and 16 lanes add up.
+struct Exchange {
+    const Group &g;
+    float (*part)[2][kMaxWarps];          // from the group's first warp on
+    __device__ Exchange(const Group &g_, RingShared &s) : g(g_), part(reinterpret_cast<float (*)[2][kMaxWarps]>(&s.part[0][0][g_.index * g_.warps])) {}
 
-// Sums of two values over the group, known to all of it.
-__device__ __forceinline__ float2 group_sum2(const Group &g, float2 (*part), float a, float b)
-{
-    float2 r = warp_sum2(a, b);
-    if (g.warps == 1) {
-        __syncwarp();
-        return r;
+    static __device__ __forceinline__ float add16(float x)
+    {
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+        return x;
     }
-    if ((threadIdx.x & 31) == 0) part[g.warp] = r;
-    g.sync();
-    r = make_float2(0.0f, 0.0f);
-    for (int i = 0; i < g.warps; ++i) {
-        const float2 o = part[i];
-        r.x += o.x;
-        r.y += o.y;
+    // what the lanes' warps hold of the k-th exchange
+    __device__ __forceinline__ float take(int k) const
+    {
+        const int lane = threadIdx.x & 31, w = lane & 15;
+        return w < g.warps ? part[k][lane >> 4][w] : 0.0f;
     }
-    return r;
-}
-__device__ __forceinline__ float group_sum(const Group &g, float2 (*part), float a)
-{
-    a = warp_sum(a);
-    if (g.warps == 1) {
-        __syncwarp();
+    __device__ __forceinline__ void leave(int k, float one) const
+    {
+        const int lane = threadIdx.x & 31;
+        if ((lane & 15) == 0) part[k][lane >> 4][g.warp] = one;
+        g.sync();
+    }
+    static __device__ __forceinline__ float2 both(float one)
+    {
+        return make_float2(__shfl_sync(0xFFFFFFFFu, one, 0), __shfl_sync(0xFFFFFFFFu, one, 16));
+    }
+    __device__ __forceinline__ float2 sums(int k, float a, float b) const
+    {
+        float v[2] = {a, b};
+        float one = warp_sum_many<2>(v);
+        if (g.warps > 1) {
+            leave(k, one);
+            one = add16(take(k));
+        } else {
+            __syncwarp();
+        }
+        return both(one);
+    }
+    __device__ __forceinline__ float sum(int k, float a) const
+    {
+        a = warp_sum(a);
+        if (g.warps > 1) {
+            if ((threadIdx.x & 31) == 0) part[k][0][g.warp] = a;
+            g.sync();
+            const int w = threadIdx.x & 15;
+            a = add16(w < g.warps ? part[k][0][w] : 0.0f);
+        } else {
+            __syncwarp();
+        }
         return a;
     }
-    if ((threadIdx.x & 31) == 0) part[g.warp].x = a;
-    g.sync();
-    a = 0.0f;
-    for (int i = 0; i < g.warps; ++i) a += part[i].x;
-    return a;
-}
+    // mean and squares around it of the group, from each warp's
+    __device__ __forceinline__ float2 join(int k, float mean, float m2, const float *count, float inv_cols) const
+    {
+        if (g.warps == 1) {
+            __syncwarp();
+            return make_float2(mean, m2);
+        }
+        const int lane = threadIdx.x & 31, w = lane & 15;
+        leave(k, lane < 16 ? mean : m2);
+        const float one = take(k), n = w < g.warps && lane < 16 ? count[w] : 0.0f;
+        mean = __shfl_sync(0xFFFFFFFFu, add16(one * n), 0) * inv_cols;
+        return make_float2(mean, warp_sum(lane < 16 ? (one - mean) * (one - mean) * n : one));
+    }
+};
 
 // Mean (0 with the RMS norm) and 1 / sqrt(variance + eps) of a row.  Layer norm in one exchange:
 // a warp has the mean of its first lane's elements as its centre c, and with n_t, m_t, Q_t each
@@ -344,9 +379,9 @@ __device__ __forceinline__ float group_sum(const Group &g, float2 (*part), float
 //   D = sum n_t (m_t - c),  Q = sum (Q_t + n_t (m_t - c)^2),
 // so that its mean is c + D / n, and its squares around that Q - D^2 / n; warps are joined by
 // M2 = sum (M2_w + n_w (mean_w - mean)^2).
-template <bool kLayer, typename T, int E, int kNV>
-__device__ __forceinline__ float2 row_statistics(const Columns<T, E, kNV> &c, const Group &g, float2 (*part), const float *count, const Vals<E> (&f)[kNV],
-                                                 float inv_cols, float eps)
+template <bool kLayer, typename T, int E, int kNV, bool kFull>
+__device__ __forceinline__ float2 row_statistics(const Columns<T, E, kNV, kFull> &c, const Exchange &x, int k, const float *count, const Vals<E> (&f)[kNV],
+                                                 float inv_mine, float inv_warp, float inv_cols, float eps)
 {
     Vals<E> acc;
     acc.set(0.0f);
@@ -354,13 +389,12 @@ __device__ __forceinline__ float2 row_statistics(const Columns<T, E, kNV> &c, co
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) acc = fma(f[i], f[i], acc);
-        const float sq = group_sum(g, part, total(acc));
-        return make_float2(0.0f, 1.0f / sqrtf(sq * inv_cols + eps));
+        return make_float2(0.0f, 1.0f / sqrtf(x.sum(k, total(acc)) * inv_cols + eps));
     } else {
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) acc = acc + f[i];
-        const float m = c.mine > 0.0f ? total(acc) / c.mine : 0.0f;
+        const float m = total(acc) * inv_mine;
         acc.set(0.0f);
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
@@ -368,20 +402,10 @@ __device__ __forceinline__ float2 row_statistics(const Columns<T, E, kNV> &c, co
                 const Vals<E> d = f[i] + -m;
                 acc = fma(d, d, acc);
             }
-        const float centre = __shfl_sync(0xFFFFFFFFu, m, 0), d = c.mine > 0.0f ? m - centre : 0.0f;
-        const float2 s = warp_sum2(d * c.mine, fmaf(d * c.mine, d, total(acc)));
-        float2 r = make_float2(centre + s.x / c.warp_n, s.y - s.x * s.x / c.warp_n);
-        if (g.warps == 1) {
-            __syncwarp();
-        } else {
-            if ((threadIdx.x & 31) == 0) part[g.warp] = r;
-            g.sync();
-            float mean = 0.0f, m2 = 0.0f;
-            for (int i = 0; i < g.warps; ++i) mean = fmaf(part[i].x, count[i], mean);
-            mean *= inv_cols;
-            for (int i = 0; i < g.warps; ++i) m2 += fmaf((part[i].x - mean) * count[i], part[i].x - mean, part[i].y);
-            r = make_float2(mean, m2);
-        }
+        const float centre = __shfl_sync(0xFFFFFFFFu, m, 0), d = kFull || c.mine > 0.0f ? m - centre : 0.0f;
+        float v[2] = {d * c.mine, fmaf(d * c.mine, d, total(acc))};
+        const float2 w = Exchange::both(warp_sum_many<2>(v));
+        const float2 r = x.join(k, centre + w.x * inv_warp, w.y - w.x * w.x * inv_warp, count, inv_cols);
         return make_float2(r.x, 1.0f / sqrtf(r.y * inv_cols + eps));
     }
 }
@@ -442,20 +466,21 @@ struct Ring {
 };
 
 // Bound: memory (two reads, two writes).
-template <typename T, bool kLayer, int kNV, int kMaxThreads>
+template <typename T, Form kForm, int kNV, bool kFull, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forward_ring_kernel(const __grid_constant__ Args a, int per_row, int stages)
 {
     constexpr int E = Vec<T>::kElems;
+    constexpr bool kLayer = kForm == kLayerNorm, kBias = kForm != kPlainRms;
     extern __shared__ __align__(128) uint8_t s_room[];
     __shared__ __align__(8) RingShared s;
     const Group g(per_row);
     Ring<2> ring(g, s, s_room, (uint32_t)a.cols * sizeof(T), stages, a.patience.of((int)blockIdx.x));
-    const Columns<T, E, kNV> c(g, (int)a.cols);
+    const Columns<T, E, kNV, kFull> c(g, (int)a.cols);
+    const Exchange x(g, s);
+    const float *count = s.count + g.index * g.warps;
     if ((threadIdx.x & 31) == 0) s.count[threadIdx.x >> 5] = c.warp_n;
+    const float inv_mine = c.mine > 0.0f ? 1.0f / c.mine : 0.0f, inv_warp = 1.0f / c.warp_n;
     __syncthreads();
-    float2 (*part)[kMaxWarps] = s.part;
-    const int w0 = g.index * g.warps;     // the group's first warp
-    const float *count = s.count + w0;
     int64_t row = ((int64_t)blockIdx.x * g.per_block + g.index) * a.each, end = row + a.each;
     if (end > a.rows) end = a.rows;
     const auto fill = [&](int at, int64_t r) {
@@ -470,10 +495,11 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forwa
     for (int i = 0; i < kNV; ++i)
         if (c.has(i)) {
             w[i] = load_params<E>(a.w, c.at(i), a.param_dtype, 1.0f);
-            if (kLayer || a.b) b[i] = load_params<E>(a.b, c.at(i), a.param_dtype, 0.0f);
+            if (kBias) b[i] = load_params<E>(a.b, c.at(i), a.param_dtype, 0.0f);
         }
     int64_t gate_end = 0;
-    for (; row < end; ++row) {
+    T *h = static_cast<T *>(a.h) + row * a.h_stride, *y = static_cast<T *>(a.y) + row * a.y_stride;
+    for (; row < end; ++row, h += a.h_stride, y += a.y_stride) {
         if (row >= gate_end) {
             const int64_t gate = row / a.group_rows;
             gate_end = (gate + 1) * a.group_rows;
@@ -482,58 +508,59 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forwa
                 if (c.has(i)) {
                     gw[i] = a.gate ? load_params<E>(static_cast<const char *>(a.gate) + gate * a.cols * (a.param_dtype == SO_DTYPE_FP32 ? 4 : 2), c.at(i), a.param_dtype, 1.0f)
                                    : spread<E>(1.0f);
-                    gb[i] = a.pb ? gw[i] * load_params<E>(a.pb, c.at(i), a.param_dtype, 0.0f) : spread<E>(0.0f);
+                    if (kBias) gb[i] = a.pb ? gw[i] * load_params<E>(a.pb, c.at(i), a.param_dtype, 0.0f) : spread<E>(0.0f);
                     if (a.pw) gw[i] = gw[i] * load_params<E>(a.pw, c.at(i), a.param_dtype, 1.0f);
                 }
         }
         ring.wait();
         float2 post = make_float2(0.0f, 1.0f);
         Vals<E> f[kNV];
-        if (a.post) {
 #pragma unroll
-            for (int i = 0; i < kNV; ++i)
-                if (c.has(i)) f[i] = from_shared<T, E>(ring.row(1) + c.at(i) * sizeof(T));
-            post = row_statistics<kLayer>(c, g, part[0] + w0, count, f, a.inv_cols, a.eps);
-        }
-        T *h = static_cast<T *>(a.h) + row * a.h_stride, *y = static_cast<T *>(a.y) + row * a.y_stride;
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) f[i] = from_shared<T, E>(ring.row(1) + c.at(i) * sizeof(T));
+        if (a.post) post = row_statistics<kLayer>(c, x, 0, count, f, inv_mine, inv_warp, a.inv_cols, a.eps);
         const float shift = -post.x * post.y;
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const Vals<E> u = from_shared<T, E>(ring.row(1) + c.at(i) * sizeof(T)), x = from_shared<T, E>(ring.row(0) + c.at(i) * sizeof(T));
+                const Vals<E> from = from_shared<T, E>(ring.row(0) + c.at(i) * sizeof(T));
                 // in fp32 the mean is taken off first: rows far from zero keep their digits
-                const Vals<E> hat = !kLayer ? u * post.y : sizeof(T) == 4 ? (u + -post.x) * post.y : fma(u, post.y, shift);
-                const uint4 bits = narrow16<T>(fma(gw[i], hat, fma(x, a.scale, gb[i])));
+                const Vals<E> hat = !kLayer ? f[i] * post.y : sizeof(T) == 4 ? (f[i] + -post.x) * post.y : fma(f[i], post.y, shift);
+                const uint4 bits = narrow16<T>(fma(gw[i], hat, kBias ? fma(from, a.scale, gb[i]) : from * a.scale));
                 *reinterpret_cast<uint4 *>(h + c.at(i)) = bits;
                 f[i] = widen16<T>(bits);
             }
-        const float2 st = row_statistics<kLayer>(c, g, part[1] + w0, count, f, a.inv_cols, a.eps);
+        const float2 st = row_statistics<kLayer>(c, x, 1, count, f, inv_mine, inv_warp, a.inv_cols, a.eps);
         if (ring.gave_up()) break;
-        if (g.thread == 0 && row + stages < end) fill(ring.stage, row + stages);
+        if (g.thread == 0) {
+            if (row + stages < end) fill(ring.stage, row + stages);
+            if (a.stats) {
+                a.stats[row] = post.x;
+                a.stats[a.rows + row] = post.y;
+                a.stats[2 * a.rows + row] = st.x;
+                a.stats[3 * a.rows + row] = st.y;
+            }
+        }
         const float back = -st.x * st.y;
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
                 const Vals<E> hat = !kLayer ? f[i] * st.y : sizeof(T) == 4 ? (f[i] + -st.x) * st.y : fma(f[i], st.y, back);
-                *reinterpret_cast<uint4 *>(y + c.at(i)) = narrow16<T>(kLayer || a.b ? fma(hat, w[i], b[i]) : hat * w[i]);
+                *reinterpret_cast<uint4 *>(y + c.at(i)) = narrow16<T>(kBias ? fma(hat, w[i], b[i]) : hat * w[i]);
             }
-        if (a.stats && g.thread == 0) {
-            a.stats[row] = post.x;
-            a.stats[a.rows + row] = post.y;
-            a.stats[2 * a.rows + row] = st.x;
-            a.stats[3 * a.rows + row] = st.y;
-        }
         ring.next();
+        // one exchange a row: its place must not be written again before all have read it
+        if (!a.post && g.warps > 1) g.sync();
     }
     if (row >= end) return;
     if (g.thread == 0) land(ring.bars, s.issued[g.index], stages);
     const uint4 nan = narrow16<T>(spread<E>(kNan));
-    for (; row < end; ++row) {
+    for (; row < end; ++row, h += a.h_stride, y += a.y_stride) {
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                *reinterpret_cast<uint4 *>(static_cast<T *>(a.h) + row * a.h_stride + c.at(i)) = nan;
-                *reinterpret_cast<uint4 *>(static_cast<T *>(a.y) + row * a.y_stride + c.at(i)) = nan;
+                *reinterpret_cast<uint4 *>(h + c.at(i)) = nan;
+                *reinterpret_cast<uint4 *>(y + c.at(i)) = nan;
             }
         if (a.stats && g.thread == 0)
             for (int k = 0; k < 4; ++k) a.stats[k * a.rows + row] = kNan;
@@ -545,18 +572,20 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forwa
 // rows of gate i.  Without kSums the rows' means are left for the sums to be taken from.
 //
 // Bound: memory (four reads, two writes).
-template <typename T, bool kLayer, bool kSums, int kNV, int kMaxThreads>
+template <typename T, Form kForm, bool kSums, int kNV, bool kFull, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backward_ring_kernel(const __grid_constant__ Args a, int per_row, int stages)
 {
     constexpr int E = Vec<T>::kElems;
+    constexpr bool kLayer = kForm == kLayerNorm, kBias = kForm != kPlainRms;
+    // what the second half of a row needs again is held in registers where a thread has 8 elements
+    constexpr bool kHold = kNV * E <= 8;
     extern __shared__ __align__(128) uint8_t s_room[];
     __shared__ __align__(8) RingShared s;
     const Group g(per_row);
     Ring<4> ring(g, s, s_room, (uint32_t)a.cols * sizeof(T), stages, a.patience.of((int)blockIdx.x));
-    const Columns<T, E, kNV> c(g, (int)a.cols);
+    const Columns<T, E, kNV, kFull> c(g, (int)a.cols);
+    const Exchange x(g, s);
     __syncthreads();
-    float2 (*part)[kMaxWarps] = s.part;
-    const int w0 = g.index * g.warps;
     const int64_t me = (int64_t)blockIdx.x * g.per_block + g.index;
     int64_t row = me * a.each, end = row + a.each;
     if (end > a.rows) end = a.rows;
@@ -564,7 +593,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
         const char *const src[4] = {reinterpret_cast<const char *>(static_cast<const T *>(a.dy) + r * a.dy_stride),
                                     reinterpret_cast<const char *>(static_cast<const T *>(a.hin) + r * a.h_stride),
                                     a.dh ? reinterpret_cast<const char *>(static_cast<const T *>(a.dh) + r * a.dh_stride) : nullptr,
-                                    a.block ? reinterpret_cast<const char *>(static_cast<const T *>(a.block) + r * a.block_stride) : nullptr};
+                                    a.needs_block ? reinterpret_cast<const char *>(static_cast<const T *>(a.block) + r * a.block_stride) : nullptr};
         ring.fill(at, src);
     };
     if (g.thread == 0)
@@ -582,7 +611,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
             if (c.has(i)) {
                 Vals<E> *const v[4] = {&s1[i], &s2[i], &t1[i], &t2[i]};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < 4; k += kBias ? 1 : 2) {
                     float f[E];
                     v[k]->get(f);
 #pragma unroll
@@ -613,22 +642,24 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
         const auto norm = [&](const Vals<E> &v, float mean, float rstd) {
             return !kLayer ? v * rstd : sizeof(T) == 4 ? (v + -mean) * rstd : fma(v, rstd, -mean * rstd);
         };
-        Vals<E> sum, dot;
+        Vals<E> sum, dot, e[kNV], hat[kNV], bhat[kNV];
         sum.set(0.0f), dot.set(0.0f);
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const Vals<E> dy = from(0, i), hat = norm(from(1, i), st.mean, st.rstd), e = dy * w[i];
-                if (kLayer) sum = sum + e;
-                dot = fma(e, hat, dot);
-                if (kSums) t1[i] = fma(dy, hat, t1[i]), t2[i] = t2[i] + dy;
+                const Vals<E> dy = from(0, i), u = norm(from(1, i), st.mean, st.rstd), q = dy * w[i];
+                if (kLayer) sum = sum + q;
+                dot = fma(q, u, dot);
+                if (kSums) t1[i] = fma(dy, u, t1[i]);
+                if (kSums && kBias) t2[i] = t2[i] + dy;
+                if (kHold) e[i] = q, hat[i] = u;
             }
         float me_ = 0.0f, meh;
         if (kLayer) {
-            const float2 r = group_sum2(g, part[0] + w0, total(sum), total(dot));
+            const float2 r = x.sums(0, total(sum), total(dot));
             me_ = r.x * a.inv_cols, meh = r.y * a.inv_cols;
         } else {
-            meh = group_sum(g, part[0] + w0, total(dot)) * a.inv_cols;
+            meh = x.sum(0, total(dot)) * a.inv_cols;
         }
         if (!kSums && a.moments && g.thread == 0) {
             a.moments[row] = me_;
@@ -641,28 +672,31 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const Vals<E> hat = norm(from(1, i), st.mean, st.rstd);
-                t[i] = fma(hat, c1, fma(from(0, i) * w[i], st.rstd, c0));
+                const Vals<E> u = kHold ? hat[i] : norm(from(1, i), st.mean, st.rstd), q = kHold ? e[i] : from(0, i) * w[i];
+                t[i] = fma(u, c1, kLayer ? fma(q, st.rstd, c0) : q * st.rstd);
                 if (a.dh) t[i] = t[i] + from(2, i);
-                if (a.post || kSums) {
-                    const Vals<E> bhat = norm(from(3, i), st.pmean, st.prstd), q = t[i] * gw[i];
-                    if (kLayer) sum = sum + q;
-                    dot = fma(q, bhat, dot);
-                    if (kSums) s1[i] = fma(t[i], bhat, s1[i]), s2[i] = s2[i] + t[i];
+                if (a.needs_block) {
+                    const Vals<E> v = norm(from(3, i), st.pmean, st.prstd), d = t[i] * gw[i];
+                    if (kLayer) sum = sum + d;
+                    dot = fma(d, v, dot);
+                    if (kSums) s1[i] = fma(t[i], v, s1[i]);
+                    if (kHold) bhat[i] = v;
                 }
+                if (kSums && kBias) s2[i] = s2[i] + t[i];
             }
-        float mq = 0.0f, mqb = 0.0f;
-        // without a first norm the exchange has nothing to tell but that everyone is done with phase 1
+        // (without a first norm the exchange has nothing to tell but that everyone is done with the first one)
+        float mq = 0.0f, mqb;
         if (kLayer) {
-            const float2 r = group_sum2(g, part[1] + w0, total(sum), total(dot));
+            const float2 r = x.sums(1, total(sum), total(dot));
             mq = r.x * a.inv_cols, mqb = r.y * a.inv_cols;
         } else {
-            mqb = group_sum(g, part[1] + w0, total(dot)) * a.inv_cols;
+            mqb = x.sum(1, total(dot)) * a.inv_cols;
         }
         if (ring.gave_up()) {
             lost = true;
             break;
         }
+        if (kHold && g.thread == 0 && row + stages < end) fill(ring.stage, row + stages);
         T *dx = static_cast<T *>(a.dx) + row * a.dx_stride, *dblock = static_cast<T *>(a.dblock) + row * a.dblock_stride;
         const float c2 = -st.prstd * mq, c3 = -st.prstd * mqb;
 #pragma unroll
@@ -670,12 +704,14 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
             if (c.has(i)) {
                 *reinterpret_cast<uint4 *>(dx + c.at(i)) = narrow16<T>(t[i] * a.scale);
                 Vals<E> d = t[i] * gw[i];
-                if (a.post) d = fma(norm(from(3, i), st.pmean, st.prstd), c3, fma(d, st.prstd, c2));
+                if (a.post) d = fma(kHold ? bhat[i] : norm(from(3, i), st.pmean, st.prstd), c3, kLayer ? fma(d, st.prstd, c2) : d * st.prstd);
                 *reinterpret_cast<uint4 *>(dblock + c.at(i)) = narrow16<T>(d);
             }
-        if (g.warps > 1) g.sync();        // the block's row has been read a last time
-        else __syncwarp();
-        if (g.thread == 0 && row + stages < end) fill(ring.stage, row + stages);
+        if (!kHold) {                     // the block's row has been read a last time
+            if (g.warps > 1) g.sync();
+            else __syncwarp();
+            if (g.thread == 0 && row + stages < end) fill(ring.stage, row + stages);
+        }
         ring.next();
     }
     if (!lost) {
@@ -752,6 +788,7 @@ __global__ void __launch_bounds__(kLoopThreads) columns_kernel(const __grid_cons
 struct Grads {
     void *dgate, *dpw, *dpb, *dw, *db;
     int32_t dtype, accumulate, groups;
+    int32_t biased;                       // the parts hold S2 and sum dy too
 };
 
 __device__ __forceinline__ void put(const Grads &g, void *p, int64_t at, float x)
@@ -782,8 +819,10 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_kernel(const __grid_consta
 #pragma unroll 4
             for (int64_t t = first + (kByGate ? 0 : warp); t <= last; t += kByGate ? 1 : kSumWarps) {
                 const float *at = a.partials + (t + gate) * 4 * a.cols + c;
-                if (gates) sum[0] += at[0], sum[1] += at[a.cols];
-                sum[2] += at[2 * a.cols], sum[3] += at[3 * a.cols];
+                if (gates) sum[0] += at[0];
+                if (gates && g.biased) sum[1] += at[a.cols];
+                sum[2] += at[2 * a.cols];
+                if (g.biased) sum[3] += at[3 * a.cols];
             }
         }
         if (!kByGate) {
@@ -863,11 +902,11 @@ so_status common(int64_t rows, int64_t cols, int64_t groups, int32_t dtype, int3
 struct Plan { int per_row, nv, block; };
 
 // The choice that leaves the fewest lanes idle, and the most vectors a thread of equals.
-Plan plan_rows(int64_t vectors, int most_nv)
+Plan plan_rows(int64_t vectors, int most_nv, int least_nv = 1)
 {
     Plan best = {0, 0, 0};
     int64_t waste = INT64_MAX;
-    for (int nv = most_nv; nv > 0; --nv) {
+    for (int nv = most_nv; nv >= least_nv; nv /= 2) {
         const int64_t threads = ((vectors + nv - 1) / nv + 31) / 32 * 32, idle = threads * nv - vectors;
         if (threads > 32 * kMaxWarps || idle >= waste) continue;
         waste = idle;
@@ -916,57 +955,60 @@ so_status launch_ring(K kernel, std::atomic<uint64_t> (&cache)[kMaxDevices], Arg
     return launch(kernel, (unsigned)((used + groups - 1) / groups), p.block, smem, st, false, a, p.per_row, stages);
 }
 
-template <typename T, bool kLayer, int kNV>
+template <typename T, Form kForm, int kNV>
 so_status forward_ring(Args &a, const Plan &p, int sms, cudaStream_t st)
 {
-    static std::atomic<uint64_t> cache[2][kMaxDevices];
-    if (p.block <= 256) return launch_ring(forward_ring_kernel<T, kLayer, kNV, 256>, cache[0], a, p, 2, sizeof(T), INT64_MAX, sms, st);
-    return launch_ring(forward_ring_kernel<T, kLayer, kNV, 512>, cache[1], a, p, 2, sizeof(T), INT64_MAX, sms, st);
+    static std::atomic<uint64_t> cache[3][kMaxDevices];
+    const bool full = (int64_t)p.per_row * p.nv * Vec<T>::kElems == a.cols;
+    if (p.block <= 256 && full) return launch_ring(forward_ring_kernel<T, kForm, kNV, true, 256>, cache[0], a, p, 2, sizeof(T), INT64_MAX, sms, st);
+    if (p.block <= 256) return launch_ring(forward_ring_kernel<T, kForm, kNV, false, 256>, cache[1], a, p, 2, sizeof(T), INT64_MAX, sms, st);
+    return launch_ring(forward_ring_kernel<T, kForm, kNV, false, 512>, cache[2], a, p, 2, sizeof(T), INT64_MAX, sms, st);
 }
 
-template <typename T, bool kLayer>
+template <typename T, Form kForm>
 so_status forward(Args &a, bool vec, int sms, cudaStream_t st)
 {
     constexpr int E = Vec<T>::kElems;
+    constexpr bool kLayer = kForm == kLayerNorm;
+    constexpr int kMost = 16 / E;         // 16 elements a thread, or half as many
     if (vec && a.cols * (int64_t)sizeof(T) * 2 * 2 <= kMostShared) {
-        const Plan p = plan_rows(a.cols / E, sizeof(T) == 4 ? 4 : 2);
-        if (sizeof(T) == 4 && p.nv == 4) return forward_ring<T, kLayer, sizeof(T) == 4 ? 4 : 1>(a, p, sms, st);
-        if (sizeof(T) == 4 && p.nv == 3) return forward_ring<T, kLayer, sizeof(T) == 4 ? 3 : 1>(a, p, sms, st);
-        if (p.nv == 2) return forward_ring<T, kLayer, 2>(a, p, sms, st);
-        if (p.nv == 1) return forward_ring<T, kLayer, 1>(a, p, sms, st);
+        const Plan p = plan_rows(a.cols / E, kMost);
+        if (p.nv == kMost) return forward_ring<T, kForm, kMost>(a, p, sms, st);
+        if (p.nv == kMost / 2) return forward_ring<T, kForm, kMost / 2>(a, p, sms, st);
     }
     const unsigned grid = (unsigned)(a.rows < 8 * sms ? a.rows : 8 * sms);
     return launch(vec ? forward_loop_kernel<T, E, kLayer> : forward_loop_kernel<T, 1, kLayer>, grid, kLoopThreads, 0, st, false, a);
 }
 
-template <typename T, bool kLayer, bool kSums, int kNV>
+template <typename T, Form kForm, bool kSums, int kNV>
 so_status backward_ring(Args &a, const Plan &p, int64_t most, int sms, cudaStream_t st)
 {
-    static std::atomic<uint64_t> cache[2][kMaxDevices];
-    if (p.block <= 256) return launch_ring(backward_ring_kernel<T, kLayer, kSums, kNV, 256>, cache[0], a, p, 4, sizeof(T), most, sms, st);
-    return launch_ring(backward_ring_kernel<T, kLayer, kSums, kNV, 512>, cache[1], a, p, 4, sizeof(T), most, sms, st);
+    static std::atomic<uint64_t> cache[3][kMaxDevices];
+    const bool full = (int64_t)p.per_row * p.nv * Vec<T>::kElems == a.cols;
+    if (p.block <= 256 && full) return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, true, 256>, cache[0], a, p, 4, sizeof(T), most, sms, st);
+    if (p.block <= 256) return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, false, 256>, cache[1], a, p, 4, sizeof(T), most, sms, st);
+    return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, false, 512>, cache[2], a, p, 4, sizeof(T), most, sms, st);
 }
 
-template <typename T, bool kLayer>
+template <typename T, Form kForm>
 so_status backward(Args &a, const Grads &g, bool sums, bool vec, int sms, cudaStream_t st)
 {
     constexpr int E = Vec<T>::kElems;
+    constexpr bool kLayer = kForm == kLayerNorm;
     const int64_t most = most_parts(a.rows, a.cols);
     a.each = 1;
+    a.needs_block = a.post || (sums && (g.dgate || g.dpw || g.dpb));
     bool taken = false;                   // the rows' kernel has left the parts of the sums
     if (a.rows > 0) {
         const bool ring = vec && a.cols * (int64_t)sizeof(T) * 4 * 2 <= kMostShared;
-        const Plan with = ring ? plan_rows(a.cols / E, sizeof(T) == 4 ? 2 : 1) : Plan{0, 0, 0}, without = ring ? plan_rows(a.cols / E, sizeof(T) == 4 ? 4 : 2) : Plan{0, 0, 0};
+        // with sums 8 elements a thread, without 16
+        const Plan with = ring && sums ? plan_rows(a.cols / E, 8 / E, 8 / E) : Plan{0, 0, 0}, without = ring ? plan_rows(a.cols / E, 16 / E, 16 / E) : Plan{0, 0, 0};
         so_status s;
-        if (sums && with.nv) {
+        if (with.nv) {
             taken = true;
-            if (sizeof(T) == 4 && with.nv == 2) s = backward_ring<T, kLayer, true, sizeof(T) == 4 ? 2 : 1>(a, with, most, sms, st);
-            else s = backward_ring<T, kLayer, true, 1>(a, with, most, sms, st);
+            s = backward_ring<T, kForm, true, 8 / E>(a, with, most, sms, st);
         } else if (without.nv) {
-            if (sizeof(T) == 4 && without.nv == 4) s = backward_ring<T, kLayer, false, sizeof(T) == 4 ? 4 : 1>(a, without, INT64_MAX, sms, st);
-            else if (sizeof(T) == 4 && without.nv == 3) s = backward_ring<T, kLayer, false, sizeof(T) == 4 ? 3 : 1>(a, without, INT64_MAX, sms, st);
-            else if (without.nv == 2) s = backward_ring<T, kLayer, false, 2>(a, without, INT64_MAX, sms, st);
-            else s = backward_ring<T, kLayer, false, 1>(a, without, INT64_MAX, sms, st);
+            s = backward_ring<T, kForm, false, 16 / E>(a, without, INT64_MAX, sms, st);
         } else {
             const unsigned grid = (unsigned)(a.rows < 8 * sms ? a.rows : 8 * sms);
             s = launch(vec ? backward_loop_kernel<T, E, kLayer> : backward_loop_kernel<T, 1, kLayer>, grid, kLoopThreads, 0, st, false, a);
@@ -990,6 +1032,14 @@ so_status backward(Args &a, const Grads &g, bool sums, bool vec, int sms, cudaSt
     }
     const auto kernel = g.groups >= kSumWarps ? sum_kernel<true> : sum_kernel<false>;
     return launch(kernel, (unsigned)((a.cols + 31) / 32), 32 * kSumWarps, 0, st, true, a, g);
+}
+
+template <typename F>
+so_status by_form(Form form, F fn)
+{
+    if (form == kLayerNorm) return fn(std::integral_constant<Form, kLayerNorm>());
+    if (form == kBiasedRms) return fn(std::integral_constant<Form, kBiasedRms>());
+    return fn(std::integral_constant<Form, kPlainRms>());
 }
 
 }  // namespace
@@ -1027,10 +1077,10 @@ so_status so_residual_norm_forward(const void *x, int64_t x_stride, const void *
     const so_status d = device_sms(&sms);
     if (d != SO_OK) return d;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool layer = kind == SO_NORM_LAYER;
-    if (dtype == SO_DTYPE_BF16) return layer ? forward<bf16_t, true>(a, vec, sms, st) : forward<bf16_t, false>(a, vec, sms, st);
-    if (dtype == SO_DTYPE_FP16) return layer ? forward<f16_t, true>(a, vec, sms, st) : forward<f16_t, false>(a, vec, sms, st);
-    return layer ? forward<float, true>(a, vec, sms, st) : forward<float, false>(a, vec, sms, st);
+    const Form form = kind == SO_NORM_LAYER ? kLayerNorm : post_bias || bias ? kBiasedRms : kPlainRms;
+    if (dtype == SO_DTYPE_BF16) return by_form(form, [&](auto f) { return forward<bf16_t, decltype(f)::value>(a, vec, sms, st); });
+    if (dtype == SO_DTYPE_FP16) return by_form(form, [&](auto f) { return forward<f16_t, decltype(f)::value>(a, vec, sms, st); });
+    return by_form(form, [&](auto f) { return forward<float, decltype(f)::value>(a, vec, sms, st); });
 }
 
 so_status so_residual_norm_backward_scratch(int64_t rows, int64_t cols, int64_t groups, uint64_t *bytes)
@@ -1089,12 +1139,12 @@ so_status so_residual_norm_backward(const void *dy, int64_t dy_stride, const voi
     a.partials = static_cast<float *>(scratch);
     a.moments = sums ? a.partials + (most_parts(rows, cols) + groups - 1) * 4 * cols : nullptr;
     a.patience = patience();
-    const Grads g = {dgate, dpost_weight, dpost_bias, dweight, dbias, grad_dtype, accumulate, (int32_t)groups};
+    const Form form = kind == SO_NORM_LAYER ? kLayerNorm : post_bias || dpost_bias || dbias ? kBiasedRms : kPlainRms;
+    const Grads g = {dgate, dpost_weight, dpost_bias, dweight, dbias, grad_dtype, accumulate, (int32_t)groups, form != kPlainRms};
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool layer = kind == SO_NORM_LAYER;
-    if (dtype == SO_DTYPE_BF16) return layer ? backward<bf16_t, true>(a, g, sums, vec, sms, st) : backward<bf16_t, false>(a, g, sums, vec, sms, st);
-    if (dtype == SO_DTYPE_FP16) return layer ? backward<f16_t, true>(a, g, sums, vec, sms, st) : backward<f16_t, false>(a, g, sums, vec, sms, st);
-    return layer ? backward<float, true>(a, g, sums, vec, sms, st) : backward<float, false>(a, g, sums, vec, sms, st);
+    if (dtype == SO_DTYPE_BF16) return by_form(form, [&](auto f) { return backward<bf16_t, decltype(f)::value>(a, g, sums, vec, sms, st); });
+    if (dtype == SO_DTYPE_FP16) return by_form(form, [&](auto f) { return backward<f16_t, decltype(f)::value>(a, g, sums, vec, sms, st); });
+    return by_form(form, [&](auto f) { return backward<float, decltype(f)::value>(a, g, sums, vec, sms, st); });
 }
 
 }  // extern "C"
