@@ -277,7 +277,7 @@ constexpr int kMaxWarps = 16;             // of a group
 
 struct RingShared {
     uint64_t full[kRingBars];
-    float part[2][2][kMaxWarps];          // of each exchange of a row: two values of every warp
+    float part[2][4][kMaxWarps];          // of an exchange and the one before: up to four values of every warp
     float count[kMaxWarps];               // elements of a warp
     int gave_up[8], issued[8];
 };
@@ -303,13 +303,13 @@ struct Columns {
     __device__ __forceinline__ bool has(int i) const { return kFull || at(i) < cols; }
 };
 
-// The exchanges of a row.  A warp sums two values at once (lanes 0 to 15 end with the first, the
-// others with the second) and leaves them in shared memory; behind the barrier lane l takes what
-// warp l & 15 left of the first or the second, and 16 lanes add up.
+// The exchanges of a row.  A warp sums N values at once (its lanes end with one each, in groups of
+// 32 / N) and leaves them in shared memory; behind the barrier a lane takes what some of the warps left
+// of its value, and 32 / N lanes add up.
 struct Exchange {
     const Group &g;
-    float (*part)[2][kMaxWarps];          // from the group's first warp on
-    __device__ Exchange(const Group &g_, RingShared &s) : g(g_), part(reinterpret_cast<float (*)[2][kMaxWarps]>(&s.part[0][0][g_.index * g_.warps])) {}
+    float (*part)[4][kMaxWarps];          // from the group's first warp on
+    __device__ Exchange(const Group &g_, RingShared &s) : g(g_), part(reinterpret_cast<float (*)[4][kMaxWarps]>(&s.part[0][0][g_.index * g_.warps])) {}
 
     static __device__ __forceinline__ float add16(float x)
     {
@@ -333,17 +333,27 @@ struct Exchange {
     {
         return make_float2(__shfl_sync(0xFFFFFFFFu, one, 0), __shfl_sync(0xFFFFFFFFu, one, 16));
     }
-    __device__ __forceinline__ float2 sums(int k, float a, float b) const
+    // N sums over the group (2 or 4)
+    template <int N>
+    __device__ __forceinline__ void sums(int k, float (&v)[N]) const
     {
-        float v[2] = {a, b};
-        float one = warp_sum_many<2>(v);
+        constexpr int kLanes = 32 / N;
+        float one = warp_sum_many<N>(v);
         if (g.warps > 1) {
-            leave(k, one);
-            one = add16(take(k));
+            const int lane = threadIdx.x & 31, value = lane / kLanes, at = lane % kLanes;
+            if (at == 0) part[k][value][g.warp] = one;
+            g.sync();
+            one = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kMaxWarps; w += kLanes)
+                if (w + at < g.warps) one += part[k][value][w + at];
+#pragma unroll
+            for (int o = kLanes / 2; o > 0; o >>= 1) one += __shfl_xor_sync(0xFFFFFFFFu, one, o);
         } else {
             __syncwarp();
         }
-        return both(one);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, one, i * kLanes);
     }
     __device__ __forceinline__ float sum(int k, float a) const
     {
@@ -571,14 +581,15 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forwa
 // of its own where a gate's rows or its own end: part t + i for the t-th group of threads in the
 // rows of gate i.  Without kSums the rows' means are left for the sums to be taken from.
 //
+// The second half of a row and the first half of the next one share an exchange and its barrier.
+//
 // Bound: memory (four reads, two writes).
 template <typename T, Form kForm, bool kSums, int kNV, bool kFull, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backward_ring_kernel(const __grid_constant__ Args a, int per_row, int stages)
 {
     constexpr int E = Vec<T>::kElems;
     constexpr bool kLayer = kForm == kLayerNorm, kBias = kForm != kPlainRms;
-    // what the second half of a row needs again is held in registers where a thread has 8 elements
-    constexpr bool kHold = kNV * E <= 8;
+    constexpr int kEach = kLayer ? 2 : 1;                    // sums of half a row
     extern __shared__ __align__(128) uint8_t s_room[];
     __shared__ __align__(8) RingShared s;
     const Group g(per_row);
@@ -621,101 +632,114 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
                 }
             }
     };
-    int64_t gate_end = 0, gate = 0;
-    bool lost = false;
-    for (; row < end; ++row) {
-        if (row >= gate_end) {
-            if (kSums && gate_end > 0) leave(gate);
-            gate = row / a.group_rows;
-            gate_end = (gate + 1) * a.group_rows;
-#pragma unroll
-            for (int i = 0; i < kNV; ++i)
-                if (c.has(i)) {
-                    gw[i] = a.gate ? load_params<E>(static_cast<const char *>(a.gate) + gate * a.cols * (a.param_dtype == SO_DTYPE_FP32 ? 4 : 2), c.at(i), a.param_dtype, 1.0f)
-                                   : spread<E>(1.0f);
-                    if (a.pw) gw[i] = gw[i] * load_params<E>(a.pw, c.at(i), a.param_dtype, 1.0f);
-                }
-        }
-        const RowStats st = row_stats(a, row);
-        ring.wait();
-        const auto from = [&](int k, int i) { return from_shared<T, E>(ring.row(k) + c.at(i) * sizeof(T)); };
-        const auto norm = [&](const Vals<E> &v, float mean, float rstd) {
-            return !kLayer ? v * rstd : sizeof(T) == 4 ? (v + -mean) * rstd : fma(v, rstd, -mean * rstd);
-        };
-        Vals<E> sum, dot, e[kNV], hat[kNV], bhat[kNV];
+    const auto norm = [&](const Vals<E> &v, float mean, float rstd) {
+        return !kLayer ? v * rstd : sizeof(T) == 4 ? (v + -mean) * rstd : fma(v, rstd, -mean * rstd);
+    };
+    // first half of a row: e and hat, their sums into v[0] (and v[1])
+    const auto first_half = [&](uint32_t at, const RowStats &st, float *v) {
+        Vals<E> sum, dot;
         sum.set(0.0f), dot.set(0.0f);
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const Vals<E> dy = from(0, i), u = norm(from(1, i), st.mean, st.rstd), q = dy * w[i];
+                const Vals<E> dy = from_shared<T, E>(at + c.at(i) * sizeof(T)), q = dy * w[i];
+                const Vals<E> u = norm(from_shared<T, E>(at + ring.row_bytes + c.at(i) * sizeof(T)), st.mean, st.rstd);
                 if (kLayer) sum = sum + q;
                 dot = fma(q, u, dot);
                 if (kSums) t1[i] = fma(dy, u, t1[i]);
                 if (kSums && kBias) t2[i] = t2[i] + dy;
-                if (kHold) e[i] = q, hat[i] = u;
             }
-        float me_ = 0.0f, meh;
-        if (kLayer) {
-            const float2 r = x.sums(0, total(sum), total(dot));
-            me_ = r.x * a.inv_cols, meh = r.y * a.inv_cols;
-        } else {
-            meh = x.sum(0, total(dot)) * a.inv_cols;
-        }
+        v[0] = total(dot);
+        if (kLayer) v[1] = total(sum);
+    };
+    if (row >= end) return;
+    int64_t gate = row / a.group_rows, gate_end = (gate + 1) * a.group_rows;
+    const auto load_gate = [&]() {
+#pragma unroll
+        for (int i = 0; i < kNV; ++i)
+            if (c.has(i)) {
+                gw[i] = a.gate ? load_params<E>(static_cast<const char *>(a.gate) + gate * a.cols * (a.param_dtype == SO_DTYPE_FP32 ? 4 : 2), c.at(i), a.param_dtype, 1.0f)
+                               : spread<E>(1.0f);
+                if (a.pw) gw[i] = gw[i] * load_params<E>(a.pw, c.at(i), a.param_dtype, 1.0f);
+            }
+    };
+    load_gate();
+    T *dx = static_cast<T *>(a.dx) + row * a.dx_stride, *dblock = static_cast<T *>(a.dblock) + row * a.dblock_stride;
+    RowStats st = row_stats(a, row), next = row + 1 < end ? row_stats(a, row + 1) : st;
+    float v[2 * kEach];                   // sums of a second half, and of the next row's first
+    ring.wait();
+    {
+        float first[2] = {0.0f, 0.0f};
+        first_half(ring.row(0), st, first);
+        x.template sums<2>(0, first);
+        v[kEach] = first[0];
+        if (kLayer) v[2 * kEach - 1] = first[1];
+    }
+    bool lost = false;
+    int turn = 1;                         // exchanges so far
+    for (; row < end; ++row, dx += a.dx_stride, dblock += a.dblock_stride) {
+        const float meh = v[kEach] * a.inv_cols, me_ = kLayer ? v[2 * kEach - 1] * a.inv_cols : 0.0f;
         if (!kSums && a.moments && g.thread == 0) {
             a.moments[row] = me_;
             a.moments[a.rows + row] = meh;
         }
-        // t = dh + rstd (e - me) - rstd meh hat
+        // second half: t = dh + rstd (e - me) - rstd meh hat
         const float c0 = -st.rstd * me_, c1 = -st.rstd * meh;
-        Vals<E> t[kNV];
+        const uint32_t at = ring.row(0);
+        Vals<E> t[kNV], bhat[kNV], sum, dot;
         sum.set(0.0f), dot.set(0.0f);
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const Vals<E> u = kHold ? hat[i] : norm(from(1, i), st.mean, st.rstd), q = kHold ? e[i] : from(0, i) * w[i];
+                const auto from = [&](int k) { return from_shared<T, E>(at + k * ring.row_bytes + c.at(i) * sizeof(T)); };
+                const Vals<E> u = norm(from(1), st.mean, st.rstd), q = from(0) * w[i];
                 t[i] = fma(u, c1, kLayer ? fma(q, st.rstd, c0) : q * st.rstd);
-                if (a.dh) t[i] = t[i] + from(2, i);
+                if (a.dh) t[i] = t[i] + from(2);
                 if (a.needs_block) {
-                    const Vals<E> v = norm(from(3, i), st.pmean, st.prstd), d = t[i] * gw[i];
+                    const Vals<E> d = t[i] * gw[i];
+                    bhat[i] = norm(from(3), st.pmean, st.prstd);
                     if (kLayer) sum = sum + d;
-                    dot = fma(d, v, dot);
-                    if (kSums) s1[i] = fma(t[i], v, s1[i]);
-                    if (kHold) bhat[i] = v;
+                    dot = fma(d, bhat[i], dot);
+                    if (kSums) s1[i] = fma(t[i], bhat[i], s1[i]);
                 }
                 if (kSums && kBias) s2[i] = s2[i] + t[i];
             }
-        // (without a first norm the exchange has nothing to tell but that everyone is done with the first one)
-        float mq = 0.0f, mqb;
-        if (kLayer) {
-            const float2 r = x.sums(1, total(sum), total(dot));
-            mq = r.x * a.inv_cols, mqb = r.y * a.inv_cols;
-        } else {
-            mqb = x.sum(1, total(dot)) * a.inv_cols;
+        v[0] = total(dot);
+        if (kLayer) v[1] = total(sum);
+        const int stage = ring.stage;
+        const RowStats now = st;
+        if (row + 1 < end) {
+            ring.next();
+            st = next;
+            if (row + 2 < end) next = row_stats(a, row + 2);
+            ring.wait();
+            first_half(ring.row(0), st, v + kEach);
         }
+        x.template sums<2 * kEach>(turn++ & 1, v);
         if (ring.gave_up()) {
             lost = true;
             break;
         }
-        if (kHold && g.thread == 0 && row + stages < end) fill(ring.stage, row + stages);
-        T *dx = static_cast<T *>(a.dx) + row * a.dx_stride, *dblock = static_cast<T *>(a.dblock) + row * a.dblock_stride;
-        const float c2 = -st.prstd * mq, c3 = -st.prstd * mqb;
+        if (g.thread == 0 && row + stages < end) fill(stage, row + stages);
+        const float c2 = kLayer ? -now.prstd * v[1] * a.inv_cols : 0.0f, c3 = -now.prstd * v[0] * a.inv_cols;
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
                 *reinterpret_cast<uint4 *>(dx + c.at(i)) = narrow16<T>(t[i] * a.scale);
                 Vals<E> d = t[i] * gw[i];
-                if (a.post) d = fma(kHold ? bhat[i] : norm(from(3, i), st.pmean, st.prstd), c3, kLayer ? fma(d, st.prstd, c2) : d * st.prstd);
+                if (a.post) d = fma(bhat[i], c3, kLayer ? fma(d, now.prstd, c2) : d * now.prstd);
                 *reinterpret_cast<uint4 *>(dblock + c.at(i)) = narrow16<T>(d);
             }
-        if (!kHold) {                     // the block's row has been read a last time
-            if (g.warps > 1) g.sync();
-            else __syncwarp();
-            if (g.thread == 0 && row + stages < end) fill(ring.stage, row + stages);
+        if (row + 1 >= gate_end && row + 1 < end) {
+            // (the sums of dy go by no gate: that of the row ahead may be in this part)
+            if (kSums) leave(gate);
+            gate = (row + 1) / a.group_rows;
+            gate_end = (gate + 1) * a.group_rows;
+            load_gate();
         }
-        ring.next();
     }
     if (!lost) {
-        if (kSums && gate_end > 0) leave(gate);
+        if (kSums) leave(gate);
         return;
     }
     if (g.thread == 0) land(ring.bars, s.issued[g.index], stages);
@@ -915,12 +939,12 @@ Plan plan_rows(int64_t vectors, int most_nv, int least_nv = 1)
     return best;
 }
 
-constexpr int kRingBytes = 100 * 1024;    // of a block's ring, if two stages fit there
+constexpr int kRingBytes = 100 * 1024;    // of a block's ring, or twice that where only one block of threads fits an SM
 constexpr int kMostShared = 220 * 1024;
 
-int ring_stages(size_t stage_bytes, int groups)
+int ring_stages(size_t stage_bytes, int groups, int block)
 {
-    int stages = (int)(kRingBytes / stage_bytes);
+    int stages = (int)((block > 256 ? 2 : 1) * kRingBytes / stage_bytes);
     stages = stages > 4 ? 4 : stages < 2 ? 2 : stages;
     return stages < kRingBars / groups ? stages : kRingBars / groups;
 }
@@ -932,7 +956,7 @@ so_status launch_ring(K kernel, std::atomic<uint64_t> (&cache)[kMaxDevices], Arg
 {
     const int groups = p.block / p.per_row;
     const size_t stage = (size_t)a.cols * size * mats * groups;
-    const int stages = ring_stages(stage, groups);
+    const int stages = ring_stages(stage, groups, p.block);
     const size_t smem = stage * stages;
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return SO_ERR_CUDA;
@@ -958,10 +982,11 @@ so_status launch_ring(K kernel, std::atomic<uint64_t> (&cache)[kMaxDevices], Arg
 template <typename T, Form kForm, int kNV>
 so_status forward_ring(Args &a, const Plan &p, int sms, cudaStream_t st)
 {
-    static std::atomic<uint64_t> cache[3][kMaxDevices];
+    static std::atomic<uint64_t> cache[4][kMaxDevices];
     const bool full = (int64_t)p.per_row * p.nv * Vec<T>::kElems == a.cols;
     if (p.block <= 256 && full) return launch_ring(forward_ring_kernel<T, kForm, kNV, true, 256>, cache[0], a, p, 2, sizeof(T), INT64_MAX, sms, st);
     if (p.block <= 256) return launch_ring(forward_ring_kernel<T, kForm, kNV, false, 256>, cache[1], a, p, 2, sizeof(T), INT64_MAX, sms, st);
+    if (full) return launch_ring(forward_ring_kernel<T, kForm, kNV, true, 512>, cache[3], a, p, 2, sizeof(T), INT64_MAX, sms, st);
     return launch_ring(forward_ring_kernel<T, kForm, kNV, false, 512>, cache[2], a, p, 2, sizeof(T), INT64_MAX, sms, st);
 }
 
@@ -983,10 +1008,11 @@ so_status forward(Args &a, bool vec, int sms, cudaStream_t st)
 template <typename T, Form kForm, bool kSums, int kNV>
 so_status backward_ring(Args &a, const Plan &p, int64_t most, int sms, cudaStream_t st)
 {
-    static std::atomic<uint64_t> cache[3][kMaxDevices];
+    static std::atomic<uint64_t> cache[4][kMaxDevices];
     const bool full = (int64_t)p.per_row * p.nv * Vec<T>::kElems == a.cols;
     if (p.block <= 256 && full) return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, true, 256>, cache[0], a, p, 4, sizeof(T), most, sms, st);
     if (p.block <= 256) return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, false, 256>, cache[1], a, p, 4, sizeof(T), most, sms, st);
+    if (full) return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, true, 512>, cache[3], a, p, 4, sizeof(T), most, sms, st);
     return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, false, 512>, cache[2], a, p, 4, sizeof(T), most, sms, st);
 }
 
