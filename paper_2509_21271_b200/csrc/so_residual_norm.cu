@@ -27,6 +27,7 @@ struct Args {
     int64_t x_stride, block_stride, dy_stride, dh_stride, h_stride, y_stride, dx_stride, dblock_stride;
     int64_t rows, cols, group_rows;       // rows that share a gate
     int32_t param_dtype, post;
+    int32_t combine;                      // backward: one gate, and several groups of threads to a block
     int32_t needs_block;                  // backward: the first norm, or a sum, goes by the block
     float scale, eps, inv_cols;
     int64_t each;                         // consecutive rows of a group of threads (or of a part of the column sums)
@@ -272,6 +273,78 @@ __global__ void __launch_bounds__(kLoopThreads) backward_loop_kernel(const __gri
 // A copy that does not arrive in time turns the rows that the group has not written into NaN,
 // statistics and gradients of parameters included.
 
+// E values one by one.  Pairs (Vals) halve the arithmetic's instructions, but a row's scalars have to be
+// paired with themselves and registers come in twos: 32768 x 4096 bf16 forward takes 195 us with
+// pairs and 173 us without, backward with sums 186 us with pairs and 195 us without.
+template <int E> struct Floats {
+    float f[E];
+    __device__ __forceinline__ void set(float x)
+    {
+#pragma unroll
+        for (int i = 0; i < E; ++i) f[i] = x;
+    }
+    __device__ __forceinline__ void get(float (&o)[E]) const
+    {
+#pragma unroll
+        for (int i = 0; i < E; ++i) o[i] = f[i];
+    }
+    __device__ __forceinline__ void put(const float (&o)[E])
+    {
+#pragma unroll
+        for (int i = 0; i < E; ++i) f[i] = o[i];
+    }
+};
+#define SO_EACH(expr) do { _Pragma("unroll") for (int i = 0; i < E; ++i) r.f[i] = (expr); return r; } while (0)
+template <int E> __device__ __forceinline__ Floats<E> operator+(const Floats<E> &a, const Floats<E> &b) { Floats<E> r; SO_EACH(a.f[i] + b.f[i]); }
+template <int E> __device__ __forceinline__ Floats<E> operator+(const Floats<E> &a, float b) { Floats<E> r; SO_EACH(a.f[i] + b); }
+template <int E> __device__ __forceinline__ Floats<E> operator*(const Floats<E> &a, const Floats<E> &b) { Floats<E> r; SO_EACH(a.f[i] * b.f[i]); }
+template <int E> __device__ __forceinline__ Floats<E> operator*(const Floats<E> &a, float b) { Floats<E> r; SO_EACH(a.f[i] * b); }
+template <int E> __device__ __forceinline__ Floats<E> fma(const Floats<E> &a, const Floats<E> &b, const Floats<E> &c) { Floats<E> r; SO_EACH(fmaf(a.f[i], b.f[i], c.f[i])); }
+template <int E> __device__ __forceinline__ Floats<E> fma(const Floats<E> &a, float b, const Floats<E> &c) { Floats<E> r; SO_EACH(fmaf(a.f[i], b, c.f[i])); }
+template <int E> __device__ __forceinline__ Floats<E> fma(const Floats<E> &a, float b, float c) { Floats<E> r; SO_EACH(fmaf(a.f[i], b, c)); }
+#undef SO_EACH
+template <int E> __device__ __forceinline__ float total(const Floats<E> &a)
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) s += a.f[i];
+    return s;
+}
+
+// V: Vals<E> or Floats<E>, E elements of 16 bytes of T
+template <typename V, typename T> __device__ __forceinline__ V widen_as(const uint4 &bits)
+{
+    V v;
+    if constexpr (std::is_same<V, Vals<Vec<T>::kElems>>::value) {
+        v = widen16<T>(bits);
+    } else {
+        float f[Vec<T>::kElems];
+        unpack<T>(bits, f);
+        v.put(f);
+    }
+    return v;
+}
+template <typename T, typename V> __device__ __forceinline__ uint4 narrow(const V &v)
+{
+    float f[Vec<T>::kElems];
+    v.get(f);
+    return pack<T>(f);
+}
+template <typename V> __device__ __forceinline__ V all(float x)
+{
+    V v;
+    v.set(x);
+    return v;
+}
+template <typename V, int E> __device__ __forceinline__ V params_as(const void *p, int64_t at, int32_t dtype, float fill)
+{
+    float f[E];
+    params_at<E>(p, at, dtype, fill, f);
+    V v;
+    v.put(f);
+    return v;
+}
+
 constexpr int kRingBars = 64;             // groups x stages of a block, at most
 constexpr int kMaxWarps = 16;             // of a group
 
@@ -389,11 +462,11 @@ struct Exchange {
 //   D = sum n_t (m_t - c),  Q = sum (Q_t + n_t (m_t - c)^2),
 // so that its mean is c + D / n, and its squares around that Q - D^2 / n; warps are joined by
 // M2 = sum (M2_w + n_w (mean_w - mean)^2).
-template <bool kLayer, typename T, int E, int kNV, bool kFull>
-__device__ __forceinline__ float2 row_statistics(const Columns<T, E, kNV, kFull> &c, const Exchange &x, int k, const float *count, const Vals<E> (&f)[kNV],
+template <bool kLayer, typename V, typename T, int E, int kNV, bool kFull>
+__device__ __forceinline__ float2 row_statistics(const Columns<T, E, kNV, kFull> &c, const Exchange &x, int k, const float *count, const V (&f)[kNV],
                                                  float inv_mine, float inv_warp, float inv_cols, float eps)
 {
-    Vals<E> acc;
+    V acc;
     acc.set(0.0f);
     if constexpr (!kLayer) {
 #pragma unroll
@@ -409,7 +482,7 @@ __device__ __forceinline__ float2 row_statistics(const Columns<T, E, kNV, kFull>
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const Vals<E> d = f[i] + -m;
+                const V d = f[i] + -m;
                 acc = fma(d, d, acc);
             }
         const float centre = __shfl_sync(0xFFFFFFFFu, m, 0), d = kFull || c.mine > 0.0f ? m - centre : 0.0f;
@@ -477,9 +550,10 @@ struct Ring {
 
 // Bound: memory (two reads, two writes).
 template <typename T, Form kForm, int kNV, bool kFull, int kMaxThreads>
-__global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forward_ring_kernel(const __grid_constant__ Args a, int per_row, int stages)
+__global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 && kNV * Vec<T>::kElems <= 16 ? 2 : 1) forward_ring_kernel(const __grid_constant__ Args a, int per_row, int stages)
 {
     constexpr int E = Vec<T>::kElems;
+    using V = Floats<E>;
     constexpr bool kLayer = kForm == kLayerNorm, kBias = kForm != kPlainRms;
     extern __shared__ __align__(128) uint8_t s_room[];
     __shared__ __align__(8) RingShared s;
@@ -500,12 +574,12 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forwa
     };
     if (g.thread == 0)
         for (int n = 0; n < stages && row + n < end; ++n) fill(n, row + n);
-    Vals<E> w[kNV], b[kNV], gw[kNV], gb[kNV];                // gw, gb: gate times the first norm's
+    V w[kNV], b[kNV], gw[kNV], gb[kNV];                // gw, gb: gate times the first norm's
 #pragma unroll
     for (int i = 0; i < kNV; ++i)
         if (c.has(i)) {
-            w[i] = load_params<E>(a.w, c.at(i), a.param_dtype, 1.0f);
-            if (kBias) b[i] = load_params<E>(a.b, c.at(i), a.param_dtype, 0.0f);
+            w[i] = params_as<V, E>(a.w, c.at(i), a.param_dtype, 1.0f);
+            if (kBias) b[i] = params_as<V, E>(a.b, c.at(i), a.param_dtype, 0.0f);
         }
     int64_t gate_end = 0;
     T *h = static_cast<T *>(a.h) + row * a.h_stride, *y = static_cast<T *>(a.y) + row * a.y_stride;
@@ -516,29 +590,29 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forwa
 #pragma unroll
             for (int i = 0; i < kNV; ++i)
                 if (c.has(i)) {
-                    gw[i] = a.gate ? load_params<E>(static_cast<const char *>(a.gate) + gate * a.cols * (a.param_dtype == SO_DTYPE_FP32 ? 4 : 2), c.at(i), a.param_dtype, 1.0f)
-                                   : spread<E>(1.0f);
-                    if (kBias) gb[i] = a.pb ? gw[i] * load_params<E>(a.pb, c.at(i), a.param_dtype, 0.0f) : spread<E>(0.0f);
-                    if (a.pw) gw[i] = gw[i] * load_params<E>(a.pw, c.at(i), a.param_dtype, 1.0f);
+                    gw[i] = a.gate ? params_as<V, E>(static_cast<const char *>(a.gate) + gate * a.cols * (a.param_dtype == SO_DTYPE_FP32 ? 4 : 2), c.at(i), a.param_dtype, 1.0f)
+                                   : all<V>(1.0f);
+                    if (kBias) gb[i] = a.pb ? gw[i] * params_as<V, E>(a.pb, c.at(i), a.param_dtype, 0.0f) : all<V>(0.0f);
+                    if (a.pw) gw[i] = gw[i] * params_as<V, E>(a.pw, c.at(i), a.param_dtype, 1.0f);
                 }
         }
         ring.wait();
         float2 post = make_float2(0.0f, 1.0f);
-        Vals<E> f[kNV];
+        V f[kNV];
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
-            if (c.has(i)) f[i] = from_shared<T, E>(ring.row(1) + c.at(i) * sizeof(T));
+            if (c.has(i)) f[i] = widen_as<V, T>(lds16(ring.row(1) + c.at(i) * sizeof(T)));
         if (a.post) post = row_statistics<kLayer>(c, x, 0, count, f, inv_mine, inv_warp, a.inv_cols, a.eps);
         const float shift = -post.x * post.y;
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const Vals<E> from = from_shared<T, E>(ring.row(0) + c.at(i) * sizeof(T));
+                const V from = widen_as<V, T>(lds16(ring.row(0) + c.at(i) * sizeof(T)));
                 // in fp32 the mean is taken off first: rows far from zero keep their digits
-                const Vals<E> hat = !kLayer ? f[i] * post.y : sizeof(T) == 4 ? (f[i] + -post.x) * post.y : fma(f[i], post.y, shift);
-                const uint4 bits = narrow16<T>(fma(gw[i], hat, kBias ? fma(from, a.scale, gb[i]) : from * a.scale));
+                const V hat = !kLayer ? f[i] * post.y : sizeof(T) == 4 ? (f[i] + -post.x) * post.y : fma(f[i], post.y, shift);
+                const uint4 bits = narrow<T>(fma(gw[i], hat, kBias ? fma(from, a.scale, gb[i]) : from * a.scale));
                 *reinterpret_cast<uint4 *>(h + c.at(i)) = bits;
-                f[i] = widen16<T>(bits);
+                f[i] = widen_as<V, T>(bits);
             }
         const float2 st = row_statistics<kLayer>(c, x, 1, count, f, inv_mine, inv_warp, a.inv_cols, a.eps);
         if (ring.gave_up()) break;
@@ -555,8 +629,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forwa
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const Vals<E> hat = !kLayer ? f[i] * st.y : sizeof(T) == 4 ? (f[i] + -st.x) * st.y : fma(f[i], st.y, back);
-                *reinterpret_cast<uint4 *>(y + c.at(i)) = narrow16<T>(kBias ? fma(hat, w[i], b[i]) : hat * w[i]);
+                const V hat = !kLayer ? f[i] * st.y : sizeof(T) == 4 ? (f[i] + -st.x) * st.y : fma(f[i], st.y, back);
+                *reinterpret_cast<uint4 *>(y + c.at(i)) = narrow<T>(kBias ? fma(hat, w[i], b[i]) : hat * w[i]);
             }
         ring.next();
         // one exchange a row: its place must not be written again before all have read it
@@ -564,7 +638,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forwa
     }
     if (row >= end) return;
     if (g.thread == 0) land(ring.bars, s.issued[g.index], stages);
-    const uint4 nan = narrow16<T>(spread<E>(kNan));
+    const uint4 nan = narrow<T>(all<V>(kNan));
     for (; row < end; ++row, h += a.h_stride, y += a.y_stride) {
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
@@ -585,9 +659,10 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) forwa
 //
 // Bound: memory (four reads, two writes).
 template <typename T, Form kForm, bool kSums, int kNV, bool kFull, int kMaxThreads>
-__global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backward_ring_kernel(const __grid_constant__ Args a, int per_row, int stages)
+__global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 && kNV * Vec<T>::kElems <= 8 ? 2 : 1) backward_ring_kernel(const __grid_constant__ Args a, int per_row, int stages)
 {
     constexpr int E = Vec<T>::kElems;
+    using V = typename std::conditional<kMaxThreads == 512, Floats<E>, Vals<E>>::type;   // (pairs spill at 128 registers)
     constexpr bool kLayer = kForm == kLayerNorm, kBias = kForm != kPlainRms;
     constexpr int kEach = kLayer ? 2 : 1;                    // sums of half a row
     extern __shared__ __align__(128) uint8_t s_room[];
@@ -609,10 +684,10 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
     };
     if (g.thread == 0)
         for (int n = 0; n < stages && row + n < end; ++n) fill(n, row + n);
-    Vals<E> w[kNV], gw[kNV], s1[kNV], s2[kNV], t1[kNV], t2[kNV];   // gw: gate times the first norm's weight
+    V w[kNV], gw[kNV], s1[kNV], s2[kNV], t1[kNV], t2[kNV];   // gw: gate times the first norm's weight
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
-        if (c.has(i)) w[i] = load_params<E>(a.w, c.at(i), a.param_dtype, 1.0f);
+        if (c.has(i)) w[i] = params_as<V, E>(a.w, c.at(i), a.param_dtype, 1.0f);
         if (kSums) s1[i].set(0.0f), s2[i].set(0.0f), t1[i].set(0.0f), t2[i].set(0.0f);
     }
     const auto leave = [&](int64_t gate) {
@@ -620,7 +695,7 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                Vals<E> *const v[4] = {&s1[i], &s2[i], &t1[i], &t2[i]};
+                V *const v[4] = {&s1[i], &s2[i], &t1[i], &t2[i]};
 #pragma unroll
                 for (int k = 0; k < 4; k += kBias ? 1 : 2) {
                     float f[E];
@@ -632,18 +707,18 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
                 }
             }
     };
-    const auto norm = [&](const Vals<E> &v, float mean, float rstd) {
+    const auto norm = [&](const V &v, float mean, float rstd) {
         return !kLayer ? v * rstd : sizeof(T) == 4 ? (v + -mean) * rstd : fma(v, rstd, -mean * rstd);
     };
     // first half of a row: e and hat, their sums into v[0] (and v[1])
     const auto first_half = [&](uint32_t at, const RowStats &st, float *v) {
-        Vals<E> sum, dot;
+        V sum, dot;
         sum.set(0.0f), dot.set(0.0f);
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const Vals<E> dy = from_shared<T, E>(at + c.at(i) * sizeof(T)), q = dy * w[i];
-                const Vals<E> u = norm(from_shared<T, E>(at + ring.row_bytes + c.at(i) * sizeof(T)), st.mean, st.rstd);
+                const V dy = widen_as<V, T>(lds16(at + c.at(i) * sizeof(T))), q = dy * w[i];
+                const V u = norm(widen_as<V, T>(lds16(at + ring.row_bytes + c.at(i) * sizeof(T))), st.mean, st.rstd);
                 if (kLayer) sum = sum + q;
                 dot = fma(q, u, dot);
                 if (kSums) t1[i] = fma(dy, u, t1[i]);
@@ -652,23 +727,26 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
         v[0] = total(dot);
         if (kLayer) v[1] = total(sum);
     };
-    if (row >= end) return;
+    const bool any = row < end;           // (the last blocks may have groups without rows)
+    if (!any && !a.combine) return;
     int64_t gate = row / a.group_rows, gate_end = (gate + 1) * a.group_rows;
     const auto load_gate = [&]() {
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                gw[i] = a.gate ? load_params<E>(static_cast<const char *>(a.gate) + gate * a.cols * (a.param_dtype == SO_DTYPE_FP32 ? 4 : 2), c.at(i), a.param_dtype, 1.0f)
-                               : spread<E>(1.0f);
-                if (a.pw) gw[i] = gw[i] * load_params<E>(a.pw, c.at(i), a.param_dtype, 1.0f);
+                gw[i] = a.gate ? params_as<V, E>(static_cast<const char *>(a.gate) + gate * a.cols * (a.param_dtype == SO_DTYPE_FP32 ? 4 : 2), c.at(i), a.param_dtype, 1.0f)
+                               : all<V>(1.0f);
+                if (a.pw) gw[i] = gw[i] * params_as<V, E>(a.pw, c.at(i), a.param_dtype, 1.0f);
             }
     };
-    load_gate();
+    if (any) load_gate();
     T *dx = static_cast<T *>(a.dx) + row * a.dx_stride, *dblock = static_cast<T *>(a.dblock) + row * a.dblock_stride;
-    RowStats st = row_stats(a, row), next = row + 1 < end ? row_stats(a, row + 1) : st;
+    RowStats st = {}, next = {};
     float v[2 * kEach];                   // sums of a second half, and of the next row's first
-    ring.wait();
-    {
+    if (any) {
+        st = row_stats(a, row);
+        if (row + 1 < end) next = row_stats(a, row + 1);
+        ring.wait();
         float first[2] = {0.0f, 0.0f};
         first_half(ring.row(0), st, first);
         x.template sums<2>(0, first);
@@ -686,17 +764,17 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
         // second half: t = dh + rstd (e - me) - rstd meh hat
         const float c0 = -st.rstd * me_, c1 = -st.rstd * meh;
         const uint32_t at = ring.row(0);
-        Vals<E> t[kNV], bhat[kNV], sum, dot;
+        V t[kNV], bhat[kNV], sum, dot;
         sum.set(0.0f), dot.set(0.0f);
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                const auto from = [&](int k) { return from_shared<T, E>(at + k * ring.row_bytes + c.at(i) * sizeof(T)); };
-                const Vals<E> u = norm(from(1), st.mean, st.rstd), q = from(0) * w[i];
+                const auto from = [&](int k) { return widen_as<V, T>(lds16(at + k * ring.row_bytes + c.at(i) * sizeof(T))); };
+                const V u = norm(from(1), st.mean, st.rstd), q = from(0) * w[i];
                 t[i] = fma(u, c1, kLayer ? fma(q, st.rstd, c0) : q * st.rstd);
                 if (a.dh) t[i] = t[i] + from(2);
                 if (a.needs_block) {
-                    const Vals<E> d = t[i] * gw[i];
+                    const V d = t[i] * gw[i];
                     bhat[i] = norm(from(3), st.pmean, st.prstd);
                     if (kLayer) sum = sum + d;
                     dot = fma(d, bhat[i], dot);
@@ -725,10 +803,10 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
             if (c.has(i)) {
-                *reinterpret_cast<uint4 *>(dx + c.at(i)) = narrow16<T>(t[i] * a.scale);
-                Vals<E> d = t[i] * gw[i];
+                *reinterpret_cast<uint4 *>(dx + c.at(i)) = narrow<T>(t[i] * a.scale);
+                V d = t[i] * gw[i];
                 if (a.post) d = fma(bhat[i], c3, kLayer ? fma(d, now.prstd, c2) : d * now.prstd);
-                *reinterpret_cast<uint4 *>(dblock + c.at(i)) = narrow16<T>(d);
+                *reinterpret_cast<uint4 *>(dblock + c.at(i)) = narrow<T>(d);
             }
         if (row + 1 >= gate_end && row + 1 < end) {
             // (the sums of dy go by no gate: that of the row ahead may be in this part)
@@ -738,18 +816,51 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 ? 2 : 1) backw
             load_gate();
         }
     }
-    if (!lost) {
-        if (kSums) leave(gate);
-        return;
-    }
-    if (g.thread == 0) land(ring.bars, s.issued[g.index], stages);
-    if (kSums)
-        for (const int64_t last = (end - 1) / a.group_rows; gate <= last; ++gate) {
+    if (lost) {
+        if (g.thread == 0) land(ring.bars, s.issued[g.index], stages);
 #pragma unroll
-            for (int i = 0; i < kNV; ++i) s1[i].set(kNan), s2[i].set(kNan), t1[i].set(kNan), t2[i].set(kNan);
-            leave(gate);
+        for (int i = 0; i < kNV; ++i)
+            if (kSums) s1[i].set(kNan), s2[i].set(kNan), t1[i].set(kNan), t2[i].set(kNan);
+    }
+    if (kSums && !a.combine) {
+        leave(gate);
+        if (lost)
+            for (const int64_t last = (end - 1) / a.group_rows; gate < last;) {
+#pragma unroll
+                for (int i = 0; i < kNV; ++i) s1[i].set(kNan), s2[i].set(kNan), t1[i].set(kNan), t2[i].set(kNan);
+                leave(++gate);
+            }
+    } else if (kSums) {
+        // one gate: the block's groups add up in shared memory, one after the other, and leave one part
+        float *room = reinterpret_cast<float *>(s_room);
+        for (int k = 0; k < g.per_block; ++k) {
+            __syncthreads();              // (first of all: nobody reads a row there any more)
+            if (k != g.index) continue;
+            float *out = a.partials + (int64_t)blockIdx.x * 4 * a.cols;
+#pragma unroll
+            for (int i = 0; i < kNV; ++i)
+                if (c.has(i)) {
+                    V *const sums[4] = {&s1[i], &s2[i], &t1[i], &t2[i]};
+#pragma unroll
+                    for (int n = 0; n < 4; n += kBias ? 1 : 2) {
+                        float f[E];
+                        sums[n]->get(f);
+#pragma unroll
+                        for (int j = 0; j < E; j += 4) {
+                            const int64_t at = n * a.cols + c.at(i) + j;
+                            float4 q = make_float4(f[j], f[j + 1], f[j + 2], f[j + 3]);
+                            if (k > 0) {
+                                const float4 o = *reinterpret_cast<const float4 *>(room + at);
+                                q.x += o.x, q.y += o.y, q.z += o.z, q.w += o.w;
+                            }
+                            *reinterpret_cast<float4 *>((k + 1 == g.per_block ? out : room) + at) = q;
+                        }
+                    }
+                }
         }
-    const uint4 nan = narrow16<T>(spread<E>(kNan));
+    }
+    if (!lost) return;
+    const uint4 nan = narrow<T>(all<V>(kNan));
     for (; row < end; ++row) {
 #pragma unroll
         for (int i = 0; i < kNV; ++i)
@@ -925,14 +1036,15 @@ so_status common(int64_t rows, int64_t cols, int64_t groups, int32_t dtype, int3
 // How a row is dealt out: `per_row` threads with `nv` vectors each, blocks of `block`; 0: by the loop.
 struct Plan { int per_row, nv, block; };
 
-// The choice that leaves the fewest lanes idle, and the most vectors a thread of equals.
-Plan plan_rows(int64_t vectors, int most_nv, int least_nv = 1)
+// The choice that leaves the fewest lanes idle, and the most vectors a thread of equals (fewer warps
+// share a row): `least`, twice or three times that many vectors, the latter two for blocks of 256 and 512.
+Plan plan_rows(int64_t vectors, int least, int most = 0, bool wide = true)
 {
     Plan best = {0, 0, 0};
     int64_t waste = INT64_MAX;
-    for (int nv = most_nv; nv >= least_nv; nv /= 2) {
+    for (int nv = most ? most : 3 * least; nv >= least; nv -= least) {
         const int64_t threads = ((vectors + nv - 1) / nv + 31) / 32 * 32, idle = threads * nv - vectors;
-        if (threads > 32 * kMaxWarps || idle >= waste) continue;
+        if (threads > (wide && (nv == 2 * least || most) ? 32 * kMaxWarps : 256) || idle >= waste) continue;
         waste = idle;
         best = {(int)threads, nv, threads >= 256 ? (int)threads : (int)(256 / threads * threads)};
     }
@@ -976,7 +1088,10 @@ so_status launch_ring(K kernel, std::atomic<uint64_t> (&cache)[kMaxDevices], Arg
     if (units < groups) units = groups;
     a.each = (a.rows + units - 1) / units;
     const int64_t used = (a.rows + a.each - 1) / a.each;
-    return launch(kernel, (unsigned)((used + groups - 1) / groups), p.block, smem, st, false, a, p.per_row, stages);
+    a.combine = a.combine && groups > 1;
+    const so_status done = launch(kernel, (unsigned)((used + groups - 1) / groups), p.block, smem, st, false, a, p.per_row, stages);
+    if (a.combine) a.each *= groups;      // of a part
+    return done;
 }
 
 template <typename T, Form kForm, int kNV>
@@ -986,8 +1101,11 @@ so_status forward_ring(Args &a, const Plan &p, int sms, cudaStream_t st)
     const bool full = (int64_t)p.per_row * p.nv * Vec<T>::kElems == a.cols;
     if (p.block <= 256 && full) return launch_ring(forward_ring_kernel<T, kForm, kNV, true, 256>, cache[0], a, p, 2, sizeof(T), INT64_MAX, sms, st);
     if (p.block <= 256) return launch_ring(forward_ring_kernel<T, kForm, kNV, false, 256>, cache[1], a, p, 2, sizeof(T), INT64_MAX, sms, st);
-    if (full) return launch_ring(forward_ring_kernel<T, kForm, kNV, true, 512>, cache[3], a, p, 2, sizeof(T), INT64_MAX, sms, st);
-    return launch_ring(forward_ring_kernel<T, kForm, kNV, false, 512>, cache[2], a, p, 2, sizeof(T), INT64_MAX, sms, st);
+    if constexpr (kNV * Vec<T>::kElems == 16) {
+        if (full) return launch_ring(forward_ring_kernel<T, kForm, kNV, true, 512>, cache[2], a, p, 2, sizeof(T), INT64_MAX, sms, st);
+        return launch_ring(forward_ring_kernel<T, kForm, kNV, false, 512>, cache[3], a, p, 2, sizeof(T), INT64_MAX, sms, st);
+    }
+    return SO_ERR_INVALID_ARG;            // no plan has long rows of other vectors
 }
 
 template <typename T, Form kForm>
@@ -995,25 +1113,38 @@ so_status forward(Args &a, bool vec, int sms, cudaStream_t st)
 {
     constexpr int E = Vec<T>::kElems;
     constexpr bool kLayer = kForm == kLayerNorm;
-    constexpr int kMost = 16 / E;         // 16 elements a thread, or half as many
     if (vec && a.cols * (int64_t)sizeof(T) * 2 * 2 <= kMostShared) {
-        const Plan p = plan_rows(a.cols / E, kMost);
-        if (p.nv == kMost) return forward_ring<T, kForm, kMost>(a, p, sms, st);
-        if (p.nv == kMost / 2) return forward_ring<T, kForm, kMost / 2>(a, p, sms, st);
+        const Plan p = plan_rows(a.cols / E, 8 / E);
+        if (p.nv == 24 / E) return forward_ring<T, kForm, 24 / E>(a, p, sms, st);
+        if (p.nv == 16 / E) return forward_ring<T, kForm, 16 / E>(a, p, sms, st);
+        if (p.nv == 8 / E) return forward_ring<T, kForm, 8 / E>(a, p, sms, st);
     }
     const unsigned grid = (unsigned)(a.rows < 8 * sms ? a.rows : 8 * sms);
     return launch(vec ? forward_loop_kernel<T, E, kLayer> : forward_loop_kernel<T, 1, kLayer>, grid, kLoopThreads, 0, st, false, a);
 }
 
-template <typename T, Form kForm, bool kSums, int kNV>
+template <typename T, Form kForm, int kNV>
 so_status backward_ring(Args &a, const Plan &p, int64_t most, int sms, cudaStream_t st)
 {
     static std::atomic<uint64_t> cache[4][kMaxDevices];
     const bool full = (int64_t)p.per_row * p.nv * Vec<T>::kElems == a.cols;
-    if (p.block <= 256 && full) return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, true, 256>, cache[0], a, p, 4, sizeof(T), most, sms, st);
-    if (p.block <= 256) return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, false, 256>, cache[1], a, p, 4, sizeof(T), most, sms, st);
-    if (full) return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, true, 512>, cache[3], a, p, 4, sizeof(T), most, sms, st);
-    return launch_ring(backward_ring_kernel<T, kForm, kSums, kNV, false, 512>, cache[2], a, p, 4, sizeof(T), most, sms, st);
+    if (p.block <= 256 && full) return launch_ring(backward_ring_kernel<T, kForm, true, kNV, true, 256>, cache[0], a, p, 4, sizeof(T), most, sms, st);
+    if (p.block <= 256) return launch_ring(backward_ring_kernel<T, kForm, true, kNV, false, 256>, cache[1], a, p, 4, sizeof(T), most, sms, st);
+    if constexpr (kNV * Vec<T>::kElems == 16 && kForm == kPlainRms) {
+        if (full) return launch_ring(backward_ring_kernel<T, kForm, true, kNV, true, 512>, cache[2], a, p, 4, sizeof(T), most, sms, st);
+        return launch_ring(backward_ring_kernel<T, kForm, true, kNV, false, 512>, cache[3], a, p, 4, sizeof(T), most, sms, st);
+    }
+    return SO_ERR_INVALID_ARG;            // no plan has long rows of other vectors
+}
+
+// Without sums: 16 elements a thread.
+template <typename T, Form kForm>
+so_status backward_rows(Args &a, const Plan &p, int sms, cudaStream_t st)
+{
+    constexpr int kNV = 16 / Vec<T>::kElems;
+    static std::atomic<uint64_t> cache[2][kMaxDevices];
+    if (p.block <= 256) return launch_ring(backward_ring_kernel<T, kForm, false, kNV, false, 256>, cache[0], a, p, 4, sizeof(T), INT64_MAX, sms, st);
+    return launch_ring(backward_ring_kernel<T, kForm, false, kNV, false, 512>, cache[1], a, p, 4, sizeof(T), INT64_MAX, sms, st);
 }
 
 template <typename T, Form kForm>
@@ -1023,18 +1154,24 @@ so_status backward(Args &a, const Grads &g, bool sums, bool vec, int sms, cudaSt
     constexpr bool kLayer = kForm == kLayerNorm;
     const int64_t most = most_parts(a.rows, a.cols);
     a.each = 1;
+    a.combine = a.group_rows == a.rows;
     a.needs_block = a.post || (sums && (g.dgate || g.dpw || g.dpb));
     bool taken = false;                   // the rows' kernel has left the parts of the sums
     if (a.rows > 0) {
         const bool ring = vec && a.cols * (int64_t)sizeof(T) * 4 * 2 <= kMostShared;
-        // with sums 8 elements a thread, without 16
-        const Plan with = ring && sums ? plan_rows(a.cols / E, 8 / E, 8 / E) : Plan{0, 0, 0}, without = ring ? plan_rows(a.cols / E, 16 / E, 16 / E) : Plan{0, 0, 0};
+        // with sums 512 threads have registers for those of the plain form alone (8192 x 8192 bf16: 220 us;
+        // layer norm 559 us, against 383 us with sums of their own)
+        const Plan with = ring && sums ? plan_rows(a.cols / E, 8 / E, 0, kForm == kPlainRms) : Plan{0, 0, 0};
+        const Plan without = ring ? plan_rows(a.cols / E, 16 / E, 16 / E) : Plan{0, 0, 0};
         so_status s;
         if (with.nv) {
             taken = true;
-            s = backward_ring<T, kForm, true, 8 / E>(a, with, most, sms, st);
+            s = with.nv == 24 / E   ? backward_ring<T, kForm, 24 / E>(a, with, most, sms, st)
+                : with.nv == 16 / E ? backward_ring<T, kForm, 16 / E>(a, with, most, sms, st)
+                                    : backward_ring<T, kForm, 8 / E>(a, with, most, sms, st);
         } else if (without.nv) {
-            s = backward_ring<T, kForm, false, 16 / E>(a, without, INT64_MAX, sms, st);
+            a.combine = 0;
+            s = backward_rows<T, kForm>(a, without, sms, st);
         } else {
             const unsigned grid = (unsigned)(a.rows < 8 * sms ? a.rows : 8 * sms);
             s = launch(vec ? backward_loop_kernel<T, E, kLayer> : backward_loop_kernel<T, 1, kLayer>, grid, kLoopThreads, 0, st, false, a);

@@ -333,7 +333,7 @@ def test_rows_whose_copies_do_not_arrive(rows, cols, dtype, groups, kind):
             assert torch.isnan(a[gone]).all() and same_bits(a[~gone], b[~gone])
         assert torch.isnan(lost[2]).any()
         for name, a, b in zip(NAMES[3:], lost[3:], grads[3:]):
-            # wide rows have sums of their own, of which those of dy alone need nothing of what was lost
+            # wide rows with biases have sums of their own, of which those of dy alone need nothing of what was lost
             if a is not None and cols == 8192 and name in ("dweight", "dbias"):
                 assert same_bits(a, b)
             elif a is not None:
