@@ -4,7 +4,7 @@
 //   m' = beta1 m + (1 - beta1) g,     v' = beta2 v + (1 - beta2) g g
 //   p' = p - (lr wd p + lr / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps))
 //
-// in fp32, every operation rounded by itself (no contraction).  The moments lie in arenas
+// in fp32, m and v with every operation rounded by itself (no contraction).  The moments lie in arenas
 // of the optimizer, each tensor's from a block of 256 elements on.
 //
 // An 8-bit moment has 4 bits of fraction and, for m, 3 bits of exponent and a sign, for v,
@@ -242,17 +242,38 @@ struct Step {
     int32_t run, stochastic;
 };
 
-// Values of 8 codes in units of 2^-4 of the block's scale, times `factor`.
+// One step of an element.  m and v operation by operation (packed pairs of operations come out
+// fused, although they name their rounding); the square root and the quotient are the hardware's,
+// good to 2^-22 together; a second moment below 2^-126 counts as 0 there.
+struct Update {
+    float factor, beta1, omb1, beta2, omb2, rsqrt_bc2, eps, decay, step;
+    __device__ __forceinline__ void operator()(float grad, float &m, float &v, float &p) const
+    {
+        const float g = __fmul_rn(grad, factor);
+        m = __fadd_rn(__fmul_rn(m, beta1), __fmul_rn(g, omb1));
+        v = __fadd_rn(__fmul_rn(v, beta2), __fmul_rn(__fmul_rn(g, omb2), g));
+        float root, inverse;
+        asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(fmaf(root, rsqrt_bc2, eps)));
+        p = fmaf(__fmul_rn(m, inverse), -step, fmaf(p, -decay, p));
+    }
+};
+
+// What 8 codes stand for.  As the top bits of binary16 numbers they are multiples of 2^-18, from
+// its subnormal numbers on; so two at a time go through binary16 to fp32.
 template <bool kSigned>
 __device__ __forceinline__ void decode(uint2 codes, uint32_t scale, float (&f)[kLane])
 {
-    const float factor = scale == 255 ? kNan : __uint_as_float((scale + 4) << 23);
-    const uint32_t w[2] = {codes.x, codes.y};
+    // 2^(scale - 127 + 18) in two factors, which fp32 holds for every scale
+    const float wide = scale == 255 ? kNan : __uint_as_float((scale + 9) << 23);
 #pragma unroll
-    for (int i = 0; i < kLane; ++i) {
-        const uint32_t c = (w[i >> 2] >> (8 * (i & 3))) & 255u;
-        const uint32_t bits = kSigned ? ((c & 127u) << 19) | ((c & 128u) << 24) : c << 19;
-        f[i] = __fmul_rn(__fmul_rn(__uint_as_float(bits), 0x1p126f), factor);
+    for (int i = 0; i < kLane / 2; ++i) {
+        const uint32_t w = __byte_perm(i < 2 ? codes.x : codes.y, 0, i & 1 ? 0x4342 : 0x4140);   // a byte to each half
+        const uint32_t bits = kSigned ? ((w << 6) & 0x1FC01FC0u) | ((w << 8) & 0x80008000u) : (w << 6) & 0x3FC03FC0u;
+        float lo, hi;
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(bits));
+        f[2 * i] = lo * 512.0f * wide;
+        f[2 * i + 1] = hi * 512.0f * wide;
     }
 }
 
@@ -268,29 +289,35 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t most)
     return s < 1 ? 1u : (uint32_t)s;
 }
 
+// 8 codes.  `noise` is what is added below a code, times 32: the code is then the top byte of
+// 32 (bits + noise), whose multiplication drops the sign.
 template <bool kSigned>
 __device__ __forceinline__ uint2 encode(const float (&f)[kLane], uint32_t scale, const uint32_t (&noise)[kLane])
 {
     if (scale == 255) return make_uint2(0, 0);
     const float up = __uint_as_float((254u - (scale < 1 ? 1u : scale)) << 23);
-    uint32_t w[2] = {0, 0};
+    uint32_t t[kLane];
 #pragma unroll
     for (int i = 0; i < kLane; ++i) {
-        const uint32_t y = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(f[i]), up), 0x1p-130f));
-        uint32_t c = (y + noise[i]) >> 19;
-        if (kSigned) c |= (__float_as_uint(f[i]) >> 24) & 128u;
-        else if (c == 0 && f[i] > 0.0f) c = 1;
-        w[i >> 2] |= c << (8 * (i & 3));
+        uint32_t c = __float_as_uint(f[i] * up * 0x1p-130f) * 32u + noise[i];
+        if (kSigned) c = (c & 0x7FFFFFFFu) | (__float_as_uint(f[i]) & 0x80000000u);
+        else if (f[i] != 0.0f) c = max(c, 1u << 24);
+        t[i] = c;
     }
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = __byte_perm(__byte_perm(t[4 * i], t[4 * i + 1], 0x0073), __byte_perm(t[4 * i + 2], t[4 * i + 3], 0x0073), 0x5410);
     return make_uint2(w[0], w[1]);
 }
 
+// Bits of the warp's largest magnitude; those of a NaN are larger than all others'.
 __device__ __forceinline__ uint32_t most_of(const float (&f)[kLane])
 {
-    uint32_t most = 0;
+    float most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kLane; ++i) most = max(most, __float_as_uint(f[i]) & 0x7FFFFFFFu);
-    return __reduce_max_sync(0xFFFFFFFFu, most);
+    for (int i = 0; i < kLane; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(fabsf(f[i])));
+    return __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
 }
 
 // A warp takes `run` blocks in a row, a lane eight consecutive elements of each.
@@ -304,8 +331,8 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ 
     int k = tensor_of(t, b);
     grid_dependency_wait();
     if (s.record->skipped != 0.0f) return;
-    const float factor = s.record->factor, rsqrt_bc2 = s.record->rsqrt_bc2, step_size = s.record->step_size;
     const uint32_t key = s.record->key;
+    const Update update = {s.record->factor, s.beta1, s.omb1, s.beta2, s.omb2, s.record->rsqrt_bc2, s.eps, s.decay, s.record->step_size};
     for (; b < end; ++b) {
         while (k + 1 < t.n && t.e[k + 1].first <= b) ++k;
         const Entry &e = t.e[k];
@@ -328,19 +355,13 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ 
             load_own(static_cast<float *>(s.v) + slot, kLane, true, v);
         }
 #pragma unroll
-        for (int i = 0; i < kLane; ++i) {
-            const float x = __fmul_rn(g[i], factor);
-            m[i] = __fadd_rn(__fmul_rn(m[i], s.beta1), __fmul_rn(x, s.omb1));
-            v[i] = __fadd_rn(__fmul_rn(v[i], s.beta2), __fmul_rn(__fmul_rn(x, s.omb2), x));
-            const float u = __fdiv_rn(m[i], __fadd_rn(__fmul_rn(__fsqrt_rn(v[i]), rsqrt_bc2), s.eps));
-            p[i] = __fsub_rn(p[i], __fadd_rn(__fmul_rn(p[i], s.decay), __fmul_rn(u, step_size)));
-            if (i >= n) m[i] = v[i] = 0.0f;   // behind a tensor's end the arenas hold zeros
-        }
+        for (int i = 0; i < kLane; ++i) update(g[i], m[i], v[i], p[i]);
         store_own(param, n, own, p);
         if constexpr (!std::is_same<C, void>::value) {
             C *copy = static_cast<C *>(e.copy) + at;
             store_copy<C>(copy, n, (reinterpret_cast<uintptr_t>(copy) & 15) == 0, p);
         }
+        // (behind a tensor's end gradients and moments are zeros, and stay so)
         if constexpr (kBits == 8) {
             const uint32_t ms = scale_of<10>(most_of(m)), vs = scale_of<18>(most_of(v));
             uint32_t nm[kLane], nv[kLane];
@@ -348,13 +369,14 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ 
                 const uint32_t high = mix(key + (uint32_t)(slot >> 32)), low = (uint32_t)slot;
 #pragma unroll
                 for (int i = 0; i < kLane; ++i) {
+                    // 8 r + 4 below the code for 16 random bits r, times 32
                     const uint32_t x = mix((low + i) ^ high);
-                    nm[i] = ((x & 0xFFFFu) << 3) + 4;
-                    nv[i] = ((x >> 16) << 3) + 4;
+                    nm[i] = ((x << 8) & 0xFFFF00u) | 128u;
+                    nv[i] = ((x >> 8) & 0xFFFF00u) | 128u;
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < kLane; ++i) nm[i] = nv[i] = 1u << 18;
+                for (int i = 0; i < kLane; ++i) nm[i] = nv[i] = 1u << 23;
             }
             *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(s.m) + slot) = encode<true>(m, ms, nm);
             *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(s.v) + slot) = encode<false>(v, vs, nv);
@@ -489,7 +511,7 @@ so_status so_tensor_adamw_step(const so_tensor *tensors, int32_t n_tensors, int3
     if ((clip != 0 && clip != 1) || (stochastic != 0 && stochastic != 1) || (stochastic && state_bits != 8)) return SO_ERR_INVALID_ARG;
     if (!hp || !record || !aligned(record, 16) || !finite32(grad_scale)) return SO_ERR_INVALID_ARG;
     if (!(hp->lr >= 0.0) || !finite32(hp->lr) || !(hp->beta1 >= 0.0 && hp->beta1 < 1.0) || !(hp->beta2 >= 0.0 && hp->beta2 < 1.0) ||
-        !(hp->eps > 0.0) || (float)hp->eps == 0.0f || !finite32(hp->eps) || !(hp->weight_decay >= 0.0) || !finite32(hp->lr * hp->weight_decay) ||
+        !((float)hp->eps >= 0x1p-126f) || !finite32(hp->eps) || !(hp->weight_decay >= 0.0) || !finite32(hp->lr * hp->weight_decay) ||
         !finite32(hp->lr / (1.0 - hp->beta1)) || std::isnan(hp->max_grad_norm))
         return SO_ERR_INVALID_ARG;
     if (clip && (!scratch || !aligned(scratch, 16) || scratch_bytes < info.bytes_scratch)) return SO_ERR_INVALID_ARG;
