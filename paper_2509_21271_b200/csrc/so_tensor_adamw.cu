@@ -30,8 +30,11 @@ namespace {
 constexpr int kBlock = SO_TENSOR_BLOCK;   // elements that share a scale, and what a warp takes at a time
 constexpr int kLane = kBlock / 32;        // consecutive elements of a lane
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMaxTensors = 640;          // of a launch: the table is a kernel parameter of 25 KB
-constexpr int kMaxRun = 8;                // blocks a warp takes in a row
+// Tensors of a launch: the table is a kernel parameter of 25 KB, or of 2.5 KB where that is enough.
+constexpr int kMaxTensors = 640, kFewTensors = 64;
+// Blocks a warp takes in a row, at most.  660 M parameters with 8-bit moments: 2.53 ms with runs of 1, 2.80
+// with 8, 2.70 with 32, 2.32 with 100, 2.34 with 128, 2.73 with one run a warp; with 32 bits the same up to 100.
+constexpr int kMaxRun8 = 100, kMaxRun32 = 8;
 constexpr int kNormBlocks = 1184;         // thread blocks of a norm launch, at most; the same on every device
 
 struct Entry {
@@ -94,14 +97,17 @@ __device__ void begin_step(Record *r, double sumsq, const Hyper &h)
 
 __global__ void begin_kernel(Record *r, const __grid_constant__ Hyper h) { begin_step(r, 0.0, h); }
 
-struct Table {
+template <int kMax>
+struct TableOf {
+    static constexpr int kRoom = kMax;
     int32_t n;
     int64_t blocks;                       // of all its tensors
     int64_t first;                        // of its first tensor
-    Entry e[kMaxTensors];
+    Entry e[kMax];
 };
 
 // Index of the tensor that holds block b (tensors without elements have none).
+template <typename Table>
 __device__ __forceinline__ int tensor_of(const Table &t, int64_t b)
 {
     int lo = 0, hi = t.n - 1;
@@ -168,7 +174,7 @@ __device__ __forceinline__ void store_copy(T *p, int n, bool vectors, const floa
 
 // Sum of the squares of all gradients: fp32 over a lane's eight, fp64 from there on, in a fixed
 // order.  The thread block that comes last adds the blocks' sums and opens the step.
-template <typename G>
+template <typename G, typename Table>
 __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ Table t, const __grid_constant__ Hyper h, Record *record,
                                                         double *sums, uint32_t first_sum, uint32_t all_sums)
 {
@@ -176,35 +182,48 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
     __shared__ bool s_last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     double sum = 0.0;
-    const int64_t warps = (int64_t)gridDim.x * kWarps, me = (int64_t)blockIdx.x * kWarps + warp;
-    const int64_t each = (t.blocks + warps - 1) / warps;
-    int64_t b = t.first + me * each, end = b + each;
-    if (end > t.first + t.blocks) end = t.first + t.blocks;
-    int k = b < end ? tensor_of(t, b) : 0;
-    while (b < end) {
+    // consecutive blocks a warp, eight at a time: where they lie in one tensor, 32 bytes a lane and load
+    const int64_t warps = (int64_t)gridDim.x * kWarps, me = (int64_t)blockIdx.x * kWarps + warp, each = (t.blocks + warps - 1) / warps;
+    int64_t i = me * each, end = i + each;
+    if (end > t.blocks) end = t.blocks;
+    int k = i < end ? tensor_of(t, t.first + i) : 0;
+    constexpr int kAtOnce = 8, kElems = 32 / (int)sizeof(G), kLoads = kAtOnce * kBlock / (32 * kElems);
+    while (i < end) {
+        const int64_t b = t.first + i;
+        while (k + 1 < t.n && t.e[k + 1].first <= b) ++k;
         const Entry &e = t.e[k];
-        const G *grad = static_cast<const G *>(e.grad);
-        const bool vectors = (reinterpret_cast<uintptr_t>(grad) & (sizeof(G) * kLane - 1)) == 0;
-        const int64_t have = (e.numel + kBlock - 1) / kBlock + e.first;
-        const int64_t stop = end < have ? end : have;
-        for (; b < stop; b += 4) {
-            float f[4][kLane];
+        const int64_t at = (b - e.first) * kBlock;
+        const G *grad = static_cast<const G *>(e.grad) + at;
+        if (i + kAtOnce <= end && at + kAtOnce * kBlock <= e.numel && (reinterpret_cast<uintptr_t>(grad) & 31) == 0) {
+            uint32_t w[kLoads][8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int64_t at = (b + u - e.first) * kBlock + lane * kLane;
-                const int64_t left = b + u < stop ? e.numel - at : 0;
-                load_lane(grad + at, left > kLane ? kLane : (int)left, vectors, f[u]);
-            }
+            for (int u = 0; u < kLoads; ++u)
+                asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(w[u][0]), "=r"(w[u][1]), "=r"(w[u][2]), "=r"(w[u][3]), "=r"(w[u][4]), "=r"(w[u][5]), "=r"(w[u][6]), "=r"(w[u][7])
+                             : "l"(grad + (u * 32 + lane) * kElems));
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < kLoads; ++u) {
                 float q = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kLane; ++i) q = fmaf(f[u][i], f[u][i], q);
+                for (int h = 0; h < 2; ++h) {
+                    float f[Vec<G>::kElems];
+                    unpack<G>(make_uint4(w[u][4 * h], w[u][4 * h + 1], w[u][4 * h + 2], w[u][4 * h + 3]), f);
+#pragma unroll
+                    for (int j = 0; j < Vec<G>::kElems; ++j) q = fmaf(f[j], f[j], q);
+                }
                 sum += (double)q;
             }
+            i += kAtOnce;
+        } else {
+            float f[kLane];
+            const int64_t left = e.numel - at - lane * kLane;
+            load_lane(grad + lane * kLane, left > kLane ? kLane : (int)left, (reinterpret_cast<uintptr_t>(grad) & (sizeof(G) * kLane - 1)) == 0, f);
+            float q = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kLane; ++j) q = fmaf(f[j], f[j], q);
+            sum += (double)q;
+            ++i;
         }
-        b = stop;
-        if (b < end) do ++k; while (k + 1 < t.n && t.e[k + 1].first <= b);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
@@ -239,7 +258,7 @@ struct Step {
     void *m, *v;
     uint8_t *m_scale, *v_scale;
     const Record *record;
-    int32_t run, stochastic;
+    int32_t run, stochastic, sms;
 };
 
 // One step of an element.  m and v operation by operation (packed pairs of operations come out
@@ -264,17 +283,24 @@ struct Update {
 template <bool kSigned>
 __device__ __forceinline__ void decode(uint2 codes, uint32_t scale, float (&f)[kLane])
 {
-    // 2^(scale - 127 + 18) in two factors, which fp32 holds for every scale
-    const float wide = scale == 255 ? kNan : __uint_as_float((scale + 9) << 23);
+    // 2^(scale - 127 + 18), in two factors where fp32 has none
+    const bool large = scale > 236;
+    const float wide = scale == 255 ? kNan : __uint_as_float((scale + (large ? 9 : 18)) << 23);
 #pragma unroll
     for (int i = 0; i < kLane / 2; ++i) {
         const uint32_t w = __byte_perm(i < 2 ? codes.x : codes.y, 0, i & 1 ? 0x4342 : 0x4140);   // a byte to each half
         const uint32_t bits = kSigned ? ((w << 6) & 0x1FC01FC0u) | ((w << 8) & 0x80008000u) : (w << 6) & 0x3FC03FC0u;
         float lo, hi;
         asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(bits));
-        f[2 * i] = lo * 512.0f * wide;
-        f[2 * i + 1] = hi * 512.0f * wide;
+        f[2 * i] = lo;
+        f[2 * i + 1] = hi;
     }
+    if (large) {
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) f[i] *= 512.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) f[i] *= wide;
 }
 
 // The scale of a block from the bit pattern of its largest magnitude: the largest code
@@ -295,11 +321,21 @@ template <bool kSigned>
 __device__ __forceinline__ uint2 encode(const float (&f)[kLane], uint32_t scale, const uint32_t (&noise)[kLane])
 {
     if (scale == 255) return make_uint2(0, 0);
-    const float up = __uint_as_float((254u - (scale < 1 ? 1u : scale)) << 23);
+    const uint32_t s = scale < 1 ? 1u : scale;
+    float y[kLane];                       // f 2^(127 - s - 130): in one product where that factor is a normal number
+    if (s <= 123) {
+        const float factor = __uint_as_float((124u - s) << 23);
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) y[i] = f[i] * factor;
+    } else {
+        const float up = __uint_as_float((254u - s) << 23);
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) y[i] = f[i] * up * 0x1p-130f;
+    }
     uint32_t t[kLane];
 #pragma unroll
     for (int i = 0; i < kLane; ++i) {
-        uint32_t c = __float_as_uint(f[i] * up * 0x1p-130f) * 32u + noise[i];
+        uint32_t c = __float_as_uint(y[i]) * 32u + noise[i];
         if (kSigned) c = (c & 0x7FFFFFFFu) | (__float_as_uint(f[i]) & 0x80000000u);
         else if (f[i] != 0.0f) c = max(c, 1u << 24);
         t[i] = c;
@@ -320,36 +356,90 @@ __device__ __forceinline__ uint32_t most_of(const float (&f)[kLane])
     return __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
 }
 
-// A warp takes `run` blocks in a row, a lane eight consecutive elements of each.
-template <int kBits, typename G, typename C>
+// What a lane reads of a block.
+template <int kBits, typename G>
+struct Block {
+    static constexpr int kWords = kLane * (int)sizeof(G) / 4;
+    float *param;
+    void *copy;
+    int n;                                // elements of this lane that there are
+    float p[kLane];
+    uint32_t g[kWords];
+    uint2 mc, vc;
+    uint32_t ms, vs;
+    // k: the tensor of the block before, brought up to this one's
+    template <typename Table>
+    __device__ __forceinline__ void load(const Table &t, const Step &s, int &k, int64_t b, int lane)
+    {
+        while (k + 1 < t.n && t.e[k + 1].first <= b) ++k;
+        const Entry &e = t.e[k];
+        const int64_t at = (b - e.first) * kBlock + lane * kLane, left = e.numel - at;
+        n = left >= kLane ? kLane : left > 0 ? (int)left : 0;
+        param = e.param + at;
+        copy = static_cast<char *>(e.copy) + at * 2;
+        const G *grad = static_cast<const G *>(e.grad) + at;
+        load_own(param, n, (reinterpret_cast<uintptr_t>(param) & 31) == 0, p);
+        if (n >= kLane && (reinterpret_cast<uintptr_t>(grad) & (sizeof(G) * kLane - 1)) == 0) {
+            if constexpr (sizeof(G) == 4) {
+                asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(g[0]), "=r"(g[1]), "=r"(g[2]), "=r"(g[3]), "=r"(g[4]), "=r"(g[5]), "=r"(g[6]), "=r"(g[7]) : "l"(grad));
+            } else {
+                const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(grad));
+                g[0] = q.x, g[1] = q.y, g[2] = q.z, g[3] = q.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+                if constexpr (sizeof(G) == 4) g[i] = i < n ? __float_as_uint(grad[i]) : 0u;
+                else g[i] = (2 * i < n ? (uint32_t)grad[2 * i].bits : 0u) | (2 * i + 1 < n ? (uint32_t)grad[2 * i + 1].bits << 16 : 0u);
+            }
+        }
+        if constexpr (kBits == 8) {
+            const int64_t slot = b * kBlock + lane * kLane;
+            mc = *reinterpret_cast<const uint2 *>(static_cast<uint8_t *>(s.m) + slot);
+            vc = *reinterpret_cast<const uint2 *>(static_cast<uint8_t *>(s.v) + slot);
+            ms = s.m_scale[b];
+            vs = s.v_scale[b];
+        }
+    }
+    __device__ __forceinline__ void gradients(float (&f)[kLane]) const
+    {
+        if constexpr (sizeof(G) == 4) {
+#pragma unroll
+            for (int i = 0; i < kLane; ++i) f[i] = __uint_as_float(g[i]);
+        } else {
+            unpack<G>(make_uint4(g[0], g[1], g[2], g[3]), f);
+        }
+    }
+};
+
+// A warp takes `run` blocks in a row, a lane eight consecutive elements of each; the grid goes through
+// the list from its begin to its end, and a warp finds its tensors by going on from the last one's.
+template <int kBits, typename G, typename C, typename Table>
 __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ Table t, const __grid_constant__ Step s)
 {
     const int lane = threadIdx.x & 31;
-    int64_t b = t.first + ((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * s.run, end = b + s.run;
-    if (end > t.first + t.blocks) end = t.first + t.blocks;
-    if (b >= end) return;
-    int k = tensor_of(t, b);
+    const int64_t begin = ((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * s.run, stride = (int64_t)gridDim.x * kWarps * s.run;
+    int k = begin < t.blocks ? tensor_of(t, t.first + begin) : 0;
     grid_dependency_wait();
     if (s.record->skipped != 0.0f) return;
     const uint32_t key = s.record->key;
     const Update update = {s.record->factor, s.beta1, s.omb1, s.beta2, s.omb2, s.record->rsqrt_bc2, s.eps, s.decay, s.record->step_size};
-    for (; b < end; ++b) {
-        while (k + 1 < t.n && t.e[k + 1].first <= b) ++k;
-        const Entry &e = t.e[k];
-        const int64_t at = (b - e.first) * kBlock + lane * kLane, left = e.numel - at;
-        const int n = left >= kLane ? kLane : left > 0 ? (int)left : 0;
+    Block<kBits, G> now;
+    for (int64_t i = begin, left = s.run; i < t.blocks; --left, left > 0 ? ++i : (i += stride - s.run + 1, left = s.run)) {
+        const int64_t b = t.first + i;
+        now.load(t, s, k, b, lane);
+        const int n = now.n;
         const int64_t slot = b * kBlock + lane * kLane;
-        float *param = e.param + at;
-        const G *grad = static_cast<const G *>(e.grad) + at;
+        float *param = now.param;
         const bool own = (reinterpret_cast<uintptr_t>(param) & 31) == 0;
         float p[kLane], g[kLane], m[kLane], v[kLane];
-        load_own(param, n, own, p);
-        load_lane(grad, n, (reinterpret_cast<uintptr_t>(grad) & (sizeof(G) * kLane - 1)) == 0, g);
+#pragma unroll
+        for (int i = 0; i < kLane; ++i) p[i] = now.p[i];
+        now.gradients(g);
         if constexpr (kBits == 8) {
-            const uint2 mc = *reinterpret_cast<const uint2 *>(static_cast<uint8_t *>(s.m) + slot);
-            const uint2 vc = *reinterpret_cast<const uint2 *>(static_cast<uint8_t *>(s.v) + slot);
-            decode<true>(mc, s.m_scale[b], m);
-            decode<false>(vc, s.v_scale[b], v);
+            decode<true>(now.mc, now.ms, m);
+            decode<false>(now.vc, now.vs, v);
         } else {
             load_own(static_cast<float *>(s.m) + slot, kLane, true, m);
             load_own(static_cast<float *>(s.v) + slot, kLane, true, v);
@@ -358,7 +448,7 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ 
         for (int i = 0; i < kLane; ++i) update(g[i], m[i], v[i], p[i]);
         store_own(param, n, own, p);
         if constexpr (!std::is_same<C, void>::value) {
-            C *copy = static_cast<C *>(e.copy) + at;
+            C *copy = static_cast<C *>(now.copy);
             store_copy<C>(copy, n, (reinterpret_cast<uintptr_t>(copy) & 15) == 0, p);
         }
         // (behind a tensor's end gradients and moments are zeros, and stay so)
@@ -366,13 +456,13 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ 
             const uint32_t ms = scale_of<10>(most_of(m)), vs = scale_of<18>(most_of(v));
             uint32_t nm[kLane], nv[kLane];
             if (s.stochastic) {
-                const uint32_t high = mix(key + (uint32_t)(slot >> 32)), low = (uint32_t)slot;
+                const uint32_t lane_key = mix(key + (uint32_t)(slot >> 32)) ^ (uint32_t)slot;
 #pragma unroll
                 for (int i = 0; i < kLane; ++i) {
                     // 8 r + 4 below the code for 16 random bits r, times 32
-                    const uint32_t x = mix((low + i) ^ high);
-                    nm[i] = ((x << 8) & 0xFFFF00u) | 128u;
-                    nv[i] = ((x >> 8) & 0xFFFF00u) | 128u;
+                    const uint32_t x = mix(lane_key ^ i);
+                    nm[i] = __byte_perm(x, 128u, 0x5104);
+                    nv[i] = __byte_perm(x, 128u, 0x5324);
                 }
             } else {
 #pragma unroll
@@ -426,14 +516,14 @@ int64_t list_blocks(const so_tensor *t, int32_t n)
 
 unsigned norm_grid(int64_t blocks)
 {
-    // a warp takes four blocks at a time
+    // a warp takes several blocks at a time
     const int64_t want = (blocks + 4 * kWarps - 1) / (4 * kWarps);
     return want < 1 ? 1u : want > kNormBlocks ? (unsigned)kNormBlocks : (unsigned)want;
 }
 
 // Calls `fn(table)` for every kMaxTensors of the list.
-template <typename F>
-so_status for_tables(const so_tensor *t, int32_t n, F fn)
+template <typename Table, typename F>
+so_status for_tables_of(const so_tensor *t, int32_t n, F fn)
 {
     Table table;
     int64_t block = 0;
@@ -441,7 +531,7 @@ so_status for_tables(const so_tensor *t, int32_t n, F fn)
     while (i < n) {
         table.n = 0;
         table.first = block;
-        for (; i < n && table.n < kMaxTensors; ++i) {
+        for (; i < n && table.n < Table::kRoom; ++i) {
             if (t[i].numel == 0) continue;
             Entry &e = table.e[table.n++];
             e.param = static_cast<float *>(t[i].param);
@@ -459,20 +549,28 @@ so_status for_tables(const so_tensor *t, int32_t n, F fn)
     return SO_OK;
 }
 
-template <int kBits, typename G, typename C>
+template <typename F>
+so_status for_tables(const so_tensor *t, int32_t n, F fn)
+{
+    if (n <= kFewTensors) return for_tables_of<TableOf<kFewTensors>>(t, n, fn);
+    return for_tables_of<TableOf<kMaxTensors>>(t, n, fn);
+}
+
+template <int kBits, typename G, typename C, typename Table>
 so_status launch_step(const Table &t, const Step &s, cudaStream_t stream)
 {
     const int64_t runs = (t.blocks + s.run - 1) / s.run;
-    return launch(step_kernel<kBits, G, C>, (unsigned)((runs + kWarps - 1) / kWarps), kThreads, 0, stream, true, t, s);
+    const int64_t grid = (runs + kWarps - 1) / kWarps, most = (int64_t)s.sms * 4;   // four blocks an SM
+    return launch(step_kernel<kBits, G, C, Table>, (unsigned)(kBits == 32 || grid < most ? grid : most), kThreads, 0, stream, true, t, s);
 }
-template <int kBits, typename G>
+template <int kBits, typename G, typename Table>
 so_status launch_step(int32_t copy_dtype, const Table &t, const Step &s, cudaStream_t stream)
 {
     if (copy_dtype == SO_DTYPE_BF16) return launch_step<kBits, G, bf16_t>(t, s, stream);
     if (copy_dtype == SO_DTYPE_FP16) return launch_step<kBits, G, f16_t>(t, s, stream);
     return launch_step<kBits, G, void>(t, s, stream);
 }
-template <int kBits>
+template <int kBits, typename Table>
 so_status launch_step(int32_t grad_dtype, int32_t copy_dtype, const Table &t, const Step &s, cudaStream_t stream)
 {
     if (grad_dtype == SO_DTYPE_BF16) return launch_step<kBits, bf16_t>(copy_dtype, t, s, stream);
@@ -525,16 +623,20 @@ so_status so_tensor_adamw_step(const so_tensor *tensors, int32_t n_tensors, int3
         if (!t.param || !aligned(t.param, 4) || !t.grad || !aligned(t.grad, elem_size(grad_dtype))) return SO_ERR_INVALID_ARG;
         if (copy_dtype != SO_TENSOR_NO_COPY && (!t.copy || !aligned(t.copy, 2))) return SO_ERR_INVALID_ARG;
     }
+    int sms;
+    const so_status dev = device_sms(&sms);
+    if (dev != SO_OK) return dev;
     const cudaStream_t cs = static_cast<cudaStream_t>(stream);
     Record *r = static_cast<Record *>(record);
     const Hyper h = {hp->lr, hp->beta1, hp->beta2, hp->max_grad_norm, grad_scale, seed, clip};
     so_status done;
     if (clip && info.blocks > 0) {
         uint32_t sums = 0, at = 0;
-        for_tables(tensors, n_tensors, [&](const Table &t) { sums += norm_grid(t.blocks); return SO_OK; });
-        done = for_tables(tensors, n_tensors, [&](const Table &t) {
+        for_tables(tensors, n_tensors, [&](const auto &t) { sums += norm_grid(t.blocks); return SO_OK; });
+        done = for_tables(tensors, n_tensors, [&](const auto &t) {
+            using Table = std::decay_t<decltype(t)>;
             const unsigned grid = norm_grid(t.blocks);
-            const auto kernel = grad_dtype == SO_DTYPE_BF16 ? norm_kernel<bf16_t> : grad_dtype == SO_DTYPE_FP16 ? norm_kernel<f16_t> : norm_kernel<float>;
+            const auto kernel = grad_dtype == SO_DTYPE_BF16 ? norm_kernel<bf16_t, Table> : grad_dtype == SO_DTYPE_FP16 ? norm_kernel<f16_t, Table> : norm_kernel<float, Table>;
             const so_status one = launch(kernel, grid, kThreads, 0, cs, false, t, h, r, static_cast<double *>(scratch), at, sums);
             at += grid;
             return one;
@@ -544,11 +646,12 @@ so_status so_tensor_adamw_step(const so_tensor *tensors, int32_t n_tensors, int3
     }
     if (done != SO_OK) return done;
     Step s = {(float)hp->beta1, (float)(1.0 - hp->beta1), (float)hp->beta2, (float)(1.0 - hp->beta2), (float)hp->eps,
-              (float)(hp->lr * hp->weight_decay), m, v, m_scale, v_scale, r, 1, stochastic};
-    return for_tables(tensors, n_tensors, [&](const Table &t) {
-        // runs as long as leave every SM of a B200 a few dozen warps
-        const int64_t run = t.blocks / (148 * 64);
-        s.run = (int32_t)(run < 1 ? 1 : run > kMaxRun ? kMaxRun : run);
+              (float)(hp->lr * hp->weight_decay), m, v, m_scale, v_scale, r, 1, stochastic, sms};
+    return for_tables(tensors, n_tensors, [&](const auto &t) {
+        // as many turns for every warp of the grid as keep runs below the limit
+        const int64_t warps = (int64_t)sms * 4 * kWarps, mine = (t.blocks + warps - 1) / warps, limit = state_bits == 8 ? kMaxRun8 : kMaxRun32;
+        const int64_t turns = mine < 2 * kMaxRun32 ? mine : (mine + limit - 1) / limit;   // short lists: a block a turn
+        s.run = (int32_t)((mine + turns - 1) / (turns < 1 ? 1 : turns));
         return state_bits == 8 ? launch_step<8>(grad_dtype, copy_dtype, t, s, cs) : launch_step<32>(grad_dtype, copy_dtype, t, s, cs);
     });
 }
