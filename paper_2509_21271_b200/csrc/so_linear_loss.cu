@@ -36,7 +36,9 @@ constexpr uint32_t kBox = 32 * 128;       // what such a warp copies out at a ti
 constexpr int kRowPad = 256;              // rows are padded to whole tiles of a pair of blocks
 constexpr float kLog2e = 1.44269504088896340736f;
 
-enum Mode { kStats, kProb, kHidden, kTable };
+// What a launch computes, and a tile of one: the tiles of both gradients are in one launch, as they
+// need the same P and fill each other's last wave.
+enum Mode { kStats, kProb, kHidden, kTable, kGradients };
 
 // What the device finds out about a call, in scratch.
 struct Control {
@@ -205,6 +207,7 @@ struct Product {
     int64_t prob_stride;
     float *part;                          // [splits][rows_pad][part_stride]
     int64_t part_stride;
+    int32_t want_hidden;
     void *table_grad;
     int64_t grad_stride;
     int32_t grad_dtype, accumulate, grad_vectors, grad_boxes;
@@ -214,56 +217,78 @@ struct Product {
 
 // Which tile, and which steps of K.
 struct Item {
-    int m, n, split, steps, k0;           // k0: first step
+    int kind, m, n, split, steps, k0;     // k0: first step
 };
 
-template <int kMode, int kCtas>
-struct Work {
-    int m_tiles, n_tiles, k_steps;
+// The tiles of one kind.
+template <int kCtas>
+struct Tiles {
+    int m, n, k_steps, splits;
     int64_t items;
-    __device__ Work(const Product &p, int live)
+    __device__ Tiles(const Product &p, int kind, int live)
     {
         constexpr int kTileM = kRowsOfCta * kCtas;
         const int row_tiles = (live + kTileM - 1) / kTileM, col_tiles = (int)((p.cols + kTileN - 1) / kTileN);
-        if (kMode == kStats || kMode == kProb) {
-            m_tiles = row_tiles;
-            n_tiles = (int)((p.width + kTileN - 1) / kTileN);
+        splits = 1;
+        if (kind == kStats || kind == kProb) {
+            m = row_tiles;
+            n = (int)((p.width + kTileN - 1) / kTileN);
             k_steps = (int)((p.cols + kTileK - 1) / kTileK);
-        } else if (kMode == kHidden) {
-            m_tiles = row_tiles;
-            n_tiles = col_tiles;
+        } else if (kind == kHidden) {
+            m = row_tiles;
+            n = col_tiles;
             k_steps = (int)((p.width + kTileK - 1) / kTileK);
+            splits = p.splits;
         } else {
-            m_tiles = live ? (int)((p.width + kTileM - 1) / kTileM) : 0;
-            n_tiles = col_tiles;
+            m = live ? (int)((p.width + kTileM - 1) / kTileM) : 0;
+            n = col_tiles;
             k_steps = (live + kTileK - 1) / kTileK;
         }
-        items = (int64_t)m_tiles * n_tiles * (kMode == kHidden ? p.splits : 1);
+        items = (int64_t)m * n * splits;
     }
-    __device__ __forceinline__ Item item(const Product &p, int64_t i) const
+    __device__ __forceinline__ Item item(const Product &p, int kind, int64_t i) const
     {
         Item r;
+        r.kind = kind;
         r.split = 0;
         r.k0 = 0;
         r.steps = k_steps;
-        if (kMode == kStats || kMode == kProb) {
+        if (kind == kStats || kind == kProb) {
             // the rows' tiles one after the other: a tile of the table is read once, the hidden states stay in L2
-            r.n = (int)(i / m_tiles);
-            r.m = (int)(i - (int64_t)r.n * m_tiles);
+            r.n = (int)(i / m);
+            r.m = (int)(i - (int64_t)r.n * m);
         } else {
-            const int64_t q = i / n_tiles;
-            r.n = (int)(i - q * n_tiles);
-            r.m = (int)(q % m_tiles);
-            r.split = (int)(q / m_tiles);
+            const int64_t q = i / n;
+            r.n = (int)(i - q * n);
+            r.m = (int)(q % m);
+            r.split = (int)(q / m);
         }
-        if (kMode == kHidden) {
-            r.k0 = (int)((int64_t)k_steps * r.split / p.splits);
-            r.steps = (int)((int64_t)k_steps * (r.split + 1) / p.splits) - r.k0;
-        } else if (kMode == kTable) {
+        if (kind == kHidden) {
+            r.k0 = (int)((int64_t)k_steps * r.split / splits);
+            r.steps = (int)((int64_t)k_steps * (r.split + 1) / splits) - r.k0;
+        } else if (kind == kTable) {
             r.steps = k_steps * p.planes;
         }
         return r;
     }
+};
+
+template <int kMode, int kCtas>
+struct Work {
+    static constexpr int kFirst = kMode == kGradients ? (int)kHidden : kMode;
+    Tiles<kCtas> first, second;           // second: kGradients' of the table, behind the longer ones of dH
+    int64_t items;
+    __device__ Work(const Product &p, int live) : first(p, kFirst, live), second(p, kTable, live)
+    {
+        if (kMode == kGradients && !p.want_hidden) first.items = 0;
+        items = first.items + (kMode == kGradients && p.table_grad ? second.items : 0);
+    }
+    __device__ __forceinline__ Item item(const Product &p, int64_t i) const
+    {
+        if (kMode != kGradients || i < first.items) return first.item(p, kFirst, i);
+        return second.item(p, kTable, i - first.items);
+    }
+    __device__ __forceinline__ int k_steps(const Item &it) const { return kMode == kGradients && it.kind == kTable ? second.k_steps : first.k_steps; }
 };
 
 template <int kCtas>
@@ -571,13 +596,16 @@ __device__ __forceinline__ void end_table_by_lanes(const Product &p, uint32_t tm
     }
 }
 
+// a, b, out: of kStats and kProb, and of the tiles of dH; a2, b2, out2: of those of dW.
+struct Maps {
+    CUtensorMap a, b, out, a2, b2, out2;
+};
+
 template <typename T, int kMode, int kCtas>
-__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                               const __grid_constant__ CUtensorMap map_out, const __grid_constant__ Product p)
+__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Product p)
 {
     using S = Shape<kCtas>;
-    constexpr bool kAK = kMode != kTable;                    // A contiguous in K: H, H, P; P transposed is not
-    constexpr bool kBK = kMode == kStats || kMode == kProb;  // B: W by its columns, else W and H by their rows
+    constexpr bool kBK = kMode != kGradients;                // B contiguous in K: W by its columns, else W and H by their rows
     extern __shared__ uint8_t s_raw[];
     __shared__ __align__(8) Shared s;
     const uint32_t tiles = (smem_addr(s_raw) + 1023u) & ~1023u;
@@ -623,6 +651,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         for (int64_t i = unit; ok && i < work.items; i += units) {
             const Item it = work.item(p, i);
             const int m0 = (it.m * kCtas + (int)rank) * kRowsOfCta, n0 = it.n * kTileN + (int)rank * (kTileN / kCtas);
+            const int k_steps = work.k_steps(it);
             int step = it.k0, row0 = 0;                      // row0: of the part of P
             for (int k = 0; k < it.steps; ++k) {
                 if (!(ok = await(empty + 8 * stage, phase, polls, s, p.control))) break;
@@ -631,24 +660,29 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 const int k0 = step * kTileK;
                 if (elected()) {
                     if (rank == 0) mbar_expect(full + 8 * stage, S::kStage * kCtas);
-                    if (kAK) tma_load<kCtas>(a, &map_a, k0, m0, bar);
-                    else tma_load_groups<kCtas>(a, &map_a, row0 + k0, m0 / 64, bar);
                     if (kBK) {
+                        tma_load<kCtas>(a, &maps.a, k0, m0, bar);
 #pragma unroll
-                        for (int g = 0; g < 2 / kCtas; ++g) tma_load<kCtas>(b + g * 128 * 128, &map_b, k0, (int)p.table_row + n0 + 128 * g, bar);
-                    } else if (kMode == kTable || p.table_groups) {
+                        for (int g = 0; g < 2 / kCtas; ++g) tma_load<kCtas>(b + g * 128 * 128, &maps.b, k0, (int)p.table_row + n0 + 128 * g, bar);
+                    } else if (it.kind == kTable) {
+                        tma_load_groups<kCtas>(a, &maps.a2, row0 + k0, m0 / 64, bar);
 #pragma unroll
-                        for (int g = 0; g < 2 / kCtas; ++g)
-                            tma_load_groups<kCtas>(b + 2 * g * kMajorStep, &map_b, (kMode == kHidden ? (int)p.table_row : 0) + k0, n0 / 64 + 2 * g, bar);
+                        for (int g = 0; g < 2 / kCtas; ++g) tma_load_groups<kCtas>(b + 2 * g * kMajorStep, &maps.b2, k0, n0 / 64 + 2 * g, bar);
                     } else {
+                        tma_load<kCtas>(a, &maps.a, k0, m0, bar);
+                        if (p.table_groups) {
 #pragma unroll
-                        for (int g = 0; g < kTileN / kCtas / 64; ++g) tma_load<kCtas>(b + g * kMajorStep, &map_b, n0 + 64 * g, (int)p.table_row + k0, bar);
+                            for (int g = 0; g < 2 / kCtas; ++g) tma_load_groups<kCtas>(b + 2 * g * kMajorStep, &maps.b, (int)p.table_row + k0, n0 / 64 + 2 * g, bar);
+                        } else {
+#pragma unroll
+                            for (int g = 0; g < kTileN / kCtas / 64; ++g) tma_load<kCtas>(b + g * kMajorStep, &maps.b, n0 + 64 * g, (int)p.table_row + k0, bar);
+                        }
                     }
                 }
                 __syncwarp();
                 ++issued;
                 if (++stage == S::kStages) stage = 0, phase ^= 1;
-                if (++step == work.k_steps && kMode == kTable) step = 0, row0 += p.rows_pad;
+                if (++step == k_steps && it.kind == kTable) step = 0, row0 += p.rows_pad;
             }
         }
         // a block that gives up waits for what is still on its way
@@ -656,7 +690,6 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             for (int k = issued > S::kStages ? issued - S::kStages : 0; k < issued; ++k)
                 mbar_wait(full + 8 * (k % S::kStages), (uint32_t)(k / S::kStages) & 1u, kPolls);
     } else if (warp == 1 && rank == 0) {
-        constexpr uint32_t kInstruction = instruction<T>(kRowsOfCta * kCtas, kTileN, kAK, kBK);
         int stage = 0, buffer = 0;
         uint32_t phase = 0, free_phase = 1;
         bool ok = true, ready = false;                       // ready: the stage is known to be filled
@@ -664,6 +697,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             const Item it = work.item(p, i);
             if (!(ok = await(free + 8 * buffer, free_phase, polls, s, p.control))) break;
             const uint32_t d = tmem + buffer * kTileN;
+            // A: H, H, P contiguous in K; P transposed is not
+            const bool a_k = kMode != kGradients || it.kind != kTable;
+            const uint32_t what = a_k ? instruction<T>(kRowsOfCta * kCtas, kTileN, true, kBK) : instruction<T>(kRowsOfCta * kCtas, kTileN, false, kBK);
+            const uint32_t a_step = (a_k ? kStepBytes<true> : kStepBytes<false>) >> 4;
             for (int k = 0; k < it.steps; ++k) {
                 if (!ready && !(ok = await(full + 8 * stage, phase, polls, s, p.control))) break;
                 fence_after();
@@ -671,11 +708,11 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 if (++stage == S::kStages) stage = 0, phase ^= 1;
                 // a look at the next stage while this one's instructions are still to come
                 ready = k + 1 < it.steps && __all_sync(0xFFFFFFFFu, mbar_test(full + 8 * stage, phase));
-                const uint64_t da = descriptor(a, kAK), db = descriptor(b, kBK);
+                const uint64_t da = descriptor(a, a_k), db = descriptor(b, kBK);
                 if (elected()) {
 #pragma unroll
                     for (int j = 0; j < kTileK / 16; ++j)
-                        mma<kCtas>(d, da + (j * kStepBytes<kAK> >> 4), db + (j * kStepBytes<kBK> >> 4), kInstruction, (k | j) != 0);
+                        mma<kCtas>(d, da + j * a_step, db + (j * kStepBytes<kBK> >> 4), what, (k | j) != 0);
                     commit<kCtas>(used);
                 }
                 __syncwarp();
@@ -705,9 +742,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             const uint32_t at = tmem + buffer * kTileN + half * kEndCols + (lanes << 16);
             const int64_t row = ((int64_t)it.m * kCtas + rank) * kRowsOfCta + lanes + lane;
             if (kMode == kStats) end_stats(p, at, row, live, 2 * it.n + half);
-            else if (kMode == kProb) end_prob<T>(p, &map_out, box, at, row, live, 2 * it.n + half);
-            else if (kMode == kHidden) end_hidden(p, &map_out, box, at, row, 2 * it.n + half, it.split, it.steps == 0);
-            else if (p.grad_boxes) end_table(p, &map_out, box, at, row, 2 * it.n + half, scale);
+            else if (kMode == kProb) end_prob<T>(p, &maps.out, box, at, row, live, 2 * it.n + half);
+            else if (it.kind == kHidden) end_hidden(p, &maps.out, box, at, row, 2 * it.n + half, it.split, it.steps == 0);
+            else if (p.grad_boxes) end_table(p, &maps.out2, box, at, row, 2 * it.n + half, scale);
             else end_table_by_lanes(p, at, row, 2 * it.n + half, scale);
             fence_before();
             __syncwarp();
@@ -1205,7 +1242,7 @@ bool make_group_map(CUtensorMap *m, const void *base, int32_t dtype, int64_t row
 }
 
 template <typename T, int kMode, int kCtas>
-so_status launch_product(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const Product &p, int units, cudaStream_t st)
+so_status launch_product(const Maps &maps, const Product &p, int units, cudaStream_t st)
 {
     static std::atomic<bool> ready[kMaxDevices];
     int dev = -1;
@@ -1228,7 +1265,7 @@ so_status launch_product(const CUtensorMap &a, const CUtensorMap &b, const CUten
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a, b, out, p) == cudaSuccess ? SO_OK : SO_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kernel, maps, p) == cudaSuccess ? SO_OK : SO_ERR_CUDA;
 }
 
 struct Call {
@@ -1280,13 +1317,16 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     // the table as it is, or a packed piece of it
     const uint16_t *table = static_cast<const uint16_t *>(c.table);
     uint16_t *packed = reinterpret_cast<uint16_t *>(scratch + l.table);
-    CUtensorMap hidden_k, hidden_m, table_k, table_m, prob_k, prob_m;
-    if (!make_map(&hidden_k, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld, kRowsOfCta) || !make_group_map(&hidden_m, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld))
+    Maps logits, gradient;                // of the products for z, and of those with P
+    CUtensorMap table_m;
+    p.want_hidden = c.dhidden != nullptr;
+    if (!make_map(&logits.a, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld, kRowsOfCta) || !make_group_map(&gradient.b2, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld))
         return SO_ERR_CUDA;
+    logits.out = logits.a2 = logits.b2 = logits.out2 = logits.a;
     const auto table_maps = [&](int64_t rows) {
         const void *at = l.packed ? static_cast<const void *>(packed) : c.table;
         const int64_t stride = l.packed ? l.ld : c.vocab == 1 ? l.ld : c.table_stride;
-        return make_map(&table_k, at, c.dtype, rows, c.cols, stride, 128) &&
+        return make_map(&logits.b, at, c.dtype, rows, c.cols, stride, 128) &&
                (p.table_groups ? make_group_map(&table_m, at, c.dtype, rows, c.cols, stride) : make_map(&table_m, at, c.dtype, rows, c.cols, stride, kTileK));
     };
     const auto pack_piece = [&](int64_t first, int64_t width) {
@@ -1300,27 +1340,26 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
             if (!table_maps(width)) return SO_ERR_CUDA;
             Product q = p;
             q.first = first, q.width = width, q.table_row = 0;
-            SO_TRY((launch_product<T, kStats, kCtas>(hidden_k, table_k, hidden_k, q, units, st)));
+            SO_TRY((launch_product<T, kStats, kCtas>(logits, q, units, st)));
         }
     } else {
         if (!table_maps(c.vocab)) return SO_ERR_CUDA;
         p.width = c.vocab;
-        SO_TRY((launch_product<T, kStats, kCtas>(hidden_k, table_k, hidden_k, p, units, st)));
+        SO_TRY((launch_product<T, kStats, kCtas>(logits, p, units, st)));
     }
     Join j = {control, p.stats, p.label_logit, w, index, lse2, coef, c.row_loss, c.loss, reinterpret_cast<double *>(scratch + l.sums), (int32_t)l.rows_pad, (int32_t)l.halves, c.rows};
     SO_TRY(launch(join_kernel, (unsigned)(l.rows_pad / 32), 32 * kJoinWarps, 0, st, true, j));
     if (gradients) {
-        if (!make_map(&prob_k, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, kRowsOfCta) ||
-            !make_group_map(&prob_m, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece))
+        // (what a warp copies out is 32 rows)
+        if (!make_map(&gradient.a, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, kRowsOfCta) ||
+            !make_group_map(&gradient.a2, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece) ||
+            !make_map(&logits.out, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, 32) ||
+            !make_map(&gradient.out, p.part, SO_DTYPE_FP32, l.rows_pad * l.splits, l.part_stride, l.part_stride, 32))
             return SO_ERR_CUDA;
-        // what a warp copies out: 32 rows
-        CUtensorMap prob_out = prob_k, part_out = prob_k, grad_out = prob_k;
-        if (!make_map(&prob_out, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, 32) ||
-            !make_map(&part_out, p.part, SO_DTYPE_FP32, l.rows_pad * l.splits, l.part_stride, l.part_stride, 32))
-            return SO_ERR_CUDA;
+        gradient.out2 = gradient.out;
         const int grad_size = elem_size(c.grad_dtype);
         p.grad_boxes = c.dtable && !c.accumulate && aligned(c.dtable, 16) && c.dtable_stride * grad_size % 16 == 0;
-        if (p.grad_boxes && !make_map(&grad_out, c.dtable, c.grad_dtype, c.vocab, c.cols, c.dtable_stride, 32)) return SO_ERR_CUDA;
+        if (p.grad_boxes && !make_map(&gradient.out2, c.dtable, c.grad_dtype, c.vocab, c.cols, c.dtable_stride, 32)) return SO_ERR_CUDA;
         for (int64_t first = 0; first < c.vocab; first += l.piece) {
             Product q = p;
             q.first = q.table_row = first;
@@ -1332,9 +1371,9 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
                 q.table_row = 0;
             }
             if (l.keep) SO_TRY(launch(prob_kernel<T>, (unsigned)(8 * sms), 256, 0, st, true, q));
-            else SO_TRY((launch_product<T, kProb, kCtas>(hidden_k, table_k, prob_out, q, units, st)));
-            if (c.dhidden) SO_TRY((launch_product<T, kHidden, kCtas>(prob_k, table_m, part_out, q, units, st)));
-            if (c.dtable) SO_TRY((launch_product<T, kTable, kCtas>(prob_m, hidden_m, grad_out, q, units, st)));
+            else SO_TRY((launch_product<T, kProb, kCtas>(logits, q, units, st)));
+            gradient.b = table_m;
+            SO_TRY((launch_product<T, kGradients, kCtas>(gradient, q, units, st)));
         }
     }
     if (!gradients) return SO_OK;
