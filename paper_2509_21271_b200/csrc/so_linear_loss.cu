@@ -376,7 +376,7 @@ __device__ __forceinline__ void copy_out(const CUtensorMap *map, uint32_t box, i
 
 // Half a tile, n-th of the columns.  A row's maximum and sum over it, its label's logit if that is
 // here, and the logits themselves where they are kept.
-__device__ __forceinline__ void end_stats(const Product &p, uint32_t tmem, int64_t row, int live, int n)
+__device__ __forceinline__ void end_stats(const Product &p, const CUtensorMap *map, uint32_t box, uint32_t tmem, int64_t row, int live, int n)
 {
     const int64_t n0 = p.first + (int64_t)n * kEndCols;
     const int cols = p.vocab - n0 < kEndCols ? (int)(p.vocab - n0) : kEndCols;
@@ -406,15 +406,11 @@ __device__ __forceinline__ void end_stats(const Product &p, uint32_t tmem, int64
     for (int c = 0; c < cols; c += 32) {
         float f[32];
         tmem_load(tmem + c, f);
-        if (p.kept && in) {
-            float *out = p.kept + row * p.prob_stride + n0 + c;
+        if (p.kept && row - (int64_t)(threadIdx.x & 31) < live) {
+            uint32_t w[32];
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-                uint32_t w[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(f[i + j]);
-                store32(out + i, w);
-            }
+            for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(f[i]);
+            copy_out(map, box, (int)n0 + c, (int)row - (int)(threadIdx.x & 31), w, false);
         }
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
@@ -423,29 +419,6 @@ __device__ __forceinline__ void end_stats(const Product &p, uint32_t tmem, int64
         }
     }
     if (in) p.stats[(n0 / kEndCols) * p.rows_pad + row] = make_float2(top, sum0 + sum1);
-}
-
-// 32 elements of P in `planes` parts of 16 bits; `f` is used up.
-template <typename T>
-__device__ __forceinline__ void store_prob(const Product &p, float (&f)[32], T *to)
-{
-    for (int plane = 0;; ++plane) {
-        uint32_t w[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = pack2<T>(f[2 * i], f[2 * i + 1]);
-        const uint32_t a[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]}, b[8] = {w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]};
-        store32(to, a);
-        store32(to + 16, b);
-        if (plane + 1 == p.planes) break;
-        to += (int64_t)p.rows_pad * p.prob_stride;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float lo, hi;
-            unpack2<T>(w[i], lo, hi);
-            f[2 * i] -= lo;
-            f[2 * i + 1] -= hi;
-        }
-    }
 }
 
 // P of the tile, in `planes` parts of 16 bits; zero in rows and columns that are not there.
@@ -741,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             fence_after();
             const uint32_t at = tmem + buffer * kTileN + half * kEndCols + (lanes << 16);
             const int64_t row = ((int64_t)it.m * kCtas + rank) * kRowsOfCta + lanes + lane;
-            if (kMode == kStats) end_stats(p, at, row, live, 2 * it.n + half);
+            if (kMode == kStats) end_stats(p, &maps.out, box, at, row, live, 2 * it.n + half);
             else if (kMode == kProb) end_prob<T>(p, &maps.out, box, at, row, live, 2 * it.n + half);
             else if (it.kind == kHidden) end_hidden(p, &maps.out, box, at, row, 2 * it.n + half, it.split, it.steps == 0);
             else if (p.grad_boxes) end_table(p, &maps.out2, box, at, row, 2 * it.n + half, scale);
@@ -755,7 +728,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             buffer ^= 1;
             if (buffer == 0) phase ^= 1;
         }
-        if (kMode != kStats && lane == 0) tma_stores_done();
+        if (lane == 0) tma_stores_done();
     }
     __syncthreads();
     if (kCtas == 2) cluster_sync();
@@ -913,35 +886,40 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
     }
 }
 
-// P from logits that were kept: 32 columns of a row a thread, rows up to whole steps of the sums over them.
+// P from logits that were kept: 8 columns of a row a thread, rows up to whole steps of the sums over them.
 template <typename T>
 __global__ void __launch_bounds__(256) prob_kernel(const __grid_constant__ Product p)
 {
     grid_dependency_wait();
     grid_dependency_release();
     const int live = p.control->live;
-    const int64_t groups = p.prob_stride / 32, all = (int64_t)((live + kTileK - 1) / kTileK * kTileK) * groups;
+    const int64_t groups = p.prob_stride / 8, all = (int64_t)((live + kTileK - 1) / kTileK * kTileK) * groups;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / groups, c = (i - row * groups) * 32;
-        const bool in = row < live;
-        float f[32] = {};
-        if (in) {
+        const int64_t row = i / groups, c = (i - row * groups) * 8;
+        float f[8] = {};
+        if (row < live) {
             const int64_t label = p.label[row] - c;
             const float lse2 = p.lse2[row], coef = p.coef[row];
-            const float *z = p.kept + row * p.prob_stride + c;
+            uint32_t w[8];
+            load32(p.kept + row * p.prob_stride + c, w);
 #pragma unroll
-            for (int k = 0; k < 32; k += 8) {
-                uint32_t w[8];
-                load32(z + k, w);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float q = exp2_fast(fmaf(__uint_as_float(w[j]), kLog2e, -lse2));
-                    if (label == k + j) q -= 1.0f;
-                    f[k + j] = c + k + j < p.vocab ? q * coef : 0.0f;
-                }
+            for (int j = 0; j < 8; ++j) {
+                float q = exp2_fast(fmaf(__uint_as_float(w[j]), kLog2e, -lse2));
+                if (label == j) q -= 1.0f;
+                f[j] = c + j < p.vocab ? q * coef : 0.0f;
             }
         }
-        store_prob<T>(p, f, static_cast<T *>(p.prob) + row * p.prob_stride + c);
+        T *to = static_cast<T *>(p.prob) + row * p.prob_stride + c;
+        for (int plane = 0;; ++plane) {
+            const uint4 w = pack<T>(f);
+            *reinterpret_cast<uint4 *>(to) = w;
+            if (plane + 1 == p.planes) break;
+            to += (int64_t)p.rows_pad * p.prob_stride;
+            float held[8];
+            unpack<T>(w, held);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] -= held[j];
+        }
     }
 }
 
@@ -1323,6 +1301,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     if (!make_map(&logits.a, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld, kRowsOfCta) || !make_group_map(&gradient.b2, r.gathered, c.dtype, l.rows_pad, c.cols, l.ld))
         return SO_ERR_CUDA;
     logits.out = logits.a2 = logits.b2 = logits.out2 = logits.a;
+    if (l.keep && !make_map(&logits.out, p.kept, SO_DTYPE_FP32, l.rows_pad, l.piece, l.piece, 32)) return SO_ERR_CUDA;
     const auto table_maps = [&](int64_t rows) {
         const void *at = l.packed ? static_cast<const void *>(packed) : c.table;
         const int64_t stride = l.packed ? l.ld : c.vocab == 1 ? l.ld : c.table_stride;
@@ -1353,7 +1332,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
         // (what a warp copies out is 32 rows)
         if (!make_map(&gradient.a, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, kRowsOfCta) ||
             !make_group_map(&gradient.a2, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece) ||
-            !make_map(&logits.out, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, 32) ||
+            (!l.keep && !make_map(&logits.out, p.prob, c.dtype, l.rows_pad * l.planes, l.piece, l.piece, 32)) ||
             !make_map(&gradient.out, p.part, SO_DTYPE_FP32, l.rows_pad * l.splits, l.part_stride, l.part_stride, 32))
             return SO_ERR_CUDA;
         gradient.out2 = gradient.out;

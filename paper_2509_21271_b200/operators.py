@@ -238,19 +238,31 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, *, dx=None, dweight=None
 
 # ---- the norms on both sides of a residual ------------------------------------------
 
-def _params(where, dt, dev, cols, gate, named):
-    """(dtype, gate's address, number of gates, the others' addresses) of parameters of one dtype."""
-    first = gate
-    for _, t in named:
-        first = t if first is None else first
-    if first is None:
-        return dt, None, 1, [None] * len(named)
-    pt = _dtype(where, "weight", first)
-    groups = 1 if gate is None or gate.dim() == 1 else gate.shape[0]
-    if gate is not None and (gate.dim() > 2 or gate.shape[-1] != cols):
+def _param(where, name, t, n, dev, dtype):
+    """_vector's address of a parameter; its checks one by one only where something is wrong."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.numel() == n and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    return _vector(where, name, t, n, dev, dtype)
+
+
+def _gate(where, gate, cols):
+    """How many gates there are."""
+    if gate is None or gate.dim() == 1 and gate.shape[0] == cols:
+        return 1
+    if gate.dim() != 2 or gate.shape[1] != cols:
         _refuse(where, "gate must be a row, or a matrix of one row per group of rows")
-    return pt, _vector(where, "gate", gate, groups * cols, dev, first.dtype), groups, \
-        [_vector(where, name, t, cols, dev, first.dtype) for name, t in named]
+    return gate.shape[0]
+
+
+def _like(where, name, t, like_name, like, dev, rows, cols):
+    """Row stride of a matrix with the shape and dtype of `like`."""
+    if t.shape != like.shape or t.dtype != like.dtype:
+        _same(where, name, t, like_name, like)
+    if t.get_device() == dev and t.is_contiguous():
+        return cols
+    return _rows(where, name, t, dev)[2]
 
 
 def residual_norm_forward(x, block, gate=None, post_weight=None, post_bias=None, weight=None, bias=None, *,
@@ -268,37 +280,38 @@ def residual_norm_forward(x, block, gate=None, post_weight=None, post_bias=None,
         return _on_stream(stream, residual_norm_forward, x, block, gate, post_weight, post_bias, weight, bias,
                           kind=kind, post=post, scale=scale, eps=eps, h=h, y=y, stats=stats, save_stats=save_stats)
     where = "residual_norm_forward"
-    if x.requires_grad or block.requires_grad or any(
-            t is not None and t.requires_grad for t in (gate, post_weight, post_bias, weight, bias)):
+    if x.requires_grad or block.requires_grad or gate is not None and gate.requires_grad \
+            or post_weight is not None and post_weight.requires_grad or post_bias is not None and post_bias.requires_grad \
+            or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad:
         _recorded(where)
     dev = _device(where, "x", x)
     dt = _dtype(where, "x", x)
-    _same(where, "block", block, "x", x)
     rows, cols, stride = _rows(where, "x", x, dev)
-    _, _, block_stride = _rows(where, "block", block, dev)
+    block_stride = _like(where, "block", block, "x", x, dev, rows, cols)
     if kind not in _KINDS:
         _refuse(where, "kind is 'layer' or 'rms'")
     if h is None:
         h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    else:
-        _same(where, "h", h, "x", x)
     if y is None:
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    else:
-        _same(where, "y", y, "x", x)
-    _, _, h_stride = _rows(where, "h", h, dev)
-    _, _, y_stride = _rows(where, "y", y, dev)
-    pt, gp, groups, (pw, pb, w, b) = _params(where, dt, dev, cols, gate, (
-        ("post_weight", post_weight), ("post_bias", post_bias), ("weight", weight), ("bias", bias)))
+    h_stride = _like(where, "h", h, "x", x, dev, rows, cols)
+    y_stride = _like(where, "y", y, "x", x, dev, rows, cols)
+    groups = _gate(where, gate, cols)
+    first = gate if gate is not None else post_weight if post_weight is not None else post_bias if post_bias is not None \
+        else weight if weight is not None else bias
+    kept = x.dtype if first is None else first.dtype
+    pt = dt if first is None else _dtype(where, "a parameter", first)
     if not save_stats:
         if stats is not None:
             _refuse(where, "stats are not written with save_stats=False")
     elif stats is None:
         stats = torch.empty(4, rows, dtype=torch.float32, device=x.device)
     _done(B.lib().so_residual_norm_forward(
-        x.data_ptr(), stride, block.data_ptr(), block_stride, gp, groups, pw, pb, w, b, h.data_ptr(), h_stride,
-        y.data_ptr(), y_stride, _vector(where, "stats", stats, 4 * rows, dev, torch.float32), rows, cols, dt, pt,
-        _KINDS[kind], int(post), scale, eps, _raw_stream(dev)), where, (h, y) if stats is None else (h, y, stats))
+        x.data_ptr(), stride, block.data_ptr(), block_stride, _param(where, "gate", gate, groups * cols, dev, kept), groups,
+        _param(where, "post_weight", post_weight, cols, dev, kept), _param(where, "post_bias", post_bias, cols, dev, kept),
+        _param(where, "weight", weight, cols, dev, kept), _param(where, "bias", bias, cols, dev, kept), h.data_ptr(),
+        h_stride, y.data_ptr(), y_stride, _param(where, "stats", stats, 4 * rows, dev, torch.float32), rows, cols, dt, pt,
+        _KINDS[kind], post, scale, eps, _raw_stream(dev)), where, (h, y) if stats is None else (h, y, stats))
     return h, y, stats
 
 
@@ -320,65 +333,63 @@ def residual_norm_backward(dy, dh, h, block, stats, gate=None, post_weight=None,
                           dpost_weight=dpost_weight, dpost_bias=dpost_bias, dweight=dweight, dbias=dbias,
                           accumulate=accumulate, scratch=scratch)
     where = "residual_norm_backward"
-    if dy.requires_grad or h.requires_grad or block.requires_grad or any(
-            t is not None and t.requires_grad for t in (dh, gate, post_weight, post_bias, weight)):
+    if dy.requires_grad or h.requires_grad or block.requires_grad or dh is not None and dh.requires_grad \
+            or gate is not None and gate.requires_grad or post_weight is not None and post_weight.requires_grad \
+            or post_bias is not None and post_bias.requires_grad or weight is not None and weight.requires_grad:
         _recorded(where)
     dev = _device(where, "h", h)
     dt = _dtype(where, "h", h)
     rows, cols, h_stride = _rows(where, "h", h, dev)
-    _same(where, "dy", dy, "h", h)
-    _same(where, "block", block, "h", h)
-    _, _, dy_stride = _rows(where, "dy", dy, dev)
-    _, _, block_stride = _rows(where, "block", block, dev)
-    dh_stride = 0
-    if dh is not None:
-        _same(where, "dh", dh, "h", h)
-        _, _, dh_stride = _rows(where, "dh", dh, dev)
+    dy_stride = _like(where, "dy", dy, "h", h, dev, rows, cols)
+    block_stride = _like(where, "block", block, "h", h, dev, rows, cols)
+    dh_stride = 0 if dh is None else _like(where, "dh", dh, "h", h, dev, rows, cols)
     if kind not in _KINDS:
         _refuse(where, "kind is 'layer' or 'rms'")
     if dx is None:
         dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-    else:
-        _same(where, "dx", dx, "h", h)
     if dblock is None:
         dblock = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-    else:
-        _same(where, "dblock", dblock, "h", h)
-    _, _, dx_stride = _rows(where, "dx", dx, dev)
-    _, _, dblock_stride = _rows(where, "dblock", dblock, dev)
-    pt, gp, groups, (pw, pb, w) = _params(where, dt, dev, cols, gate, (
-        ("post_weight", post_weight), ("post_bias", post_bias), ("weight", weight)))
-    kind_of = next((t.dtype for t in (gate, post_weight, post_bias, weight) if t is not None), h.dtype)
-    grads = []
-    for name, g, n, wanted in (("dgate", dgate, groups * cols, gate is not None),
-                               ("dpost_weight", dpost_weight, cols, post_weight is not None),
-                               ("dpost_bias", dpost_bias, cols, post_bias is not None),
-                               ("dweight", dweight, cols, True), ("dbias", dbias, cols, kind == "layer")):
-        if g is None and wanted:
-            if accumulate:
-                _refuse(where, f"accumulate needs {name} (or False)")
-            g = torch.empty(gate.shape if name == "dgate" else (cols,), dtype=kind_of, device=h.device)
-        elif g is False:
-            g = None
-        elif g is not None and not wanted and name == "dgate":
-            _refuse(where, "there is no gate to have a gradient")
-        grads.append((name, g, n))
-    some = next((g for _, g, _ in grads if g is not None), None)
-    gt, need, ws = dt, 0, None
+    dx_stride = _like(where, "dx", dx, "h", h, dev, rows, cols)
+    dblock_stride = _like(where, "dblock", dblock, "h", h, dev, rows, cols)
+    groups = _gate(where, gate, cols)
+    first = gate if gate is not None else post_weight if post_weight is not None else post_bias if post_bias is not None \
+        else weight
+    kept = h.dtype if first is None else first.dtype
+    pt = dt if first is None else _dtype(where, "a parameter", first)
+    if accumulate and (dgate is None and gate is not None or dpost_weight is None and post_weight is not None
+                       or dpost_bias is None and post_bias is not None or dweight is None
+                       or dbias is None and kind == "layer"):
+        _refuse(where, "accumulate needs the gradients to add to (or False)")
+    if gate is None and dgate is not None and dgate is not False:
+        _refuse(where, "there is no gate to have a gradient")
+    new = lambda shape: torch.empty(shape, dtype=kept, device=h.device)  # noqa: E731
+    dgate = None if dgate is False else new(gate.shape) if dgate is None and gate is not None else dgate
+    dpost_weight = None if dpost_weight is False else new(cols) if dpost_weight is None and post_weight is not None \
+        else dpost_weight
+    dpost_bias = None if dpost_bias is False else new(cols) if dpost_bias is None and post_bias is not None else dpost_bias
+    dweight = None if dweight is False else new(cols) if dweight is None else dweight
+    dbias = None if dbias is False else new(cols) if dbias is None and kind == "layer" else dbias
+    out = (dx, dblock, dgate, dpost_weight, dpost_bias, dweight, dbias)
+    some = dweight if dweight is not None else dgate if dgate is not None else dpost_weight if dpost_weight is not None \
+        else dpost_bias if dpost_bias is not None else dbias
+    gt, need, ws, kind_of = dt, 0, None, None
     if some is not None:
+        kind_of = some.dtype
         gt = _dtype(where, "a parameter's gradient", some)
         if scratch is None:
             scratch = torch.empty(_residual_scratch(rows, cols, groups), dtype=torch.uint8, device=h.device)
         need, ws = _scratch(where, scratch, dev), scratch.data_ptr()
-    out = tuple(g for _, g, _ in grads)
     _done(B.lib().so_residual_norm_backward(
         dy.data_ptr(), dy_stride, None if dh is None else dh.data_ptr(), dh_stride, h.data_ptr(), h_stride,
-        block.data_ptr(), block_stride, _vector(where, "stats", stats, 4 * rows, dev, torch.float32), gp, groups, pw, pb,
-        w, dx.data_ptr(), dx_stride, dblock.data_ptr(), dblock_stride,
-        *[_vector(where, name, g, n, dev, some.dtype if g is not None else None) for name, g, n in grads], rows, cols, dt,
-        pt, gt, _KINDS[kind], int(post), int(accumulate), scale, ws, need, _raw_stream(dev)), where,
-        [t for t in (dx, dblock, *out) if t is not None])
-    return (dx, dblock, *out)
+        block.data_ptr(), block_stride, _param(where, "stats", stats, 4 * rows, dev, torch.float32),
+        _param(where, "gate", gate, groups * cols, dev, kept), groups, _param(where, "post_weight", post_weight, cols, dev, kept),
+        _param(where, "post_bias", post_bias, cols, dev, kept), _param(where, "weight", weight, cols, dev, kept),
+        dx.data_ptr(), dx_stride, dblock.data_ptr(), dblock_stride, _param(where, "dgate", dgate, groups * cols, dev, kind_of),
+        _param(where, "dpost_weight", dpost_weight, cols, dev, kind_of), _param(where, "dpost_bias", dpost_bias, cols, dev, kind_of),
+        _param(where, "dweight", dweight, cols, dev, kind_of), _param(where, "dbias", dbias, cols, dev, kind_of), rows, cols, dt,
+        pt, gt, _KINDS[kind], post, accumulate, scale, ws, need, _raw_stream(dev)), where,
+        [t for t in out if t is not None])
+    return out
 
 
 # ---- embedding -------------------------------------------------------------------

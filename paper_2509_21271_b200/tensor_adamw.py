@@ -76,6 +76,11 @@ class TensorAdamW:
         self._scratch = zeros(info.bytes_scratch, torch.uint8)
         #: norm of the gradients, clip factor and whether the step was skipped (1.0), of the last step
         self.stats = self._record[8:20].view(torch.float32)
+        eight = state_bits == 8
+        self._state = (state_bits, self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr() if eight else None,
+                       self.v_scale.data_ptr() if eight else None)
+        self._work = (self._record.data_ptr(), self._scratch.data_ptr(), self._scratch.numel())
+        self._hp = B.so_hparams()
         self._written = [*self.params, *(self.copies or ()), self.m, self.v, self._record]
         if state_bits == 8:
             self._written += [self.m_scale, self.v_scale]
@@ -112,12 +117,12 @@ class TensorAdamW:
             _refuse(where, "the parameters are not on the current device")
         if seed is not None and self.state_bits != 8:
             _refuse(where, "a seed is for 8-bit moments")
-        eight = self.state_bits == 8
+        h = self._hp
+        h.lr, h.beta1, h.beta2, h.eps = hp.lr, hp.beta1, hp.beta2, hp.eps
+        h.weight_decay, h.max_grad_norm = hp.weight_decay, hp.max_grad_norm
         status = B.lib().so_tensor_adamw_step(
-            self._list, len(self._list), self._grad_dtype, self._copy_dtype, self.state_bits, self.m.data_ptr(),
-            self.v.data_ptr(), self.m_scale.data_ptr() if eight else None, self.v_scale.data_ptr() if eight else None,
-            C.byref(B._hp(hp)), grad_scale, int(clip), int(seed is not None), (seed or 0) & 0xFFFFFFFFFFFFFFFF,
-            self._record.data_ptr(), self._scratch.data_ptr(), self._scratch.numel(),
+            self._list, len(self._list), self._grad_dtype, self._copy_dtype, *self._state, C.byref(h), grad_scale, bool(clip),
+            seed is not None, (seed or 0) & 0xFFFFFFFFFFFFFFFF, *self._work,
             _raw_stream(self.device.index) if stream is None else stream.cuda_stream)
         if status != B.SO_OK:
             raise B.SuperOffloadError(status, "so_" + where)
