@@ -9,8 +9,14 @@ Activations are bf16; every parameter's gradient is written straight into the
 optimizer's bf16 gradient arena, the table's in two parts: the head's matrix
 product writes it, the embedding's backward pass adds to it.
 
+With ``--labels`` another student learns the next token from labels: RMS norms on both
+sides of every residual with a learned gate, the cross entropy and both gradients of the
+head straight from the hidden states, and parameters in tensors of their own under AdamW
+with 8-bit moments.
+
     python examples/train_student.py --steps 40
     python examples/train_student.py --steps 40 --policy
+    python examples/train_student.py --steps 40 --labels
 """
 from __future__ import annotations
 
@@ -26,6 +32,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2509_21271_b200 import binding as B                      # noqa: E402
 from paper_2509_21271_b200 import operators as ops                  # noqa: E402
 from paper_2509_21271_b200.optimizer import BucketedAdamW           # noqa: E402
+from paper_2509_21271_b200.tensor_adamw import TensorAdamW          # noqa: E402
 
 
 @dataclass
@@ -98,6 +105,79 @@ class Student:
         return self.opt.iteration(hp, stream=torch.cuda.current_stream())
 
 
+class LabelStudent:
+    """A student of labels: parameters, gradients and bf16 copies in tensors of their own."""
+
+    def __init__(self, vocab: int = 4001, width: int = 256, blocks: int = 2, seed: int = 0, state_bits: int = 8):
+        self.vocab, self.width, self.blocks = vocab, width, blocks
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+        one = lambda at: torch.full((width,), at, device="cuda")  # noqa: E731
+        self.master = {"table": rand(vocab, width) * width ** -0.5, "norm.w": one(1.0), "norm.b": one(0.0)}
+        for i in range(blocks):
+            self.master.update({f"up{i}": rand(width, 4 * width) * width ** -0.5, f"gate{i}": one(0.5), f"post{i}": one(1.0),
+                                f"down{i}": rand(4 * width, width) * (4 * width) ** -0.5, f"pre{i}": one(1.0)})
+        self.param = {k: v.to(torch.bfloat16) for k, v in self.master.items()}
+        self.grad = {k: torch.zeros_like(v) for k, v in self.param.items()}
+        self.opt = TensorAdamW(list(self.master.values()), list(self.grad.values()), copies=list(self.param.values()),
+                               state_bits=state_bits)
+
+    def forward(self, ids):
+        """(hidden states, what the backward pass needs)."""
+        p, kept = self.param, []
+        h = ops.embedding_forward(ids, p["table"], self.width ** 0.5)
+        x, mean, rstd = ops.layer_norm_forward(h, p["norm.w"], p["norm.b"])
+        first = (h, mean, rstd)
+        for i in range(self.blocks):
+            up = torch.matmul(x, p[f"up{i}"])
+            act = torch.relu(up).square_()
+            block = torch.matmul(act, p[f"down{i}"])
+            before = x
+            h, x, stats = ops.residual_norm_forward(h, block, p[f"gate{i}"], p[f"post{i}"], None, p[f"pre{i}"], None,
+                                                    kind="rms")
+            kept.append((before, up, act, block, h, stats))
+        return x, (ids, first, kept)
+
+    def loss_and_gradients(self, ids, labels, weight):
+        """The loss; the gradients of all parameters."""
+        p, g = self.param, self.grad
+        hidden, (ids, first, kept) = self.forward(ids)
+        loss, _, dx, _ = ops.linear_cross_entropy(hidden, p["table"], labels, weight, dtable=g["table"])
+        dh = None
+        for i in reversed(range(self.blocks)):
+            before, up, act, block, h, stats = kept[i]
+            dh, dblock, *_ = ops.residual_norm_backward(
+                dx, dh, h, block, stats, p[f"gate{i}"], p[f"post{i}"], None, p[f"pre{i}"], kind="rms", dgate=g[f"gate{i}"],
+                dpost_weight=g[f"post{i}"], dweight=g[f"pre{i}"])
+            torch.mm(act.t(), dblock, out=g[f"down{i}"])
+            dup = torch.matmul(dblock, p[f"down{i}"].t()).mul_(torch.relu(up).mul_(2.0))
+            torch.mm(before.t(), dup, out=g[f"up{i}"])
+            dx = torch.matmul(dup, p[f"up{i}"].t())
+        h, mean, rstd = first
+        dx, _, _ = ops.layer_norm_backward(dx, h, mean, rstd, p["norm.w"], dweight=g["norm.w"], dbias=g["norm.b"])
+        ops.embedding_backward(ids, dx if dh is None else dx + dh, g["table"], self.width ** 0.5, accumulate=True)
+        return loss
+
+    def step(self, hp: HParams, seed: int | None = 0):
+        return self.opt.step(hp, seed=seed if self.opt.state_bits == 8 else None)
+
+
+def train_labels(steps: int = 40, tokens: int = 512, student: LabelStudent | None = None, hp=None):
+    """Losses by step, and whether each was skipped: the next token is a fixed function of the last."""
+    student, hp = student or LabelStudent(), hp or HParams()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    follows = torch.randint(student.vocab, (student.vocab,), generator=gen, device="cuda")
+    losses, skipped = [], []
+    for _ in range(steps):
+        ids = torch.randint(64, (tokens,), generator=gen, device="cuda")
+        labels = follows[ids]
+        labels[::8] = -100                            # as where a prompt is not learned
+        weight = (labels >= 0) / (labels >= 0).sum()
+        losses.append(student.loss_and_gradients(ids, labels, weight)[0])
+        skipped.append(student.step(hp)[2].clone())
+    return [float(x) for x in losses], [bool(x) for x in skipped]
+
+
 def teacher_lists(vocab: int, top_k: int, seed: int = 1):
     """A fixed teacher: for each token the ids that may follow, and their logits."""
     gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -136,7 +216,12 @@ def main():
     parser.add_argument("--steps", type=int, default=40)
     parser.add_argument("--tokens", type=int, default=512)
     parser.add_argument("--policy", action="store_true")
+    parser.add_argument("--labels", action="store_true")
     args = parser.parse_args()
+    if args.labels:
+        for i, (v, gone) in enumerate(zip(*train_labels(args.steps, args.tokens)), 1):
+            print(f"step {i:3d}  loss {v:8.4f}  {'SKIP' if gone else 'STEP'}")
+        return
     values, decisions = train(args.steps, args.tokens, args.policy)
     what = "mean advantage" if args.policy else "loss"
     for i, (v, d) in enumerate(zip(values, decisions), 1):

@@ -201,6 +201,7 @@ struct Product {
     float *label_logit;                   // [rows_pad]
     const float *lse2;                    // [rows_pad], in units of log 2
     const float *coef;                    // [rows_pad], w over the unit
+    float *residual;                      // [rows_pad]: what P at the label lost when it was rounded
     float2 *stats;                        // [half tiles of the vocabulary][rows_pad]: maximum, sum
     float *kept;                          // kStats: [rows_pad][prob_stride], where all logits are kept
     void *prob;                           // [planes][rows_pad][prob_stride]
@@ -444,6 +445,7 @@ __device__ __forceinline__ void end_prob(const Product &p, const CUtensorMap *ma
                 float q = exp2_fast(fmaf(f[h][i], kLog2e, -lse2));
                 if (here && label == c0 + i) q -= 1.0f;
                 f[h][i] = in && c0 + i < cols ? q * coef : 0.0f;
+                if (here && label == c0 + i) p.residual[row] = f[h][i] - to_f32(from_f32<T>(f[h][i]));
             }
         }
         for (int plane = 0;; ++plane) {
@@ -600,7 +602,6 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         mbar_init(smem_addr(&s.last), 1);
         mbar_init_fence();
         s.gave_up = polls == 0;
-        if (polls == 0) atomicExch(&p.control->gave_up, 1);
     }
     if (warp == 1) tmem_alloc<kCtas>(smem_addr(&s.tmem), 512);
     fence_before();
@@ -610,6 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const uint32_t tmem = s.tmem;
     grid_dependency_wait();
     grid_dependency_release();            // the next launch waits for this one's end before it reads anything
+    if (polls == 0 && threadIdx.x == 0) atomicExch(&p.control->gave_up, 1);
     const int live = p.control->live;
     const Work<kMode, kCtas> work(p, live);
 
@@ -907,6 +909,7 @@ __global__ void __launch_bounds__(256) prob_kernel(const __grid_constant__ Produ
                 float q = exp2_fast(fmaf(__uint_as_float(w[j]), kLog2e, -lse2));
                 if (label == j) q -= 1.0f;
                 f[j] = c + j < p.vocab ? q * coef : 0.0f;
+                if (label == j) p.residual[row] = f[j] - to_f32(from_f32<T>(f[j]));
             }
         }
         T *to = static_cast<T *>(p.prob) + row * p.prob_stride + c;
@@ -1015,18 +1018,21 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_cons
 
 struct Finish {
     Control *control;
-    const float *part;
-    const int32_t *index;
+    const float *part, *residual;
+    const int32_t *index, *label;
+    const void *table;
+    int64_t table_stride;
     void *dhidden, *table_grad;
     float *row_loss, *loss;
     int64_t rows, vocab, cols, dhidden_stride, grad_stride, part_stride;
-    int32_t rows_pad, splits, grad_dtype, vectors, accumulate;
+    int32_t rows_pad, splits, grad_dtype, vectors, table_vectors, accumulate;
     float grad_scale;
 };
 
 constexpr int kFinishThreads = 128;
 
-// dH from its parts.  dW where no row took part: zeros, unless it
+// dH from its parts, and what the label's P lost in its rounding times the label's row: where one row
+// of the table outweighs the others, that rounding would be all of dH's.  dW where no row took part: zeros, unless it
 // is added to.  NaN everywhere after a wait that ran out.
 template <typename T>
 __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ Finish f)
@@ -1080,8 +1086,18 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_con
         }
         if (!in || (share && warp > 0)) continue;
         T *out = static_cast<T *>(f.dhidden) + (int64_t)f.index[row] * f.dhidden_stride + c;
+        const T *at = static_cast<const T *>(f.table) + (int64_t)f.label[row] * f.table_stride + c;
+        const float residual = f.residual[row];
+        float w[8] = {};
+        if (f.table_vectors && c + 8 <= f.cols) {
+            unpack<T>(*reinterpret_cast<const uint4 *>(at), w);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] *= scale;
+            for (int i = 0; i < 8; ++i)
+                if (c + i < f.cols) w[i] = to_f32(at[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = fmaf(residual, w[i], sum[i]) * scale;
         if (f.vectors && c + 8 <= f.cols) {
             *reinterpret_cast<uint4 *>(out) = pack<T>(sum);
         } else {
@@ -1109,7 +1125,7 @@ int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 struct Layout {
     int64_t rows_pad, ld, pieces, piece, splits, planes, part_stride, halves;
     bool packed, keep;
-    uint64_t control, counts, index, label, w, label_logit, lse2, coef, sums, stats, gathered, kept, prob, part, table, bytes;
+    uint64_t control, counts, index, label, w, label_logit, lse2, coef, residual, sums, stats, gathered, kept, prob, part, table, bytes;
 };
 
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of P, unless rows are so many that pieces would get short
@@ -1162,6 +1178,7 @@ Layout layout(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t 
     l.label_logit = take(rp * 4);
     l.lse2 = take(rp * 4);
     l.coef = take(rp * 4);
+    l.residual = take(rp * 4);
     l.sums = take(rp / 32 * 8);
     l.stats = take(rp * (uint64_t)l.halves * 8);
     l.gathered = take(rp * (uint64_t)l.ld * 2);
@@ -1283,6 +1300,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     p.label_logit = reinterpret_cast<float *>(scratch + l.label_logit);
     float *lse2 = reinterpret_cast<float *>(scratch + l.lse2), *coef = reinterpret_cast<float *>(scratch + l.coef);
     p.lse2 = lse2, p.coef = coef;
+    p.residual = reinterpret_cast<float *>(scratch + l.residual);
     p.stats = reinterpret_cast<float2 *>(scratch + l.stats);
     p.prob = scratch + l.prob, p.prob_stride = l.piece;
     p.kept = l.keep ? reinterpret_cast<float *>(scratch + l.kept) : nullptr;
@@ -1356,8 +1374,8 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
         }
     }
     if (!gradients) return SO_OK;
-    Finish f = {control, p.part, index, c.dhidden, c.dtable, c.row_loss, c.loss, c.rows, c.vocab, c.cols, c.dhidden_stride, c.dtable_stride, l.part_stride,
-                (int32_t)l.rows_pad, (int32_t)l.splits, c.grad_dtype, r.dhidden_vectors, c.accumulate, c.grad_scale};
+    Finish f = {control, p.part, p.residual, index, label, c.table, c.table_stride, c.dhidden, c.dtable, c.row_loss, c.loss, c.rows, c.vocab, c.cols, c.dhidden_stride, c.dtable_stride, l.part_stride,
+                (int32_t)l.rows_pad, (int32_t)l.splits, c.grad_dtype, r.dhidden_vectors, !l.packed, c.accumulate, c.grad_scale};
     return launch(finish_kernel<T>, (unsigned)(16 * sms), kFinishThreads, 0, st, true, f);
 }
 

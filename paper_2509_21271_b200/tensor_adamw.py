@@ -51,10 +51,14 @@ class TensorAdamW:
         if self.device.index != _current_device():
             _refuse(where, "the parameters are not on the current device")
         self._list = (B.so_tensor * n)()
+        seen = set()
         for e, p in zip(self._list, self.params):
             if p.dtype != torch.float32:
                 _refuse(where, "parameters are float32")
             self._check(where, "parameter", p, p.numel())
+            if p.numel() and p.data_ptr() in seen:
+                _refuse(where, "a parameter is in the list twice")
+            seen.add(p.data_ptr())
             e.param, e.numel = p.data_ptr(), p.numel()
         self._copy_dtype = B.SO_TENSOR_NO_COPY
         if self.copies is not None:
@@ -108,7 +112,8 @@ class TensorAdamW:
         weight_decay, max_grad_norm).  `clip` looks at the gradients first: their norm
         is brought down to ``hp.max_grad_norm`` (where that is positive), and a step
         whose norm is not finite is skipped.  `grad_scale` multiplies the gradients (1 /
-        loss scale).  `seed` rounds 8-bit moments stochastically.  Returns `stats`.
+        loss scale).  `seed` rounds 8-bit moments stochastically.  Returns `stats`.  What is
+        given here is a captured step's for all its replays; t and the random numbers go on.
 
         Runs on the current stream, or on `stream`; the tensors are the optimizer's, which
         the caller keeps until that stream is done with them."""

@@ -277,5 +277,6 @@ def test_waits_that_run_out_make_everything_nan(rows):
     for unit in (-1, 0):
         with no_patience(unit):
             got = ops.linear_cross_entropy(hidden, table, labels)
-        assert all(torch.isnan(t).all() for t in got)
+            alone = ops.linear_cross_entropy(hidden, table, labels, dhidden=False, dtable=False)
+        assert all(torch.isnan(t).all() for t in (*got, *alone[:2]))
     assert all(same_bits(a, b) for a, b in zip(ops.linear_cross_entropy(hidden, table, labels), want))

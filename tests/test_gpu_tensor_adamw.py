@@ -352,7 +352,7 @@ def test_refusals():
            lambda: TensorAdamW([p.half()], [g]), lambda: TensorAdamW([p], [g[:7]]), lambda: TensorAdamW([p[::2]], [g[:4]]),
            lambda: TensorAdamW([p], [g.long()]), lambda: TensorAdamW([p, p], [g, g.half()]),
            lambda: TensorAdamW([p], [g], copies=[p]), lambda: TensorAdamW([p], [g], copies=[]),
-           lambda: TensorAdamW([p], [g.cpu()]), lambda: TensorAdamW([p.cpu()], [g]),
+           lambda: TensorAdamW([p], [g.cpu()]), lambda: TensorAdamW([p, p], [g, g]), lambda: TensorAdamW([p.cpu()], [g]),
            lambda: TensorAdamW([p], [g]).step(HP(), seed=1), lambda: TensorAdamW([p], [g]).set_step(-1)]
     for name, value in (("lr", -1.0), ("lr", float("nan")), ("beta1", 1.0), ("beta2", -0.1), ("eps", 0.0), ("eps", 1e-60),
                         ("weight_decay", -1.0), ("max_grad_norm", float("nan"))):
