@@ -211,7 +211,7 @@ struct Product {
     int32_t want_hidden;
     void *table_grad;
     int64_t grad_stride;
-    int32_t grad_dtype, accumulate, grad_vectors, grad_boxes;
+    int32_t grad_dtype, accumulate, grad_boxes;
     float grad_scale;
     Patience patience;
 };
@@ -336,12 +336,7 @@ __device__ __forceinline__ bool elected()
     return yes != 0;
 }
 
-// 16 elements of a row as T (or 8 as fp32) in one store
-__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8])
-{
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
-                 "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
-}
+// 32 bytes
 __device__ __forceinline__ void load32(const void *p, uint32_t (&w)[8])
 {
     asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -359,8 +354,8 @@ template <typename T> __device__ __forceinline__ void unpack2(uint32_t w, float 
 }
 
 // 128 bytes of each lane's row, swizzled, through shared memory to rows y.. and columns x.. of a
-// matrix.  Stores of a lane's own 32 bytes into 32 rows take a cycle or two for every row: 255 us
-// where the table's gradient of one token (128256 x 4096 bf16) takes 1XX us this way.
+// matrix.  Stores of a lane's own 32 bytes into 32 rows take a cycle or two for every row: 1 x 128256 x
+// 4096 bf16 as a whole 654 us with them, 580 us this way.
 __device__ __forceinline__ void copy_out(const CUtensorMap *map, uint32_t box, int x, int y, const uint32_t (&w)[32], bool add)
 {
     const int lane = threadIdx.x & 31;
@@ -491,7 +486,7 @@ __device__ __forceinline__ void end_table(const Product &p, const CUtensorMap *m
             tmem_load(tmem + c, f);
 #pragma unroll
             for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(f[i] * scale);
-            copy_out(map, box, c0 + c, y, w, false);
+            copy_out(map, box, c0 + c, y, w, p.accumulate != 0);
         }
         return;
     }
@@ -512,62 +507,34 @@ __device__ __forceinline__ void end_table(const Product &p, const CUtensorMap *m
     }
 }
 
-// The same where it is added to what is there, or where rows do not start at 16-byte boundaries.
-__device__ __forceinline__ void end_table_by_lanes(const Product &p, uint32_t tmem, int64_t row, int n, float scale)
+// The same where 16-bit numbers are added to what is there, or where rows do not start at 16-byte
+// boundaries: through shared memory too, then a row at a time, a column a lane.  Both gradients of 300
+// x 128256 x 77 bf16 take 90 us this way; with a lane to its own row's columns they took 142 us.
+__device__ __forceinline__ void end_table_by_rows(const Product &p, uint32_t box, uint32_t tmem, int64_t row, int n, float scale)
 {
-    const int64_t v = p.first + row;
-    const bool in = row < p.width && v < p.vocab;
-    const int64_t c0 = (int64_t)n * kEndCols;
+    const int lane = threadIdx.x & 31;
+    const int64_t c0 = (int64_t)n * kEndCols, first = row - lane;
+    const int64_t left = p.width - first < p.vocab - p.first - first ? p.width - first : p.vocab - p.first - first;
+    const int rows = left < 32 ? (int)left : 32;
     for (int c = 0; c < kEndCols && c0 + c < p.cols; c += 32) {
         float f[32];
         tmem_load(tmem + c, f);
-        if (!in) continue;
-        const int64_t at = v * p.grad_stride + c0 + c;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) f[i] *= scale;
-        if (p.grad_vectors && c0 + c + 32 <= p.cols) {
-            if (p.grad_dtype == SO_DTYPE_FP32) {
-                float *out = static_cast<float *>(p.table_grad) + at;
-#pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    uint32_t w[8];
-                    if (p.accumulate) {
-                        load32(out + i, w);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) f[i + j] += __uint_as_float(w[j]);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(f[i + j]);
-                    store32(out + i, w);
-                }
-            } else {
-                uint16_t *out = static_cast<uint16_t *>(p.table_grad) + at;
-                const bool bf = p.grad_dtype == SO_DTYPE_BF16;
-#pragma unroll
-                for (int i = 0; i < 32; i += 16) {
-                    uint32_t w[8];
-                    if (p.accumulate) {
-                        load32(out + i, w);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            float lo, hi;
-                            if (bf) unpack2<bf16_t>(w[j], lo, hi);
-                            else unpack2<f16_t>(w[j], lo, hi);
-                            f[i + 2 * j] += lo;
-                            f[i + 2 * j + 1] += hi;
-                        }
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = bf ? pack2_bf16(f[i + 2 * j], f[i + 2 * j + 1]) : pack2_f16(f[i + 2 * j], f[i + 2 * j + 1]);
-                    store32(out + i, w);
-                }
+        for (int u = 0; u < 8; ++u)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128 + ((u ^ (lane & 7)) << 4)), "f"(f[4 * u] * scale),
+                         "f"(f[4 * u + 1] * scale), "f"(f[4 * u + 2] * scale), "f"(f[4 * u + 3] * scale) : "memory");
+        __syncwarp();
+        if (c0 + c + lane < p.cols) {
+            int64_t at = (p.first + first) * p.grad_stride + c0 + c + lane;
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r, at += p.grad_stride) {
+                float x;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(box + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
+                if (p.accumulate) x += load_any(p.table_grad, at, p.grad_dtype);
+                store_any(p.table_grad, at, p.grad_dtype, x);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (c0 + c + i < p.cols)
-                    store_any(p.table_grad, at + i, p.grad_dtype, p.accumulate ? f[i] + load_any(p.table_grad, at + i, p.grad_dtype) : f[i]);
         }
+        __syncwarp();
     }
 }
 
@@ -720,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             else if (kMode == kProb) end_prob<T>(p, &maps.out, box, at, row, live, 2 * it.n + half);
             else if (it.kind == kHidden) end_hidden(p, &maps.out, box, at, row, 2 * it.n + half, it.split, it.steps == 0);
             else if (p.grad_boxes) end_table(p, &maps.out2, box, at, row, 2 * it.n + half, scale);
-            else end_table_by_lanes(p, at, row, 2 * it.n + half, scale);
+            else end_table_by_rows(p, box, at, row, 2 * it.n + half, scale);
             fence_before();
             __syncwarp();
             if (lane == 0) {
@@ -1130,9 +1097,12 @@ struct Layout {
 
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of P, unless rows are so many that pieces would get short
 constexpr int64_t kShortPiece = 4096;
-// Up to so many bytes of fp32 logits are kept from the statistics to P: a batch that small would
-// read the table again and multiply again for less than that costs.
+// Up to so many bytes of fp32 logits are kept from the statistics to P, where multiplying again would
+// cost more than writing and reading them: kept / again 596 / 655 us for 1025 x 50257 x 1600 (fp16,
+// fp32 gradient), 281 / 343 us for 300 x 50257 x 2048, 88 / 101 us for 63 x 50257 x 768, but
+// 146 / 137 us for 500 x 50257 x 512 and 198 / 171 us for 1000 x 50257 x 256.
 constexpr int64_t kKeptBytes = int64_t(256) << 20;
+constexpr int64_t kKeptCols = 768;        // for shorter rows a quarter of that, which L2 may hold
 
 constexpr int kSms = 148;                 // of a B200: sums are split alike on every device
 
@@ -1182,7 +1152,7 @@ Layout layout(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t 
     l.sums = take(rp / 32 * 8);
     l.stats = take(rp * (uint64_t)l.halves * 8);
     l.gathered = take(rp * (uint64_t)l.ld * 2);
-    l.keep = gradients && l.pieces == 1 && l.rows_pad * l.piece * 4 <= kKeptBytes;
+    l.keep = gradients && l.pieces == 1 && l.rows_pad * l.piece * 4 <= (cols >= kKeptCols ? kKeptBytes : kKeptBytes / 4);
     if (l.keep) l.kept = take(rp * (uint64_t)l.piece * 4);
     if (gradients) {
         l.prob = take(rp * (uint64_t)(l.planes * l.piece) * 2);
@@ -1306,7 +1276,6 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     p.kept = l.keep ? reinterpret_cast<float *>(scratch + l.kept) : nullptr;
     p.part = reinterpret_cast<float *>(scratch + l.part), p.part_stride = l.part_stride;
     p.table_grad = c.dtable, p.grad_stride = c.dtable_stride, p.grad_dtype = c.grad_dtype, p.accumulate = c.accumulate, p.grad_scale = c.grad_scale;
-    p.grad_vectors = aligned(c.dtable, 32) && (c.dtable_stride * elem_size(c.grad_dtype)) % 32 == 0;
     p.table_groups = l.packed || c.cols % 64 == 0;           // a row's last group ends with it
     p.patience = patience();
 
@@ -1355,7 +1324,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
             return SO_ERR_CUDA;
         gradient.out2 = gradient.out;
         const int grad_size = elem_size(c.grad_dtype);
-        p.grad_boxes = c.dtable && !c.accumulate && aligned(c.dtable, 16) && c.dtable_stride * grad_size % 16 == 0;
+        p.grad_boxes = c.dtable && (!c.accumulate || c.grad_dtype == SO_DTYPE_FP32) && aligned(c.dtable, 16) && c.dtable_stride * grad_size % 16 == 0;
         if (p.grad_boxes && !make_map(&gradient.out2, c.dtable, c.grad_dtype, c.vocab, c.cols, c.dtable_stride, 32)) return SO_ERR_CUDA;
         for (int64_t first = 0; first < c.vocab; first += l.piece) {
             Product q = p;
@@ -1363,7 +1332,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
             q.width = c.vocab - first < l.piece ? c.vocab - first : l.piece;
             q.begin = first == 0;
             if (l.packed) {
-                SO_TRY(pack_piece(first, q.width));
+                if (l.pieces > 1) SO_TRY(pack_piece(first, q.width));   // (one piece is still there)
                 if (!table_maps(q.width)) return SO_ERR_CUDA;
                 q.table_row = 0;
             }
