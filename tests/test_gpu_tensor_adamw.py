@@ -362,3 +362,15 @@ def test_refusals():
         with pytest.raises(B.SuperOffloadError) as err:
             call()
         assert err.value.status == B.SO_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_no_elements(bits):
+    """Tensors without elements are passed over; a list of nothing else still counts its steps."""
+    none = torch.zeros(0, device="cuda")
+    opt = TensorAdamW([none, none], [none, none], state_bits=bits)
+    assert opt.blocks == 0
+    for clip in (True, False):
+        stats = opt.step(HP(max_grad_norm=1.0), clip=clip)
+        assert stats.tolist() == [0.0, 1.0, 0.0]
+    assert opt.step_count == 2
