@@ -766,7 +766,7 @@ so_status so_residual_norm_backward(const void *dy, int64_t dy_stride, const voi
  *   int64 t; float norm, c, skipped (0 or 1)
  * `scratch` (so_tensor_adamw_layout's bytes, 16-byte aligned) is needed with `clip` and free
  * for other use once the call has run on its stream.  Calls on one record are made one after
- * the other.  Tensors of no elements are passed over; the sums' order depends on the sizes
+ * the other.  What is written is apart from everything else.  Tensors of no elements are passed over; the sums' order depends on the sizes
  * alone, and results repeat bit for bit.
  * Errors: SO_ERR_INVALID_ARG, SO_ERR_CUDA.
  */

@@ -24,7 +24,8 @@ class TensorAdamW:
 
     `params` are contiguous fp32 tensors, `grads` contiguous and of one dtype (bf16,
     fp16 or fp32), `copies` (None: none) bf16 or fp16; each list has the same sizes, on
-    the current device.  The optimizer keeps them; gradients are read where they are
+    the current device.  Parameters and copies are apart from each other and from the
+    gradients.  The optimizer keeps them; gradients are read where they are
     when :meth:`step` runs.  Parameters may require grad: a step counts as a
     modification in place.
 
@@ -69,6 +70,14 @@ class TensorAdamW:
             for e, c in zip(self._list, self.copies):
                 self._check(where, "copy", c, e.numel)
                 e.copy = c.data_ptr()
+        # what is written is written by one warp alone
+        end = 0
+        for at, size in sorted((t.data_ptr(), t.numel() * t.element_size()) for t in [*self.params, *(self.copies or ())]):
+            if size == 0:
+                continue
+            if at < end:
+                _refuse(where, "parameters and copies overlap")
+            end = at + size
         self.set_grads(grads)
         info = B.so_tensor_adamw_layout(self._list, n, state_bits)
         self.blocks = info.blocks

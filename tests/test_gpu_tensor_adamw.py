@@ -374,3 +374,18 @@ def test_no_elements(bits):
         stats = opt.step(HP(max_grad_norm=1.0), clip=clip)
         assert stats.tolist() == [0.0, 1.0, 0.0]
     assert opt.step_count == 2
+
+
+def test_what_is_written_must_not_overlap():
+    arena = torch.zeros(1000, device="cuda")
+    a, b, c = arena[:300], arena[299:600], arena[600:1000]
+    grads = [torch.zeros_like(t) for t in (a, b)]
+    with pytest.raises(B.SuperOffloadError, match="overlap"):
+        TensorAdamW([a, b], grads)
+    with pytest.raises(B.SuperOffloadError, match="overlap"):      # one copy for two parameters
+        copy = torch.zeros(300, device="cuda", dtype=BF16)
+        TensorAdamW([arena[:300], arena[300:600]], [grads[0]] * 2, copies=[copy, copy])
+    with pytest.raises(B.SuperOffloadError, match="overlap"):      # a copy inside a parameter
+        TensorAdamW([c], [torch.zeros_like(c)], copies=[c.view(BF16)[:400]])
+    # neighbours are apart, an empty tensor anywhere is, and a gradient may serve two parameters
+    TensorAdamW([arena[300:600], arena[:300], arena[100:100]], [grads[0], grads[0], arena[:0]])
