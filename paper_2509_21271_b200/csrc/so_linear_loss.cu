@@ -516,6 +516,8 @@ __device__ __forceinline__ void end_table_by_rows(const Product &p, uint32_t box
     const int64_t c0 = (int64_t)n * kEndCols, first = row - lane;
     const int64_t left = p.width - first < p.vocab - p.first - first ? p.width - first : p.vocab - p.first - first;
     const int rows = left < 32 ? (int)left : 32;
+    if (lane == 0) tma_stores_read();     // the box may still be on its way out with a tile of dH
+    __syncwarp();
     for (int c = 0; c < kEndCols && c0 + c < p.cols; c += 32) {
         float f[32];
         tmem_load(tmem + c, f);
