@@ -13,6 +13,12 @@
 // through TMA into swizzled shared memory, two accumulators of 256 columns in tensor
 // memory, so that one is read while the next is computed) with four ways to end a tile.
 //
+// With top = max z and others = sum of exp(z_j - top) but for the label's,
+//   q_j = exp(z_j - top) / total,  total = others + exp(z_label - top),  q_label - 1 = -others / total,
+// and the loss is log(1 + others / exp(z_label - top)): where a label has nearly all the probability,
+// both are as good relative to 1 - q as other rows' are to 1.  (One number for log sum exp z would do
+// for q, but its rounding, 1e-6 for logits near 20, is all of q - 1 there.)
+//
 // P is w (q - [label]) as a multiple of a power of two near the largest |w| (for fp16 of
 // 2^-15 of it: its normal numbers then reach down to 2^-29 of a row's largest).  Its
 // rounding to 16 bits is one rounding of every term of sums that are themselves
@@ -199,10 +205,9 @@ struct Product {
     int32_t begin;                        // kHidden: the sums begin here rather than going on
     const int32_t *label;                 // [rows_pad], of the gathered rows
     float *label_logit;                   // [rows_pad]
-    const float *lse2;                    // [rows_pad], in units of log 2
-    const float *coef;                    // [rows_pad], w over the unit
+    const float4 *terms;                  // [rows_pad]: largest logit, log2 of the sum relative to it, w over the unit, q - 1 of the label
     float *residual;                      // [rows_pad]: what P at the label lost when it was rounded
-    float2 *stats;                        // [half tiles of the vocabulary][rows_pad]: maximum, sum
+    float2 *stats;                        // [half tiles of the vocabulary][rows_pad]: maximum, sum without the label's
     float *kept;                          // kStats: [rows_pad][prob_stride], where all logits are kept
     void *prob;                           // [planes][rows_pad][prob_stride]
     int64_t prob_stride;
@@ -371,7 +376,7 @@ __device__ __forceinline__ void copy_out(const CUtensorMap *map, uint32_t box, i
 }
 
 // Half a tile, n-th of the columns.  A row's maximum and sum over it, its label's logit if that is
-// here, and the logits themselves where they are kept.
+// here (which the sum leaves out), and the logits themselves where they are kept.
 __device__ __forceinline__ void end_stats(const Product &p, const CUtensorMap *map, uint32_t box, uint32_t tmem, int64_t row, int live, int n)
 {
     const int64_t n0 = p.first + (int64_t)n * kEndCols;
@@ -397,7 +402,7 @@ __device__ __forceinline__ void end_stats(const Product &p, const CUtensorMap *m
                 if (label == c + i) p.label_logit[row] = f[i];
         }
     }
-    const float ref = top == -kInf ? 0.0f : top * kLog2e;   // a tile of nothing else adds nothing
+    const float ref = top == -kInf ? 0.0f : top;            // a tile of nothing else adds nothing
     float sum0 = 0.0f, sum1 = 0.0f;
     for (int c = 0; c < cols; c += 32) {
         float f[32];
@@ -408,10 +413,16 @@ __device__ __forceinline__ void end_stats(const Product &p, const CUtensorMap *m
             for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(f[i]);
             copy_out(map, box, (int)n0 + c, (int)row - (int)(threadIdx.x & 31), w, false);
         }
+        if (__any_sync(0xFFFFFFFFu, label >= c && label < c + 32)) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (label == c + i) f[i] = -kInf;
+        }
+        // (the difference first: large logits keep their digits)
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            sum0 += c + i < cols ? exp2_fast(fmaf(f[i], kLog2e, -ref)) : 0.0f;
-            sum1 += c + i + 1 < cols ? exp2_fast(fmaf(f[i + 1], kLog2e, -ref)) : 0.0f;
+            sum0 += c + i < cols ? exp2_fast((f[i] - ref) * kLog2e) : 0.0f;
+            sum1 += c + i + 1 < cols ? exp2_fast((f[i + 1] - ref) * kLog2e) : 0.0f;
         }
     }
     if (in) p.stats[(n0 / kEndCols) * p.rows_pad + row] = make_float2(top, sum0 + sum1);
@@ -425,7 +436,7 @@ __device__ __forceinline__ void end_prob(const Product &p, const CUtensorMap *ma
     const int cols = p.vocab - n0 < kEndCols ? (int)(p.vocab - n0) : kEndCols;
     const bool in = row < live;
     const int64_t label = in ? (int64_t)p.label[row] - n0 : -1;
-    const float lse2 = in ? p.lse2[row] : 0.0f, coef = in ? p.coef[row] : 0.0f;
+    const float4 t = in ? p.terms[row] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     const int y = (int)row - (int)(threadIdx.x & 31);
     for (int c = 0; c < kEndCols; c += 64) {
         float f[2][32];
@@ -437,9 +448,9 @@ __device__ __forceinline__ void end_prob(const Product &p, const CUtensorMap *ma
             const bool here = __any_sync(0xFFFFFFFFu, label >= c0 && label < c0 + 32);
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-                float q = exp2_fast(fmaf(f[h][i], kLog2e, -lse2));
-                if (here && label == c0 + i) q -= 1.0f;
-                f[h][i] = in && c0 + i < cols ? q * coef : 0.0f;
+                float q = exp2_fast(fmaf(f[h][i] - t.x, kLog2e, -t.y));
+                if (here && label == c0 + i) q = t.w;
+                f[h][i] = in && c0 + i < cols ? q * t.z : 0.0f;
                 if (here && label == c0 + i) p.residual[row] = f[h][i] - to_f32(from_f32<T>(f[h][i]));
             }
         }
@@ -883,14 +894,14 @@ __global__ void __launch_bounds__(256) prob_kernel(const __grid_constant__ Produ
         float f[8] = {};
         if (row < live) {
             const int64_t label = p.label[row] - c;
-            const float lse2 = p.lse2[row], coef = p.coef[row];
+            const float4 t = p.terms[row];
             uint32_t w[8];
             load32(p.kept + row * p.prob_stride + c, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float q = exp2_fast(fmaf(__uint_as_float(w[j]), kLog2e, -lse2));
-                if (label == j) q -= 1.0f;
-                f[j] = c + j < p.vocab ? q * coef : 0.0f;
+                float q = exp2_fast(fmaf(__uint_as_float(w[j]) - t.x, kLog2e, -t.y));
+                if (label == j) q = t.w;
+                f[j] = c + j < p.vocab ? q * t.z : 0.0f;
                 if (label == j) p.residual[row] = f[j] - to_f32(from_f32<T>(f[j]));
             }
         }
@@ -913,7 +924,8 @@ struct Join {
     const float2 *stats;
     const float *label_logit, *w;
     const int32_t *index;
-    float *lse2, *coef, *row_loss, *loss;
+    float4 *terms;
+    float *row_loss, *loss;
     double *sums;                         // [blocks]
     int32_t rows_pad, halves;
     int64_t rows;
@@ -965,13 +977,13 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_cons
         if (row < live) {
             float most = -kInf;
             for (int i = 0; i < kJoinWarps; ++i) most = fmaxf(most, s_part[i][lane].x);
-            float total = 0.0f;
+            float others = 0.0f;
             for (int i = 0; i < kJoinWarps; ++i)
-                total += s_part[i][lane].y == 0.0f ? 0.0f : s_part[i][lane].y * exp2_fast((s_part[i][lane].x - most) * kLog2e);
-            const float w = j.w[row], loss = (most - j.label_logit[row]) + logf(total);
+                others += s_part[i][lane].y == 0.0f ? 0.0f : s_part[i][lane].y * exp2_fast((s_part[i][lane].x - most) * kLog2e);
+            const float w = j.w[row], below = most - j.label_logit[row], own = exp2_fast(-below * kLog2e), total = others + own;
+            const float loss = own > 0.5f ? log1pf(others / own) : below + logf(total);
             j.row_loss[j.index[row]] = loss;
-            j.lse2[row] = fmaf(most, kLog2e, log2f(total));
-            j.coef[row] = w / j.control->unit;
+            j.terms[row] = make_float4(most, log2f(total), w / j.control->unit, -(others / total));
             mine = (double)w * (double)loss;
         }
 #pragma unroll
@@ -1107,7 +1119,7 @@ int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 struct Layout {
     int64_t rows_pad, ld, pieces, piece, splits, planes, part_stride, halves;
     bool packed, keep;
-    uint64_t control, counts, index, label, w, label_logit, lse2, coef, residual, sums, stats, gathered, kept, prob, part, table, bytes;
+    uint64_t control, counts, index, label, w, label_logit, terms, residual, sums, stats, gathered, kept, prob, part, table, bytes;
 };
 
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of P, unless rows are so many that pieces would get short
@@ -1161,8 +1173,7 @@ Layout layout(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t 
     l.label = take(rp * 4);
     l.w = take(rp * 4);
     l.label_logit = take(rp * 4);
-    l.lse2 = take(rp * 4);
-    l.coef = take(rp * 4);
+    l.terms = take(rp * sizeof(float4));
     l.residual = take(rp * 4);
     l.sums = take(rp / 32 * 8);
     l.stats = take(rp * (uint64_t)l.halves * 8);
@@ -1283,8 +1294,8 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
     p.control = control, p.vocab = c.vocab, p.cols = c.cols, p.rows_pad = (int32_t)l.rows_pad, p.splits = (int32_t)l.splits, p.planes = (int32_t)l.planes;
     p.label = label;
     p.label_logit = reinterpret_cast<float *>(scratch + l.label_logit);
-    float *lse2 = reinterpret_cast<float *>(scratch + l.lse2), *coef = reinterpret_cast<float *>(scratch + l.coef);
-    p.lse2 = lse2, p.coef = coef;
+    float4 *terms = reinterpret_cast<float4 *>(scratch + l.terms);
+    p.terms = terms;
     p.residual = reinterpret_cast<float *>(scratch + l.residual);
     p.stats = reinterpret_cast<float2 *>(scratch + l.stats);
     p.prob = scratch + l.prob, p.prob_stride = l.piece;
@@ -1328,7 +1339,7 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
         p.width = c.vocab;
         SO_TRY((launch_product<T, kStats, kCtas>(logits, p, units, st)));
     }
-    Join j = {control, p.stats, p.label_logit, w, index, lse2, coef, c.row_loss, c.loss, reinterpret_cast<double *>(scratch + l.sums), (int32_t)l.rows_pad, (int32_t)l.halves, c.rows};
+    Join j = {control, p.stats, p.label_logit, w, index, terms, c.row_loss, c.loss, reinterpret_cast<double *>(scratch + l.sums), (int32_t)l.rows_pad, (int32_t)l.halves, c.rows};
     SO_TRY(launch(join_kernel, (unsigned)(l.rows_pad / 32), 32 * kJoinWarps, 0, st, true, j));
     if (gradients) {
         // (what a warp copies out is 32 rows)
