@@ -307,8 +307,25 @@ struct Shape {
 struct Shared {
     uint64_t full[8], empty[8], done[2], free[2], last;
     uint32_t tmem;
+    int issued[2];                        // stages that this block has filled; of the second block of a pair
     volatile uint32_t gave_up;
 };
+
+// Waits, after a wait that ran out, for the copies that are still on their way into the first block's
+// stages, and the second's, which are counted by the first's barriers too.  Where one of them had
+// gone on further than the other, the barrier is given what the other left out.
+template <int kCtas>
+__device__ __noinline__ void land_stages(Shared &s)
+{
+    using S = Shape<kCtas>;
+    const int mine = s.issued[0], other = kCtas == 2 ? s.issued[1] : mine, most = mine > other ? mine : other;
+    for (int k = most > S::kStages ? most - S::kStages : 0; k < most; ++k) {
+        const uint32_t bar = smem_addr(s.full + k % S::kStages);
+        if (k >= mine) mbar_expect(bar, S::kStage);
+        else if (k >= other) asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(S::kStage) : "memory");
+        mbar_wait(bar, (uint32_t)(k / S::kStages) & 1u, kPolls);
+    }
+}
 
 // A wait that ends when the barrier's phase does, when it runs out, or when another of the block
 // has run out; false unless the first.
@@ -653,10 +670,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 if (++step == k_steps && it.kind == kTable) step = 0, row0 += p.rows_pad;
             }
         }
-        // a block that gives up waits for what is still on its way
-        if (!ok && rank == 0)
-            for (int k = issued > S::kStages ? issued - S::kStages : 0; k < issued; ++k)
-                mbar_wait(full + 8 * (k % S::kStages), (uint32_t)(k / S::kStages) & 1u, kPolls);
+        if (lane == 0) {
+            if (rank == 0) s.issued[0] = issued;
+            else asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(of_rank(smem_addr(s.issued + 1), 0)), "r"(issued) : "memory");
+        }
     } else if (warp == 1 && rank == 0) {
         int stage = 0, buffer = 0;
         uint32_t phase = 0, free_phase = 1;
@@ -727,7 +744,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     }
     __syncthreads();
     if (kCtas == 2) cluster_sync();
+    if (rank == 0 && threadIdx.x == 0 && s.gave_up) land_stages<kCtas>(s);
     __syncwarp();
+    if (kCtas == 2) cluster_sync();       // the second block stays as long as its copies do
     if (warp == 1) tmem_free<kCtas>(tmem, 512);
 }
 
