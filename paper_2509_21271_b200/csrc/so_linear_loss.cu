@@ -1430,7 +1430,7 @@ so_status so_linear_cross_entropy(const void *hidden, int64_t hidden_stride, con
         if (!hidden || !aligned(hidden, 2) || !valid_extent(rows, hidden_stride) || !valid_in_stride(rows, hidden_stride, cols)) return SO_ERR_INVALID_ARG;
         if (!labels || !aligned(labels, ids_dtype == SO_IDS_INT64 ? 8 : 4)) return SO_ERR_INVALID_ARG;
         if (dhidden && (!aligned(dhidden, 2) || !valid_extent(rows, dhidden_stride) || !valid_out_stride(rows, dhidden_stride, cols))) return SO_ERR_INVALID_ARG;
-        if (dhidden && dhidden == hidden && dhidden_stride != hidden_stride) return SO_ERR_INVALID_ARG;
+        if (dhidden && dhidden == hidden && rows > 1 && dhidden_stride != hidden_stride) return SO_ERR_INVALID_ARG;
     }
     if (dtable && (dtable == table || dtable == hidden || dtable == dhidden)) return SO_ERR_INVALID_ARG;
     if (dhidden && dhidden == table) return SO_ERR_INVALID_ARG;

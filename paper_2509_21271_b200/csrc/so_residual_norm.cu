@@ -1232,8 +1232,8 @@ so_status so_residual_norm_forward(const void *x, int64_t x_stride, const void *
     if (!row_ok(x, x_stride, rows, cols, size, false) || !row_ok(block, block_stride, rows, cols, size, false) ||
         !row_ok(h, h_stride, rows, cols, size, true) || !row_ok(y, y_stride, rows, cols, size, true))
         return SO_ERR_INVALID_ARG;
-    // h may take x's or the block's place, row for row; y is apart
-    if (h == y || y == x || y == block || (h == x && h_stride != x_stride) || (h == block && h_stride != block_stride)) return SO_ERR_INVALID_ARG;
+    // h may take x's or the block's place, row for row (one row has no stride); y is apart
+    if (h == y || y == x || y == block || (rows > 1 && ((h == x && h_stride != x_stride) || (h == block && h_stride != block_stride)))) return SO_ERR_INVALID_ARG;
     Args a = {};
     a.x = x, a.block = block, a.h = h, a.y = y, a.gate = gate, a.pw = post_weight, a.pb = post_bias, a.w = weight, a.b = bias;
     a.stats = stats;
