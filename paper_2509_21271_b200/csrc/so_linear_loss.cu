@@ -1369,8 +1369,9 @@ so_status run(const Call &c, const Layout &l, char *scratch, int sms, cudaStream
             return SO_ERR_CUDA;
         gradient.out2 = gradient.out;
         const int grad_size = elem_size(c.grad_dtype);
-        p.grad_boxes = c.dtable && (!c.accumulate || c.grad_dtype == SO_DTYPE_FP32) && aligned(c.dtable, 16) && c.dtable_stride * grad_size % 16 == 0;
-        if (p.grad_boxes && !make_map(&gradient.out2, c.dtable, c.grad_dtype, c.vocab, c.cols, c.dtable_stride, 32)) return SO_ERR_CUDA;
+        const int64_t grad_stride = c.vocab == 1 ? l.ld : c.dtable_stride;   // (of one row: any)
+        p.grad_boxes = c.dtable && (!c.accumulate || c.grad_dtype == SO_DTYPE_FP32) && aligned(c.dtable, 16) && grad_stride * grad_size % 16 == 0;
+        if (p.grad_boxes && !make_map(&gradient.out2, c.dtable, c.grad_dtype, c.vocab, c.cols, grad_stride, 32)) return SO_ERR_CUDA;
         for (int64_t first = 0; first < c.vocab; first += l.piece) {
             Product q = p;
             q.first = q.table_row = first;

@@ -1,4 +1,5 @@
-"""Matrices of one row, whose row stride says nothing: a row of a wider buffer in place."""
+"""Matrices of one row, whose row stride says nothing: a row of a wider buffer in place, and
+strides that no matrix of more rows could have."""
 from __future__ import annotations
 
 import pytest
@@ -6,8 +7,8 @@ import torch
 
 from paper_2509_21271_b200 import build as so_build
 from paper_2509_21271_b200 import operators as ops
-from test_gpu_linear_loss import inputs
-from test_gpu_operators import BF16, gen, randn, same_bits
+from test_gpu_linear_loss import check, inputs
+from test_gpu_operators import BF16, FP32, gen, randn, same_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -35,6 +36,17 @@ def test_residual_norm_in_place(where):
     place = last_token(x if where == "x" else block)
     got = ops.residual_norm_forward(place if where == "x" else x, place if where == "block" else block, kind="rms", h=place)
     assert got[0] is place and all(same_bits(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("stride", [0, 8, 13, 1 << 45])
+@pytest.mark.parametrize("out", [BF16, FP32])
+def test_linear_cross_entropy_with_a_vocabulary_of_one(stride, out):
+    _, hidden, table, _ = inputs(2, 200, 1, 72, BF16)
+    labels = torch.zeros(200, dtype=torch.int64, device="cuda")
+    place = torch.ones(72, dtype=out, device="cuda")
+    for accumulate in (False, True):
+        check(hidden, table.as_strided((1, 72), (stride, 1)), labels, dtable=place.as_strided((1, 72), (stride, 1)),
+              accumulate=accumulate)
 
 
 def test_linear_cross_entropy_of_one_row_in_place():
