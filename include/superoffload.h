@@ -666,6 +666,8 @@ so_status so_policy_loss(const void *logits, int64_t logits_stride, const void *
  *   dtable  [vocab, cols] of `grad_dtype`, NULL: not wanted; with `accumulate` added to
  *           what is there (one rounding)
  *   row_loss fp32 [rows], loss fp32 [1]
+ *   the gradients are apart from each other and from hidden and table otherwise (between
+ *            their rows will do)
  *   scratch  so_linear_cross_entropy_scratch bytes, 256-byte aligned, contents irrelevant;
  *           free for other use once the call has run on its stream.  `packed`: 1 unless
  *           table is 16-byte aligned and its stride a multiple of 8; such a table is copied,
@@ -696,7 +698,8 @@ so_status so_linear_cross_entropy(const void *hidden, int64_t hidden_stride, con
  *   u = N(block) * post_weight + post_bias   (post = 1; otherwise u = block)
  *   h = scale * x + gate * u                 rounded to `dtype`
  *   y = N(h) * weight + bias                 of h as rounded
- *   x, block, h, y  [rows, cols] of `dtype`; h may be x or block (same stride)
+ *   x, block, h, y  [rows, cols] of `dtype`; h may be x or block (same stride); otherwise
+ *           h and y are apart from each other and from those (between their rows will do)
  *   gate    [groups, cols] or NULL (1): group i gates the i-th of `groups` equal runs
  *           of rows (a sequence each; 1 for a gate per channel).  groups <= 65535
  *   post_weight, post_bias, weight, bias  [cols], each may be NULL; these and gate are of

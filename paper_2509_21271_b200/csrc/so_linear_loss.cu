@@ -1431,10 +1431,14 @@ so_status so_linear_cross_entropy(const void *hidden, int64_t hidden_stride, con
         if (!hidden || !aligned(hidden, 2) || !valid_extent(rows, hidden_stride) || !valid_in_stride(rows, hidden_stride, cols)) return SO_ERR_INVALID_ARG;
         if (!labels || !aligned(labels, ids_dtype == SO_IDS_INT64 ? 8 : 4)) return SO_ERR_INVALID_ARG;
         if (dhidden && (!aligned(dhidden, 2) || !valid_extent(rows, dhidden_stride) || !valid_out_stride(rows, dhidden_stride, cols))) return SO_ERR_INVALID_ARG;
-        if (dhidden && dhidden == hidden && rows > 1 && dhidden_stride != hidden_stride) return SO_ERR_INVALID_ARG;
     }
-    if (dtable && (dtable == table || dtable == hidden || dtable == dhidden)) return SO_ERR_INVALID_ARG;
-    if (dhidden && dhidden == table) return SO_ERR_INVALID_ARG;
+    // dhidden may take hidden's place, row for row; otherwise the gradients are apart
+    const int size = elem_size(dtype);
+    const Span at_hidden(hidden, rows, hidden_stride, cols, size), at_table(table, vocab, table_stride, cols, size),
+        at_dhidden(dhidden, dhidden ? rows : 0, dhidden_stride, cols, size), at_dtable(dtable, dtable ? vocab : 0, dtable_stride, cols, elem_size(grad_dtype));
+    if ((!at_dhidden.same(at_hidden) && overlap(at_dhidden, at_hidden)) || overlap(at_dhidden, at_table) || overlap(at_dtable, at_hidden) ||
+        overlap(at_dtable, at_table) || overlap(at_dtable, at_dhidden))
+        return SO_ERR_INVALID_ARG;
     if (!scratch || !aligned(scratch, 256)) return SO_ERR_INVALID_ARG;
     const Layout l = layout(rows, vocab, cols, dtype, grad_dtype, dhidden || dtable, needs_packing(table, table_stride, vocab));
     if (scratch_bytes < l.bytes) return SO_ERR_INVALID_ARG;

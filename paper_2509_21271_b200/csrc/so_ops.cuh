@@ -398,6 +398,44 @@ inline bool valid_in_stride(int64_t rows, int64_t stride, int64_t cols)
     return rows <= 1 || stride == 0 || stride >= cols;
 }
 
+// Where the rows of a matrix lie: `width` bytes each, `stride` bytes apart.
+struct Span {
+    intptr_t at;
+    int64_t rows, stride, width;
+    Span(const void *p, int64_t rows_, int64_t stride_, int64_t cols, int size)
+        : at(reinterpret_cast<intptr_t>(p)), rows(rows_), stride(stride_ * size), width(cols * size)
+    {
+        if (rows > 1 && stride == 0) rows = 1;               // one row, over and over
+        if (rows == 1) stride = width;
+    }
+    intptr_t end() const { return at + (rows - 1) * stride + width; }
+    bool same(const Span &b) const { return at == b.at && rows == b.rows && stride == b.stride && width == b.width; }
+};
+
+// Whether two matrices share a byte.  Rows that lie between the other's rows do not.  In one step
+// for equal strides, else a step for each row of the one with fewer.
+inline bool overlap(const Span &a, const Span &b)
+{
+    if (a.rows <= 0 || b.rows <= 0 || a.end() <= b.at || b.end() <= a.at) return false;
+    if (a.rows > b.rows) return overlap(b, a);
+    const auto floor_div = [](int64_t x, int64_t y) { return x / y - (x % y != 0 && x < 0); };
+    if (a.stride == b.stride) {
+        // row i + k of b and row i of a are `apart + k stride` bytes apart: the first k where that is above -b.width
+        const int64_t apart = b.at - a.at;
+        int64_t k = floor_div(-b.width - apart, a.stride) + 1;
+        if (k < 1 - a.rows) k = 1 - a.rows;
+        return k < b.rows && apart + k * a.stride < a.width;
+    }
+    for (int64_t i = 0; i < a.rows; ++i) {
+        // the last row of b that begins before this one's end
+        const int64_t row = a.at + i * a.stride;
+        int64_t k = floor_div(row + a.width - 1 - b.at, b.stride);
+        if (k >= b.rows) k = b.rows - 1;
+        if (k >= 0 && b.at + k * b.stride + b.width > row) return true;
+    }
+    return false;
+}
+
 // Number of SMs of the current device, asked for once per device.
 inline so_status device_sms(int *sms)
 {

@@ -1232,8 +1232,12 @@ so_status so_residual_norm_forward(const void *x, int64_t x_stride, const void *
     if (!row_ok(x, x_stride, rows, cols, size, false) || !row_ok(block, block_stride, rows, cols, size, false) ||
         !row_ok(h, h_stride, rows, cols, size, true) || !row_ok(y, y_stride, rows, cols, size, true))
         return SO_ERR_INVALID_ARG;
-    // h may take x's or the block's place, row for row (one row has no stride); y is apart
-    if (h == y || y == x || y == block || (rows > 1 && ((h == x && h_stride != x_stride) || (h == block && h_stride != block_stride)))) return SO_ERR_INVALID_ARG;
+    // h may take x's or the block's place, row for row; y is apart
+    const Span at_x(x, rows, x_stride, cols, size), at_block(block, rows, block_stride, cols, size), at_h(h, rows, h_stride, cols, size),
+        at_y(y, rows, y_stride, cols, size);
+    if ((!at_h.same(at_x) && overlap(at_h, at_x)) || (!at_h.same(at_block) && overlap(at_h, at_block)) || overlap(at_y, at_x) ||
+        overlap(at_y, at_block) || overlap(at_y, at_h))
+        return SO_ERR_INVALID_ARG;
     Args a = {};
     a.x = x, a.block = block, a.h = h, a.y = y, a.gate = gate, a.pw = post_weight, a.pb = post_bias, a.w = weight, a.b = bias;
     a.stats = stats;
@@ -1288,9 +1292,11 @@ so_status so_residual_norm_backward(const void *dy, int64_t dy_stride, const voi
             !row_ok(dx, dx_stride, rows, cols, size, true) || !row_ok(dblock, dblock_stride, rows, cols, size, true) ||
             !stats || !aligned(stats, 4))
             return SO_ERR_INVALID_ARG;
-        if (dx == dblock) return SO_ERR_INVALID_ARG;
-        for (const void *p : {dy, dh, h, block})
-            if (p == dx || p == dblock) return SO_ERR_INVALID_ARG;
+        const Span at_dx(dx, rows, dx_stride, cols, size), at_dblock(dblock, rows, dblock_stride, cols, size);
+        if (overlap(at_dx, at_dblock)) return SO_ERR_INVALID_ARG;
+        for (const Span &in : {Span(dy, rows, dy_stride, cols, size), Span(dh, dh ? rows : 0, dh_stride, cols, size),
+                               Span(h, rows, h_stride, cols, size), Span(block, rows, block_stride, cols, size)})
+            if (overlap(at_dx, in) || overlap(at_dblock, in)) return SO_ERR_INVALID_ARG;
     }
     Args a = {};
     a.dy = dy, a.dh = dh, a.hin = h, a.block = block, a.dx = dx, a.dblock = dblock;
