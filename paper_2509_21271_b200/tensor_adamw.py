@@ -18,6 +18,8 @@ import torch
 from . import binding as B
 from .operators import _DTYPES, _current_device, _increment_version, _raw_stream, _refuse
 
+_data_ptr = torch.Tensor.data_ptr
+
 
 class TensorAdamW:
     """The moments and the progress of AdamW over `params`.
@@ -26,8 +28,10 @@ class TensorAdamW:
     fp16 or fp32), `copies` (None: none) bf16 or fp16; each list has the same sizes, on
     the current device.  Parameters and copies are apart from each other and from the
     gradients.  The optimizer keeps them; gradients are read where they are
-    when :meth:`step` runs.  Parameters may require grad: a step counts as a
-    modification in place.
+    when :meth:`step` runs.  A tensor that has been given other storage
+    (``p.data = other``) is taken up with it by the next step, and refused there where it no
+    longer fits; a captured step goes on with the storage of its capture, which the caller
+    keeps.  Parameters may require grad: a step counts as a modification in place.
 
     `m` and `v` are arenas of blocks of 256 elements, every tensor from a block of its
     own on (:meth:`block_of`): fp32, or codes with a byte of scale per block in
@@ -52,32 +56,16 @@ class TensorAdamW:
         if self.device.index != _current_device():
             _refuse(where, "the parameters are not on the current device")
         self._list = (B.so_tensor * n)()
-        seen = set()
-        for e, p in zip(self._list, self.params):
-            if p.dtype != torch.float32:
-                _refuse(where, "parameters are float32")
-            self._check(where, "parameter", p, p.numel())
-            if p.numel() and p.data_ptr() in seen:
-                _refuse(where, "a parameter is in the list twice")
-            seen.add(p.data_ptr())
-            e.param, e.numel = p.data_ptr(), p.numel()
+        self._numels = [p.numel() for p in self.params]
+        for e, numel in zip(self._list, self._numels):
+            e.numel = numel
         self._copy_dtype = B.SO_TENSOR_NO_COPY
         if self.copies is not None:
             dtypes = {c.dtype for c in self.copies}
             if len(self.copies) != n or len(dtypes) != 1 or not dtypes <= {torch.bfloat16, torch.float16}:
                 _refuse(where, "there must be a copy for each parameter, all bfloat16 or all float16")
             self._copy_dtype = _DTYPES[self.copies[0].dtype]
-            for e, c in zip(self._list, self.copies):
-                self._check(where, "copy", c, e.numel)
-                e.copy = c.data_ptr()
-        # what is written is written by one warp alone
-        end = 0
-        for at, size in sorted((t.data_ptr(), t.numel() * t.element_size()) for t in [*self.params, *(self.copies or ())]):
-            if size == 0:
-                continue
-            if at < end:
-                _refuse(where, "parameters and copies overlap")
-            end = at + size
+        self._take_written(where)
         self.set_grads(grads)
         info = B.so_tensor_adamw_layout(self._list, n, state_bits)
         self.blocks = info.blocks
@@ -104,6 +92,37 @@ class TensorAdamW:
         if t.numel() != numel or not t.is_contiguous():
             _refuse(where, f"a {what} is not contiguous with its parameter's size")
 
+    def _take_written(self, where):
+        """Checks the parameters and copies, and takes their addresses."""
+        seen = set()
+        for p, numel in zip(self.params, self._numels):
+            if p.dtype != torch.float32:
+                _refuse(where, "parameters are float32")
+            self._check(where, "parameter", p, numel)
+            if numel and p.data_ptr() in seen:
+                _refuse(where, "a parameter is in the list twice")
+            seen.add(p.data_ptr())
+        for c, numel in zip(self.copies or (), self._numels):
+            if _DTYPES.get(c.dtype) != self._copy_dtype:
+                _refuse(where, "there must be a copy for each parameter, all bfloat16 or all float16")
+            self._check(where, "copy", c, numel)
+        # what is written is written by one warp alone
+        end = 0
+        for at, size in sorted((t.data_ptr(), t.numel() * t.element_size()) for t in [*self.params, *(self.copies or ())]):
+            if size == 0:
+                continue
+            if at < end:
+                _refuse(where, "parameters and copies overlap")
+            end = at + size
+        for e, p in zip(self._list, self.params):
+            e.param = p.data_ptr()
+        for e, c in zip(self._list, self.copies or ()):
+            e.copy = c.data_ptr()
+        both = [*self.params, *(self.copies or ())]
+        self._at_written = both, list(map(_data_ptr, both))
+        # an address in use stays its tensor's, also when the tensor has gone elsewhere
+        self._held_written = [t.untyped_storage() for t in both]
+
     def set_grads(self, grads: Sequence[torch.Tensor]) -> None:
         """Other gradient tensors from the next step on."""
         grads = list(grads)
@@ -115,6 +134,8 @@ class TensorAdamW:
         for e, g in zip(self._list, grads):
             e.grad = g.data_ptr()
         self.grads, self._grad_dtype = grads, _DTYPES[grads[0].dtype]
+        self._at_grads = grads, list(map(_data_ptr, grads))
+        self._held_grads = [g.untyped_storage() for g in grads]
 
     def step(self, hp, *, clip: bool = True, grad_scale: float = 1.0, seed: Optional[int] = None, stream=None):
         """One step with the hyper-parameters of `hp` (lr, beta1, beta2, eps,
@@ -131,6 +152,12 @@ class TensorAdamW:
             _refuse(where, "the parameters are not on the current device")
         if seed is not None and self.state_bits != 8:
             _refuse(where, "a seed is for 8-bit moments")
+        tensors, addresses = self._at_written
+        if list(map(_data_ptr, tensors)) != addresses:
+            self._take_written(where)
+        tensors, addresses = self._at_grads
+        if list(map(_data_ptr, tensors)) != addresses:
+            self.set_grads(tensors)
         h = self._hp
         h.lr, h.beta1, h.beta2, h.eps = hp.lr, hp.beta1, hp.beta2, hp.eps
         h.weight_decay, h.max_grad_norm = hp.weight_decay, hp.max_grad_norm
