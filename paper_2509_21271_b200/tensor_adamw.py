@@ -11,6 +11,7 @@ kernels, and nothing here waits for the device but ``step_count``.
 from __future__ import annotations
 
 import ctypes as C
+from bisect import bisect_left
 from typing import Optional, Sequence
 
 import torch
@@ -27,7 +28,7 @@ class TensorAdamW:
     `params` are contiguous fp32 tensors, `grads` contiguous and of one dtype (bf16,
     fp16 or fp32), `copies` (None: none) bf16 or fp16; each list has the same sizes, on
     the current device.  Parameters and copies are apart from each other and from the
-    gradients.  The optimizer keeps them; gradients are read where they are
+    gradients, which may share memory with each other.  The optimizer keeps them; gradients are read where they are
     when :meth:`step` runs.  A tensor that has been given other storage
     (``p.data = other``) is taken up with it by the next step, and refused there where it no
     longer fits; a captured step goes on with the storage of its capture, which the caller
@@ -65,6 +66,7 @@ class TensorAdamW:
             if len(self.copies) != n or len(dtypes) != 1 or not dtypes <= {torch.bfloat16, torch.float16}:
                 _refuse(where, "there must be a copy for each parameter, all bfloat16 or all float16")
             self._copy_dtype = _DTYPES[self.copies[0].dtype]
+        self.grads = None
         self._take_written(where)
         self.set_grads(grads)
         info = B.so_tensor_adamw_layout(self._list, n, state_bits)
@@ -108,29 +110,44 @@ class TensorAdamW:
             self._check(where, "copy", c, numel)
         # what is written is written by one warp alone
         end = 0
-        for at, size in sorted((t.data_ptr(), t.numel() * t.element_size()) for t in [*self.params, *(self.copies or ())]):
-            if size == 0:
-                continue
+        both = [*self.params, *(self.copies or ())]
+        spans = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in both if t.numel())
+        for at, size in spans:
             if at < end:
                 _refuse(where, "parameters and copies overlap")
             end = at + size
+        self._spans = [at for at, _ in spans], [at + size for at, size in spans]
         for e, p in zip(self._list, self.params):
             e.param = p.data_ptr()
         for e, c in zip(self._list, self.copies or ()):
             e.copy = c.data_ptr()
-        both = [*self.params, *(self.copies or ())]
         self._at_written = both, list(map(_data_ptr, both))
         # an address in use stays its tensor's, also when the tensor has gone elsewhere
         self._held_written = [t.untyped_storage() for t in both]
+        self._at_grads = self.grads, None                     # to be compared with these
+
+    def _look(self, where):
+        """Parameters and copies that have been given other storage are taken anew."""
+        tensors, addresses = self._at_written
+        if list(map(_data_ptr, tensors)) != addresses:
+            self._take_written(where)
 
     def set_grads(self, grads: Sequence[torch.Tensor]) -> None:
         """Other gradient tensors from the next step on."""
+        self._look("TensorAdamW")
         grads = list(grads)
         dtypes = {g.dtype for g in grads}
         if len(grads) != len(self.params) or len(dtypes) != 1 or not dtypes <= set(_DTYPES):
             _refuse("TensorAdamW", "there must be a gradient for each parameter, all bfloat16, float16 or float32")
         for e, g in zip(self._list, grads):
             self._check("TensorAdamW", "gradient", g, e.numel)
+        # gradients are read as what no one writes
+        starts, ends = self._spans
+        for g in grads:
+            if g.numel():
+                at = bisect_left(starts, g.data_ptr() + g.numel() * g.element_size())   # (those before begin below its end)
+                if at > 0 and ends[at - 1] > g.data_ptr():
+                    _refuse("TensorAdamW", "a gradient overlaps a parameter or a copy")
         for e, g in zip(self._list, grads):
             e.grad = g.data_ptr()
         self.grads, self._grad_dtype = grads, _DTYPES[grads[0].dtype]
@@ -152,9 +169,7 @@ class TensorAdamW:
             _refuse(where, "the parameters are not on the current device")
         if seed is not None and self.state_bits != 8:
             _refuse(where, "a seed is for 8-bit moments")
-        tensors, addresses = self._at_written
-        if list(map(_data_ptr, tensors)) != addresses:
-            self._take_written(where)
+        self._look(where)
         tensors, addresses = self._at_grads
         if list(map(_data_ptr, tensors)) != addresses:
             self.set_grads(tensors)

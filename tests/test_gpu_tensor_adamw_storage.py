@@ -1,4 +1,5 @@
-"""AdamW over a list of tensors whose storage is exchanged underneath (``t.data = other``)."""
+"""AdamW over a list of tensors whose storage is exchanged underneath (``t.data = other``),
+and gradients that lie in what a step writes."""
 from __future__ import annotations
 
 import pytest
@@ -74,3 +75,39 @@ def test_storage_that_does_not_fit_is_refused():
     opt.params[0].data = opt.params[2].detach()[100:1100]
     with pytest.raises(B.SuperOffloadError, match="overlap"):
         opt.step(hp)
+
+
+def test_gradients_apart_from_what_is_written():
+    arena, low = torch.zeros(2000, device="cuda"), torch.zeros(2000, dtype=BF16, device="cuda")
+    p, c = [arena[:300], arena[700:1200]], [low[:300], low[700:1200]]
+    apart = [low[300:600], low[1200:1700]]
+    for grads in ([arena[:300], arena[1200:1700]],                    # a parameter itself
+                  [arena[400:700], arena[299:799]],                   # across a parameter's end and another's start
+                  [arena[300:600], arena[1199:1699]]):
+        with pytest.raises(B.SuperOffloadError, match="overlap"):
+            TensorAdamW(p, grads)
+    for grads in ([low[299:599], apart[1]], [apart[0], low[300:800]], [low[100:400], apart[1]]):
+        with pytest.raises(B.SuperOffloadError, match="overlap"):
+            TensorAdamW(p, grads, copies=c)
+        opt = TensorAdamW(p, apart, copies=c)
+        with pytest.raises(B.SuperOffloadError, match="overlap"):
+            opt.set_grads(grads)
+        assert opt.grads[0] is apart[0]
+        opt.step(HP())
+    # neighbours, an empty tensor anywhere, and gradients in each other are fine
+    opt = TensorAdamW([*p, arena[:0]], [arena[300:600], arena[200:700][:0].new_zeros(500), arena[:0]])
+    opt.set_grads([arena[1200:1500], arena[1300:1800], arena[100:100]])
+    opt.step(HP())
+
+
+def test_a_parameter_that_moves_into_a_gradient():
+    """The step that would take it up is refused, and so is the next one."""
+    opt = make()
+    opt.set_grads([g.float() for g in opt.grads])
+    opt.params[0].data = opt.grads[0]
+    for _ in range(2):
+        with pytest.raises(B.SuperOffloadError, match="overlap"):
+            opt.step(HP())
+    assert opt.step_count == 0
+    opt.set_grads([torch.zeros_like(opt.grads[0]), *opt.grads[1:]])
+    opt.step(HP())
