@@ -1172,7 +1172,7 @@ Layout layout(int64_t rows, int64_t vocab, int64_t cols, int32_t dtype, int32_t 
     // parts of the sums over the vocabulary: as many as fill the units best, each split costing
     // its write and reading
     const int64_t tile_m = rows > kRowsOfCta ? 2 * kRowsOfCta : kRowsOfCta;
-    const int64_t tiles = (l.rows_pad < tile_m ? 1 : up(rows > 0 ? rows : 1, tile_m) / tile_m) * (l.part_stride / kTileN);
+    const int64_t tiles = up(rows > 0 ? rows : 1, tile_m) / tile_m * (l.part_stride / kTileN);
     l.splits = 1;
     double best = 1e30;
     for (int64_t s = 1; s <= 64 && s * 4 <= l.piece / kTileK; ++s) {
