@@ -672,8 +672,8 @@ so_status so_policy_loss(const void *logits, int64_t logits_stride, const void *
  *           free for other use once the call has run on its stream.  `packed`: 1 unless
  *           table is 16-byte aligned and its stride a multiple of 8; such a table is copied,
  *           piece by piece.  `gradients`: 1 if either is wanted
- * Products are summed in fp32.  P is rounded to `dtype`, relative to a power of two near the
- * largest |weight| (fp16 holds what is above 2^-39 of that); where dtable is fp32 it is summed
+ * Products are summed in fp32.  P is rounded to `dtype` as a multiple of the largest
+ * |weight| (fp16 holds what is above 2^-39 of that); where dtable is fp32 it is summed
  * from parts that hold P to 24 bits.  A row with a logit of NaN or +inf, or of -inf throughout,
  * has a NaN loss, and NaN in its row of dhidden and in all of dtable.
  */

@@ -19,8 +19,10 @@
 // both are as good relative to 1 - q as other rows' are to 1.  (One number for log sum exp z would do
 // for q, but its rounding, 1e-6 for logits near 20, is all of q - 1 there.)
 //
-// P is w (q - [label]) as a multiple of a power of two near the largest |w| (for fp16 of
-// 2^-15 of it: its normal numbers then reach down to 2^-29 of a row's largest).  Its
+// P is w (q - [label]) as a multiple of the largest |w| (for fp16 of 2^-15 of it: its normal
+// numbers then reach down to 2^-29 of a row's largest).  A mean's weights are all the same: as
+// multiples of a power of two, P at the labels would be rounded the same way in every row, which made
+// dW of 255 rows 0.4 % too long; so it is close to -1.  Its
 // rounding to 16 bits is one rounding of every term of sums that are themselves
 // rounded to 16 bits; where dW is fp32, it sums P in several parts of 16 bits that
 // together hold all 24.
@@ -49,7 +51,7 @@ enum Mode { kStats, kProb, kHidden, kTable, kGradients };
 // What the device finds out about a call, in scratch.
 struct Control {
     int32_t live;                         // rows that take part
-    float unit;                           // P is a multiple of this: a power of two
+    float unit;                           // P is held as a multiple of this
     uint32_t ticket;                      // blocks of the statistics' join that are done
     int32_t gave_up;                      // a wait ran out: every result becomes NaN
 };
@@ -889,12 +891,9 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
     if (blockIdx.x != gridDim.x - 1) return;
     const int live = base;
     if (threadIdx.x == 0) {
-        int e = 0;
-        if (top > 0.0f && top < kInf) frexpf(top, &e);       // top < 2^e
-        if (r.fp16) e -= 15;
-        e = e < -126 ? -126 : e > 126 ? 126 : e;
+        const float unit = (top > 0.0f && top < kInf ? top : 1.0f) * (r.fp16 ? 0x1p-15f : 1.0f);
         r.control->live = live;
-        r.control->unit = ldexpf(1.0f, e);
+        r.control->unit = fminf(fmaxf(unit, 0x1p-126f), 0x1p126f);
         r.control->ticket = 0;
         r.control->gave_up = 0;
     }
