@@ -654,7 +654,8 @@ so_status so_policy_loss(const void *logits, int64_t logits_stride, const void *
 /*
  * so_linear_cross_entropy -- cross entropy of labels, from the hidden states and the
  * table of the head, with both gradients, in pieces of the vocabulary: the logits
- * z = hidden table^T are never kept.
+ * z = hidden table^T never leave the scratch, which holds them whole only where that is
+ * quicker than computing them twice and takes no more than 256 MB in fp32.
  *   row_loss = log sum_j exp z_j - z_label,  loss = sum_rows weight * row_loss
  *   P        = weight (softmax(z) - [label])
  *   dhidden  = grad_scale P table,  dtable = grad_scale P^T hidden
@@ -674,8 +675,11 @@ so_status so_policy_loss(const void *logits, int64_t logits_stride, const void *
  *           piece by piece.  `gradients`: 1 if either is wanted
  * Products are summed in fp32.  P is rounded to `dtype` as a multiple of the largest
  * |weight| (fp16 holds what is above 2^-39 of that); where dtable is fp32 it is summed
- * from parts that hold P to 24 bits.  A row with a logit of NaN or +inf, or of -inf throughout,
- * has a NaN loss, and NaN in its row of dhidden and in all of dtable.
+ * from parts that hold P to 24 bits (bf16) or 22 (fp16).  The tensor cores round a logit's sum
+ * after every 16 products: what is fp32, the losses and through P such a dtable, is good to
+ * some 2e-6 at 4096 columns.  A label's loss and P are good relative to 1 - its probability.
+ * A row with a logit of NaN or +inf, or of -inf throughout, has a NaN loss, and NaN in its
+ * row of dhidden and in all of dtable.
  */
 #define SO_LINEAR_MAX_ROWS (INT64_C(1) << 22)
 #define SO_LINEAR_MAX_VOCAB (INT64_C(1) << 26)
@@ -750,9 +754,11 @@ so_status so_residual_norm_backward(const void *dy, int64_t dy_stride, const voi
  *   p' = p - (lr wd p + lr / (1 - beta1^t) m' / (sqrt(v') / sqrt(1 - beta2^t) + eps))
  *
  * in fp32, operation by operation; parameters are fp32 and may have a copy in bf16 or
- * fp16, written in the same pass.  With `clip` the gradients are read once more, before:
- * norm is that of all gradients times grad_scale, in fp64; where it is not finite (a
- * square beyond fp32 counts) nothing is written and t stays.  max_grad_norm <= 0 then
+ * fp16, written in the same pass; the square root and the quotient are the hardware's, good
+ * to 2^-21, and a v' below 2^-126 counts as 0 there.  With `clip` the gradients are read once
+ * more, before: norm is that of all gradients times grad_scale, of their squares in fp32
+ * summed in fp64, so that a gradient below 2^-75 (2.6e-23) counts as nothing; where it is
+ * not finite (a square beyond fp32 counts) nothing is written and t stays.  max_grad_norm <= 0 then
  * looks without clipping.  Without `clip` c = 1 and every gradient is taken as it is.
  *
  * The moments belong to the caller: arenas of `blocks` blocks of 256 elements, in which
@@ -769,8 +775,8 @@ so_status so_residual_norm_backward(const void *dy, int64_t dy_stride, const voi
  *   int64 t; float norm, c, skipped (0 or 1)
  * `scratch` (so_tensor_adamw_layout's bytes, 16-byte aligned) is needed with `clip` and free
  * for other use once the call has run on its stream.  Calls on one record are made one after
- * the other.  What is written is apart from everything else.  Tensors of no elements are passed over; the sums' order depends on the sizes
- * alone, and results repeat bit for bit.
+ * the other.  What is written is apart from everything else.  Tensors of no elements are
+ * passed over; the sums' order depends on the sizes alone, and results repeat bit for bit.
  * Errors: SO_ERR_INVALID_ARG, SO_ERR_CUDA.
  */
 #define SO_TENSOR_BLOCK 256

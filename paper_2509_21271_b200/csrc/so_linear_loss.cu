@@ -1,5 +1,5 @@
 // Cross entropy of labels from the hidden states and the table of the head, with both
-// gradients, in pieces of the vocabulary: the logits are never kept.
+// gradients, in pieces of the vocabulary: the logits of a large batch are never all there.
 //
 //   z = H W^T,  row_loss = log sum_j exp z_j - z_label,  loss = sum w row_loss
 //   P = w (softmax(z) - [label]),  dH = s P W,  dW = s P^T H
@@ -8,7 +8,8 @@
 // others are gathered into a matrix of their own, which also gives every row an aligned
 // start and whole tiles.  Then
 //   statistics     a pass over all logits, tile by tile: each row's maximum and sum
-//   for each piece the piece's logits once more, as P in 16 bits; dH += P W; dW = P^T H
+//   for each piece the piece's logits once more (a small batch has kept them), as P in 16 bits;
+//                  dH += P W; dW = P^T H
 // are all one kernel, a persistent matrix product on the tensor cores (tcgen05: operands
 // through TMA into swizzled shared memory, two accumulators of 256 columns in tensor
 // memory, so that one is read while the next is computed) with four ways to end a tile.
@@ -24,8 +25,8 @@
 // multiples of a power of two, P at the labels would be rounded the same way in every row, which made
 // dW of 255 rows 0.4 % too long; so it is close to -1.  Its
 // rounding to 16 bits is one rounding of every term of sums that are themselves
-// rounded to 16 bits; where dW is fp32, it sums P in several parts of 16 bits that
-// together hold all 24.
+// rounded to 16 bits; where dW is fp32, it sums P in parts of 16 bits that together hold 24
+// bits (bf16, three parts) or 22 (fp16, two).
 #include <cuda.h>
 
 #include "so_ops.cuh"
@@ -575,13 +576,13 @@ __device__ __forceinline__ void end_table_by_rows(const Product &p, uint32_t box
 // B a stage, one issues the instructions, eight end the tile before while the next is computed.
 //
 // Bound: the tensor cores and the power limit.  8192 x 128256 x 4096 bf16 with 5734 rows that take part
-// does 2.4e13 operations in 17.0 to 18.4 ms, 1.31 to 1.42 PFLOP/s; a library's product sustains 1.41.  The
-// statistics alone of 4095 x 128256 x 2048: 1.29 to 1.53 ms, 1.41 to 1.66 PFLOP/s (a library's burst: 1.68).
+// does 2.4e13 operations in 17.0 (a short run) to 18.9 ms, 1.28 to 1.42 PFLOP/s; a library's product sustains
+// 1.41.  The statistics alone of 4095 x 128256 x 2048: 1.29 to 1.56 ms, 1.38 to 1.66 PFLOP/s (a library's burst: 1.68).
 // On the way: one lane alone in the loops of the first two warps 22.1 ms, six or seven stages the same
 // within 0.1 %, P in pieces of 128 MB instead of 256 MB 5 % more, both gradients in two launches 2 % more.
 // Small batches are bound by the chain of six launches and the table's reading: 63 x 50257 x 768 85 to 93
 // us for 24 us of bytes.  The sums of a logit's 16-column products are rounded to fp32 one after the
-// other, d / 16 of them: losses come out good to 4e-7 (d = 512) to 1.3e-6 (d = 4096).
+// other, d / 16 of them: losses come out good to 4e-7 (d = 512) to 1.6e-6 (d = 4096).
 //
 // a, b, out: of kStats and kProb, and of the tiles of dH; a2, b2, out2: of those of dW.
 struct Maps {
@@ -1142,12 +1143,13 @@ struct Layout {
 
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of P, unless rows are so many that pieces would get short
 constexpr int64_t kShortPiece = 4096;
-// Up to so many bytes of fp32 logits are kept from the statistics to P, where multiplying again would
-// cost more than writing and reading them: kept / again 596 / 655 us for 1025 x 50257 x 1600 (fp16,
+// Logits are kept from the statistics to P where multiplying again would cost more than writing and
+// reading them, 8 bytes each, which goes by the row's length; the bytes are a limit of what scratch
+// should take, all logits of 1025 x 50257 with some left.  Kept / again 596 / 655 us for 1025 x 50257 x 1600 (fp16,
 // fp32 gradient), 281 / 343 us for 300 x 50257 x 2048, 88 / 101 us for 63 x 50257 x 768, but
 // 146 / 137 us for 500 x 50257 x 512 and 198 / 171 us for 1000 x 50257 x 256.
 constexpr int64_t kKeptBytes = int64_t(256) << 20;
-constexpr int64_t kKeptCols = 768;        // for shorter rows a quarter of that, which L2 may hold
+constexpr int64_t kKeptCols = 768;        // with shorter rows only a quarter of that, which L2 may hold, is worth it
 
 constexpr int kSms = 148;                 // of a B200: sums are split alike on every device
 

@@ -548,8 +548,8 @@ struct Ring {
     }
 };
 
-// Bound: memory (two reads, two writes).  32768 x 4096 bf16: 173 us, 6.2 TB/s, 95 % of a copy's rate (188 to 207 us
-// in long runs); 8192 x 8192 94 us for 82 of bytes; 65536 x 768 92 us for 61 (a warp to a row,
+// Bound: memory (two reads, two writes).  32768 x 4096 bf16: 173 us in a short run, 6.2 TB/s, 95 % of a copy's rate
+// (186 to 207 us in long ones); 8192 x 8192 94 us for 82 of bytes; 65536 x 768 92 us for 61 (a warp to a row,
 // 24 elements a lane; with three warps to a row 139 us).  One row of 4096: 5 us on the device.  Rows read once
 // for each pass from L2, without the ring: 32768 x 4096 290 us.
 template <typename T, Form kForm, int kNV, bool kFull, int kMaxThreads>
@@ -662,8 +662,8 @@ __global__ void __launch_bounds__(kMaxThreads, kMaxThreads <= 256 && kNV * Vec<T
 //
 // Bound: what a row costs the few warps that the registers leave room for, then memory (four reads, two writes).
 // 16384 x 4096 layer norm: 220 registers, eight warps an SM, 570 instructions a row and warp of 16 elements a lane
-// with its two exchanges, at 36 % of the issue slots and 54 % of DRAM's peak rate.  32768 x 2048 bf16 with 16 gates 184 us for 123 of bytes, 16384 x 4096 187 us with
-// layer norm and 166 us in the plain form, 32768 x 1024 fp32 145 us for 123, 65536 x 768 bf16 147 us for 92.
+// with its exchange, at 36 % of the issue slots and 54 % of DRAM's peak rate.  32768 x 2048 bf16 with 16 gates 184 us
+// for 123 of bytes, 16384 x 4096 187 us with layer norm and 166 us in the plain form, 32768 x 1024 fp32 145 us for 123, 65536 x 768 bf16 147 us for 92.
 // Two exchanges a row instead of one: 224 us for the first of these; two rows a turn: 257 us; 8 elements a thread
 // instead of 16: 206 us.  The loop, with rows and columns' sums in passes of their own: 579 us.
 template <typename T, Form kForm, bool kSums, int kNV, bool kFull, int kMaxThreads>

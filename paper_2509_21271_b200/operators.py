@@ -551,8 +551,8 @@ def policy_loss(logits, tokens, advantage, weight=None, *, old_logp=None, ref_lo
 
 def linear_cross_entropy(hidden, table, labels, weight=None, *, grad_scale: float = 1.0, dhidden=None, dtable=None,
                          accumulate: bool = False, loss=None, row_loss=None, scratch=None, stream=None):
-    """Cross entropy of `labels` under the logits hidden @ table.T, which are never kept;
-    returns (loss, row_loss, dhidden, dtable).
+    """Cross entropy of `labels` under the logits hidden @ table.T, which never leave
+    the scratch (whole only where 256 MB hold them); returns (loss, row_loss, dhidden, dtable).
 
     `hidden` [rows, cols] and `table` [vocab, cols] are bfloat16 or float16, `labels`
     [rows], `weight` fp32 [rows] (None: 1 each; 0 masks a row, as does a label outside
